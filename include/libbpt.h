@@ -317,6 +317,120 @@ typedef struct {
 bpt_status bpt_adamw_step(const bpt_adamw_config* cfg, int64_t n, float* p, const float* g, float* m, float* v,
                           void* p_lowp, void* stream);
 
+/* ------------------------------------------------------------------ long contexts
+ * What a GPT trained or run at long contexts takes beside the layer: positions that go past a
+ * learned table, attention whose work and cache grow with a window instead of the sequence, and
+ * an optimiser whose states take a quarter of the memory. Same conventions as above. */
+
+/* Rotary positions. Pair i < rot/2 of a head at position p turns by the angle p f_i, f_i =
+ * theta^(-2i/rot): (a, b) -> mscale (c a - s b, s a + c b), c and s its cosine and sine. A head's
+ * features from rot on are copied. Contexts longer than a model was trained for:
+ *   BPT_ROPE_LINEAR    f_i / factor
+ *   BPT_ROPE_BASE      theta replaced by theta factor^(rot/(rot - 2))
+ *   BPT_ROPE_BY_PARTS  f_i (g + (1 - g)/factor), g = clamp((turns - beta_slow)/(beta_fast -
+ *                      beta_slow), 0, 1), turns = orig_len f_i / (2 pi): pairs that turn often
+ *                      within the original length stay, those that hardly turn are stretched  */
+typedef enum { BPT_ROPE_NONE = 0, BPT_ROPE_LINEAR = 1, BPT_ROPE_BASE = 2, BPT_ROPE_BY_PARTS = 3 } bpt_rope_scaling;
+
+typedef struct {
+  int64_t rows;          /* tokens of X [rows, H, dh]                                          */
+  int64_t S;             /* without positions, row t stands at pos0 + t mod S                  */
+  int64_t H, dh;         /* heads that turn (those of Q and K of a projection in one call), head width: a multiple of 8 */
+  int64_t rot;           /* features of a head that turn: even, 2 <= rot <= min(dh, 128)       */
+  int64_t ldx, ldy;      /* elements between rows of X (and dX), of Y (and dY): >= H dh, multiples of 8 */
+  int64_t pos0;
+  int64_t orig_len;      /* BY_PARTS: the original context length                              */
+  double theta, factor;  /* > 0, >= 1                                                           */
+  double beta_fast, beta_slow, mscale;   /* BY_PARTS: e.g. 32 and 1; mscale: 1 without one      */
+  int32_t interleaved;   /* pairs (x_2i, x_2i+1) if 1, (x_i, x_i+rot/2) if 0                    */
+  int32_t scaling;       /* bpt_rope_scaling                                                    */
+  int32_t dtype;         /* bpt_dtype of X and Y                                                */
+  int32_t reserved;      /* 0                                                                   */
+} bpt_rope_config;
+
+bpt_status bpt_rope_validate(const bpt_rope_config* cfg);
+
+/* Y = the rotated X. positions: [rows] int32 (any values) or NULL. Y may be X (in place, if ldy
+ * == ldx); otherwise they must not overlap. Angles are reduced in 64 bits, cosine and sine formed in fp32, each
+ * result rounded once. */
+bpt_status bpt_rope_fwd(const bpt_rope_config* cfg, const int32_t* positions, const void* X, void* Y, void* stream);
+/* dX from dY: the rotation by the opposite angles, times mscale. dX may be dY (if ldx == ldy). */
+bpt_status bpt_rope_bwd(const bpt_rope_config* cfg, const int32_t* positions, const void* dY, void* dX, void* stream);
+
+/* Attention with a sliding window and sinks: softmax(scale Q K^T + mask) V per head, without a projection. Query
+ * i of a sequence of nq queries and nk keys stands at position p = nk - nq + i (its last query at its last
+ * key: a prompt, a piece of one or single tokens against a cache) and sees key k iff
+ *     k < nk, and (not causal or k <= p), and (window = 0 or |p - k| < window or k < sinks).
+ * Query head h reads key head h / (Hq / Hkv). A query that sees nothing (its sequence empty, or p < 0
+ * with the causal mask) gives O = 0, lse = -inf and no gradients. Keys that no query of the call sees are not
+ * read, whatever they hold.
+ * Tensors are [B, S, heads, dh] in any order of strides: element (b, t, h, d) at b sb + t st + h sh + d. */
+typedef struct {
+  int64_t sb, st, sh;    /* elements between sequences, tokens, heads; multiples of 16 bytes    */
+} bpt_attn_strides;
+
+typedef struct {
+  int64_t B, Sq, Skv;    /* sequences, queries and keys of each (or as many as there are lengths for at most) */
+  int64_t Hq, Hkv, dh;   /* query heads, a multiple of the key heads; dh 64 or 128              */
+  bpt_attn_strides q, k, v, o;   /* Q (and dQ), K (and dK), V (and dV), O (and dO)              */
+  int64_t window;        /* tokens a query sees, itself included; 0 = all                       */
+  int64_t sinks;         /* first tokens that stay visible; 0 without a window                  */
+  float scale;           /* of the scores, > 0; e.g. 1/sqrt(dh)                                  */
+  int32_t causal;        /* 0 or 1                                                              */
+  int32_t dtype;         /* bpt_dtype of every tensor but lse                                   */
+  int32_t reserved;      /* 0                                                                   */
+} bpt_attn_config;
+
+bpt_status bpt_attn_validate(const bpt_attn_config* cfg);
+
+/* Workspace of bpt_attn_fwd (backward = 0; 0 unless few queries meet many keys) or bpt_attn_bwd
+ * (backward = 1). 0 for an invalid configuration. Host-only. */
+size_t bpt_attn_workspace_bytes(const bpt_attn_config* cfg, int backward);
+
+/* Forward: O, and lse [B, Hq, Sq] (fp32, natural log), which the backward takes. q_lens, kv_lens: [B]
+ * int32, the queries and keys of each sequence that exist (its first ones; values are clamped to [0, Sq] and
+ * [0, Skv]), or NULL: all. Queries behind q_lens are treated as those that see nothing. */
+bpt_status bpt_attn_fwd(const bpt_attn_config* cfg, const void* Q, const void* K, const void* V, const int32_t* q_lens,
+                        const int32_t* kv_lens, void* O, float* lse, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Backward, given the forward's O and lse and the upstream gradient dO. dQ, dK, dV are OVERWRITTEN (zeros
+ * at queries and keys behind the lengths); dQ NULL, or dK and dV both NULL, skips them. The sums over a key head's query
+ * heads and over queries are taken in a fixed order. */
+bpt_status bpt_attn_bwd(const bpt_attn_config* cfg, const void* Q, const void* K, const void* V, const int32_t* q_lens,
+                        const int32_t* kv_lens, const void* O, const float* lse, const void* dO, void* dQ, void* dK,
+                        void* dV, void* workspace, size_t workspace_bytes, void* stream);
+
+/* One AdamW step on a list of tensors (bpt_adamw_step's formula on each, weight decay per tensor). Moments in 32
+ * bits: m and v, fp32. In 8 bits: m and r = sqrt(v), each as one e4m3 byte (sign, 4 exponent and
+ * 3 mantissa bits; 2^-9 .. 448) per element, and per block of 256 elements two bytes in `exps`: the moments of
+ * block j are the codes' values times 2^(exps[2j] - 134) and 2^(exps[2j + 1] - 134). All bytes 0: zero
+ * moments, the start of a training run. A code is rounded up with the probability of its value's place
+ * between two codes; the random bits are a function of element, place in the list, step and seed, so
+ * a step gives the same bytes every time it is repeated. A gradient that is not finite makes the moments
+ * of its block meaningless. */
+typedef struct {
+  int64_t n;             /* elements; 0: nothing to do                                          */
+  float* p;              /* [n] fp32                                                            */
+  const void* g;         /* [n] cfg->grad_dtype                                                 */
+  void *m, *v;           /* [n] fp32, or [n] bytes                                              */
+  uint8_t* exps;         /* state_bits 8: [2 ceil(n / 256)]; else not read                      */
+  void* p_lowp;          /* [n] cfg->lowp_dtype, gets p rounded; or NULL                        */
+  double weight_decay;
+} bpt_adamw_tensor;
+
+typedef struct {
+  double lr, beta1, beta2, eps;
+  int64_t step;          /* 1-based step count                                                  */
+  uint64_t seed;         /* state_bits 8: of the rounding                                       */
+  int32_t state_bits;    /* 32 or 8                                                             */
+  int32_t grad_dtype, lowp_dtype;
+  int32_t reserved;      /* 0                                                                   */
+} bpt_adamw_multi_config;
+
+/* tensors: a HOST array of `count`, read during the call. Different tensors' p must not overlap, nor may any
+ * other of their buffers (the p are checked). */
+bpt_status bpt_adamw_multi(const bpt_adamw_multi_config* cfg, const bpt_adamw_tensor* tensors, int64_t count, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

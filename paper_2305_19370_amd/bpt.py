@@ -23,6 +23,7 @@ STATUS = {0: "BPT_OK", 1: "BPT_ERR_INVALID_ARG", 2: "BPT_ERR_UNSUPPORTED", 3: "B
           4: "BPT_ERR_HIP"}
 
 c_i64, c_i32, c_f32, c_sz, c_vp = ctypes.c_int64, ctypes.c_int32, ctypes.c_float, ctypes.c_size_t, ctypes.c_void_p
+c_f64 = ctypes.c_double
 
 
 class Config(ctypes.Structure):
@@ -68,12 +69,40 @@ class AdamWConfig(ctypes.Structure):
                 ("lowp_dtype", c_i32), ("step", c_i64)]
 
 
+class RopeConfig(ctypes.Structure):
+    _fields_ = [("rows", c_i64), ("S", c_i64), ("H", c_i64), ("dh", c_i64), ("rot", c_i64), ("ldx", c_i64), ("ldy", c_i64),
+                ("pos0", c_i64), ("orig_len", c_i64), ("theta", c_f64), ("factor", c_f64), ("beta_fast", c_f64),
+                ("beta_slow", c_f64), ("mscale", c_f64), ("interleaved", c_i32), ("scaling", c_i32), ("dtype", c_i32),
+                ("reserved", c_i32)]
+
+
+class AttnStrides(ctypes.Structure):
+    _fields_ = [("sb", c_i64), ("st", c_i64), ("sh", c_i64)]
+
+
+class AttnConfig(ctypes.Structure):
+    _fields_ = [("B", c_i64), ("Sq", c_i64), ("Skv", c_i64), ("Hq", c_i64), ("Hkv", c_i64), ("dh", c_i64), ("q", AttnStrides),
+                ("k", AttnStrides), ("v", AttnStrides), ("o", AttnStrides), ("window", c_i64), ("sinks", c_i64), ("scale", c_f32),
+                ("causal", c_i32), ("dtype", c_i32), ("reserved", c_i32)]
+
+
+class AdamWTensor(ctypes.Structure):
+    _fields_ = [("n", c_i64), ("p", c_vp), ("g", c_vp), ("m", c_vp), ("v", c_vp), ("exps", c_vp), ("p_lowp", c_vp),
+                ("weight_decay", c_f64)]
+
+
+class AdamWMultiConfig(ctypes.Structure):
+    _fields_ = [("lr", c_f64), ("beta1", c_f64), ("beta2", c_f64), ("eps", c_f64), ("step", c_i64), ("seed", ctypes.c_uint64),
+                ("state_bits", c_i32), ("grad_dtype", c_i32), ("lowp_dtype", c_i32), ("reserved", c_i32)]
+
+
 EXPORTS = ("bpt_validate", "bpt_group_rows", "bpt_saved_bytes", "bpt_saved_layout_of", "bpt_workspace_bytes",
            "bpt_layer_fwd", "bpt_layer_bwd", "bpt_status_string", "bpt_last_error", "bpt_describe",
            "bpt_profile_enable", "bpt_profile_report", "bpt_xent_validate", "bpt_xent_workspace_bytes",
            "bpt_xent_fwd", "bpt_xent_bwd", "bpt_embed_fwd", "bpt_embed_bwd", "bpt_ln_workspace_bytes",
            "bpt_ln_fwd", "bpt_ln_bwd", "bpt_adamw_step", "bpt_bwd_qkv_grad_offset",
-           "bpt_layer_fwd_noalloc")
+           "bpt_layer_fwd_noalloc", "bpt_rope_validate", "bpt_rope_fwd", "bpt_rope_bwd", "bpt_attn_validate",
+           "bpt_attn_workspace_bytes", "bpt_attn_fwd", "bpt_attn_bwd", "bpt_adamw_multi")
 
 _lib = None
 
@@ -136,6 +165,21 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.bpt_ln_bwd.restype = c_i32
     lib.bpt_adamw_step.argtypes = [P(AdamWConfig), c_i64, c_vp, c_vp, c_vp, c_vp, c_vp, c_vp]
     lib.bpt_adamw_step.restype = c_i32
+    lib.bpt_rope_validate.argtypes = [P(RopeConfig)]
+    lib.bpt_rope_validate.restype = c_i32
+    for fn in (lib.bpt_rope_fwd, lib.bpt_rope_bwd):
+        fn.argtypes = [P(RopeConfig), c_vp, c_vp, c_vp, c_vp]
+        fn.restype = c_i32
+    lib.bpt_attn_validate.argtypes = [P(AttnConfig)]
+    lib.bpt_attn_validate.restype = c_i32
+    lib.bpt_attn_workspace_bytes.argtypes = [P(AttnConfig), c_i32]
+    lib.bpt_attn_workspace_bytes.restype = c_sz
+    lib.bpt_attn_fwd.argtypes = [P(AttnConfig)] + [c_vp] * 8 + [c_sz, c_vp]
+    lib.bpt_attn_fwd.restype = c_i32
+    lib.bpt_attn_bwd.argtypes = [P(AttnConfig)] + [c_vp] * 12 + [c_sz, c_vp]
+    lib.bpt_attn_bwd.restype = c_i32
+    lib.bpt_adamw_multi.argtypes = [P(AdamWMultiConfig), P(AdamWTensor), c_i64, c_vp]
+    lib.bpt_adamw_multi.restype = c_i32
     _lib = lib
     return lib
 
@@ -432,3 +476,146 @@ def adamw_step(p: torch.Tensor, g: torch.Tensor, m: torch.Tensor, v: torch.Tenso
     cfg = AdamWConfig(lr, beta1, beta2, eps, weight_decay, lowp, step)
     _check(load().bpt_adamw_step(ctypes.byref(cfg), p.numel(), p.data_ptr(), g.data_ptr(), m.data_ptr(),
                                  v.data_ptr(), _ptr(p_lowp), _stream()))
+
+
+# ---------------------------------------------------------------- rotary positions
+ROPE_SCALING = {"none": 0, "linear": 1, "base": 2, "by_parts": 3}
+
+
+def make_rope_config(rows: int, S: int, H: int, dh: int, rot: Optional[int] = None, ldx: Optional[int] = None,
+                     ldy: Optional[int] = None, layout: str = "half", theta: float = 10000.0, scaling: str = "none",
+                     factor: float = 1.0, orig_len: int = 0, beta_fast: float = 32.0, beta_slow: float = 1.0,
+                     mscale: float = 1.0, pos0: int = 0, dtype: str = "bf16") -> RopeConfig:
+    """Rotary positions of H heads of width dh on `rows` tokens; see include/libbpt.h."""
+    w = H * dh
+    return RopeConfig(rows, S, H, dh, dh if rot is None else rot, w if ldx is None else ldx, w if ldy is None else ldy, pos0,
+                      orig_len, theta, factor, beta_fast, beta_slow, mscale, {"half": 0, "interleaved": 1}[layout],
+                      ROPE_SCALING[scaling], _DT[dtype], 0)
+
+
+def rope_validate(cfg: RopeConfig) -> int:
+    return load().bpt_rope_validate(ctypes.byref(cfg))
+
+
+def rope_fwd(cfg: RopeConfig, X: torch.Tensor, Y: torch.Tensor, positions: Optional[torch.Tensor] = None) -> None:
+    _check(load().bpt_rope_fwd(ctypes.byref(cfg), _ptr(positions), X.data_ptr(), Y.data_ptr(), _stream()))
+
+
+def rope_bwd(cfg: RopeConfig, dY: torch.Tensor, dX: torch.Tensor, positions: Optional[torch.Tensor] = None) -> None:
+    _check(load().bpt_rope_bwd(ctypes.byref(cfg), _ptr(positions), dY.data_ptr(), dX.data_ptr(), _stream()))
+
+
+# ---------------------------------------------------------------- attention with a window and sinks
+def _strides(t: torch.Tensor) -> AttnStrides:
+    if t.dim() != 4 or (t.shape[3] > 1 and t.stride(3) != 1):
+        raise ValueError("attention tensors are [B, S, heads, dh] with adjacent features")
+    return AttnStrides(t.stride(0), t.stride(1), t.stride(2))
+
+
+def attn_config_of(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, o: torch.Tensor, causal: bool = True, window: int = 0,
+                   sinks: int = 0, scale: Optional[float] = None) -> AttnConfig:
+    """The configuration of attention on tensors of these shapes and strides: q, o [B, Sq, Hq, dh],
+    k, v [B, Skv, Hkv, dh] (dq, dk, dv laid out like q, k, v; do like o)."""
+    B, Sq, Hq, dh = q.shape
+    if k.shape != v.shape or k.shape[0] != B or k.shape[3] != dh or o.shape != q.shape:
+        raise ValueError(f"shapes do not fit: q {tuple(q.shape)}, k {tuple(k.shape)}, v {tuple(v.shape)}, o {tuple(o.shape)}")
+    if not q.dtype == k.dtype == v.dtype == o.dtype or q.dtype not in (torch.float32, torch.bfloat16):
+        raise ValueError("q, k, v and o must share a type, float32 or bfloat16")
+    return AttnConfig(B, Sq, k.shape[1], Hq, k.shape[2], dh, _strides(q), _strides(k), _strides(v), _strides(o), window, sinks,
+                      dh ** -0.5 if scale is None else scale, int(bool(causal)), BPT_BF16 if q.dtype == torch.bfloat16 else BPT_F32,
+                      0)
+
+
+def attn_validate(cfg: AttnConfig) -> int:
+    return load().bpt_attn_validate(ctypes.byref(cfg))
+
+
+def attn_workspace_bytes(cfg: AttnConfig, backward: bool) -> int:
+    return load().bpt_attn_workspace_bytes(ctypes.byref(cfg), int(backward))
+
+
+def attn_fwd(cfg: AttnConfig, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, o: torch.Tensor, lse: torch.Tensor,
+             workspace: Optional[torch.Tensor] = None, q_lens: Optional[torch.Tensor] = None,
+             kv_lens: Optional[torch.Tensor] = None) -> None:
+    nb = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    _check(load().bpt_attn_fwd(ctypes.byref(cfg), q.data_ptr(), k.data_ptr(), v.data_ptr(), _ptr(q_lens), _ptr(kv_lens),
+                               o.data_ptr(), lse.data_ptr(), _ptr(workspace) if nb else None, nb, _stream()))
+
+
+def attn_bwd(cfg: AttnConfig, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, o: torch.Tensor, lse: torch.Tensor,
+             do: torch.Tensor, dq: Optional[torch.Tensor], dk: Optional[torch.Tensor], dv: Optional[torch.Tensor],
+             workspace: torch.Tensor, q_lens: Optional[torch.Tensor] = None, kv_lens: Optional[torch.Tensor] = None) -> None:
+    _check(load().bpt_attn_bwd(ctypes.byref(cfg), q.data_ptr(), k.data_ptr(), v.data_ptr(), _ptr(q_lens), _ptr(kv_lens),
+                               o.data_ptr(), lse.data_ptr(), do.data_ptr(), _ptr(dq), _ptr(dk), _ptr(dv), workspace.data_ptr(),
+                               workspace.numel() * workspace.element_size(), _stream()))
+
+
+class WindowAttention:
+    """Attention with a window and sinks through libbpt; allocates its buffers with torch."""
+
+    def __init__(self, causal: bool = True, window: int = 0, sinks: int = 0, scale: Optional[float] = None):
+        self.kw = dict(causal=causal, window=window, sinks=sinks, scale=scale)
+
+    @staticmethod
+    def _bytes(n: int, device) -> torch.Tensor:
+        return torch.empty(max(n, 256), dtype=torch.uint8, device=device)
+
+    def forward(self, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, q_lens: Optional[torch.Tensor] = None,
+                kv_lens: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:
+        """O [B, Sq, Hq, dh] and the log-sum-exp [B, Hq, Sq]."""
+        o = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        lse = torch.empty((q.shape[0], q.shape[2], q.shape[1]), dtype=torch.float32, device=q.device)
+        cfg = attn_config_of(q, k, v, o, **self.kw)
+        attn_fwd(cfg, q, k, v, o, lse, self._bytes(attn_workspace_bytes(cfg, False), q.device), q_lens, kv_lens)
+        return o, lse
+
+    def backward(self, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, o: torch.Tensor, lse: torch.Tensor, do: torch.Tensor,
+                 q_lens: Optional[torch.Tensor] = None,
+                 kv_lens: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor, torch.Tensor]:
+        """dQ, dK, dV; q, k, v as they were, o, lse from forward."""
+        q, k, v, do = (t.contiguous() for t in (q, k, v, do))
+        dq, dk, dv = torch.empty_like(q), torch.empty_like(k), torch.empty_like(v)
+        cfg = attn_config_of(q, k, v, o, **self.kw)
+        attn_bwd(cfg, q, k, v, o, lse, do, dq, dk, dv, self._bytes(attn_workspace_bytes(cfg, True), q.device), q_lens, kv_lens)
+        return dq, dk, dv
+
+
+# ---------------------------------------------------------------- AdamW over many tensors
+class AdamWTensors:
+    """A list of tensors that adamw_multi updates together: dicts of p, g, m and v (32-bit moments, fp32) or
+    r and exps (8-bit moments: e4m3 bytes and two exponent bytes per block of 256 elements, all zero at the
+    start), p_lowp (None: no copy) and weight_decay. Keeps the tensors alive."""
+
+    def __init__(self, tensors, bits: int = 32):
+        if bits not in (8, 32):
+            raise ValueError("bits must be 8 or 32")
+        self.tensors, self.bits = list(tensors), bits
+        second = "r" if bits == 8 else "v"
+        state = torch.uint8 if bits == 8 else torch.float32
+        gts = {t["g"].dtype for t in self.tensors}
+        lows = {t["p_lowp"].dtype for t in self.tensors if t.get("p_lowp") is not None}
+        if len(gts) > 1 or len(lows) > 1 or not (gts | lows) <= {torch.float32, torch.bfloat16}:
+            raise ValueError("gradients share one type, low-precision copies too: float32 or bfloat16")
+        for t in self.tensors:
+            n = t["p"].numel()
+            need = {"p": (torch.float32, n), "g": (t["g"].dtype, n), "m": (state, n), second: (state, n)}
+            if bits == 8:
+                need["exps"] = (torch.uint8, 2 * ((n + 255) // 256))
+            if t.get("p_lowp") is not None:
+                need["p_lowp"] = (t["p_lowp"].dtype, n)
+            for name, (dt, size) in need.items():
+                if t[name].dtype != dt or t[name].numel() != size or not t[name].is_contiguous():
+                    raise ValueError(f"{name} must be contiguous, of type {dt} and of {size} elements")
+        self.grad_dtype = BPT_BF16 if gts == {torch.bfloat16} else BPT_F32
+        self.lowp_dtype = BPT_BF16 if lows == {torch.bfloat16} else BPT_F32
+        self.array = (AdamWTensor * max(len(self.tensors), 1))(*[
+            AdamWTensor(t["p"].numel(), t["p"].data_ptr(), t["g"].data_ptr(), t["m"].data_ptr(), t[second].data_ptr(),
+                        _ptr(t.get("exps")) if bits == 8 else None, _ptr(t.get("p_lowp")), float(t.get("weight_decay", 0.0)))
+            for t in self.tensors])
+
+
+def adamw_multi(tensors: AdamWTensors, step: int, lr: float, beta1: float = 0.9, beta2: float = 0.95, eps: float = 1e-8,
+                seed: int = 0) -> None:
+    """One AdamW update of every tensor of the list, in place."""
+    cfg = AdamWMultiConfig(lr, beta1, beta2, eps, step, seed & (2 ** 64 - 1), tensors.bits, tensors.grad_dtype, tensors.lowp_dtype, 0)
+    _check(load().bpt_adamw_multi(ctypes.byref(cfg), tensors.array, len(tensors.tensors), _stream()))

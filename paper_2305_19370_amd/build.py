@@ -16,7 +16,8 @@ import tempfile
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
-SOURCES = ["libbpt.cpp", "gemm.hip", "attn_fwd.hip", "attn_bwd_dq.hip", "attn_bwd_dkdv.hip", "rowwise.hip", "gpt.hip", "dropout.hip"]
+SOURCES = ["libbpt.cpp", "gemm.hip", "attn_fwd.hip", "attn_bwd_dq.hip", "attn_bwd_dkdv.hip", "rowwise.hip", "gpt.hip", "dropout.hip",
+           "win_attn_fwd.hip", "win_attn_bwd.hip", "win_attn_f32.hip", "rope.hip", "adamw_multi.hip"]
 # per-source code generation options: the attention kernels keep the accumulators of
 # their MFMAs in architectural VGPRs (the default placement copies them between the
 # register files every iteration)
@@ -24,6 +25,8 @@ EXTRA_FLAGS = {
     "attn_fwd.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
     "attn_bwd_dq.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
     "attn_bwd_dkdv.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
+    "win_attn_fwd.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
+    "win_attn_bwd.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
 }
 LIB = os.path.join(PKG, "libbpt.so")
 # the matrix-core ceiling probe that bench.py --mfma-probe times (measurement only)

@@ -125,6 +125,70 @@ hipError_t attn_fwd(Dt dt, const AttnArgs& a, hipStream_t s);
 hipError_t attn_bwd_dkdv(Dt dt, const AttnArgs& a, hipStream_t s);
 hipError_t attn_bwd_dq(Dt dt, const AttnArgs& a, hipStream_t s);
 
+// ---------------------------------------------------------------- attention with a window and sinks
+// Element (b, t, h, d) of a tensor is at b * sb + t * st + h * sh + d. dout is laid out like o, dq, dk and
+// dv like q, k and v.
+struct WinArgs {
+  const void *q = nullptr, *k = nullptr, *v = nullptr, *dout = nullptr;
+  void *o = nullptr, *dq = nullptr, *dk = nullptr, *dv = nullptr;
+  int64_t q_sb = 0, q_sh = 0, k_sb = 0, k_sh = 0, v_sb = 0, v_sh = 0, o_sb = 0, o_sh = 0;
+  int q_st = 0, k_st = 0, v_st = 0, o_st = 0;
+  float* lse = nullptr;                 // [B, Hq] rows of lse_ld, natural log
+  int64_t lse_ld = 0;
+  const int32_t *q_lens = nullptr, *kv_lens = nullptr;   // [B] or null: all of Sq, Skv
+  int B = 0, Sq = 0, Skv = 0, Hq = 0, Hkv = 0, G = 1, dh = 0;   // G = Hq / Hkv
+  int causal = 0, window = 0, sinks = 0;   // window 0: none
+  float scale = 1.0f;                   // of the scores
+  int nsplit = 1;                       // slices of the keys (forward of few rows)
+  float *part_o = nullptr, *part_ml = nullptr;   // nsplit > 1: [nsplit, B Hkv Sq G] rows of dh, of (max, sum)
+  int64_t Sqp = 0;                      // Sq rounded up to 64
+  float *ndelta = nullptr, *nlse2 = nullptr;     // [B, Hq, Sqp]: -rowsum(dO O), -lse log2(e)
+};
+hipError_t win_fwd_bf16(const WinArgs& a, hipStream_t s);
+hipError_t win_fwd_f32(const WinArgs& a, hipStream_t s);
+hipError_t win_join(Dt t, const WinArgs& a, hipStream_t s);    // joins the slices of a forward
+hipError_t win_delta(Dt t, const WinArgs& a, hipStream_t s);   // ndelta, nlse2
+hipError_t win_dkdv_bf16(const WinArgs& a, hipStream_t s);
+hipError_t win_dkdv_f32(const WinArgs& a, hipStream_t s);
+hipError_t win_dq_bf16(const WinArgs& a, hipStream_t s);
+hipError_t win_dq_f32(const WinArgs& a, hipStream_t s);
+
+// ---------------------------------------------------------------- rotary positions
+struct RopeArgs {
+  const void* x = nullptr;
+  void* y = nullptr;                    // may be x
+  const int32_t* positions = nullptr;   // [rows], or null: pos0 + row % S
+  int64_t rows = 0, S = 1, ldx = 0, ldy = 0, pos0 = 0;
+  int H = 0, dh = 0, rot = 0, interleaved = 0;
+  float mscale = 1.0f;                  // both cosine and sine are multiplied by it
+  float sign = 1.0f;                    // -1: the transposed rotation (the gradient)
+  double turns[64];                     // full turns per position of pair i < rot / 2
+};
+hipError_t rope(Dt t, const RopeArgs& a, hipStream_t s);
+
+// ---------------------------------------------------------------- AdamW over many tensors
+struct AdamTensor {
+  float* p;
+  const void* g;
+  void* m;                              // fp32 [n], or e4m3 codes
+  void* v;                              // fp32 [n], or e4m3 codes of its square root
+  uint8_t* exps;                        // 8-bit moments: exponents of each block's m and r
+  void* low;                            // rounded copy of p, or null
+  int64_t n;
+  uint32_t first;                       // its first block of 256 elements among those of the launch
+  uint32_t key;                         // 8-bit moments: key of the rounding's random bits
+  float decay;                          // 1 - lr * weight decay
+};
+constexpr int kAdamTensors = 48;        // of one launch: what fits the kernel's arguments
+struct AdamArgs {
+  AdamTensor t[kAdamTensors];
+  int count = 0;
+  uint32_t blocks = 0;
+  float lr = 0, b1 = 0, nb1 = 0, b2 = 0, nb2 = 0, eps = 0;   // nb = 1 - b
+  float c1 = 0, rc2 = 0;                // 1 / (1 - b1^t), 1 / sqrt(1 - b2^t)
+};
+hipError_t adamw_multi(Dt tg, Dt tl, int bits, const AdamArgs& a, hipStream_t s);
+
 // ---------------------------------------------------------------- residual-branch dropout
 // Element (t, n) of branch `site` is kept iff word n % 4 of Philox4x32-10 at counter
 // (n / 4, t, site, 0), key (k0, k1), is >= threshold; kept values are multiplied by scale.

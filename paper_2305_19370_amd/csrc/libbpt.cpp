@@ -1194,4 +1194,314 @@ bpt_status bpt_adamw_step(const bpt_adamw_config* cfg, int64_t n, float* p, cons
   return BPT_OK;
 }
 
+// ---------------------------------------------------------------- rotary positions
+static bpt_status rope_check(const bpt_rope_config* c) {
+  if (!c) return fail(BPT_ERR_INVALID_ARG, "config is NULL");
+  if (c->rows < 1 || c->S < 1 || c->H < 1 || c->dh < 1) return fail(BPT_ERR_INVALID_ARG, "rows, S, H and dh must be >= 1");
+  if (c->rot < 2 || c->rot % 2 || c->rot > c->dh)
+    return fail(BPT_ERR_INVALID_ARG, "rot = %lld must be even and lie in [2, dh]", (long long)c->rot);
+  if (c->scaling < BPT_ROPE_NONE || c->scaling > BPT_ROPE_BY_PARTS) return fail(BPT_ERR_INVALID_ARG, "scaling is not a bpt_rope_scaling");
+  if (!(c->theta > 0.0) || !std::isfinite(c->theta)) return fail(BPT_ERR_INVALID_ARG, "theta must be > 0");
+  if (!std::isfinite(c->mscale)) return fail(BPT_ERR_INVALID_ARG, "mscale must be finite");
+  if (c->scaling != BPT_ROPE_NONE && (!(c->factor >= 1.0) || !std::isfinite(c->factor)))
+    return fail(BPT_ERR_INVALID_ARG, "factor must be >= 1");
+  if (c->scaling == BPT_ROPE_BASE && c->rot == 2) return fail(BPT_ERR_INVALID_ARG, "BPT_ROPE_BASE needs rot > 2");
+  if (c->scaling == BPT_ROPE_BY_PARTS && (c->orig_len < 1 || !(c->beta_fast > c->beta_slow) || !std::isfinite(c->beta_fast) || !std::isfinite(c->beta_slow)))
+    return fail(BPT_ERR_INVALID_ARG, "BPT_ROPE_BY_PARTS needs orig_len >= 1 and beta_fast > beta_slow");
+  if ((c->interleaved != 0 && c->interleaved != 1) || c->reserved != 0)
+    return fail(BPT_ERR_INVALID_ARG, "interleaved must be 0 or 1, reserved 0");
+  if (c->H > (int64_t)1 << 20 || c->dh > (int64_t)1 << 16) return fail(BPT_ERR_UNSUPPORTED, "H or dh too large");
+  if (c->ldx < c->H * c->dh || c->ldy < c->H * c->dh) return fail(BPT_ERR_INVALID_ARG, "ldx and ldy must be >= H dh");
+  bpt_status st = dtype_ok(c->dtype, "dtype");
+  if (st != BPT_OK) return st;
+  if (c->dh % 8 || c->ldx % 8 || c->ldy % 8) return fail(BPT_ERR_UNSUPPORTED, "dh, ldx and ldy must be multiples of 8");
+  if (c->rot > 128) return fail(BPT_ERR_UNSUPPORTED, "rot = %lld > 128", (long long)c->rot);
+  if (c->rows > INT32_MAX || c->H * c->dh > INT32_MAX / 8 || c->ldx > (int64_t)1 << 40 || c->ldy > (int64_t)1 << 40)
+    return fail(BPT_ERR_UNSUPPORTED, "rows, H dh or a row stride too large");
+  const int64_t most = (int64_t)1 << 52;             // positions are exact in a double
+  if (c->pos0 > most || c->pos0 < -most || c->S > most) return fail(BPT_ERR_UNSUPPORTED, "pos0 or S too large");
+  return BPT_OK;
+}
+
+static bpt_status rope_run(const bpt_rope_config* c, const int32_t* positions, const void* x, int64_t ldx, void* y, int64_t ldy,
+                           float sign, void* stream) {
+  bpt_status st = rope_check(c);
+  if (st != BPT_OK) return st;
+  if (!x || !y) return fail(BPT_ERR_INVALID_ARG, "NULL tensor");
+  if (!aligned16(x) || !aligned16(y) || (positions && ((uintptr_t)positions & 3)))
+    return fail(BPT_ERR_INVALID_ARG, "tensors must be 16-byte aligned");
+  if (x == y && ldx != ldy) return fail(BPT_ERR_INVALID_ARG, "in place needs ldx == ldy");
+  RopeArgs a;
+  a.x = x; a.y = y; a.positions = positions;
+  a.rows = c->rows; a.S = c->S; a.ldx = ldx; a.ldy = ldy; a.pos0 = c->pos0;
+  a.H = (int)c->H; a.dh = (int)c->dh; a.rot = (int)c->rot; a.interleaved = c->interleaved;
+  a.mscale = (float)c->mscale; a.sign = sign;
+  const double pi2 = 6.283185307179586476925;
+  const double rot = (double)c->rot;
+  const double theta = c->scaling == BPT_ROPE_BASE ? c->theta * std::pow(c->factor, rot / (rot - 2.0)) : c->theta;
+  for (int i = 0; i < c->rot / 2; ++i) {
+    double f = std::pow(theta, -2.0 * i / rot);
+    if (c->scaling == BPT_ROPE_LINEAR) f /= c->factor;
+    if (c->scaling == BPT_ROPE_BY_PARTS) {
+      const double turns = (double)c->orig_len * f / pi2;
+      const double g = std::min(1.0, std::max(0.0, (turns - c->beta_slow) / (c->beta_fast - c->beta_slow)));
+      f *= g + (1.0 - g) / c->factor;
+    }
+    a.turns[i] = f / pi2;
+  }
+  hipStream_t s = (hipStream_t)stream;
+  const int64_t moved = (x == y ? c->rot : c->dh) * c->H;
+  RUN(sign > 0 ? "rope.fwd" : "rope.bwd", 3.0 * c->rows * c->H * c->rot, 2.0 * c->rows * moved * esize(c->dtype) + (positions ? 4.0 * c->rows : 0.0),
+      rope(dt_of(c->dtype), a, s));
+  return BPT_OK;
+}
+
+bpt_status bpt_rope_validate(const bpt_rope_config* cfg) { return rope_check(cfg); }
+
+bpt_status bpt_rope_fwd(const bpt_rope_config* cfg, const int32_t* positions, const void* X, void* Y, void* stream) {
+  return rope_run(cfg, positions, X, cfg ? cfg->ldx : 0, Y, cfg ? cfg->ldy : 0, 1.0f, stream);
+}
+bpt_status bpt_rope_bwd(const bpt_rope_config* cfg, const int32_t* positions, const void* dY, void* dX, void* stream) {
+  return rope_run(cfg, positions, dY, cfg ? cfg->ldy : 0, dX, cfg ? cfg->ldx : 0, -1.0f, stream);
+}
+
+// ---------------------------------------------------------------- attention with a window and sinks
+// Whether no two elements of a tensor share a place (dims of stride and size; features are adjacent)
+static bool apart(const bpt_attn_strides& t, int64_t B, int64_t S, int64_t H, int64_t dh) {
+  std::pair<int64_t, int64_t> d[] = {{t.sb, B}, {t.st, S}, {t.sh, H}};
+  std::sort(d, d + 3);
+  int64_t span = dh;
+  for (auto& e : d) {
+    if (e.second == 1) continue;
+    if (e.first < span) return false;
+    span += e.first * (e.second - 1);
+  }
+  return true;
+}
+
+constexpr int64_t kAttnMax = (int64_t)1 << 28;      // sums of a few lengths stay within 32 bits
+
+static bpt_status attn_check(const bpt_attn_config* c) {
+  if (!c) return fail(BPT_ERR_INVALID_ARG, "config is NULL");
+  if (c->B < 1 || c->Sq < 1 || c->Skv < 1 || c->Hq < 1 || c->Hkv < 1 || c->dh < 1)
+    return fail(BPT_ERR_INVALID_ARG, "B, Sq, Skv, Hq, Hkv, dh must be >= 1");
+  if (c->Hq % c->Hkv) return fail(BPT_ERR_INVALID_ARG, "Hq=%lld is not a multiple of Hkv=%lld", (long long)c->Hq, (long long)c->Hkv);
+  if (c->window < 0 || c->sinks < 0 || (c->window == 0 && c->sinks != 0))
+    return fail(BPT_ERR_INVALID_ARG, "window and sinks must be >= 0, and sinks 0 without a window");
+  if (!(c->scale > 0.0f) || !std::isfinite(c->scale)) return fail(BPT_ERR_INVALID_ARG, "scale must be > 0");
+  if ((c->causal != 0 && c->causal != 1) || c->reserved != 0) return fail(BPT_ERR_INVALID_ARG, "causal must be 0 or 1, reserved 0");
+  bpt_status st = dtype_ok(c->dtype, "dtype");
+  if (st != BPT_OK) return st;
+  const bpt_attn_strides* all[] = {&c->q, &c->k, &c->v, &c->o};
+  const int64_t unit = 16 / (int64_t)esize(c->dtype);
+  for (auto* t : all) {
+    if (t->sb < 0 || t->st < 0 || t->sh < 0) return fail(BPT_ERR_INVALID_ARG, "strides must be >= 0");
+    if (t->sb % unit || t->st % unit || t->sh % unit) return fail(BPT_ERR_INVALID_ARG, "strides must be multiples of 16 bytes");
+    if (t->st >= (int64_t)1 << 22 || t->sb >= (int64_t)1 << 40 || t->sh >= (int64_t)1 << 40)
+      return fail(BPT_ERR_UNSUPPORTED, "a stride is too large");
+  }
+  if (c->dh != 64 && c->dh != 128) return fail(BPT_ERR_UNSUPPORTED, "head dim %lld unsupported (64 or 128)", (long long)c->dh);
+  if (c->B > 65535 || c->Hkv > 65535 || c->Hq > 65535) return fail(BPT_ERR_UNSUPPORTED, "B and heads must be <= 65535");
+  if (c->Sq > kAttnMax || c->Skv > kAttnMax || c->window > kAttnMax || c->sinks > kAttnMax || c->Sq * (c->Hq / c->Hkv) > kAttnMax)
+    return fail(BPT_ERR_UNSUPPORTED, "lengths, window and sinks must be <= 2^28, and Sq Hq / Hkv too");
+  // workgroups of 16 rows and rows of the log-sum-exp
+  if (c->B * c->Hkv * ((std::max(c->Sq * (c->Hq / c->Hkv), c->Skv) + 15) / 16) > (int64_t)1 << 26 || c->B * c->Hq * rup(c->Sq, 64) > (int64_t)1 << 32)
+    return fail(BPT_ERR_UNSUPPORTED, "B * heads * length too large");
+  if (!apart(c->o, c->B, c->Sq, c->Hq, c->dh)) return fail(BPT_ERR_INVALID_ARG, "strides of O overlap");
+  return BPT_OK;
+}
+
+// Slices of the keys for a forward of few rows
+static int attn_nsplit(const bpt_attn_config& c) {
+  if (c.dtype == BPT_BF16) return 1;
+  const int64_t rows = c.Sq * (c.Hq / c.Hkv), groups = (rows + 15) / 16 * c.Hkv * c.B;
+  const int64_t span = c.window ? std::min(c.Skv, c.window + c.sinks + c.Sq) : c.Skv;
+  return (int)std::max<int64_t>(1, std::min<int64_t>({512 / groups, span / 512, 64}));
+}
+
+struct AttnWs {
+  float *part_o, *part_ml;     // forward: slices
+  float *ndelta, *nlse2;       // backward
+};
+static AttnWs attn_ws(const bpt_attn_config& c, void* base, int backward, int64_t* total) {
+  Bump bp(base);
+  AttnWs w{};
+  if (backward) {
+    const int64_t n = c.B * c.Hq * rup(c.Sq, 64) * 4;
+    w.ndelta = (float*)bp.take(n);
+    w.nlse2 = (float*)bp.take(n);
+  } else if (const int z = attn_nsplit(c); z > 1) {
+    w.part_o = (float*)bp.take(z * c.B * c.Hq * c.Sq * c.dh * 4);
+    w.part_ml = (float*)bp.take(z * c.B * c.Hq * c.Sq * 8);
+  }
+  *total = rup(bp.off, kAlign);
+  return w;
+}
+
+static WinArgs attn_args(const bpt_attn_config& c, const void* Q, const void* K, const void* V, const int32_t* q_lens,
+                         const int32_t* kv_lens, const void* O, const float* lse) {
+  WinArgs a;
+  a.q = Q; a.k = K; a.v = V; a.o = (void*)O; a.lse = (float*)lse; a.lse_ld = c.Sq;
+  a.q_sb = c.q.sb; a.q_st = (int)c.q.st; a.q_sh = c.q.sh;
+  a.k_sb = c.k.sb; a.k_st = (int)c.k.st; a.k_sh = c.k.sh;
+  a.v_sb = c.v.sb; a.v_st = (int)c.v.st; a.v_sh = c.v.sh;
+  a.o_sb = c.o.sb; a.o_st = (int)c.o.st; a.o_sh = c.o.sh;
+  a.q_lens = q_lens; a.kv_lens = kv_lens;
+  a.B = (int)c.B; a.Sq = (int)c.Sq; a.Skv = (int)c.Skv;
+  a.Hq = (int)c.Hq; a.Hkv = (int)c.Hkv; a.G = (int)(c.Hq / c.Hkv); a.dh = (int)c.dh;
+  a.causal = c.causal; a.window = (int)c.window; a.sinks = (int)c.sinks; a.scale = c.scale;
+  a.Sqp = rup(c.Sq, 64);
+  return a;
+}
+
+// visible pairs of a sequence of whole length, for the launch record
+static double attn_seen(const bpt_attn_config& c) {
+  const double per = c.window ? (double)std::min(c.Skv, (c.causal ? 1 : 2) * c.window + c.sinks) : (double)c.Skv;
+  return (double)c.B * c.Hq * c.Sq * (c.causal && !c.window ? per - 0.5 * (double)std::min(c.Sq, c.Skv) : per);
+}
+
+bpt_status bpt_attn_validate(const bpt_attn_config* cfg) { return attn_check(cfg); }
+
+size_t bpt_attn_workspace_bytes(const bpt_attn_config* cfg, int backward) {
+  if (attn_check(cfg) != BPT_OK) return 0;
+  int64_t total;
+  attn_ws(*cfg, nullptr, backward, &total);
+  return (size_t)total;
+}
+
+bpt_status bpt_attn_fwd(const bpt_attn_config* cfg, const void* Q, const void* K, const void* V, const int32_t* q_lens,
+                        const int32_t* kv_lens, void* O, float* lse, void* ws, size_t ws_bytes, void* stream) {
+  bpt_status st = attn_check(cfg);
+  if (st != BPT_OK) return st;
+  if (!Q || !K || !V || !O || !lse) return fail(BPT_ERR_INVALID_ARG, "NULL Q, K, V, O or lse");
+  if (O == Q || O == K || O == V) return fail(BPT_ERR_INVALID_ARG, "O must not alias Q, K or V");
+  const void* ptrs[] = {Q, K, V, O, lse, ws, q_lens, kv_lens};
+  for (const void* q : ptrs)
+    if (q && !aligned16(q)) return fail(BPT_ERR_INVALID_ARG, "pointer %p is not 16-byte aligned", q);
+  int64_t need;
+  const AttnWs w = attn_ws(*cfg, ws, 0, &need);
+  if (need > 0 && (!ws || (int64_t)ws_bytes < need))
+    return fail(BPT_ERR_WORKSPACE, "workspace %zu bytes < required %lld", ws ? ws_bytes : (size_t)0, (long long)need);
+  WinArgs a = attn_args(*cfg, Q, K, V, q_lens, kv_lens, O, lse);
+  a.nsplit = attn_nsplit(*cfg);
+  a.part_o = w.part_o; a.part_ml = w.part_ml;
+  hipStream_t s = (hipStream_t)stream;
+  const bool bf = cfg->dtype == BPT_BF16;
+  const double E_ = bf ? 2 : 4, seen = attn_seen(*cfg);
+  RUN("win.fwd", 4.0 * cfg->dh * seen, E_ * cfg->dh * (2.0 * cfg->B * cfg->Hq * cfg->Sq + 2.0 * cfg->B * cfg->Hkv * cfg->Skv),
+      bf ? win_fwd_bf16(a, s) : win_fwd_f32(a, s));
+  if (a.nsplit > 1)
+    RUN("win.join", 0, (double)cfg->B * cfg->Hq * cfg->Sq * cfg->dh * (4.0 * a.nsplit + E_), win_join(dt_of(cfg->dtype), a, s));
+  return BPT_OK;
+}
+
+bpt_status bpt_attn_bwd(const bpt_attn_config* cfg, const void* Q, const void* K, const void* V, const int32_t* q_lens,
+                        const int32_t* kv_lens, const void* O, const float* lse, const void* dO, void* dQ, void* dK,
+                        void* dV, void* ws, size_t ws_bytes, void* stream) {
+  bpt_status st = attn_check(cfg);
+  if (st != BPT_OK) return st;
+  if (!Q || !K || !V || !O || !lse || !dO || !ws) return fail(BPT_ERR_INVALID_ARG, "NULL Q, K, V, O, lse, dO or workspace");
+  if ((dK == nullptr) != (dV == nullptr)) return fail(BPT_ERR_INVALID_ARG, "dK and dV must both be given or both be NULL");
+  const void* in[] = {Q, K, V, O, lse, dO, ws, q_lens, kv_lens};
+  void* out[] = {dQ, dK, dV};
+  for (const void* q : in)
+    if (q && !aligned16(q)) return fail(BPT_ERR_INVALID_ARG, "pointer %p is not 16-byte aligned", q);
+  for (int i = 0; i < 3; ++i) {
+    if (!out[i]) continue;
+    if (!aligned16(out[i])) return fail(BPT_ERR_INVALID_ARG, "pointer %p is not 16-byte aligned", out[i]);
+    for (const void* q : in)
+      if (q == out[i]) return fail(BPT_ERR_INVALID_ARG, "dQ, dK and dV must not alias an input");
+    for (int j = 0; j < i; ++j)
+      if (out[j] == out[i]) return fail(BPT_ERR_INVALID_ARG, "dQ, dK and dV must not alias one another");
+  }
+  if ((dQ && !apart(cfg->q, cfg->B, cfg->Sq, cfg->Hq, cfg->dh)) ||
+      (dK && (!apart(cfg->k, cfg->B, cfg->Skv, cfg->Hkv, cfg->dh) || !apart(cfg->v, cfg->B, cfg->Skv, cfg->Hkv, cfg->dh))))
+    return fail(BPT_ERR_INVALID_ARG, "strides of dQ, dK or dV overlap");
+  int64_t need;
+  const AttnWs w = attn_ws(*cfg, ws, 1, &need);
+  if ((int64_t)ws_bytes < need) return fail(BPT_ERR_WORKSPACE, "workspace %zu bytes < required %lld", ws_bytes, (long long)need);
+  WinArgs a = attn_args(*cfg, Q, K, V, q_lens, kv_lens, O, lse);
+  a.dout = dO; a.dq = dQ; a.dk = dK; a.dv = dV;
+  a.ndelta = w.ndelta; a.nlse2 = w.nlse2;
+  hipStream_t s = (hipStream_t)stream;
+  const bool bf = cfg->dtype == BPT_BF16;
+  const double E_ = bf ? 2 : 4, seen = attn_seen(*cfg), q = (double)cfg->B * cfg->Hq * cfg->Sq * cfg->dh, kv = (double)cfg->B * cfg->Hkv * cfg->Skv * cfg->dh;
+  RUN("win.delta", 0, 2.0 * q * E_, win_delta(dt_of(cfg->dtype), a, s));
+  if (dK) RUN("win.dkdv", 8.0 * cfg->dh * seen, (2.0 * q + 4.0 * kv) * E_, bf ? win_dkdv_bf16(a, s) : win_dkdv_f32(a, s));
+  if (dQ) RUN("win.dq", 6.0 * cfg->dh * seen, (3.0 * q + 2.0 * kv) * E_, bf ? win_dq_bf16(a, s) : win_dq_f32(a, s));
+  return BPT_OK;
+}
+
+// ---------------------------------------------------------------- AdamW over many tensors
+static uint32_t mix32(uint32_t x) {                  // the kernel's, for the tensors' keys
+  x ^= x >> 16;
+  x *= 0x9E3779B1u;
+  x ^= x >> 15;
+  x *= 0x6A09E667u;
+  return x ^ (x >> 16);
+}
+
+bpt_status bpt_adamw_multi(const bpt_adamw_multi_config* cfg, const bpt_adamw_tensor* tensors, int64_t count, void* stream) {
+  if (!cfg) return fail(BPT_ERR_INVALID_ARG, "NULL config");
+  if (count < 0 || (count > 0 && !tensors)) return fail(BPT_ERR_INVALID_ARG, "count must be >= 0, tensors not NULL");
+  if (count > (int64_t)1 << 20) return fail(BPT_ERR_UNSUPPORTED, "more than 2^20 tensors");
+  if (cfg->step < 1) return fail(BPT_ERR_INVALID_ARG, "step must be >= 1");
+  if (!(cfg->beta1 >= 0.0 && cfg->beta1 < 1.0 && cfg->beta2 >= 0.0 && cfg->beta2 < 1.0))
+    return fail(BPT_ERR_INVALID_ARG, "beta1 and beta2 must lie in [0, 1)");
+  if (!((float)cfg->eps > 0.0f) || !(cfg->lr >= 0.0) || !std::isfinite(cfg->lr) || !std::isfinite(cfg->eps))
+    return fail(BPT_ERR_INVALID_ARG, "eps must be > 0, lr >= 0");
+  if (cfg->state_bits != 32 && cfg->state_bits != 8) return fail(BPT_ERR_INVALID_ARG, "state_bits must be 32 or 8");
+  if (cfg->reserved != 0) return fail(BPT_ERR_INVALID_ARG, "reserved must be 0");
+  bpt_status st = dtype_ok(cfg->grad_dtype, "grad_dtype");
+  if (st != BPT_OK || (st = dtype_ok(cfg->lowp_dtype, "lowp_dtype")) != BPT_OK) return st;
+  const bool small = cfg->state_bits == 8;
+  std::vector<std::pair<uintptr_t, uintptr_t>> at;
+  at.reserve(count);
+  for (int64_t i = 0; i < count; ++i) {
+    const bpt_adamw_tensor& t = tensors[i];
+    if (t.n < 0) return fail(BPT_ERR_INVALID_ARG, "tensor %lld: n must be >= 0", (long long)i);
+    if (t.n == 0) continue;
+    if (t.n > (int64_t)1 << 38) return fail(BPT_ERR_UNSUPPORTED, "tensor %lld too large", (long long)i);
+    if (!t.p || !t.g || !t.m || !t.v || (small && !t.exps))
+      return fail(BPT_ERR_INVALID_ARG, "tensor %lld: NULL p, g, m, v or exps", (long long)i);
+    if (!(t.weight_decay >= 0.0) || !std::isfinite(t.weight_decay))
+      return fail(BPT_ERR_INVALID_ARG, "tensor %lld: weight_decay must be >= 0", (long long)i);
+    const void* ptrs[] = {t.p, t.g, t.m, t.v, t.p_lowp};
+    for (const void* q : ptrs)
+      if (q && !aligned16(q)) return fail(BPT_ERR_INVALID_ARG, "tensor %lld: pointer %p is not 16-byte aligned", (long long)i, q);
+    if (small && ((uintptr_t)t.exps & 1)) return fail(BPT_ERR_INVALID_ARG, "tensor %lld: exps is not 2-byte aligned", (long long)i);
+    at.push_back({(uintptr_t)t.p, (uintptr_t)t.p + 4 * (uintptr_t)t.n});
+  }
+  std::sort(at.begin(), at.end());
+  for (size_t i = 1; i < at.size(); ++i)
+    if (at[i].first < at[i - 1].second) return fail(BPT_ERR_INVALID_ARG, "two tensors' p overlap (the same tensor twice?)");
+  hipStream_t s = (hipStream_t)stream;
+  const uint32_t key = mix32(mix32((uint32_t)cfg->seed) ^ (uint32_t)(cfg->seed >> 32) ^ (uint32_t)cfg->step);
+  const int64_t kMostBlocks = (int64_t)1 << 31;      // of one launch
+  AdamArgs a;
+  a.lr = (float)cfg->lr; a.eps = (float)cfg->eps;
+  a.b1 = (float)cfg->beta1; a.nb1 = (float)(1.0 - cfg->beta1);
+  a.b2 = (float)cfg->beta2; a.nb2 = (float)(1.0 - cfg->beta2);
+  a.c1 = (float)(1.0 / (1.0 - std::pow(cfg->beta1, (double)cfg->step)));
+  a.rc2 = (float)std::sqrt(1.0 / (1.0 - std::pow(cfg->beta2, (double)cfg->step)));
+  const Dt tg = dt_of(cfg->grad_dtype), tl = dt_of(cfg->lowp_dtype);
+  double bytes = 0;
+  for (int64_t i = 0; i <= count; ++i) {
+    const bool more = i < count;
+    const int64_t nb = more ? (tensors[i].n + 255) / 256 : 0;
+    if (a.count > 0 && (!more || a.count == kAdamTensors || a.blocks + nb > kMostBlocks)) {
+      RUN("adamw.multi", 0, bytes, adamw_multi(tg, tl, cfg->state_bits, a, s));
+      a.count = 0;
+      a.blocks = 0;
+      bytes = 0;
+    }
+    if (!more || nb == 0) continue;
+    const bpt_adamw_tensor& t = tensors[i];
+    a.t[a.count++] = AdamTensor{t.p, t.g, t.m, t.v, t.exps, t.p_lowp, t.n, a.blocks, mix32(key ^ (uint32_t)i), (float)(1.0 - cfg->lr * t.weight_decay)};
+    a.blocks += (uint32_t)nb;
+    bytes += (double)t.n * (8 + esize(cfg->grad_dtype) + (small ? 4 : 16) + (t.p_lowp ? esize(cfg->lowp_dtype) : 0));
+  }
+  return BPT_OK;
+}
+
 }  // extern "C"

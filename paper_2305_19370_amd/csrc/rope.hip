@@ -1,0 +1,138 @@
+// Rotary positions: pair (a, b) of a head at position p becomes (c a - s b, s a + c b), c and s the cosine and
+// sine of p times the pair's frequency, times mscale; the gradient is the rotation by the opposite angle.
+//
+// A workgroup takes a few rows (tokens): it forms their cosines and sines once, in LDS, for all heads, then streams the heads
+// through, 16 bytes per access. The angle is reduced in full turns in 64 bits (positions of a million
+// leave no digits of it in 32), the remainder of a turn in fp32.
+#include "common.h"
+#include "internal.h"
+
+namespace bpt {
+
+namespace {
+
+constexpr int kRopeRows = 4;             // rows of a workgroup, at most
+constexpr int kMaxPairs = 64;
+
+template <int N> BPT_DEV void ld(const float* p, float* v) {
+  if constexpr (N == 1) {
+    v[0] = p[0];
+  } else {
+#pragma unroll
+    for (int q = 0; q < N / 4; ++q) {
+      const f32x4 x = *(const f32x4*)(p + 4 * q);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[4 * q + e] = x[e];
+    }
+  }
+}
+template <int N> BPT_DEV void ld(const bf16* p, float* v) {
+  if constexpr (N == 1) {
+    v[0] = (float)p[0];
+  } else {
+    const bf16x8 x = *(const bf16x8*)p;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = (float)x[e];
+  }
+}
+template <int N> BPT_DEV void st(float* p, const float* v) {
+  if constexpr (N == 1) {
+    p[0] = v[0];
+  } else {
+#pragma unroll
+    for (int q = 0; q < N / 4; ++q) *(f32x4*)(p + 4 * q) = f32x4{v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]};
+  }
+}
+template <int N> BPT_DEV void st(bf16* p, const float* v) {
+  if constexpr (N == 1) {
+    p[0] = (bf16)v[0];
+  } else {
+    bf16x8 x;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = (bf16)v[e];
+    *(bf16x8*)p = x;
+  }
+}
+
+}  // namespace
+
+// Units of a head: half layout, N elements of the first half of the rotated part and their partners; interleaved,
+// N elements (a pair for N = 1); behind the rotated part, N elements that are copied. N = 8 or 1.
+template <typename T, int N, bool INTER>
+__global__ __launch_bounds__(256) void rope_kernel(RopeArgs a, int rows_per) {
+  __shared__ float2 cs[kRopeRows][kMaxPairs];
+  const int tid = threadIdx.x, pairs = a.rot / 2;
+  const int64_t r0 = (int64_t)blockIdx.x * rows_per;
+  const int nr = (int)(a.rows - r0 < rows_per ? a.rows - r0 : rows_per);
+  for (int e = tid; e < nr * pairs; e += 256) {
+    const int r = e / pairs, i = e - r * pairs;
+    const int64_t p = a.positions ? (int64_t)a.positions[r0 + r] : a.pos0 + (r0 + r) % a.S;
+    const double t = (double)p * a.turns[i];
+    float s, c;
+    sincospif(2.0f * (float)(t - rint(t)), &s, &c);
+    cs[r][i] = float2{c * a.mscale, s * a.mscale * a.sign};
+  }
+  __syncthreads();
+  const int turned = INTER ? (N == 1 ? pairs : a.rot / N) : pairs / N;
+  const int units = turned + (a.x == a.y ? 0 : (a.dh - a.rot) / N);
+  const T* X = (const T*)a.x + r0 * a.ldx;
+  T* Y = (T*)a.y + r0 * a.ldy;
+  const int per_row = units * a.H;
+  for (int e = tid; e < nr * per_row; e += 256) {
+    const int r = e / per_row, f = e - r * per_row, h = f / units, u = f - h * units;
+    const T* x = X + r * a.ldx + (int64_t)h * a.dh;
+    T* y = Y + r * a.ldy + (int64_t)h * a.dh;
+    if (u >= turned) {
+      const int d = a.rot + (u - turned) * N;
+      float v[N];
+      ld<N>(x + d, v);
+      st<N>(y + d, v);
+    } else if (!INTER) {
+      float v[N], w[N], p[N], q[N];
+      ld<N>(x + N * u, v);
+      ld<N>(x + pairs + N * u, w);
+#pragma unroll
+      for (int k = 0; k < N; ++k) {
+        const float2 z = cs[r][N * u + k];
+        p[k] = z.x * v[k] - z.y * w[k];
+        q[k] = z.x * w[k] + z.y * v[k];
+      }
+      st<N>(y + N * u, p);
+      st<N>(y + pairs + N * u, q);
+    } else if (N == 1) {
+      const float2 z = cs[r][u];
+      const float v = to_f32<T>(x[2 * u]), w = to_f32<T>(x[2 * u + 1]);
+      y[2 * u] = from_f32<T>(z.x * v - z.y * w);
+      y[2 * u + 1] = from_f32<T>(z.x * w + z.y * v);
+    } else {
+      float v[N];
+      ld<N>(x + N * u, v);
+#pragma unroll
+      for (int k = 0; k < N / 2; ++k) {
+        const float2 z = cs[r][N / 2 * u + k];
+        const float p = v[2 * k], q = v[2 * k + 1];
+        v[2 * k] = z.x * p - z.y * q;
+        v[2 * k + 1] = z.x * q + z.y * p;
+      }
+      st<N>(y + N * u, v);
+    }
+  }
+}
+
+template <typename T, int N, bool INTER>
+static hipError_t launch(const RopeArgs& a, hipStream_t s) {
+  const int rows_per = a.rows >= 4096 ? kRopeRows : 1;   // few rows: one per workgroup
+  const int64_t grid = (a.rows + rows_per - 1) / rows_per;
+  hipLaunchKernelGGL((rope_kernel<T, N, INTER>), dim3((unsigned)grid), dim3(256), 0, s, a, rows_per);
+  return hipGetLastError();
+}
+template <typename T>
+static hipError_t launch_t(const RopeArgs& a, hipStream_t s) {
+  const bool wide = a.rot % (a.interleaved ? 8 : 16) == 0;   // 16-byte pieces; dh and the row strides are multiples of 8
+  if (a.interleaved) return wide ? launch<T, 8, true>(a, s) : launch<T, 1, true>(a, s);
+  return wide ? launch<T, 8, false>(a, s) : launch<T, 1, false>(a, s);
+}
+
+hipError_t rope(Dt t, const RopeArgs& a, hipStream_t s) { return t == BF16 ? launch_t<bf16>(a, s) : launch_t<float>(a, s); }
+
+}  // namespace bpt

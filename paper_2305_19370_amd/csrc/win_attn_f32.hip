@@ -1,0 +1,346 @@
+// Attention with a sliding window and sinks, fp32: forward (whole, or one of several slices of
+// the keys), its join, and the backward. Matrix products on v_mfma_f32_16x16x4_f32 (attn_common.h:
+// row and column fragments straight from memory, 4 waves sharing 16 rows).
+//
+// The query heads of a kv head and their tokens are one list of rows, r = token * G + head: a
+// workgroup's 16 rows then cover few tokens, see nearly the same keys, and a single token's heads
+// fill one workgroup.
+#include "win_attn.h"
+
+namespace bpt {
+
+namespace {
+
+// Column fragment of rows given by a clamp of the key index
+template <int DH>
+BPT_DEV ColFrag<DH> col_frag_vis(const float* X, int64_t ld, int key0, const Vis& v, int g, int c16) {
+  ColFrag<DH> f;
+#pragma unroll
+  for (int r = 0; r < 4; ++r) {
+    const int64_t row = v.clamp(key0 + 4 * g + r);
+#pragma unroll
+    for (int t = 0; t < DH / 16; ++t) f.v[r][t] = X[row * ld + 16 * t + c16];
+  }
+  return f;
+}
+
+}  // namespace
+
+// 16 rows of one kv head; wave w takes the key tiles of 32 w, w + 4, ... of the slice, with its own
+// running maximum and sum (both in units of the raw products; -inf and 0 until a row has seen a
+// key), merged at the end in wave order. Several slices: the unnormalised numerator, maximum and sum go to
+// the workspace, for win_join.
+template <int DH>
+__global__ __launch_bounds__(256) void win_fwd_f32_kernel(WinArgs a) {
+  constexpr int NC = DH / 16;
+  __shared__ __attribute__((aligned(16))) float red[4][16][DH + 4];
+  __shared__ float red_m[4][16], red_l[4][16];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, g = lane >> 4, c16 = lane & 15;
+  const int rows = a.Sq * a.G, nblk = (rows + 15) / 16;
+  const int slice = blockIdx.x / nblk, blk = nblk - 1 - blockIdx.x % nblk;   // most keys first
+  const int kvh = blockIdx.y, b = blockIdx.z;
+  const Seq sq = seq_of(a, b);
+  const int r0 = blk * 16;
+  const int i0 = r0 / a.G, i1 = min((r0 + 15) / a.G, sq.nq - 1);
+  const int row = r0 + c16, i = row / a.G, h = kvh * a.G + row % a.G;
+  const float c = a.scale * LOG2E;
+
+  Vis mine{0, -1, 0}, run{0, -1, 0};
+  if (i < sq.nq) mine = vis_of(a, sq, sq.off + i, sq.off + i);
+  if (i0 <= i1) run = vis_run(a, sq, sq.off + i0, sq.off + i1);
+  const Tiles<32> tiles(run);
+  const int per = (tiles.n + a.nsplit - 1) / a.nsplit, j0 = slice * per, j1 = min(j0 + per, tiles.n);
+
+  const float* Kb = (const float*)a.k + (int64_t)b * a.k_sb + (int64_t)kvh * a.k_sh;
+  const float* Vb = (const float*)a.v + (int64_t)b * a.v_sb + (int64_t)kvh * a.v_sh;
+  f32x4 acc[NC];
+#pragma unroll
+  for (int t = 0; t < NC; ++t) acc[t] = f32x4{};
+  float m_run = NEG_INF, l_run = 0.0f;
+  if (j0 < j1) {                                   // the run has a query: row i1 exists
+    const int qi = min(i, sq.nq - 1);
+    const RowFrag<DH> qf = row_frag<DH>((const float*)a.q + (int64_t)b * a.q_sb + (int64_t)qi * a.q_st + (int64_t)h * a.q_sh, g);
+    for (int j = j0 + wave; j < j1; j += 4) {
+      const int k0 = tiles.key0(j);
+      f32x4 s[2];
+      ColFrag<DH> vf[2];
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        const RowFrag<DH> kf = row_frag<DH>(Kb + (int64_t)run.clamp(k0 + 16 * u + c16) * a.k_st, g);
+        s[u] = dot_frags<DH>(kf, qf);
+      }
+#pragma unroll
+      for (int u = 0; u < 2; ++u) vf[u] = col_frag_vis<DH>(Vb, a.v_st, k0 + 16 * u, run, g, c16);
+      float mx = NEG_INF;
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          if (!mine.sees(k0 + 16 * u + 4 * g + r)) s[u][r] = NEG_INF;
+          else s[u][r] *= c;
+          mx = fmaxf(mx, s[u][r]);
+        }
+      const float m_new = fmaxf(m_run, max_groups(mx));
+      const float m_use = m_new == NEG_INF ? 0.0f : m_new;
+      const float corr = m_run == NEG_INF ? 0.0f : fast_exp2(m_run - m_use);
+      l_run *= corr;
+#pragma unroll
+      for (int t = 0; t < NC; ++t) acc[t] *= corr;
+      m_run = m_new;
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          s[u][r] = fast_exp2(s[u][r] - m_use);
+          l_run += s[u][r];
+        }
+#pragma unroll
+      for (int u = 0; u < 2; ++u) add_outer<DH>(acc, vf[u], s[u]);
+    }
+  }
+  l_run = sum_groups(l_run);
+  if (g == 0) {
+    red_m[wave][c16] = m_run;
+    red_l[wave][c16] = l_run;
+  }
+#pragma unroll
+  for (int t = 0; t < NC; ++t) *(f32x4*)&red[wave][c16][16 * t + 4 * g] = acc[t];
+  __syncthreads();
+  for (int e = tid; e < 16 * (DH / 4); e += 256) {
+    const int ri = e / (DH / 4), d = 4 * (e % (DH / 4)), rr = r0 + ri;
+    if (rr >= rows) continue;
+    float m = NEG_INF, l = 0.0f;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) m = fmaxf(m, red_m[w][ri]);
+    f32x4 o = {};
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      const float f = red_m[w][ri] == NEG_INF ? 0.0f : fast_exp2(red_m[w][ri] - m);
+      l = fmaf(red_l[w][ri], f, l);
+      o += f * *(const f32x4*)&red[w][ri][d];
+    }
+    if (a.nsplit > 1) {
+      const int64_t at = ((int64_t)slice * a.B * a.Hkv + (int64_t)b * a.Hkv + kvh) * rows + rr;
+      *(f32x4*)(a.part_o + at * DH + d) = o;
+      if (d == 0) {
+        a.part_ml[2 * at] = m;
+        a.part_ml[2 * at + 1] = l;
+      }
+      continue;
+    }
+    const int ii = rr / a.G, hh = kvh * a.G + rr % a.G;
+    const float inv = l > 0.0f ? 1.0f / l : 0.0f;   // a row that sees nothing: 0
+    *(f32x4*)((float*)a.o + (int64_t)b * a.o_sb + (int64_t)ii * a.o_st + (int64_t)hh * a.o_sh + d) = l > 0.0f ? o * inv : f32x4{};
+    if (d == 0) a.lse[((int64_t)b * a.Hq + hh) * a.lse_ld + ii] = l > 0.0f ? (m + log2f(l)) * LN2 : NEG_INF;
+  }
+}
+
+// Joins the slices of a row: one wave per row, the slices in order.
+template <typename T>
+__global__ __launch_bounds__(256) void win_join_kernel(WinArgs a) {
+  const int lane = threadIdx.x & 63;
+  const int rows = a.Sq * a.G;
+  const int64_t all = (int64_t)a.B * a.Hkv * rows, at = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (at >= all) return;
+  float m = NEG_INF;
+  for (int z = 0; z < a.nsplit; ++z) m = fmaxf(m, a.part_ml[2 * (z * all + at)]);
+  const int d = a.dh == 128 ? 2 * lane : lane;
+  float l = 0.0f, o0 = 0.0f, o1 = 0.0f;
+  if (m > NEG_INF)
+    for (int z = 0; z < a.nsplit; ++z) {
+      const int64_t p = z * all + at;
+      const float f = fast_exp2(a.part_ml[2 * p] - m);   // 0 for a slice without keys
+      l = fmaf(a.part_ml[2 * p + 1], f, l);
+      o0 = fmaf(a.part_o[p * a.dh + d], f, o0);
+      if (a.dh == 128) o1 = fmaf(a.part_o[p * a.dh + d + 1], f, o1);
+    }
+  const float inv = l > 0.0f ? 1.0f / l : 0.0f;
+  const int rr = (int)(at % rows), i = rr / a.G, bh = (int)(at / rows), b = bh / a.Hkv, h = bh % a.Hkv * a.G + rr % a.G;
+  T* o = (T*)a.o + (int64_t)b * a.o_sb + (int64_t)i * a.o_st + (int64_t)h * a.o_sh + d;
+  o[0] = from_f32<T>(o0 * inv);
+  if (a.dh == 128) o[1] = from_f32<T>(o1 * inv);
+  if (lane == 0) a.lse[((int64_t)b * a.Hq + h) * a.lse_ld + i] = l > 0.0f ? (m + log2f(l)) * LN2 : NEG_INF;
+}
+
+// -Delta = -sum_d dO O and minus the base-2 log-sum-exp of every row, [B, Hq, Sqp]; 0 where a row
+// sees nothing, and behind the rows. One wave per 64 / (dh / 8) rows, 8 features a lane.
+template <typename T, int DH>
+__global__ __launch_bounds__(256) void win_delta_kernel(WinArgs a) {
+  constexpr int LPR = DH / 8;                       // lanes per row
+  const int64_t at = ((int64_t)blockIdx.x * 256 + threadIdx.x) / LPR;
+  const int d = 8 * (threadIdx.x % LPR);
+  if (at >= (int64_t)a.B * a.Hq * a.Sqp) return;    // whole groups of LPR lanes leave together
+  const int i = (int)(at % a.Sqp), h = (int)(at / a.Sqp % a.Hq), b = (int)(at / a.Sqp / a.Hq);
+  const Seq sq = seq_of(a, b);
+  float s = 0.0f, nl = 0.0f;
+  if (i < sq.nq) {
+    const float l = a.lse[((int64_t)b * a.Hq + h) * a.lse_ld + i];
+    if (l > NEG_INF) {
+      const int64_t o = (int64_t)b * a.o_sb + (int64_t)i * a.o_st + (int64_t)h * a.o_sh + d;
+      const T *x = (const T*)a.o + o, *y = (const T*)a.dout + o;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) s = fmaf(to_f32<T>(x[e]), to_f32<T>(y[e]), s);
+      nl = -l * LOG2E;
+    }
+  }
+#pragma unroll
+  for (int o = LPR / 2; o >= 1; o >>= 1) s += __shfl_xor(s, o, 64);
+  if (d == 0) {
+    a.ndelta[at] = -s;
+    a.nlse2[at] = nl;
+  }
+}
+
+// dQ: 16 rows as in the forward, wave w takes the key tiles of 16 w, w + 4, ...; dS^T has the row on the
+// lane axis and is the B operand of dQ^T += K^T dS^T.
+template <int DH>
+__global__ __launch_bounds__(256) void win_dq_f32_kernel(WinArgs a) {
+  constexpr int NC = DH / 16;
+  __shared__ __attribute__((aligned(16))) float red[4][16][DH + 4];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, g = lane >> 4, c16 = lane & 15;
+  const int rows = a.Sq * a.G, r0 = (int)(gridDim.x - 1 - blockIdx.x) * 16;
+  const int kvh = blockIdx.y, b = blockIdx.z;
+  const Seq sq = seq_of(a, b);
+  const int i0 = r0 / a.G, i1 = min((r0 + 15) / a.G, sq.nq - 1);
+  const int row = r0 + c16, i = row / a.G, h = kvh * a.G + row % a.G;
+  const float c = a.scale * LOG2E;
+  Vis mine{0, -1, 0}, run{0, -1, 0};
+  if (i < sq.nq) mine = vis_of(a, sq, sq.off + i, sq.off + i);
+  if (i0 <= i1) run = vis_run(a, sq, sq.off + i0, sq.off + i1);
+  const Tiles<16> tiles(run);
+  const float* Kb = (const float*)a.k + (int64_t)b * a.k_sb + (int64_t)kvh * a.k_sh;
+  const float* Vb = (const float*)a.v + (int64_t)b * a.v_sb + (int64_t)kvh * a.v_sh;
+  f32x4 dq[NC];
+#pragma unroll
+  for (int t = 0; t < NC; ++t) dq[t] = f32x4{};
+  if (tiles.n > 0) {
+    const int qi = min(i, sq.nq - 1);
+    const RowFrag<DH> qf = row_frag<DH>((const float*)a.q + (int64_t)b * a.q_sb + (int64_t)qi * a.q_st + (int64_t)h * a.q_sh, g);
+    const RowFrag<DH> of = row_frag<DH>((const float*)a.dout + (int64_t)b * a.o_sb + (int64_t)qi * a.o_st + (int64_t)h * a.o_sh, g);
+    const int64_t sidx = ((int64_t)b * a.Hq + h) * a.Sqp + qi;
+    const float nl = a.nlse2[sidx], ndl = a.ndelta[sidx];
+    for (int j = wave; j < tiles.n; j += 4) {
+      const int k0 = tiles.key0(j);
+      const int64_t kr = run.clamp(k0 + c16);
+      const RowFrag<DH> kf = row_frag<DH>(Kb + kr * a.k_st, g), vf = row_frag<DH>(Vb + kr * a.v_st, g);
+      const ColFrag<DH> kc = col_frag_vis<DH>(Kb, a.k_st, k0, run, g, c16);
+      const f32x4 s = dot_frags<DH>(kf, qf);
+      f32x4 ds = dot_frags<DH>(vf, of);
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+        ds[r] = mine.sees(k0 + 4 * g + r) ? fast_exp2(fmaf(s[r], c, nl)) * (ds[r] + ndl) : 0.0f;
+      add_outer<DH>(dq, kc, ds);
+    }
+  }
+#pragma unroll
+  for (int t = 0; t < NC; ++t) *(f32x4*)&red[wave][c16][16 * t + 4 * g] = dq[t];
+  __syncthreads();
+  for (int e = tid; e < 16 * (DH / 4); e += 256) {
+    const int ri = e / (DH / 4), d = 4 * (e % (DH / 4)), rr = r0 + ri;
+    if (rr >= rows) continue;
+    const f32x4 x = ((*(const f32x4*)&red[0][ri][d] + *(const f32x4*)&red[1][ri][d]) + *(const f32x4*)&red[2][ri][d]) +
+                    *(const f32x4*)&red[3][ri][d];
+    const int ii = rr / a.G, hh = kvh * a.G + rr % a.G;
+    *(f32x4*)((float*)a.dq + (int64_t)b * a.q_sb + (int64_t)ii * a.q_st + (int64_t)hh * a.q_sh + d) = x * a.scale;
+  }
+}
+
+// dK, dV: 16 keys; wave w takes every fourth (query head, tile of 16 queries) pair of the kv head, in order. P
+// and dS have the key on the lane axis and are the B operands of dV^T += dO^T P, dK^T += Q^T dS.
+template <int DH>
+__global__ __launch_bounds__(256) void win_dkdv_f32_kernel(WinArgs a) {
+  constexpr int NC = DH / 16;
+  __shared__ __attribute__((aligned(16))) float red[4][16][DH + 4];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, g = lane >> 4, c16 = lane & 15;
+  const int kvh = blockIdx.y, b = blockIdx.z, k0 = blockIdx.x * 16, key = k0 + c16;
+  const Seq sq = seq_of(a, b);
+  const float c = a.scale * LOG2E;
+  f32x4 dk[NC], dv[NC];
+#pragma unroll
+  for (int t = 0; t < NC; ++t) dk[t] = dv[t] = f32x4{};
+  if (k0 < sq.nk) {
+    const int kr = min(key, sq.nk - 1);
+    QVis mine = qvis_of(a, sq, key, key, false);
+    if (key >= sq.nk) mine.hi = -1;
+    const int kl = min(k0 + 15, sq.nk - 1);
+    const QVis run = qvis_of(a, sq, k0, kl, false);
+    const RowFrag<DH> kf = row_frag<DH>((const float*)a.k + (int64_t)b * a.k_sb + (int64_t)kvh * a.k_sh + (int64_t)kr * a.k_st, g);
+    const RowFrag<DH> vf = row_frag<DH>((const float*)a.v + (int64_t)b * a.v_sb + (int64_t)kvh * a.v_sh + (int64_t)kr * a.v_st, g);
+    const int t0 = run.lo / 16, nt = run.hi >= run.lo ? run.hi / 16 + 1 - t0 : 0;
+    for (int it = wave; it < nt * a.G; it += 4) {
+      const int h = kvh * a.G + it / nt, q0 = 16 * (t0 + it % nt);
+      const float* Qb = (const float*)a.q + (int64_t)b * a.q_sb + (int64_t)h * a.q_sh;
+      const float* dOb = (const float*)a.dout + (int64_t)b * a.o_sb + (int64_t)h * a.o_sh;
+      const int64_t qr = min(max(q0 + c16, run.lo), run.hi);
+      const RowFrag<DH> qf = row_frag<DH>(Qb + qr * a.q_st, g), of = row_frag<DH>(dOb + qr * a.o_st, g);
+      const int64_t sidx = ((int64_t)b * a.Hq + h) * a.Sqp + q0 + 4 * g;   // Sqp % 64 == 0
+      const f32x4 l4 = *(const f32x4*)(a.nlse2 + sidx), d4 = *(const f32x4*)(a.ndelta + sidx);
+      Vis qv{run.lo, run.hi, 0};
+      f32x4 p = dot_frags<DH>(qf, kf), ds = dot_frags<DH>(of, vf);
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int q = q0 + 4 * g + r;
+        const bool ok = q >= mine.lo && q <= mine.hi;
+        p[r] = ok ? fast_exp2(fmaf(p[r], c, l4[r])) : 0.0f;
+        ds[r] = ok ? p[r] * (ds[r] + d4[r]) : 0.0f;
+      }
+      const ColFrag<DH> oc = col_frag_vis<DH>(dOb, a.o_st, q0, qv, g, c16);
+      add_outer<DH>(dv, oc, p);
+      const ColFrag<DH> qc = col_frag_vis<DH>(Qb, a.q_st, q0, qv, g, c16);
+      add_outer<DH>(dk, qc, ds);
+    }
+  }
+#pragma unroll
+  for (int which = 0; which < 2; ++which) {
+    __syncthreads();
+#pragma unroll
+    for (int t = 0; t < NC; ++t) *(f32x4*)&red[wave][c16][16 * t + 4 * g] = which ? dv[t] : dk[t];
+    __syncthreads();
+    const int64_t base = which ? (int64_t)b * a.v_sb + (int64_t)kvh * a.v_sh : (int64_t)b * a.k_sb + (int64_t)kvh * a.k_sh;
+    float* out = (float*)(which ? a.dv : a.dk) + base;
+    for (int e = tid; e < 16 * (DH / 4); e += 256) {
+      const int ki = e / (DH / 4), d = 4 * (e % (DH / 4));
+      if (k0 + ki >= a.Skv) continue;
+      const f32x4 x = ((*(const f32x4*)&red[0][ki][d] + *(const f32x4*)&red[1][ki][d]) + *(const f32x4*)&red[2][ki][d]) +
+                      *(const f32x4*)&red[3][ki][d];
+      *(f32x4*)(out + (int64_t)(k0 + ki) * (which ? a.v_st : a.k_st) + d) = x * (which ? 1.0f : a.scale);
+    }
+  }
+}
+
+template <int DH>
+static hipError_t fwd_f32(const WinArgs& a, hipStream_t s) {
+  const unsigned nblk = (unsigned)(((int64_t)a.Sq * a.G + 15) / 16);
+  hipLaunchKernelGGL(win_fwd_f32_kernel<DH>, dim3(nblk * a.nsplit, a.Hkv, a.B), dim3(256), 0, s, a);
+  return hipGetLastError();
+}
+template <int DH>
+static hipError_t dkdv_f32(const WinArgs& a, hipStream_t s) {
+  hipLaunchKernelGGL(win_dkdv_f32_kernel<DH>, dim3((a.Skv + 15) / 16, a.Hkv, a.B), dim3(256), 0, s, a);
+  return hipGetLastError();
+}
+template <int DH>
+static hipError_t dq_f32(const WinArgs& a, hipStream_t s) {
+  const unsigned nblk = (unsigned)(((int64_t)a.Sq * a.G + 15) / 16);
+  hipLaunchKernelGGL(win_dq_f32_kernel<DH>, dim3(nblk, a.Hkv, a.B), dim3(256), 0, s, a);
+  return hipGetLastError();
+}
+hipError_t win_fwd_f32(const WinArgs& a, hipStream_t s) { return a.dh == 64 ? fwd_f32<64>(a, s) : fwd_f32<128>(a, s); }
+hipError_t win_dkdv_f32(const WinArgs& a, hipStream_t s) { return a.dh == 64 ? dkdv_f32<64>(a, s) : dkdv_f32<128>(a, s); }
+hipError_t win_dq_f32(const WinArgs& a, hipStream_t s) { return a.dh == 64 ? dq_f32<64>(a, s) : dq_f32<128>(a, s); }
+
+hipError_t win_join(Dt t, const WinArgs& a, hipStream_t s) {
+  const int64_t all = (int64_t)a.B * a.Hq * a.Sq;
+  auto k = t == BF16 ? win_join_kernel<bf16> : win_join_kernel<float>;
+  hipLaunchKernelGGL(k, dim3((unsigned)((all + 3) / 4)), dim3(256), 0, s, a);
+  return hipGetLastError();
+}
+hipError_t win_delta(Dt t, const WinArgs& a, hipStream_t s) {
+  const int64_t n = (int64_t)a.B * a.Hq * a.Sqp * (a.dh / 8);
+  auto k = t == BF16 ? (a.dh == 64 ? win_delta_kernel<bf16, 64> : win_delta_kernel<bf16, 128>)
+                     : (a.dh == 64 ? win_delta_kernel<float, 64> : win_delta_kernel<float, 128>);
+  hipLaunchKernelGGL(k, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, s, a);
+  return hipGetLastError();
+}
+
+}  // namespace bpt

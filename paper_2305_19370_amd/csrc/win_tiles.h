@@ -1,0 +1,128 @@
+// What the bf16 kernels of attention with a window and sinks share: the rows of a wave, copies of
+// tiles whose invisible rows are not read, the LDS ring's loop and the store of a transposed result.
+#pragma once
+
+#include "win_attn.h"
+
+namespace bpt {
+
+// NW waves of 32 rows (keys, in the dK dV kernel) share tiles of 64 rows of two tensors in a ring
+template <int DH, int NWAVES>
+struct WinCfg {
+  static constexpr int KSTEPS = DH / 16, DT = DH / 32;
+  static constexpr int NW = NWAVES, ROWS = 32 * NW;
+  static constexpr int TB = RmTile<DH>::BYTES, STAGE = 2 * TB;
+  static constexpr int NS = NW == 8 || DH == 64 ? 4 : 2;   // stages in the ring
+  static constexpr int LDS = NS * STAGE;
+  static constexpr int DPS = Ring2<DH, NW>::DPW;    // copies per wave per stage
+};
+
+// Row r0 + w0 + lane % 32 of a kv head's list r = token * G + head, what it sees, and what its wave and its
+// workgroup of n rows (from r0) see.
+struct Rows {
+  int i, head;                 // token, query head in its group
+  bool full;                   // all the wave's rows exist
+  Vis mine, first, last, run;  // the row; the wave's first and last row that exist; the workgroup
+  BPT_DEV Rows(const WinArgs& a, const Seq& s, int r0, int w0, int n, int lane) {
+    const int r = r0 + w0 + (lane & 31);
+    i = r / a.G;
+    head = r - i * a.G;
+    const int last_i = s.nq - 1;
+    mine = first = last = run = Vis{0, -1, 0};
+    if (i <= last_i) mine = vis_of(a, s, s.off + i, s.off + i);
+    const int i0 = r0 / a.G, i1 = min((r0 + n - 1) / a.G, last_i);
+    if (i0 <= i1) run = vis_run(a, s, s.off + i0, s.off + i1);
+    const int wi0 = (r0 + w0) / a.G, wi1 = (r0 + w0 + 31) / a.G;
+    full = wi1 <= last_i;
+    if (wi0 <= last_i) {
+      first = vis_of(a, s, s.off + wi0, s.off + wi0);
+      const int e = s.off + min(wi1, last_i);
+      last = vis_of(a, s, e, e);
+    }
+  }
+  // a row that exists, for rows that do not
+  BPT_DEV int safe(const Seq& s) const { return min(i, s.nq - 1); }
+  // whether all the wave's rows see all of keys k0 .. k0 + 63, or none sees any
+  BPT_DEV bool all(int k0) const { return full && ((k0 >= last.lo && k0 + 63 <= first.hi) || k0 + 63 < first.se); }
+  BPT_DEV bool none(int k0) const { return !(k0 <= last.hi && k0 + 63 >= first.lo) && k0 >= last.se; }
+  // scores t[mt][r] of keys k0 + 32 mt + acc_row(r, lane)
+  template <typename V>
+  BPT_DEV void mask(V (&t)[2], int k0, int lane, float out) const {
+    const int base = k0 + 4 * (lane >> 5);
+    const int lo = mine.lo - base, hi = mine.hi - base, se = mine.se - base;
+#pragma unroll
+    for (int mt = 0; mt < 2; ++mt)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const int k = 32 * mt + 8 * (r >> 2) + (r & 3);
+        t[mt][r] = (k >= lo && k <= hi) || k < se ? t[mt][r] : out;
+      }
+  }
+};
+
+// ring_issue for rows row0 .. row0 + 63 of two tensors where only rows that `pick` returns may be
+// read: pick(row) is a row of the tile itself.
+template <int DH, int NW, class Pick>
+BPT_DEV void issue_picked(char* stage, const bf16* src0, int ld0, const bf16* src1, int ld1, int row0, int wave, int lane,
+                          const Pick& pick) {
+  using T = RmTile<DH>;
+  const bf16* org0 = src0 + (int64_t)row0 * ld0;
+  const bf16* org1 = src1 + (int64_t)row0 * ld1;
+  asm volatile("" : "+v"(lane));                    // recomputed at every call, as in ring_issue
+#pragma unroll
+  for (int i = 0; i < Ring2<DH, NW>::DPW; ++i) {
+    const int b = ring_block<DH, NW>(wave, i), t = b >= T::BLOCKS, blk = b - t * T::BLOCKS;
+    const int slot = blk * 64 + lane, col = slot % T::SLOTS, row = pick(row0 + slot / T::SLOTS) - row0;
+    const uint32_t off = 2u * (uint32_t)(row * (t ? ld1 : ld0) + (col < DH / 8 ? col : 0) * 8);
+    dma16s(scalar_ptr(t ? org1 : org0), off, stage + t * T::BYTES + blk * 1024);
+  }
+}
+
+// K and V of keys k0 .. k0 + 63, a tile that holds a key which v's run of rows sees; a key that none of
+// them sees is replaced by one of the tile that is.
+template <int DH, int NW>
+BPT_DEV void issue_keys(char* stage, const bf16* K, int ldk, const bf16* V, int ldv, int k0, const Vis& v,
+                        const RingOff<DH, NW>& roff, int wave, int lane) {
+  if ((k0 >= v.lo && k0 + 63 <= v.hi) || k0 + 63 < v.se) {
+    ring_issue_full<DH, NW>(stage, K, ldk, k0, V, ldv, k0, roff, wave);
+    return;
+  }
+  const int lo = max(v.lo, k0), hi = min(v.hi, k0 + 63);
+  const int se = min(v.se, k0 + 64);
+  issue_picked<DH, NW>(stage, K, ldk, V, ldv, k0, wave, lane,
+                       [&](int k) { return k < se ? k : lo <= hi ? min(max(k, lo), hi) : se - 1; });
+}
+
+// Walks n stages of the ring (C::NS slots, DPS copies per wave and stage): body(j) runs with stage j in
+// LDS. Every wave of the workgroup reaches every barrier.
+template <class C, int DPS, class Issue, class Body>
+BPT_DEV void ring_loop(int n, const Issue& issue, const Body& body) {
+#pragma unroll
+  for (int st = 0; st < C::NS - 1; ++st)
+    if (st < n) issue(st);
+  for (int j = 0; j < n; ++j) {
+    // stage j has landed once at most the stages issued after it are pending
+    if (C::NS == 4 && j + 2 < n) wait_vmcnt<2 * DPS>();
+    else if (C::NS == 4 && j + 1 < n) wait_vmcnt<DPS>();
+    else wait_vmcnt<0>();
+    __syncthreads();                                // stage j visible; every wave is done with stage j - 1
+    if (j + C::NS - 1 < n) issue(j + C::NS - 1);    // into the slot of stage j - 1
+    body(j);
+  }
+}
+
+// A transposed result (features x 32 rows) times f: 4 consecutive features per store at p, the lane's row
+template <int DH>
+BPT_DEV void store_rows(bf16* p, const f32x16 (&acc)[DH / 32], float f, int lane) {
+#pragma unroll
+  for (int t = 0; t < DH / 32; ++t)
+#pragma unroll
+    for (int rg = 0; rg < 4; ++rg) {
+      bf16x4 v;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] = (bf16)(acc[t][4 * rg + e] * f);
+      *(bf16x4*)(p + 32 * t + 8 * rg + 4 * (lane >> 5)) = v;
+    }
+}
+
+}  // namespace bpt

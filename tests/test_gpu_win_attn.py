@@ -1,0 +1,298 @@
+"""Attention with a sliding window and sinks on the GPU against its formula in float64: every element of
+O, lse, dQ, dK and dV within a bound derived from the roundings the kernels make."""
+import math
+
+import pytest
+import torch
+
+from gpu_util import say
+from long_context_ref import attention, check
+from paper_2305_19370_amd import bpt
+
+pytestmark = pytest.mark.gpu
+DT = {"bf16": torch.bfloat16, "f32": torch.float32}
+
+
+def make(B, Sq, Skv, Hq, Hkv, dh, dtype, seed=0, layout="token"):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    rn = lambda *s: torch.randn(s, generator=g, device="cuda").to(DT[dtype])  # noqa: E731
+    if layout == "packed":                           # q, k, v columns of one projection
+        assert Sq == Skv
+        x = rn(B, Sq, Hq + 2 * Hkv, dh)
+        q, k, v = x[:, :, :Hq], x[:, :, Hq:Hq + Hkv], x[:, :, Hq + Hkv:]
+    elif layout == "heads":
+        q, k, v = (rn(B, h, s, dh).permute(0, 2, 1, 3) for h, s in ((Hq, Sq), (Hkv, Skv), (Hkv, Skv)))
+    else:
+        q, k, v = rn(B, Sq, Hq, dh), rn(B, Skv, Hkv, dh), rn(B, Skv, Hkv, dh)
+    return q, k, v, rn(B, Sq, Hq, dh)
+
+
+def like(t):
+    """A tensor of t's strides filled with NaN, and the buffer it lies in."""
+    n = sum((s - 1) * st for s, st in zip(t.shape, t.stride())) + 1
+    buf = torch.full((n,), math.nan, dtype=t.dtype, device=t.device)
+    return buf.as_strided(t.shape, t.stride()), buf
+
+
+def run(q, k, v, do, q_lens=None, kv_lens=None, **kw):
+    o = torch.full(q.shape, math.nan, dtype=q.dtype, device="cuda")
+    lse = torch.full((q.shape[0], q.shape[2], q.shape[1]), math.nan, device="cuda")
+    cfg = bpt.attn_config_of(q, k, v, o, **kw)
+    bpt._check(bpt.attn_validate(cfg))
+    ws = torch.full((max(bpt.attn_workspace_bytes(cfg, False), bpt.attn_workspace_bytes(cfg, True)),), 255, dtype=torch.uint8,
+                    device="cuda")
+    ql, kl = (None if t is None else torch.tensor(t, dtype=torch.int32, device="cuda") for t in (q_lens, kv_lens))
+    bpt.attn_fwd(cfg, q, k, v, o, lse, ws, ql, kl)
+    out = {"O": o, "lse": lse}
+    if do is not None:
+        ws.fill_(255)
+        (dq, bq), (dk, bk), (dv, bv) = like(q), like(k), like(v)
+        bpt.attn_bwd(cfg, q, k, v, o, lse, do, dq, dk, dv, ws, ql, kl)
+        out.update(dQ=dq, dK=dk, dV=dv)
+        for t, buf in ((dq, bq), (dk, bk), (dv, bv)):      # nothing between the rows is written
+            assert int(torch.isnan(buf.float()).sum()) == buf.numel() - t.numel()
+    torch.cuda.synchronize()
+    return out
+
+
+SHAPES = [
+    # B, Sq, Skv, Hq, Hkv, causal, window, sinks
+    (1, 1, 1, 1, 1, True, 0, 0),
+    (1, 2, 2, 2, 1, True, 1, 0),
+    (2, 63, 63, 2, 2, True, 0, 0),
+    (1, 65, 65, 3, 1, True, 7, 2),
+    (1, 300, 300, 4, 4, True, 64, 4),
+    (2, 517, 517, 4, 2, True, 100, 70),
+    (1, 700, 700, 8, 1, True, 256, 1),
+    (1, 1100, 1100, 5, 1, True, 129, 130),
+    (1, 400, 400, 2, 2, False, 0, 0),
+    (1, 400, 400, 2, 2, False, 33, 5),
+    (1, 333, 333, 4, 2, False, 20, 100),
+    (2, 100, 900, 4, 2, True, 0, 0),                # a piece of a prompt
+    (1, 77, 1500, 2, 2, True, 200, 3),
+    (1, 130, 50, 2, 1, True, 0, 0),                 # more queries than keys: 80 rows see nothing
+    (1, 130, 50, 2, 1, True, 9, 2),
+    (1, 130, 50, 2, 1, False, 9, 2),
+    (1, 2100, 2100, 2, 2, True, 300, 4),
+    (1, 260, 260, 2, 2, True, 5000, 4),             # a window longer than the sequence
+    (1, 260, 260, 2, 2, True, 16, 1000),            # more sinks than keys
+]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("dh", [64, 128])
+@pytest.mark.parametrize("shape", SHAPES, ids=lambda s: "-".join(str(int(x)) for x in s))
+def test_forward_and_backward(shape, dh, dtype):
+    B, Sq, Skv, Hq, Hkv, causal, window, sinks = shape
+    say(f"case attn {shape} dh {dh} {dtype}")
+    q, k, v, do = make(B, Sq, Skv, Hq, Hkv, dh, dtype, seed=Sq)
+    kw = dict(causal=causal, window=window, sinks=sinks)
+    got = run(q, k, v, do, **kw)
+    ref, err = attention(q, k, v, do, **kw)
+    for n in ref:
+        check(got[n], ref[n], err[n], n)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("layout", ["packed", "heads"])
+def test_layouts(layout, dtype):
+    q, k, v, do = make(2, 330, 330, 6, 2, 64, dtype, seed=5, layout=layout)
+    kw = dict(causal=True, window=90, sinks=3)
+    got = run(q, k, v, do, **kw)
+    ref, err = attention(q, k, v, do, **kw)
+    for n in ref:
+        check(got[n], ref[n], err[n], n)
+
+
+LENS = [
+    # B, Sq, Skv, q_lens, kv_lens, window, sinks, causal
+    (4, 200, 200, [200, 131, 1, 0], [200, 131, 1, 0], 50, 3, True),
+    (3, 40, 500, [40, 17, 0], [500, 64, 77], 0, 0, True),
+    (3, 40, 500, [40, 40, 3], [20, 0, 500], 30, 2, True),      # fewer keys than queries, no keys
+    (2, 70, 300, [70, 9], [299, 65], 33, 4, False),
+]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("case", LENS, ids=str)
+def test_lengths_and_garbage_behind_them(case, dtype):
+    """Lengths per sequence; what lies behind them (NaN, infinity) changes nothing and rows that see
+    nothing give zeros and -inf."""
+    B, Sq, Skv, ql, kl, window, sinks, causal = case
+    q, k, v, do = make(B, Sq, Skv, 4, 2, 128, dtype, seed=9)
+    for b in range(B):
+        q[b, ql[b]:], do[b, ql[b]:] = math.nan, math.inf
+        k[b, kl[b]:], v[b, kl[b]:] = math.inf, math.nan
+    kw = dict(causal=causal, window=window, sinks=sinks)
+    got = run(q, k, v, do, q_lens=ql, kv_lens=kl, **kw)
+    ref, err = attention(q, k, v, do, q_lens=ql, kv_lens=kl, **kw)
+    for n in ref:
+        check(got[n], ref[n], err[n], n)
+
+
+def test_lengths_are_clamped():
+    q, k, v, do = make(2, 50, 80, 2, 2, 64, "bf16")
+    a = run(q, k, v, do, q_lens=[999, -5], kv_lens=[2 ** 30, 80], window=20, sinks=2)
+    b = run(q, k, v, do, q_lens=[50, 0], kv_lens=[80, 80], window=20, sinks=2)
+    assert all(torch.equal(a[n], b[n]) for n in a)
+
+
+TOKENS = [
+    # B, Sq, L, Hq, Hkv, window, sinks
+    (1, 1, 1, 4, 4, 0, 0), (1, 1, 70, 8, 1, 0, 0), (3, 1, 1000, 4, 2, 0, 0), (2, 1, 5000, 8, 8, 512, 4),
+    (2, 3, 3001, 16, 2, 0, 0), (1, 5, 9000, 10, 2, 1000, 70), (1, 1, 20000, 32, 1, 0, 0), (1, 7, 64, 3, 3, 0, 0),
+    (40, 1, 600, 4, 1, 100, 1),
+]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("dh", [64, 128])
+@pytest.mark.parametrize("case", TOKENS, ids=str)
+def test_new_tokens_against_a_cache(case, dh, dtype):
+    """Few queries at the end of caches of unequal length, keys outside the window NaN (given up by a
+    rolling cache): forward, in slices of the keys where it is cut."""
+    B, Sq, L, Hq, Hkv, window, sinks = case
+    say(f"case tokens {case} dh {dh} {dtype}")
+    q, k, v, _ = make(B, Sq, L, Hq, Hkv, dh, dtype, seed=L, layout="heads")
+    lens = [L - (b * L) // B for b in range(B)]
+    if B > 2:
+        lens[1] = 0
+    for b in range(B):
+        k[b, lens[b]:], v[b, lens[b]:] = math.nan, math.nan
+        gone = max(lens[b] - Sq - window + 1, 0) if window else 0
+        if gone > sinks:
+            k[b, sinks:gone], v[b, sinks:gone] = math.nan, math.inf
+    kw = dict(causal=True, window=window, sinks=sinks)
+    got = run(q, k, v, None, kv_lens=lens, **kw)
+    ref, err = attention(q, k, v, None, kv_lens=lens, **kw)
+    for n in ref:
+        check(got[n], ref[n], err[n], n)
+
+
+def test_large_scores():
+    """Scores of hundreds, above and below zero, rising and falling along the keys: no weight overflows
+    and no row loses its sum."""
+    q, k, v, do = make(1, 300, 300, 2, 2, 64, "f32", seed=3)
+    ramp = torch.linspace(-40, 40, 300, device="cuda")[None, :, None, None]
+    for s in (1.0, -1.0):
+        kk = k * 0.05 + s * ramp
+        qq = q.abs()
+        for dt in (torch.float32, torch.bfloat16):
+            kw = dict(causal=True, window=90, sinks=2)
+            args = [t.to(dt) for t in (qq, kk, v, do)]
+            got = run(*args, **kw)
+            ref, err = attention(*args, **kw)
+            for n in ("O", "lse"):
+                check(got[n], ref[n], err[n], f"{n} {s} {dt}")
+
+
+def test_gradients_against_differences():
+    """Directional derivatives of sum(O dO) in float64 differences of the reference (which the other tests
+    hold the kernels to) against the kernel's gradients, fp32."""
+    q, k, v, do = make(1, 90, 90, 4, 2, 64, "f32", seed=11)
+    kw = dict(causal=True, window=21, sinks=2)
+    got = run(q, k, v, do, **kw)
+    g = torch.Generator(device="cuda").manual_seed(1)
+    f = lambda *t: float((attention(*t, **kw)[0]["O"] * do.double()).sum())  # noqa: E731
+    for n, i in (("dQ", 0), ("dK", 1), ("dV", 2)):
+        base = [q.double(), k.double(), v.double()]
+        d = torch.randn(base[i].shape, generator=g, device="cuda", dtype=torch.float64)
+        e = 1e-5
+        hi, lo = list(base), list(base)
+        hi[i], lo[i] = base[i] + e * d, base[i] - e * d
+        want = (f(*hi) - f(*lo)) / (2 * e)
+        have = float((got[n].double() * d).sum())
+        # third-order term of the difference ~ e^2, its rounding 1e-16 * |f| / e ~ 1e-8, fp32 gradients 1e-5
+        assert abs(have - want) <= 1e-4 * max(1.0, float(got[n].double().norm())), (n, have, want)
+
+
+def test_same_bits_on_another_stream_and_in_parts():
+    q, k, v, do = make(1, 700, 700, 8, 2, 128, "bf16", seed=2)
+    kw = dict(causal=True, window=130, sinks=4)
+    a = run(q, k, v, do, **kw)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        b = run(q, k, v, do, **kw)
+    torch.cuda.current_stream().wait_stream(s)
+    assert all(torch.equal(a[n], b[n]) for n in a)
+    # dQ alone, dK and dV alone
+    cfg = bpt.attn_config_of(q, k, v, a["O"], **kw)
+    ws = torch.empty(bpt.attn_workspace_bytes(cfg, True), dtype=torch.uint8, device="cuda")
+    dq, dk, dv = torch.empty_like(q), torch.empty_like(k), torch.empty_like(v)
+    bpt.attn_bwd(cfg, q, k, v, a["O"], a["lse"], do, dq, None, None, ws)
+    bpt.attn_bwd(cfg, q, k, v, a["O"], a["lse"], do, None, dk, dv, ws)
+    torch.cuda.synchronize()
+    assert torch.equal(dq, a["dQ"]) and torch.equal(dk, a["dK"]) and torch.equal(dv, a["dV"])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_replays_from_a_graph(dtype):
+    q, k, v, do = make(2, 500, 500, 4, 2, 64, dtype, seed=4)
+    lens = torch.tensor([500, 321], dtype=torch.int32, device="cuda")
+    o, lse = torch.empty_like(q), torch.empty(2, 4, 500, device="cuda")
+    tok, tlse = torch.empty_like(q[:, :1]), torch.empty(2, 4, 1, device="cuda")
+    dq, dk, dv = torch.empty_like(q), torch.empty_like(k), torch.empty_like(v)
+    cfg = bpt.attn_config_of(q, k, v, o, window=100, sinks=4)
+    one = bpt.attn_config_of(q[:, -1:], k, v, tok)
+    n = max(bpt.attn_workspace_bytes(c, b) for c in (cfg, one) for b in (False, True))
+    ws = torch.empty(n, dtype=torch.uint8, device="cuda")
+
+    def step():
+        bpt.attn_fwd(cfg, q, k, v, o, lse, ws, lens, lens)
+        bpt.attn_bwd(cfg, q, k, v, o, lse, do, dq, dk, dv, ws, lens, lens)
+        bpt.attn_fwd(one, q[:, -1:], k, v, tok, tlse, ws, None, lens)
+
+    outs = (o, lse, dq, dk, dv, tok, tlse)
+    step()
+    torch.cuda.synchronize()
+    ref = [t.clone() for t in outs]
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        step()
+    for r in range(3):
+        for t in outs:
+            t.fill_(math.nan)
+        ws.fill_(255)
+        (torch.randn(4096, device="cuda") * 2).sum().item()
+        torch.cuda.synchronize()
+        g.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(outs, ref)), r
+    # lengths are read on the GPU: the same graph for other lengths
+    lens.copy_(torch.tensor([3, 500], dtype=torch.int32))
+    g.replay()
+    torch.cuda.synchronize()
+    again = [t.clone() for t in outs]
+    step()
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(outs, again))
+
+
+def test_window_attention_class():
+    q, k, v, do = make(1, 200, 200, 4, 2, 64, "bf16", seed=6, layout="packed")
+    att = bpt.WindowAttention(window=50, sinks=2)
+    o, lse = att.forward(q, k, v)
+    dq, dk, dv = att.backward(q, k, v, o, lse, do)
+    ref = run(q, k, v, do, window=50, sinks=2)
+    torch.cuda.synchronize()
+    for n, t in (("O", o), ("lse", lse), ("dQ", dq), ("dK", dk), ("dV", dv)):
+        assert torch.equal(t, ref[n]), n
+
+
+def test_cache_past_32_bit_offsets():
+    """A token against the last sequence of a cache whose elements pass 2^31 (4.3 GB)."""
+    L, Hkv, dh = 131072, 8, 128
+    k = torch.zeros(18, L, Hkv, dh, dtype=torch.bfloat16, device="cuda")
+    v = torch.zeros_like(k)
+    g = torch.Generator(device="cuda").manual_seed(1)
+    n = 300
+    k[17, :n] = torch.randn(n, Hkv, dh, generator=g, device="cuda").bfloat16()
+    v[17, :n] = torch.randn(n, Hkv, dh, generator=g, device="cuda").bfloat16()
+    assert k.numel() > 2 ** 31
+    q = torch.randn(18, 1, 16, dh, generator=g, device="cuda").bfloat16()
+    lens = [0] * 17 + [n]
+    got = run(q, k, v, None, kv_lens=lens)
+    ref, err = attention(q[17:], k[17:, :n], v[17:, :n], None)
+    check(got["O"][17:], ref["O"], err["O"], "O")
+    assert not bool(got["O"][:17].any()) and bool((got["lse"][:17] == -math.inf).all())
