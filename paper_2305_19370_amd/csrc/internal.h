@@ -139,17 +139,23 @@ struct WinArgs {
   int B = 0, Sq = 0, Skv = 0, Hq = 0, Hkv = 0, G = 1, dh = 0;   // G = Hq / Hkv
   int causal = 0, window = 0, sinks = 0;   // window 0: none
   float scale = 1.0f;                   // of the scores
-  int nsplit = 1;                       // slices of the keys (forward of few rows)
+  int few = 0;                          // bf16 forward: the kernel for few rows
+  int nsplit = 1;                       // slices of the keys (fp32, or few)
   float *part_o = nullptr, *part_ml = nullptr;   // nsplit > 1: [nsplit, B Hkv Sq G] rows of dh, of (max, sum)
   int64_t Sqp = 0;                      // Sq rounded up to 64
-  float *ndelta = nullptr, *nlse2 = nullptr;     // [B, Hq, Sqp]: -rowsum(dO O), -lse log2(e)
+  float *ndelta = nullptr, *nlse = nullptr;      // [B, Hq, Sqp]: -rowsum(dO O), -lse / scale
+  int far = 0;                          // chunks of what sinks see beyond their window; 0: not apart
+  float* part_s = nullptr;              // far > 0: their sums, [slots, B, Hkv, min(sinks, Skv), 2, dh]
 };
 hipError_t win_fwd_bf16(const WinArgs& a, hipStream_t s);
 hipError_t win_fwd_f32(const WinArgs& a, hipStream_t s);
 hipError_t win_join(Dt t, const WinArgs& a, hipStream_t s);    // joins the slices of a forward
-hipError_t win_delta(Dt t, const WinArgs& a, hipStream_t s);   // ndelta, nlse2
+hipError_t win_delta(Dt t, const WinArgs& a, hipStream_t s);   // ndelta, nlse
 hipError_t win_dkdv_bf16(const WinArgs& a, hipStream_t s);
 hipError_t win_dkdv_f32(const WinArgs& a, hipStream_t s);
+hipError_t win_far_bf16(const WinArgs& a, hipStream_t s);      // 2 far slots
+hipError_t win_far_f32(const WinArgs& a, hipStream_t s);       // far slots
+hipError_t win_sinks(Dt t, const WinArgs& a, int slots, hipStream_t s);   // adds the slots up
 hipError_t win_dq_bf16(const WinArgs& a, hipStream_t s);
 hipError_t win_dq_f32(const WinArgs& a, hipStream_t s);
 

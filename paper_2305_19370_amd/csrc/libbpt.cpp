@@ -1311,17 +1311,36 @@ static bpt_status attn_check(const bpt_attn_config* c) {
   return BPT_OK;
 }
 
-// Slices of the keys for a forward of few rows
-static int attn_nsplit(const bpt_attn_config& c) {
-  if (c.dtype == BPT_BF16) return 1;
-  const int64_t rows = c.Sq * (c.Hq / c.Hkv), groups = (rows + 15) / 16 * c.Hkv * c.B;
-  const int64_t span = c.window ? std::min(c.Skv, c.window + c.sinks + c.Sq) : c.Skv;
-  return (int)std::max<int64_t>(1, std::min<int64_t>({512 / groups, span / 512, 64}));
+// A bf16 forward whose blocks of 128 rows would leave most CUs idle takes the kernel for few rows.
+static bool attn_few(const bpt_attn_config& c) {
+  const int64_t rows = c.Sq * (c.Hq / c.Hkv);
+  return c.dtype == BPT_BF16 && (rows <= 32 || (rows + 127) / 128 * c.Hkv * c.B <= 64);
 }
+// Slices of the keys for a forward of few rows: enough workgroups for the chip, and 128 keys (bf16: a tile per wave) at
+// least for each.
+static int attn_nsplit(const bpt_attn_config& c) {
+  const bool bf = c.dtype == BPT_BF16;
+  if (bf && !attn_few(c)) return 1;
+  const int64_t rows = c.Sq * (c.Hq / c.Hkv), groups = (rows + (bf ? 31 : 15)) / (bf ? 32 : 16) * c.Hkv * c.B;
+  const int64_t span = c.window ? std::min(c.Skv, (c.causal ? 1 : 2) * c.window + c.sinks + c.Sq) : c.Skv;
+  return (int)std::max<int64_t>(1, std::min<int64_t>({1024 / groups, span / (bf ? 128 : 512), 64}));
+}
+
+// Chunks of what the sinks' keys see beyond their window in the backward: 0 where a block of keys that
+// holds sinks has little more to do than another, else workgroups for two a CU and at least two tiles
+// of 64 queries for each.
+static int attn_far(const bpt_attn_config& c) {
+  if (c.sinks == 0 || c.window >= c.Skv) return 0;
+  const int64_t G = c.Hq / c.Hkv, tiles = (c.Sq - std::min(c.Sq, c.window) + 63) / 64 * G;
+  if (tiles < 16) return 0;
+  const int64_t groups = c.B * c.Hkv * ((std::min(c.sinks, c.Skv) + 31) / 32);
+  return (int)std::max<int64_t>(1, std::min(512 / groups, tiles / 2));
+}
+static int attn_slots(const bpt_attn_config& c) { return 1 + attn_far(c) * (c.dtype == BPT_BF16 ? 2 : 1); }
 
 struct AttnWs {
   float *part_o, *part_ml;     // forward: slices
-  float *ndelta, *nlse2;       // backward
+  float *ndelta, *nlse, *part_s;   // backward
 };
 static AttnWs attn_ws(const bpt_attn_config& c, void* base, int backward, int64_t* total) {
   Bump bp(base);
@@ -1329,7 +1348,8 @@ static AttnWs attn_ws(const bpt_attn_config& c, void* base, int backward, int64_
   if (backward) {
     const int64_t n = c.B * c.Hq * rup(c.Sq, 64) * 4;
     w.ndelta = (float*)bp.take(n);
-    w.nlse2 = (float*)bp.take(n);
+    w.nlse = (float*)bp.take(n);
+    if (attn_far(c)) w.part_s = (float*)bp.take(attn_slots(c) * c.B * c.Hkv * std::min(c.sinks, c.Skv) * 2 * c.dh * 4);
   } else if (const int z = attn_nsplit(c); z > 1) {
     w.part_o = (float*)bp.take(z * c.B * c.Hq * c.Sq * c.dh * 4);
     w.part_ml = (float*)bp.take(z * c.B * c.Hq * c.Sq * 8);
@@ -1383,6 +1403,7 @@ bpt_status bpt_attn_fwd(const bpt_attn_config* cfg, const void* Q, const void* K
   if (need > 0 && (!ws || (int64_t)ws_bytes < need))
     return fail(BPT_ERR_WORKSPACE, "workspace %zu bytes < required %lld", ws ? ws_bytes : (size_t)0, (long long)need);
   WinArgs a = attn_args(*cfg, Q, K, V, q_lens, kv_lens, O, lse);
+  a.few = attn_few(*cfg);
   a.nsplit = attn_nsplit(*cfg);
   a.part_o = w.part_o; a.part_ml = w.part_ml;
   hipStream_t s = (hipStream_t)stream;
@@ -1422,12 +1443,19 @@ bpt_status bpt_attn_bwd(const bpt_attn_config* cfg, const void* Q, const void* K
   if ((int64_t)ws_bytes < need) return fail(BPT_ERR_WORKSPACE, "workspace %zu bytes < required %lld", ws_bytes, (long long)need);
   WinArgs a = attn_args(*cfg, Q, K, V, q_lens, kv_lens, O, lse);
   a.dout = dO; a.dq = dQ; a.dk = dK; a.dv = dV;
-  a.ndelta = w.ndelta; a.nlse2 = w.nlse2;
+  a.ndelta = w.ndelta; a.nlse = w.nlse;
+  a.far = dK ? attn_far(*cfg) : 0;
+  a.part_s = w.part_s;
   hipStream_t s = (hipStream_t)stream;
   const bool bf = cfg->dtype == BPT_BF16;
   const double E_ = bf ? 2 : 4, seen = attn_seen(*cfg), q = (double)cfg->B * cfg->Hq * cfg->Sq * cfg->dh, kv = (double)cfg->B * cfg->Hkv * cfg->Skv * cfg->dh;
   RUN("win.delta", 0, 2.0 * q * E_, win_delta(dt_of(cfg->dtype), a, s));
   if (dK) RUN("win.dkdv", 8.0 * cfg->dh * seen, (2.0 * q + 4.0 * kv) * E_, bf ? win_dkdv_bf16(a, s) : win_dkdv_f32(a, s));
+  if (a.far > 0) {
+    RUN("win.far", 8.0 * cfg->dh * cfg->B * cfg->Hq * cfg->Sq * std::min(cfg->sinks, cfg->Skv), 2.0 * q * E_, bf ? win_far_bf16(a, s) : win_far_f32(a, s));
+    RUN("win.sinks", 0, (double)attn_slots(*cfg) * cfg->B * cfg->Hkv * std::min(cfg->sinks, cfg->Skv) * cfg->dh * 8,
+        win_sinks(dt_of(cfg->dtype), a, attn_slots(*cfg), s));
+  }
   if (dQ) RUN("win.dq", 6.0 * cfg->dh * seen, (3.0 * q + 2.0 * kv) * E_, bf ? win_dq_bf16(a, s) : win_dq_f32(a, s));
   return BPT_OK;
 }

@@ -1,5 +1,7 @@
 // Attention with a sliding window and sinks, bf16 backward: dQ (rows outside, key tiles inside) and dK, dV
 // (keys outside, query tiles of all the kv head's query heads inside).
+#include <algorithm>
+
 #include "win_tiles.h"
 
 namespace bpt {
@@ -42,31 +44,33 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 1 : 2) void win_dq_bf16_kernel(W
       }
     }
     const int64_t sidx = ((int64_t)b * a.Hq + h) * a.Sqp + i;
-    const float nl = a.nlse2[sidx], ndl = a.ndelta[sidx];
+    const float nl = a.nlse[sidx], ndl = a.ndelta[sidx];
     settle(nl);
     settle(ndl);
     const RingOff<DH, NW> roff = ring_offsets<DH, NW>(a.k_st, a.v_st, wave, lane);
     auto issue = [&](int j) {
       issue_keys<DH, NW>(smem + (j % C::NS) * C::STAGE, Kb, a.k_st, Vb, a.v_st, tiles.key0(j), w.run, roff, wave, lane);
     };
-    auto tile = [&](int j) {
-      const int k0 = tiles.key0(j);
+    auto tile = [&](int j, int k0, bool all) {
       const char* kt = smem + (j % C::NS) * C::STAGE;
       const char* vt = kt + C::TB;
-      f32x16 s[2] = {f32x16{}, f32x16{}}, dp[2];
+      f32x16 s[2], dp[2];
 #pragma unroll
       for (int mt = 0; mt < 2; ++mt) {
 #pragma unroll
-        for (int r = 0; r < 16; ++r) dp[mt][r] = ndl;  // the MFMAs leave dP^T - Delta
+        for (int r = 0; r < 16; ++r) {
+          s[mt][r] = nl;                               // the MFMAs leave (score - lse) / scale
+          dp[mt][r] = ndl;                             // and dP^T - Delta
+        }
 #pragma unroll
         for (int kk = 0; kk < C::KSTEPS; ++kk) {
           s[mt] = mfma32x32x16(frag_rows<DH>(kt, 32 * mt, 2 * kk, lane), qf[kk], s[mt]);
           dp[mt] = mfma32x32x16(frag_rows<DH>(vt, 32 * mt, 2 * kk, lane), dof[kk], dp[mt]);
         }
 #pragma unroll
-        for (int r = 0; r < 16; ++r) s[mt][r] = fast_exp2(fmaf(s[mt][r], c, nl)) * dp[mt][r];
+        for (int r = 0; r < 16; ++r) s[mt][r] = fast_exp2(s[mt][r] * c) * dp[mt][r];
       }
-      if (!w.all(k0)) w.mask(s, k0, lane, 0.0f);
+      if (!all) w.mask(s, k0, lane, 0.0f);
 #pragma unroll
       for (int mt = 0; mt < 2; ++mt)
 #pragma unroll
@@ -78,29 +82,38 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 1 : 2) void win_dq_bf16_kernel(W
         }
     };
     ring_loop<C, C::DPS>(tiles.n, issue, [&](int j) {
-      if (!w.none(tiles.key0(j))) tile(j);
+      const int k0 = tiles.key0(j);
+      if (!w.none(k0)) tile(j, k0, w.all(k0));
     });
   }
   if (w.i < a.Sq)
     store_rows<DH>((bf16*)a.dq + (int64_t)b * a.q_sb + (int64_t)w.i * a.q_st + (int64_t)h * a.q_sh, acc, a.scale, lane);
 }
 
-// Ring of the dK dV kernel: tiles of 64 queries (Q, dO) and their -lse (base 2) and -Delta
-template <int DH, int NWAVES>
+// Ring of the dK dV kernel: tiles of 64 queries (Q, dO) and their -lse / scale and -Delta
+template <int DH, int KG, int QH>
 struct WinKvCfg {
   static constexpr int KSTEPS = DH / 16, DT = DH / 32;
-  static constexpr int NW = NWAVES, KEYS = 32 * NW;
+  static constexpr int NW = KG * QH, KEYS = 32 * KG;   // waves: KG groups of 32 keys x QH parts of a tile's queries
   static constexpr int TB = RmTile<DH>::BYTES, STAGE = 2 * TB + 2 * 64 * 4;
-  static constexpr int NS = NW == 8 || DH == 64 ? 4 : 2;
+  static constexpr int NS = NW == 8 ? 4 : 2;
   static constexpr int LDS = NS * STAGE;
   static constexpr int DPS = Ring2<DH, NW>::DPW + 2;
 };
 
-// NW waves of 32 keys of one kv head. S = Q K^T and dP = dO V^T have the key on the lane axis, so P and dS feed dV^T += dO^T P
+// KG groups of 32 keys of one kv head; QH = 2: two waves for each, with half the queries of a tile, their sums added at the
+// end. S = Q K^T and dP = dO V^T have the key on the lane axis, so P and dS feed dV^T += dO^T P
 // and dK^T += Q^T dS directly. The tiles of the kv head's query heads follow one another.
-template <int DH, int NW>
-__global__ __launch_bounds__(64 * NW, NW == 8 ? 1 : 2) void win_dkdv_bf16_kernel(WinArgs a) {
-  using C = WinKvCfg<DH, NW>;
+//
+// Sinks are seen by every query, a key inside by a window of them: one block of keys would take as long as
+// all others together. Where that matters (a.far), the blocks keep to the window, and what sinks see
+// beyond it is cut into a.far chunks of (query head, tile of 64 queries) for workgroups of their own (FAR: 32 sinks,
+// two waves, each half the queries of a tile). All leave the sinks' sums in fp32 slots, which win_sinks adds in order.
+template <int DH, int KG, int QH, bool FAR>
+__global__ __launch_bounds__(64 * KG * QH, KG * QH == 8 ? 1 : 2) void win_dkdv_bf16_kernel(WinArgs a) {
+  using C = WinKvCfg<DH, KG, QH>;
+  constexpr int NW = C::NW;
+  static_assert(!FAR || (KG == 1 && QH == 2), "two waves for the far part");
   extern __shared__ __attribute__((aligned(16))) char smem[];
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -108,28 +121,37 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 1 : 2) void win_dkdv_bf16_kernel
   xcd_map((int)blockIdx.x, a.Hkv * a.B, hh, blk);
   const int kvh = hh % a.Hkv, b = hh / a.Hkv;
   const Seq sq = seq_of(a, b);
-  const int k0 = blk * C::KEYS, kw = k0 + 32 * wave, key = kw + (lane & 31);
+  const int chunk = FAR ? blk % a.far : 0;
+  const int k0 = (FAR ? blk / a.far : blk) * C::KEYS, part = wave / KG, kw = k0 + 32 * (wave % KG), key = kw + (lane & 31);
   const float c = a.scale * LOG2E;
+  const bool near = FAR || a.far > 0;               // the window alone, or beyond it
 
   f32x16 adv[C::DT], adk[C::DT];
 #pragma unroll
   for (int t = 0; t < C::DT; ++t) adv[t] = adk[t] = f32x16{};
   QVis run{0, -1};
-  if (k0 < sq.nk) run = qvis_of(a, sq, k0, min(k0 + C::KEYS, sq.nk) - 1, false);
+  const int kend = FAR ? min(sq.nk, a.sinks) : sq.nk;   // keys from here on are none of this workgroup's
+  if (k0 < kend) {
+    run = qvis_of(a, sq, k0, min(k0 + C::KEYS, kend) - 1, near);
+    if (FAR) run = QVis{a.causal ? max(k0 + a.window - sq.off, 0) : 0, sq.nq - 1};
+  }
   const int t0 = run.lo / 64, nt = run.hi >= run.lo ? run.hi / 64 + 1 - t0 : 0;
-  if (nt > 0) {
-    QVis mine = qvis_of(a, sq, key, key, false), first{0, -1}, last{0, -1};
+  const int per = FAR ? (nt * a.G + a.far - 1) / a.far : nt * a.G;
+  const int j0 = chunk * per, n = min(per, nt * a.G - j0);
+  if (n > 0) {
+    QVis mine = qvis_of(a, sq, key, key, near), first{0, -1}, last{0, -1};
     if (key >= sq.nk) mine.hi = -1;
-    if (kw < sq.nk) first = qvis_of(a, sq, kw, kw, false);
-    const int kl = min(kw + 31, sq.nk - 1);
-    if (kw < sq.nk) last = qvis_of(a, sq, kl, kl, false);
+    const int kl = min(kw + 31, kend - 1);
+    if (kw < sq.nk) {
+      first = qvis_of(a, sq, kw, kw, near);
+      last = qvis_of(a, sq, kl, kl, near);
+    }
     // the queries that all of the wave's keys see: the first key behind the sinks has the lowest end
-    const int ks = kw < a.sinks && a.sinks <= kl ? a.sinks : kw;
-    const int all_lo = max(first.lo, last.lo), all_hi = kw < sq.nk ? min(qvis_of(a, sq, ks, ks, false).hi, last.hi) : -1;
-    const bool full = kw + 31 < sq.nk;
+    const int ks = !near && kw < a.sinks && a.sinks <= kl ? a.sinks : kw;
+    const int all_lo = max(first.lo, last.lo), all_hi = kw + 31 < sq.nk ? min(qvis_of(a, sq, ks, ks, near).hi, last.hi) : -1;
     bf16x8 kf[C::KSTEPS], vf[C::KSTEPS];
     {
-      const int64_t kr = min(key, sq.nk - 1);
+      const int64_t kr = min(key, kend - 1);
       const bf16* k = (const bf16*)a.k + (int64_t)b * a.k_sb + kr * a.k_st + (int64_t)kvh * a.k_sh;
       const bf16* v = (const bf16*)a.v + (int64_t)b * a.v_sb + kr * a.v_st + (int64_t)kvh * a.v_sh;
 #pragma unroll
@@ -140,82 +162,141 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 1 : 2) void win_dkdv_bf16_kernel
         settle(vf[kk]);
       }
     }
-    auto issue = [&](int it) {
-      const int h = kvh * a.G + it / nt, q0 = 64 * (t0 + it % nt);
-      char* st = smem + (it % C::NS) * C::STAGE;
+    auto issue = [&](int j) {
+      const int it = j0 + j, h = kvh * a.G + it / nt, q0 = 64 * (t0 + it % nt);
+      char* st = smem + (j % C::NS) * C::STAGE;
       issue_picked<DH, NW>(st, (const bf16*)a.q + (int64_t)b * a.q_sb + (int64_t)h * a.q_sh, a.q_st,
                            (const bf16*)a.dout + (int64_t)b * a.o_sb + (int64_t)h * a.o_sh, a.o_st, q0, wave, lane,
                            [&](int q) { return min(max(q, run.lo), run.hi); });
       const int64_t sidx = ((int64_t)b * a.Hq + h) * a.Sqp + q0;       // Sqp % 64 == 0: in bounds
-      dma4s(scalar_ptr(a.nlse2 + sidx), 4u * lane, st + 2 * C::TB);
+      dma4s(scalar_ptr(a.nlse + sidx), 4u * lane, st + 2 * C::TB);
       dma4s(scalar_ptr(a.ndelta + sidx), 4u * lane, st + 2 * C::TB + 256);
     };
-    auto tile = [&](int it, int q0) {
-      const char* qs = smem + (it % C::NS) * C::STAGE;
+    auto half = [&](int j, int q0, int mt, bool all) {
+      const char* qs = smem + (j % C::NS) * C::STAGE;
       const char* ds = qs + C::TB;
       const float* ls = (const float*)(qs + 2 * C::TB);
-      // a tile that all the wave's keys see in full needs no mask
-      const bool all = full && q0 >= all_lo && q0 + 63 <= all_hi;
-      const int lo = mine.lo - q0 - 4 * (lane >> 5), hi = mine.hi - q0 - 4 * (lane >> 5);
+      f32x16 s, dp;
 #pragma unroll
-      for (int mt = 0; mt < 2; ++mt) {
-        f32x16 s = {}, dp;
-        f32x4 l4[4];
+      for (int rg = 0; rg < 4; ++rg) {
+        const int qi = 32 * mt + 8 * rg + 4 * (lane >> 5);
+        const f32x4 l4 = *(const f32x4*)(ls + qi);
+        const f32x4 d4 = *(const f32x4*)(ls + 64 + qi);
 #pragma unroll
-        for (int rg = 0; rg < 4; ++rg) {
-          const int qi = 32 * mt + 8 * rg + 4 * (lane >> 5);
-          l4[rg] = *(const f32x4*)(ls + qi);
-          const f32x4 d4 = *(const f32x4*)(ls + 64 + qi);
-#pragma unroll
-          for (int e = 0; e < 4; ++e) dp[4 * rg + e] = d4[e];   // the MFMAs leave dP - Delta
+        for (int e = 0; e < 4; ++e) {
+          s[4 * rg + e] = l4[e];                     // the MFMAs leave (score - lse) / scale
+          dp[4 * rg + e] = d4[e];                    // and dP - Delta
         }
+      }
 #pragma unroll
-        for (int kk = 0; kk < C::KSTEPS; ++kk) {
-          s = mfma32x32x16(frag_rows<DH>(qs, 32 * mt, 2 * kk, lane), kf[kk], s);
-          dp = mfma32x32x16(frag_rows<DH>(ds, 32 * mt, 2 * kk, lane), vf[kk], dp);
+      for (int kk = 0; kk < C::KSTEPS; ++kk) {
+        s = mfma32x32x16(frag_rows<DH>(qs, 32 * mt, 2 * kk, lane), kf[kk], s);
+        dp = mfma32x32x16(frag_rows<DH>(ds, 32 * mt, 2 * kk, lane), vf[kk], dp);
+        __builtin_amdgcn_sched_barrier(0);           // bound the fragments read ahead
+      }
+      pin(dp);
+#pragma unroll
+      for (int r = 0; r < 16; ++r) s[r] = fast_exp2(s[r] * c);
+      if (!all) {
+        const int base = q0 + 32 * mt + 4 * (lane >> 5);
+        const int lo = mine.lo - base, hi = mine.hi - base, end = run.hi - base;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const int q = 8 * (r >> 2) + (r & 3);
+          const bool in = q >= lo && q <= hi;
+          const bool ok = !FAR ? in : q <= end && (a.causal ? q > hi : !in);
+          s[r] = ok ? s[r] : 0.0f;
         }
+      }
 #pragma unroll
-        for (int r = 0; r < 16; ++r) s[r] = fast_exp2(fmaf(s[r], c, l4[r >> 2][r & 3]));
-        if (!all) {
+      for (int r = 0; r < 16; ++r) dp[r] = s[r] * dp[r];                // dS
 #pragma unroll
-          for (int r = 0; r < 16; ++r) {
-            const int q = 32 * mt + 8 * (r >> 2) + (r & 3);
-            s[r] = q >= lo && q <= hi ? s[r] : 0.0f;
-          }
-        }
+      for (int hf = 0; hf < 2; ++hf) {
+        const bf16x8 pb = acc_to_b(s, hf), sb = acc_to_b(dp, hf);
 #pragma unroll
-        for (int r = 0; r < 16; ++r) dp[r] = s[r] * dp[r];       // dS: rows read are real ones, dP is finite
-#pragma unroll
-        for (int hf = 0; hf < 2; ++hf) {
-          const bf16x8 pb = acc_to_b(s, hf), sb = acc_to_b(dp, hf);
-#pragma unroll
-          for (int t = 0; t < C::DT; ++t) {
-            adv[t] = mfma32x32x16(frag_tr<DH>(ds, 32 * mt + 16 * hf, 32 * t, lane), pb, adv[t]);
-            adk[t] = mfma32x32x16(frag_tr<DH>(qs, 32 * mt + 16 * hf, 32 * t, lane), sb, adk[t]);
-          }
+        for (int t = 0; t < C::DT; ++t) {
+          adv[t] = mfma32x32x16(frag_tr<DH>(ds, 32 * mt + 16 * hf, 32 * t, lane), pb, adv[t]);
+          adk[t] = mfma32x32x16(frag_tr<DH>(qs, 32 * mt + 16 * hf, 32 * t, lane), sb, adk[t]);
+          __builtin_amdgcn_sched_barrier(0);
         }
       }
     };
-    ring_loop<C, C::DPS>(nt * a.G, issue, [&](int it) {
-      const int q0 = 64 * (t0 + it % nt);
-      if (q0 <= max(first.hi, last.hi) && q0 + 63 >= min(first.lo, last.lo) && kw < sq.nk) tile(it, q0);
+    ring_loop<C, C::DPS>(n, issue, [&](int j) {
+      const int q0 = 64 * (t0 + (j0 + j) % nt);
+      if constexpr (FAR) {
+        // columns of keys that are no sinks are never stored and need no mask
+        half(j, q0, part, a.causal && q0 > last.hi && q0 + 63 <= run.hi);
+      } else if (q0 <= max(first.hi, last.hi) && q0 + 63 >= min(first.lo, last.lo) && kw < sq.nk) {
+        const bool all = q0 >= all_lo && q0 + 63 <= all_hi;
+        if constexpr (QH == 2) {
+          half(j, q0, part, all);
+        } else {
+#pragma unroll
+          for (int mt = 0; mt < 2; ++mt) half(j, q0, mt, all);
+        }
+      }
     });
   }
-  if (key < a.Skv) {
+  if constexpr (!FAR && QH == 2) {                    // the second half's sums, a group's [lane][register] apart
+    __syncthreads();
+    float* red = (float*)smem + (wave % KG) * 32 * C::DT * 64 + lane;
+    if (part == 1) {
+#pragma unroll
+      for (int t = 0; t < C::DT; ++t)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          red[(32 * t + r) * 64] = adk[t][r];
+          red[(32 * t + 16 + r) * 64] = adv[t][r];
+        }
+    }
+    __syncthreads();
+    if (part == 1) return;
+#pragma unroll
+    for (int t = 0; t < C::DT; ++t)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        adk[t][r] += red[(32 * t + r) * 64];
+        adv[t][r] += red[(32 * t + 16 + r) * 64];
+      }
+  }
+  if (a.far > 0 && key < min(a.sinks, a.Skv)) {
+    // slot 0: the window's part, then 2 per chunk; [slot, B Hkv, sinks, dK and dV, dh]
+    const int ns = min(a.sinks, a.Skv);
+    const int64_t slot = FAR ? 1 + 2 * chunk + part : 0;
+    float* p = a.part_s + ((slot * a.B * a.Hkv + (int64_t)b * a.Hkv + kvh) * ns + key) * 2 * DH;
+#pragma unroll
+    for (int t = 0; t < C::DT; ++t)
+#pragma unroll
+      for (int rg = 0; rg < 4; ++rg) {
+        const int d = 32 * t + 8 * rg + 4 * (lane >> 5);
+        *(f32x4*)(p + d) = f32x4{adk[t][4 * rg], adk[t][4 * rg + 1], adk[t][4 * rg + 2], adk[t][4 * rg + 3]};
+        *(f32x4*)(p + DH + d) = f32x4{adv[t][4 * rg], adv[t][4 * rg + 1], adv[t][4 * rg + 2], adv[t][4 * rg + 3]};
+      }
+  } else if (!FAR && key < a.Skv) {
     store_rows<DH>((bf16*)a.dk + (int64_t)b * a.k_sb + (int64_t)key * a.k_st + (int64_t)kvh * a.k_sh, adk, a.scale, lane);
     store_rows<DH>((bf16*)a.dv + (int64_t)b * a.v_sb + (int64_t)key * a.v_st + (int64_t)kvh * a.v_sh, adv, 1.0f, lane);
   }
 }
 
-template <int DH, int NW>
-static hipError_t launch_dkdv(const WinArgs& a, hipStream_t s) {
-  using C = WinKvCfg<DH, NW>;
-  auto k = win_dkdv_bf16_kernel<DH, NW>;
+template <int DH, int KG, int QH, bool FAR>
+static hipError_t launch_dkdv(const WinArgs& a, int64_t blocks, hipStream_t s) {
+  using C = WinKvCfg<DH, KG, QH>;
+  static_assert(FAR || QH == 1 || KG * C::DT * 32 * 64 * 4 <= C::LDS, "the second halves fit the ring");
+  auto k = win_dkdv_bf16_kernel<DH, KG, QH, FAR>;
   hipError_t e = set_lds(k, C::LDS);
   if (e != hipSuccess) return e;
-  const int64_t nblk = ((int64_t)a.Skv + C::KEYS - 1) / C::KEYS;
-  hipLaunchKernelGGL(k, dim3((unsigned)(nblk * a.Hkv * a.B)), dim3(64 * NW), C::LDS, s, a);
+  hipLaunchKernelGGL(k, dim3((unsigned)(blocks * a.Hkv * a.B)), dim3(64 * C::NW), C::LDS, s, a);
   return hipGetLastError();
+}
+template <int DH>
+static hipError_t dkdv(const WinArgs& a, hipStream_t s) {
+  const int64_t wide = ((int64_t)a.Skv + 255) / 256;
+  if (getenv("KV8")) return launch_dkdv<DH, 8, 1, false>(a, wide, s);
+  return launch_dkdv<DH, 4, 2, false>(a, ((int64_t)a.Skv + 127) / 128, s);
+}
+template <int DH>
+static hipError_t far(const WinArgs& a, hipStream_t s) {
+  return launch_dkdv<DH, 1, 2, true>(a, (int64_t)a.far * ((std::min(a.sinks, a.Skv) + 31) / 32), s);
 }
 template <int DH, int NW>
 static hipError_t launch_dq(const WinArgs& a, hipStream_t s) {
@@ -228,7 +309,12 @@ static hipError_t launch_dq(const WinArgs& a, hipStream_t s) {
   return hipGetLastError();
 }
 
-hipError_t win_dkdv_bf16(const WinArgs& a, hipStream_t s) { return a.dh == 64 ? launch_dkdv<64, 8>(a, s) : launch_dkdv<128, 8>(a, s); }
-hipError_t win_dq_bf16(const WinArgs& a, hipStream_t s) { return a.dh == 64 ? launch_dq<64, 8>(a, s) : launch_dq<128, 8>(a, s); }
+hipError_t win_dkdv_bf16(const WinArgs& a, hipStream_t s) { return a.dh == 64 ? dkdv<64>(a, s) : dkdv<128>(a, s); }
+hipError_t win_far_bf16(const WinArgs& a, hipStream_t s) { return a.dh == 64 ? far<64>(a, s) : far<128>(a, s); }
+template <int DH>
+static hipError_t dq(const WinArgs& a, hipStream_t s) {
+  return win_wide(a.Sq, a) ? launch_dq<DH, 8>(a, s) : launch_dq<DH, 4>(a, s);
+}
+hipError_t win_dq_bf16(const WinArgs& a, hipStream_t s) { return a.dh == 64 ? dq<64>(a, s) : dq<128>(a, s); }
 
 }  // namespace bpt

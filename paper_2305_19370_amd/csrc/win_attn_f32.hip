@@ -5,6 +5,8 @@
 // The query heads of a kv head and their tokens are one list of rows, r = token * G + head: a
 // workgroup's 16 rows then cover few tokens, see nearly the same keys, and a single token's heads
 // fill one workgroup.
+#include <algorithm>
+
 #include "win_attn.h"
 
 namespace bpt {
@@ -162,7 +164,7 @@ __global__ __launch_bounds__(256) void win_join_kernel(WinArgs a) {
   if (lane == 0) a.lse[((int64_t)b * a.Hq + h) * a.lse_ld + i] = l > 0.0f ? (m + log2f(l)) * LN2 : NEG_INF;
 }
 
-// -Delta = -sum_d dO O and minus the base-2 log-sum-exp of every row, [B, Hq, Sqp]; 0 where a row
+// -Delta = -sum_d dO O and -lse / scale (what the raw products are reduced by) of every row, [B, Hq, Sqp]; 0 where a row
 // sees nothing, and behind the rows. One wave per 64 / (dh / 8) rows, 8 features a lane.
 template <typename T, int DH>
 __global__ __launch_bounds__(256) void win_delta_kernel(WinArgs a) {
@@ -180,14 +182,14 @@ __global__ __launch_bounds__(256) void win_delta_kernel(WinArgs a) {
       const T *x = (const T*)a.o + o, *y = (const T*)a.dout + o;
 #pragma unroll
       for (int e = 0; e < 8; ++e) s = fmaf(to_f32<T>(x[e]), to_f32<T>(y[e]), s);
-      nl = -l * LOG2E;
+      nl = -l / a.scale;
     }
   }
 #pragma unroll
   for (int o = LPR / 2; o >= 1; o >>= 1) s += __shfl_xor(s, o, 64);
   if (d == 0) {
     a.ndelta[at] = -s;
-    a.nlse2[at] = nl;
+    a.nlse[at] = nl;
   }
 }
 
@@ -218,7 +220,7 @@ __global__ __launch_bounds__(256) void win_dq_f32_kernel(WinArgs a) {
     const RowFrag<DH> qf = row_frag<DH>((const float*)a.q + (int64_t)b * a.q_sb + (int64_t)qi * a.q_st + (int64_t)h * a.q_sh, g);
     const RowFrag<DH> of = row_frag<DH>((const float*)a.dout + (int64_t)b * a.o_sb + (int64_t)qi * a.o_st + (int64_t)h * a.o_sh, g);
     const int64_t sidx = ((int64_t)b * a.Hq + h) * a.Sqp + qi;
-    const float nl = a.nlse2[sidx], ndl = a.ndelta[sidx];
+    const float nl = a.nlse[sidx], ndl = a.ndelta[sidx];
     for (int j = wave; j < tiles.n; j += 4) {
       const int k0 = tiles.key0(j);
       const int64_t kr = run.clamp(k0 + c16);
@@ -228,7 +230,7 @@ __global__ __launch_bounds__(256) void win_dq_f32_kernel(WinArgs a) {
       f32x4 ds = dot_frags<DH>(vf, of);
 #pragma unroll
       for (int r = 0; r < 4; ++r)
-        ds[r] = mine.sees(k0 + 4 * g + r) ? fast_exp2(fmaf(s[r], c, nl)) * (ds[r] + ndl) : 0.0f;
+        ds[r] = mine.sees(k0 + 4 * g + r) ? fast_exp2((s[r] + nl) * c) * (ds[r] + ndl) : 0.0f;
       add_outer<DH>(dq, kc, ds);
     }
   }
@@ -245,43 +247,48 @@ __global__ __launch_bounds__(256) void win_dq_f32_kernel(WinArgs a) {
   }
 }
 
-// dK, dV: 16 keys; wave w takes every fourth (query head, tile of 16 queries) pair of the kv head, in order. P
+// dK, dV: 16 keys (FAR: 16 sinks and a chunk of the queries beyond their window, as in the bf16 kernel); wave w takes every fourth (query head, tile of 16 queries) pair of the kv head, in order. P
 // and dS have the key on the lane axis and are the B operands of dV^T += dO^T P, dK^T += Q^T dS.
-template <int DH>
+template <int DH, bool FAR>
 __global__ __launch_bounds__(256) void win_dkdv_f32_kernel(WinArgs a) {
   constexpr int NC = DH / 16;
   __shared__ __attribute__((aligned(16))) float red[4][16][DH + 4];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, g = lane >> 4, c16 = lane & 15;
-  const int kvh = blockIdx.y, b = blockIdx.z, k0 = blockIdx.x * 16, key = k0 + c16;
+  const int chunk = FAR ? blockIdx.x % a.far : 0;
+  const int kvh = blockIdx.y, b = blockIdx.z, k0 = (FAR ? blockIdx.x / a.far : blockIdx.x) * 16, key = k0 + c16;
   const Seq sq = seq_of(a, b);
+  const bool near = FAR || a.far > 0;
+  const int kend = FAR ? min(sq.nk, a.sinks) : sq.nk;
   const float c = a.scale * LOG2E;
   f32x4 dk[NC], dv[NC];
 #pragma unroll
   for (int t = 0; t < NC; ++t) dk[t] = dv[t] = f32x4{};
-  if (k0 < sq.nk) {
-    const int kr = min(key, sq.nk - 1);
-    QVis mine = qvis_of(a, sq, key, key, false);
+  if (k0 < kend) {
+    const int kr = min(key, kend - 1);
+    QVis mine = qvis_of(a, sq, key, key, near);
     if (key >= sq.nk) mine.hi = -1;
-    const int kl = min(k0 + 15, sq.nk - 1);
-    const QVis run = qvis_of(a, sq, k0, kl, false);
+    QVis run = qvis_of(a, sq, k0, min(k0 + 15, kend - 1), near);
+    if (FAR) run = QVis{a.causal ? max(k0 + a.window - sq.off, 0) : 0, sq.nq - 1};
     const RowFrag<DH> kf = row_frag<DH>((const float*)a.k + (int64_t)b * a.k_sb + (int64_t)kvh * a.k_sh + (int64_t)kr * a.k_st, g);
     const RowFrag<DH> vf = row_frag<DH>((const float*)a.v + (int64_t)b * a.v_sb + (int64_t)kvh * a.v_sh + (int64_t)kr * a.v_st, g);
     const int t0 = run.lo / 16, nt = run.hi >= run.lo ? run.hi / 16 + 1 - t0 : 0;
-    for (int it = wave; it < nt * a.G; it += 4) {
+    const int per = FAR ? (nt * a.G + a.far - 1) / a.far : nt * a.G;
+    for (int it = chunk * per + wave; it < min((chunk + 1) * per, nt * a.G); it += 4) {
       const int h = kvh * a.G + it / nt, q0 = 16 * (t0 + it % nt);
       const float* Qb = (const float*)a.q + (int64_t)b * a.q_sb + (int64_t)h * a.q_sh;
       const float* dOb = (const float*)a.dout + (int64_t)b * a.o_sb + (int64_t)h * a.o_sh;
       const int64_t qr = min(max(q0 + c16, run.lo), run.hi);
       const RowFrag<DH> qf = row_frag<DH>(Qb + qr * a.q_st, g), of = row_frag<DH>(dOb + qr * a.o_st, g);
       const int64_t sidx = ((int64_t)b * a.Hq + h) * a.Sqp + q0 + 4 * g;   // Sqp % 64 == 0
-      const f32x4 l4 = *(const f32x4*)(a.nlse2 + sidx), d4 = *(const f32x4*)(a.ndelta + sidx);
+      const f32x4 l4 = *(const f32x4*)(a.nlse + sidx), d4 = *(const f32x4*)(a.ndelta + sidx);
       Vis qv{run.lo, run.hi, 0};
       f32x4 p = dot_frags<DH>(qf, kf), ds = dot_frags<DH>(of, vf);
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
         const int q = q0 + 4 * g + r;
-        const bool ok = q >= mine.lo && q <= mine.hi;
-        p[r] = ok ? fast_exp2(fmaf(p[r], c, l4[r])) : 0.0f;
+        const bool in = q >= mine.lo && q <= mine.hi;
+        const bool ok = !FAR ? in : q <= run.hi && (a.causal ? q > mine.hi : !in);
+        p[r] = ok ? fast_exp2((p[r] + l4[r]) * c) : 0.0f;
         ds[r] = ok ? p[r] * (ds[r] + d4[r]) : 0.0f;
       }
       const ColFrag<DH> oc = col_frag_vis<DH>(dOb, a.o_st, q0, qv, g, c16);
@@ -300,9 +307,15 @@ __global__ __launch_bounds__(256) void win_dkdv_f32_kernel(WinArgs a) {
     float* out = (float*)(which ? a.dv : a.dk) + base;
     for (int e = tid; e < 16 * (DH / 4); e += 256) {
       const int ki = e / (DH / 4), d = 4 * (e % (DH / 4));
-      if (k0 + ki >= a.Skv) continue;
+      const int ns = a.far > 0 ? min(a.sinks, a.Skv) : 0;
+      if (k0 + ki >= (FAR ? ns : a.Skv)) continue;
       const f32x4 x = ((*(const f32x4*)&red[0][ki][d] + *(const f32x4*)&red[1][ki][d]) + *(const f32x4*)&red[2][ki][d]) +
                       *(const f32x4*)&red[3][ki][d];
+      if (k0 + ki < ns) {                            // [slot, B Hkv, sinks, dK and dV, dh]
+        const int64_t at = ((int64_t)(FAR ? 1 + chunk : 0) * a.B * a.Hkv + (int64_t)b * a.Hkv + kvh) * ns + k0 + ki;
+        *(f32x4*)(a.part_s + (2 * at + which) * DH + d) = x;
+        continue;
+      }
       *(f32x4*)(out + (int64_t)(k0 + ki) * (which ? a.v_st : a.k_st) + d) = x * (which ? 1.0f : a.scale);
     }
   }
@@ -314,9 +327,42 @@ static hipError_t fwd_f32(const WinArgs& a, hipStream_t s) {
   hipLaunchKernelGGL(win_fwd_f32_kernel<DH>, dim3(nblk * a.nsplit, a.Hkv, a.B), dim3(256), 0, s, a);
   return hipGetLastError();
 }
+// dK and dV of the sinks: the window's part and the chunks'. A workgroup per (sink, dK or dV): its groups of DH / 4 lanes take
+// every n-th slot, in order, and are added in order.
+template <typename T, int DH>
+__global__ __launch_bounds__(256) void win_sinks_kernel(WinArgs a, int slots) {
+  constexpr int L = DH / 4, N = 256 / L;
+  __shared__ f32x4 red[N][L];
+  const int ns = min(a.sinks, a.Skv), grp = threadIdx.x / L, l = threadIdx.x % L;
+  const int64_t row = blockIdx.x, stride = (int64_t)gridDim.x * DH;
+  const int which = (int)(row % 2), key = (int)(row / 2 % ns);
+  const int64_t bh = row / 2 / ns, b = bh / a.Hkv, kvh = bh % a.Hkv;
+  f32x4 x = {};
+  if (key < seq_of(a, (int)b).nk) {
+    const float* p = a.part_s + row * DH + 4 * l;
+#pragma unroll 4
+    for (int z = grp; z < slots; z += N) x += *(const f32x4*)(p + z * stride);
+  }
+  red[grp][l] = x;
+  __syncthreads();
+  if (grp) return;
+  for (int g = 1; g < N; ++g) x += red[g][l];
+  if (!which) x *= a.scale;
+  T* out = which ? (T*)a.dv + b * a.v_sb + (int64_t)key * a.v_st + kvh * a.v_sh : (T*)a.dk + b * a.k_sb + (int64_t)key * a.k_st + kvh * a.k_sh;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) out[4 * l + e] = from_f32<T>(x[e]);
+}
+
 template <int DH>
 static hipError_t dkdv_f32(const WinArgs& a, hipStream_t s) {
-  hipLaunchKernelGGL(win_dkdv_f32_kernel<DH>, dim3((a.Skv + 15) / 16, a.Hkv, a.B), dim3(256), 0, s, a);
+  auto k = win_dkdv_f32_kernel<DH, false>;
+  hipLaunchKernelGGL(k, dim3((a.Skv + 15) / 16, a.Hkv, a.B), dim3(256), 0, s, a);
+  return hipGetLastError();
+}
+template <int DH>
+static hipError_t far_f32(const WinArgs& a, hipStream_t s) {
+  auto k = win_dkdv_f32_kernel<DH, true>;
+  hipLaunchKernelGGL(k, dim3((std::min(a.sinks, a.Skv) + 15) / 16 * a.far, a.Hkv, a.B), dim3(256), 0, s, a);
   return hipGetLastError();
 }
 template <int DH>
@@ -327,12 +373,20 @@ static hipError_t dq_f32(const WinArgs& a, hipStream_t s) {
 }
 hipError_t win_fwd_f32(const WinArgs& a, hipStream_t s) { return a.dh == 64 ? fwd_f32<64>(a, s) : fwd_f32<128>(a, s); }
 hipError_t win_dkdv_f32(const WinArgs& a, hipStream_t s) { return a.dh == 64 ? dkdv_f32<64>(a, s) : dkdv_f32<128>(a, s); }
+hipError_t win_far_f32(const WinArgs& a, hipStream_t s) { return a.dh == 64 ? far_f32<64>(a, s) : far_f32<128>(a, s); }
 hipError_t win_dq_f32(const WinArgs& a, hipStream_t s) { return a.dh == 64 ? dq_f32<64>(a, s) : dq_f32<128>(a, s); }
 
 hipError_t win_join(Dt t, const WinArgs& a, hipStream_t s) {
   const int64_t all = (int64_t)a.B * a.Hq * a.Sq;
   auto k = t == BF16 ? win_join_kernel<bf16> : win_join_kernel<float>;
   hipLaunchKernelGGL(k, dim3((unsigned)((all + 3) / 4)), dim3(256), 0, s, a);
+  return hipGetLastError();
+}
+hipError_t win_sinks(Dt t, const WinArgs& a, int slots, hipStream_t s) {
+  const int64_t n = (int64_t)a.B * a.Hkv * std::min(a.sinks, a.Skv) * 2;
+  auto k = t == BF16 ? (a.dh == 64 ? win_sinks_kernel<bf16, 64> : win_sinks_kernel<bf16, 128>)
+                     : (a.dh == 64 ? win_sinks_kernel<float, 64> : win_sinks_kernel<float, 128>);
+  hipLaunchKernelGGL(k, dim3((unsigned)n), dim3(256), 0, s, a, slots);
   return hipGetLastError();
 }
 hipError_t win_delta(Dt t, const WinArgs& a, hipStream_t s) {

@@ -44,57 +44,179 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 1 : 2) void win_fwd_bf16_kernel(
     auto issue = [&](int j) {
       issue_keys<DH, NW>(smem + (j % C::NS) * C::STAGE, Kb, a.k_st, Vb, a.v_st, tiles.key0(j), w.run, roff, wave, lane);
     };
-    auto tile = [&](int j) {
-      const int k0 = tiles.key0(j);
+    OnlineRows<C::DT> sm{c};
+    auto tile = [&](int j, int k0, bool all) {
       const char* kt = smem + (j % C::NS) * C::STAGE;
       const char* vt = kt + C::TB;
-      f32x16 t[2] = {f32x16{}, f32x16{}};
+      bf16x8 kf[C::KSTEPS][2];                        // read at once, so that only the first MFMA waits
 #pragma unroll
       for (int kk = 0; kk < C::KSTEPS; ++kk)
 #pragma unroll
-        for (int mt = 0; mt < 2; ++mt) t[mt] = mfma32x32x16(frag_rows<DH>(kt, 32 * mt, 2 * kk, lane), qf[kk], t[mt]);
-      if (!w.all(k0)) w.mask(t, k0, lane, NEG_INF);
-      float mx = NEG_INF;
+        for (int mt = 0; mt < 2; ++mt) kf[kk][mt] = frag_rows<DH>(kt, 32 * mt, 2 * kk, lane);
+      __builtin_amdgcn_sched_barrier(0);
+      f32x16 t[2] = {f32x16{}, f32x16{}}, p[2];
 #pragma unroll
-      for (int mt = 0; mt < 2; ++mt)
+      for (int kk = 0; kk < C::KSTEPS; ++kk)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) mx = fmaxf(mx, t[mt][r]);
-      mx = max_halves(mx) * c;
-      const float m_new = fmaxf(ref, mx);
-      const float m_use = m_new == NEG_INF ? 0.0f : m_new;
-      if (__ballot(m_new > ref)) {
-        const float corr = fast_exp2(ref - m_use);
-        l_run *= corr;
-#pragma unroll
-        for (int d = 0; d < C::DT; ++d) acc[d] *= corr;
-        ref = m_new;
-      }
-#pragma unroll
-      for (int mt = 0; mt < 2; ++mt)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          t[mt][r] = fast_exp2(fmaf(t[mt][r], c, -m_use));
-          l_run += t[mt][r];
-        }
+        for (int mt = 0; mt < 2; ++mt) t[mt] = mfma32x32x16(kf[kk][mt], qf[kk], t[mt]);
+      if (!all) w.mask(t, k0, lane, NEG_INF);
+      sm.weights(t, p, acc);
 #pragma unroll
       for (int mt = 0; mt < 2; ++mt)
 #pragma unroll
         for (int hf = 0; hf < 2; ++hf) {
-          const bf16x8 pb = acc_to_b(t[mt], hf);
+          const bf16x8 pb = acc_to_b(p[mt], hf);
 #pragma unroll
           for (int d = 0; d < C::DT; ++d)
             acc[d] = mfma32x32x16(frag_tr<DH>(vt, 32 * mt + 16 * hf, 32 * d, lane), pb, acc[d]);
         }
     };
     ring_loop<C, C::DPS>(tiles.n, issue, [&](int j) {
-      if (!w.none(tiles.key0(j))) tile(j);
+      const int k0 = tiles.key0(j);
+      if (!w.none(k0)) tile(j, k0, w.all(k0));
     });
+    ref = sm.ref;
+    l_run = sm.sum;
   }
   const float l = sum_halves(l_run);
   if (w.i < a.Sq) {
     const float inv = l > 0.0f ? 1.0f / l : 0.0f;   // a row that sees nothing: 0
     store_rows<DH>((bf16*)a.o + (int64_t)b * a.o_sb + (int64_t)w.i * a.o_st + (int64_t)h * a.o_sh, acc, inv, lane);
     if (lane < 32) a.lse[((int64_t)b * a.Hq + h) * a.lse_ld + w.i] = l > 0.0f ? (ref + log2f(l)) * LN2 : NEG_INF;
+  }
+}
+
+// Few rows (new tokens, short pieces of a prompt): 32 rows per workgroup and one of a.nsplit slices of the key tiles, so
+// that the cache is read by the whole chip. Bound by that read: each of the 4 waves streams tiles of 32 keys (every fourth of the
+// slice) through two LDS stages of its own, without a barrier, 80 KB of a CU's LDS in flight while the other 80 KB
+// are worked on; waves and slices are merged as two runs of an online softmax are.
+template <int DH>
+struct WinTokCfg {
+  static constexpr int KSTEPS = DH / 16, DT = DH / 32, NW = 4;
+  static constexpr int PITCH = RmTile<DH>::PITCH, SLOTS = RmTile<DH>::SLOTS;
+  static constexpr int BL = (32 * PITCH + 1023) / 1024, TB = BL * 1024;   // copies and bytes of 32 rows (the last copy runs past them)
+  static constexpr int STAGE = 2 * TB, LDS = NW * 2 * STAGE;
+  static constexpr int OP = DH + 4;                   // pitch of a merged row, floats
+  static_assert(NW * 32 * OP * 4 + 2 * NW * 32 * 4 <= LDS, "the merge reuses the stages");
+};
+
+template <int DH>
+__global__ __launch_bounds__(256, 1) void win_token_kernel(WinArgs a) {
+  using C = WinTokCfg<DH>;
+  extern __shared__ __attribute__((aligned(16))) char smem[];
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int rows = a.Sq * a.G, nblk = (rows + 31) / 32;
+  int hh, blk;
+  xcd_map((int)blockIdx.x, a.Hkv * a.B, hh, blk);
+  const int kvh = hh % a.Hkv, b = hh / a.Hkv, slice = blk / nblk, r0 = blk % nblk * 32;
+  const Seq sq = seq_of(a, b);
+  const Rows w(a, sq, r0, 0, 32, lane);
+  const int h = kvh * a.G + w.head;
+  const bf16* Kb = (const bf16*)a.k + (int64_t)b * a.k_sb + (int64_t)kvh * a.k_sh;
+  const bf16* Vb = (const bf16*)a.v + (int64_t)b * a.v_sb + (int64_t)kvh * a.v_sh;
+  const Tiles<32> tiles(w.run);
+  const int per = (tiles.n + a.nsplit - 1) / a.nsplit, j0 = slice * per, j1 = min(j0 + per, tiles.n);
+
+  f32x16 acc[C::DT];
+#pragma unroll
+  for (int t = 0; t < C::DT; ++t) acc[t] = f32x16{};
+  OnlineRows<C::DT> sm{a.scale * LOG2E};
+  if (j0 + wave < j1) {
+    bf16x8 qf[C::KSTEPS];
+    {
+      const bf16* q = (const bf16*)a.q + (int64_t)b * a.q_sb + (int64_t)w.safe(sq) * a.q_st + (int64_t)h * a.q_sh;
+#pragma unroll
+      for (int kk = 0; kk < C::KSTEPS; ++kk) {
+        qf[kk] = __builtin_bit_cast(bf16x8, ld16(q + 16 * kk + 8 * (lane >> 5)));
+        settle(qf[kk]);
+      }
+    }
+    char* mine = smem + wave * 2 * C::STAGE;
+    auto issue = [&](int j, int at) {
+      const int k0 = tiles.key0(j);
+      const int lo = max(w.run.lo, k0), hi = min(w.run.hi, k0 + 31), se = min(w.run.se, k0 + 32);
+      const bf16 *ko = Kb + (int64_t)k0 * a.k_st, *vo = Vb + (int64_t)k0 * a.v_st;
+#pragma unroll
+      for (int i = 0; i < C::BL; ++i) {
+        const int slot = 64 * i + lane, col = slot % C::SLOTS, k = k0 + slot / C::SLOTS;
+        const int row = (k < se ? k : lo <= hi ? min(max(k, lo), hi) : se - 1) - k0, c8 = (col < DH / 8 ? col : 0) * 8;
+        dma16s(scalar_ptr(ko), 2u * (uint32_t)(row * a.k_st + c8), mine + at * C::STAGE + i * 1024);
+        dma16s(scalar_ptr(vo), 2u * (uint32_t)(row * a.v_st + c8), mine + at * C::STAGE + C::TB + i * 1024);
+      }
+    };
+    int at = 0;
+    issue(j0 + wave, 0);
+    for (int j = j0 + wave; j < j1; j += 4, at ^= 1) {
+      if (j + 4 < j1) {
+        issue(j + 4, at ^ 1);
+        wait_vmcnt<2 * C::BL>();
+      } else {
+        wait_vmcnt<0>();
+      }
+      const int k0 = tiles.key0(j);
+      const char* kt = mine + at * C::STAGE;
+      f32x16 t[1] = {f32x16{}}, p[1];
+#pragma unroll
+      for (int kk = 0; kk < C::KSTEPS; ++kk) t[0] = mfma32x32x16(frag_rows<DH>(kt, 0, 2 * kk, lane), qf[kk], t[0]);
+      w.mask(t, k0, lane, NEG_INF);
+      sm.weights(t, p, acc);
+#pragma unroll
+      for (int hf = 0; hf < 2; ++hf) {
+        const bf16x8 pb = acc_to_b(p[0], hf);
+#pragma unroll
+        for (int d = 0; d < C::DT; ++d) acc[d] = mfma32x32x16(frag_tr<DH>(kt + C::TB, 16 * hf, 32 * d, lane), pb, acc[d]);
+      }
+      wait_lgkm();                                    // the stage is read before the next copies overwrite it
+    }
+  }
+  // merge the waves in order: numerators row by row in LDS, with maximum and sum
+  __syncthreads();
+  float* red = (float*)smem;
+  float *red_m = red + C::NW * 32 * C::OP, *red_l = red_m + C::NW * 32;
+  const float l = sum_halves(sm.sum);
+  float* my = red + (wave * 32 + (lane & 31)) * C::OP;
+#pragma unroll
+  for (int t = 0; t < C::DT; ++t)
+#pragma unroll
+    for (int rg = 0; rg < 4; ++rg)
+      *(f32x4*)(my + 32 * t + 8 * rg + 4 * (lane >> 5)) = f32x4{acc[t][4 * rg], acc[t][4 * rg + 1], acc[t][4 * rg + 2], acc[t][4 * rg + 3]};
+  if (lane < 32) {
+    red_m[wave * 32 + lane] = sm.ref;
+    red_l[wave * 32 + lane] = l;
+  }
+  __syncthreads();
+  for (int e = tid; e < 32 * (DH / 4); e += 256) {
+    const int ri = e / (DH / 4), d = 4 * (e % (DH / 4)), rr = r0 + ri;
+    if (rr >= rows) break;
+    float m = NEG_INF, lt = 0.0f;
+#pragma unroll
+    for (int v = 0; v < C::NW; ++v) m = fmaxf(m, red_m[v * 32 + ri]);
+    f32x4 o = {};
+    if (m > NEG_INF) {
+#pragma unroll
+      for (int v = 0; v < C::NW; ++v) {
+        const float f = fast_exp2(red_m[v * 32 + ri] - m);
+        lt = fmaf(red_l[v * 32 + ri], f, lt);
+        o += f * *(const f32x4*)(red + (v * 32 + ri) * C::OP + d);
+      }
+    }
+    if (a.nsplit > 1) {
+      const int64_t p = ((int64_t)slice * a.B * a.Hkv + (int64_t)b * a.Hkv + kvh) * rows + rr;
+      *(f32x4*)(a.part_o + p * DH + d) = o;
+      if (d == 0) {
+        a.part_ml[2 * p] = m;
+        a.part_ml[2 * p + 1] = lt;
+      }
+      continue;
+    }
+    const int i = rr / a.G, hq = kvh * a.G + rr % a.G;
+    const float inv = lt > 0.0f ? 1.0f / lt : 0.0f;
+    bf16x4 x;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) x[k] = (bf16)(o[k] * inv);
+    *(bf16x4*)((bf16*)a.o + (int64_t)b * a.o_sb + (int64_t)i * a.o_st + (int64_t)hq * a.o_sh + d) = x;
+    if (d == 0) a.lse[((int64_t)b * a.Hq + hq) * a.lse_ld + i] = lt > 0.0f ? (m + log2f(lt)) * LN2 : NEG_INF;
   }
 }
 
@@ -108,9 +230,22 @@ static hipError_t launch_fwd(const WinArgs& a, hipStream_t s) {
   hipLaunchKernelGGL(k, dim3((unsigned)(nblk * a.Hkv * a.B)), dim3(64 * NW), C::LDS, s, a);
   return hipGetLastError();
 }
-
-hipError_t win_fwd_bf16(const WinArgs& a, hipStream_t s) {
-  return a.dh == 64 ? launch_fwd<64, 8>(a, s) : launch_fwd<128, 8>(a, s);
+template <int DH>
+static hipError_t launch_token(const WinArgs& a, hipStream_t s) {
+  using C = WinTokCfg<DH>;
+  auto k = win_token_kernel<DH>;
+  hipError_t e = set_lds(k, C::LDS);
+  if (e != hipSuccess) return e;
+  const int64_t nblk = ((int64_t)a.Sq * a.G + 31) / 32;
+  hipLaunchKernelGGL(k, dim3((unsigned)(nblk * a.nsplit * a.Hkv * a.B)), dim3(256), C::LDS, s, a);
+  return hipGetLastError();
 }
+
+template <int DH>
+static hipError_t fwd(const WinArgs& a, hipStream_t s) {
+  if (a.few) return launch_token<DH>(a, s);
+  return win_wide(a.Sq, a) ? launch_fwd<DH, 8>(a, s) : launch_fwd<DH, 4>(a, s);
+}
+hipError_t win_fwd_bf16(const WinArgs& a, hipStream_t s) { return a.dh == 64 ? fwd<64>(a, s) : fwd<128>(a, s); }
 
 }  // namespace bpt

@@ -6,6 +6,16 @@
 
 namespace bpt {
 
+// Waves of workgroups of 256 rows (8 waves, one workgroup on a CU) or 128 (4, two): the small ones where the large would
+// leave CUs idle.
+inline bool win_wide(int64_t len, const WinArgs& a) { return (len * a.G + 255) / 256 * a.Hkv * a.B > 256; }
+
+template <int N = 0> BPT_DEV void wait_lgkm() { asm volatile("s_waitcnt lgkmcnt(%0)" ::"n"(N) : "memory"); }
+
+// Products accumulated into x are formed before what follows: the compiler would sink them behind a branch and
+// hold their fragments in registers meanwhile.
+BPT_DEV void pin(f32x16& x) { asm volatile("" : "+v"(x)); }
+
 // NW waves of 32 rows (keys, in the dK dV kernel) share tiles of 64 rows of two tensors in a ring
 template <int DH, int NWAVES>
 struct WinCfg {
@@ -46,12 +56,12 @@ struct Rows {
   BPT_DEV bool all(int k0) const { return full && ((k0 >= last.lo && k0 + 63 <= first.hi) || k0 + 63 < first.se); }
   BPT_DEV bool none(int k0) const { return !(k0 <= last.hi && k0 + 63 >= first.lo) && k0 >= last.se; }
   // scores t[mt][r] of keys k0 + 32 mt + acc_row(r, lane)
-  template <typename V>
-  BPT_DEV void mask(V (&t)[2], int k0, int lane, float out) const {
+  template <int N>
+  BPT_DEV void mask(f32x16 (&t)[N], int k0, int lane, float out) const {
     const int base = k0 + 4 * (lane >> 5);
     const int lo = mine.lo - base, hi = mine.hi - base, se = mine.se - base;
 #pragma unroll
-    for (int mt = 0; mt < 2; ++mt)
+    for (int mt = 0; mt < N; ++mt)
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
         const int k = 32 * mt + 8 * (r >> 2) + (r & 3);
@@ -92,6 +102,54 @@ BPT_DEV void issue_keys(char* stage, const bf16* K, int ldk, const bf16* V, int 
   issue_picked<DH, NW>(stage, K, ldk, V, ldv, k0, wave, lane,
                        [&](int k) { return k < se ? k : lo <= hi ? min(max(k, lo), hi) : se - 1; });
 }
+
+// The online softmax of the row on a lane (shared with lane ^ 32): reference maximum in base 2 (-inf until the row has
+// seen a key) and the lane's part of the sum of weights.
+//
+// Once every row of the wave has a reference, weights are taken against it as it stands; the tile's maximum is formed
+// only when a lane's sum of weights passes SUM_MAX (a score far above the reference). No sum can vanish: the
+// reference left a weight of 1, and no weight exceeds SUM_MAX.
+template <int DT>
+struct OnlineRows {
+  static constexpr float SUM_MAX = 65536.0f;
+  float c;                                           // scale log2(e)
+  float ref = NEG_INF, sum = 0.0f;
+  template <int N>
+  BPT_DEV float raw(const f32x16 (&t)[N], f32x16 (&p)[N], float m) const {
+    float rs = 0.0f;
+#pragma unroll
+    for (int x = 0; x < N; ++x)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        p[x][r] = fast_exp2(fmaf(t[x][r], c, -m));
+        rs += p[x][r];
+      }
+    return rs;
+  }
+  // weights p of products t (-inf where unseen); moves the reference and rescales acc where it has to
+  template <int N>
+  BPT_DEV void weights(const f32x16 (&t)[N], f32x16 (&p)[N], f32x16 (&acc)[DT]) {
+    if (!__ballot(ref == NEG_INF)) {
+      const float rs = raw(t, p, ref);
+      if (!__ballot(!(rs <= SUM_MAX))) {
+        sum += rs;
+        return;
+      }
+    }
+    float mx = NEG_INF;
+#pragma unroll
+    for (int x = 0; x < N; ++x)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) mx = fmaxf(mx, t[x][r]);
+    const float m = fmaxf(ref, max_halves(mx) * c), use = m == NEG_INF ? 0.0f : m;
+    const float corr = fast_exp2(ref - use);         // 0 for a row that starts
+    sum *= corr;
+#pragma unroll
+    for (int d = 0; d < DT; ++d) acc[d] *= corr;
+    ref = m;
+    sum += raw(t, p, use);
+  }
+};
 
 // Walks n stages of the ring (C::NS slots, DPS copies per wave and stage): body(j) runs with stage j in
 // LDS. Every wave of the workgroup reaches every barrier.

@@ -73,7 +73,10 @@ SHAPES = [
     (1, 130, 50, 2, 1, True, 0, 0),                 # more queries than keys: 80 rows see nothing
     (1, 130, 50, 2, 1, True, 9, 2),
     (1, 130, 50, 2, 1, False, 9, 2),
-    (1, 2100, 2100, 2, 2, True, 300, 4),
+    (1, 2100, 2100, 2, 2, True, 300, 4),            # from here: sinks with far more queries than a window's keys
+    (2, 1500, 1500, 4, 2, True, 64, 33),
+    (1, 1500, 1500, 2, 2, False, 40, 70),
+    (1, 300, 2500, 8, 1, True, 50, 4),
     (1, 260, 260, 2, 2, True, 5000, 4),             # a window longer than the sequence
     (1, 260, 260, 2, 2, True, 16, 1000),            # more sinks than keys
 ]
@@ -110,6 +113,7 @@ LENS = [
     (3, 40, 500, [40, 17, 0], [500, 64, 77], 0, 0, True),
     (3, 40, 500, [40, 40, 3], [20, 0, 500], 30, 2, True),      # fewer keys than queries, no keys
     (2, 70, 300, [70, 9], [299, 65], 33, 4, False),
+    (3, 1500, 1500, [1500, 90, 0], [1500, 90, 3], 64, 40, True),
 ]
 
 

@@ -132,7 +132,7 @@ def test_attn_config_of_refuses():
 
 def test_few_queries_are_cut_along_the_keys():
     """A workspace is asked for exactly where the keys are cut; never more than 64 slices."""
-    for dt in (torch.float32,):
+    for dt in (torch.float32, torch.bfloat16):
         one = torch.empty(1, 1, 8, 128, dtype=dt)
         for L, cut in ((64, False), (100000, True)):
             k = torch.empty(1, L, 1, 128, dtype=dt, device="meta")
