@@ -48,24 +48,18 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 1 : 2) void win_fwd_bf16_kernel(
     auto tile = [&](int j, int k0, bool all) {
       const char* kt = smem + (j % C::NS) * C::STAGE;
       const char* vt = kt + C::TB;
-      bf16x8 kf[C::KSTEPS][2];                        // read at once, so that only the first MFMA waits
+      f32x16 t[2] = {f32x16{}, f32x16{}};
 #pragma unroll
       for (int kk = 0; kk < C::KSTEPS; ++kk)
 #pragma unroll
-        for (int mt = 0; mt < 2; ++mt) kf[kk][mt] = frag_rows<DH>(kt, 32 * mt, 2 * kk, lane);
-      __builtin_amdgcn_sched_barrier(0);
-      f32x16 t[2] = {f32x16{}, f32x16{}}, p[2];
-#pragma unroll
-      for (int kk = 0; kk < C::KSTEPS; ++kk)
-#pragma unroll
-        for (int mt = 0; mt < 2; ++mt) t[mt] = mfma32x32x16(kf[kk][mt], qf[kk], t[mt]);
+        for (int mt = 0; mt < 2; ++mt) t[mt] = mfma32x32x16(frag_rows<DH>(kt, 32 * mt, 2 * kk, lane), qf[kk], t[mt]);
       if (!all) w.mask(t, k0, lane, NEG_INF);
-      sm.weights(t, p, acc);
+      sm.weights(t, acc);
 #pragma unroll
       for (int mt = 0; mt < 2; ++mt)
 #pragma unroll
         for (int hf = 0; hf < 2; ++hf) {
-          const bf16x8 pb = acc_to_b(p[mt], hf);
+          const bf16x8 pb = acc_to_b(t[mt], hf);
 #pragma unroll
           for (int d = 0; d < C::DT; ++d)
             acc[d] = mfma32x32x16(frag_tr<DH>(vt, 32 * mt + 16 * hf, 32 * d, lane), pb, acc[d]);
@@ -156,14 +150,14 @@ __global__ __launch_bounds__(256, 1) void win_token_kernel(WinArgs a) {
       }
       const int k0 = tiles.key0(j);
       const char* kt = mine + at * C::STAGE;
-      f32x16 t[1] = {f32x16{}}, p[1];
+      f32x16 t[1] = {f32x16{}};
 #pragma unroll
       for (int kk = 0; kk < C::KSTEPS; ++kk) t[0] = mfma32x32x16(frag_rows<DH>(kt, 0, 2 * kk, lane), qf[kk], t[0]);
       w.mask(t, k0, lane, NEG_INF);
-      sm.weights(t, p, acc);
+      sm.weights(t, acc);
 #pragma unroll
       for (int hf = 0; hf < 2; ++hf) {
-        const bf16x8 pb = acc_to_b(p[0], hf);
+        const bf16x8 pb = acc_to_b(t[0], hf);
 #pragma unroll
         for (int d = 0; d < C::DT; ++d) acc[d] = mfma32x32x16(frag_tr<DH>(kt + C::TB, 16 * hf, 32 * d, lane), pb, acc[d]);
       }

@@ -103,51 +103,40 @@ BPT_DEV void issue_keys(char* stage, const bf16* K, int ldk, const bf16* V, int 
                        [&](int k) { return k < se ? k : lo <= hi ? min(max(k, lo), hi) : se - 1; });
 }
 
-// The online softmax of the row on a lane (shared with lane ^ 32): reference maximum in base 2 (-inf until the row has
-// seen a key) and the lane's part of the sum of weights.
-//
-// Once every row of the wave has a reference, weights are taken against it as it stands; the tile's maximum is formed
-// only when a lane's sum of weights passes SUM_MAX (a score far above the reference). No sum can vanish: the
-// reference left a weight of 1, and no weight exceeds SUM_MAX.
+// The online softmax of the row on a lane (shared with lane ^ 32): reference in base 2 (-inf until the row has seen a key) and
+// the lane's part of the sum of weights. The reference moves to a tile's maximum only where that lies more than GROWTH
+// above it: weights stay <= 2^GROWTH, the reference left a weight of at least 1 so that no sum vanishes, and the
+// numerator is rescaled in few tiles (any of a wave's 32 rows has a new maximum in most).
 template <int DT>
 struct OnlineRows {
-  static constexpr float SUM_MAX = 65536.0f;
+  static constexpr float GROWTH = 8.0f;
   float c;                                           // scale log2(e)
   float ref = NEG_INF, sum = 0.0f;
+  // products t (-inf where unseen) become weights; acc is rescaled where the reference moves
   template <int N>
-  BPT_DEV float raw(const f32x16 (&t)[N], f32x16 (&p)[N], float m) const {
-    float rs = 0.0f;
-#pragma unroll
-    for (int x = 0; x < N; ++x)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        p[x][r] = fast_exp2(fmaf(t[x][r], c, -m));
-        rs += p[x][r];
-      }
-    return rs;
-  }
-  // weights p of products t (-inf where unseen); moves the reference and rescales acc where it has to
-  template <int N>
-  BPT_DEV void weights(const f32x16 (&t)[N], f32x16 (&p)[N], f32x16 (&acc)[DT]) {
-    if (!__ballot(ref == NEG_INF)) {
-      const float rs = raw(t, p, ref);
-      if (!__ballot(!(rs <= SUM_MAX))) {
-        sum += rs;
-        return;
-      }
-    }
+  BPT_DEV void weights(f32x16 (&t)[N], f32x16 (&acc)[DT]) {
     float mx = NEG_INF;
 #pragma unroll
     for (int x = 0; x < N; ++x)
 #pragma unroll
       for (int r = 0; r < 16; ++r) mx = fmaxf(mx, t[x][r]);
-    const float m = fmaxf(ref, max_halves(mx) * c), use = m == NEG_INF ? 0.0f : m;
-    const float corr = fast_exp2(ref - use);         // 0 for a row that starts
-    sum *= corr;
+    mx = max_halves(mx) * c;
+    const bool move = mx > ref + GROWTH;             // also from -inf
+    if (__ballot(move)) {
+      const float corr = move ? fast_exp2(ref - mx) : 1.0f;   // 0 for a row that starts
+      sum *= corr;
 #pragma unroll
-    for (int d = 0; d < DT; ++d) acc[d] *= corr;
-    ref = m;
-    sum += raw(t, p, use);
+      for (int d = 0; d < DT; ++d) acc[d] *= corr;
+      ref = move ? mx : ref;
+    }
+    const float use = ref == NEG_INF ? 0.0f : ref;
+#pragma unroll
+    for (int x = 0; x < N; ++x)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        t[x][r] = fast_exp2(fmaf(t[x][r], c, -use));
+        sum += t[x][r];
+      }
   }
 };
 
