@@ -1317,12 +1317,13 @@ static bool attn_few(const bpt_attn_config& c) {
   return c.dtype == BPT_BF16 && (rows <= 32 || (rows + 127) / 128 * c.Hkv * c.B <= 64);
 }
 // Slices of the keys for a forward of few rows: enough workgroups for the chip, and 128 keys (bf16: a tile per wave) at
-// least for each.
+// least for each; none where a workgroup is done with them before a second launch would be.
 static int attn_nsplit(const bpt_attn_config& c) {
   const bool bf = c.dtype == BPT_BF16;
   if (bf && !attn_few(c)) return 1;
   const int64_t rows = c.Sq * (c.Hq / c.Hkv), groups = (rows + (bf ? 31 : 15)) / (bf ? 32 : 16) * c.Hkv * c.B;
   const int64_t span = c.window ? std::min(c.Skv, (c.causal ? 1 : 2) * c.window + c.sinks + c.Sq) : c.Skv;
+  if (span <= 512) return 1;
   return (int)std::max<int64_t>(1, std::min<int64_t>({1024 / groups, span / (bf ? 128 : 512), 64}));
 }
 

@@ -30,6 +30,11 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 1 : 2) void win_dq_bf16_kernel(W
 #pragma unroll
   for (int t = 0; t < C::DT; ++t) acc[t] = f32x16{};
   if (tiles.n > 0) {
+    const RingOff<DH, NW> roff = ring_offsets<DH, NW>(a.k_st, a.v_st, wave, lane);
+    auto issue = [&](int j) {
+      issue_keys<DH, NW>(smem + (j % C::NS) * C::STAGE, Kb, a.k_st, Vb, a.v_st, tiles.key0(j), w.run, roff, wave, lane);
+    };
+    ring_start<C>(tiles.n, issue);                     // on their way before anything is waited for
     bf16x8 qf[C::KSTEPS], dof[C::KSTEPS];
     const int64_t i = w.safe(sq);
     {
@@ -47,44 +52,45 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 1 : 2) void win_dq_bf16_kernel(W
     const float nl = a.nlse[sidx], ndl = a.ndelta[sidx];
     settle(nl);
     settle(ndl);
-    const RingOff<DH, NW> roff = ring_offsets<DH, NW>(a.k_st, a.v_st, wave, lane);
-    auto issue = [&](int j) {
-      issue_keys<DH, NW>(smem + (j % C::NS) * C::STAGE, Kb, a.k_st, Vb, a.v_st, tiles.key0(j), w.run, roff, wave, lane);
-    };
     auto tile = [&](int j, int k0, bool all) {
       const char* kt = smem + (j % C::NS) * C::STAGE;
       const char* vt = kt + C::TB;
-      f32x16 s[2], dp[2];
 #pragma unroll
       for (int mt = 0; mt < 2; ++mt) {
+        f32x16 s[1], dp;
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
-          s[mt][r] = nl;                               // the MFMAs leave (score - lse) / scale
-          dp[mt][r] = ndl;                             // and dP^T - Delta
+          s[0][r] = nl;                                // the MFMAs leave (score - lse) / scale
+          dp[r] = ndl;                                 // and dP^T - Delta
         }
 #pragma unroll
         for (int kk = 0; kk < C::KSTEPS; ++kk) {
-          s[mt] = mfma32x32x16(frag_rows<DH>(kt, 32 * mt, 2 * kk, lane), qf[kk], s[mt]);
-          dp[mt] = mfma32x32x16(frag_rows<DH>(vt, 32 * mt, 2 * kk, lane), dof[kk], dp[mt]);
+          s[0] = mfma32x32x16(frag_rows<DH>(kt, 32 * mt, 2 * kk, lane), qf[kk], s[0]);
+          dp = mfma32x32x16(frag_rows<DH>(vt, 32 * mt, 2 * kk, lane), dof[kk], dp);
         }
 #pragma unroll
-        for (int r = 0; r < 16; ++r) s[mt][r] = fast_exp2(s[mt][r] * c) * dp[mt][r];
-      }
-      if (!all) w.mask(s, k0, lane, 0.0f);
-#pragma unroll
-      for (int mt = 0; mt < 2; ++mt)
+        for (int r = 0; r < 16; ++r) s[0][r] = fast_exp2(s[0][r] * c) * dp[r];
+        if (!all) {
+          pin(s[0]);
+          w.mask(s, k0 + 32 * mt, lane, 0.0f);
+        }
 #pragma unroll
         for (int hf = 0; hf < 2; ++hf) {
-          const bf16x8 sb = acc_to_b(s[mt], hf);
+          const bf16x8 sb = acc_to_b(s[0], hf);
 #pragma unroll
           for (int t = 0; t < C::DT; ++t)
             acc[t] = mfma32x32x16(frag_tr<DH>(kt, 32 * mt + 16 * hf, 32 * t, lane), sb, acc[t]);
         }
+      }
     };
     ring_loop<C, C::DPS>(tiles.n, issue, [&](int j) {
       const int k0 = tiles.key0(j);
       if (!w.none(k0)) tile(j, k0, w.all(k0));
     });
+  }
+  if (!w.exists) {
+#pragma unroll
+    for (int t = 0; t < C::DT; ++t) acc[t] = f32x16{};
   }
   if (w.i < a.Sq)
     store_rows<DH>((bf16*)a.dq + (int64_t)b * a.q_sb + (int64_t)w.i * a.q_st + (int64_t)h * a.q_sh, acc, a.scale, lane);
@@ -139,8 +145,8 @@ __global__ __launch_bounds__(64 * KG * QH, KG * QH == 8 ? 1 : 2) void win_dkdv_b
   const int per = FAR ? (nt * a.G + a.far - 1) / a.far : nt * a.G;
   const int j0 = chunk * per, n = min(per, nt * a.G - j0);
   if (n > 0) {
-    QVis mine = qvis_of(a, sq, key, key, near), first{0, -1}, last{0, -1};
-    if (key >= sq.nk) mine.hi = -1;
+    // keys behind the sequence's last stand for it; their results are left out in the end
+    QVis mine = qvis_of(a, sq, min(key, sq.nk - 1), min(key, sq.nk - 1), near), first{0, -1}, last{0, -1};
     const int kl = min(kw + 31, kend - 1);
     if (kw < sq.nk) {
       first = qvis_of(a, sq, kw, kw, near);
@@ -148,7 +154,18 @@ __global__ __launch_bounds__(64 * KG * QH, KG * QH == 8 ? 1 : 2) void win_dkdv_b
     }
     // the queries that all of the wave's keys see: the first key behind the sinks has the lowest end
     const int ks = !near && kw < a.sinks && a.sinks <= kl ? a.sinks : kw;
-    const int all_lo = max(first.lo, last.lo), all_hi = kw + 31 < sq.nk ? min(qvis_of(a, sq, ks, ks, near).hi, last.hi) : -1;
+    const int all_lo = max(first.lo, last.lo), all_hi = min(qvis_of(a, sq, ks, ks, near).hi, last.hi);
+    auto issue = [&](int j) {
+      const int it = j0 + j, h = kvh * a.G + it / nt, q0 = 64 * (t0 + it % nt);
+      char* st = smem + (j % C::NS) * C::STAGE;
+      issue_picked<DH, NW>(st, (const bf16*)a.q + (int64_t)b * a.q_sb + (int64_t)h * a.q_sh, a.q_st,
+                           (const bf16*)a.dout + (int64_t)b * a.o_sb + (int64_t)h * a.o_sh, a.o_st, q0, wave, lane,
+                           [&](int q) { return min(max(q, run.lo), run.hi); });
+      const int64_t sidx = ((int64_t)b * a.Hq + h) * a.Sqp + q0;       // Sqp % 64 == 0: in bounds
+      dma4s(scalar_ptr(a.nlse + sidx), 4u * lane, st + 2 * C::TB);
+      dma4s(scalar_ptr(a.ndelta + sidx), 4u * lane, st + 2 * C::TB + 256);
+    };
+    ring_start<C>(n, issue);
     bf16x8 kf[C::KSTEPS], vf[C::KSTEPS];
     {
       const int64_t kr = min(key, kend - 1);
@@ -162,16 +179,6 @@ __global__ __launch_bounds__(64 * KG * QH, KG * QH == 8 ? 1 : 2) void win_dkdv_b
         settle(vf[kk]);
       }
     }
-    auto issue = [&](int j) {
-      const int it = j0 + j, h = kvh * a.G + it / nt, q0 = 64 * (t0 + it % nt);
-      char* st = smem + (j % C::NS) * C::STAGE;
-      issue_picked<DH, NW>(st, (const bf16*)a.q + (int64_t)b * a.q_sb + (int64_t)h * a.q_sh, a.q_st,
-                           (const bf16*)a.dout + (int64_t)b * a.o_sb + (int64_t)h * a.o_sh, a.o_st, q0, wave, lane,
-                           [&](int q) { return min(max(q, run.lo), run.hi); });
-      const int64_t sidx = ((int64_t)b * a.Hq + h) * a.Sqp + q0;       // Sqp % 64 == 0: in bounds
-      dma4s(scalar_ptr(a.nlse + sidx), 4u * lane, st + 2 * C::TB);
-      dma4s(scalar_ptr(a.ndelta + sidx), 4u * lane, st + 2 * C::TB + 256);
-    };
     auto half = [&](int j, int q0, int mt, bool all) {
       const char* qs = smem + (j % C::NS) * C::STAGE;
       const char* ds = qs + C::TB;
@@ -200,12 +207,15 @@ __global__ __launch_bounds__(64 * KG * QH, KG * QH == 8 ? 1 : 2) void win_dkdv_b
       if (!all) {
         const int base = q0 + 32 * mt + 4 * (lane >> 5);
         const int lo = mine.lo - base, hi = mine.hi - base, end = run.hi - base;
+        auto where = [&](auto seen) {
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          const int q = 8 * (r >> 2) + (r & 3);
-          const bool in = q >= lo && q <= hi;
-          const bool ok = !FAR ? in : q <= end && (a.causal ? q > hi : !in);
-          s[r] = ok ? s[r] : 0.0f;
+          for (int r = 0; r < 16; ++r) s[r] = seen(8 * (r >> 2) + (r & 3)) ? s[r] : 0.0f;
+        };
+        if constexpr (FAR) {
+          where([&](int q) { return q <= end && (q > hi || (!a.causal && q < lo)); });
+        } else {                                     // one comparison per score across one end of the window
+          if (q0 + 63 > all_hi) where([&](int q) { return q <= hi; });
+          if (q0 < all_lo) where([&](int q) { return q >= lo; });
         }
       }
 #pragma unroll
@@ -258,6 +268,10 @@ __global__ __launch_bounds__(64 * KG * QH, KG * QH == 8 ? 1 : 2) void win_dkdv_b
         adk[t][r] += red[(32 * t + r) * 64];
         adv[t][r] += red[(32 * t + 16 + r) * 64];
       }
+  }
+  if (key >= sq.nk) {
+#pragma unroll
+    for (int t = 0; t < C::DT; ++t) adv[t] = adk[t] = f32x16{};
   }
   if (a.far > 0 && key < min(a.sinks, a.Skv)) {
     // slot 0: the window's part, then 2 per chunk; [slot, B Hkv, sinks, dK and dV, dh]

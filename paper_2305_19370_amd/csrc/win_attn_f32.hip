@@ -247,10 +247,10 @@ __global__ __launch_bounds__(256) void win_dq_f32_kernel(WinArgs a) {
   }
 }
 
-// dK, dV: 16 keys (FAR: 16 sinks and a chunk of the queries beyond their window, as in the bf16 kernel); wave w takes every fourth (query head, tile of 16 queries) pair of the kv head, in order. P
+// dK, dV: 16 keys (FAR: 16 sinks and a chunk of the queries beyond their window, as in the bf16 kernel); each of 8 waves takes every eighth (query head, tile of 16 queries) pair of the kv head, in order. P
 // and dS have the key on the lane axis and are the B operands of dV^T += dO^T P, dK^T += Q^T dS.
 template <int DH, bool FAR>
-__global__ __launch_bounds__(256) void win_dkdv_f32_kernel(WinArgs a) {
+__global__ __launch_bounds__(512) void win_dkdv_f32_kernel(WinArgs a) {
   constexpr int NC = DH / 16;
   __shared__ __attribute__((aligned(16))) float red[4][16][DH + 4];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, g = lane >> 4, c16 = lane & 15;
@@ -273,7 +273,7 @@ __global__ __launch_bounds__(256) void win_dkdv_f32_kernel(WinArgs a) {
     const RowFrag<DH> vf = row_frag<DH>((const float*)a.v + (int64_t)b * a.v_sb + (int64_t)kvh * a.v_sh + (int64_t)kr * a.v_st, g);
     const int t0 = run.lo / 16, nt = run.hi >= run.lo ? run.hi / 16 + 1 - t0 : 0;
     const int per = FAR ? (nt * a.G + a.far - 1) / a.far : nt * a.G;
-    for (int it = chunk * per + wave; it < min((chunk + 1) * per, nt * a.G); it += 4) {
+    for (int it = chunk * per + wave; it < min((chunk + 1) * per, nt * a.G); it += 8) {
       const int h = kvh * a.G + it / nt, q0 = 16 * (t0 + it % nt);
       const float* Qb = (const float*)a.q + (int64_t)b * a.q_sb + (int64_t)h * a.q_sh;
       const float* dOb = (const float*)a.dout + (int64_t)b * a.o_sb + (int64_t)h * a.o_sh;
@@ -299,13 +299,22 @@ __global__ __launch_bounds__(256) void win_dkdv_f32_kernel(WinArgs a) {
   }
 #pragma unroll
   for (int which = 0; which < 2; ++which) {
+    f32x4 (&x)[NC] = which ? dv : dk;
     __syncthreads();
+    if (wave >= 4)
 #pragma unroll
-    for (int t = 0; t < NC; ++t) *(f32x4*)&red[wave][c16][16 * t + 4 * g] = which ? dv[t] : dk[t];
+      for (int t = 0; t < NC; ++t) *(f32x4*)&red[wave - 4][c16][16 * t + 4 * g] = x[t];
+    __syncthreads();
+    if (wave < 4)
+#pragma unroll
+      for (int t = 0; t < NC; ++t) {
+        f32x4* at = (f32x4*)&red[wave][c16][16 * t + 4 * g];
+        *at = x[t] + *at;
+      }
     __syncthreads();
     const int64_t base = which ? (int64_t)b * a.v_sb + (int64_t)kvh * a.v_sh : (int64_t)b * a.k_sb + (int64_t)kvh * a.k_sh;
     float* out = (float*)(which ? a.dv : a.dk) + base;
-    for (int e = tid; e < 16 * (DH / 4); e += 256) {
+    for (int e = tid; e < 16 * (DH / 4); e += 512) {
       const int ki = e / (DH / 4), d = 4 * (e % (DH / 4));
       const int ns = a.far > 0 ? min(a.sinks, a.Skv) : 0;
       if (k0 + ki >= (FAR ? ns : a.Skv)) continue;
@@ -356,13 +365,13 @@ __global__ __launch_bounds__(256) void win_sinks_kernel(WinArgs a, int slots) {
 template <int DH>
 static hipError_t dkdv_f32(const WinArgs& a, hipStream_t s) {
   auto k = win_dkdv_f32_kernel<DH, false>;
-  hipLaunchKernelGGL(k, dim3((a.Skv + 15) / 16, a.Hkv, a.B), dim3(256), 0, s, a);
+  hipLaunchKernelGGL(k, dim3((a.Skv + 15) / 16, a.Hkv, a.B), dim3(512), 0, s, a);
   return hipGetLastError();
 }
 template <int DH>
 static hipError_t far_f32(const WinArgs& a, hipStream_t s) {
   auto k = win_dkdv_f32_kernel<DH, true>;
-  hipLaunchKernelGGL(k, dim3((std::min(a.sinks, a.Skv) + 15) / 16 * a.far, a.Hkv, a.B), dim3(256), 0, s, a);
+  hipLaunchKernelGGL(k, dim3((std::min(a.sinks, a.Skv) + 15) / 16 * a.far, a.Hkv, a.B), dim3(512), 0, s, a);
   return hipGetLastError();
 }
 template <int DH>

@@ -31,6 +31,11 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 1 : 2) void win_fwd_bf16_kernel(
   for (int t = 0; t < C::DT; ++t) acc[t] = f32x16{};
   float ref = NEG_INF, l_run = 0.0f;                // the row's reference maximum, base 2
   if (tiles.n > 0) {
+    const RingOff<DH, NW> roff = ring_offsets<DH, NW>(a.k_st, a.v_st, wave, lane);
+    auto issue = [&](int j) {
+      issue_keys<DH, NW>(smem + (j % C::NS) * C::STAGE, Kb, a.k_st, Vb, a.v_st, tiles.key0(j), w.run, roff, wave, lane);
+    };
+    ring_start<C>(tiles.n, issue);                     // on their way before anything is waited for
     bf16x8 qf[C::KSTEPS];
     {
       const bf16* q = (const bf16*)a.q + (int64_t)b * a.q_sb + (int64_t)w.safe(sq) * a.q_st + (int64_t)h * a.q_sh;
@@ -40,21 +45,17 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 1 : 2) void win_fwd_bf16_kernel(
         settle(qf[kk]);
       }
     }
-    const RingOff<DH, NW> roff = ring_offsets<DH, NW>(a.k_st, a.v_st, wave, lane);
-    auto issue = [&](int j) {
-      issue_keys<DH, NW>(smem + (j % C::NS) * C::STAGE, Kb, a.k_st, Vb, a.v_st, tiles.key0(j), w.run, roff, wave, lane);
-    };
     OnlineRows<C::DT> sm{c};
-    auto tile = [&](int j, int k0, bool all) {
+    auto scores = [&](int j, f32x16 (&t)[2]) {
       const char* kt = smem + (j % C::NS) * C::STAGE;
-      const char* vt = kt + C::TB;
-      f32x16 t[2] = {f32x16{}, f32x16{}};
+      t[0] = t[1] = f32x16{};
 #pragma unroll
       for (int kk = 0; kk < C::KSTEPS; ++kk)
 #pragma unroll
         for (int mt = 0; mt < 2; ++mt) t[mt] = mfma32x32x16(frag_rows<DH>(kt, 32 * mt, 2 * kk, lane), qf[kk], t[mt]);
-      if (!all) w.mask(t, k0, lane, NEG_INF);
-      sm.weights(t, acc);
+    };
+    auto add_values = [&](int j, const f32x16 (&t)[2]) {
+      const char* vt = smem + (j % C::NS) * C::STAGE + C::TB;
 #pragma unroll
       for (int mt = 0; mt < 2; ++mt)
 #pragma unroll
@@ -65,18 +66,55 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 1 : 2) void win_fwd_bf16_kernel(
             acc[d] = mfma32x32x16(frag_tr<DH>(vt, 32 * mt + 16 * hf, 32 * d, lane), pb, acc[d]);
         }
     };
-    ring_loop<C, C::DPS>(tiles.n, issue, [&](int j) {
+    auto edge = [&](int j) {                          // a tile that not every row sees in full, or has no reference for
       const int k0 = tiles.key0(j);
-      if (!w.none(k0)) tile(j, k0, w.all(k0));
-    });
+      if (w.none(k0)) return;
+      f32x16 t[2];
+      scores(j, t);
+      if (!w.all(k0)) w.mask(t, k0, lane, NEG_INF);
+      sm.weights(t, acc);
+      add_values(j, t);
+    };
+    auto inner = [&](int j) {                         // weights against the reference as it stands
+      f32x16 t[2];
+      scores(j, t);
+      const float rs = sm.raw(t, sm.ref);
+      if (sm.over(rs)) {                              // rare: a score far above the reference
+        scores(j, t);
+        sm.weights(t, acc);
+      } else {
+        sm.sum += rs;
+      }
+      add_values(j, t);
+    };
+    auto step = [&](int j) { ring_step<C, C::DPS>(j, tiles.n, issue); };
+    int ja, jb, j = 0;
+    w.full_tiles(tiles, ja, jb);
+    for (; j < min(ja + 1, tiles.n); ++j) {           // the first full tile gives every row a reference
+      step(j);
+      edge(j);
+    }
+    for (; j < jb; ++j) {
+      step(j);
+      inner(j);
+    }
+    for (; j < tiles.n; ++j) {
+      step(j);
+      edge(j);
+    }
     ref = sm.ref;
     l_run = sm.sum;
   }
   const float l = sum_halves(l_run);
   if (w.i < a.Sq) {
-    const float inv = l > 0.0f ? 1.0f / l : 0.0f;   // a row that sees nothing: 0
+    const bool sees = l > 0.0f && w.exists;          // a row that sees nothing: 0
+    const float inv = sees ? 1.0f / l : 0.0f;
+    if (!sees) {
+#pragma unroll
+      for (int d = 0; d < C::DT; ++d) acc[d] = f32x16{};
+    }
     store_rows<DH>((bf16*)a.o + (int64_t)b * a.o_sb + (int64_t)w.i * a.o_st + (int64_t)h * a.o_sh, acc, inv, lane);
-    if (lane < 32) a.lse[((int64_t)b * a.Hq + h) * a.lse_ld + w.i] = l > 0.0f ? (ref + log2f(l)) * LN2 : NEG_INF;
+    if (lane < 32) a.lse[((int64_t)b * a.Hq + h) * a.lse_ld + w.i] = sees ? (ref + log2f(l)) * LN2 : NEG_INF;
   }
 }
 
@@ -186,6 +224,7 @@ __global__ __launch_bounds__(256, 1) void win_token_kernel(WinArgs a) {
     float m = NEG_INF, lt = 0.0f;
 #pragma unroll
     for (int v = 0; v < C::NW; ++v) m = fmaxf(m, red_m[v * 32 + ri]);
+    if (rr / a.G >= sq.nq) m = NEG_INF;
     f32x4 o = {};
     if (m > NEG_INF) {
 #pragma unroll
@@ -205,7 +244,7 @@ __global__ __launch_bounds__(256, 1) void win_token_kernel(WinArgs a) {
       continue;
     }
     const int i = rr / a.G, hq = kvh * a.G + rr % a.G;
-    const float inv = lt > 0.0f ? 1.0f / lt : 0.0f;
+    const float inv = lt > 0.0f ? 1.0f / lt : 0.0f;   // a row that sees nothing: 0
     bf16x4 x;
 #pragma unroll
     for (int k = 0; k < 4; ++k) x[k] = (bf16)(o[k] * inv);

@@ -6,9 +6,11 @@
 
 namespace bpt {
 
-// Waves of workgroups of 256 rows (8 waves, one workgroup on a CU) or 128 (4, two): the small ones where the large would
-// leave CUs idle.
-inline bool win_wide(int64_t len, const WinArgs& a) { return (len * a.G + 255) / 256 * a.Hkv * a.B > 256; }
+// Workgroups of 256 rows (8 waves, one on a CU) or of 128 (4, two on a CU, one at its start or end while the other works): large
+// ones for long runs of tiles that fill the chip. Full attention, 32768 tokens, 32 heads of 128, forward / dQ: 9.1 / 11.0 ms
+// (small: 9.5 / 11.3). Window of 1024, 8192 tokens, 16 heads: small 105 / 135 us (large: 120 / 146); of 4096, 16384 tokens: 544 / 677
+// (573 / 697).
+inline bool win_wide(int64_t len, const WinArgs& a) { return !a.window && (len * a.G + 255) / 256 * a.Hkv * a.B > 256; }
 
 template <int N = 0> BPT_DEV void wait_lgkm() { asm volatile("s_waitcnt lgkmcnt(%0)" ::"n"(N) : "memory"); }
 
@@ -28,45 +30,59 @@ struct WinCfg {
 };
 
 // Row r0 + w0 + lane % 32 of a kv head's list r = token * G + head, what it sees, and what its wave and its
-// workgroup of n rows (from r0) see.
+// workgroup of n rows (from r0) see. Rows behind the sequence's last stand for its last: they need no masks of their own, and
+// their results are left out in the end.
 struct Rows {
   int i, head;                 // token, query head in its group
-  bool full;                   // all the wave's rows exist
-  Vis mine, first, last, run;  // the row; the wave's first and last row that exist; the workgroup
+  bool exists;
+  Vis mine, first, last, run;  // the row; the wave's first and last row; the workgroup
+  int f_lo, f_hi;              // keys that all rows of the workgroup see
   BPT_DEV Rows(const WinArgs& a, const Seq& s, int r0, int w0, int n, int lane) {
     const int r = r0 + w0 + (lane & 31);
     i = r / a.G;
     head = r - i * a.G;
-    const int last_i = s.nq - 1;
+    const int end = s.nq - 1;
+    exists = i <= end;
+    const int i0 = r0 / a.G, i1 = (r0 + n - 1) / a.G;
     mine = first = last = run = Vis{0, -1, 0};
-    if (i <= last_i) mine = vis_of(a, s, s.off + i, s.off + i);
-    const int i0 = r0 / a.G, i1 = min((r0 + n - 1) / a.G, last_i);
-    if (i0 <= i1) run = vis_run(a, s, s.off + i0, s.off + i1);
-    const int wi0 = (r0 + w0) / a.G, wi1 = (r0 + w0 + 31) / a.G;
-    full = wi1 <= last_i;
-    if (wi0 <= last_i) {
-      first = vis_of(a, s, s.off + wi0, s.off + wi0);
-      const int e = s.off + min(wi1, last_i);
-      last = vis_of(a, s, e, e);
-    }
+    f_lo = 0, f_hi = -1;
+    if (i0 > end) return;      // the workgroup has no row
+    auto at = [&](int t) { const int p = s.off + min(t, end); return vis_of(a, s, p, p); };
+    mine = at(i);
+    first = at((r0 + w0) / a.G);
+    last = at((r0 + w0 + 31) / a.G);
+    run = vis_run(a, s, s.off + i0, s.off + min(i1, end));
+    f_lo = at(i1).lo;
+    f_hi = at(i0).hi;
   }
-  // a row that exists, for rows that do not
+  // the token whose row is read
   BPT_DEV int safe(const Seq& s) const { return min(i, s.nq - 1); }
   // whether all the wave's rows see all of keys k0 .. k0 + 63, or none sees any
-  BPT_DEV bool all(int k0) const { return full && ((k0 >= last.lo && k0 + 63 <= first.hi) || k0 + 63 < first.se); }
+  BPT_DEV bool all(int k0) const { return (k0 >= last.lo && k0 + 63 <= first.hi) || k0 + 63 < first.se; }
   BPT_DEV bool none(int k0) const { return !(k0 <= last.hi && k0 + 63 >= first.lo) && k0 >= last.se; }
-  // scores t[mt][r] of keys k0 + 32 mt + acc_row(r, lane)
+  // the tiles ja <= j < jb of the list (behind those of the sinks) that all rows of the workgroup see in full
+  BPT_DEV void full_tiles(const Tiles<64>& t, int& ja, int& jb) const {
+    ja = max((f_lo + 63) / 64 - t.first, 0) + t.ns;
+    jb = max(min(max(f_hi + 1, 0) / 64 - t.first + t.ns, t.n), ja);
+  }
+  // `out` in place of the scores t[mt][r] of keys k0 + 32 mt + acc_row(r, lane) that the row does not see. One comparison per
+  // score where the tile lies across one end of the window only.
   template <int N>
   BPT_DEV void mask(f32x16 (&t)[N], int k0, int lane, float out) const {
     const int base = k0 + 4 * (lane >> 5);
     const int lo = mine.lo - base, hi = mine.hi - base, se = mine.se - base;
+    auto where = [&](auto seen) {
 #pragma unroll
-    for (int mt = 0; mt < N; ++mt)
+      for (int mt = 0; mt < N; ++mt)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        const int k = 32 * mt + 8 * (r >> 2) + (r & 3);
-        t[mt][r] = (k >= lo && k <= hi) || k < se ? t[mt][r] : out;
-      }
+        for (int r = 0; r < 16; ++r) t[mt][r] = seen(32 * mt + 8 * (r >> 2) + (r & 3)) ? t[mt][r] : out;
+    };
+    if (k0 < last.se) {
+      where([&](int k) { return (k >= lo && k <= hi) || k < se; });
+    } else {
+      if (k0 + 32 * N - 1 > first.hi) where([&](int k) { return k <= hi; });
+      if (k0 < last.lo) where([&](int k) { return k >= lo; });
+    }
   }
 };
 
@@ -112,6 +128,21 @@ struct OnlineRows {
   static constexpr float GROWTH = 8.0f;
   float c;                                           // scale log2(e)
   float ref = NEG_INF, sum = 0.0f;
+  // whether a lane's sum of weights against the present references is too large
+  BPT_DEV static bool over(float rs) { return __ballot(!(rs <= 65536.0f)) != 0; }
+  // products t become weights against m; the lane's sum
+  template <int N>
+  BPT_DEV float raw(f32x16 (&t)[N], float m) const {
+    float rs = 0.0f;
+#pragma unroll
+    for (int x = 0; x < N; ++x)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        t[x][r] = fast_exp2(fmaf(t[x][r], c, -m));
+        rs += t[x][r];
+      }
+    return rs;
+  }
   // products t (-inf where unseen) become weights; acc is rescaled where the reference moves
   template <int N>
   BPT_DEV void weights(f32x16 (&t)[N], f32x16 (&acc)[DT]) {
@@ -129,31 +160,31 @@ struct OnlineRows {
       for (int d = 0; d < DT; ++d) acc[d] *= corr;
       ref = move ? mx : ref;
     }
-    const float use = ref == NEG_INF ? 0.0f : ref;
-#pragma unroll
-    for (int x = 0; x < N; ++x)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        t[x][r] = fast_exp2(fmaf(t[x][r], c, -use));
-        sum += t[x][r];
-      }
+    sum += raw(t, ref == NEG_INF ? 0.0f : ref);
   }
 };
 
-// Walks n stages of the ring (C::NS slots, DPS copies per wave and stage): body(j) runs with stage j in
-// LDS. Every wave of the workgroup reaches every barrier.
-template <class C, int DPS, class Issue, class Body>
-BPT_DEV void ring_loop(int n, const Issue& issue, const Body& body) {
+// Makes stage j of n visible to the workgroup and fills the slot of stage j - 1 (C::NS slots; DPS copies per wave and
+// stage): stage j has landed once at most the stages issued after it are pending. Every wave calls it.
+template <class C, int DPS, class Issue>
+BPT_DEV void ring_step(int j, int n, const Issue& issue) {
+  if (C::NS == 4 && j + 2 < n) wait_vmcnt<2 * DPS>();
+  else if (C::NS == 4 && j + 1 < n) wait_vmcnt<DPS>();
+  else wait_vmcnt<0>();
+  __syncthreads();                                  // every wave is done with stage j - 1
+  if (j + C::NS - 1 < n) issue(j + C::NS - 1);
+}
+template <class C, class Issue>
+BPT_DEV void ring_start(int n, const Issue& issue) {
 #pragma unroll
   for (int st = 0; st < C::NS - 1; ++st)
     if (st < n) issue(st);
+}
+// Walks n stages of a ring that has been started: body(j) runs with stage j in LDS
+template <class C, int DPS, class Issue, class Body>
+BPT_DEV void ring_loop(int n, const Issue& issue, const Body& body) {
   for (int j = 0; j < n; ++j) {
-    // stage j has landed once at most the stages issued after it are pending
-    if (C::NS == 4 && j + 2 < n) wait_vmcnt<2 * DPS>();
-    else if (C::NS == 4 && j + 1 < n) wait_vmcnt<DPS>();
-    else wait_vmcnt<0>();
-    __syncthreads();                                // stage j visible; every wave is done with stage j - 1
-    if (j + C::NS - 1 < n) issue(j + C::NS - 1);    // into the slot of stage j - 1
+    ring_step<C, DPS>(j, n, issue);
     body(j);
   }
 }
