@@ -400,6 +400,27 @@ bpt_status bpt_attn_bwd(const bpt_attn_config* cfg, const void* Q, const void* K
                         const int32_t* kv_lens, const void* O, const float* lse, const void* dO, void* dQ, void* dK,
                         void* dV, void* workspace, size_t workspace_bytes, void* stream);
 
+/* The layer with rotary positions and / or windowed attention: Q and K turn after their projection (both
+ * heads' worth in place in `saved`), and a query sees window tokens and the sinks. rot = 0: no rotary
+ * positions; window = 0: full attention. Everything else, `saved` and the workspace sizes included, is as for
+ * bpt_layer_fwd / bpt_layer_bwd, whose results a call with rot = window = 0 gives; give the same options to
+ * both. (bpt_bwd_qkv_grad_offset holds for window = 0: with a window the backward leaves dQ, dK, dV
+ * token-major, [T, 3D].) */
+typedef struct {
+  int64_t rot, pos0, orig_len;           /* as in bpt_rope_config; token s stands at pos0 + s     */
+  double theta, factor, beta_fast, beta_slow, mscale;
+  int32_t interleaved, scaling;
+  int64_t window, sinks;                 /* as in bpt_attn_config                                 */
+} bpt_layer_options;
+
+bpt_status bpt_layer_options_validate(const bpt_config* cfg, const bpt_layer_options* options);
+bpt_status bpt_layer_fwd_options(const bpt_config* cfg, const bpt_layer_options* options, const void* X,
+                                 const bpt_params* params, void* Y, void* saved, void* workspace, size_t workspace_bytes,
+                                 void* stream);
+bpt_status bpt_layer_bwd_options(const bpt_config* cfg, const bpt_layer_options* options, const void* X,
+                                 const bpt_params* params, const void* saved, const void* dY, void* dX,
+                                 const bpt_grads* grads, void* workspace, size_t workspace_bytes, void* stream);
+
 /* One AdamW step on a list of tensors (bpt_adamw_step's formula on each, weight decay per tensor). Moments in 32
  * bits: m and v, fp32. In 8 bits: m and r = sqrt(v), each as one e4m3 byte (sign, 4 exponent and
  * 3 mantissa bits; 2^-9 .. 448) per element, and per block of 256 elements two bytes in `exps`: the moments of

@@ -138,7 +138,8 @@ struct WinArgs {
   const int32_t *q_lens = nullptr, *kv_lens = nullptr;   // [B] or null: all of Sq, Skv
   int B = 0, Sq = 0, Skv = 0, Hq = 0, Hkv = 0, G = 1, dh = 0;   // G = Hq / Hkv
   int causal = 0, window = 0, sinks = 0;   // window 0: none
-  float scale = 1.0f;                   // of the scores
+  float scale = 1.0f;                   // of the scores, and of dK
+  float dq_scale = 1.0f;                // of dQ: `scale`, unless q carries a factor of its own
   int few = 0;                          // bf16 forward: the kernel for few rows
   int nsplit = 1;                       // slices of the keys (fp32, or few)
   float *part_o = nullptr, *part_ml = nullptr;   // nsplit > 1: [nsplit, B Hkv Sq G] rows of dh, of (max, sum)
@@ -171,6 +172,9 @@ struct RopeArgs {
   double turns[64];                     // full turns per position of pair i < rot / 2
 };
 hipError_t rope(Dt t, const RopeArgs& a, hipStream_t s);
+// The same in place on a feature-major matrix: element (row, h, d) at x[(h dh + d) ldx + row / S Sp + row % S]; ldx, Sp
+// multiples of 8, columns S .. Sp of a sequence zero (they stay so). positions must be null.
+hipError_t rope_t(Dt t, const RopeArgs& a, int64_t Sp, hipStream_t s);
 
 // ---------------------------------------------------------------- AdamW over many tensors
 struct AdamTensor {

@@ -416,6 +416,185 @@ XentWs xent_ws(const XentDims& d, void* base, int backward, int64_t* total) {
   return w;
 }
 
+// ---------------------------------------------------------------- rotary positions, windowed attention: checks and arguments
+bpt_status dtype_ok(int32_t t, const char* what) {
+  if (t != BPT_F32 && t != BPT_BF16) return fail(BPT_ERR_INVALID_ARG, "%s %d is not a bpt_dtype", what, (int)t);
+  return BPT_OK;
+}
+Dt dt_of(int32_t t) { return t == BPT_BF16 ? BF16 : F32; }
+
+bpt_status rope_check(const bpt_rope_config* c) {
+  if (!c) return fail(BPT_ERR_INVALID_ARG, "config is NULL");
+  if (c->rows < 1 || c->S < 1 || c->H < 1 || c->dh < 1) return fail(BPT_ERR_INVALID_ARG, "rows, S, H and dh must be >= 1");
+  if (c->rot < 2 || c->rot % 2 || c->rot > c->dh)
+    return fail(BPT_ERR_INVALID_ARG, "rot = %lld must be even and lie in [2, dh]", (long long)c->rot);
+  if (c->scaling < BPT_ROPE_NONE || c->scaling > BPT_ROPE_BY_PARTS) return fail(BPT_ERR_INVALID_ARG, "scaling is not a bpt_rope_scaling");
+  if (!(c->theta > 0.0) || !std::isfinite(c->theta)) return fail(BPT_ERR_INVALID_ARG, "theta must be > 0");
+  if (!std::isfinite(c->mscale)) return fail(BPT_ERR_INVALID_ARG, "mscale must be finite");
+  if (c->scaling != BPT_ROPE_NONE && (!(c->factor >= 1.0) || !std::isfinite(c->factor)))
+    return fail(BPT_ERR_INVALID_ARG, "factor must be >= 1");
+  if (c->scaling == BPT_ROPE_BASE && c->rot == 2) return fail(BPT_ERR_INVALID_ARG, "BPT_ROPE_BASE needs rot > 2");
+  if (c->scaling == BPT_ROPE_BY_PARTS && (c->orig_len < 1 || !(c->beta_fast > c->beta_slow) || !std::isfinite(c->beta_fast) || !std::isfinite(c->beta_slow)))
+    return fail(BPT_ERR_INVALID_ARG, "BPT_ROPE_BY_PARTS needs orig_len >= 1 and beta_fast > beta_slow");
+  if ((c->interleaved != 0 && c->interleaved != 1) || c->reserved != 0)
+    return fail(BPT_ERR_INVALID_ARG, "interleaved must be 0 or 1, reserved 0");
+  if (c->H > (int64_t)1 << 20 || c->dh > (int64_t)1 << 16) return fail(BPT_ERR_UNSUPPORTED, "H or dh too large");
+  if (c->ldx < c->H * c->dh || c->ldy < c->H * c->dh) return fail(BPT_ERR_INVALID_ARG, "ldx and ldy must be >= H dh");
+  bpt_status st = dtype_ok(c->dtype, "dtype");
+  if (st != BPT_OK) return st;
+  if (c->dh % 8 || c->ldx % 8 || c->ldy % 8) return fail(BPT_ERR_UNSUPPORTED, "dh, ldx and ldy must be multiples of 8");
+  if (c->rot > 128) return fail(BPT_ERR_UNSUPPORTED, "rot = %lld > 128", (long long)c->rot);
+  if (c->rows > INT32_MAX || c->H * c->dh > INT32_MAX / 8 || c->ldx > (int64_t)1 << 40 || c->ldy > (int64_t)1 << 40)
+    return fail(BPT_ERR_UNSUPPORTED, "rows, H dh or a row stride too large");
+  const int64_t most = (int64_t)1 << 52;             // positions are exact in a double
+  if (c->pos0 > most || c->pos0 < -most || c->S > most) return fail(BPT_ERR_UNSUPPORTED, "pos0 or S too large");
+  return BPT_OK;
+}
+
+RopeArgs rope_args(const bpt_rope_config& c, const int32_t* positions, const void* x, int64_t ldx, void* y, int64_t ldy,
+                          float sign) {
+  RopeArgs a;
+  a.x = x; a.y = y; a.positions = positions;
+  a.rows = c.rows; a.S = c.S; a.ldx = ldx; a.ldy = ldy; a.pos0 = c.pos0;
+  a.H = (int)c.H; a.dh = (int)c.dh; a.rot = (int)c.rot; a.interleaved = c.interleaved;
+  a.mscale = (float)c.mscale; a.sign = sign;
+  const double pi2 = 6.283185307179586476925;
+  const double rot = (double)c.rot;
+  const double theta = c.scaling == BPT_ROPE_BASE ? c.theta * std::pow(c.factor, rot / (rot - 2.0)) : c.theta;
+  for (int i = 0; i < c.rot / 2; ++i) {
+    double f = std::pow(theta, -2.0 * i / rot);
+    if (c.scaling == BPT_ROPE_LINEAR) f /= c.factor;
+    if (c.scaling == BPT_ROPE_BY_PARTS) {
+      const double turns = (double)c.orig_len * f / pi2;
+      const double g = std::min(1.0, std::max(0.0, (turns - c.beta_slow) / (c.beta_fast - c.beta_slow)));
+      f *= g + (1.0 - g) / c.factor;
+    }
+    a.turns[i] = f / pi2;
+  }
+  return a;
+}
+
+// Chunks of what the sinks' keys see beyond their window in the backward: 0 where a block of keys that
+// holds sinks has little more to do than another, else workgroups for two a CU and at least two tiles
+// of 64 queries for each.
+int attn_far(const bpt_attn_config& c) {
+  if (c.sinks == 0 || c.window >= c.Skv) return 0;
+  const int64_t G = c.Hq / c.Hkv, tiles = (c.Sq - std::min(c.Sq, c.window) + 63) / 64 * G;
+  if (tiles < 16) return 0;
+  const int64_t groups = c.B * c.Hkv * ((std::min(c.sinks, c.Skv) + 31) / 32);
+  return (int)std::max<int64_t>(1, std::min(512 / groups, tiles / 2));
+}
+int attn_slots(const bpt_attn_config& c, int far) { return 1 + far * (c.dtype == BPT_BF16 ? 2 : 1); }
+
+// Whether no two elements of a tensor share a place (dims of stride and size; features are adjacent)
+bool apart(const bpt_attn_strides& t, int64_t B, int64_t S, int64_t H, int64_t dh) {
+  std::pair<int64_t, int64_t> d[] = {{t.sb, B}, {t.st, S}, {t.sh, H}};
+  std::sort(d, d + 3);
+  int64_t span = dh;
+  for (auto& e : d) {
+    if (e.second == 1) continue;
+    if (e.first < span) return false;
+    span += e.first * (e.second - 1);
+  }
+  return true;
+}
+
+constexpr int64_t kAttnMax = (int64_t)1 << 28;      // sums of a few lengths stay within 32 bits
+
+bpt_status attn_check(const bpt_attn_config* c) {
+  if (!c) return fail(BPT_ERR_INVALID_ARG, "config is NULL");
+  if (c->B < 1 || c->Sq < 1 || c->Skv < 1 || c->Hq < 1 || c->Hkv < 1 || c->dh < 1)
+    return fail(BPT_ERR_INVALID_ARG, "B, Sq, Skv, Hq, Hkv, dh must be >= 1");
+  if (c->Hq % c->Hkv) return fail(BPT_ERR_INVALID_ARG, "Hq=%lld is not a multiple of Hkv=%lld", (long long)c->Hq, (long long)c->Hkv);
+  if (c->window < 0 || c->sinks < 0 || (c->window == 0 && c->sinks != 0))
+    return fail(BPT_ERR_INVALID_ARG, "window and sinks must be >= 0, and sinks 0 without a window");
+  if (!(c->scale > 0.0f) || !std::isfinite(c->scale)) return fail(BPT_ERR_INVALID_ARG, "scale must be > 0");
+  if ((c->causal != 0 && c->causal != 1) || c->reserved != 0) return fail(BPT_ERR_INVALID_ARG, "causal must be 0 or 1, reserved 0");
+  bpt_status st = dtype_ok(c->dtype, "dtype");
+  if (st != BPT_OK) return st;
+  const bpt_attn_strides* all[] = {&c->q, &c->k, &c->v, &c->o};
+  const int64_t unit = 16 / (int64_t)esize(c->dtype);
+  for (auto* t : all) {
+    if (t->sb < 0 || t->st < 0 || t->sh < 0) return fail(BPT_ERR_INVALID_ARG, "strides must be >= 0");
+    if (t->sb % unit || t->st % unit || t->sh % unit) return fail(BPT_ERR_INVALID_ARG, "strides must be multiples of 16 bytes");
+    if (t->st >= (int64_t)1 << 22 || t->sb >= (int64_t)1 << 40 || t->sh >= (int64_t)1 << 40)
+      return fail(BPT_ERR_UNSUPPORTED, "a stride is too large");
+  }
+  if (c->dh != 64 && c->dh != 128) return fail(BPT_ERR_UNSUPPORTED, "head dim %lld unsupported (64 or 128)", (long long)c->dh);
+  if (c->B > 65535 || c->Hkv > 65535 || c->Hq > 65535) return fail(BPT_ERR_UNSUPPORTED, "B and heads must be <= 65535");
+  if (c->Sq > kAttnMax || c->Skv > kAttnMax || c->window > kAttnMax || c->sinks > kAttnMax || c->Sq * (c->Hq / c->Hkv) > kAttnMax)
+    return fail(BPT_ERR_UNSUPPORTED, "lengths, window and sinks must be <= 2^28, and Sq Hq / Hkv too");
+  // workgroups of 16 rows and rows of the log-sum-exp
+  if (c->B * c->Hkv * ((std::max(c->Sq * (c->Hq / c->Hkv), c->Skv) + 15) / 16) > (int64_t)1 << 26 || c->B * c->Hq * rup(c->Sq, 64) > (int64_t)1 << 32)
+    return fail(BPT_ERR_UNSUPPORTED, "B * heads * length too large");
+  if (!apart(c->o, c->B, c->Sq, c->Hq, c->dh)) return fail(BPT_ERR_INVALID_ARG, "strides of O overlap");
+  return BPT_OK;
+}
+
+WinArgs attn_args(const bpt_attn_config& c, const void* Q, const void* K, const void* V, const int32_t* q_lens,
+                         const int32_t* kv_lens, const void* O, const float* lse) {
+  WinArgs a;
+  a.q = Q; a.k = K; a.v = V; a.o = (void*)O; a.lse = (float*)lse; a.lse_ld = c.Sq;
+  a.q_sb = c.q.sb; a.q_st = (int)c.q.st; a.q_sh = c.q.sh;
+  a.k_sb = c.k.sb; a.k_st = (int)c.k.st; a.k_sh = c.k.sh;
+  a.v_sb = c.v.sb; a.v_st = (int)c.v.st; a.v_sh = c.v.sh;
+  a.o_sb = c.o.sb; a.o_st = (int)c.o.st; a.o_sh = c.o.sh;
+  a.q_lens = q_lens; a.kv_lens = kv_lens;
+  a.B = (int)c.B; a.Sq = (int)c.Sq; a.Skv = (int)c.Skv;
+  a.Hq = (int)c.Hq; a.Hkv = (int)c.Hkv; a.G = (int)(c.Hq / c.Hkv); a.dh = (int)c.dh;
+  a.causal = c.causal; a.window = (int)c.window; a.sinks = (int)c.sinks; a.scale = a.dq_scale = c.scale;
+  a.Sqp = rup(c.Sq, 64);
+  return a;
+}
+
+// visible pairs of a sequence of whole length, for the launch record
+double attn_seen(const bpt_attn_config& c) {
+  const double per = c.window ? (double)std::min(c.Skv, (c.causal ? 1 : 2) * c.window + c.sinks) : (double)c.Skv;
+  return (double)c.B * c.Hq * c.Sq * (c.causal && !c.window ? per - 0.5 * (double)std::min(c.Sq, c.Skv) : per);
+}
+
+// ---------------------------------------------------------------- a layer's options
+// The rotary configuration of the Q and K heads (columns [0, 2D) of the projection), and the window kernels' view of the
+// projection [T, 3D], for a layer with options.
+bpt_rope_config layer_rope(const bpt_config& c, const bpt_layer_options& o) {
+  bpt_rope_config r = {};
+  r.rows = c.B * c.S; r.S = c.S; r.H = 2 * c.H; r.dh = c.D / c.H; r.rot = o.rot;
+  r.ldx = r.ldy = 3 * c.D;
+  r.pos0 = o.pos0; r.orig_len = o.orig_len; r.theta = o.theta; r.factor = o.factor;
+  r.beta_fast = o.beta_fast; r.beta_slow = o.beta_slow; r.mscale = o.mscale;
+  r.interleaved = o.interleaved; r.scaling = o.scaling; r.dtype = c.dtype;
+  return r;
+}
+bpt_attn_config layer_attn(const bpt_config& c, const bpt_layer_options& o) {
+  bpt_attn_config a = {};
+  a.B = c.B; a.Sq = a.Skv = c.S; a.Hq = a.Hkv = c.H; a.dh = c.D / c.H;
+  a.q = a.k = a.v = {c.S * 3 * c.D, 3 * c.D, a.dh};
+  a.o = {c.S * c.D, c.D, a.dh};
+  a.window = o.window; a.sinks = o.sinks; a.causal = c.causal; a.dtype = c.dtype;
+  // bf16: Q carries log2(e)/sqrt(dh), so Q K^T are the scores times log2(e)
+  a.scale = c.dtype == BPT_BF16 ? (float)0.693147180559945309 : (float)(1.0 / std::sqrt((double)a.dh));
+  return a;
+}
+bpt_status options_check(const bpt_config* c, const bpt_layer_options* o) {
+  bpt_status st = check(c);
+  if (st != BPT_OK) return st;
+  if (!o) return fail(BPT_ERR_INVALID_ARG, "options is NULL");
+  if (o->rot != 0) {
+    const bpt_rope_config r = layer_rope(*c, *o);
+    if ((st = rope_check(&r)) != BPT_OK) return st;
+  }
+  if (o->window == 0 && o->sinks == 0) return BPT_OK;
+  const bpt_attn_config a = layer_attn(*c, *o);
+  return attn_check(&a);
+}
+WinArgs layer_win(const bpt_config& c, const bpt_layer_options& o, const Dims& d, const SavedPtrs& sv) {
+  const bpt_attn_config ac = layer_attn(c, o);
+  WinArgs a = attn_args(ac, sv.qkv, off(sv.qkv, d.D * (int64_t)d.E), off(sv.qkv, 2 * d.D * (int64_t)d.E), nullptr, nullptr, sv.o, sv.lse);
+  a.lse_ld = d.Sp;
+  a.dq_scale = (float)(1.0 / std::sqrt((double)d.dh));
+  return a;
+}
+
 }  // namespace
 
 // Workspace of bpt_layer_fwd_noalloc: the library's own device memory, one copy per GPU,
@@ -599,9 +778,9 @@ bpt_status bpt_layer_fwd_noalloc(const bpt_config* cfg, const void* X, const bpt
   return bpt_layer_fwd(cfg, X, p, Y, saved, ws, kScratchBytes, stream);
 }
 
-bpt_status bpt_layer_fwd(const bpt_config* cfg, const void* X, const bpt_params* p, void* Y, void* saved,
-                         void* ws, size_t ws_bytes, void* stream) {
-  bpt_status st = check(cfg);
+static bpt_status layer_fwd(const bpt_config* cfg, const bpt_layer_options* opt, const void* X, const bpt_params* p, void* Y,
+                            void* saved, void* ws, size_t ws_bytes, void* stream) {
+  bpt_status st = opt ? options_check(cfg, opt) : check(cfg);
   if (st != BPT_OK) return st;
   if (!X || !p || !Y || !saved || !ws) return fail(BPT_ERR_INVALID_ARG, "NULL X, params, Y, saved or workspace");
   if (!p->Wq || !p->Wk || !p->Wv || !p->Wo || !p->W1 || !p->W2)
@@ -643,6 +822,18 @@ bpt_status bpt_layer_fwd(const bpt_config* cfg, const void* X, const bpt_params*
     RUN("gemm.qkv", gemm_flops(g), gemm_bytes(g, E_, E_), gemm(E, EPI_STORE, E, F32, g, s));
   }
 
+  const bool win = opt && opt->window > 0;
+  if (opt && opt->rot) {   // Q and K turn in place
+    const bpt_rope_config rc = layer_rope(*cfg, *opt);
+    RUN("rope.fwd", 6.0 * T * d.H * opt->rot, 4.0 * T * d.H * opt->rot * E_,
+        rope(E, rope_args(rc, nullptr, sv.qkv, 3 * D, sv.qkv, 3 * D, 1.0f), s));
+  }
+  if (win) {               // linear in S: all groups' attention at once
+    const bpt_attn_config ac = layer_attn(*cfg, *opt);
+    const WinArgs a = layer_win(*cfg, *opt, d, sv);
+    RUN("win.fwd", 4.0 * d.dh * attn_seen(ac), 4.0 * T * D * E_, E == BF16 ? win_fwd_bf16(a, s) : win_fwd_f32(a, s));
+  }
+
   // Outer loop over groups of query blocks: attention for the group, then the
   // output projection, LN2, FFN and both residuals for the same rows.
   for (int64_t b = 0; b < d.B; b += d.nbg) {
@@ -659,7 +850,7 @@ bpt_status bpt_layer_fwd(const bpt_config* cfg, const void* X, const bpt_params*
       a.S = d.S; a.Sp = d.Sp; a.B = (int)d.B; a.H = (int)d.H; a.dh = (int)d.dh; a.causal = cfg->causal;
       a.q_begin = s0; a.q_end = s0 + rs; a.b_begin = (int)b; a.nb = (int)nb;
       const double pairs = attn_pairs(s0, s0 + rs, d.S, cfg->causal) * d.H * nb;
-      RUN("attn.fwd", 4.0 * d.dh * pairs, (3.0 * rs + 2.0 * (s0 + rs)) * nb * D * E_, attn_fwd(E, a, s));
+      if (!win) RUN("attn.fwd", 4.0 * d.dh * pairs, (3.0 * rs + 2.0 * (s0 + rs)) * nb * D * E_, attn_fwd(E, a, s));
 
       GemmArgs go;     // h = X + O Wo
       go.A = off(sv.o, t0 * D * E_); go.lda = D; go.B = p->Wo; go.ldb = D; go.trans_b = 1;
@@ -711,10 +902,60 @@ bpt_status bpt_layer_fwd(const bpt_config* cfg, const void* X, const bpt_params*
   return BPT_OK;
 }
 
-bpt_status bpt_layer_bwd(const bpt_config* cfg, const void* X, const bpt_params* p, const void* saved,
-                         const void* dY, void* dX, const bpt_grads* gr, void* ws, size_t ws_bytes,
-                         void* stream) {
-  bpt_status st = check(cfg);
+bpt_status bpt_layer_fwd(const bpt_config* cfg, const void* X, const bpt_params* p, void* Y, void* saved,
+                         void* ws, size_t ws_bytes, void* stream) {
+  return layer_fwd(cfg, nullptr, X, p, Y, saved, ws, ws_bytes, stream);
+}
+
+bpt_status bpt_layer_options_validate(const bpt_config* cfg, const bpt_layer_options* options) {
+  return options_check(cfg, options);
+}
+
+bpt_status bpt_layer_fwd_options(const bpt_config* cfg, const bpt_layer_options* options, const void* X, const bpt_params* p,
+                                 void* Y, void* saved, void* ws, size_t ws_bytes, void* stream) {
+  if (!options) return fail(BPT_ERR_INVALID_ARG, "options is NULL");
+  return layer_fwd(cfg, options, X, p, Y, saved, ws, ws_bytes, stream);
+}
+
+// QKV projection and LN1 backward from dQ, dK, dV token-major in w.dqkvT ([T, 3D], as the window kernels leave them)
+static bpt_status layer_bwd_proj(const bpt_config& cfg, const Dims& d, Dt E, Dt OUT, const void* X, const bpt_params* p,
+                                 const SavedPtrs& sv, const BwdWs& w, const bpt_grads& G, void* dX, float* ln_part,
+                                 int64_t ln_part_n, hipStream_t s) {
+  const int64_t D = d.D, T = d.T, E_ = (int64_t)d.E;
+  const size_t EO = esize(cfg.out_dtype);
+  float* outs[3] = {G.dWq, G.dWk, G.dWv};
+  const void* W[3] = {p->Wq, p->Wk, p->Wv};
+  if (G.dWq || G.dWk || G.dWv)
+    RUN("layernorm.fwd", 0, 2.0 * T * D * E_,
+        layer_norm(E, E, X, D, p->ln1_g, p->ln1_b, w.u, D, sv.mu1, sv.rstd1, T, D, cfg.ln_eps, 1, s));
+  for (int i = 0; i < 3; ++i) {
+    if (!outs[i]) continue;
+    GemmArgs g;   // dW = u^T d., both K-major, K = T: cut as dWo is
+    g.A = w.u; g.lda = D; g.trans_a = 1; g.B = off(w.dqkvT, i * D * E_); g.ldb = 3 * D; g.trans_b = 1;
+    g.C = outs[i]; g.ldc = D; g.M = D; g.N = D; g.K = T;
+    if (w.zo > 1) {
+      g.ksplit = w.zo; g.C = w.kpart; g.sC = D * D;
+    }
+    RUN("gemm.bwd_dwqkv", gemm_flops(g), gemm_bytes(g, E_, 4), gemm(E, EPI_STORE, F32, F32, g, s));
+    float* o1[3] = {outs[i], nullptr, nullptr};
+    if (w.zo > 1) RUN("reduce.ksplit", 0, (double)(w.zo + 1) * D * D * 4, sum_slices(w.kpart, w.zo, D, D, o1, 0, 0, s));
+  }
+  for (int i = 0; i < 3; ++i) {   // dU = dQ Wq^T + dK Wk^T + dV Wv^T
+    GemmArgs g;
+    g.A = off(w.dqkvT, i * D * E_); g.lda = 3 * D; g.B = W[i]; g.ldb = D; g.C = w.dU; g.ldc = D;
+    g.M = T; g.N = D; g.K = D; g.accumulate = i > 0;
+    RUN("gemm.bwd_du", gemm_flops(g), gemm_bytes(g, E_, 4), gemm(E, EPI_STORE, F32, F32, g, s));
+  }
+  RUN("layernorm.bwd", 0, (double)T * D * (E_ + 4 + 4 + EO),
+      layer_norm_bwd(E, X, sv.mu1, sv.rstd1, p->ln1_g, F32, w.dU, F32, w.dh, OUT, dX, OUT, nullptr, G.dln1_g, G.dln1_b,
+                     ln_part, ln_part_n, T, D, 0, 0, nullptr, s));
+  return BPT_OK;
+}
+
+static bpt_status layer_bwd(const bpt_config* cfg, const bpt_layer_options* opt, const void* X, const bpt_params* p,
+                            const void* saved, const void* dY, void* dX, const bpt_grads* gr, void* ws, size_t ws_bytes,
+                            void* stream) {
+  bpt_status st = opt ? options_check(cfg, opt) : check(cfg);
   if (st != BPT_OK) return st;
   if (!X || !p || !saved || !dY || !dX || !ws)
     return fail(BPT_ERR_INVALID_ARG, "NULL X, params, saved, dY, dX or workspace");
@@ -864,7 +1105,34 @@ bpt_status bpt_layer_bwd(const bpt_config* cfg, const void* X, const bpt_params*
     if ((st = wgrad("gemm.bwd_dwo", g, w.zo, outs)) != BPT_OK) return st;
   }
 
+  const bool win = opt && opt->window > 0;
+  bpt_rope_config rc = {};
+  if (opt && opt->rot) rc = layer_rope(*cfg, *opt);
   // ---- attention backward, probabilities rebuilt from the saved log-sum-exp
+  if (win) {   // dQ, dK, dV token-major, as the projection is
+    const bpt_attn_config ac = layer_attn(*cfg, *opt);
+    WinArgs a = layer_win(*cfg, *opt, d, sv);
+    a.dout = w.dO;
+    a.dq = w.dqkvT; a.dk = off(w.dqkvT, D * E_); a.dv = off(w.dqkvT, 2 * D * E_);
+    a.ndelta = w.ndelta; a.nlse = w.nlse2;
+    // the sums of the sinks' chunks go where the FFN group's buffers are idle; fewer chunks if they do not fit
+    const int64_t sinks = std::min(ac.sinks, ac.Skv), room = (char*)w.dh - (char*)w.vg;
+    a.part_s = (float*)w.vg;
+    a.far = attn_far(ac);
+    while (a.far > 0 && attn_slots(ac, a.far) * ac.B * ac.Hkv * sinks * 2 * ac.dh * 4 > room) a.far /= 2;
+    const double seen = attn_seen(ac);
+    RUN("win.delta", 0, 2.0 * T * D * E_, win_delta(E, a, s));
+    RUN("win.dkdv", 8.0 * d.dh * seen, 6.0 * T * D * E_, E == BF16 ? win_dkdv_bf16(a, s) : win_dkdv_f32(a, s));
+    if (a.far > 0) {
+      RUN("win.far", 8.0 * d.dh * T * d.H * sinks, 2.0 * T * D * E_, E == BF16 ? win_far_bf16(a, s) : win_far_f32(a, s));
+      RUN("win.sinks", 0, (double)attn_slots(ac, a.far) * B * d.H * sinks * d.dh * 8, win_sinks(E, a, attn_slots(ac, a.far), s));
+    }
+    RUN("win.dq", 6.0 * d.dh * seen, 5.0 * T * D * E_, E == BF16 ? win_dq_bf16(a, s) : win_dq_f32(a, s));
+    if (opt->rot)
+      RUN("rope.bwd", 6.0 * T * d.H * opt->rot, 4.0 * T * d.H * opt->rot * E_,
+          rope(E, rope_args(rc, nullptr, w.dqkvT, 3 * D, w.dqkvT, 3 * D, -1.0f), s));
+    return layer_bwd_proj(*cfg, d, E, OUT, X, p, sv, w, G, dX, ln_part, ln_part_n, s);
+  }
   RUN("attn.delta", 0, 2.0 * T * D * E_, attn_delta(E, w.dO, sv.o, D, sv.lse, w.ndelta, w.nlse2, B, S, Sp, (int)d.H, (int)d.dh, s));
   {
     AttnArgs a;
@@ -881,6 +1149,10 @@ bpt_status bpt_layer_bwd(const bpt_config* cfg, const void* X, const bpt_params*
     // query-outer: S^T, dP^T, dQ += dS K (3 contractions)
     RUN("attn.bwd_dq", 6.0 * d.dh * pairs, 6.0 * T * D * E_, attn_bwd_dq(E, a, s));
   }
+
+  if (opt && opt->rot)
+    RUN("rope.bwd", 6.0 * T * d.H * opt->rot, 4.0 * T * d.H * opt->rot * E_,
+        rope_t(E, rope_args(rc, nullptr, w.dqkvT, Tp, w.dqkvT, Tp, -1.0f), Sp, s));
 
   // ---- QKV projection and LN1 backward
   if (G.dWq || G.dWk || G.dWv) {
@@ -924,6 +1196,18 @@ bpt_status bpt_layer_bwd(const bpt_config* cfg, const void* X, const bpt_params*
       layer_norm_bwd(E, X, sv.mu1, sv.rstd1, p->ln1_g, F32, w.dU, F32, w.dh, OUT, dX, OUT, nullptr, G.dln1_g, G.dln1_b,
                      ln_part, ln_part_n, T, D, S, Sp, nullptr, s));
   return BPT_OK;
+}
+
+bpt_status bpt_layer_bwd(const bpt_config* cfg, const void* X, const bpt_params* p, const void* saved,
+                         const void* dY, void* dX, const bpt_grads* gr, void* ws, size_t ws_bytes, void* stream) {
+  return layer_bwd(cfg, nullptr, X, p, saved, dY, dX, gr, ws, ws_bytes, stream);
+}
+
+bpt_status bpt_layer_bwd_options(const bpt_config* cfg, const bpt_layer_options* options, const void* X, const bpt_params* p,
+                                 const void* saved, const void* dY, void* dX, const bpt_grads* gr, void* ws, size_t ws_bytes,
+                                 void* stream) {
+  if (!options) return fail(BPT_ERR_INVALID_ARG, "options is NULL");
+  return layer_bwd(cfg, options, X, p, saved, dY, dX, gr, ws, ws_bytes, stream);
 }
 
 // ---------------------------------------------------------------- cross-entropy of an LM head
@@ -1035,12 +1319,6 @@ bpt_status bpt_xent_bwd(const bpt_xent_config* cfg, const void* h, const void* W
 }
 
 // ---------------------------------------------------------------- GPT training step pieces
-static bpt_status dtype_ok(int32_t t, const char* what) {
-  if (t != BPT_F32 && t != BPT_BF16) return fail(BPT_ERR_INVALID_ARG, "%s %d is not a bpt_dtype", what, (int)t);
-  return BPT_OK;
-}
-static Dt dt_of(int32_t t) { return t == BPT_BF16 ? BF16 : F32; }
-
 static bpt_status embed_check(const bpt_embed_config* c) {
   if (!c) return fail(BPT_ERR_INVALID_ARG, "NULL config");
   if (c->B < 1 || c->S < 1 || c->D < 1 || c->V < 1)
@@ -1195,34 +1473,6 @@ bpt_status bpt_adamw_step(const bpt_adamw_config* cfg, int64_t n, float* p, cons
 }
 
 // ---------------------------------------------------------------- rotary positions
-static bpt_status rope_check(const bpt_rope_config* c) {
-  if (!c) return fail(BPT_ERR_INVALID_ARG, "config is NULL");
-  if (c->rows < 1 || c->S < 1 || c->H < 1 || c->dh < 1) return fail(BPT_ERR_INVALID_ARG, "rows, S, H and dh must be >= 1");
-  if (c->rot < 2 || c->rot % 2 || c->rot > c->dh)
-    return fail(BPT_ERR_INVALID_ARG, "rot = %lld must be even and lie in [2, dh]", (long long)c->rot);
-  if (c->scaling < BPT_ROPE_NONE || c->scaling > BPT_ROPE_BY_PARTS) return fail(BPT_ERR_INVALID_ARG, "scaling is not a bpt_rope_scaling");
-  if (!(c->theta > 0.0) || !std::isfinite(c->theta)) return fail(BPT_ERR_INVALID_ARG, "theta must be > 0");
-  if (!std::isfinite(c->mscale)) return fail(BPT_ERR_INVALID_ARG, "mscale must be finite");
-  if (c->scaling != BPT_ROPE_NONE && (!(c->factor >= 1.0) || !std::isfinite(c->factor)))
-    return fail(BPT_ERR_INVALID_ARG, "factor must be >= 1");
-  if (c->scaling == BPT_ROPE_BASE && c->rot == 2) return fail(BPT_ERR_INVALID_ARG, "BPT_ROPE_BASE needs rot > 2");
-  if (c->scaling == BPT_ROPE_BY_PARTS && (c->orig_len < 1 || !(c->beta_fast > c->beta_slow) || !std::isfinite(c->beta_fast) || !std::isfinite(c->beta_slow)))
-    return fail(BPT_ERR_INVALID_ARG, "BPT_ROPE_BY_PARTS needs orig_len >= 1 and beta_fast > beta_slow");
-  if ((c->interleaved != 0 && c->interleaved != 1) || c->reserved != 0)
-    return fail(BPT_ERR_INVALID_ARG, "interleaved must be 0 or 1, reserved 0");
-  if (c->H > (int64_t)1 << 20 || c->dh > (int64_t)1 << 16) return fail(BPT_ERR_UNSUPPORTED, "H or dh too large");
-  if (c->ldx < c->H * c->dh || c->ldy < c->H * c->dh) return fail(BPT_ERR_INVALID_ARG, "ldx and ldy must be >= H dh");
-  bpt_status st = dtype_ok(c->dtype, "dtype");
-  if (st != BPT_OK) return st;
-  if (c->dh % 8 || c->ldx % 8 || c->ldy % 8) return fail(BPT_ERR_UNSUPPORTED, "dh, ldx and ldy must be multiples of 8");
-  if (c->rot > 128) return fail(BPT_ERR_UNSUPPORTED, "rot = %lld > 128", (long long)c->rot);
-  if (c->rows > INT32_MAX || c->H * c->dh > INT32_MAX / 8 || c->ldx > (int64_t)1 << 40 || c->ldy > (int64_t)1 << 40)
-    return fail(BPT_ERR_UNSUPPORTED, "rows, H dh or a row stride too large");
-  const int64_t most = (int64_t)1 << 52;             // positions are exact in a double
-  if (c->pos0 > most || c->pos0 < -most || c->S > most) return fail(BPT_ERR_UNSUPPORTED, "pos0 or S too large");
-  return BPT_OK;
-}
-
 static bpt_status rope_run(const bpt_rope_config* c, const int32_t* positions, const void* x, int64_t ldx, void* y, int64_t ldy,
                            float sign, void* stream) {
   bpt_status st = rope_check(c);
@@ -1231,24 +1481,7 @@ static bpt_status rope_run(const bpt_rope_config* c, const int32_t* positions, c
   if (!aligned16(x) || !aligned16(y) || (positions && ((uintptr_t)positions & 3)))
     return fail(BPT_ERR_INVALID_ARG, "tensors must be 16-byte aligned");
   if (x == y && ldx != ldy) return fail(BPT_ERR_INVALID_ARG, "in place needs ldx == ldy");
-  RopeArgs a;
-  a.x = x; a.y = y; a.positions = positions;
-  a.rows = c->rows; a.S = c->S; a.ldx = ldx; a.ldy = ldy; a.pos0 = c->pos0;
-  a.H = (int)c->H; a.dh = (int)c->dh; a.rot = (int)c->rot; a.interleaved = c->interleaved;
-  a.mscale = (float)c->mscale; a.sign = sign;
-  const double pi2 = 6.283185307179586476925;
-  const double rot = (double)c->rot;
-  const double theta = c->scaling == BPT_ROPE_BASE ? c->theta * std::pow(c->factor, rot / (rot - 2.0)) : c->theta;
-  for (int i = 0; i < c->rot / 2; ++i) {
-    double f = std::pow(theta, -2.0 * i / rot);
-    if (c->scaling == BPT_ROPE_LINEAR) f /= c->factor;
-    if (c->scaling == BPT_ROPE_BY_PARTS) {
-      const double turns = (double)c->orig_len * f / pi2;
-      const double g = std::min(1.0, std::max(0.0, (turns - c->beta_slow) / (c->beta_fast - c->beta_slow)));
-      f *= g + (1.0 - g) / c->factor;
-    }
-    a.turns[i] = f / pi2;
-  }
+  const RopeArgs a = rope_args(*c, positions, x, ldx, y, ldy, sign);
   hipStream_t s = (hipStream_t)stream;
   const int64_t moved = (x == y ? c->rot : c->dh) * c->H;
   RUN(sign > 0 ? "rope.fwd" : "rope.bwd", 3.0 * c->rows * c->H * c->rot, 2.0 * c->rows * moved * esize(c->dtype) + (positions ? 4.0 * c->rows : 0.0),
@@ -1266,51 +1499,6 @@ bpt_status bpt_rope_bwd(const bpt_rope_config* cfg, const int32_t* positions, co
 }
 
 // ---------------------------------------------------------------- attention with a window and sinks
-// Whether no two elements of a tensor share a place (dims of stride and size; features are adjacent)
-static bool apart(const bpt_attn_strides& t, int64_t B, int64_t S, int64_t H, int64_t dh) {
-  std::pair<int64_t, int64_t> d[] = {{t.sb, B}, {t.st, S}, {t.sh, H}};
-  std::sort(d, d + 3);
-  int64_t span = dh;
-  for (auto& e : d) {
-    if (e.second == 1) continue;
-    if (e.first < span) return false;
-    span += e.first * (e.second - 1);
-  }
-  return true;
-}
-
-constexpr int64_t kAttnMax = (int64_t)1 << 28;      // sums of a few lengths stay within 32 bits
-
-static bpt_status attn_check(const bpt_attn_config* c) {
-  if (!c) return fail(BPT_ERR_INVALID_ARG, "config is NULL");
-  if (c->B < 1 || c->Sq < 1 || c->Skv < 1 || c->Hq < 1 || c->Hkv < 1 || c->dh < 1)
-    return fail(BPT_ERR_INVALID_ARG, "B, Sq, Skv, Hq, Hkv, dh must be >= 1");
-  if (c->Hq % c->Hkv) return fail(BPT_ERR_INVALID_ARG, "Hq=%lld is not a multiple of Hkv=%lld", (long long)c->Hq, (long long)c->Hkv);
-  if (c->window < 0 || c->sinks < 0 || (c->window == 0 && c->sinks != 0))
-    return fail(BPT_ERR_INVALID_ARG, "window and sinks must be >= 0, and sinks 0 without a window");
-  if (!(c->scale > 0.0f) || !std::isfinite(c->scale)) return fail(BPT_ERR_INVALID_ARG, "scale must be > 0");
-  if ((c->causal != 0 && c->causal != 1) || c->reserved != 0) return fail(BPT_ERR_INVALID_ARG, "causal must be 0 or 1, reserved 0");
-  bpt_status st = dtype_ok(c->dtype, "dtype");
-  if (st != BPT_OK) return st;
-  const bpt_attn_strides* all[] = {&c->q, &c->k, &c->v, &c->o};
-  const int64_t unit = 16 / (int64_t)esize(c->dtype);
-  for (auto* t : all) {
-    if (t->sb < 0 || t->st < 0 || t->sh < 0) return fail(BPT_ERR_INVALID_ARG, "strides must be >= 0");
-    if (t->sb % unit || t->st % unit || t->sh % unit) return fail(BPT_ERR_INVALID_ARG, "strides must be multiples of 16 bytes");
-    if (t->st >= (int64_t)1 << 22 || t->sb >= (int64_t)1 << 40 || t->sh >= (int64_t)1 << 40)
-      return fail(BPT_ERR_UNSUPPORTED, "a stride is too large");
-  }
-  if (c->dh != 64 && c->dh != 128) return fail(BPT_ERR_UNSUPPORTED, "head dim %lld unsupported (64 or 128)", (long long)c->dh);
-  if (c->B > 65535 || c->Hkv > 65535 || c->Hq > 65535) return fail(BPT_ERR_UNSUPPORTED, "B and heads must be <= 65535");
-  if (c->Sq > kAttnMax || c->Skv > kAttnMax || c->window > kAttnMax || c->sinks > kAttnMax || c->Sq * (c->Hq / c->Hkv) > kAttnMax)
-    return fail(BPT_ERR_UNSUPPORTED, "lengths, window and sinks must be <= 2^28, and Sq Hq / Hkv too");
-  // workgroups of 16 rows and rows of the log-sum-exp
-  if (c->B * c->Hkv * ((std::max(c->Sq * (c->Hq / c->Hkv), c->Skv) + 15) / 16) > (int64_t)1 << 26 || c->B * c->Hq * rup(c->Sq, 64) > (int64_t)1 << 32)
-    return fail(BPT_ERR_UNSUPPORTED, "B * heads * length too large");
-  if (!apart(c->o, c->B, c->Sq, c->Hq, c->dh)) return fail(BPT_ERR_INVALID_ARG, "strides of O overlap");
-  return BPT_OK;
-}
-
 // A bf16 forward whose blocks of 128 rows would leave most CUs idle takes the kernel for few rows.
 static bool attn_few(const bpt_attn_config& c) {
   const int64_t rows = c.Sq * (c.Hq / c.Hkv);
@@ -1327,18 +1515,6 @@ static int attn_nsplit(const bpt_attn_config& c) {
   return (int)std::max<int64_t>(1, std::min<int64_t>({1024 / groups, span / (bf ? 128 : 512), 64}));
 }
 
-// Chunks of what the sinks' keys see beyond their window in the backward: 0 where a block of keys that
-// holds sinks has little more to do than another, else workgroups for two a CU and at least two tiles
-// of 64 queries for each.
-static int attn_far(const bpt_attn_config& c) {
-  if (c.sinks == 0 || c.window >= c.Skv) return 0;
-  const int64_t G = c.Hq / c.Hkv, tiles = (c.Sq - std::min(c.Sq, c.window) + 63) / 64 * G;
-  if (tiles < 16) return 0;
-  const int64_t groups = c.B * c.Hkv * ((std::min(c.sinks, c.Skv) + 31) / 32);
-  return (int)std::max<int64_t>(1, std::min(512 / groups, tiles / 2));
-}
-static int attn_slots(const bpt_attn_config& c) { return 1 + attn_far(c) * (c.dtype == BPT_BF16 ? 2 : 1); }
-
 struct AttnWs {
   float *part_o, *part_ml;     // forward: slices
   float *ndelta, *nlse, *part_s;   // backward
@@ -1350,35 +1526,13 @@ static AttnWs attn_ws(const bpt_attn_config& c, void* base, int backward, int64_
     const int64_t n = c.B * c.Hq * rup(c.Sq, 64) * 4;
     w.ndelta = (float*)bp.take(n);
     w.nlse = (float*)bp.take(n);
-    if (attn_far(c)) w.part_s = (float*)bp.take(attn_slots(c) * c.B * c.Hkv * std::min(c.sinks, c.Skv) * 2 * c.dh * 4);
+    if (attn_far(c)) w.part_s = (float*)bp.take(attn_slots(c, attn_far(c)) * c.B * c.Hkv * std::min(c.sinks, c.Skv) * 2 * c.dh * 4);
   } else if (const int z = attn_nsplit(c); z > 1) {
     w.part_o = (float*)bp.take(z * c.B * c.Hq * c.Sq * c.dh * 4);
     w.part_ml = (float*)bp.take(z * c.B * c.Hq * c.Sq * 8);
   }
   *total = rup(bp.off, kAlign);
   return w;
-}
-
-static WinArgs attn_args(const bpt_attn_config& c, const void* Q, const void* K, const void* V, const int32_t* q_lens,
-                         const int32_t* kv_lens, const void* O, const float* lse) {
-  WinArgs a;
-  a.q = Q; a.k = K; a.v = V; a.o = (void*)O; a.lse = (float*)lse; a.lse_ld = c.Sq;
-  a.q_sb = c.q.sb; a.q_st = (int)c.q.st; a.q_sh = c.q.sh;
-  a.k_sb = c.k.sb; a.k_st = (int)c.k.st; a.k_sh = c.k.sh;
-  a.v_sb = c.v.sb; a.v_st = (int)c.v.st; a.v_sh = c.v.sh;
-  a.o_sb = c.o.sb; a.o_st = (int)c.o.st; a.o_sh = c.o.sh;
-  a.q_lens = q_lens; a.kv_lens = kv_lens;
-  a.B = (int)c.B; a.Sq = (int)c.Sq; a.Skv = (int)c.Skv;
-  a.Hq = (int)c.Hq; a.Hkv = (int)c.Hkv; a.G = (int)(c.Hq / c.Hkv); a.dh = (int)c.dh;
-  a.causal = c.causal; a.window = (int)c.window; a.sinks = (int)c.sinks; a.scale = c.scale;
-  a.Sqp = rup(c.Sq, 64);
-  return a;
-}
-
-// visible pairs of a sequence of whole length, for the launch record
-static double attn_seen(const bpt_attn_config& c) {
-  const double per = c.window ? (double)std::min(c.Skv, (c.causal ? 1 : 2) * c.window + c.sinks) : (double)c.Skv;
-  return (double)c.B * c.Hq * c.Sq * (c.causal && !c.window ? per - 0.5 * (double)std::min(c.Sq, c.Skv) : per);
 }
 
 bpt_status bpt_attn_validate(const bpt_attn_config* cfg) { return attn_check(cfg); }
@@ -1454,8 +1608,8 @@ bpt_status bpt_attn_bwd(const bpt_attn_config* cfg, const void* Q, const void* K
   if (dK) RUN("win.dkdv", 8.0 * cfg->dh * seen, (2.0 * q + 4.0 * kv) * E_, bf ? win_dkdv_bf16(a, s) : win_dkdv_f32(a, s));
   if (a.far > 0) {
     RUN("win.far", 8.0 * cfg->dh * cfg->B * cfg->Hq * cfg->Sq * std::min(cfg->sinks, cfg->Skv), 2.0 * q * E_, bf ? win_far_bf16(a, s) : win_far_f32(a, s));
-    RUN("win.sinks", 0, (double)attn_slots(*cfg) * cfg->B * cfg->Hkv * std::min(cfg->sinks, cfg->Skv) * cfg->dh * 8,
-        win_sinks(dt_of(cfg->dtype), a, attn_slots(*cfg), s));
+    RUN("win.sinks", 0, (double)attn_slots(*cfg, a.far) * cfg->B * cfg->Hkv * std::min(cfg->sinks, cfg->Skv) * cfg->dh * 8,
+        win_sinks(dt_of(cfg->dtype), a, attn_slots(*cfg, a.far), s));
   }
   if (dQ) RUN("win.dq", 6.0 * cfg->dh * seen, (3.0 * q + 2.0 * kv) * E_, bf ? win_dq_bf16(a, s) : win_dq_f32(a, s));
   return BPT_OK;

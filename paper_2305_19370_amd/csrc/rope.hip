@@ -119,6 +119,43 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a, int rows_per) {
   }
 }
 
+// Feature-major, in place: a thread turns 8 consecutive tokens of one pair in every head, its cosines and sines formed once.
+template <typename T>
+__global__ __launch_bounds__(256) void rope_t_kernel(RopeArgs a, int64_t Sp) {
+  const int i = blockIdx.y, pairs = a.rot / 2;
+  const int64_t c0 = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 8;   // column, within one sequence: Sp % 8 == 0
+  if (c0 >= a.rows / a.S * Sp) return;
+  float cs[8], sn[8];
+#pragma unroll
+  for (int k = 0; k < 8; ++k) {
+    const double t = (double)(a.pos0 + (c0 + k) % Sp) * a.turns[i];
+    sincospif(2.0f * (float)(t - rint(t)), &sn[k], &cs[k]);
+    cs[k] *= a.mscale;
+    sn[k] *= a.mscale * a.sign;
+  }
+  T* x = (T*)a.y + (int64_t)(a.interleaved ? 2 * i : i) * a.ldx + c0;
+  const int64_t other = (a.interleaved ? 1 : pairs) * a.ldx, head = a.dh * a.ldx;
+  for (int h = 0; h < a.H; ++h, x += head) {
+    float v[8], w[8], p[8], q[8];
+    ld<8>(x, v);
+    ld<8>(x + other, w);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      p[k] = cs[k] * v[k] - sn[k] * w[k];
+      q[k] = cs[k] * w[k] + sn[k] * v[k];
+    }
+    st<8>(x, p);
+    st<8>(x + other, q);
+  }
+}
+
+hipError_t rope_t(Dt t, const RopeArgs& a, int64_t Sp, hipStream_t s) {
+  const int64_t cols = a.rows / a.S * Sp;
+  auto k = t == BF16 ? rope_t_kernel<bf16> : rope_t_kernel<float>;
+  hipLaunchKernelGGL(k, dim3((unsigned)((cols / 8 + 255) / 256), a.rot / 2), dim3(256), 0, s, a, Sp);
+  return hipGetLastError();
+}
+
 template <typename T, int N, bool INTER>
 static hipError_t launch(const RopeArgs& a, hipStream_t s) {
   const int rows_per = a.rows >= 4096 ? kRopeRows : 1;   // few rows: one per workgroup

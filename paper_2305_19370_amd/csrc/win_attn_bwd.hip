@@ -93,7 +93,7 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 1 : 2) void win_dq_bf16_kernel(W
     for (int t = 0; t < C::DT; ++t) acc[t] = f32x16{};
   }
   if (w.i < a.Sq)
-    store_rows<DH>((bf16*)a.dq + (int64_t)b * a.q_sb + (int64_t)w.i * a.q_st + (int64_t)h * a.q_sh, acc, a.scale, lane);
+    store_rows<DH>((bf16*)a.dq + (int64_t)b * a.q_sb + (int64_t)w.i * a.q_st + (int64_t)h * a.q_sh, acc, a.dq_scale, lane);
 }
 
 // Ring of the dK dV kernel: tiles of 64 queries (Q, dO) and their -lse / scale and -Delta

@@ -243,7 +243,7 @@ __global__ __launch_bounds__(256) void win_dq_f32_kernel(WinArgs a) {
     const f32x4 x = ((*(const f32x4*)&red[0][ri][d] + *(const f32x4*)&red[1][ri][d]) + *(const f32x4*)&red[2][ri][d]) +
                     *(const f32x4*)&red[3][ri][d];
     const int ii = rr / a.G, hh = kvh * a.G + rr % a.G;
-    *(f32x4*)((float*)a.dq + (int64_t)b * a.q_sb + (int64_t)ii * a.q_st + (int64_t)hh * a.q_sh + d) = x * a.scale;
+    *(f32x4*)((float*)a.dq + (int64_t)b * a.q_sb + (int64_t)ii * a.q_st + (int64_t)hh * a.q_sh + d) = x * a.dq_scale;
   }
 }
 
@@ -281,7 +281,13 @@ __global__ __launch_bounds__(512) void win_dkdv_f32_kernel(WinArgs a) {
       const RowFrag<DH> qf = row_frag<DH>(Qb + qr * a.q_st, g), of = row_frag<DH>(dOb + qr * a.o_st, g);
       const int64_t sidx = ((int64_t)b * a.Hq + h) * a.Sqp + q0 + 4 * g;   // Sqp % 64 == 0
       const f32x4 l4 = *(const f32x4*)(a.nlse + sidx), d4 = *(const f32x4*)(a.ndelta + sidx);
-      Vis qv{run.lo, run.hi, 0};
+      const Vis qv{run.lo, run.hi, 0};
+      ColFrag<DH> oc, qc;                            // fetched with the rest where registers allow
+      if constexpr (DH == 64) {
+        oc = col_frag_vis<DH>(dOb, a.o_st, q0, qv, g, c16);
+        qc = col_frag_vis<DH>(Qb, a.q_st, q0, qv, g, c16);
+        __builtin_amdgcn_sched_barrier(0);
+      }
       f32x4 p = dot_frags<DH>(qf, kf), ds = dot_frags<DH>(of, vf);
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
@@ -291,9 +297,9 @@ __global__ __launch_bounds__(512) void win_dkdv_f32_kernel(WinArgs a) {
         p[r] = ok ? fast_exp2((p[r] + l4[r]) * c) : 0.0f;
         ds[r] = ok ? p[r] * (ds[r] + d4[r]) : 0.0f;
       }
-      const ColFrag<DH> oc = col_frag_vis<DH>(dOb, a.o_st, q0, qv, g, c16);
+      if constexpr (DH != 64) oc = col_frag_vis<DH>(dOb, a.o_st, q0, qv, g, c16);
       add_outer<DH>(dv, oc, p);
-      const ColFrag<DH> qc = col_frag_vis<DH>(Qb, a.q_st, q0, qv, g, c16);
+      if constexpr (DH != 64) qc = col_frag_vis<DH>(Qb, a.q_st, q0, qv, g, c16);
       add_outer<DH>(dk, qc, ds);
     }
   }

@@ -10,6 +10,10 @@ and bpt_embed_bwd, and AdamW (bpt_adamw_step) on fp32 master weights, which also
 writes the bf16 copies the kernels read. Every step runs in libbpt's kernels; this
 module allocates the buffers (torch) and sequences the calls on the current stream.
 
+For long contexts the layers' Q and K may carry rotary positions (GPTShape.rope) in place of the position
+table, attention may be limited to a window and sinks (window, sinks), and AdamW may hold its moments in
+8 bits (opt_bits = 8: bpt_adamw_multi, both groups in one launch).
+
 Parameters live in two flat fp32 buffers (weight matrices and embeddings, which take
 weight decay; LayerNorm gains/shifts and biases, which do not), each with matching
 flat gradient and moment buffers, so one optimiser step is two launches. Entries
@@ -49,6 +53,15 @@ class GPTShape:
     xent_block_rows: int = 0       # 0 = the library's default
     dropout: float = 0.0           # residual-branch dropout rate of every layer
     dropout_seed: int = 0          # base of the per-layer, per-step mask keys
+    rope: str = "none"             # rotary positions of every layer: "half" or "interleaved" pairs
+    rope_theta: float = 10000.0
+    rope_scaling: str = "none"     # "linear", "base" or "by_parts", with rope_factor (and rope_orig_len)
+    rope_factor: float = 1.0
+    rope_orig_len: int = 0
+    window: int = 0                # tokens that attention sees, 0 = all
+    sinks: int = 0                 # first tokens that stay visible beyond the window
+    opt_bits: int = 32             # AdamW moments: 32 or 8 bits
+    opt_seed: int = 0              # of the 8-bit moments' rounding
 
     @property
     def ldw(self) -> int:
@@ -63,7 +76,7 @@ class GPTShape:
 class _Flat:
     """One flat group of fp32 parameters with gradient, moments and a low-precision copy."""
 
-    def __init__(self, shapes: List[Tuple[str, Tuple[int, ...]]], device, lowp: Optional[torch.dtype]):
+    def __init__(self, shapes: List[Tuple[str, Tuple[int, ...]]], device, lowp: Optional[torch.dtype], bits: int = 32):
         self.index: Dict[str, Tuple[int, Tuple[int, ...]]] = {}
         off = 0
         for name, shp in shapes:
@@ -71,7 +84,12 @@ class _Flat:
             off += (math.prod(shp) + 63) // 64 * 64
         self.n = max(off, 64)
         z = lambda dt: torch.zeros(self.n, dtype=dt, device=device)
-        self.p, self.g, self.m, self.v = z(torch.float32), z(torch.float32), z(torch.float32), z(torch.float32)
+        self.p, self.g = z(torch.float32), z(torch.float32)
+        if bits == 8:                # e4m3 moments m and r = sqrt(v), two exponents per block of 256
+            self.m, self.r = z(torch.uint8), z(torch.uint8)
+            self.exps = torch.zeros((self.n + 255) // 256, 2, dtype=torch.uint8, device=device)
+        else:
+            self.m, self.v = z(torch.float32), z(torch.float32)
         self.low = z(lowp) if lowp is not None else None
 
     def view(self, buf: torch.Tensor, name: str) -> torch.Tensor:
@@ -90,6 +108,13 @@ class GPT:
         self.cfg = bpt.make_config(s.B, s.S, s.D, s.H, s.F, s.Bq, s.Bkv, causal=s.causal, dtype=s.dtype,
                                    out_dtype=s.dtype, ln_eps=s.ln_eps, activation=s.activation,
                                    dropout=s.dropout)
+        self.options = None
+        if s.rope != "none" or s.window:
+            rot = 0 if s.rope == "none" else s.D // s.H
+            self.options = bpt.make_layer_options(rot=rot, layout=s.rope if rot else "half", theta=s.rope_theta,
+                                                  scaling=s.rope_scaling if rot else "none", factor=s.rope_factor,
+                                                  orig_len=s.rope_orig_len, window=s.window, sinks=s.sinks)
+            bpt._check(bpt.layer_options_validate(self.cfg, self.options))
         bpt._check(bpt.validate(self.cfg))
         T = s.B * s.S
         self.xcfg = bpt.make_xent_config(T, s.D, s.V, ldw=s.ldw, block_rows=s.xent_block_rows, dtype=s.dtype)
@@ -105,8 +130,8 @@ class GPT:
         for l in range(s.L):
             mats += [(f"{l}.{k}", dims[k]) for k in LAYER_MATS]
             vecs += [(f"{l}.{k}", dims[k]) for k in LAYER_VECS if s.biases or k not in ("b1", "b2")]
-        self.decay = _Flat(mats, device, lowp)
-        self.nodecay = _Flat(vecs, device, None)     # vectors are read in fp32 by the kernels
+        self.decay = _Flat(mats, device, lowp, s.opt_bits)
+        self.nodecay = _Flat(vecs, device, None, s.opt_bits)     # vectors are read in fp32 by the kernels
         self.step_count = 0
 
         # activations, saved state, workspace
@@ -196,7 +221,8 @@ class GPT:
         s = self.shape
         bpt.embed_fwd(self.ecfg, tokens, self.weight("Wte"), self.weight("Wpe") if s.pos_table else None, self.X[0])
         for l in range(s.L):
-            bpt.layer_fwd(self._layer_cfg(l), self.X[l], self.layer_params(l), self.X[l + 1], self.saved[l], self.ws)
+            bpt.layer_fwd(self._layer_cfg(l), self.X[l], self.layer_params(l), self.X[l + 1], self.saved[l], self.ws,
+                          self.options)
         bpt.ln_fwd(self.lcfg, self.X[s.L], self.master("lnf_g"), self.master("lnf_b"), self.hf, self.mean, self.rstd)
         bpt.xent_fwd(self.xcfg, self.hf, self.weight("Wout"), targets, self.loss, self.lse, self.ws)
         return self.loss
@@ -211,7 +237,7 @@ class GPT:
                    self.grad("lnf_g"), self.grad("lnf_b"), self.ws)
         for l in range(s.L - 1, -1, -1):
             bpt.layer_bwd(self._layer_cfg(l), self.X[l], self.layer_params(l), self.saved[l], cur, nxt, self.layer_grads(l),
-                          self.ws)
+                          self.ws, self.options)
             cur, nxt = nxt, cur
         bpt.embed_bwd(self.ecfg, tokens, cur, self.grad("Wte"), self.grad("Wpe") if s.pos_table else None)
         self.dX0 = cur
@@ -219,6 +245,11 @@ class GPT:
     def optimizer_step(self, lr: float, weight_decay: float = 0.1, beta1: float = 0.9, beta2: float = 0.95,
                        eps: float = 1e-8) -> None:
         self.step_count += 1
+        if self.shape.opt_bits == 8:
+            both = bpt.AdamWTensors([dict(p=grp.p, g=grp.g, m=grp.m, r=grp.r, exps=grp.exps, p_lowp=grp.low, weight_decay=wd)
+                                     for grp, wd in ((self.decay, weight_decay), (self.nodecay, 0.0))], bits=8)
+            bpt.adamw_multi(both, self.step_count, lr, beta1, beta2, eps, seed=self.shape.opt_seed)
+            return
         for grp, wd in ((self.decay, weight_decay), (self.nodecay, 0.0)):
             bpt.adamw_step(grp.p, grp.g, grp.m, grp.v, self.step_count, lr, beta1, beta2, eps, wd, p_lowp=grp.low)
 

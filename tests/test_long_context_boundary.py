@@ -203,3 +203,31 @@ def test_adamw_tensors_refuses():
         bpt.AdamWTensors([good], bits=16)
     with pytest.raises(ValueError):
         bpt.AdamWTensors([good, dict(good, g=p.bfloat16())])
+
+
+# ---------------------------------------------------------------- a layer's options
+@pytest.mark.parametrize("kw,code", [
+    (dict(), 0), (dict(rot=64), 0), (dict(window=100, sinks=4), 0), (dict(rot=16, window=1), 0), (dict(rot=63), 1), (dict(rot=128), 1),
+    (dict(rot=-2), 1), (dict(rot=64, theta=0.0), 1), (dict(rot=64, scaling="linear", factor=0.1), 1), (dict(rot=64, scaling="by_parts"), 1),
+    (dict(sinks=4), 1), (dict(window=-1), 1), (dict(window=4, sinks=-1), 1), (dict(window=1 << 40), 2),
+])
+def test_layer_options(kw, code):
+    cfg = bpt.make_config(1, 512, 256, 4, 1024, 128, 128, dtype="bf16")
+    o = bpt.make_layer_options(**kw)
+    assert bpt.layer_options_validate(cfg, o) == code, err()
+    lib = bpt.load()
+    if code:
+        p = bpt.Params(*([A] * 12))
+        assert lib.bpt_layer_fwd_options(ctypes.byref(cfg), ctypes.byref(o), A, ctypes.byref(p), 2 * A, 3 * A, 4 * A, 1 << 40, None) == code
+        assert lib.bpt_layer_bwd_options(ctypes.byref(cfg), ctypes.byref(o), A, ctypes.byref(p), 3 * A, 2 * A, 5 * A,
+                                         ctypes.byref(bpt.Grads()), 4 * A, 1 << 40, None) == code
+
+
+def test_layer_options_null():
+    cfg = bpt.make_config(1, 512, 256, 4, 1024, 128, 128, dtype="bf16")
+    lib, p = bpt.load(), bpt.Params(*([A] * 12))
+    assert lib.bpt_layer_options_validate(ctypes.byref(cfg), None) == 1
+    assert lib.bpt_layer_fwd_options(ctypes.byref(cfg), None, A, ctypes.byref(p), 2 * A, 3 * A, 4 * A, 1 << 40, None) == 1
+    assert lib.bpt_layer_bwd_options(ctypes.byref(cfg), None, A, ctypes.byref(p), 3 * A, 2 * A, 5 * A, None, 4 * A, 1 << 40, None) == 1
+    cfg.H = 3                                        # the layer's own refusals come first
+    assert lib.bpt_layer_options_validate(ctypes.byref(cfg), ctypes.byref(bpt.make_layer_options())) == 1
