@@ -146,7 +146,8 @@ struct WinArgs {
   int64_t Sqp = 0;                      // Sq rounded up to 64
   float *ndelta = nullptr, *nlse = nullptr;      // [B, Hq, Sqp]: -rowsum(dO O), -lse / scale
   int far = 0;                          // chunks of what sinks see beyond their window; 0: not apart
-  float* part_s = nullptr;              // far > 0: their sums, [slots, B, Hkv, min(sinks, Skv), 2, dh]
+  int chunks = 1;                       // of every block of keys in dK, dV; > 1: far = 0
+  float* part_s = nullptr;              // far > 0, chunks > 1: sums, [slots, B, Hkv, min(sinks, Skv) or Skv, 2, dh]
 };
 hipError_t win_fwd_bf16(const WinArgs& a, hipStream_t s);
 hipError_t win_fwd_f32(const WinArgs& a, hipStream_t s);
@@ -156,6 +157,7 @@ hipError_t win_dkdv_bf16(const WinArgs& a, hipStream_t s);
 hipError_t win_dkdv_f32(const WinArgs& a, hipStream_t s);
 hipError_t win_far_bf16(const WinArgs& a, hipStream_t s);      // 2 far slots
 hipError_t win_far_f32(const WinArgs& a, hipStream_t s);       // far slots
+hipError_t win_chunks(Dt t, const WinArgs& a, hipStream_t s);  // adds the chunks up
 hipError_t win_sinks(Dt t, const WinArgs& a, int slots, hipStream_t s);   // adds the slots up
 hipError_t win_dq_bf16(const WinArgs& a, hipStream_t s);
 hipError_t win_dq_f32(const WinArgs& a, hipStream_t s);

@@ -485,6 +485,28 @@ int attn_far(const bpt_attn_config& c) {
   return (int)std::max<int64_t>(1, std::min(512 / groups, tiles / 2));
 }
 int attn_slots(const bpt_attn_config& c, int far) { return 1 + far * (c.dtype == BPT_BF16 ? 2 : 1); }
+// Chunks of every block of keys' tiles in dK and dV: where the blocks (64 keys; fp32: 16) leave CUs idle, enough for two workgroups a CU
+// with at least 4 tiles of 64 queries (fp32: 8 of 16, one a wave) each. Their sums cost a pass over `chunks` fp32 copies of dK and dV.
+int attn_chunks(const bpt_attn_config& c) {
+  const bool bf = c.dtype == BPT_BF16;
+  const int64_t keys = bf ? 64 : 16, blocks = (c.Skv + keys - 1) / keys * c.Hkv * c.B;
+  if (blocks >= 256) return 1;
+  const int64_t span = c.window && !c.sinks ? std::min(c.Sq, (c.causal ? 1 : 2) * c.window + keys) : c.Sq;
+  const int64_t tiles = (span + keys - 1) / keys * (c.Hq / c.Hkv);
+  return (int)std::max<int64_t>(1, std::min<int64_t>({512 / blocks, tiles / (bf ? 4 : 8), 16}));
+}
+// Chunks and far chunks (with chunks, sinks are not apart) and the bytes of their sums
+struct AttnCut {
+  int chunks, far;
+  int64_t bytes;
+};
+AttnCut attn_cut(const bpt_attn_config& c, int chunks, int far) {
+  AttnCut r{chunks, chunks > 1 ? 0 : far, 0};
+  const int64_t row = c.B * c.Hkv * 2 * c.dh * 4;
+  if (r.chunks > 1) r.bytes = r.chunks * row * c.Skv;
+  else if (r.far > 0) r.bytes = attn_slots(c, r.far) * row * std::min(c.sinks, c.Skv);
+  return r;
+}
 
 // Whether no two elements of a tensor share a place (dims of stride and size; features are adjacent)
 bool apart(const bpt_attn_strides& t, int64_t B, int64_t S, int64_t H, int64_t dh) {
@@ -1118,11 +1140,14 @@ static bpt_status layer_bwd(const bpt_config* cfg, const bpt_layer_options* opt,
     // the sums of the sinks' chunks go where the FFN group's buffers are idle; fewer chunks if they do not fit
     const int64_t sinks = std::min(ac.sinks, ac.Skv), room = (char*)w.dh - (char*)w.vg;
     a.part_s = (float*)w.vg;
-    a.far = attn_far(ac);
-    while (a.far > 0 && attn_slots(ac, a.far) * ac.B * ac.Hkv * sinks * 2 * ac.dh * 4 > room) a.far /= 2;
+    AttnCut cut = attn_cut(ac, attn_chunks(ac), attn_far(ac));
+    while (cut.bytes > room) cut = attn_cut(ac, std::max(cut.chunks / 2, 1), cut.far / 2);
+    a.chunks = cut.chunks;
+    a.far = cut.far;
     const double seen = attn_seen(ac);
     RUN("win.delta", 0, 2.0 * T * D * E_, win_delta(E, a, s));
     RUN("win.dkdv", 8.0 * d.dh * seen, 6.0 * T * D * E_, E == BF16 ? win_dkdv_bf16(a, s) : win_dkdv_f32(a, s));
+    if (a.chunks > 1) RUN("win.chunks", 0, (double)cut.bytes + 2.0 * T * D * E_, win_chunks(E, a, s));
     if (a.far > 0) {
       RUN("win.far", 8.0 * d.dh * T * d.H * sinks, 2.0 * T * D * E_, E == BF16 ? win_far_bf16(a, s) : win_far_f32(a, s));
       RUN("win.sinks", 0, (double)attn_slots(ac, a.far) * B * d.H * sinks * d.dh * 8, win_sinks(E, a, attn_slots(ac, a.far), s));
@@ -1526,7 +1551,8 @@ static AttnWs attn_ws(const bpt_attn_config& c, void* base, int backward, int64_
     const int64_t n = c.B * c.Hq * rup(c.Sq, 64) * 4;
     w.ndelta = (float*)bp.take(n);
     w.nlse = (float*)bp.take(n);
-    if (attn_far(c)) w.part_s = (float*)bp.take(attn_slots(c, attn_far(c)) * c.B * c.Hkv * std::min(c.sinks, c.Skv) * 2 * c.dh * 4);
+    const AttnCut cut = attn_cut(c, attn_chunks(c), attn_far(c));
+    if (cut.bytes > 0) w.part_s = (float*)bp.take(cut.bytes);
   } else if (const int z = attn_nsplit(c); z > 1) {
     w.part_o = (float*)bp.take(z * c.B * c.Hq * c.Sq * c.dh * 4);
     w.part_ml = (float*)bp.take(z * c.B * c.Hq * c.Sq * 8);
@@ -1599,14 +1625,18 @@ bpt_status bpt_attn_bwd(const bpt_attn_config* cfg, const void* Q, const void* K
   WinArgs a = attn_args(*cfg, Q, K, V, q_lens, kv_lens, O, lse);
   a.dout = dO; a.dq = dQ; a.dk = dK; a.dv = dV;
   a.ndelta = w.ndelta; a.nlse = w.nlse;
-  a.far = dK ? attn_far(*cfg) : 0;
+  const AttnCut cut = attn_cut(*cfg, attn_chunks(*cfg), attn_far(*cfg));
+  a.far = cut.far;
+  a.chunks = cut.chunks;
   a.part_s = w.part_s;
   hipStream_t s = (hipStream_t)stream;
   const bool bf = cfg->dtype == BPT_BF16;
   const double E_ = bf ? 2 : 4, seen = attn_seen(*cfg), q = (double)cfg->B * cfg->Hq * cfg->Sq * cfg->dh, kv = (double)cfg->B * cfg->Hkv * cfg->Skv * cfg->dh;
   RUN("win.delta", 0, 2.0 * q * E_, win_delta(dt_of(cfg->dtype), a, s));
   if (dK) RUN("win.dkdv", 8.0 * cfg->dh * seen, (2.0 * q + 4.0 * kv) * E_, bf ? win_dkdv_bf16(a, s) : win_dkdv_f32(a, s));
-  if (a.far > 0) {
+  if (dK && a.chunks > 1)
+    RUN("win.chunks", 0, (double)cut.bytes + 2.0 * kv * E_, win_chunks(dt_of(cfg->dtype), a, s));
+  if (dK && a.far > 0) {
     RUN("win.far", 8.0 * cfg->dh * cfg->B * cfg->Hq * cfg->Sq * std::min(cfg->sinks, cfg->Skv), 2.0 * q * E_, bf ? win_far_bf16(a, s) : win_far_f32(a, s));
     RUN("win.sinks", 0, (double)attn_slots(*cfg, a.far) * cfg->B * cfg->Hkv * std::min(cfg->sinks, cfg->Skv) * cfg->dh * 8,
         win_sinks(dt_of(cfg->dtype), a, attn_slots(*cfg, a.far), s));

@@ -58,6 +58,9 @@ BPT_DEV QVis qvis_of(const WinArgs& a, const Seq& s, int k0, int k1, bool near) 
   return v;
 }
 
+// Keys (the first ones) whose dK and dV are left in slots, [slot, B Hkv, keys, dK and dV, dh] fp32, dK without its scale
+BPT_DEV int win_slot_keys(const WinArgs& a) { return a.chunks > 1 ? a.Skv : a.far > 0 ? min(a.sinks, a.Skv) : 0; }
+
 // Key tiles of T keys that a run of queries visits, in ascending order: those of the sinks, then
 // those of the interval.
 template <int T>

@@ -115,6 +115,7 @@ struct WinKvCfg {
 // all others together. Where that matters (a.far), the blocks keep to the window, and what sinks see
 // beyond it is cut into a.far chunks of (query head, tile of 64 queries) for workgroups of their own (FAR: 32 sinks,
 // two waves, each half the queries of a tile). All leave the sinks' sums in fp32 slots, which win_sinks adds in order.
+// Few blocks of keys with many tiles (grouped heads, small batches) are cut into a.chunks of those in the same way, for all keys.
 template <int DH, int KG, int QH, bool FAR>
 __global__ __launch_bounds__(64 * KG * QH, KG * QH == 8 ? 1 : 2) void win_dkdv_bf16_kernel(WinArgs a) {
   using C = WinKvCfg<DH, KG, QH>;
@@ -127,8 +128,8 @@ __global__ __launch_bounds__(64 * KG * QH, KG * QH == 8 ? 1 : 2) void win_dkdv_b
   xcd_map((int)blockIdx.x, a.Hkv * a.B, hh, blk);
   const int kvh = hh % a.Hkv, b = hh / a.Hkv;
   const Seq sq = seq_of(a, b);
-  const int chunk = FAR ? blk % a.far : 0;
-  const int k0 = (FAR ? blk / a.far : blk) * C::KEYS, part = wave / KG, kw = k0 + 32 * (wave % KG), key = kw + (lane & 31);
+  const int chunks = FAR ? a.far : a.chunks, chunk = blk % chunks;
+  const int k0 = blk / chunks * C::KEYS, part = wave / KG, kw = k0 + 32 * (wave % KG), key = kw + (lane & 31);
   const float c = a.scale * LOG2E;
   const bool near = FAR || a.far > 0;               // the window alone, or beyond it
 
@@ -141,8 +142,8 @@ __global__ __launch_bounds__(64 * KG * QH, KG * QH == 8 ? 1 : 2) void win_dkdv_b
     run = qvis_of(a, sq, k0, min(k0 + C::KEYS, kend) - 1, near);
     if (FAR) run = QVis{a.causal ? max(k0 + a.window - sq.off, 0) : 0, sq.nq - 1};
   }
-  const int t0 = run.lo / 64, nt = run.hi >= run.lo ? run.hi / 64 + 1 - t0 : 0;
-  const int per = FAR ? (nt * a.G + a.far - 1) / a.far : nt * a.G;
+  const int t0 = run.lo / 64, nt = run.hi >= run.lo ? run.hi / 64 + 1 - t0 : 0;   // tiles of a query head
+  const int per = (nt * a.G + chunks - 1) / chunks;
   const int j0 = chunk * per, n = min(per, nt * a.G - j0);
   if (n > 0) {
     // keys behind the sequence's last stand for it; their results are left out in the end
@@ -155,15 +156,24 @@ __global__ __launch_bounds__(64 * KG * QH, KG * QH == 8 ? 1 : 2) void win_dkdv_b
     // the queries that all of the wave's keys see: the first key behind the sinks has the lowest end
     const int ks = !near && kw < a.sinks && a.sinks <= kl ? a.sinks : kw;
     const int all_lo = max(first.lo, last.lo), all_hi = min(qvis_of(a, sq, ks, ks, near).hi, last.hi);
+    // stages are requested, and worked on, in order: each keeps its own place (query head, tile) of the list
+    RingOff<DH, NW> roff;                             // two waves have 19 copies each: too many registers
+    if constexpr (!FAR) roff = ring_offsets<DH, NW>(a.q_st, a.o_st, wave, lane);
+    int ih = kvh * a.G + j0 / nt, it = j0 % nt, at = it;
     auto issue = [&](int j) {
-      const int it = j0 + j, h = kvh * a.G + it / nt, q0 = 64 * (t0 + it % nt);
+      const int q0 = 64 * (t0 + it);
       char* st = smem + (j % C::NS) * C::STAGE;
-      issue_picked<DH, NW>(st, (const bf16*)a.q + (int64_t)b * a.q_sb + (int64_t)h * a.q_sh, a.q_st,
-                           (const bf16*)a.dout + (int64_t)b * a.o_sb + (int64_t)h * a.o_sh, a.o_st, q0, wave, lane,
-                           [&](int q) { return min(max(q, run.lo), run.hi); });
-      const int64_t sidx = ((int64_t)b * a.Hq + h) * a.Sqp + q0;       // Sqp % 64 == 0: in bounds
+      const bf16* q = (const bf16*)a.q + (int64_t)b * a.q_sb + (int64_t)ih * a.q_sh;
+      const bf16* o = (const bf16*)a.dout + (int64_t)b * a.o_sb + (int64_t)ih * a.o_sh;
+      if (!FAR && q0 >= run.lo && q0 + 63 <= run.hi) ring_issue_full<DH, NW>(st, q, a.q_st, q0, o, a.o_st, q0, roff, wave);
+      else issue_picked<DH, NW>(st, q, a.q_st, o, a.o_st, q0, wave, lane, [&](int r) { return min(max(r, run.lo), run.hi); });
+      const int64_t sidx = ((int64_t)b * a.Hq + ih) * a.Sqp + q0;      // Sqp % 64 == 0: in bounds
       dma4s(scalar_ptr(a.nlse + sidx), 4u * lane, st + 2 * C::TB);
       dma4s(scalar_ptr(a.ndelta + sidx), 4u * lane, st + 2 * C::TB + 256);
+      if (++it == nt) {
+        it = 0;
+        ++ih;
+      }
     };
     ring_start<C>(n, issue);
     bf16x8 kf[C::KSTEPS], vf[C::KSTEPS];
@@ -199,7 +209,7 @@ __global__ __launch_bounds__(64 * KG * QH, KG * QH == 8 ? 1 : 2) void win_dkdv_b
       for (int kk = 0; kk < C::KSTEPS; ++kk) {
         s = mfma32x32x16(frag_rows<DH>(qs, 32 * mt, 2 * kk, lane), kf[kk], s);
         dp = mfma32x32x16(frag_rows<DH>(ds, 32 * mt, 2 * kk, lane), vf[kk], dp);
-        __builtin_amdgcn_sched_barrier(0);           // bound the fragments read ahead
+        if constexpr (DH == 128) __builtin_amdgcn_sched_barrier(0);   // bound the fragments read ahead
       }
       pin(dp);
 #pragma unroll
@@ -227,12 +237,13 @@ __global__ __launch_bounds__(64 * KG * QH, KG * QH == 8 ? 1 : 2) void win_dkdv_b
         for (int t = 0; t < C::DT; ++t) {
           adv[t] = mfma32x32x16(frag_tr<DH>(ds, 32 * mt + 16 * hf, 32 * t, lane), pb, adv[t]);
           adk[t] = mfma32x32x16(frag_tr<DH>(qs, 32 * mt + 16 * hf, 32 * t, lane), sb, adk[t]);
-          __builtin_amdgcn_sched_barrier(0);
+          if constexpr (DH == 128) __builtin_amdgcn_sched_barrier(0);
         }
       }
     };
     ring_loop<C, C::DPS>(n, issue, [&](int j) {
-      const int q0 = 64 * (t0 + (j0 + j) % nt);
+      const int q0 = 64 * (t0 + at);
+      at = at + 1 == nt ? 0 : at + 1;
       if constexpr (FAR) {
         // columns of keys that are no sinks are never stored and need no mask
         half(j, q0, part, a.causal && q0 > last.hi && q0 + 63 <= run.hi);
@@ -247,36 +258,28 @@ __global__ __launch_bounds__(64 * KG * QH, KG * QH == 8 ? 1 : 2) void win_dkdv_b
       }
     });
   }
-  if constexpr (!FAR && QH == 2) {                    // the second half's sums, a group's [lane][register] apart
-    __syncthreads();
-    float* red = (float*)smem + (wave % KG) * 32 * C::DT * 64 + lane;
-    if (part == 1) {
+  if constexpr (!FAR && QH == 2) {
+    f32x16 both[2 * C::DT];
 #pragma unroll
-      for (int t = 0; t < C::DT; ++t)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          red[(32 * t + r) * 64] = adk[t][r];
-          red[(32 * t + 16 + r) * 64] = adv[t][r];
-        }
+    for (int t = 0; t < C::DT; ++t) {
+      both[t] = adk[t];
+      both[C::DT + t] = adv[t];
     }
-    __syncthreads();
-    if (part == 1) return;
+    if (add_halves<KG, 2 * C::DT>(smem, both, wave, lane)) return;
 #pragma unroll
-    for (int t = 0; t < C::DT; ++t)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        adk[t][r] += red[(32 * t + r) * 64];
-        adv[t][r] += red[(32 * t + 16 + r) * 64];
-      }
+    for (int t = 0; t < C::DT; ++t) {
+      adk[t] = both[t];
+      adv[t] = both[C::DT + t];
+    }
   }
   if (key >= sq.nk) {
 #pragma unroll
     for (int t = 0; t < C::DT; ++t) adv[t] = adk[t] = f32x16{};
   }
-  if (a.far > 0 && key < min(a.sinks, a.Skv)) {
-    // slot 0: the window's part, then 2 per chunk; [slot, B Hkv, sinks, dK and dV, dh]
-    const int ns = min(a.sinks, a.Skv);
-    const int64_t slot = FAR ? 1 + 2 * chunk + part : 0;
+  const int ns = win_slot_keys(a);
+  if (key < ns) {
+    // chunks: one slot for each; far: slot 0 the window's part, then two for each of its chunks
+    const int64_t slot = FAR ? 1 + 2 * chunk + part : chunk;
     float* p = a.part_s + ((slot * a.B * a.Hkv + (int64_t)b * a.Hkv + kvh) * ns + key) * 2 * DH;
 #pragma unroll
     for (int t = 0; t < C::DT; ++t)
@@ -295,7 +298,7 @@ __global__ __launch_bounds__(64 * KG * QH, KG * QH == 8 ? 1 : 2) void win_dkdv_b
 template <int DH, int KG, int QH, bool FAR>
 static hipError_t launch_dkdv(const WinArgs& a, int64_t blocks, hipStream_t s) {
   using C = WinKvCfg<DH, KG, QH>;
-  static_assert(FAR || QH == 1 || KG * C::DT * 32 * 64 * 4 <= C::LDS, "the second halves fit the ring");
+  static_assert(FAR || QH == 1 || KG * 2 * C::DT * 4096 <= C::LDS, "the second halves fit the ring");
   auto k = win_dkdv_bf16_kernel<DH, KG, QH, FAR>;
   hipError_t e = set_lds(k, C::LDS);
   if (e != hipSuccess) return e;
@@ -304,9 +307,14 @@ static hipError_t launch_dkdv(const WinArgs& a, int64_t blocks, hipStream_t s) {
 }
 template <int DH>
 static hipError_t dkdv(const WinArgs& a, hipStream_t s) {
+  // Long runs of tiles that fill the chip twice over: blocks of 256 keys (full attention of 32768 tokens, 32 heads of 128: 16.1
+  // ms, blocks of 64 17.7). Else of 64, two to three workgroups on a CU, one at its start or end while others work: 4000
+  // tokens, 16 heads, window 512 66 us (74); 4 x 1000 tokens, 12 heads of 64, window 256 25 (29); heads of 64 at any length: 16384
+  // tokens, window 2048 289 (331), full attention of 32768 tokens, 16 heads 4.24 ms (4.37).
   const int64_t wide = ((int64_t)a.Skv + 255) / 256;
-  if (getenv("KV8")) return launch_dkdv<DH, 8, 1, false>(a, wide, s);
-  return launch_dkdv<DH, 4, 2, false>(a, ((int64_t)a.Skv + 127) / 128, s);
+  if constexpr (DH == 128)
+    if (!a.window && wide * a.Hkv * a.B >= 512) return launch_dkdv<DH, 8, 1, false>(a, wide, s);
+  return launch_dkdv<DH, 2, 2, false>(a, ((int64_t)a.Skv + 63) / 64 * a.chunks, s);
 }
 template <int DH>
 static hipError_t far(const WinArgs& a, hipStream_t s) {

@@ -305,8 +305,8 @@ __global__ __launch_bounds__(512) void win_dkdv_f32_kernel(WinArgs a) {
   constexpr int NC = DH / 16;
   __shared__ __attribute__((aligned(16))) float red[4][16][DH + 4];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, g = lane >> 4, c16 = lane & 15;
-  const int chunk = FAR ? blockIdx.x % a.far : 0;
-  const int kvh = blockIdx.y, b = blockIdx.z, k0 = (FAR ? blockIdx.x / a.far : blockIdx.x) * 16, key = k0 + c16;
+  const int chunks = FAR ? a.far : a.chunks, chunk = blockIdx.x % chunks;
+  const int kvh = blockIdx.y, b = blockIdx.z, k0 = blockIdx.x / chunks * 16, key = k0 + c16;
   const Seq sq = seq_of(a, b);
   const bool near = FAR || a.far > 0;
   const int kend = FAR ? min(sq.nk, a.sinks) : sq.nk;
@@ -323,7 +323,7 @@ __global__ __launch_bounds__(512) void win_dkdv_f32_kernel(WinArgs a) {
     const RowFrag<DH> kf = row_frag<DH>((const float*)a.k + (int64_t)b * a.k_sb + (int64_t)kvh * a.k_sh + (int64_t)kr * a.k_st, g);
     const RowFrag<DH> vf = row_frag<DH>((const float*)a.v + (int64_t)b * a.v_sb + (int64_t)kvh * a.v_sh + (int64_t)kr * a.v_st, g);
     const int t0 = run.lo / 16, nt = run.hi >= run.lo ? run.hi / 16 + 1 - t0 : 0;
-    const int per = FAR ? (nt * a.G + a.far - 1) / a.far : nt * a.G;
+    const int per = (nt * a.G + chunks - 1) / chunks;
     for (int it = chunk * per + wave; it < min((chunk + 1) * per, nt * a.G); it += 8) {
       const int h = kvh * a.G + it / nt, q0 = 16 * (t0 + it % nt);
       const float* Qb = (const float*)a.q + (int64_t)b * a.q_sb + (int64_t)h * a.q_sh;
@@ -373,12 +373,12 @@ __global__ __launch_bounds__(512) void win_dkdv_f32_kernel(WinArgs a) {
     float* out = (float*)(which ? a.dv : a.dk) + base;
     for (int e = tid; e < 16 * (DH / 4); e += 512) {
       const int ki = e / (DH / 4), d = 4 * (e % (DH / 4));
-      const int ns = a.far > 0 ? min(a.sinks, a.Skv) : 0;
+      const int ns = win_slot_keys(a);
       if (k0 + ki >= (FAR ? ns : a.Skv)) continue;
       const f32x4 x = ((*(const f32x4*)&red[0][ki][d] + *(const f32x4*)&red[1][ki][d]) + *(const f32x4*)&red[2][ki][d]) +
                       *(const f32x4*)&red[3][ki][d];
-      if (k0 + ki < ns) {                            // [slot, B Hkv, sinks, dK and dV, dh]
-        const int64_t at = ((int64_t)(FAR ? 1 + chunk : 0) * a.B * a.Hkv + (int64_t)b * a.Hkv + kvh) * ns + k0 + ki;
+      if (k0 + ki < ns) {
+        const int64_t at = ((int64_t)(FAR ? 1 + chunk : chunk) * a.B * a.Hkv + (int64_t)b * a.Hkv + kvh) * ns + k0 + ki;
         *(f32x4*)(a.part_s + (2 * at + which) * DH + d) = x;
         continue;
       }
@@ -419,10 +419,26 @@ __global__ __launch_bounds__(256) void win_sinks_kernel(WinArgs a, int slots) {
   for (int e = 0; e < 4; ++e) out[4 * l + e] = from_f32<T>(x[e]);
 }
 
+// dK and dV of all keys from a few slots, in order: 4 features a thread.
+template <typename T>
+__global__ __launch_bounds__(256) void win_chunks_kernel(WinArgs a) {
+  const int L = a.dh / 4, at = blockIdx.x * 256 + threadIdx.x, key = at / (2 * L), which = at / L % 2, d = 4 * (at % L);
+  const int kvh = blockIdx.y, b = blockIdx.z;
+  if (key >= a.Skv) return;
+  const int64_t rows = (int64_t)a.B * a.Hkv * a.Skv * 2, row = (((int64_t)b * a.Hkv + kvh) * a.Skv + key) * 2 + which;
+  f32x4 x = {};
+  if (key < seq_of(a, b).nk)
+    for (int z = 0; z < a.chunks; ++z) x += *(const f32x4*)(a.part_s + (z * rows + row) * a.dh + d);
+  if (!which) x *= a.scale;
+  T* out = which ? (T*)a.dv + b * a.v_sb + (int64_t)key * a.v_st + kvh * a.v_sh : (T*)a.dk + b * a.k_sb + (int64_t)key * a.k_st + kvh * a.k_sh;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) out[d + e] = from_f32<T>(x[e]);
+}
+
 template <int DH>
 static hipError_t dkdv_f32(const WinArgs& a, hipStream_t s) {
   auto k = win_dkdv_f32_kernel<DH, false>;
-  hipLaunchKernelGGL(k, dim3((a.Skv + 15) / 16, a.Hkv, a.B), dim3(512), 0, s, a);
+  hipLaunchKernelGGL(k, dim3((a.Skv + 15) / 16 * a.chunks, a.Hkv, a.B), dim3(512), 0, s, a);
   return hipGetLastError();
 }
 template <int DH>
@@ -445,6 +461,11 @@ hipError_t win_dq_f32(const WinArgs& a, hipStream_t s) { return a.dh == 64 ? dq_
 hipError_t win_join(Dt t, const WinArgs& a, hipStream_t s) {
   auto k = t == BF16 ? win_join_kernel<bf16> : win_join_kernel<float>;
   hipLaunchKernelGGL(k, dim3((unsigned)(((int64_t)a.Sq * a.G + 3) / 4), a.Hkv, a.B), dim3(256), 0, s, a);
+  return hipGetLastError();
+}
+hipError_t win_chunks(Dt t, const WinArgs& a, hipStream_t s) {
+  auto k = t == BF16 ? win_chunks_kernel<bf16> : win_chunks_kernel<float>;
+  hipLaunchKernelGGL(k, dim3((unsigned)(((int64_t)a.Skv * a.dh / 2 + 255) / 256), a.Hkv, a.B), dim3(256), 0, s, a);
   return hipGetLastError();
 }
 hipError_t win_sinks(Dt t, const WinArgs& a, int slots, hipStream_t s) {

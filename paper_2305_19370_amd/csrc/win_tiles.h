@@ -18,7 +18,7 @@ template <int N = 0> BPT_DEV void wait_lgkm() { asm volatile("s_waitcnt lgkmcnt(
 // hold their fragments in registers meanwhile.
 BPT_DEV void pin(f32x16& x) { asm volatile("" : "+v"(x)); }
 
-// NW waves of 32 rows (keys, in the dK dV kernel) share tiles of 64 rows of two tensors in a ring
+// NW waves of 32 rows share tiles of 64 rows of two tensors in a ring
 template <int DH, int NWAVES>
 struct WinCfg {
   static constexpr int KSTEPS = DH / 16, DT = DH / 32;
@@ -28,6 +28,26 @@ struct WinCfg {
   static constexpr int LDS = NS * STAGE;
   static constexpr int DPS = Ring2<DH, NW>::DPW;    // copies per wave per stage
 };
+
+// Adds the sums of wave g + G to those of wave g, g < G, through LDS that is done with. True: a wave that has given its own.
+template <int G, int N>
+BPT_DEV bool add_halves(char* smem, f32x16 (&x)[N], int wave, int lane) {
+  float* red = (float*)smem + (wave % G) * N * 1024 + lane;   // [register][lane]
+  __syncthreads();
+  if (wave >= G) {
+#pragma unroll
+    for (int t = 0; t < N; ++t)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) red[(16 * t + r) * 64] = x[t][r];
+  }
+  __syncthreads();
+  if (wave >= G) return true;
+#pragma unroll
+  for (int t = 0; t < N; ++t)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) x[t][r] += red[(16 * t + r) * 64];
+  return false;
+}
 
 // Row r0 + w0 + lane % 32 of a kv head's list r = token * G + head, what it sees, and what its wave and its
 // workgroup of n rows (from r0) see. Rows behind the sequence's last stand for its last: they need no masks of their own, and

@@ -77,6 +77,9 @@ SHAPES = [
     (2, 1500, 1500, 4, 2, True, 64, 33),
     (1, 1500, 1500, 2, 2, False, 40, 70),
     (1, 300, 2500, 8, 1, True, 50, 4),
+    (4, 600, 600, 16, 8, True, 40, 5),              # blocks of keys enough for the chip: sinks apart
+    (5, 530, 530, 16, 8, False, 30, 40),
+    (1, 900, 900, 16, 2, True, 0, 0),               # few blocks, many heads: cut into chunks
     (1, 260, 260, 2, 2, True, 5000, 4),             # a window longer than the sequence
     (1, 260, 260, 2, 2, True, 16, 1000),            # more sinks than keys
 ]
@@ -115,6 +118,17 @@ LENS = [
     (2, 70, 300, [70, 9], [299, 65], 33, 4, False),
     (3, 1500, 1500, [1500, 90, 0], [1500, 90, 3], 64, 40, True),
 ]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_lengths_of_a_batch_with_sinks_apart(dtype):
+    ql = kl = [700, 333, 5, 0]
+    q, k, v, do = make(4, 700, 700, 16, 8, 64, dtype, seed=21)
+    kw = dict(causal=True, window=33, sinks=7)
+    got = run(q, k, v, do, q_lens=ql, kv_lens=kl, **kw)
+    ref, err = attention(q, k, v, do, q_lens=ql, kv_lens=kl, **kw)
+    for n in ref:
+        check(got[n], ref[n], err[n], n)
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
