@@ -271,6 +271,15 @@ def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
     return None if t is None else t.data_ptr()
 
 
+def _int32(t: Optional[torch.Tensor], n: int, name: str) -> Optional[int]:
+    """The address of n contiguous int32 on the GPU, or None."""
+    if t is None:
+        return None
+    if t.dtype != torch.int32 or t.numel() != n or not t.is_contiguous() or not t.is_cuda:
+        raise ValueError(f"{name} must be {n} contiguous int32 on the GPU")
+    return t.data_ptr()
+
+
 def _stream() -> int:
     """The current device's current stream (read without torch's stream object, 2.4 us less a call)."""
     if torch.cuda.is_initialized():
@@ -538,11 +547,11 @@ def rope_validate(cfg: RopeConfig) -> int:
 
 
 def rope_fwd(cfg: RopeConfig, X: torch.Tensor, Y: torch.Tensor, positions: Optional[torch.Tensor] = None) -> None:
-    _check(load().bpt_rope_fwd(ctypes.byref(cfg), _ptr(positions), X.data_ptr(), Y.data_ptr(), _stream()))
+    _check(load().bpt_rope_fwd(ctypes.byref(cfg), _int32(positions, cfg.rows, "positions"), X.data_ptr(), Y.data_ptr(), _stream()))
 
 
 def rope_bwd(cfg: RopeConfig, dY: torch.Tensor, dX: torch.Tensor, positions: Optional[torch.Tensor] = None) -> None:
-    _check(load().bpt_rope_bwd(ctypes.byref(cfg), _ptr(positions), dY.data_ptr(), dX.data_ptr(), _stream()))
+    _check(load().bpt_rope_bwd(ctypes.byref(cfg), _int32(positions, cfg.rows, "positions"), dY.data_ptr(), dX.data_ptr(), _stream()))
 
 
 # ---------------------------------------------------------------- attention with a window and sinks
@@ -578,14 +587,16 @@ def attn_fwd(cfg: AttnConfig, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
              workspace: Optional[torch.Tensor] = None, q_lens: Optional[torch.Tensor] = None,
              kv_lens: Optional[torch.Tensor] = None) -> None:
     nb = 0 if workspace is None else workspace.numel() * workspace.element_size()
-    _check(load().bpt_attn_fwd(ctypes.byref(cfg), q.data_ptr(), k.data_ptr(), v.data_ptr(), _ptr(q_lens), _ptr(kv_lens),
+    _check(load().bpt_attn_fwd(ctypes.byref(cfg), q.data_ptr(), k.data_ptr(), v.data_ptr(),
+                               _int32(q_lens, cfg.B, "q_lens"), _int32(kv_lens, cfg.B, "kv_lens"),
                                o.data_ptr(), lse.data_ptr(), _ptr(workspace) if nb else None, nb, _stream()))
 
 
 def attn_bwd(cfg: AttnConfig, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, o: torch.Tensor, lse: torch.Tensor,
              do: torch.Tensor, dq: Optional[torch.Tensor], dk: Optional[torch.Tensor], dv: Optional[torch.Tensor],
              workspace: torch.Tensor, q_lens: Optional[torch.Tensor] = None, kv_lens: Optional[torch.Tensor] = None) -> None:
-    _check(load().bpt_attn_bwd(ctypes.byref(cfg), q.data_ptr(), k.data_ptr(), v.data_ptr(), _ptr(q_lens), _ptr(kv_lens),
+    _check(load().bpt_attn_bwd(ctypes.byref(cfg), q.data_ptr(), k.data_ptr(), v.data_ptr(),
+                               _int32(q_lens, cfg.B, "q_lens"), _int32(kv_lens, cfg.B, "kv_lens"),
                                o.data_ptr(), lse.data_ptr(), do.data_ptr(), _ptr(dq), _ptr(dk), _ptr(dv), workspace.data_ptr(),
                                workspace.numel() * workspace.element_size(), _stream()))
 
@@ -603,6 +614,8 @@ class WindowAttention:
     def forward(self, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, q_lens: Optional[torch.Tensor] = None,
                 kv_lens: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:
         """O [B, Sq, Hq, dh] and the log-sum-exp [B, Hq, Sq]."""
+        if not (q.is_cuda and q.device == k.device == v.device):
+            raise ValueError("q, k and v must be on one GPU")
         o = torch.empty(q.shape, dtype=q.dtype, device=q.device)
         lse = torch.empty((q.shape[0], q.shape[2], q.shape[1]), dtype=torch.float32, device=q.device)
         cfg = attn_config_of(q, k, v, o, **self.kw)
@@ -646,6 +659,9 @@ class AdamWTensors:
             for name, (dt, size) in need.items():
                 if t[name].dtype != dt or t[name].numel() != size or not t[name].is_contiguous():
                     raise ValueError(f"{name} must be contiguous, of type {dt} and of {size} elements")
+        self.device = self.tensors[0]["p"].device if self.tensors else None
+        if any(x.device != self.device for t in self.tensors for x in t.values() if isinstance(x, torch.Tensor)):
+            raise ValueError("the tensors of a list must be on one device")
         self.grad_dtype = BPT_BF16 if gts == {torch.bfloat16} else BPT_F32
         self.lowp_dtype = BPT_BF16 if lows == {torch.bfloat16} else BPT_F32
         self.array = (AdamWTensor * max(len(self.tensors), 1))(*[
@@ -657,5 +673,7 @@ class AdamWTensors:
 def adamw_multi(tensors: AdamWTensors, step: int, lr: float, beta1: float = 0.9, beta2: float = 0.95, eps: float = 1e-8,
                 seed: int = 0) -> None:
     """One AdamW update of every tensor of the list, in place."""
+    if tensors.device is not None and tensors.device.type != "cuda":
+        raise ValueError("the tensors must be on the GPU")
     cfg = AdamWMultiConfig(lr, beta1, beta2, eps, step, seed & (2 ** 64 - 1), tensors.bits, tensors.grad_dtype, tensors.lowp_dtype, 0)
     _check(load().bpt_adamw_multi(ctypes.byref(cfg), tensors.array, len(tensors.tensors), _stream()))

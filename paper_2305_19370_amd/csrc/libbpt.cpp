@@ -482,6 +482,7 @@ int attn_far(const bpt_attn_config& c) {
   const int64_t G = c.Hq / c.Hkv, tiles = (c.Sq - std::min(c.Sq, c.window) + 63) / 64 * G;
   if (tiles < 16) return 0;
   const int64_t groups = c.B * c.Hkv * ((std::min(c.sinks, c.Skv) + 31) / 32);
+  if (groups >= 512) return 0;                       // so many that their own blocks fill the chip
   return (int)std::max<int64_t>(1, std::min(512 / groups, tiles / 2));
 }
 int attn_slots(const bpt_attn_config& c, int far) { return 1 + far * (c.dtype == BPT_BF16 ? 2 : 1); }
@@ -1524,19 +1525,21 @@ bpt_status bpt_rope_bwd(const bpt_rope_config* cfg, const int32_t* positions, co
 }
 
 // ---------------------------------------------------------------- attention with a window and sinks
-// A bf16 forward whose blocks of 128 rows would leave most CUs idle takes the kernel for few rows.
+// A bf16 forward whose blocks of 128 rows would leave most CUs idle takes the kernel for few rows: 512 tokens, 8 heads of
+// 128 13.3 us (blocks of 128: 19.7); 1000 tokens, 4 key heads of 4 50 (30).
 static bool attn_few(const bpt_attn_config& c) {
   const int64_t rows = c.Sq * (c.Hq / c.Hkv);
   return c.dtype == BPT_BF16 && (rows <= 32 || (rows + 127) / 128 * c.Hkv * c.B <= 64);
 }
-// Slices of the keys for a forward of few rows: enough workgroups for the chip, and 128 keys (bf16: a tile per wave) at
-// least for each; none where a workgroup is done with them before a second launch would be.
+// Slices of the keys for a forward of few rows: workgroups for the chip several times over (sequences are of unequal length),
+// and 128 keys (bf16: a tile per wave) at least for each; none where a workgroup is done before a second launch would be, or
+// where the rows alone fill the chip.
 static int attn_nsplit(const bpt_attn_config& c) {
   const bool bf = c.dtype == BPT_BF16;
   if (bf && !attn_few(c)) return 1;
   const int64_t rows = c.Sq * (c.Hq / c.Hkv), groups = (rows + (bf ? 31 : 15)) / (bf ? 32 : 16) * c.Hkv * c.B;
   const int64_t span = c.window ? std::min(c.Skv, (c.causal ? 1 : 2) * c.window + c.sinks + c.Sq) : c.Skv;
-  if (span <= 512) return 1;
+  if (span <= 512 || groups >= 256) return 1;
   return (int)std::max<int64_t>(1, std::min<int64_t>({1024 / groups, span / (bf ? 128 : 512), 64}));
 }
 
@@ -1661,15 +1664,19 @@ bpt_status bpt_adamw_multi(const bpt_adamw_multi_config* cfg, const bpt_adamw_te
   if (cfg->step < 1) return fail(BPT_ERR_INVALID_ARG, "step must be >= 1");
   if (!(cfg->beta1 >= 0.0 && cfg->beta1 < 1.0 && cfg->beta2 >= 0.0 && cfg->beta2 < 1.0))
     return fail(BPT_ERR_INVALID_ARG, "beta1 and beta2 must lie in [0, 1)");
-  if (!((float)cfg->eps > 0.0f) || !(cfg->lr >= 0.0) || !std::isfinite(cfg->lr) || !std::isfinite(cfg->eps))
-    return fail(BPT_ERR_INVALID_ARG, "eps must be > 0, lr >= 0");
+  if (!(cfg->eps >= 1.1754943508222875e-38) || !(cfg->lr >= 0.0) || !std::isfinite(cfg->lr) || !std::isfinite(cfg->eps))
+    return fail(BPT_ERR_INVALID_ARG, "eps must be > 0 (a normal fp32 number), lr >= 0");
   if (cfg->state_bits != 32 && cfg->state_bits != 8) return fail(BPT_ERR_INVALID_ARG, "state_bits must be 32 or 8");
   if (cfg->reserved != 0) return fail(BPT_ERR_INVALID_ARG, "reserved must be 0");
   bpt_status st = dtype_ok(cfg->grad_dtype, "grad_dtype");
   if (st != BPT_OK || (st = dtype_ok(cfg->lowp_dtype, "lowp_dtype")) != BPT_OK) return st;
   const bool small = cfg->state_bits == 8;
   std::vector<std::pair<uintptr_t, uintptr_t>> at;
-  at.reserve(count);
+  try {
+    at.reserve(count);
+  } catch (const std::exception&) {
+    return fail(BPT_ERR_UNSUPPORTED, "no host memory for the list of tensors");
+  }
   for (int64_t i = 0; i < count; ++i) {
     const bpt_adamw_tensor& t = tensors[i];
     if (t.n < 0) return fail(BPT_ERR_INVALID_ARG, "tensor %lld: n must be >= 0", (long long)i);

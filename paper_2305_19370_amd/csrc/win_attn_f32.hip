@@ -117,7 +117,7 @@ __global__ __launch_bounds__(256) void win_fwd_f32_kernel(WinArgs a) {
     f32x4 o = {};
 #pragma unroll
     for (int w = 0; w < 4; ++w) {
-      const float f = red_m[w][ri] == NEG_INF ? 0.0f : fast_exp2(red_m[w][ri] - m);
+      const float f = red_m[w][ri] == NEG_INF ? 1.0f : fast_exp2(red_m[w][ri] - m);   // without keys: zeros (or a NaN)
       l = fmaf(red_l[w][ri], f, l);
       o += f * *(const f32x4*)&red[w][ri][d];
     }
@@ -131,9 +131,9 @@ __global__ __launch_bounds__(256) void win_fwd_f32_kernel(WinArgs a) {
       continue;
     }
     const int ii = rr / a.G, hh = kvh * a.G + rr % a.G;
-    const float inv = l > 0.0f ? 1.0f / l : 0.0f;   // a row that sees nothing: 0
-    *(f32x4*)((float*)a.o + (int64_t)b * a.o_sb + (int64_t)ii * a.o_st + (int64_t)hh * a.o_sh + d) = l > 0.0f ? o * inv : f32x4{};
-    if (d == 0) a.lse[((int64_t)b * a.Hq + hh) * a.lse_ld + ii] = l > 0.0f ? (m + log2f(l)) * LN2 : NEG_INF;
+    const float inv = l != 0.0f ? 1.0f / l : 0.0f;  // a row that sees nothing: 0 (a NaN stays one)
+    *(f32x4*)((float*)a.o + (int64_t)b * a.o_sb + (int64_t)ii * a.o_st + (int64_t)hh * a.o_sh + d) = l != 0.0f ? o * inv : f32x4{};
+    if (d == 0) a.lse[((int64_t)b * a.Hq + hh) * a.lse_ld + ii] = l != 0.0f ? (m + log2f(l)) * LN2 : NEG_INF;
   }
 }
 
@@ -149,20 +149,19 @@ __global__ __launch_bounds__(256) void win_join_kernel(WinArgs a) {
   for (int z = 0; z < a.nsplit; ++z) m = fmaxf(m, a.part_ml[2 * (z * all + at)]);
   const int d = a.dh == 128 ? 2 * lane : lane;
   float l = 0.0f, o0 = 0.0f, o1 = 0.0f;
-  if (m > NEG_INF)
-    for (int z = 0; z < a.nsplit; ++z) {
-      const int64_t p = z * all + at;
-      const float f = fast_exp2(a.part_ml[2 * p] - m);   // 0 for a slice without keys
-      l = fmaf(a.part_ml[2 * p + 1], f, l);
-      o0 = fmaf(a.part_o[p * a.dh + d], f, o0);
-      if (a.dh == 128) o1 = fmaf(a.part_o[p * a.dh + d + 1], f, o1);
-    }
-  const float inv = l > 0.0f ? 1.0f / l : 0.0f;
+  for (int z = 0; z < a.nsplit; ++z) {
+    const int64_t p = z * all + at;
+    const float f = a.part_ml[2 * p] == NEG_INF ? 1.0f : fast_exp2(a.part_ml[2 * p] - m);   // without keys: zeros (or a NaN)
+    l = fmaf(a.part_ml[2 * p + 1], f, l);
+    o0 = fmaf(a.part_o[p * a.dh + d], f, o0);
+    if (a.dh == 128) o1 = fmaf(a.part_o[p * a.dh + d + 1], f, o1);
+  }
+  const float inv = l != 0.0f ? 1.0f / l : 0.0f;
   const int i = rr / a.G, h = kvh * a.G + rr % a.G;
   T* o = (T*)a.o + (int64_t)b * a.o_sb + (int64_t)i * a.o_st + (int64_t)h * a.o_sh + d;
   o[0] = from_f32<T>(o0 * inv);
   if (a.dh == 128) o[1] = from_f32<T>(o1 * inv);
-  if (lane == 0) a.lse[((int64_t)b * a.Hq + h) * a.lse_ld + i] = l > 0.0f ? (m + log2f(l)) * LN2 : NEG_INF;
+  if (lane == 0) a.lse[((int64_t)b * a.Hq + h) * a.lse_ld + i] = l != 0.0f ? (m + log2f(l)) * LN2 : NEG_INF;
 }
 
 // -Delta = -sum_d dO O and -lse / scale (what the raw products are reduced by) of every row, [B, Hq, Sqp]; 0 where a row
@@ -209,7 +208,7 @@ __global__ __launch_bounds__(256) void win_delta_kernel(WinArgs a) {
     const int64_t o = (int64_t)b * a.o_sb + (int64_t)i * a.o_st + (int64_t)h * a.o_sh + d;
     const Row8 g((const T*)a.dout + o), out((const T*)a.o + o);
     const float lse = a.lse[((int64_t)b * a.Hq + h) * a.lse_ld + i];
-    const bool sees = lse > NEG_INF;
+    const bool sees = lse != NEG_INF;
     nl = sees ? -lse / a.scale : 0.0f;
     const Vis v = vis_of(a, sq, sq.off + i, sq.off + i);
     const int from = max(v.lo, v.se), n = v.se + max(v.hi + 1 - from, 0);   // keys 0 .. se - 1 and from .. hi

@@ -107,7 +107,7 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 1 : 2) void win_fwd_bf16_kernel(
   }
   const float l = sum_halves(l_run);
   if (w.i < a.Sq) {
-    const bool sees = l > 0.0f && w.exists;          // a row that sees nothing: 0
+    const bool sees = l != 0.0f && w.exists;         // a row that sees nothing: 0 (a NaN stays one)
     const float inv = sees ? 1.0f / l : 0.0f;
     if (!sees) {
 #pragma unroll
@@ -224,15 +224,17 @@ __global__ __launch_bounds__(256, 1) void win_token_kernel(WinArgs a) {
     float m = NEG_INF, lt = 0.0f;
 #pragma unroll
     for (int v = 0; v < C::NW; ++v) m = fmaxf(m, red_m[v * 32 + ri]);
-    if (rr / a.G >= sq.nq) m = NEG_INF;
     f32x4 o = {};
-    if (m > NEG_INF) {
 #pragma unroll
-      for (int v = 0; v < C::NW; ++v) {
-        const float f = fast_exp2(red_m[v * 32 + ri] - m);
-        lt = fmaf(red_l[v * 32 + ri], f, lt);
-        o += f * *(const f32x4*)(red + (v * 32 + ri) * C::OP + d);
-      }
+    for (int v = 0; v < C::NW; ++v) {                 // a wave without keys: zeros (or a NaN)
+      const float f = red_m[v * 32 + ri] == NEG_INF ? 1.0f : fast_exp2(red_m[v * 32 + ri] - m);
+      lt = fmaf(red_l[v * 32 + ri], f, lt);
+      o += f * *(const f32x4*)(red + (v * 32 + ri) * C::OP + d);
+    }
+    if (rr / a.G >= sq.nq) {
+      m = NEG_INF;
+      lt = 0.0f;
+      o = f32x4{};
     }
     if (a.nsplit > 1) {
       const int64_t p = ((int64_t)slice * a.B * a.Hkv + (int64_t)b * a.Hkv + kvh) * rows + rr;
@@ -244,12 +246,12 @@ __global__ __launch_bounds__(256, 1) void win_token_kernel(WinArgs a) {
       continue;
     }
     const int i = rr / a.G, hq = kvh * a.G + rr % a.G;
-    const float inv = lt > 0.0f ? 1.0f / lt : 0.0f;   // a row that sees nothing: 0
+    const float inv = lt != 0.0f ? 1.0f / lt : 0.0f;  // a row that sees nothing: 0
     bf16x4 x;
 #pragma unroll
     for (int k = 0; k < 4; ++k) x[k] = (bf16)(o[k] * inv);
     *(bf16x4*)((bf16*)a.o + (int64_t)b * a.o_sb + (int64_t)i * a.o_st + (int64_t)hq * a.o_sh + d) = x;
-    if (d == 0) a.lse[((int64_t)b * a.Hq + hq) * a.lse_ld + i] = lt > 0.0f ? (m + log2f(lt)) * LN2 : NEG_INF;
+    if (d == 0) a.lse[((int64_t)b * a.Hq + hq) * a.lse_ld + i] = lt != 0.0f ? (m + log2f(lt)) * LN2 : NEG_INF;
   }
 }
 

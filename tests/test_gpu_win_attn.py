@@ -34,7 +34,7 @@ def like(t):
     return buf.as_strided(t.shape, t.stride()), buf
 
 
-def run(q, k, v, do, q_lens=None, kv_lens=None, **kw):
+def run(q, k, v, do, q_lens=None, kv_lens=None, gaps=True, **kw):
     o = torch.full(q.shape, math.nan, dtype=q.dtype, device="cuda")
     lse = torch.full((q.shape[0], q.shape[2], q.shape[1]), math.nan, device="cuda")
     cfg = bpt.attn_config_of(q, k, v, o, **kw)
@@ -50,7 +50,7 @@ def run(q, k, v, do, q_lens=None, kv_lens=None, **kw):
         bpt.attn_bwd(cfg, q, k, v, o, lse, do, dq, dk, dv, ws, ql, kl)
         out.update(dQ=dq, dK=dk, dV=dv)
         for t, buf in ((dq, bq), (dk, bk), (dv, bv)):      # nothing between the rows is written
-            assert int(torch.isnan(buf.float()).sum()) == buf.numel() - t.numel()
+            assert not gaps or int(torch.isnan(buf.float()).sum()) == buf.numel() - t.numel()
     torch.cuda.synchronize()
     return out
 
@@ -202,6 +202,29 @@ def test_large_scores():
             ref, err = attention(*args, **kw)
             for n in ("O", "lse"):
                 check(got[n], ref[n], err[n], f"{n} {s} {dt}")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("Sq,L", [(300, 300), (1, 3000)])
+def test_a_nan_stays_one_where_it_belongs(Sq, L, dtype):
+    """A NaN in a query's row gives that row's O, lse and dQ; one in a key gives those of the queries that see it."""
+    q, k, v, do = make(1, Sq, L, 4, 2, 64, dtype, seed=8)
+    kw = dict(causal=True, window=50 if Sq > 1 else 0)
+    clean = run(q, k, v, do, **kw)
+    q2 = q.clone()
+    q2[0, Sq - 1, 1, 5] = math.nan
+    got = run(q2, k, v, do, gaps=False, **kw)
+    bad = torch.zeros(1, Sq, 4, dtype=torch.bool, device="cuda")
+    bad[0, Sq - 1, 1] = True
+    for n in ("O", "dQ"):
+        assert torch.equal(torch.isnan(got[n]).all(dim=3), bad) and torch.equal(torch.isnan(got[n]).any(dim=3), bad), n
+    assert torch.equal(torch.isnan(got["lse"]), bad.permute(0, 2, 1))
+    assert torch.equal(got["O"][~bad], clean["O"][~bad])
+    k2 = k.clone()
+    k2[0, L - 1, 0, 3] = math.nan                    # seen by the last query's heads 0 and 1 alone
+    got = run(q, k2, v, None, **kw)
+    assert bool(torch.isnan(got["O"][0, Sq - 1, :2]).all()) and bool(torch.isfinite(got["O"][0, Sq - 1, 2:].float()).all())
+    assert torch.equal(got["O"][0, :Sq - 1], clean["O"][0, :Sq - 1])
 
 
 def test_gradients_against_differences():

@@ -158,7 +158,7 @@ def adam(cfg=None, tensors=None, count=None):
 
 
 @pytest.mark.parametrize("kw", [
-    dict(step=0), dict(beta1=1.0), dict(beta2=-0.1), dict(beta1=math.nan), dict(eps=0.0), dict(eps=1e-60), dict(eps=math.inf),
+    dict(step=0), dict(beta1=1.0), dict(beta2=-0.1), dict(beta1=math.nan), dict(eps=0.0), dict(eps=1e-60), dict(eps=1e-40), dict(eps=math.inf),
     dict(lr=-1.0), dict(lr=math.inf), dict(lr=math.nan), dict(state_bits=16), dict(reserved=1), dict(grad_dtype=2), dict(lowp_dtype=-1),
 ])
 def test_adamw_refuses_configs(kw):
@@ -203,6 +203,24 @@ def test_adamw_tensors_refuses():
         bpt.AdamWTensors([good], bits=16)
     with pytest.raises(ValueError):
         bpt.AdamWTensors([good, dict(good, g=p.bfloat16())])
+    with pytest.raises(ValueError):
+        bpt.adamw_multi(bpt.AdamWTensors([good]), 1, 1e-3)              # on the CPU
+    with pytest.raises(ValueError):
+        bpt.AdamWTensors([dict(good, m=torch.zeros(300, device="meta"))])
+
+
+def test_lengths_and_positions_are_int32_on_the_gpu():
+    c, q = attn(), torch.empty(2, 10, 4, 64, dtype=torch.bfloat16)
+    lse = torch.empty(2, 4, 10)
+    for bad in (torch.zeros(2, dtype=torch.int64), torch.zeros(2, dtype=torch.int32), torch.zeros(3, dtype=torch.int32)):
+        with pytest.raises(ValueError):
+            bpt.attn_fwd(c, q, q, q, q, lse, None, bad)
+        with pytest.raises(ValueError):
+            bpt.attn_fwd(c, q, q, q, q, lse, None, None, bad)
+        with pytest.raises(ValueError):
+            bpt.rope_fwd(rope(), q, q, bad)
+    with pytest.raises(ValueError):
+        bpt.WindowAttention().forward(q, q, q)
 
 
 # ---------------------------------------------------------------- a layer's options
