@@ -27,7 +27,10 @@ struct Vis {
   BPT_DEV bool any() const { return hi >= lo || se > 0; }
   // a key that is seen, in place of one that is not: what a tile holds beyond the visible keys is
   // never read, whatever it contains
-  BPT_DEV int clamp(int k) const { return k < se ? k : min(max(k, lo), hi); }
+  BPT_DEV int clamp(int k) const {
+    const int in = min(max(k, lo), hi);
+    return k < se ? k : in;
+  }
 };
 // Keys of the queries at positions p0 .. p1. Where nothing but sinks is left, lo = hi = se - 1.
 BPT_DEV Vis vis_of(const WinArgs& a, const Seq& s, int p0, int p1) {

@@ -167,12 +167,12 @@ __global__ __launch_bounds__(256, 1) void win_token_kernel(WinArgs a) {
     char* mine = smem + wave * 2 * C::STAGE;
     auto issue = [&](int j, int at) {
       const int k0 = tiles.key0(j);
-      const int lo = max(w.run.lo, k0), hi = min(w.run.hi, k0 + 31), se = min(w.run.se, k0 + 32);
+      const Vis seen = seen_in(w.run, k0, 32);
       const bf16 *ko = Kb + (int64_t)k0 * a.k_st, *vo = Vb + (int64_t)k0 * a.v_st;
 #pragma unroll
       for (int i = 0; i < C::BL; ++i) {
         const int slot = 64 * i + lane, col = slot % C::SLOTS, k = k0 + slot / C::SLOTS;
-        const int row = (k < se ? k : lo <= hi ? min(max(k, lo), hi) : se - 1) - k0, c8 = (col < DH / 8 ? col : 0) * 8;
+        const int row = seen.clamp(k) - k0, c8 = (col < DH / 8 ? col : 0) * 8;
         dma16s(scalar_ptr(ko), 2u * (uint32_t)(row * a.k_st + c8), mine + at * C::STAGE + i * 1024);
         dma16s(scalar_ptr(vo), 2u * (uint32_t)(row * a.v_st + c8), mine + at * C::STAGE + C::TB + i * 1024);
       }

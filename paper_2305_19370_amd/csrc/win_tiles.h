@@ -124,6 +124,13 @@ BPT_DEV void issue_picked(char* stage, const bf16* src0, int ld0, const bf16* sr
   }
 }
 
+// What of v lies in a tile of n keys from k0, of which v sees some: clamp() of it stays in the tile.
+BPT_DEV Vis seen_in(const Vis& v, int k0, int n) {
+  Vis t{max(v.lo, k0), min(v.hi, k0 + n - 1), min(v.se, k0 + n)};
+  if (t.lo > t.hi) t.lo = t.hi = t.se - 1;            // sinks alone
+  return t;
+}
+
 // K and V of keys k0 .. k0 + 63, a tile that holds a key which v's run of rows sees; a key that none of
 // them sees is replaced by one of the tile that is.
 template <int DH, int NW>
@@ -133,10 +140,8 @@ BPT_DEV void issue_keys(char* stage, const bf16* K, int ldk, const bf16* V, int 
     ring_issue_full<DH, NW>(stage, K, ldk, k0, V, ldv, k0, roff, wave);
     return;
   }
-  const int lo = max(v.lo, k0), hi = min(v.hi, k0 + 63);
-  const int se = min(v.se, k0 + 64);
-  issue_picked<DH, NW>(stage, K, ldk, V, ldv, k0, wave, lane,
-                       [&](int k) { return k < se ? k : lo <= hi ? min(max(k, lo), hi) : se - 1; });
+  const Vis t = seen_in(v, k0, 64);
+  issue_picked<DH, NW>(stage, K, ldk, V, ldv, k0, wave, lane, [&](int k) { return t.clamp(k); });
 }
 
 // The online softmax of the row on a lane (shared with lane ^ 32): reference in base 2 (-inf until the row has seen a key) and
