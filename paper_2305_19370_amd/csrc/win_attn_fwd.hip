@@ -66,7 +66,7 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 1 : 2) void win_fwd_bf16_kernel(
             acc[d] = mfma32x32x16(frag_tr<DH>(vt, 32 * mt + 16 * hf, 32 * d, lane), pb, acc[d]);
         }
     };
-    auto edge = [&](int j) {                          // a tile that not every row sees in full, or has no reference for
+    auto tile = [&](int j) {
       const int k0 = tiles.key0(j);
       if (w.none(k0)) return;
       f32x16 t[2];
@@ -75,33 +75,7 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 1 : 2) void win_fwd_bf16_kernel(
       sm.weights(t, acc);
       add_values(j, t);
     };
-    auto inner = [&](int j) {                         // weights against the reference as it stands
-      f32x16 t[2];
-      scores(j, t);
-      const float rs = sm.raw(t, sm.ref);
-      if (sm.over(rs)) {                              // rare: a score far above the reference
-        scores(j, t);
-        sm.weights(t, acc);
-      } else {
-        sm.sum += rs;
-      }
-      add_values(j, t);
-    };
-    auto step = [&](int j) { ring_step<C, C::DPS>(j, tiles.n, issue); };
-    int ja, jb, j = 0;
-    w.full_tiles(tiles, ja, jb);
-    for (; j < min(ja + 1, tiles.n); ++j) {           // the first full tile gives every row a reference
-      step(j);
-      edge(j);
-    }
-    for (; j < jb; ++j) {
-      step(j);
-      inner(j);
-    }
-    for (; j < tiles.n; ++j) {
-      step(j);
-      edge(j);
-    }
+    ring_loop<C, C::DPS>(tiles.n, issue, tile);
     ref = sm.ref;
     l_run = sm.sum;
   }

@@ -56,7 +56,6 @@ struct Rows {
   int i, head;                 // token, query head in its group
   bool exists;
   Vis mine, first, last, run;  // the row; the wave's first and last row; the workgroup
-  int f_lo, f_hi;              // keys that all rows of the workgroup see
   BPT_DEV Rows(const WinArgs& a, const Seq& s, int r0, int w0, int n, int lane) {
     const int r = r0 + w0 + (lane & 31);
     i = r / a.G;
@@ -65,26 +64,18 @@ struct Rows {
     exists = i <= end;
     const int i0 = r0 / a.G, i1 = (r0 + n - 1) / a.G;
     mine = first = last = run = Vis{0, -1, 0};
-    f_lo = 0, f_hi = -1;
     if (i0 > end) return;      // the workgroup has no row
     auto at = [&](int t) { const int p = s.off + min(t, end); return vis_of(a, s, p, p); };
     mine = at(i);
     first = at((r0 + w0) / a.G);
     last = at((r0 + w0 + 31) / a.G);
     run = vis_run(a, s, s.off + i0, s.off + min(i1, end));
-    f_lo = at(i1).lo;
-    f_hi = at(i0).hi;
   }
   // the token whose row is read
   BPT_DEV int safe(const Seq& s) const { return min(i, s.nq - 1); }
   // whether all the wave's rows see all of keys k0 .. k0 + 63, or none sees any
   BPT_DEV bool all(int k0) const { return (k0 >= last.lo && k0 + 63 <= first.hi) || k0 + 63 < first.se; }
   BPT_DEV bool none(int k0) const { return !(k0 <= last.hi && k0 + 63 >= first.lo) && k0 >= last.se; }
-  // the tiles ja <= j < jb of the list (behind those of the sinks) that all rows of the workgroup see in full
-  BPT_DEV void full_tiles(const Tiles<64>& t, int& ja, int& jb) const {
-    ja = max((f_lo + 63) / 64 - t.first, 0) + t.ns;
-    jb = max(min(max(f_hi + 1, 0) / 64 - t.first + t.ns, t.n), ja);
-  }
   // `out` in place of the scores t[mt][r] of keys k0 + 32 mt + acc_row(r, lane) that the row does not see. One comparison per
   // score where the tile lies across one end of the window only.
   template <int N>
@@ -153,8 +144,6 @@ struct OnlineRows {
   static constexpr float GROWTH = 8.0f;
   float c;                                           // scale log2(e)
   float ref = NEG_INF, sum = 0.0f;
-  // whether a lane's sum of weights against the present references is too large
-  BPT_DEV static bool over(float rs) { return __ballot(!(rs <= 65536.0f)) != 0; }
   // products t become weights against m; the lane's sum
   template <int N>
   BPT_DEV float raw(f32x16 (&t)[N], float m) const {
