@@ -9,8 +9,11 @@ namespace bpt {
 // S^T = K Q^T, dP^T = V dO^T, dS^T = P^T (dP^T - Delta), dQ^T += K^T dS^T; P from the saved
 // log-sum-exp. Rows and ring as in the forward.
 template <int DH, int NW>
+using WinDqCfg = WinCfg<DH, NW, NW == 8 || DH == 64 ? 4 : 2>;
+
+template <int DH, int NW>
 __global__ __launch_bounds__(64 * NW, NW == 8 ? 1 : 2) void win_dq_bf16_kernel(WinArgs a) {
-  using C = WinCfg<DH, NW>;
+  using C = WinDqCfg<DH, NW>;
   extern __shared__ __attribute__((aligned(16))) char smem[];
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -322,7 +325,7 @@ static hipError_t far(const WinArgs& a, hipStream_t s) {
 }
 template <int DH, int NW>
 static hipError_t launch_dq(const WinArgs& a, hipStream_t s) {
-  using C = WinCfg<DH, NW>;
+  using C = WinDqCfg<DH, NW>;
   auto k = win_dq_bf16_kernel<DH, NW>;
   hipError_t e = set_lds(k, C::LDS);
   if (e != hipSuccess) return e;

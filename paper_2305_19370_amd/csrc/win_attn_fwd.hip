@@ -7,9 +7,13 @@ namespace bpt {
 // r = token * G + head, so its maximum and sum are register reductions and one exchange), P^T straight from the accumulators into
 // O^T += V^T P^T. NW waves of 32 rows share the K and V tiles of an LDS ring. The scores are scaled
 // in fp32 (the FMA that subtracts the reference), so q is used as it is.
+// Two stages for 4 waves: heads of 64 then have three workgroups on a CU (16384 tokens, window 2048: 211 -> 190 us).
+template <int DH, int NW>
+using WinFwdCfg = WinCfg<DH, NW, NW == 8 ? 4 : 2>;
+
 template <int DH, int NW>
 __global__ __launch_bounds__(64 * NW, NW == 8 ? 1 : 2) void win_fwd_bf16_kernel(WinArgs a) {
-  using C = WinCfg<DH, NW>;
+  using C = WinFwdCfg<DH, NW>;
   extern __shared__ __attribute__((aligned(16))) char smem[];
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -231,7 +235,7 @@ __global__ __launch_bounds__(256, 1) void win_token_kernel(WinArgs a) {
 
 template <int DH, int NW>
 static hipError_t launch_fwd(const WinArgs& a, hipStream_t s) {
-  using C = WinCfg<DH, NW>;
+  using C = WinFwdCfg<DH, NW>;
   auto k = win_fwd_bf16_kernel<DH, NW>;
   hipError_t e = set_lds(k, C::LDS);
   if (e != hipSuccess) return e;

@@ -18,13 +18,13 @@ template <int N = 0> BPT_DEV void wait_lgkm() { asm volatile("s_waitcnt lgkmcnt(
 // hold their fragments in registers meanwhile.
 BPT_DEV void pin(f32x16& x) { asm volatile("" : "+v"(x)); }
 
-// NW waves of 32 rows share tiles of 64 rows of two tensors in a ring
-template <int DH, int NWAVES>
+// NW waves of 32 rows share tiles of 64 rows of two tensors in a ring of NS stages
+template <int DH, int NWAVES, int NSTAGES>
 struct WinCfg {
   static constexpr int KSTEPS = DH / 16, DT = DH / 32;
   static constexpr int NW = NWAVES, ROWS = 32 * NW;
   static constexpr int TB = RmTile<DH>::BYTES, STAGE = 2 * TB;
-  static constexpr int NS = NW == 8 || DH == 64 ? 4 : 2;   // stages in the ring
+  static constexpr int NS = NSTAGES;
   static constexpr int LDS = NS * STAGE;
   static constexpr int DPS = Ring2<DH, NW>::DPW;    // copies per wave per stage
 };
