@@ -153,14 +153,12 @@ hipError_t win_fwd_bf16(const WinArgs& a, hipStream_t s);
 hipError_t win_fwd_f32(const WinArgs& a, hipStream_t s);
 hipError_t win_join(Dt t, const WinArgs& a, hipStream_t s);    // joins the slices of a forward
 hipError_t win_delta(Dt t, const WinArgs& a, hipStream_t s);   // ndelta, nlse
-hipError_t win_dkdv_bf16(const WinArgs& a, hipStream_t s);
-hipError_t win_dkdv_f32(const WinArgs& a, hipStream_t s);
+hipError_t win_bwd_bf16(const WinArgs& a, hipStream_t s);      // dQ; dK and dV; either may be NULL
+hipError_t win_bwd_f32(const WinArgs& a, hipStream_t s);
 hipError_t win_far_bf16(const WinArgs& a, hipStream_t s);      // 2 far slots
 hipError_t win_far_f32(const WinArgs& a, hipStream_t s);       // far slots
 hipError_t win_chunks(Dt t, const WinArgs& a, hipStream_t s);  // adds the chunks up
 hipError_t win_sinks(Dt t, const WinArgs& a, int slots, hipStream_t s);   // adds the slots up
-hipError_t win_dq_bf16(const WinArgs& a, hipStream_t s);
-hipError_t win_dq_f32(const WinArgs& a, hipStream_t s);
 
 // ---------------------------------------------------------------- rotary positions
 struct RopeArgs {

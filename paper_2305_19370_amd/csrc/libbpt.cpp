@@ -1147,13 +1147,12 @@ static bpt_status layer_bwd(const bpt_config* cfg, const bpt_layer_options* opt,
     a.far = cut.far;
     const double seen = attn_seen(ac);
     RUN("win.delta", 0, 2.0 * T * D * E_, win_delta(E, a, s));
-    RUN("win.dkdv", 8.0 * d.dh * seen, 6.0 * T * D * E_, E == BF16 ? win_dkdv_bf16(a, s) : win_dkdv_f32(a, s));
+    RUN("win.bwd", 14.0 * d.dh * seen, 7.0 * T * D * E_, E == BF16 ? win_bwd_bf16(a, s) : win_bwd_f32(a, s));
     if (a.chunks > 1) RUN("win.chunks", 0, (double)cut.bytes + 2.0 * T * D * E_, win_chunks(E, a, s));
     if (a.far > 0) {
       RUN("win.far", 8.0 * d.dh * T * d.H * sinks, 2.0 * T * D * E_, E == BF16 ? win_far_bf16(a, s) : win_far_f32(a, s));
       RUN("win.sinks", 0, (double)attn_slots(ac, a.far) * B * d.H * sinks * d.dh * 8, win_sinks(E, a, attn_slots(ac, a.far), s));
     }
-    RUN("win.dq", 6.0 * d.dh * seen, 5.0 * T * D * E_, E == BF16 ? win_dq_bf16(a, s) : win_dq_f32(a, s));
     if (opt->rot)
       RUN("rope.bwd", 6.0 * T * d.H * opt->rot, 4.0 * T * d.H * opt->rot * E_,
           rope(E, rope_args(rc, nullptr, w.dqkvT, 3 * D, w.dqkvT, 3 * D, -1.0f), s));
@@ -1636,7 +1635,8 @@ bpt_status bpt_attn_bwd(const bpt_attn_config* cfg, const void* Q, const void* K
   const bool bf = cfg->dtype == BPT_BF16;
   const double E_ = bf ? 2 : 4, seen = attn_seen(*cfg), q = (double)cfg->B * cfg->Hq * cfg->Sq * cfg->dh, kv = (double)cfg->B * cfg->Hkv * cfg->Skv * cfg->dh;
   RUN("win.delta", 0, 2.0 * q * E_, win_delta(dt_of(cfg->dtype), a, s));
-  if (dK) RUN("win.dkdv", 8.0 * cfg->dh * seen, (2.0 * q + 4.0 * kv) * E_, bf ? win_dkdv_bf16(a, s) : win_dkdv_f32(a, s));
+  RUN("win.bwd", ((dK ? 8.0 : 0) + (dQ ? 6.0 : 0)) * cfg->dh * seen,
+      (2.0 * q + 2.0 * kv + (dQ ? q : 0) + (dK ? 2.0 * kv : 0)) * E_, bf ? win_bwd_bf16(a, s) : win_bwd_f32(a, s));
   if (dK && a.chunks > 1)
     RUN("win.chunks", 0, (double)cut.bytes + 2.0 * kv * E_, win_chunks(dt_of(cfg->dtype), a, s));
   if (dK && a.far > 0) {
@@ -1644,7 +1644,6 @@ bpt_status bpt_attn_bwd(const bpt_attn_config* cfg, const void* Q, const void* K
     RUN("win.sinks", 0, (double)attn_slots(*cfg, a.far) * cfg->B * cfg->Hkv * std::min(cfg->sinks, cfg->Skv) * cfg->dh * 8,
         win_sinks(dt_of(cfg->dtype), a, attn_slots(*cfg, a.far), s));
   }
-  if (dQ) RUN("win.dq", 6.0 * cfg->dh * seen, (3.0 * q + 2.0 * kv) * E_, bf ? win_dq_bf16(a, s) : win_dq_f32(a, s));
   return BPT_OK;
 }
 

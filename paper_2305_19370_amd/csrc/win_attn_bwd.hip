@@ -9,17 +9,16 @@ namespace bpt {
 // S^T = K Q^T, dP^T = V dO^T, dS^T = P^T (dP^T - Delta), dQ^T += K^T dS^T; P from the saved
 // log-sum-exp. Rows and ring as in the forward.
 template <int DH, int NW>
-using WinDqCfg = WinCfg<DH, NW, NW == 8 || DH == 64 ? 4 : 2>;
+using WinDqCfg = WinCfg<DH, NW, NW == 8 ? 4 : 2>;
 
 template <int DH, int NW>
-__global__ __launch_bounds__(64 * NW, NW == 8 ? 1 : 2) void win_dq_bf16_kernel(WinArgs a) {
+BPT_DEV void dq_rows(const WinArgs& a, char* smem, int id) {
   using C = WinDqCfg<DH, NW>;
-  extern __shared__ __attribute__((aligned(16))) char smem[];
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int nblk = (a.Sq * a.G + C::ROWS - 1) / C::ROWS;
   int hh, blk;
-  xcd_map((int)blockIdx.x, a.Hkv * a.B, hh, blk);
+  xcd_map(id, a.Hkv * a.B, hh, blk);
   const int kvh = hh % a.Hkv, b = hh / a.Hkv;
   const Seq sq = seq_of(a, b);
   const Rows w(a, sq, (nblk - 1 - blk) * C::ROWS, 32 * wave, C::ROWS, lane);   // most keys first
@@ -120,15 +119,15 @@ struct WinKvCfg {
 // two waves, each half the queries of a tile). All leave the sinks' sums in fp32 slots, which win_sinks adds in order.
 // Few blocks of keys with many tiles (grouped heads, small batches) are cut into a.chunks of those in the same way, for all keys.
 template <int DH, int KG, int QH, bool FAR>
-__global__ __launch_bounds__(64 * KG * QH, KG * QH == 8 ? 1 : 2) void win_dkdv_bf16_kernel(WinArgs a) {
+BPT_DEV void dkdv_keys(const WinArgs& a, char* smem, int id) {
   using C = WinKvCfg<DH, KG, QH>;
   constexpr int NW = C::NW;
   static_assert(!FAR || (KG == 1 && QH == 2), "two waves for the far part");
-  extern __shared__ __attribute__((aligned(16))) char smem[];
+  static_assert(FAR || QH == 1 || KG * 2 * C::DT * 4096 <= C::LDS, "the second halves fit the ring");
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   int hh, blk;
-  xcd_map((int)blockIdx.x, a.Hkv * a.B, hh, blk);
+  xcd_map(id, a.Hkv * a.B, hh, blk);
   const int kvh = hh % a.Hkv, b = hh / a.Hkv;
   const Seq sq = seq_of(a, b);
   const int chunks = FAR ? a.far : a.chunks, chunk = blk % chunks;
@@ -298,48 +297,64 @@ __global__ __launch_bounds__(64 * KG * QH, KG * QH == 8 ? 1 : 2) void win_dkdv_b
   }
 }
 
+template <int DH, int NW>
+__global__ __launch_bounds__(64 * NW, 1) void win_dq_bf16_kernel(WinArgs a) {
+  extern __shared__ __attribute__((aligned(16))) char smem[];
+  dq_rows<DH, NW>(a, smem, (int)blockIdx.x);
+}
 template <int DH, int KG, int QH, bool FAR>
-static hipError_t launch_dkdv(const WinArgs& a, int64_t blocks, hipStream_t s) {
-  using C = WinKvCfg<DH, KG, QH>;
-  static_assert(FAR || QH == 1 || KG * 2 * C::DT * 4096 <= C::LDS, "the second halves fit the ring");
-  auto k = win_dkdv_bf16_kernel<DH, KG, QH, FAR>;
-  hipError_t e = set_lds(k, C::LDS);
+__global__ __launch_bounds__(64 * KG * QH, KG * QH == 8 ? 1 : 2) void win_dkdv_bf16_kernel(WinArgs a) {
+  extern __shared__ __attribute__((aligned(16))) char smem[];
+  dkdv_keys<DH, KG, QH, FAR>(a, smem, (int)blockIdx.x);
+}
+// dK dV in blocks of 64 keys, by the first nkv workgroups, and dQ in blocks of 128 rows by the others: neither needs the
+// other, and short runs leave a chip that one of them alone does not fill (4 x 1000 tokens, 12 heads of 64, window 256: 39
+// us, in two launches 50). Heads of 64: three workgroups on a CU, at two stages for dQ and 24 bytes of spills a
+// lane (16384 tokens, 16 heads, window 2048: 590 us, two workgroups 645).
+template <int DH>
+__global__ __launch_bounds__(256, DH == 64 ? 3 : 2) void win_bwd_bf16_kernel(WinArgs a, int nkv) {
+  extern __shared__ __attribute__((aligned(16))) char smem[];
+  const int id = (int)blockIdx.x;
+  if (id < nkv) dkdv_keys<DH, 2, 2, false>(a, smem, id);
+  else dq_rows<DH, 4>(a, smem, id - nkv);
+}
+
+template <class K>
+static hipError_t launch(K k, int64_t blocks, int threads, int lds, const WinArgs& a, hipStream_t s) {
+  hipError_t e = set_lds(k, lds);
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(k, dim3((unsigned)(blocks * a.Hkv * a.B)), dim3(64 * C::NW), C::LDS, s, a);
+  hipLaunchKernelGGL(k, dim3((unsigned)blocks), dim3(threads), lds, s, a);
   return hipGetLastError();
 }
 template <int DH>
-static hipError_t dkdv(const WinArgs& a, hipStream_t s) {
-  // Long runs of tiles that fill the chip twice over: blocks of 256 keys (full attention of 32768 tokens, 32 heads of 128: 16.1
-  // ms, blocks of 64 17.7). Else of 64, two to three workgroups on a CU, one at its start or end while others work: 4000
-  // tokens, 16 heads, window 512 66 us (74); 4 x 1000 tokens, 12 heads of 64, window 256 25 (29); heads of 64 at any length: 16384
-  // tokens, window 2048 289 (331), full attention of 32768 tokens, 16 heads 4.24 ms (4.37).
-  const int64_t wide = ((int64_t)a.Skv + 255) / 256;
+static hipError_t bwd(const WinArgs& a, hipStream_t s) {
+  // dK dV: long runs of tiles that fill the chip twice over in blocks of 256 keys (full attention of 32768 tokens, 32 heads of 128:
+  // 16.1 ms, blocks of 64 17.7). Else of 64, two to three workgroups on a CU, one at its start or end while others work: 4000
+  // tokens, 16 heads, window 512 66 us (74); heads of 64 at any length: 16384 tokens, window 2048 289 (331), full attention of
+  // 32768 tokens, 16 heads 4.24 ms (4.37).
+  const int64_t heads = (int64_t)a.Hkv * a.B, wide = ((int64_t)a.Skv + 255) / 256 * heads;
+  const bool wide_kv = DH == 128 && !a.window && wide >= 512, wide_q = win_wide(a.Sq, a);
+  hipError_t e = hipSuccess;
   if constexpr (DH == 128)
-    if (!a.window && wide * a.Hkv * a.B >= 512) return launch_dkdv<DH, 8, 1, false>(a, wide, s);
-  return launch_dkdv<DH, 2, 2, false>(a, ((int64_t)a.Skv + 63) / 64 * a.chunks, s);
+    if (a.dk && wide_kv) e = launch(win_dkdv_bf16_kernel<DH, 8, 1, false>, wide, 512, WinKvCfg<DH, 8, 1>::LDS, a, s);
+  if (e == hipSuccess && a.dq && wide_q)
+    e = launch(win_dq_bf16_kernel<DH, 8>, ((int64_t)a.Sq * a.G + 255) / 256 * heads, 512, WinDqCfg<DH, 8>::LDS, a, s);
+  const int64_t nkv = a.dk && !wide_kv ? ((int64_t)a.Skv + 63) / 64 * a.chunks * heads : 0;
+  const int64_t nq = a.dq && !wide_q ? ((int64_t)a.Sq * a.G + 127) / 128 * heads : 0;
+  if (e != hipSuccess || nkv + nq == 0) return e;
+  auto k = win_bwd_bf16_kernel<DH>;
+  constexpr int lds = std::max(WinKvCfg<DH, 2, 2>::LDS, WinDqCfg<DH, 4>::LDS);
+  if ((e = set_lds(k, lds)) != hipSuccess) return e;
+  hipLaunchKernelGGL(k, dim3((unsigned)(nkv + nq)), dim3(256), lds, s, a, (int)nkv);
+  return hipGetLastError();
 }
 template <int DH>
 static hipError_t far(const WinArgs& a, hipStream_t s) {
-  return launch_dkdv<DH, 1, 2, true>(a, (int64_t)a.far * ((std::min(a.sinks, a.Skv) + 31) / 32), s);
-}
-template <int DH, int NW>
-static hipError_t launch_dq(const WinArgs& a, hipStream_t s) {
-  using C = WinDqCfg<DH, NW>;
-  auto k = win_dq_bf16_kernel<DH, NW>;
-  hipError_t e = set_lds(k, C::LDS);
-  if (e != hipSuccess) return e;
-  const int64_t nblk = ((int64_t)a.Sq * a.G + C::ROWS - 1) / C::ROWS;
-  hipLaunchKernelGGL(k, dim3((unsigned)(nblk * a.Hkv * a.B)), dim3(64 * NW), C::LDS, s, a);
-  return hipGetLastError();
+  return launch(win_dkdv_bf16_kernel<DH, 1, 2, true>, (int64_t)a.far * ((std::min(a.sinks, a.Skv) + 31) / 32) * a.Hkv * a.B, 128,
+                WinKvCfg<DH, 1, 2>::LDS, a, s);
 }
 
-hipError_t win_dkdv_bf16(const WinArgs& a, hipStream_t s) { return a.dh == 64 ? dkdv<64>(a, s) : dkdv<128>(a, s); }
+hipError_t win_bwd_bf16(const WinArgs& a, hipStream_t s) { return a.dh == 64 ? bwd<64>(a, s) : bwd<128>(a, s); }
 hipError_t win_far_bf16(const WinArgs& a, hipStream_t s) { return a.dh == 64 ? far<64>(a, s) : far<128>(a, s); }
-template <int DH>
-static hipError_t dq(const WinArgs& a, hipStream_t s) {
-  return win_wide(a.Sq, a) ? launch_dq<DH, 8>(a, s) : launch_dq<DH, 4>(a, s);
-}
-hipError_t win_dq_bf16(const WinArgs& a, hipStream_t s) { return a.dh == 64 ? dq<64>(a, s) : dq<128>(a, s); }
 
 }  // namespace bpt

@@ -243,14 +243,35 @@ __global__ __launch_bounds__(256) void win_delta_kernel(WinArgs a) {
   }
 }
 
-// dQ: 16 rows as in the forward, wave w takes the key tiles of 16 w, w + 4, ...; dS^T has the row on the
+// Sums of 8 waves' 16 x DH results (rows on lanes), in LDS: red[0 .. 3] are left to be added
+template <int DH>
+BPT_DEV void add_eight(float (&red)[4][16][DH + 4], const f32x4 (&x)[DH / 16], int wave, int g, int c16) {
+  __syncthreads();
+  if (wave >= 4)
+#pragma unroll
+    for (int t = 0; t < DH / 16; ++t) *(f32x4*)&red[wave - 4][c16][16 * t + 4 * g] = x[t];
+  __syncthreads();
+  if (wave < 4)
+#pragma unroll
+    for (int t = 0; t < DH / 16; ++t) {
+      f32x4* at = (f32x4*)&red[wave][c16][16 * t + 4 * g];
+      *at = x[t] + *at;
+    }
+  __syncthreads();
+}
+template <int DH>
+BPT_DEV f32x4 add_four(const float (&red)[4][16][DH + 4], int row, int d) {
+  return ((*(const f32x4*)&red[0][row][d] + *(const f32x4*)&red[1][row][d]) + *(const f32x4*)&red[2][row][d]) +
+         *(const f32x4*)&red[3][row][d];
+}
+
+// dQ: 16 rows as in the forward, each of 8 waves takes every eighth key tile of 16; dS^T has the row on the
 // lane axis and is the B operand of dQ^T += K^T dS^T.
 template <int DH>
-__global__ __launch_bounds__(256) void win_dq_f32_kernel(WinArgs a) {
+BPT_DEV void dq_f32(const WinArgs& a, float (&red)[4][16][DH + 4], int blk) {
   constexpr int NC = DH / 16;
-  __shared__ __attribute__((aligned(16))) float red[4][16][DH + 4];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, g = lane >> 4, c16 = lane & 15;
-  const int rows = a.Sq * a.G, r0 = (int)(gridDim.x - 1 - blockIdx.x) * 16;
+  const int rows = a.Sq * a.G, r0 = blk * 16;
   const int kvh = blockIdx.y, b = blockIdx.z;
   const Seq sq = seq_of(a, b);
   const int i0 = r0 / a.G, i1 = min((r0 + 15) / a.G, sq.nq - 1);
@@ -271,7 +292,7 @@ __global__ __launch_bounds__(256) void win_dq_f32_kernel(WinArgs a) {
     const RowFrag<DH> of = row_frag<DH>((const float*)a.dout + (int64_t)b * a.o_sb + (int64_t)qi * a.o_st + (int64_t)h * a.o_sh, g);
     const int64_t sidx = ((int64_t)b * a.Hq + h) * a.Sqp + qi;
     const float nl = a.nlse[sidx], ndl = a.ndelta[sidx];
-    for (int j = wave; j < tiles.n; j += 4) {
+    for (int j = wave; j < tiles.n; j += 8) {
       const int k0 = tiles.key0(j);
       const int64_t kr = run.clamp(k0 + c16);
       const RowFrag<DH> kf = row_frag<DH>(Kb + kr * a.k_st, g), vf = row_frag<DH>(Vb + kr * a.v_st, g);
@@ -284,14 +305,11 @@ __global__ __launch_bounds__(256) void win_dq_f32_kernel(WinArgs a) {
       add_outer<DH>(dq, kc, ds);
     }
   }
-#pragma unroll
-  for (int t = 0; t < NC; ++t) *(f32x4*)&red[wave][c16][16 * t + 4 * g] = dq[t];
-  __syncthreads();
-  for (int e = tid; e < 16 * (DH / 4); e += 256) {
+  add_eight<DH>(red, dq, wave, g, c16);
+  for (int e = tid; e < 16 * (DH / 4); e += 512) {
     const int ri = e / (DH / 4), d = 4 * (e % (DH / 4)), rr = r0 + ri;
     if (rr >= rows) continue;
-    const f32x4 x = ((*(const f32x4*)&red[0][ri][d] + *(const f32x4*)&red[1][ri][d]) + *(const f32x4*)&red[2][ri][d]) +
-                    *(const f32x4*)&red[3][ri][d];
+    const f32x4 x = add_four<DH>(red, ri, d);
     const int ii = rr / a.G, hh = kvh * a.G + rr % a.G;
     *(f32x4*)((float*)a.dq + (int64_t)b * a.q_sb + (int64_t)ii * a.q_st + (int64_t)hh * a.q_sh + d) = x * a.dq_scale;
   }
@@ -300,12 +318,11 @@ __global__ __launch_bounds__(256) void win_dq_f32_kernel(WinArgs a) {
 // dK, dV: 16 keys (FAR: 16 sinks and a chunk of the queries beyond their window, as in the bf16 kernel); each of 8 waves takes every eighth (query head, tile of 16 queries) pair of the kv head, in order. P
 // and dS have the key on the lane axis and are the B operands of dV^T += dO^T P, dK^T += Q^T dS.
 template <int DH, bool FAR>
-__global__ __launch_bounds__(512) void win_dkdv_f32_kernel(WinArgs a) {
+BPT_DEV void dkdv_f32(const WinArgs& a, float (&red)[4][16][DH + 4], int blk) {
   constexpr int NC = DH / 16;
-  __shared__ __attribute__((aligned(16))) float red[4][16][DH + 4];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, g = lane >> 4, c16 = lane & 15;
-  const int chunks = FAR ? a.far : a.chunks, chunk = blockIdx.x % chunks;
-  const int kvh = blockIdx.y, b = blockIdx.z, k0 = blockIdx.x / chunks * 16, key = k0 + c16;
+  const int chunks = FAR ? a.far : a.chunks, chunk = blk % chunks;
+  const int kvh = blockIdx.y, b = blockIdx.z, k0 = blk / chunks * 16, key = k0 + c16;
   const Seq sq = seq_of(a, b);
   const bool near = FAR || a.far > 0;
   const int kend = FAR ? min(sq.nk, a.sinks) : sq.nk;
@@ -356,26 +373,14 @@ __global__ __launch_bounds__(512) void win_dkdv_f32_kernel(WinArgs a) {
 #pragma unroll
   for (int which = 0; which < 2; ++which) {
     f32x4 (&x)[NC] = which ? dv : dk;
-    __syncthreads();
-    if (wave >= 4)
-#pragma unroll
-      for (int t = 0; t < NC; ++t) *(f32x4*)&red[wave - 4][c16][16 * t + 4 * g] = x[t];
-    __syncthreads();
-    if (wave < 4)
-#pragma unroll
-      for (int t = 0; t < NC; ++t) {
-        f32x4* at = (f32x4*)&red[wave][c16][16 * t + 4 * g];
-        *at = x[t] + *at;
-      }
-    __syncthreads();
+    add_eight<DH>(red, x, wave, g, c16);
     const int64_t base = which ? (int64_t)b * a.v_sb + (int64_t)kvh * a.v_sh : (int64_t)b * a.k_sb + (int64_t)kvh * a.k_sh;
     float* out = (float*)(which ? a.dv : a.dk) + base;
     for (int e = tid; e < 16 * (DH / 4); e += 512) {
       const int ki = e / (DH / 4), d = 4 * (e % (DH / 4));
       const int ns = win_slot_keys(a);
       if (k0 + ki >= (FAR ? ns : a.Skv)) continue;
-      const f32x4 x = ((*(const f32x4*)&red[0][ki][d] + *(const f32x4*)&red[1][ki][d]) + *(const f32x4*)&red[2][ki][d]) +
-                      *(const f32x4*)&red[3][ki][d];
+      const f32x4 x = add_four<DH>(red, ki, d);
       if (k0 + ki < ns) {
         const int64_t at = ((int64_t)(FAR ? 1 + chunk : chunk) * a.B * a.Hkv + (int64_t)b * a.Hkv + kvh) * ns + k0 + ki;
         *(f32x4*)(a.part_s + (2 * at + which) * DH + d) = x;
@@ -384,6 +389,19 @@ __global__ __launch_bounds__(512) void win_dkdv_f32_kernel(WinArgs a) {
       *(f32x4*)(out + (int64_t)(k0 + ki) * (which ? a.v_st : a.k_st) + d) = x * (which ? 1.0f : a.scale);
     }
   }
+}
+
+// dK dV by the first nkv workgroups of a kv head, dQ by the others: neither needs the other
+template <int DH>
+__global__ __launch_bounds__(512) void win_bwd_f32_kernel(WinArgs a, int nkv) {
+  __shared__ __attribute__((aligned(16))) float red[4][16][DH + 4];
+  if ((int)blockIdx.x < nkv) dkdv_f32<DH, false>(a, red, blockIdx.x);
+  else dq_f32<DH>(a, red, gridDim.x - 1 - blockIdx.x);
+}
+template <int DH>
+__global__ __launch_bounds__(512) void win_far_f32_kernel(WinArgs a) {
+  __shared__ __attribute__((aligned(16))) float red[4][16][DH + 4];
+  dkdv_f32<DH, true>(a, red, blockIdx.x);
 }
 
 template <int DH>
@@ -435,27 +453,20 @@ __global__ __launch_bounds__(256) void win_chunks_kernel(WinArgs a) {
 }
 
 template <int DH>
-static hipError_t dkdv_f32(const WinArgs& a, hipStream_t s) {
-  auto k = win_dkdv_f32_kernel<DH, false>;
-  hipLaunchKernelGGL(k, dim3((a.Skv + 15) / 16 * a.chunks, a.Hkv, a.B), dim3(512), 0, s, a);
+static hipError_t bwd_f32(const WinArgs& a, hipStream_t s) {
+  const int nkv = a.dk ? (a.Skv + 15) / 16 * a.chunks : 0, nq = a.dq ? (int)(((int64_t)a.Sq * a.G + 15) / 16) : 0;
+  if (nkv + nq == 0) return hipSuccess;
+  hipLaunchKernelGGL(win_bwd_f32_kernel<DH>, dim3(nkv + nq, a.Hkv, a.B), dim3(512), 0, s, a, nkv);
   return hipGetLastError();
 }
 template <int DH>
 static hipError_t far_f32(const WinArgs& a, hipStream_t s) {
-  auto k = win_dkdv_f32_kernel<DH, true>;
-  hipLaunchKernelGGL(k, dim3((std::min(a.sinks, a.Skv) + 15) / 16 * a.far, a.Hkv, a.B), dim3(512), 0, s, a);
-  return hipGetLastError();
-}
-template <int DH>
-static hipError_t dq_f32(const WinArgs& a, hipStream_t s) {
-  const unsigned nblk = (unsigned)(((int64_t)a.Sq * a.G + 15) / 16);
-  hipLaunchKernelGGL(win_dq_f32_kernel<DH>, dim3(nblk, a.Hkv, a.B), dim3(256), 0, s, a);
+  hipLaunchKernelGGL(win_far_f32_kernel<DH>, dim3((std::min(a.sinks, a.Skv) + 15) / 16 * a.far, a.Hkv, a.B), dim3(512), 0, s, a);
   return hipGetLastError();
 }
 hipError_t win_fwd_f32(const WinArgs& a, hipStream_t s) { return a.dh == 64 ? fwd_f32<64>(a, s) : fwd_f32<128>(a, s); }
-hipError_t win_dkdv_f32(const WinArgs& a, hipStream_t s) { return a.dh == 64 ? dkdv_f32<64>(a, s) : dkdv_f32<128>(a, s); }
+hipError_t win_bwd_f32(const WinArgs& a, hipStream_t s) { return a.dh == 64 ? bwd_f32<64>(a, s) : bwd_f32<128>(a, s); }
 hipError_t win_far_f32(const WinArgs& a, hipStream_t s) { return a.dh == 64 ? far_f32<64>(a, s) : far_f32<128>(a, s); }
-hipError_t win_dq_f32(const WinArgs& a, hipStream_t s) { return a.dh == 64 ? dq_f32<64>(a, s) : dq_f32<128>(a, s); }
 
 hipError_t win_join(Dt t, const WinArgs& a, hipStream_t s) {
   auto k = t == BF16 ? win_join_kernel<bf16> : win_join_kernel<float>;
