@@ -431,7 +431,7 @@ bpt_status bpt_layer_bwd_options(const bpt_config* cfg, const bpt_layer_options*
  * a step gives the same bytes every time it is repeated. A gradient that is not finite makes the moments
  * of its block meaningless. */
 typedef struct {
-  int64_t n;             /* elements; 0: nothing to do                                          */
+  int64_t n;             /* elements, at most 2^33; 0: nothing to do                            */
   float* p;              /* [n] fp32                                                            */
   const void* g;         /* [n] cfg->grad_dtype                                                 */
   void *m, *v;           /* [n] fp32, or [n] bytes                                              */

@@ -1670,6 +1670,7 @@ bpt_status bpt_adamw_multi(const bpt_adamw_multi_config* cfg, const bpt_adamw_te
   bpt_status st = dtype_ok(cfg->grad_dtype, "grad_dtype");
   if (st != BPT_OK || (st = dtype_ok(cfg->lowp_dtype, "lowp_dtype")) != BPT_OK) return st;
   const bool small = cfg->state_bits == 8;
+  const int64_t kMostBlocks = (int64_t)1 << 25;      // of one launch: 64 threads each, below 2^32
   std::vector<std::pair<uintptr_t, uintptr_t>> at;
   try {
     at.reserve(count);
@@ -1680,7 +1681,7 @@ bpt_status bpt_adamw_multi(const bpt_adamw_multi_config* cfg, const bpt_adamw_te
     const bpt_adamw_tensor& t = tensors[i];
     if (t.n < 0) return fail(BPT_ERR_INVALID_ARG, "tensor %lld: n must be >= 0", (long long)i);
     if (t.n == 0) continue;
-    if (t.n > (int64_t)1 << 38) return fail(BPT_ERR_UNSUPPORTED, "tensor %lld too large", (long long)i);
+    if (t.n > 256 * kMostBlocks) return fail(BPT_ERR_UNSUPPORTED, "tensor %lld: more than 2^33 elements", (long long)i);
     if (!t.p || !t.g || !t.m || !t.v || (small && !t.exps))
       return fail(BPT_ERR_INVALID_ARG, "tensor %lld: NULL p, g, m, v or exps", (long long)i);
     if (!(t.weight_decay >= 0.0) || !std::isfinite(t.weight_decay))
@@ -1696,7 +1697,6 @@ bpt_status bpt_adamw_multi(const bpt_adamw_multi_config* cfg, const bpt_adamw_te
     if (at[i].first < at[i - 1].second) return fail(BPT_ERR_INVALID_ARG, "two tensors' p overlap (the same tensor twice?)");
   hipStream_t s = (hipStream_t)stream;
   const uint32_t key = mix32(mix32((uint32_t)cfg->seed) ^ (uint32_t)(cfg->seed >> 32) ^ (uint32_t)cfg->step);
-  const int64_t kMostBlocks = (int64_t)1 << 31;      // of one launch
   AdamArgs a;
   a.lr = (float)cfg->lr; a.eps = (float)cfg->eps;
   a.b1 = (float)cfg->beta1; a.nb1 = (float)(1.0 - cfg->beta1);

@@ -178,6 +178,10 @@ def test_adamw_refuses_the_same_tensor_twice():
     assert adam(tensors=[dict(p=A, n=100), dict(p=A + 384)]) == 1
 
 
+def test_adamw_refuses_a_tensor_beyond_a_launch():
+    assert adam(tensors=[dict(n=2 ** 33 + 1)]) == 2 and "2^33" in err()
+
+
 def test_adamw_refuses_counts():
     assert adam(count=-1) == 1
     assert bpt.load().bpt_adamw_multi(None, None, 0, None) == 1
