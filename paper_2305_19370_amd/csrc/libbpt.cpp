@@ -487,14 +487,24 @@ int attn_far(const bpt_attn_config& c) {
 }
 int attn_slots(const bpt_attn_config& c, int far) { return 1 + far * (c.dtype == BPT_BF16 ? 2 : 1); }
 // Chunks of every block of keys' tiles in dK and dV: where the blocks (64 keys; fp32: 16) leave CUs idle, enough for two workgroups a CU
-// with at least 4 tiles of 64 queries (fp32: 8 of 16, one a wave) each. Their sums cost a pass over `chunks` fp32 copies of dK and dV.
+// with at least 4 tiles of 64 queries (fp32: 8 of 16, one a wave) each. Their sums cost a pass over `chunks` fp32 copies of dK
+// and dV and its launch, 8 us: as long as 4 tiles (fp32: 24) that a workgroup takes more than the longest of the
+// chunks and of dQ's beside it. 512 tokens, bf16, heads of 128: 4 heads 39 us (in chunks 42), 8 heads, 4 key heads in chunks 44 (50);
+// fp32, 4 heads of 64: 33 (44), 16 heads of 128, 4 key heads in chunks 133 (190).
+// With sinks, keeping those apart (attn_far) instead, if every block then has fewer tiles than a chunk of theirs: 4096 tokens,
+// 8 heads of 128, 2 key heads, window 512 119 us (in chunks 161); 2500 tokens, 12 heads of 64, 4 key heads, window
+// 1000 in chunks 85 (97).
 int attn_chunks(const bpt_attn_config& c) {
   const bool bf = c.dtype == BPT_BF16;
-  const int64_t keys = bf ? 64 : 16, blocks = (c.Skv + keys - 1) / keys * c.Hkv * c.B;
+  const int64_t keys = bf ? 64 : 16, G = c.Hq / c.Hkv, blocks = (c.Skv + keys - 1) / keys * c.Hkv * c.B;
   if (blocks >= 256) return 1;
-  const int64_t span = c.window && !c.sinks ? std::min(c.Sq, (c.causal ? 1 : 2) * c.window + keys) : c.Sq;
-  const int64_t tiles = (span + keys - 1) / keys * (c.Hq / c.Hkv);
-  return (int)std::max<int64_t>(1, std::min<int64_t>({512 / blocks, tiles / (bf ? 4 : 8), 16}));
+  const int64_t near = (c.causal ? 1 : 2) * c.window + keys;   // queries of a block of keys, or keys of rows
+  auto tiles_of = [&](int64_t len, bool all) { return ((all || !c.window ? len : std::min(len, near)) + keys - 1) / keys; };
+  const int64_t tiles = tiles_of(c.Sq, c.sinks > 0) * G, dq = tiles_of(c.Skv, false);
+  const int64_t chunks = std::max<int64_t>(1, std::min<int64_t>({512 / blocks, tiles / (bf ? 4 : 8), 16}));
+  if (tiles - std::max(tiles / chunks, dq) <= (bf ? 4 : 24)) return 1;
+  if (attn_far(c) > 0 && tiles_of(c.Sq, false) * G <= tiles / chunks) return 1;
+  return (int)chunks;
 }
 // Chunks and far chunks (with chunks, sinks are not apart) and the bytes of their sums
 struct AttnCut {
