@@ -8,6 +8,10 @@
 // place between two codes (16 bits of a mix of element, tensor, step and seed): a moment that moves by
 // less than a step per update, as r does with beta2 near 1, still follows its expectation, where
 // rounding to nearest would never move it. A root above zero keeps a code above zero, so m / r stays bounded.
+//
+// Bound by the copy (16 bytes an access and lane; a list costs one launch per kAdamTensors tensors): 50 million elements, 30 bytes
+// each with 32-bit moments and a bf16 copy 283 us, 5.3 TB/s; 142 million, 16 bytes each with 8-bit ones, bf16 gradients
+// and a bf16 copy 436 us, 5.2 TB/s.
 #include "common.h"
 #include "internal.h"
 

@@ -1540,16 +1540,27 @@ static bool attn_few(const bpt_attn_config& c) {
   const int64_t rows = c.Sq * (c.Hq / c.Hkv);
   return c.dtype == BPT_BF16 && (rows <= 32 || (rows + 127) / 128 * c.Hkv * c.B <= 64);
 }
-// Slices of the keys for a forward of few rows: workgroups for the chip several times over (sequences are of unequal length),
-// and 128 keys (bf16: a tile per wave) at least for each; none where a workgroup is done before a second launch would be, or
-// where the rows alone fill the chip.
+// Slices of the keys for a forward of few rows: none where a workgroup is done before a second launch would be, or where the
+// rows alone fill the chip. bf16, where a CU holds one workgroup: the number, of at least 128 keys each (a tile per wave), that
+// makes rounds of 256 workgroups times their length least, a workgroup's start and merge taking as long as 384 keys
+// and the join as 340. 128 tokens, 8 heads, 4096 keys: 8 slices 19 us (16: 28, 32: 48); 1 token of 4 sequences, 8
+// key heads, 8192 keys: 8 slices 31 us (32: 53).
 static int attn_nsplit(const bpt_attn_config& c) {
   const bool bf = c.dtype == BPT_BF16;
   if (bf && !attn_few(c)) return 1;
   const int64_t rows = c.Sq * (c.Hq / c.Hkv), groups = (rows + (bf ? 31 : 15)) / (bf ? 32 : 16) * c.Hkv * c.B;
   const int64_t span = c.window ? std::min(c.Skv, (c.causal ? 1 : 2) * c.window + c.sinks + c.Sq) : c.Skv;
   if (span <= 512 || groups >= 256) return 1;
-  return (int)std::max<int64_t>(1, std::min<int64_t>({1024 / groups, span / (bf ? 128 : 512), 64}));
+  if (!bf) return (int)std::max<int64_t>(1, std::min<int64_t>({1024 / groups, span / 512, 64}));
+  int64_t best = 1, least = 384 + span;
+  for (int64_t z = 2; z <= std::min<int64_t>(span / 128, 64); ++z) {
+    const int64_t cost = (groups * z + 255) / 256 * (384 + (span + z - 1) / z) + 340;
+    if (cost < least) {
+      least = cost;
+      best = z;
+    }
+  }
+  return (int)best;
 }
 
 struct AttnWs {

