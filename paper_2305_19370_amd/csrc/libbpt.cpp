@@ -1543,8 +1543,8 @@ static bool attn_few(const bpt_attn_config& c) {
 // Slices of the keys for a forward of few rows: none where a workgroup is done before a second launch would be, or where the
 // rows alone fill the chip. bf16, where a CU holds one workgroup: the number, of at least 128 keys each (a tile per wave), that
 // makes rounds of 256 workgroups times their length least, a workgroup's start and merge taking as long as 384 keys
-// and the join as 340. 128 tokens, 8 heads, 4096 keys: 8 slices 19 us (16: 28, 32: 48); 1 token of 4 sequences, 8
-// key heads, 8192 keys: 8 slices 31 us (32: 53).
+// and the join as 340 (5 - 8 us). 128 tokens, 8 heads, 4096 keys: 8 slices 18 us (16: 27, 32: 46); 1 token of 4 sequences, 8
+// key heads, 8192 keys: 8 slices 29 us (32: 51).
 static int attn_nsplit(const bpt_attn_config& c) {
   const bool bf = c.dtype == BPT_BF16;
   if (bf && !attn_few(c)) return 1;

@@ -1,7 +1,7 @@
 // Attention with a sliding window and sinks, bf16 backward: dQ (rows outside, key tiles inside) and dK, dV
 // (keys outside, query tiles of all the kv head's query heads inside): 3 and 4 products a visible pair, 2 of them the same,
 // so that neither needs atomics. Full attention of 32768 tokens, 32 heads of 128: 27.0 ms, 1140 TFLOP/s; 8192 tokens, 16 heads,
-// 4 key heads, window 1024: 285 us, 790. Bound by issue and LDS: each product reads an LDS fragment for every MFMA, and the
+// 4 key heads, window 1024: 274 us, 820. Bound by issue and LDS: each product reads an LDS fragment for every MFMA, and the
 // registers of a wave (the sums, its rows' fragments) leave room for one workgroup's latency to be hidden by one other.
 #include <algorithm>
 
@@ -312,7 +312,7 @@ __global__ __launch_bounds__(64 * KG * QH, KG * QH == 8 ? 1 : 2) void win_dkdv_b
 }
 // dK dV in blocks of 64 keys, by the first nkv workgroups, and dQ in blocks of 128 rows by the others: neither needs the
 // other, and short runs leave a chip that one of them alone does not fill (4 x 1000 tokens, 12 heads of 64, window 256: 39
-// us, in two launches 50). Heads of 64: three workgroups on a CU, at two stages for dQ and 24 bytes of spills a
+// us, in two launches 50, launch gaps included). Heads of 64: three workgroups on a CU, at two stages for dQ and 24 bytes of spills a
 // lane (16384 tokens, 16 heads, window 2048: 590 us, two workgroups 645).
 template <int DH>
 __global__ __launch_bounds__(256, DH == 64 ? 3 : 2) void win_bwd_bf16_kernel(WinArgs a, int nkv) {

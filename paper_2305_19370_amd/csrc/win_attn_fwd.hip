@@ -104,7 +104,7 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 1 : 2) void win_fwd_bf16_kernel(
 // that the cache is read by the whole chip. Bound by that read: each of the 4 waves streams tiles of 32 keys (every fourth of the
 // slice) through two LDS stages of its own, without a barrier, 80 KB of a CU's LDS in flight while the other 80 KB
 // are worked on; waves and slices are merged as two runs of an online softmax are. 24 sequences of up to 16384 keys, 32 heads of 128,
-// 8 key heads, all keys visible: 282 us, 5.7 TB/s; one of 65536: 65 us, 4.1 TB/s with the join.
+// 8 key heads, all keys visible: 285 us, 5.7 TB/s; one of 65536: 57 us, 4.7 TB/s with the join.
 template <int DH>
 struct WinTokCfg {
   static constexpr int KSTEPS = DH / 16, DT = DH / 32, NW = 4;
