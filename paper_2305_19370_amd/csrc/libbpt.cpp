@@ -560,6 +560,12 @@ bpt_status attn_check(const bpt_attn_config* c) {
   // workgroups of 16 rows and rows of the log-sum-exp
   if (c->B * c->Hkv * ((std::max(c->Sq * (c->Hq / c->Hkv), c->Skv) + 15) / 16) > (int64_t)1 << 26 || c->B * c->Hq * rup(c->Sq, 64) > (int64_t)1 << 32)
     return fail(BPT_ERR_UNSUPPORTED, "B * heads * length too large");
+  // threads of a launch: the backward's rows of Delta, and dK dV and dQ together
+  const int64_t rows = c->Sq * (c->Hq / c->Hkv), most = (int64_t)1 << 32;
+  if (rup(c->Sq, 64) * c->dh / 8 >= most ||
+      (c->dtype == BPT_F32 ? ((rows + 15) / 16 + (c->Skv + 15) / 16) * 512
+                           : ((rows + 127) / 128 + (c->Skv + 63) / 64) * c->Hkv * c->B * 256) >= most)
+    return fail(BPT_ERR_UNSUPPORTED, "length too large for a launch");
   if (!apart(c->o, c->B, c->Sq, c->Hq, c->dh)) return fail(BPT_ERR_INVALID_ARG, "strides of O overlap");
   return BPT_OK;
 }

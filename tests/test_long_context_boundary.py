@@ -89,6 +89,19 @@ def test_attn_refuses(kw, code):
     assert lib.bpt_attn_bwd(ctypes.byref(c), *p[:3], None, None, *p[3:9], p[9], 1 << 30, None) == code
 
 
+def test_attn_refuses_lengths_beyond_a_launch():
+    # fp32: workgroups of 512 threads for every 16 rows and every 16 keys, in one launch of fewer than 2^32 threads
+    small = dict(B=1, Hq=1, Hkv=1, q_sb=1 << 36, k_sb=1 << 36, v_sb=1 << 36, o_sb=1 << 36, q_st=64, k_st=64, v_st=64, o_st=64,
+                 q_sh=64, k_sh=64, v_sh=64, o_sh=64, dtype=bpt.BPT_F32)
+    assert bpt.attn_validate(attn(Sq=2 ** 26 - 16, Skv=2 ** 26, **small)) == 0, err()
+    assert bpt.attn_validate(attn(Sq=2 ** 26, Skv=2 ** 26, **small)) == 2
+    small["dtype"] = bpt.BPT_BF16
+    assert bpt.attn_validate(attn(Sq=2 ** 26, Skv=2 ** 26, **small)) == 0, err()
+    small.update({k: 128 for k in small if k.endswith(("_st", "_sh"))}, dh=128)
+    assert bpt.attn_validate(attn(Sq=2 ** 28 - 64, Skv=2 ** 28, **small)) == 0, err()
+    assert bpt.attn_validate(attn(Sq=2 ** 28, Skv=2 ** 28, **small)) == 2
+
+
 def test_attn_refuses_pointers():
     lib, c = bpt.load(), attn()
     need = bpt.attn_workspace_bytes(c, True)
