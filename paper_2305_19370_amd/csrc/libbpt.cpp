@@ -474,6 +474,14 @@ RopeArgs rope_args(const bpt_rope_config& c, const int32_t* positions, const voi
   return a;
 }
 
+// A bf16 forward whose blocks of 128 rows would leave most CUs idle takes the kernel for few rows, while its blocks of 32 are one
+// round of the chip: 512 tokens, 8 heads of 128 13.3 us (blocks of 128: 19.7); beyond, 1000 tokens, 16 heads, 4 key
+// heads, blocks of 128 30 (50).
+bool attn_few(const bpt_attn_config& c) {
+  const int64_t rows = c.Sq * (c.Hq / c.Hkv);
+  return c.dtype == BPT_BF16 && (rows <= 32 || (rows + 127) / 128 * c.Hkv * c.B <= 64);
+}
+
 // Chunks of what the sinks' keys see beyond their window in the backward: 0 where a block of keys that
 // holds sinks has little more to do than another, else workgroups for two a CU and at least two tiles
 // of 64 queries for each.
@@ -869,7 +877,8 @@ static bpt_status layer_fwd(const bpt_config* cfg, const bpt_layer_options* opt,
   }
   if (win) {               // linear in S: all groups' attention at once
     const bpt_attn_config ac = layer_attn(*cfg, *opt);
-    const WinArgs a = layer_win(*cfg, *opt, d, sv);
+    WinArgs a = layer_win(*cfg, *opt, d, sv);
+    a.few = attn_few(ac);
     RUN("win.fwd", 4.0 * d.dh * attn_seen(ac), 4.0 * T * D * E_, E == BF16 ? win_fwd_bf16(a, s) : win_fwd_f32(a, s));
   }
 
@@ -1540,12 +1549,6 @@ bpt_status bpt_rope_bwd(const bpt_rope_config* cfg, const int32_t* positions, co
 }
 
 // ---------------------------------------------------------------- attention with a window and sinks
-// A bf16 forward whose blocks of 128 rows would leave most CUs idle takes the kernel for few rows: 512 tokens, 8 heads of
-// 128 13.3 us (blocks of 128: 19.7); 1000 tokens, 4 key heads of 4 50 (30).
-static bool attn_few(const bpt_attn_config& c) {
-  const int64_t rows = c.Sq * (c.Hq / c.Hkv);
-  return c.dtype == BPT_BF16 && (rows <= 32 || (rows + 127) / 128 * c.Hkv * c.B <= 64);
-}
 // Slices of the keys for a forward of few rows: none where a workgroup is done before a second launch would be, or where the
 // rows alone fill the chip. bf16, where a CU holds one workgroup: the number, of at least 128 keys each (a tile per wave), that
 // makes rounds of 256 workgroups times their length least, a workgroup's start and merge taking as long as 384 keys

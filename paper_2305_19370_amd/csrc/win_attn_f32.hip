@@ -1,6 +1,6 @@
 // Attention with a sliding window and sinks, fp32: forward (whole, or one of several slices of
 // the keys), its join, and the backward. Matrix products on v_mfma_f32_16x16x4_f32 (attn_common.h:
-// row and column fragments straight from memory, 4 waves sharing 16 rows).
+// row and column fragments straight from memory, 4 waves, in the backward 8, sharing 16 rows).
 //
 // The query heads of a kv head and their tokens are one list of rows, r = token * G + head: a
 // workgroup's 16 rows then cover few tokens, see nearly the same keys, and a single token's heads
