@@ -88,6 +88,7 @@ CASES = [
     dict(B=2, S=200, H=2, opt=dict(rot=32, layout="interleaved", pos0=1000, mscale=1.1)),
     dict(B=1, S=1300, H=2, opt=dict(rot=128, scaling="by_parts", factor=4.0, orig_len=256, window=100, sinks=40)),
     dict(B=1, S=150, H=4, causal=False, opt=dict(rot=64, layout="interleaved", window=20, sinks=2)),
+    dict(B=3, S=700, H=4, opt=dict(rot=64, window=130, sinks=2)),            # more rows than the forward for few takes
 ]
 
 
