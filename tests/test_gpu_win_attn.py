@@ -80,6 +80,7 @@ SHAPES = [
     (4, 600, 600, 16, 8, True, 40, 5),              # blocks of keys enough for the chip: sinks apart
     (5, 530, 530, 16, 8, False, 30, 40),
     (1, 900, 900, 16, 2, True, 0, 0),               # few blocks, many heads: cut into chunks
+    (8, 1000, 1000, 4, 1, True, 100, 3),            # half the chip: sinks apart are the shorter way
     (1, 260, 260, 2, 2, True, 5000, 4),             # a window longer than the sequence
     (1, 260, 260, 2, 2, True, 16, 1000),            # more sinks than keys
 ]
@@ -106,6 +107,19 @@ def test_layouts(layout, dtype):
     kw = dict(causal=True, window=90, sinks=3)
     got = run(q, k, v, do, **kw)
     ref, err = attention(q, k, v, do, **kw)
+    for n in ref:
+        check(got[n], ref[n], err[n], n)
+
+
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("dh", [64, 128])
+def test_full_attention_in_large_blocks(dh, causal):
+    """Blocks of 256 rows and of 256 keys: as many as fill the chip twice over."""
+    lens = [1030, 1030, 1030, 1030, 1030, 700, 64, 0]
+    say(f"case attn 8 x {lens} dh {dh} causal {causal}")
+    q, k, v, do = make(8, 1030, 1030, 16, 16, dh, "bf16", seed=11)
+    got = run(q, k, v, do, q_lens=lens, kv_lens=lens, causal=causal)
+    ref, err = attention(q, k, v, do, q_lens=lens, kv_lens=lens, causal=causal)
     for n in ref:
         check(got[n], ref[n], err[n], n)
 
