@@ -423,7 +423,7 @@ bpt_status bpt_layer_bwd_options(const bpt_config* cfg, const bpt_layer_options*
                                  const bpt_grads* grads, void* workspace, size_t workspace_bytes, void* stream);
 
 /* One AdamW step on a list of tensors (bpt_adamw_step's formula on each, weight decay per tensor). Moments in 32
- * bits: m and v, fp32. In 8 bits: m and r = sqrt(v), each as one e4m3 byte (sign, 4 exponent and
+ * bits: m and v, fp32. In 8 bits: m and r = sqrt(v) (fp32, every operation rounded to nearest), each as one e4m3 byte (sign, 4 exponent and
  * 3 mantissa bits; 2^-9 .. 448) per element, and per block of 256 elements two bytes in `exps`: the moments of
  * block j are the codes' values times 2^(exps[2j] - 134) and 2^(exps[2j + 1] - 134). All bytes 0: zero
  * moments, the start of a training run. A code is rounded up with the probability of its value's place

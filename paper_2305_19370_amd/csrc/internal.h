@@ -195,7 +195,7 @@ struct AdamArgs {
   int count = 0;
   uint32_t blocks = 0;
   float lr = 0, b1 = 0, nb1 = 0, b2 = 0, nb2 = 0, eps = 0;   // nb = 1 - b
-  float c1 = 0, rc2 = 0;                // 1 / (1 - b1^t), 1 / sqrt(1 - b2^t)
+  float c1 = 0, c2 = 0, rc2 = 0;        // 1 / (1 - b1^t), 1 / (1 - b2^t) and its root
 };
 hipError_t adamw_multi(Dt tg, Dt tl, int bits, const AdamArgs& a, hipStream_t s);
 

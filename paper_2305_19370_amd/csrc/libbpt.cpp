@@ -1732,7 +1732,8 @@ bpt_status bpt_adamw_multi(const bpt_adamw_multi_config* cfg, const bpt_adamw_te
   a.b1 = (float)cfg->beta1; a.nb1 = (float)(1.0 - cfg->beta1);
   a.b2 = (float)cfg->beta2; a.nb2 = (float)(1.0 - cfg->beta2);
   a.c1 = (float)(1.0 / (1.0 - std::pow(cfg->beta1, (double)cfg->step)));
-  a.rc2 = (float)std::sqrt(1.0 / (1.0 - std::pow(cfg->beta2, (double)cfg->step)));
+  const double c2 = 1.0 / (1.0 - std::pow(cfg->beta2, (double)cfg->step));
+  a.c2 = (float)c2; a.rc2 = (float)std::sqrt(c2);
   const Dt tg = dt_of(cfg->grad_dtype), tl = dt_of(cfg->lowp_dtype);
   double bytes = 0;
   for (int64_t i = 0; i <= count; ++i) {
