@@ -5,6 +5,8 @@
 // through, 16 bytes per access. The angle is reduced in full turns in 64 bits (positions of a million
 // leave no digits of it in 32), the remainder of a turn in fp32. Bound by the copy: 16384 tokens, 32 heads of 128, bf16
 // 52 us, 5.1 TB/s (a large copy: 5.2).
+#include <algorithm>
+
 #include "common.h"
 #include "internal.h"
 
@@ -158,12 +160,27 @@ hipError_t rope_t(Dt t, const RopeArgs& a, int64_t Sp, hipStream_t s) {
   return hipGetLastError();
 }
 
+// Launches of at most 2^25 rows (2^26, four to a workgroup, would be 2^32 threads, which are refused). Where rows stand at pos0 + row %
+// S, a launch takes whole runs of S or a part of one, pos0 moved to its start.
 template <typename T, int N, bool INTER>
 static hipError_t launch(const RopeArgs& a, hipStream_t s) {
   const int rows_per = a.rows >= 4096 ? kRopeRows : 1;   // few rows: one per workgroup
-  const int64_t grid = (a.rows + rows_per - 1) / rows_per;
-  hipLaunchKernelGGL((rope_kernel<T, N, INTER>), dim3((unsigned)grid), dim3(256), 0, s, a, rows_per);
-  return hipGetLastError();
+  const int64_t most = (int64_t)1 << 25;
+  for (int64_t r = 0, n; r < a.rows; r += n) {
+    const int64_t at = r % a.S;
+    n = std::min(a.rows - r, most);
+    if (a.rows > most) n = at == 0 && n >= a.S ? n / a.S * a.S : std::min(n, a.S - at);
+    RopeArgs b = a;
+    b.rows = n;
+    b.x = (const T*)a.x + r * a.ldx;
+    b.y = (T*)a.y + r * a.ldy;
+    if (a.positions) b.positions = a.positions + r;
+    b.pos0 = a.pos0 + at;
+    hipLaunchKernelGGL((rope_kernel<T, N, INTER>), dim3((unsigned)((n + rows_per - 1) / rows_per)), dim3(256), 0, s, b, rows_per);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
 }
 template <typename T>
 static hipError_t launch_t(const RopeArgs& a, hipStream_t s) {
