@@ -9,6 +9,7 @@ is no fallback implementation.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 from typing import Dict, Optional, Tuple
 
@@ -280,6 +281,24 @@ def _int32(t: Optional[torch.Tensor], n: int, name: str) -> Optional[int]:
     return t.data_ptr()
 
 
+def _stream_on(dev: int, same: bool) -> int:
+    """The current stream of the current GPU, where a call's kernels run. dev: the device of one of its tensors; same: whether the
+    others are there too."""
+    if dev < 0:
+        raise ValueError("the tensors must be on the GPU")
+    if not same or dev != torch._C._cuda_getDevice():
+        raise ValueError(f"the tensors must be on the current device, cuda:{torch._C._cuda_getDevice()}")
+    return torch._C._cuda_getCurrentRawStream(dev)
+
+
+def _check_layout(t: torch.Tensor, layout: Tuple[torch.dtype, Tuple[int, ...], Tuple[int, ...]], name: str) -> None:
+    """Raises unless a tensor has this type, shape and strides (those of dimensions of one element count for nothing)."""
+    dtype, shape, strides = layout
+    if t.dtype != dtype or t.shape != shape or any(n > 1 and a != b for n, a, b in zip(shape, t.stride(), strides)):
+        raise ValueError(f"{name} must be {shape} of {dtype} with strides {strides}, as the configuration has it; not "
+                         f"{tuple(t.shape)} of {t.dtype} with strides {t.stride()}")
+
+
 def _stream() -> int:
     """The current device's current stream (read without torch's stream object, 2.4 us less a call)."""
     if torch.cuda.is_initialized():
@@ -546,12 +565,56 @@ def rope_validate(cfg: RopeConfig) -> int:
     return load().bpt_rope_validate(ctypes.byref(cfg))
 
 
+@functools.lru_cache(maxsize=1024)
+def _rope_layout(cfg: bytes):
+    """(type, shape, strides) of the rows at ldx and of those at ldy, as a tensor [rows, H, dh]."""
+    c = RopeConfig.from_buffer_copy(cfg)
+    return tuple((_TORCH_DT.get(c.dtype), (c.rows, c.H, c.dh), (ld, c.dh, 1)) for ld in (c.ldx, c.ldy))
+
+
+def _check_rows(t: torch.Tensor, layout, name: str) -> None:
+    """Raises unless a tensor holds a configuration's rows: its last dimensions are one row's heads (and what follows them there)
+    and its first ones count the rows, or it is a flat buffer of them."""
+    dtype, (rows, H, dh), (ld, _, _) = layout
+    if t.dtype == dtype:
+        dims = [(n, st) for n, st in zip(t.shape, t.stride()) if n != 1]
+        if len(dims) == 1 and dims[0][1] == 1 and dims[0][0] >= (rows - 1) * ld + H * dh:
+            return
+        inner, outer = 1, 1
+        while dims and inner < H * dh and dims[-1][1] == inner:
+            inner *= dims.pop()[0]
+        while dims and dims[-1][1] == outer * ld:
+            outer *= dims.pop()[0]
+        if not dims and inner >= H * dh and outer == rows:
+            return
+    raise ValueError(f"{name} must hold {rows} rows of {H} x {dh} {dtype}, {ld} elements apart, as the configuration has it; not "
+                     f"{tuple(t.shape)} of {t.dtype} with strides {t.stride()}")
+
+
 def rope_fwd(cfg: RopeConfig, X: torch.Tensor, Y: torch.Tensor, positions: Optional[torch.Tensor] = None) -> None:
-    _check(load().bpt_rope_fwd(ctypes.byref(cfg), _int32(positions, cfg.rows, "positions"), X.data_ptr(), Y.data_ptr(), _stream()))
+    at_x, at_y = _rope_layout(bytes(cfg))
+    if (X.dtype, X.shape, X.stride()) != at_x:
+        _check_rows(X, at_x, "X")
+    if (Y.dtype, Y.shape, Y.stride()) != at_y:
+        _check_rows(Y, at_y, "Y")
+    dev, pos = X.get_device(), None
+    same = Y.get_device() == dev
+    if positions is not None:
+        pos, same = _int32(positions, at_x[1][0], "positions"), same and positions.get_device() == dev
+    _check(load().bpt_rope_fwd(cfg, pos, X.data_ptr(), Y.data_ptr(), _stream_on(dev, same)))
 
 
 def rope_bwd(cfg: RopeConfig, dY: torch.Tensor, dX: torch.Tensor, positions: Optional[torch.Tensor] = None) -> None:
-    _check(load().bpt_rope_bwd(ctypes.byref(cfg), _int32(positions, cfg.rows, "positions"), dY.data_ptr(), dX.data_ptr(), _stream()))
+    at_x, at_y = _rope_layout(bytes(cfg))
+    if (dY.dtype, dY.shape, dY.stride()) != at_y:
+        _check_rows(dY, at_y, "dY")
+    if (dX.dtype, dX.shape, dX.stride()) != at_x:
+        _check_rows(dX, at_x, "dX")
+    dev, pos = dX.get_device(), None
+    same = dY.get_device() == dev
+    if positions is not None:
+        pos, same = _int32(positions, at_x[1][0], "positions"), same and positions.get_device() == dev
+    _check(load().bpt_rope_bwd(cfg, pos, dY.data_ptr(), dX.data_ptr(), _stream_on(dev, same)))
 
 
 # ---------------------------------------------------------------- attention with a window and sinks
@@ -583,22 +646,63 @@ def attn_workspace_bytes(cfg: AttnConfig, backward: bool) -> int:
     return load().bpt_attn_workspace_bytes(ctypes.byref(cfg), int(backward))
 
 
+@functools.lru_cache(maxsize=1024)
+def _attn_layout(cfg: bytes):
+    """(type, shape, strides) that a configuration gives q, k, v and o; sequences; rows of the log-sum-exp."""
+    c = AttnConfig.from_buffer_copy(cfg)
+    dt, qs, ks = _TORCH_DT.get(c.dtype), (c.B, c.Sq, c.Hq, c.dh), (c.B, c.Skv, c.Hkv, c.dh)
+    return (*((dt, shape, (s.sb, s.st, s.sh, 1)) for shape, s in ((qs, c.q), (ks, c.k), (ks, c.v), (qs, c.o))),
+            c.B, c.B * c.Hq * c.Sq)
+
+
+def _check_lse(lse: torch.Tensor, n: int) -> None:
+    if lse.dtype != torch.float32 or lse.numel() != n or not lse.is_contiguous():
+        raise ValueError(f"lse must be [B, Hq, Sq] contiguous float32, {n} elements; not {tuple(lse.shape)} of {lse.dtype}")
+
+
 def attn_fwd(cfg: AttnConfig, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, o: torch.Tensor, lse: torch.Tensor,
              workspace: Optional[torch.Tensor] = None, q_lens: Optional[torch.Tensor] = None,
              kv_lens: Optional[torch.Tensor] = None) -> None:
+    """Every tensor has the shape, strides and type that cfg gives it."""
+    at_q, at_k, at_v, at_o, B, rows = _attn_layout(bytes(cfg))
+    if (q.dtype, q.shape, q.stride()) != at_q:
+        _check_layout(q, at_q, "q")
+    if (k.dtype, k.shape, k.stride()) != at_k:
+        _check_layout(k, at_k, "k")
+    if (v.dtype, v.shape, v.stride()) != at_v:
+        _check_layout(v, at_v, "v")
+    ql, kl = _int32(q_lens, B, "q_lens"), _int32(kv_lens, B, "kv_lens")
+    if (o.dtype, o.shape, o.stride()) != at_o:
+        _check_layout(o, at_o, "o")
+    _check_lse(lse, rows)
+    dev = q.get_device()
+    same = dev == k.get_device() == v.get_device() == o.get_device() == lse.get_device()
+    for t in (q_lens, kv_lens, workspace):
+        same = same and (t is None or t.get_device() == dev)
     nb = 0 if workspace is None else workspace.numel() * workspace.element_size()
-    _check(load().bpt_attn_fwd(ctypes.byref(cfg), q.data_ptr(), k.data_ptr(), v.data_ptr(),
-                               _int32(q_lens, cfg.B, "q_lens"), _int32(kv_lens, cfg.B, "kv_lens"),
-                               o.data_ptr(), lse.data_ptr(), _ptr(workspace) if nb else None, nb, _stream()))
+    _check(load().bpt_attn_fwd(cfg, q.data_ptr(), k.data_ptr(), v.data_ptr(), ql, kl, o.data_ptr(), lse.data_ptr(),
+                               workspace.data_ptr() if nb else None, nb, _stream_on(dev, same)))
 
 
 def attn_bwd(cfg: AttnConfig, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, o: torch.Tensor, lse: torch.Tensor,
              do: torch.Tensor, dq: Optional[torch.Tensor], dk: Optional[torch.Tensor], dv: Optional[torch.Tensor],
              workspace: torch.Tensor, q_lens: Optional[torch.Tensor] = None, kv_lens: Optional[torch.Tensor] = None) -> None:
-    _check(load().bpt_attn_bwd(ctypes.byref(cfg), q.data_ptr(), k.data_ptr(), v.data_ptr(),
-                               _int32(q_lens, cfg.B, "q_lens"), _int32(kv_lens, cfg.B, "kv_lens"),
-                               o.data_ptr(), lse.data_ptr(), do.data_ptr(), _ptr(dq), _ptr(dk), _ptr(dv), workspace.data_ptr(),
-                               workspace.numel() * workspace.element_size(), _stream()))
+    """Every tensor has the shape, strides and type that cfg gives it: dq, dk and dv those of q, k and v, do those of o."""
+    at_q, at_k, at_v, at_o, B, rows = _attn_layout(bytes(cfg))
+    dev, same = q.get_device(), True
+    for t, at, name in ((q, at_q, "q"), (k, at_k, "k"), (v, at_v, "v"), (o, at_o, "o"), (do, at_o, "do"), (dq, at_q, "dq"),
+                        (dk, at_k, "dk"), (dv, at_v, "dv")):
+        if t is not None:
+            if (t.dtype, t.shape, t.stride()) != at:
+                _check_layout(t, at, name)
+            same = same and t.get_device() == dev
+    _check_lse(lse, rows)
+    ql, kl = _int32(q_lens, B, "q_lens"), _int32(kv_lens, B, "kv_lens")
+    for t in (lse, workspace, q_lens, kv_lens):
+        same = same and (t is None or t.get_device() == dev)
+    _check(load().bpt_attn_bwd(cfg, q.data_ptr(), k.data_ptr(), v.data_ptr(), ql, kl, o.data_ptr(), lse.data_ptr(), do.data_ptr(),
+                               _ptr(dq), _ptr(dk), _ptr(dv), workspace.data_ptr(), workspace.numel() * workspace.element_size(),
+                               _stream_on(dev, same)))
 
 
 class WindowAttention:
@@ -675,5 +779,6 @@ def adamw_multi(tensors: AdamWTensors, step: int, lr: float, beta1: float = 0.9,
     """One AdamW update of every tensor of the list, in place."""
     if tensors.device is not None and tensors.device.type != "cuda":
         raise ValueError("the tensors must be on the GPU")
+    stream = _stream_on(tensors.device.index, True) if tensors.tensors else _stream()
     cfg = AdamWMultiConfig(lr, beta1, beta2, eps, step, seed & (2 ** 64 - 1), tensors.bits, tensors.grad_dtype, tensors.lowp_dtype, 0)
-    _check(load().bpt_adamw_multi(ctypes.byref(cfg), tensors.array, len(tensors.tensors), _stream()))
+    _check(load().bpt_adamw_multi(ctypes.byref(cfg), tensors.array, len(tensors.tensors), stream))
