@@ -11,7 +11,7 @@ from __future__ import annotations
 import ctypes
 import functools
 import os
-from typing import Dict, Optional, Tuple
+from typing import Dict, List, Optional, Tuple
 
 import torch
 
@@ -621,7 +621,10 @@ def rope_bwd(cfg: RopeConfig, dY: torch.Tensor, dX: torch.Tensor, positions: Opt
 def _strides(t: torch.Tensor) -> AttnStrides:
     if t.dim() != 4 or (t.shape[3] > 1 and t.stride(3) != 1):
         raise ValueError("attention tensors are [B, S, heads, dh] with adjacent features")
-    return AttnStrides(t.stride(0), t.stride(1), t.stride(2))
+    unit = 16 // t.element_size()
+    # the stride of a dimension of one element says nothing and may be any number
+    return AttnStrides(*(0 if n == 1 and (st % unit or not 0 <= st < most) else st
+                         for n, st, most in zip(t.shape, t.stride(), (1 << 40, 1 << 22, 1 << 40))))
 
 
 def attn_config_of(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, o: torch.Tensor, causal: bool = True, window: int = 0,
@@ -705,6 +708,41 @@ def attn_bwd(cfg: AttnConfig, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
                                _stream_on(dev, same)))
 
 
+def _span(t: torch.Tensor) -> int:
+    """Elements from a tensor's first to behind its last."""
+    return 1 + sum((n - 1) * st for n, st in zip(t.shape, t.stride()))
+
+
+def _apart(t: torch.Tensor) -> bool:
+    """Whether no two elements of a tensor share a place, features are adjacent and rows of heads start at whole 16 bytes."""
+    dims = sorted((st, n) for st, n in zip(t.stride(), t.shape) if n > 1)
+    end, unit = 1, 16 // t.element_size()
+    for st, n in dims:
+        if st < end:
+            return False
+        end += st * (n - 1)
+    return t.data_ptr() % 16 == 0 and t.stride(-1) == 1 and all(st % unit == 0 for st, n in dims if st > 1)
+
+
+def _side_by_side(tensors: Tuple[torch.Tensor, ...]) -> Optional[List[torch.Tensor]]:
+    """For parts of the rows of one tensor (Q, K and V as columns of one projection): new tensors that are such parts of
+    a new one. None for others."""
+    first = tensors[0]
+    st, (B, S) = first.stride(), first.shape[:2]
+    at = sorted((t.storage_offset(), t.storage_offset() + (t.shape[2] - 1) * st[2] + t.shape[3]) for t in tensors)
+    low, high = at[0][0], at[-1][1]
+    if (any(t.stride() != st or t.shape[:2] != (B, S) or t.dtype != first.dtype
+            or t.untyped_storage().data_ptr() != first.untyped_storage().data_ptr() or not _apart(t) for t in tensors)
+            or any(a[1] > b[0] for a, b in zip(at, at[1:])) or (S > 1 and high - low > st[1])
+            or (B > 1 and (S - 1) * st[1] + high - low > st[0])):
+        return None
+    n = (B - 1) * st[0] + (S - 1) * st[1] + high - low
+    if n > 2 * sum(t.numel() for t in tensors):      # mostly something else
+        return None
+    buf = torch.empty(n, dtype=first.dtype, device=first.device)
+    return [buf.as_strided(t.shape, st, t.storage_offset() - low) for t in tensors]
+
+
 class WindowAttention:
     """Attention with a window and sinks through libbpt; allocates its buffers with torch."""
 
@@ -729,12 +767,21 @@ class WindowAttention:
     def backward(self, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, o: torch.Tensor, lse: torch.Tensor, do: torch.Tensor,
                  q_lens: Optional[torch.Tensor] = None,
                  kv_lens: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor, torch.Tensor]:
-        """dQ, dK, dV; q, k, v as they were, o, lse from forward."""
-        q, k, v, do = (t.contiguous() for t in (q, k, v, do))
-        dq, dk, dv = torch.empty_like(q), torch.empty_like(k), torch.empty_like(v)
+        """dQ, dK, dV; q, k, v as they were, o, lse from forward. Gradients of columns of one projection are columns of one
+        tensor, those of a tensor without gaps are laid out like it, others are contiguous (and their input is copied)."""
+        if any(t.dim() != 4 for t in (q, k, v, o)):
+            raise ValueError("attention tensors are [B, S, heads, dh]")
+        if do.shape != o.shape or do.dtype != o.dtype:
+            raise ValueError(f"do must be {tuple(o.shape)} of {o.dtype}, not {tuple(do.shape)} of {do.dtype}")
+        if do.stride() != o.stride():                # they share their strides
+            o, do = o.contiguous(), do.contiguous()
+        grads = _side_by_side((q, k, v))
+        if grads is None:
+            q, k, v = (t if _apart(t) and _span(t) == t.numel() else t.contiguous() for t in (q, k, v))
+            grads = [torch.empty_strided(t.shape, t.stride(), dtype=t.dtype, device=t.device) for t in (q, k, v)]
         cfg = attn_config_of(q, k, v, o, **self.kw)
-        attn_bwd(cfg, q, k, v, o, lse, do, dq, dk, dv, self._bytes(attn_workspace_bytes(cfg, True), q.device), q_lens, kv_lens)
-        return dq, dk, dv
+        attn_bwd(cfg, q, k, v, o, lse, do, *grads, self._bytes(attn_workspace_bytes(cfg, True), q.device), q_lens, kv_lens)
+        return tuple(grads)
 
 
 # ---------------------------------------------------------------- AdamW over many tensors

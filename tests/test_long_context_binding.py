@@ -65,6 +65,17 @@ def test_attention_refuses(call, name, bad):
             bpt.attn_fwd(cfg, **{n: t[n] for n in FWD})
 
 
+def test_strides_of_single_elements_count_for_nothing():
+    """One sequence, one token: whatever stride such a dimension shows is taken, and is a valid one in the configuration."""
+    x = torch.zeros(7 * 5 * 3 * 64 + 8, dtype=BF)
+    q = x.as_strided((1, 1, 3, 64), (13, 7, 64, 1))
+    k = x.as_strided((1, 5, 3, 64), (3, 192, 64, 1))
+    cfg = bpt.attn_config_of(q, k, k, q)
+    assert bpt.attn_validate(cfg) == 0
+    with pytest.raises(ValueError, match="on the GPU"):
+        bpt.attn_fwd(cfg, q, k, k, torch.empty(1, 1, 3, 64, dtype=BF), torch.empty(1, 3, 1), None)
+
+
 # ---------------------------------------------------------------- rotary positions
 def rope_cfg(**kw):
     return bpt.make_rope_config(12, 4, 2, 64, **kw)
@@ -119,3 +130,44 @@ def test_rope_of_one_row():
     for x in (torch.empty(1, 2, 64, dtype=BF), torch.empty(128, dtype=BF), torch.empty(2, 64, dtype=BF), torch.empty(1, 400, dtype=BF)):
         with pytest.raises(ValueError, match="on the GPU"):
             bpt.rope_fwd(cfg, x, torch.empty(1, 2, 64, dtype=BF))
+
+
+# ---------------------------------------------------------------- WindowAttention
+def test_window_attention_refuses_gradients_of_another_kind():
+    q, k, v = packed()
+    o, lse = torch.empty(q.shape, dtype=BF), torch.empty(2, 4, 10)
+    att = bpt.WindowAttention(window=4)
+    for do in (torch.empty(q.shape), torch.empty(2, 9, 4, 64, dtype=BF)):
+        with pytest.raises(ValueError, match="^do must"):
+            att.backward(q, k, v, o, lse, do)
+    with pytest.raises(ValueError, match="^lse must"):
+        att.backward(q, k, v, o, lse[:1], torch.empty_like(o))
+    with pytest.raises(ValueError, match="on the GPU"):
+        att.backward(q, k, v, o, lse, torch.empty_like(o))
+
+
+def test_gradients_side_by_side():
+    """Columns of a projection give columns of one gradient, without a gap; tensors of their own, or of which another is most of the
+    rows, do not."""
+    q, k, v = packed()
+    g = bpt._side_by_side((q, k, v))
+    assert [t.stride() for t in g] == [q.stride()] * 3 and [t.shape for t in g] == [q.shape, k.shape, v.shape]
+    assert len({t.untyped_storage().data_ptr() for t in g}) == 1 and g[0].untyped_storage().nbytes() == 2 * 2 * 10 * 8 * 64
+    assert [t.storage_offset() for t in g] == [0, 256, 384]
+    assert [t.storage_offset() for t in bpt._side_by_side((v, q, k))] == [384, 0, 256]
+    x = torch.zeros(2, 10, 40, 64, dtype=BF)
+    assert bpt._side_by_side((x[:, :, :4], x[:, :, 4:6], x[:, :, 6:8])) is None        # a fifth of the rows
+    assert bpt._side_by_side((q, k, k)) is None and bpt._side_by_side((q, k, v.clone())) is None
+    assert bpt._side_by_side((q, k, v.contiguous())) is None
+    assert bpt._side_by_side((q[:, :, :3], k, v[:, :9])) is None
+    y = torch.zeros(2, 10, 8, 72, dtype=BF)
+    z = y[..., 4:68]                                                                   # not at 16 bytes
+    assert bpt._side_by_side((z[:, :, :4], z[:, :, 4:6], z[:, :, 6:])) is None
+
+
+def test_what_a_gradient_can_be_laid_out_like():
+    x = torch.zeros(2, 10, 4, 64, dtype=BF)
+    assert bpt._apart(x) and bpt._apart(x.transpose(1, 2)) and bpt._apart(x[:, :, 1:3]) and bpt._span(x) == x.numel()
+    assert bpt._span(x[:, :5]) > x[:, :5].numel()
+    assert not bpt._apart(x[:1].expand(2, 10, 4, 64)) and not bpt._apart(x.transpose(2, 3)) and not bpt._apart(x[..., ::2])
+    assert not bpt._apart(torch.zeros(2, 10, 4, 68, dtype=BF)[..., 4:])
