@@ -674,15 +674,18 @@ def attn_fwd(cfg: AttnConfig, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
         _check_layout(k, at_k, "k")
     if (v.dtype, v.shape, v.stride()) != at_v:
         _check_layout(v, at_v, "v")
-    ql, kl = _int32(q_lens, B, "q_lens"), _int32(kv_lens, B, "kv_lens")
     if (o.dtype, o.shape, o.stride()) != at_o:
         _check_layout(o, at_o, "o")
     _check_lse(lse, rows)
-    dev = q.get_device()
+    dev, nb = q.get_device(), 0
     same = dev == k.get_device() == v.get_device() == o.get_device() == lse.get_device()
-    for t in (q_lens, kv_lens, workspace):
-        same = same and (t is None or t.get_device() == dev)
-    nb = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    ql = kl = None
+    if q_lens is not None:
+        ql, same = _int32(q_lens, B, "q_lens"), same and q_lens.get_device() == dev
+    if kv_lens is not None:
+        kl, same = _int32(kv_lens, B, "kv_lens"), same and kv_lens.get_device() == dev
+    if workspace is not None:
+        nb, same = workspace.numel() * workspace.element_size(), same and workspace.get_device() == dev
     _check(load().bpt_attn_fwd(cfg, q.data_ptr(), k.data_ptr(), v.data_ptr(), ql, kl, o.data_ptr(), lse.data_ptr(),
                                workspace.data_ptr() if nb else None, nb, _stream_on(dev, same)))
 
@@ -692,17 +695,36 @@ def attn_bwd(cfg: AttnConfig, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
              workspace: torch.Tensor, q_lens: Optional[torch.Tensor] = None, kv_lens: Optional[torch.Tensor] = None) -> None:
     """Every tensor has the shape, strides and type that cfg gives it: dq, dk and dv those of q, k and v, do those of o."""
     at_q, at_k, at_v, at_o, B, rows = _attn_layout(bytes(cfg))
-    dev, same = q.get_device(), True
-    for t, at, name in ((q, at_q, "q"), (k, at_k, "k"), (v, at_v, "v"), (o, at_o, "o"), (do, at_o, "do"), (dq, at_q, "dq"),
-                        (dk, at_k, "dk"), (dv, at_v, "dv")):
-        if t is not None:
-            if (t.dtype, t.shape, t.stride()) != at:
-                _check_layout(t, at, name)
-            same = same and t.get_device() == dev
+    if (q.dtype, q.shape, q.stride()) != at_q:
+        _check_layout(q, at_q, "q")
+    if (k.dtype, k.shape, k.stride()) != at_k:
+        _check_layout(k, at_k, "k")
+    if (v.dtype, v.shape, v.stride()) != at_v:
+        _check_layout(v, at_v, "v")
+    if (o.dtype, o.shape, o.stride()) != at_o:
+        _check_layout(o, at_o, "o")
+    if (do.dtype, do.shape, do.stride()) != at_o:
+        _check_layout(do, at_o, "do")
     _check_lse(lse, rows)
-    ql, kl = _int32(q_lens, B, "q_lens"), _int32(kv_lens, B, "kv_lens")
-    for t in (lse, workspace, q_lens, kv_lens):
-        same = same and (t is None or t.get_device() == dev)
+    dev = q.get_device()
+    same = dev == k.get_device() == v.get_device() == o.get_device() == do.get_device() == lse.get_device() == workspace.get_device()
+    if dq is not None:
+        if (dq.dtype, dq.shape, dq.stride()) != at_q:
+            _check_layout(dq, at_q, "dq")
+        same = same and dq.get_device() == dev
+    if dk is not None:
+        if (dk.dtype, dk.shape, dk.stride()) != at_k:
+            _check_layout(dk, at_k, "dk")
+        same = same and dk.get_device() == dev
+    if dv is not None:
+        if (dv.dtype, dv.shape, dv.stride()) != at_v:
+            _check_layout(dv, at_v, "dv")
+        same = same and dv.get_device() == dev
+    ql = kl = None
+    if q_lens is not None:
+        ql, same = _int32(q_lens, B, "q_lens"), same and q_lens.get_device() == dev
+    if kv_lens is not None:
+        kl, same = _int32(kv_lens, B, "kv_lens"), same and kv_lens.get_device() == dev
     _check(load().bpt_attn_bwd(cfg, q.data_ptr(), k.data_ptr(), v.data_ptr(), ql, kl, o.data_ptr(), lse.data_ptr(), do.data_ptr(),
                                _ptr(dq), _ptr(dk), _ptr(dv), workspace.data_ptr(), workspace.numel() * workspace.element_size(),
                                _stream_on(dev, same)))
