@@ -362,8 +362,8 @@ bpt_status bpt_rope_bwd(const bpt_rope_config* cfg, const int32_t* positions, co
  * key: a prompt, a piece of one or single tokens against a cache) and sees key k iff
  *     k < nk, and (not causal or k <= p), and (window = 0 or |p - k| < window or k < sinks).
  * Query head h reads key head h / (Hq / Hkv). A query that sees nothing (its sequence empty, or p < 0
- * with the causal mask) gives O = 0, lse = -inf and no gradients. Keys that no query of the call sees are not
- * read, whatever they hold. A NaN or infinity in Q or K reaches the queries whose scores it enters; one in V (or, in the
+ * with the causal mask) gives O = 0, lse = -inf and no gradients. Keys that no query of the call sees change
+ * nothing, whatever they hold, and get none. A NaN or infinity in Q or K reaches the queries whose scores it enters; one in V (or, in the
  * backward, anywhere) can reach other queries and keys of the same blocks, whose weight for it is 0.
  * Tensors are [B, S, heads, dh] in any order of strides: element (b, t, h, d) at b sb + t st + h sh + d. */
 typedef struct {

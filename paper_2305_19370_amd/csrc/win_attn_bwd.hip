@@ -150,9 +150,11 @@ BPT_DEV void dkdv_keys(const WinArgs& a, char* smem, int id) {
   const int t0 = run.lo / 64, nt = run.hi >= run.lo ? run.hi / 64 + 1 - t0 : 0;   // tiles of a query head
   const int per = (nt * a.G + chunks - 1) / chunks;
   const int j0 = chunk * per, n = min(per, nt * a.G - j0);
+  QVis mine{0, -1};
   if (n > 0) {
     // keys behind the sequence's last stand for it; their results are left out in the end
-    QVis mine = qvis_of(a, sq, min(key, sq.nk - 1), min(key, sq.nk - 1), near), first{0, -1}, last{0, -1};
+    mine = qvis_of(a, sq, min(key, sq.nk - 1), min(key, sq.nk - 1), near);
+    QVis first{0, -1}, last{0, -1};
     const int kl = min(kw + 31, kend - 1);
     if (kw < sq.nk) {
       first = qvis_of(a, sq, kw, kw, near);
@@ -277,7 +279,9 @@ BPT_DEV void dkdv_keys(const WinArgs& a, char* smem, int id) {
       adv[t] = both[C::DT + t];
     }
   }
-  if (key >= sq.nk) {
+  // a key that no query sees, behind the sequence's last or in front of the first query's window: whatever it holds is in its own
+  // column alone (0 times its dP)
+  if (key >= sq.nk || (!FAR && mine.hi < mine.lo)) {
 #pragma unroll
     for (int t = 0; t < C::DT; ++t) adv[t] = adk[t] = f32x16{};
   }
