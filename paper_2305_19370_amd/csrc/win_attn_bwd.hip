@@ -93,7 +93,7 @@ BPT_DEV void dq_rows(const WinArgs& a, char* smem, int id) {
       if (!w.none(k0)) tile(j, k0, w.all(k0));
     });
   }
-  if (!w.exists) {
+  if (!w.exists || !w.mine.any()) {                  // nothing seen: 0, beside rows that see a NaN too
 #pragma unroll
     for (int t = 0; t < C::DT; ++t) acc[t] = f32x16{};
   }

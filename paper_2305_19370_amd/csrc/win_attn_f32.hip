@@ -173,8 +173,8 @@ __global__ __launch_bounds__(256) void win_join_kernel(WinArgs a) {
   const float inv = l != 0.0f ? 1.0f / l : 0.0f;
   const int i = rr / a.G, h = kvh * a.G + rr % a.G;
   T* o = (T*)a.o + (int64_t)b * a.o_sb + (int64_t)i * a.o_st + (int64_t)h * a.o_sh + d;
-  o[0] = from_f32<T>(o0 * inv);
-  if (a.dh == 128) o[1] = from_f32<T>(o1 * inv);
+  o[0] = from_f32<T>(l != 0.0f ? o0 * inv : 0.0f);   // a row that sees nothing: 0, beside rows that see a NaN too
+  if (a.dh == 128) o[1] = from_f32<T>(l != 0.0f ? o1 * inv : 0.0f);
   if (lane == 0) a.lse[((int64_t)b * a.Hq + h) * a.lse_ld + i] = l != 0.0f ? (m + log2f(l)) * LN2 : NEG_INF;
 }
 
@@ -318,6 +318,10 @@ BPT_DEV void dq_f32(const WinArgs& a, float (&red)[4][16][DH + 4], int blk) {
         ds[r] = mine.sees(k0 + 4 * g + r) ? fast_exp2((s[r] + nl) * c) * (ds[r] + ndl) : 0.0f;
       add_outer<DH>(dq, kc, ds);
     }
+  }
+  if (!mine.any()) {                                 // nothing seen: 0, beside rows that see a NaN too
+#pragma unroll
+    for (int t = 0; t < NC; ++t) dq[t] = f32x4{};
   }
   add_eight<DH>(red, dq, wave, g, c16);
   for (int e = tid; e < 16 * (DH / 4); e += 512) {

@@ -232,7 +232,7 @@ __global__ __launch_bounds__(256, 1) void win_token_kernel(WinArgs a) {
     const float inv = lt != 0.0f ? 1.0f / lt : 0.0f;  // a row that sees nothing: 0
     bf16x4 x;
 #pragma unroll
-    for (int k = 0; k < 4; ++k) x[k] = (bf16)(o[k] * inv);
+    for (int k = 0; k < 4; ++k) x[k] = (bf16)(lt != 0.0f ? o[k] * inv : 0.0f);   // beside rows that see a NaN too
     *(bf16x4*)((bf16*)a.o + (int64_t)b * a.o_sb + (int64_t)i * a.o_st + (int64_t)hq * a.o_sh + d) = x;
     if (d == 0) a.lse[((int64_t)b * a.Hq + hq) * a.lse_ld + i] = lt != 0.0f ? (m + log2f(lt)) * LN2 : NEG_INF;
   }

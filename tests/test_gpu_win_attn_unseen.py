@@ -1,5 +1,5 @@
 """What windowed attention promises about what is not seen: keys that no query of the call sees change nothing, whatever they hold,
-in the backward too."""
+in the backward too; a query that sees nothing has O = 0, lse = -inf and dQ = 0 beside queries that see a NaN."""
 import math
 
 import pytest
@@ -64,3 +64,31 @@ def test_keys_that_a_rolling_cache_gave_up(case, dh, dtype):
     for n in ref:
         check(got[n], ref[n], err[n], n)
     assert not bool(got["dK"][:, sinks:gone].any()) and not bool(got["dV"][:, sinks:gone].any())
+
+
+BLIND = [
+    # B, Sq, Skv, Hq, Hkv, causal, window, sinks: queries in front of the first key see nothing
+    (1, 20, 10, 2, 1, True, 0, 0),                   # few rows
+    (1, 1200, 1100, 1, 1, True, 0, 0),               # few rows in slices
+    (8, 300, 130, 16, 8, True, 0, 0),
+    (8, 300, 130, 16, 8, True, 20, 3),
+    (2, 130, 50, 2, 1, False, 9, 2),
+    (4, 700, 650, 16, 8, True, 33, 7),               # sinks apart
+]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("dh", [64, 128])
+@pytest.mark.parametrize("case", BLIND, ids=lambda s: "-".join(str(int(x)) for x in s))
+def test_queries_that_see_nothing_beside_a_nan(case, dh, dtype):
+    """The first keys, which the blind queries' neighbours see, hold NaN (V) and infinity (K)."""
+    B, Sq, Skv, Hq, Hkv, causal, window, sinks = case
+    say(f"case blind {case} dh {dh} {dtype}")
+    q, k, v, do = make(B, Sq, Skv, Hq, Hkv, dh, dtype, Sq)
+    k[:, 0], k[:, 1], v[:, 0], v[:, 2] = math.inf, math.nan, math.nan, math.inf
+    blind = Sq - Skv - (0 if causal else window - 1)
+    if sinks and not causal:
+        blind = 0                                    # sinks are seen by all
+    got = run(q, k, v, do, causal=causal, window=window, sinks=sinks)
+    assert not bool(got["O"][:, :blind].any()) and not bool(got["dQ"][:, :blind].any())
+    assert bool((got["lse"][:, :, :blind] == -math.inf).all()) and not bool((got["lse"][:, :, blind:] == -math.inf).any())
