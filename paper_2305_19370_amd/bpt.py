@@ -387,8 +387,10 @@ class Layer:
                  dY: torch.Tensor, want: Optional[Tuple[str, ...]] = None,
                  workspace: Optional[torch.Tensor] = None,
                  qkv_grads: bool = False) -> Tuple[torch.Tensor, Dict[str, torch.Tensor]]:
-        """dX and the parameter gradients; with qkv_grads, also "dQ", "dK", "dV" [B, S, D]
-        (copies of what the backward leaves in its workspace, bpt_bwd_qkv_grad_offset)."""
+        """dX and the parameter gradients; with qkv_grads, also "dQ", "dK", "dV" [B, S, D], the gradients of
+        Q = U Wq, K, V (copies of what the backward leaves in its workspace, bpt_bwd_qkv_grad_offset; not with a window)."""
+        if qkv_grads and self.options is not None and self.options.window:
+            raise ValueError("qkv_grads is for a layer without a window")
         D, F = self.cfg.D, self.cfg.F
         shapes = {"dln1_g": (D,), "dln1_b": (D,), "dWq": (D, D), "dWk": (D, D), "dWv": (D, D), "dWo": (D, D),
                   "dln2_g": (D,), "dln2_b": (D,), "dW1": (D, F), "db1": (F,), "dW2": (F, D), "db2": (D,)}
@@ -404,8 +406,6 @@ class Layer:
         ws = workspace if workspace is not None else self._bytes(workspace_bytes(self.cfg, True))
         layer_bwd(self.cfg, X, params, saved, dY, dX, grads, ws, self.options)
         if qkv_grads:
-            if self.options is not None:
-                raise ValueError("qkv_grads is for a layer without options")
             c = self.cfg
             E = _TORCH_DT[c.dtype]
             Sp = (c.S + 63) // 64 * 64
