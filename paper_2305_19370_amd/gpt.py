@@ -109,7 +109,11 @@ class GPT:
                                    out_dtype=s.dtype, ln_eps=s.ln_eps, activation=s.activation,
                                    dropout=s.dropout)
         self.options = None
-        if s.rope != "none" or s.window:
+        if s.opt_bits not in (8, 32):
+            raise ValueError(f"opt_bits must be 8 or 32, not {s.opt_bits}")
+        if s.rope == "none" and (s.rope_scaling != "none" or s.rope_factor != 1.0 or s.rope_orig_len != 0):
+            raise ValueError("rope_scaling, rope_factor and rope_orig_len need rope")
+        if s.rope != "none" or s.window or s.sinks:
             rot = 0 if s.rope == "none" else s.D // s.H
             self.options = bpt.make_layer_options(rot=rot, layout=s.rope if rot else "half", theta=s.rope_theta,
                                                   scaling=s.rope_scaling if rot else "none", factor=s.rope_factor,
