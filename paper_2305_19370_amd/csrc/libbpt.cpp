@@ -965,7 +965,9 @@ bpt_status bpt_layer_fwd_options(const bpt_config* cfg, const bpt_layer_options*
   return layer_fwd(cfg, options, X, p, Y, saved, ws, ws_bytes, stream);
 }
 
-// QKV projection and LN1 backward from dQ, dK, dV token-major in w.dqkvT ([T, 3D], as the window kernels leave them)
+// QKV projection and LN1 backward from dQ, dK, dV token-major in w.dqkvT ([T, 3D], as the window kernels leave them). dU is three
+// products that add up and the weight gradients three products (kper and nper take the other order of their operand): 16384
+// tokens, D = 2048, 450 and 407 us with the joins of their slices, where the layer without a window takes 343 and 348.
 static bpt_status layer_bwd_proj(const bpt_config& cfg, const Dims& d, Dt E, Dt OUT, const void* X, const bpt_params* p,
                                  const SavedPtrs& sv, const BwdWs& w, const bpt_grads& G, void* dX, float* ln_part,
                                  int64_t ln_part_n, hipStream_t s) {

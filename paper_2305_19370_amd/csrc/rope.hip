@@ -122,8 +122,9 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a, int rows_per) {
   }
 }
 
-// Feature-major, in place (the layer's saved projection and its gradient): a thread turns 8 consecutive tokens of one pair in every
-// head, its cosines and sines formed once.
+// Feature-major, in place (the gradient of a layer's projection, without a window): a thread turns 8 consecutive tokens of one pair in every
+// head, its cosines and sines formed once. 16384 tokens, 32 heads of 128, bf16 48 us (token-major 45); 2048 tokens 22 (10), 64 workgroups
+// of pairs by 1 of tokens, each a chain over the heads.
 template <typename T>
 __global__ __launch_bounds__(256) void rope_t_kernel(RopeArgs a, int64_t Sp) {
   const int i = blockIdx.y, pairs = a.rot / 2;

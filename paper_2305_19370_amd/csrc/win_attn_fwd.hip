@@ -7,8 +7,11 @@ namespace bpt {
 // r = token * G + head, so its maximum and sum are register reductions and one exchange), P^T straight from the accumulators into
 // O^T += V^T P^T. NW waves of 32 rows share the K and V tiles of an LDS ring. The scores are scaled
 // in fp32 (the FMA that subtracts the reference), so q is used as it is.
-// 16384 tokens, 16 heads of 128, 8 key heads, window 4096: 510 us, 955 TFLOP/s (full attention of 32768 tokens, 32 heads: 8.5 ms,
-// 1030; heads of 64, 16 of them: 2.7-3.0 ms, 730-820). Bound by issue: beside 32 MFMAs a tile costs a wave 32 exponentials, FMAs, sums,
+// Weights are rounded to bf16 where they become an MFMA's operand, as in the layer's attention: products of fp32 operands run at a
+// sixteenth of the rate. The sum that divides them stays fp32 and unrounded. Outputs are 2.2e-3 off (fp32 weights and the output's own
+// rounding: 1.6e-3).
+// 16384 tokens, 16 heads of 128, 8 key heads, window 4096: 502 us, 970 TFLOP/s (full attention of 32768 tokens, 32 heads: 8.5-8.7 ms,
+// 1010-1030; heads of 64, 16 of them: 2.7-3.0 ms, 730-820). Bound by issue: beside 32 MFMAs a tile costs a wave 32 exponentials, FMAs, sums,
 // maxima and 16 conversions, and as many LDS fragments. Window 1024, 8192 tokens: 94 us, 690, tiles at both ends of the
 // window half used and a workgroup's start and end for 18 tiles.
 // Two stages for 4 waves: heads of 64 then have three workgroups on a CU (16384 tokens, window 2048: 211 -> 190 us).
