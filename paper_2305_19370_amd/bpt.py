@@ -574,9 +574,11 @@ def _rope_layout(cfg: bytes):
 
 def _check_rows(t: torch.Tensor, layout, name: str) -> None:
     """Raises unless a tensor holds a configuration's rows: its last dimensions are one row's heads (and what follows them there)
-    and its first ones count the rows, or it is a flat buffer of them."""
+    and its first ones count the rows, or it is a buffer of them, flat or contiguous and just as long."""
     dtype, (rows, H, dh), (ld, _, _) = layout
     if t.dtype == dtype:
+        if t.numel() == rows * ld and t.is_contiguous():
+            return
         dims = [(n, st) for n, st in zip(t.shape, t.stride()) if n != 1]
         if len(dims) == 1 and dims[0][1] == 1 and dims[0][0] >= (rows - 1) * ld + H * dh:
             return

@@ -84,6 +84,7 @@ def rope_cfg(**kw):
 GOOD = [
     lambda: torch.empty(12, 2, 64, dtype=BF), lambda: torch.empty(12, 128, dtype=BF), lambda: torch.empty(3, 4, 2, 64, dtype=BF),
     lambda: torch.empty(3, 4, 128, dtype=BF), lambda: torch.empty(12 * 128, dtype=BF), lambda: torch.empty(3, 4, 1, 2, 64, dtype=BF),
+    lambda: torch.empty(3, 4 * 128, dtype=BF), lambda: torch.empty(6, 256, dtype=BF),   # rows side by side
 ]
 WIDE = [
     lambda: torch.empty(12, 400, dtype=BF), lambda: torch.empty(12, 400, dtype=BF)[:, :128].view(12, 2, 64),
