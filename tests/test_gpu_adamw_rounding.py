@@ -83,6 +83,33 @@ def test_tiny_second_moments_byte_for_byte():
             assert torch.equal(a[k], b[k]), (step, k, int((a[k] != b[k]).sum()))
 
 
+def test_moments_of_every_size_byte_for_byte():
+    """Blocks from 1e-22 to 1e17, within a block elements from 1e-8 of the largest up, and zeros: m from its least block scale on, r
+    from squares below fp32's normal numbers to near its largest."""
+    case = dict(plain.ADAMW, tensors="layers", L=1, D=264, F=1055, V=501, bits=8)
+    a, b = (plain.prepare(case, 7) for _ in range(2))
+    plan = plain._plan(b)
+    n = a["g"].numel()
+    real = (a["p"] != 0).float()
+    for s in (a, b):
+        for k in ("m", "r", "exps"):
+            s[k].zero_()
+    gen = torch.Generator(device="cuda").manual_seed(2)
+    u = lambda *s: torch.rand(*s, generator=gen, device="cuda")  # noqa: E731
+    for step in range(1, 13):
+        size = 10.0 ** (39.0 * u(n // 256, 1) - 22.0) * 10.0 ** (-8.0 * u(n // 256, 256)) * (u(n // 256, 256) > 0.1)
+        g = (torch.randn(n // 256, 256, generator=gen, device="cuda") * size).view(-1) * real
+        for s in (a, b):
+            s["g"].copy_(g)
+            s["step"] = step
+        plain._run_adamw(a)
+        bpt.adamw_multi(plan, step, plain.LR, plain.B1, plain.B2, plain.EPS, seed=plain.SEED)
+        torch.cuda.synchronize()
+        for k in ("m", "r", "exps"):
+            assert torch.equal(a[k], b[k]), (step, k, int((a[k] != b[k]).sum()))
+        assert bool(torch.isfinite(b["p"]).all())
+
+
 def make(sizes, bits, seed):
     g = torch.Generator(device="cuda").manual_seed(seed)
     rn = lambda n, s: torch.randn(n, generator=g, device="cuda") * s  # noqa: E731
