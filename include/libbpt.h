@@ -453,6 +453,51 @@ typedef struct {
  * other of their buffers (the p are checked). */
 bpt_status bpt_adamw_multi(const bpt_adamw_multi_config* cfg, const bpt_adamw_tensor* tensors, int64_t count, void* stream);
 
+/* ------------------------------------------------------------------ linear time
+ * What a GPT takes whose cost per token is not to grow with the context: a mixer of the sequence with a state of fixed size,
+ * and a loss that teaches it what a model with attention answers. Same conventions as above. */
+
+/* Gated linear recurrence, per channel d of [B, S, D]:
+ *     a_t = exp(-c softplus(lambda) sigmoid(r_t)),   h_t = a_t h_{t-1} + sqrt(1 - a_t^2) sigmoid(i_t) x_t,   y_t = h_t
+ * x the input, r and i the two gates before their sigmoid (say, three projections of one activation). Element (b, t, d) of a
+ * tensor is at b sb + t st + d. Gates, states and sums are held in fp32, 1 - a^2 without cancellation; y is rounded once.
+ * A sequence may be shorter than S (lens): behind its length y and the gradients are 0, whatever the inputs hold there, and
+ * its last state is that of its last step (h0 if it has none). */
+typedef struct {
+  int64_t sb, st;        /* elements between sequences and tokens; multiples of 16 bytes       */
+} bpt_recur_strides;
+
+typedef struct {
+  int64_t B, S, D;       /* sequences, steps, channels (a multiple of 8)                        */
+  bpt_recur_strides x, r, i, y;   /* x (and dx), r (and dr), i (and di), y (and dy)             */
+  float c;               /* > 0; e.g. 8                                                         */
+  int32_t dtype;         /* bpt_dtype of x, r, i, y and their gradients                         */
+  int64_t reserved;      /* 0                                                                   */
+} bpt_recur_config;
+
+bpt_status bpt_recur_validate(const bpt_recur_config* cfg);
+
+/* What the forward keeps for the backward: the states before steps 128, 256, .. (fp32 [B, (S - 1) / 128, D]), 0 bytes for
+ * S <= 128. And the workspace of bpt_recur_fwd (backward = 0) or bpt_recur_bwd (backward = 1). 0 for an invalid configuration.
+ * Host-only. */
+size_t bpt_recur_saved_bytes(const bpt_recur_config* cfg);
+size_t bpt_recur_workspace_bytes(const bpt_recur_config* cfg, int backward);
+
+/* Forward. lambda [D] fp32; lens [B] int32 (clamped to [0, S]) or NULL: all of S; h0 [B, D] fp32, the states before the first
+ * step, or NULL: zeros; hT [B, D] fp32, gets the last states, or NULL. hT may be h0: a serving loop
+ * calls with S = 1 and updates its states in place. saved: bpt_recur_saved_bytes, or NULL without a backward. y must not
+ * alias an input. */
+bpt_status bpt_recur_fwd(const bpt_recur_config* cfg, const void* x, const void* r, const void* i, const float* lambda,
+                         const int32_t* lens, const float* h0, void* y, float* hT, void* saved, void* workspace,
+                         size_t workspace_bytes, void* stream);
+
+/* Backward for upstream gradients dy and dhT (of the last states, [B, D] fp32, or NULL: zeros), with the inputs, lens and h0 of
+ * the forward and what it saved. Writes dx, dr, di, and unless NULL dlambda [D] and dh0 [B, D] (fp32; dh0 may be dhT). All are
+ * OVERWRITTEN and alias no input but that. Sums are taken in a fixed order. */
+bpt_status bpt_recur_bwd(const bpt_recur_config* cfg, const void* x, const void* r, const void* i, const float* lambda,
+                         const int32_t* lens, const float* h0, const void* saved, const void* dy, const float* dhT, void* dx,
+                         void* dr, void* di, float* dlambda, float* dh0, void* workspace, size_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

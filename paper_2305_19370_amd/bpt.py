@@ -93,6 +93,15 @@ class AttnConfig(ctypes.Structure):
                 ("causal", c_i32), ("dtype", c_i32), ("reserved", c_i32)]
 
 
+class RecurStrides(ctypes.Structure):
+    _fields_ = [("sb", c_i64), ("st", c_i64)]
+
+
+class RecurConfig(ctypes.Structure):
+    _fields_ = [("B", c_i64), ("S", c_i64), ("D", c_i64), ("x", RecurStrides), ("r", RecurStrides), ("i", RecurStrides),
+                ("y", RecurStrides), ("c", c_f32), ("dtype", c_i32), ("reserved", c_i64)]
+
+
 class AdamWTensor(ctypes.Structure):
     _fields_ = [("n", c_i64), ("p", c_vp), ("g", c_vp), ("m", c_vp), ("v", c_vp), ("exps", c_vp), ("p_lowp", c_vp),
                 ("weight_decay", c_f64)]
@@ -110,7 +119,8 @@ EXPORTS = ("bpt_validate", "bpt_group_rows", "bpt_saved_bytes", "bpt_saved_layou
            "bpt_ln_fwd", "bpt_ln_bwd", "bpt_adamw_step", "bpt_bwd_qkv_grad_offset",
            "bpt_layer_fwd_noalloc", "bpt_rope_validate", "bpt_rope_fwd", "bpt_rope_bwd", "bpt_attn_validate",
            "bpt_attn_workspace_bytes", "bpt_attn_fwd", "bpt_attn_bwd", "bpt_adamw_multi", "bpt_layer_options_validate",
-           "bpt_layer_fwd_options", "bpt_layer_bwd_options")
+           "bpt_layer_fwd_options", "bpt_layer_bwd_options", "bpt_recur_validate", "bpt_recur_saved_bytes",
+           "bpt_recur_workspace_bytes", "bpt_recur_fwd", "bpt_recur_bwd")
 
 _lib = None
 
@@ -194,6 +204,16 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.bpt_layer_bwd_options.restype = c_i32
     lib.bpt_adamw_multi.argtypes = [P(AdamWMultiConfig), P(AdamWTensor), c_i64, c_vp]
     lib.bpt_adamw_multi.restype = c_i32
+    lib.bpt_recur_validate.argtypes = [P(RecurConfig)]
+    lib.bpt_recur_validate.restype = c_i32
+    lib.bpt_recur_saved_bytes.argtypes = [P(RecurConfig)]
+    lib.bpt_recur_saved_bytes.restype = c_sz
+    lib.bpt_recur_workspace_bytes.argtypes = [P(RecurConfig), c_i32]
+    lib.bpt_recur_workspace_bytes.restype = c_sz
+    lib.bpt_recur_fwd.argtypes = [P(RecurConfig)] + [c_vp] * 10 + [c_sz, c_vp]
+    lib.bpt_recur_fwd.restype = c_i32
+    lib.bpt_recur_bwd.argtypes = [P(RecurConfig)] + [c_vp] * 15 + [c_sz, c_vp]
+    lib.bpt_recur_bwd.restype = c_i32
     _lib = lib
     return lib
 
@@ -853,3 +873,147 @@ def adamw_multi(tensors: AdamWTensors, step: int, lr: float, beta1: float = 0.9,
     stream = _stream_on(tensors.device.index, True) if tensors.tensors else _stream()
     cfg = AdamWMultiConfig(lr, beta1, beta2, eps, step, seed & (2 ** 64 - 1), tensors.bits, tensors.grad_dtype, tensors.lowp_dtype, 0)
     _check(load().bpt_adamw_multi(ctypes.byref(cfg), tensors.array, len(tensors.tensors), stream))
+
+
+# ---------------------------------------------------------------- gated linear recurrence
+def recur_config_of(x: torch.Tensor, r: torch.Tensor, i: torch.Tensor, y: torch.Tensor, c: float = 8.0) -> RecurConfig:
+    """The configuration of a recurrence over [B, S, D] tensors of any strides with adjacent channels; see include/libbpt.h."""
+    if x.dim() != 3 or r.shape != x.shape or i.shape != x.shape or y.shape != x.shape:
+        raise ValueError("x, r, i and y are [B, S, D], all the same")
+    if x.dtype not in (torch.float32, torch.bfloat16) or not (x.dtype == r.dtype == i.dtype == y.dtype):
+        raise ValueError("x, r, i and y must share a type, float32 or bfloat16")
+    B, S, D = x.shape
+    unit = 16 // x.element_size()
+
+    def strides(t: torch.Tensor) -> RecurStrides:
+        sb, st, sd = t.stride()
+        if sd != 1 and D > 1:
+            raise ValueError("channels must be adjacent")
+        # the stride of a dimension of one element counts for nothing
+        return RecurStrides(sb if B > 1 else 0, st if S > 1 else (D + unit - 1) // unit * unit)
+
+    return RecurConfig(B, S, D, strides(x), strides(r), strides(i), strides(y), c, BPT_BF16 if x.dtype == torch.bfloat16 else BPT_F32, 0)
+
+
+def recur_validate(cfg: RecurConfig) -> int:
+    return load().bpt_recur_validate(ctypes.byref(cfg))
+
+
+def recur_saved_bytes(cfg: RecurConfig) -> int:
+    return load().bpt_recur_saved_bytes(ctypes.byref(cfg))
+
+
+def recur_workspace_bytes(cfg: RecurConfig, backward: bool) -> int:
+    return load().bpt_recur_workspace_bytes(ctypes.byref(cfg), int(backward))
+
+
+@functools.lru_cache(maxsize=1024)
+def _recur_layout(cfg: bytes):
+    """(type, shape, strides) that a configuration gives x, r, i and y."""
+    c = RecurConfig.from_buffer_copy(cfg)
+    return tuple((_TORCH_DT.get(c.dtype), (c.B, c.S, c.D), (s.sb, s.st, 1)) for s in (c.x, c.r, c.i, c.y))
+
+
+def _f32(t: Optional[torch.Tensor], shape: Tuple[int, ...], name: str) -> Optional[int]:
+    """The address of contiguous float32 of a shape, or None."""
+    if t is None:
+        return None
+    if t.dtype != torch.float32 or tuple(t.shape) != shape or not t.is_contiguous():
+        raise ValueError(f"{name} must be {list(shape)} contiguous float32, not {list(t.shape)} of {t.dtype}")
+    return t.data_ptr()
+
+
+def _nbytes(t: Optional[torch.Tensor]) -> int:
+    return 0 if t is None else t.numel() * t.element_size()
+
+
+def _saved_ptr(t: Optional[torch.Tensor], need: int) -> Optional[int]:
+    if t is not None and (not t.is_contiguous() or _nbytes(t) < need):
+        raise ValueError(f"saved must be {need} contiguous bytes, not {_nbytes(t)}")
+    return t.data_ptr() if need and t is not None else None
+
+
+def recur_fwd(cfg: RecurConfig, x: torch.Tensor, r: torch.Tensor, i: torch.Tensor, lam: torch.Tensor, y: torch.Tensor,
+              h0: Optional[torch.Tensor] = None, hT: Optional[torch.Tensor] = None, saved: Optional[torch.Tensor] = None,
+              workspace: Optional[torch.Tensor] = None, lens: Optional[torch.Tensor] = None) -> None:
+    """Every tensor has the shape, strides and type that cfg gives it. hT may be h0."""
+    for t, at, name in zip((x, r, i, y), _recur_layout(bytes(cfg)), "xriy"):
+        if (t.dtype, t.shape, t.stride()) != at:
+            _check_layout(t, at, name)
+    B, D = cfg.B, cfg.D
+    lp, h0p, hTp = _f32(lam, (D,), "lam"), _f32(h0, (B, D), "h0"), _f32(hT, (B, D), "hT")
+    dev, nb = x.get_device(), _nbytes(workspace)
+    same = all(t is None or t.get_device() == dev for t in (r, i, lam, y, h0, hT, saved, workspace, lens))
+    stream = _stream_on(dev, same)
+    _check(load().bpt_recur_fwd(cfg, x.data_ptr(), r.data_ptr(), i.data_ptr(), lp, _int32(lens, B, "lens"), h0p, y.data_ptr(), hTp,
+                                None if saved is None else _saved_ptr(saved, recur_saved_bytes(cfg)),
+                                workspace.data_ptr() if nb else None, nb, stream))
+
+
+def recur_bwd(cfg: RecurConfig, x: torch.Tensor, r: torch.Tensor, i: torch.Tensor, lam: torch.Tensor, saved: Optional[torch.Tensor],
+              dy: torch.Tensor, dx: torch.Tensor, dr: torch.Tensor, di: torch.Tensor, workspace: torch.Tensor,
+              dlam: Optional[torch.Tensor] = None, h0: Optional[torch.Tensor] = None, dhT: Optional[torch.Tensor] = None,
+              dh0: Optional[torch.Tensor] = None, lens: Optional[torch.Tensor] = None) -> None:
+    """Every tensor has the shape, strides and type that cfg gives it: dx, dr and di those of x, r and i, dy those of y. dh0 may
+    be dhT."""
+    at = _recur_layout(bytes(cfg))
+    for t, lay, name in zip((x, r, i, dy, dx, dr, di), at + at[:3], ("x", "r", "i", "dy", "dx", "dr", "di")):
+        if (t.dtype, t.shape, t.stride()) != lay:
+            _check_layout(t, lay, name)
+    B, D = cfg.B, cfg.D
+    lp, dlp = _f32(lam, (D,), "lam"), _f32(dlam, (D,), "dlam")
+    h0p, dhTp, dh0p = _f32(h0, (B, D), "h0"), _f32(dhT, (B, D), "dhT"), _f32(dh0, (B, D), "dh0")
+    dev = x.get_device()
+    same = all(t is None or t.get_device() == dev for t in (r, i, lam, saved, dy, dx, dr, di, workspace, dlam, h0, dhT, dh0, lens))
+    stream = _stream_on(dev, same)
+    _check(load().bpt_recur_bwd(cfg, x.data_ptr(), r.data_ptr(), i.data_ptr(), lp, _int32(lens, B, "lens"), h0p,
+                                _saved_ptr(saved, recur_saved_bytes(cfg)), dy.data_ptr(), dhTp, dx.data_ptr(), dr.data_ptr(),
+                                di.data_ptr(), dlp, dh0p, workspace.data_ptr(), _nbytes(workspace), stream))
+
+
+class GatedRecurrence:
+    """A gated linear recurrence through libbpt; allocates its buffers with torch. For one new token of each sequence, call
+    forward with S = 1 and the states as h0."""
+
+    def __init__(self, c: float = 8.0):
+        self.c = c
+
+    @staticmethod
+    def _bytes(n: int, device) -> torch.Tensor:
+        return torch.empty(max(n, 256), dtype=torch.uint8, device=device)
+
+    def forward(self, x: torch.Tensor, r: torch.Tensor, i: torch.Tensor, lam: torch.Tensor, h0: Optional[torch.Tensor] = None,
+                lens: Optional[torch.Tensor] = None,
+                save: bool = False) -> Tuple[torch.Tensor, torch.Tensor, Optional[torch.Tensor]]:
+        """y [B, S, D], the last states [B, D] (float32), and with `save` what backward takes."""
+        y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        cfg = recur_config_of(x, r, i, y, self.c)
+        hT = torch.empty((cfg.B, cfg.D), dtype=torch.float32, device=x.device)
+        saved = self._bytes(recur_saved_bytes(cfg), x.device) if save else None
+        nb = recur_workspace_bytes(cfg, False)
+        recur_fwd(cfg, x, r, i, lam, y, h0, hT, saved, self._bytes(nb, x.device) if nb else None, lens)
+        return y, hT, saved
+
+    def backward(self, x: torch.Tensor, r: torch.Tensor, i: torch.Tensor, lam: torch.Tensor, saved: torch.Tensor, dy: torch.Tensor,
+                 dhT: Optional[torch.Tensor] = None, h0: Optional[torch.Tensor] = None,
+                 lens: Optional[torch.Tensor] = None) -> Dict[str, torch.Tensor]:
+        """dx, dr, di, dlam and dh0; x, r, i, lam, h0 and lens as they were, saved from forward. Gradients of columns of one
+        projection are columns of one tensor, those of a tensor without gaps are laid out like it, others are contiguous (and
+        their input is copied)."""
+        if dy.dim() != 3 or dy.shape != x.shape or dy.dtype != x.dtype:
+            raise ValueError(f"dy must be {tuple(x.shape)} of {x.dtype}, not {tuple(dy.shape)} of {dy.dtype}")
+        unit = 16 // dy.element_size()
+        if dy.stride(2) != 1 or any(n > 1 and st % unit for n, st in zip(dy.shape[:2], dy.stride())) or dy.data_ptr() % 16:
+            dy = dy.contiguous()
+        four = tuple(t.unsqueeze(2) for t in (x, r, i))
+        grads = _side_by_side(four)
+        if grads is None:
+            x, r, i = (t if _apart(f) and _span(t) == t.numel() else t.contiguous() for t, f in zip((x, r, i), four))
+            grads = [torch.empty_strided(t.shape, t.stride(), dtype=t.dtype, device=t.device) for t in (x, r, i)]
+        else:
+            grads = [g.squeeze(2) for g in grads]
+        cfg = recur_config_of(x, r, i, dy, self.c)
+        dlam = torch.empty(cfg.D, dtype=torch.float32, device=x.device)
+        dh0 = torch.empty((cfg.B, cfg.D), dtype=torch.float32, device=x.device)
+        recur_bwd(cfg, x, r, i, lam, saved, dy, *grads, self._bytes(recur_workspace_bytes(cfg, True), x.device), dlam, h0, dhT, dh0, lens)
+        return dict(zip(("dx", "dr", "di"), grads), dlam=dlam, dh0=dh0)

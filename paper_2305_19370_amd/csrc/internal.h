@@ -160,6 +160,29 @@ hipError_t win_far_f32(const WinArgs& a, hipStream_t s);       // far slots
 hipError_t win_chunks(Dt t, const WinArgs& a, hipStream_t s);  // adds the chunks up
 hipError_t win_sinks(Dt t, const WinArgs& a, int slots, hipStream_t s);   // adds the slots up
 
+// ---------------------------------------------------------------- gated linear recurrence
+constexpr int kRecurCh = 64;            // channels of a workgroup
+constexpr int kRecurKeep = 128;         // steps between the states that the forward keeps
+// Element (b, t, d) of a tensor is at b * sb + t * st + d; dy is laid out like y, dx, dr and di like x, r and i.
+struct RecurArgs {
+  const void *x = nullptr, *r = nullptr, *i = nullptr, *dy = nullptr;
+  void *y = nullptr, *dx = nullptr, *dr = nullptr, *di = nullptr;
+  int64_t x_sb = 0, x_st = 0, r_sb = 0, r_st = 0, i_sb = 0, i_st = 0, y_sb = 0, y_st = 0;
+  const float* lam = nullptr;           // [D]
+  const float *h0 = nullptr, *dhT = nullptr;   // [B, D] or null: zeros
+  float *hT = nullptr, *dh0 = nullptr;  // [B, D] or null; may be h0, dhT
+  float* saved = nullptr;               // [B, (S - 1) / kRecurKeep, D]: the states before steps kRecurKeep, 2 kRecurKeep .., or null
+  const int32_t* lens = nullptr;        // [B] or null: all of S
+  float* part = nullptr;                // backward: [B, recur_bwd_chunks(S), D] sums of w
+  int64_t S = 0, nchunks = 0;           // nchunks, nct: the launcher's
+  int B = 0, D = 0, nct = 0;
+  float c = 0;
+};
+int64_t recur_bwd_chunks(int64_t S);
+hipError_t recur_fwd(Dt t, RecurArgs p, hipStream_t s);
+hipError_t recur_bwd(Dt t, RecurArgs p, hipStream_t s);
+hipError_t recur_dlam(const RecurArgs& p, float* dlam, hipStream_t s);
+
 // ---------------------------------------------------------------- rotary positions
 struct RopeArgs {
   const void* x = nullptr;

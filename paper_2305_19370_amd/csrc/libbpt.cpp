@@ -1756,4 +1756,119 @@ bpt_status bpt_adamw_multi(const bpt_adamw_multi_config* cfg, const bpt_adamw_te
   return BPT_OK;
 }
 
+// ---------------------------------------------------------------- gated linear recurrence
+static bpt_status recur_check(const bpt_recur_config* c) {
+  if (!c) return fail(BPT_ERR_INVALID_ARG, "config is NULL");
+  if (c->B < 1 || c->S < 1 || c->D < 1) return fail(BPT_ERR_INVALID_ARG, "B, S, D must be >= 1");
+  if (!(c->c > 0.0f) || !std::isfinite(c->c)) return fail(BPT_ERR_INVALID_ARG, "c must be > 0");
+  if (c->reserved != 0) return fail(BPT_ERR_INVALID_ARG, "reserved must be 0");
+  bpt_status st = dtype_ok(c->dtype, "dtype");
+  if (st != BPT_OK) return st;
+  const int64_t unit = 16 / (int64_t)esize(c->dtype);
+  for (const bpt_recur_strides* t : {&c->x, &c->r, &c->i, &c->y}) {
+    if (t->sb < 0 || t->st < 0) return fail(BPT_ERR_INVALID_ARG, "strides must be >= 0");
+    if (t->sb % unit || t->st % unit) return fail(BPT_ERR_INVALID_ARG, "strides must be multiples of 16 bytes");
+    if (t->sb >= (int64_t)1 << 40 || t->st >= (int64_t)1 << 40) return fail(BPT_ERR_UNSUPPORTED, "a stride is too large");
+  }
+  if (c->D % 8) return fail(BPT_ERR_UNSUPPORTED, "D must be a multiple of 8 (got %lld)", (long long)c->D);
+  if (c->S > kAttnMax || c->D > (int64_t)1 << 20) return fail(BPT_ERR_UNSUPPORTED, "S must be <= 2^28 and D <= 2^20");
+  // workgroups of a launch, 512 threads each
+  if (c->B > (int64_t)1 << 22 || c->B * ((c->D + kRecurCh - 1) / kRecurCh) > (int64_t)1 << 22)
+    return fail(BPT_ERR_UNSUPPORTED, "B * D too large");
+  if (!apart({c->y.sb, c->y.st, 0}, c->B, c->S, 1, c->D)) return fail(BPT_ERR_INVALID_ARG, "strides of y overlap");
+  return BPT_OK;
+}
+
+static int64_t recur_saved(const bpt_recur_config& c) { return c.B * ((c.S - 1) / kRecurKeep) * c.D * 4; }
+
+struct RecurWs {
+  float* part;           // backward: sums of w per chunk
+};
+static RecurWs recur_ws(const bpt_recur_config& c, void* base, int backward, int64_t* total) {
+  Bump bp(base);
+  RecurWs w{};
+  if (backward) w.part = (float*)bp.take(c.B * recur_bwd_chunks(c.S) * c.D * 4);
+  *total = rup(bp.off, kAlign);
+  return w;
+}
+
+static RecurArgs recur_args(const bpt_recur_config& c, const void* x, const void* r, const void* i, const float* lambda,
+                            const int32_t* lens, const float* h0, const void* saved) {
+  RecurArgs a;
+  a.x = x; a.r = r; a.i = i; a.lam = lambda; a.lens = lens; a.h0 = h0; a.saved = (float*)saved;
+  a.x_sb = c.x.sb; a.x_st = c.x.st; a.r_sb = c.r.sb; a.r_st = c.r.st;
+  a.i_sb = c.i.sb; a.i_st = c.i.st; a.y_sb = c.y.sb; a.y_st = c.y.st;
+  a.B = (int)c.B; a.S = c.S; a.D = (int)c.D; a.c = c.c;
+  return a;
+}
+
+bpt_status bpt_recur_validate(const bpt_recur_config* cfg) { return recur_check(cfg); }
+
+size_t bpt_recur_saved_bytes(const bpt_recur_config* cfg) { return recur_check(cfg) == BPT_OK ? (size_t)recur_saved(*cfg) : 0; }
+
+size_t bpt_recur_workspace_bytes(const bpt_recur_config* cfg, int backward) {
+  if (recur_check(cfg) != BPT_OK) return 0;
+  int64_t total;
+  recur_ws(*cfg, nullptr, backward, &total);
+  return (size_t)total;
+}
+
+bpt_status bpt_recur_fwd(const bpt_recur_config* cfg, const void* x, const void* r, const void* i, const float* lambda,
+                         const int32_t* lens, const float* h0, void* y, float* hT, void* saved, void* ws, size_t ws_bytes,
+                         void* stream) {
+  bpt_status st = recur_check(cfg);
+  if (st != BPT_OK) return st;
+  if (!x || !r || !i || !lambda || !y) return fail(BPT_ERR_INVALID_ARG, "NULL x, r, i, lambda or y");
+  if (y == x || y == r || y == i) return fail(BPT_ERR_INVALID_ARG, "y must not alias x, r or i");
+  for (const void* q : {x, r, i, (const void*)lambda, (const void*)lens, (const void*)h0, (const void*)y, (const void*)hT,
+                        (const void*)saved, (const void*)ws})
+    if (q && !aligned16(q)) return fail(BPT_ERR_INVALID_ARG, "pointer %p is not 16-byte aligned", q);
+  int64_t need;
+  recur_ws(*cfg, ws, 0, &need);
+  if (need > 0 && (!ws || (int64_t)ws_bytes < need))
+    return fail(BPT_ERR_WORKSPACE, "workspace %zu bytes < required %lld", ws ? ws_bytes : (size_t)0, (long long)need);
+  RecurArgs a = recur_args(*cfg, x, r, i, lambda, lens, h0, saved);
+  a.y = y; a.hT = hT;
+  hipStream_t s = (hipStream_t)stream;
+  const double n = (double)cfg->B * cfg->S * cfg->D;
+  RUN("recur.fwd", 20.0 * n, 4.0 * n * esize(cfg->dtype), recur_fwd(dt_of(cfg->dtype), a, s));
+  return BPT_OK;
+}
+
+bpt_status bpt_recur_bwd(const bpt_recur_config* cfg, const void* x, const void* r, const void* i, const float* lambda,
+                         const int32_t* lens, const float* h0, const void* saved, const void* dy, const float* dhT, void* dx,
+                         void* dr, void* di, float* dlambda, float* dh0, void* ws, size_t ws_bytes, void* stream) {
+  bpt_status st = recur_check(cfg);
+  if (st != BPT_OK) return st;
+  if (!x || !r || !i || !lambda || !dy || !dx || !dr || !di || !ws)
+    return fail(BPT_ERR_INVALID_ARG, "NULL x, r, i, lambda, dy, dx, dr, di or workspace");
+  if (!saved && recur_saved(*cfg) > 0) return fail(BPT_ERR_INVALID_ARG, "NULL saved");
+  const void* in[] = {x, r, i, lambda, lens, h0, saved, dy, ws};
+  void* out[] = {dx, dr, di, dlambda, dh0};
+  for (const void* q : in)
+    if (q && !aligned16(q)) return fail(BPT_ERR_INVALID_ARG, "pointer %p is not 16-byte aligned", q);
+  if (!aligned16(dhT)) return fail(BPT_ERR_INVALID_ARG, "pointer %p is not 16-byte aligned", (const void*)dhT);
+  for (int k = 0; k < 5; ++k) {
+    if (!out[k]) continue;
+    if (!aligned16(out[k])) return fail(BPT_ERR_INVALID_ARG, "pointer %p is not 16-byte aligned", out[k]);
+    for (const void* q : in)
+      if (q == out[k]) return fail(BPT_ERR_INVALID_ARG, "gradients must not alias an input");
+    if (k < 4 && out[k] == (const void*)dhT) return fail(BPT_ERR_INVALID_ARG, "gradients must not alias an input");
+    for (int j = 0; j < k; ++j)
+      if (out[j] == out[k]) return fail(BPT_ERR_INVALID_ARG, "gradients must not alias one another");
+  }
+  for (const bpt_recur_strides* t : {&cfg->x, &cfg->r, &cfg->i})
+    if (!apart({t->sb, t->st, 0}, cfg->B, cfg->S, 1, cfg->D)) return fail(BPT_ERR_INVALID_ARG, "strides of dx, dr or di overlap");
+  int64_t need;
+  const RecurWs w = recur_ws(*cfg, ws, 1, &need);
+  if ((int64_t)ws_bytes < need) return fail(BPT_ERR_WORKSPACE, "workspace %zu bytes < required %lld", ws_bytes, (long long)need);
+  RecurArgs a = recur_args(*cfg, x, r, i, lambda, lens, h0, saved);
+  a.dy = dy; a.dhT = dhT; a.dx = dx; a.dr = dr; a.di = di; a.dh0 = dh0; a.part = w.part;
+  hipStream_t s = (hipStream_t)stream;
+  const double n = (double)cfg->B * cfg->S * cfg->D;
+  RUN("recur.bwd", 35.0 * n, 7.0 * n * esize(cfg->dtype), recur_bwd(dt_of(cfg->dtype), a, s));
+  if (dlambda) RUN("recur.dlambda", 0, (double)cfg->B * recur_bwd_chunks(cfg->S) * cfg->D * 4, recur_dlam(a, dlambda, s));
+  return BPT_OK;
+}
+
 }  // extern "C"
