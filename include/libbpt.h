@@ -498,6 +498,47 @@ bpt_status bpt_recur_bwd(const bpt_recur_config* cfg, const void* x, const void*
                          const int32_t* lens, const float* h0, const void* saved, const void* dy, const float* dhT, void* dx,
                          void* dr, void* di, float* dlambda, float* dh0, void* workspace, size_t workspace_bytes, void* stream);
 
+/* Distillation of a language-model head from a teacher's largest logits, blockwise over tokens like bpt_xent_*: the [T, V]
+ * logits never exist at once. Token t has the student's logits z = h W and a list of K pairs of the teacher, values v_j
+ * and vocabulary indices k_j in any order:
+ *     q = softmax(v / tau) over the list,   p_tau = softmax(z / tau) over the vocabulary
+ *     kl_t = sum_j q_j log(q_j / p_tau[k_j]),   ce_t = -log p_1[y_t]
+ *     loss = sum_t w_t (soft tau^2 kl_t + hard ce_t)
+ * An entry whose index lies outside [0, V) or whose value is -inf is left out (a list may be shorter than K); an index that is
+ * given twice counts with the sum of its probabilities; a token without entries has kl_t = 0, one whose target lies outside
+ * [0, V) ce_t = 0. A token of weight 0, or that has neither, is left out of losses and gradients whatever its row of h holds
+ * (its own row of dh is 0). Logits, sums and losses are fp32; the gradient of the logits is rounded to cfg->dtype as the operand of
+ * dh = G W^T and dW = h^T G. */
+typedef struct {
+  int64_t T, D, V, K;    /* tokens, hidden width, vocabulary, pairs of a list (<= 256)           */
+  int64_t ldw;           /* columns of W as stored, as in bpt_xent_config                       */
+  int64_t block_rows;    /* tokens whose logits are live at once; 0 = automatic (8192)          */
+  float tau;             /* temperature, > 0                                                    */
+  float soft, hard;      /* >= 0; hard = 0: no targets                                          */
+  int32_t dtype;         /* bpt_dtype of h, W and dh                                            */
+  int32_t grad_dtype;    /* bpt_dtype of dW (BPT_BF16 with dtype BPT_BF16 only)                 */
+  int32_t reserved;      /* 0                                                                   */
+} bpt_distill_config;
+
+bpt_status bpt_distill_validate(const bpt_distill_config* cfg);
+
+/* What the forward keeps for the backward (lists sorted by index, their probabilities and logits, row statistics: 12 bytes a
+ * pair and 36 a token); workspace of bpt_distill_fwd (backward = 0) or bpt_distill_bwd (1). 0 for an invalid configuration. Host-only. */
+size_t bpt_distill_saved_bytes(const bpt_distill_config* cfg);
+size_t bpt_distill_workspace_bytes(const bpt_distill_config* cfg, int backward);
+
+/* Forward. values [T, K] fp32, index [T, K] int32; targets [T] int32 if hard > 0, else not read; weights [T] fp32 or NULL: 1/T
+ * each. Writes loss: three floats, the loss, sum w kl and sum w ce; tokens [2, T] fp32: kl_t, then ce_t (0 for a token of weight
+ * 0); saved. */
+bpt_status bpt_distill_fwd(const bpt_distill_config* cfg, const void* h, const void* W, const float* values, const int32_t* index,
+                           const int32_t* targets, const float* weights, float* loss, float* tokens, void* saved, void* workspace,
+                           size_t workspace_bytes, void* stream);
+
+/* Backward for an upstream gradient dloss of the loss (host scalar), with the forward's h, W and saved: dh [T, D] in cfg->dtype and,
+ * unless NULL, dW [D, ldw] in cfg->grad_dtype (columns from V on get 0). Both are OVERWRITTEN. */
+bpt_status bpt_distill_bwd(const bpt_distill_config* cfg, const void* h, const void* W, const void* saved, float dloss, void* dh,
+                           void* dW, void* workspace, size_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

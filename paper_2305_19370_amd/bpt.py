@@ -102,6 +102,11 @@ class RecurConfig(ctypes.Structure):
                 ("y", RecurStrides), ("c", c_f32), ("dtype", c_i32), ("reserved", c_i64)]
 
 
+class DistillConfig(ctypes.Structure):
+    _fields_ = [("T", c_i64), ("D", c_i64), ("V", c_i64), ("K", c_i64), ("ldw", c_i64), ("block_rows", c_i64), ("tau", c_f32),
+                ("soft", c_f32), ("hard", c_f32), ("dtype", c_i32), ("grad_dtype", c_i32), ("reserved", c_i32)]
+
+
 class AdamWTensor(ctypes.Structure):
     _fields_ = [("n", c_i64), ("p", c_vp), ("g", c_vp), ("m", c_vp), ("v", c_vp), ("exps", c_vp), ("p_lowp", c_vp),
                 ("weight_decay", c_f64)]
@@ -120,7 +125,8 @@ EXPORTS = ("bpt_validate", "bpt_group_rows", "bpt_saved_bytes", "bpt_saved_layou
            "bpt_layer_fwd_noalloc", "bpt_rope_validate", "bpt_rope_fwd", "bpt_rope_bwd", "bpt_attn_validate",
            "bpt_attn_workspace_bytes", "bpt_attn_fwd", "bpt_attn_bwd", "bpt_adamw_multi", "bpt_layer_options_validate",
            "bpt_layer_fwd_options", "bpt_layer_bwd_options", "bpt_recur_validate", "bpt_recur_saved_bytes",
-           "bpt_recur_workspace_bytes", "bpt_recur_fwd", "bpt_recur_bwd")
+           "bpt_recur_workspace_bytes", "bpt_recur_fwd", "bpt_recur_bwd", "bpt_distill_validate", "bpt_distill_saved_bytes",
+           "bpt_distill_workspace_bytes", "bpt_distill_fwd", "bpt_distill_bwd")
 
 _lib = None
 
@@ -214,6 +220,16 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.bpt_recur_fwd.restype = c_i32
     lib.bpt_recur_bwd.argtypes = [P(RecurConfig)] + [c_vp] * 15 + [c_sz, c_vp]
     lib.bpt_recur_bwd.restype = c_i32
+    lib.bpt_distill_validate.argtypes = [P(DistillConfig)]
+    lib.bpt_distill_validate.restype = c_i32
+    lib.bpt_distill_saved_bytes.argtypes = [P(DistillConfig)]
+    lib.bpt_distill_saved_bytes.restype = c_sz
+    lib.bpt_distill_workspace_bytes.argtypes = [P(DistillConfig), c_i32]
+    lib.bpt_distill_workspace_bytes.restype = c_sz
+    lib.bpt_distill_fwd.argtypes = [P(DistillConfig)] + [c_vp] * 10 + [c_sz, c_vp]
+    lib.bpt_distill_fwd.restype = c_i32
+    lib.bpt_distill_bwd.argtypes = [P(DistillConfig)] + [c_vp] * 3 + [c_f32] + [c_vp] * 3 + [c_sz, c_vp]
+    lib.bpt_distill_bwd.restype = c_i32
     _lib = lib
     return lib
 
@@ -1017,3 +1033,89 @@ class GatedRecurrence:
         dh0 = torch.empty((cfg.B, cfg.D), dtype=torch.float32, device=x.device)
         recur_bwd(cfg, x, r, i, lam, saved, dy, *grads, self._bytes(recur_workspace_bytes(cfg, True), x.device), dlam, h0, dhT, dh0, lens)
         return dict(zip(("dx", "dr", "di"), grads), dlam=dlam, dh0=dh0)
+
+
+# ---------------------------------------------------------------- distillation from a teacher's largest logits
+def make_distill_config(T: int, D: int, V: int, K: int, ldw: Optional[int] = None, block_rows: int = 0, tau: float = 1.0,
+                        soft: float = 1.0, hard: float = 0.0, dtype: str = "bf16", grad_dtype: str = "f32") -> DistillConfig:
+    """T tokens of width D, V logits, lists of K; see include/libbpt.h."""
+    return DistillConfig(T, D, V, K, ldw if ldw is not None else (V + 63) // 64 * 64, block_rows, tau, soft, hard, _DT[dtype],
+                         _DT[grad_dtype], 0)
+
+
+def distill_validate(cfg: DistillConfig) -> int:
+    return load().bpt_distill_validate(ctypes.byref(cfg))
+
+
+def distill_saved_bytes(cfg: DistillConfig) -> int:
+    return load().bpt_distill_saved_bytes(ctypes.byref(cfg))
+
+
+def distill_workspace_bytes(cfg: DistillConfig, backward: bool) -> int:
+    return load().bpt_distill_workspace_bytes(ctypes.byref(cfg), int(backward))
+
+
+def _dense(t: Optional[torch.Tensor], dtype: torch.dtype, shape: Tuple[int, ...], name: str) -> Optional[int]:
+    """The address of a contiguous tensor of a type and shape, or None."""
+    if t is None:
+        return None
+    if t.dtype != dtype or tuple(t.shape) != shape or not t.is_contiguous():
+        raise ValueError(f"{name} must be {list(shape)} contiguous {dtype}, not {list(t.shape)} of {t.dtype}")
+    return t.data_ptr()
+
+
+def distill_fwd(cfg: DistillConfig, h: torch.Tensor, W: torch.Tensor, values: torch.Tensor, index: torch.Tensor, loss: torch.Tensor,
+                tokens: torch.Tensor, saved: torch.Tensor, workspace: torch.Tensor, targets: Optional[torch.Tensor] = None,
+                weights: Optional[torch.Tensor] = None) -> None:
+    T, D, K, dt = cfg.T, cfg.D, cfg.K, _TORCH_DT.get(cfg.dtype)
+    ptrs = (_dense(h, dt, (T, D), "h"), _dense(W, dt, (D, cfg.ldw), "W"), _dense(values, torch.float32, (T, K), "values"),
+            _dense(index, torch.int32, (T, K), "index"), _dense(targets, torch.int32, (T,), "targets"),
+            _dense(weights, torch.float32, (T,), "weights"), _dense(loss, torch.float32, (3,), "loss"),
+            _dense(tokens, torch.float32, (2, T), "tokens"))
+    dev = h.get_device()
+    same = all(t is None or t.get_device() == dev for t in (W, values, index, targets, weights, loss, tokens, saved, workspace))
+    stream = _stream_on(dev, same)
+    _check(load().bpt_distill_fwd(cfg, *ptrs, _saved_ptr(saved, distill_saved_bytes(cfg)), workspace.data_ptr(), _nbytes(workspace),
+                                  stream))
+
+
+def distill_bwd(cfg: DistillConfig, h: torch.Tensor, W: torch.Tensor, saved: torch.Tensor, dloss: float, dh: torch.Tensor,
+                dW: Optional[torch.Tensor], workspace: torch.Tensor) -> None:
+    T, D, dt = cfg.T, cfg.D, _TORCH_DT.get(cfg.dtype)
+    hp, Wp = _dense(h, dt, (T, D), "h"), _dense(W, dt, (D, cfg.ldw), "W")
+    dhp, dWp = _dense(dh, dt, (T, D), "dh"), _dense(dW, _TORCH_DT.get(cfg.grad_dtype), (D, cfg.ldw), "dW")
+    dev = h.get_device()
+    same = all(t is None or t.get_device() == dev for t in (W, saved, dh, dW, workspace))
+    stream = _stream_on(dev, same)
+    _check(load().bpt_distill_bwd(cfg, hp, Wp, _saved_ptr(saved, distill_saved_bytes(cfg)), float(dloss), dhp, dWp,
+                                  workspace.data_ptr(), _nbytes(workspace), stream))
+
+
+class DistillLoss:
+    """Distillation loss of an LM head through libbpt; allocates its buffers with torch."""
+
+    def __init__(self, cfg: DistillConfig):
+        _check(distill_validate(cfg))
+        self.cfg = cfg
+
+    @staticmethod
+    def _bytes(n: int, device) -> torch.Tensor:
+        return torch.empty(max(n, 256), dtype=torch.uint8, device=device)
+
+    def forward(self, h: torch.Tensor, W: torch.Tensor, values: torch.Tensor, index: torch.Tensor, targets: Optional[torch.Tensor] = None,
+                weights: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor, torch.Tensor]:
+        """(loss, sum w kl, sum w ce) as three floats, kl and ce of each token [2, T], and what backward takes."""
+        c, dev = self.cfg, h.device
+        loss = torch.empty(3, dtype=torch.float32, device=dev)
+        tokens = torch.empty((2, c.T), dtype=torch.float32, device=dev)
+        saved = self._bytes(distill_saved_bytes(c), dev)
+        distill_fwd(c, h, W, values, index, loss, tokens, saved, self._bytes(distill_workspace_bytes(c, False), dev), targets, weights)
+        return loss, tokens, saved
+
+    def backward(self, h: torch.Tensor, W: torch.Tensor, saved: torch.Tensor, dloss: float = 1.0,
+                 want_dW: bool = True) -> Tuple[torch.Tensor, Optional[torch.Tensor]]:
+        c = self.cfg
+        dh = torch.empty(h.shape, dtype=h.dtype, device=h.device)
+        dW = torch.empty((c.D, c.ldw), dtype=_TORCH_DT[c.grad_dtype], device=h.device) if want_dW else None
+        distill_bwd(c, h, W, saved, dloss, dh, dW, self._bytes(distill_workspace_bytes(c, True), h.device))
+        return dh, dW

@@ -17,7 +17,7 @@ PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 SOURCES = ["libbpt.cpp", "gemm.hip", "attn_fwd.hip", "attn_bwd_dq.hip", "attn_bwd_dkdv.hip", "rowwise.hip", "gpt.hip", "dropout.hip",
-           "win_attn_fwd.hip", "win_attn_bwd.hip", "win_attn_f32.hip", "rope.hip", "adamw_multi.hip", "recur.hip"]
+           "win_attn_fwd.hip", "win_attn_bwd.hip", "win_attn_f32.hip", "rope.hip", "adamw_multi.hip", "recur.hip", "distill.hip"]
 # per-source code generation options: the attention kernels keep the accumulators of
 # their MFMAs in architectural VGPRs (the default placement copies them between the
 # register files every iteration)

@@ -1,0 +1,301 @@
+// Distillation of a language-model head from a teacher's largest logits: what stands around the products.
+// Token t has student logits z over the vocabulary and a list of (v_j, k_j); q = softmax(v / tau) over the list, p_tau =
+// softmax(z / tau):
+//   kl_t = sum_j q_j log(q_j / p_tau(k_j)),  ce_t = -log p_1(y_t),  loss = sum_t w_t (soft tau^2 kl_t + hard ce_t)
+//   d loss / d z = w (soft tau (p_tau - q) + hard (p_1 - onehot(y)))
+// The list (and the target, an entry of q = 0) is sorted by index first. The product that forms the logits then reduces them to
+// maximum and sums of 64 columns in its epilogue and picks the listed ones out (a table says which entries fall into which 64
+// columns), and its transposed repetition in the backward writes the gradient of a token without a list; the listed elements
+// are overwritten afterwards from the picked logits, so that p - q is rounded once.
+#include <algorithm>
+
+#include "common.h"
+#include "internal.h"
+
+namespace bpt {
+
+namespace {
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr int kPer = (kDistillMaxK + 1 + 63) / 64;   // entries of a lane
+constexpr int kNone = 0x7FFFFFFF;
+
+BPT_DEV float wave_max(float v) {
+#pragma unroll
+  for (int o = 32; o >= 1; o >>= 1) v = fmaxf(v, __shfl_xor(v, o, 64));
+  return v;
+}
+}  // namespace
+
+// One wave per token: valid entries sorted by index, an index that is given twice once with the sum of its probabilities; the
+// target's place among them; the token's factors. With seg, also how many entries lie before every 64 columns.
+// The order comes from counting smaller indices: K steps over LDS, 256 entries 4 times 256.
+__global__ __launch_bounds__(256) void distill_prep_kernel(DistillArgs a) {
+  __shared__ int skey[4][64 * kPer];
+  __shared__ float sq[4][64 * kPer];
+  const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
+  const int64_t t = (int64_t)blockIdx.x * 4 + wv;      // a wave past the end works on the last token and stores nothing
+  const bool real = t < a.T;
+  const int64_t tt = real ? t : a.T - 1;
+  const int K = a.K, K1 = a.K1;
+  int key[kPer];
+  float q[kPer], mx = -__builtin_inff();
+  const int y = a.targets ? a.targets[tt] : -1;
+  const bool has_y = y >= 0 && y < a.V;
+#pragma unroll
+  for (int e = 0; e < kPer; ++e) {
+    const int j = lane + 64 * e;
+    key[e] = kNone;
+    q[e] = -__builtin_inff();
+    if (j < K) {
+      const int k = a.index[tt * K + j];
+      const float v = a.values[tt * K + j];
+      if (k >= 0 && k < a.V && !(v == -__builtin_inff())) {
+        key[e] = k;
+        q[e] = v;
+        mx = fmaxf(mx, v);
+      }
+    } else if (j < K1 && has_y) {
+      key[e] = y;
+    }
+  }
+  mx = wave_max(mx);
+  float sum = 0.0f;
+  bool mine = false;
+#pragma unroll
+  for (int e = 0; e < kPer; ++e) {
+    const int j = lane + 64 * e;
+    const bool listed = j < K && key[e] != kNone;
+    q[e] = listed ? __builtin_amdgcn_exp2f((q[e] - mx) * a.scale) : 0.0f;
+    sum += q[e];
+    mine |= listed;
+  }
+  sum = warp_sum(sum);
+  const bool some = __any(mine);
+  const float inv = some ? 1.0f / sum : 0.0f;
+#pragma unroll
+  for (int e = 0; e < kPer; ++e) {
+    q[e] = q[e] * inv;
+    skey[wv][lane + 64 * e] = key[e];
+    sq[wv][lane + 64 * e] = q[e];
+  }
+  __syncthreads();
+  bool first[kPer];
+  float qs[kPer];
+#pragma unroll
+  for (int e = 0; e < kPer; ++e) first[e] = key[e] != kNone, qs[e] = 0.0f;
+  for (int i = 0; i < K1; ++i) {
+    const int k = skey[wv][i];
+    const float v = sq[wv][i];
+#pragma unroll
+    for (int e = 0; e < kPer; ++e) {
+      if (k == key[e]) {
+        qs[e] += v;
+        if (i < lane + 64 * e) first[e] = false;
+      }
+    }
+  }
+  __syncthreads();
+#pragma unroll
+  for (int e = 0; e < kPer; ++e)
+    if (!first[e]) skey[wv][lane + 64 * e] = kNone;
+  __syncthreads();
+  int rank[kPer], n = 0;
+#pragma unroll
+  for (int e = 0; e < kPer; ++e) rank[e] = 0;
+  for (int i = 0; i < K1; ++i) {
+    const int k = skey[wv][i];
+    n += k != kNone;
+#pragma unroll
+    for (int e = 0; e < kPer; ++e) rank[e] += k < key[e];
+  }
+  __syncthreads();
+#pragma unroll
+  for (int e = 0; e < kPer; ++e) {
+    if (!first[e]) continue;
+    skey[wv][rank[e]] = key[e];
+    if (real) {
+      a.sidx[t * K1 + rank[e]] = key[e];
+      a.sq[t * K1 + rank[e]] = qs[e];
+      if (a.targets && key[e] == y) a.ypos[t] = rank[e];
+    }
+  }
+  __syncthreads();
+  if (!real) return;
+  if (lane == 0) {
+    const float w = a.weights ? a.weights[t] : a.weight;
+    a.count[t] = n;
+    if (!has_y) a.ypos[t] = -1;
+    a.gs[t] = some ? w * a.soft * a.tau : 0.0f;
+    a.gh[t] = has_y ? w * a.hard : 0.0f;
+    a.w[t] = w;
+  }
+  if (a.seg) {
+    for (int g = lane; g <= a.ng; g += 64) {
+      int lo = 0, hi = n;                              // entries below 64 g
+      while (lo < hi) {
+        const int mid = (lo + hi) >> 1;
+        if (skey[wv][mid] < 64 * g) lo = mid + 1;
+        else hi = mid;
+      }
+      a.seg[(t - a.t0) * a.ldseg + g] = (uint16_t)lo;
+    }
+  }
+}
+
+namespace {
+// (m, l) of two sets: l = sum of 2^((z - m) s)
+BPT_DEV void join(float& m, float& l, float& l1, float m2, float l2, float l12, float s) {
+  const float M = fmaxf(m, m2);
+  if (M == -__builtin_inff()) return;
+  const float f = __builtin_amdgcn_exp2f((m - M) * s), f2 = __builtin_amdgcn_exp2f((m2 - M) * s);
+  const float g = __builtin_amdgcn_exp2f((m - M) * kLog2e), g2 = __builtin_amdgcn_exp2f((m2 - M) * kLog2e);
+  l = l * f + l2 * f2;
+  l1 = l1 * g + l12 * g2;
+  m = M;
+}
+
+// the token's log-sum-exps and losses, by its wave
+BPT_DEV void finish(const DistillArgs& a, int64_t t, int lane, float m, float l, float l1) {
+#pragma unroll
+  for (int o = 32; o >= 1; o >>= 1) join(m, l, l1, __shfl_xor(m, o, 64), __shfl_xor(l, o, 64), __shfl_xor(l1, o, 64), a.scale);
+  const float lt = m / a.tau + logf(l), lo = a.two ? m + logf(l1) : lt;
+  float kl = 0.0f;
+  for (int j = lane; j < a.count[t]; j += 64) {
+    const float q = a.sq[t * a.K1 + j];
+    if (q != 0.0f) kl += q * (logf(q) - a.sz[t * a.K1 + j] / a.tau + lt);
+  }
+  kl = warp_sum(kl);
+  if (lane) return;
+  const int y = a.ypos[t];
+  const bool in = a.w[t] != 0.0f;                      // a token of no weight is left out, whatever it holds
+  a.lt[t] = lt;
+  a.l1[t] = lo;
+  a.tokens[t] = in ? kl : 0.0f;
+  a.tokens[a.Tall + t] = in && y >= 0 ? lo - a.sz[t * a.K1 + y] : 0.0f;
+}
+}  // namespace
+
+// bf16: from the summaries of 64 columns, [rows, ng] of (max, sum) and with two temperatures the second sums
+__global__ __launch_bounds__(256) void distill_merge_kernel(DistillArgs a, const float* part, const float* part1) {
+  const int lane = threadIdx.x & 63;
+  const int64_t t = a.t0 + (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (t >= a.T) return;
+  float m = -__builtin_inff(), l = 0.0f, l1 = 0.0f;
+  for (int64_t j = lane; j < a.ng; j += 64) {
+    const int64_t at = (t - a.t0) * a.ng + j;
+    const u32x2 v = *(const u32x2*)(part + 2 * at);
+    join(m, l, l1, __uint_as_float(v[0]), __uint_as_float(v[1]), a.two ? part1[at] : 0.0f, a.scale);
+  }
+  finish(a, t, lane, m, l, l1);
+}
+
+// fp32: from the logits [rows, ld]
+__global__ __launch_bounds__(256) void distill_rows_kernel(DistillArgs a, const float* z, int64_t ld) {
+  const int lane = threadIdx.x & 63;
+  const int64_t t = a.t0 + (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (t >= a.T) return;
+  const float* row = z + (t - a.t0) * ld;
+  float m = -__builtin_inff(), l = 0.0f, l1 = 0.0f;
+  for (int64_t j = lane; j < a.V; j += 64) m = fmaxf(m, row[j]);
+  for (int64_t j = lane; j < a.V; j += 64) {
+    l += __builtin_amdgcn_exp2f((row[j] - m) * a.scale);
+    if (a.two) l1 += __builtin_amdgcn_exp2f((row[j] - m) * kLog2e);
+  }
+  const int n = a.count[t];
+  for (int j = lane; j < n; j += 64) a.sz[t * a.K1 + j] = row[a.sidx[t * a.K1 + j]];
+  finish(a, t, lane, m, l, l1);
+}
+
+// loss = (sum w (soft tau^2 kl + hard ce), sum w kl, sum w ce), in a fixed order by one workgroup
+__global__ __launch_bounds__(1024) void distill_loss_kernel(DistillArgs a, float* loss) {
+  __shared__ float part[2][1024];
+  const int tid = threadIdx.x;
+  float kl = 0.0f, ce = 0.0f;
+  for (int64_t t = tid; t < a.Tall; t += 1024) {
+    const float w = a.w[t];
+    if (w != 0.0f) {
+      kl += w * a.tokens[t];
+      ce += w * a.tokens[a.Tall + t];
+    }
+  }
+  part[0][tid] = kl;
+  part[1][tid] = ce;
+  __syncthreads();
+  for (int o = 512; o >= 1; o >>= 1) {
+    if (tid < o) {
+      part[0][tid] += part[0][tid + o];
+      part[1][tid] += part[1][tid + o];
+    }
+    __syncthreads();
+  }
+  if (tid == 0) {
+    loss[0] = a.soft * a.tau * a.tau * part[0][0] + a.hard * part[1][0];
+    loss[1] = part[0][0];
+    loss[2] = part[1][0];
+  }
+}
+
+// The listed elements of the logits' gradient, transposed [V, ld] with the block's tokens as columns
+template <typename T>
+__global__ __launch_bounds__(256) void distill_listed_kernel(DistillArgs a, float dloss, T* G, int64_t ld) {
+  const int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x, rows = a.T - a.t0;
+  // neighbouring threads take neighbouring tokens: their lists' columns of G are neighbours
+  const int64_t j = e / rows, t = a.t0 + e % rows;
+  if (j >= a.K1 || j >= a.count[t]) return;
+  const float gs = a.gs[t], gh = a.gh[t], z = a.sz[t * a.K1 + j];
+  if (gs == 0.0f && gh == 0.0f) return;
+  const float p = __builtin_amdgcn_exp2f(z * a.scale - a.lt[t] * kLog2e), p1 = a.two ? __builtin_amdgcn_exp2f((z - a.l1[t]) * kLog2e) : p;
+  const float g = gs * (p - a.sq[t * a.K1 + j]) + gh * (a.ypos[t] == j ? p1 - 1.0f : p1);
+  G[(int64_t)a.sidx[t * a.K1 + j] * ld + (t - a.t0)] = from_f32<T>(dloss * g);
+}
+
+// h of the tokens that have a gradient, zeros for the others, so that what those hold does not reach dW
+template <typename T>
+__global__ __launch_bounds__(256) void distill_rows_of_kernel(DistillArgs a, const T* h, T* out, int64_t D) {
+  constexpr int N = 16 / sizeof(T);
+  const int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x, per = D / N, t = e / per;
+  if (t >= a.T - a.t0) return;
+  const bool in = a.gs[a.t0 + t] != 0.0f || a.gh[a.t0 + t] != 0.0f;
+  ((u32x4*)out)[e] = in ? ((const u32x4*)h)[e] : u32x4{0, 0, 0, 0};
+}
+
+// ------------------------------------------------------------------ launchers
+hipError_t distill_prep(const DistillArgs& a, hipStream_t s) {
+  // tokens t0 .. T: pointers of whole tensors
+  DistillArgs b = a;
+  const int64_t n = a.T - a.t0;
+  b.index += a.t0 * a.K; b.values += a.t0 * a.K;
+  if (b.targets) b.targets += a.t0;
+  if (b.weights) b.weights += a.t0;
+  b.sidx += a.t0 * a.K1; b.sq += a.t0 * a.K1; b.ypos += a.t0; b.count += a.t0; b.gs += a.t0; b.gh += a.t0; b.w += a.t0;
+  b.T = n; b.t0 = 0;
+  hipLaunchKernelGGL(distill_prep_kernel, dim3((unsigned)((n + 3) / 4)), dim3(256), 0, s, b);
+  return hipGetLastError();
+}
+hipError_t distill_merge(const DistillArgs& a, const float* part, const float* part1, hipStream_t s) {
+  hipLaunchKernelGGL(distill_merge_kernel, dim3((unsigned)((a.T - a.t0 + 3) / 4)), dim3(256), 0, s, a, part, part1);
+  return hipGetLastError();
+}
+hipError_t distill_rows(const DistillArgs& a, const float* z, int64_t ld, hipStream_t s) {
+  hipLaunchKernelGGL(distill_rows_kernel, dim3((unsigned)((a.T - a.t0 + 3) / 4)), dim3(256), 0, s, a, z, ld);
+  return hipGetLastError();
+}
+hipError_t distill_loss(const DistillArgs& a, float* loss, hipStream_t s) {
+  hipLaunchKernelGGL(distill_loss_kernel, dim3(1), dim3(1024), 0, s, a, loss);
+  return hipGetLastError();
+}
+hipError_t distill_listed(Dt t, const DistillArgs& a, float dloss, void* G, int64_t ld, hipStream_t s) {
+  const dim3 grid((unsigned)(((a.T - a.t0) * a.K1 + 255) / 256));
+  if (t == F32) hipLaunchKernelGGL((distill_listed_kernel<float>), grid, dim3(256), 0, s, a, dloss, (float*)G, ld);
+  else hipLaunchKernelGGL((distill_listed_kernel<bf16>), grid, dim3(256), 0, s, a, dloss, (bf16*)G, ld);
+  return hipGetLastError();
+}
+hipError_t distill_rows_of(Dt t, const DistillArgs& a, const void* h, void* out, int64_t D, hipStream_t s) {
+  const int64_t n = (a.T - a.t0) * D / (t == F32 ? 4 : 8);
+  const dim3 grid((unsigned)((n + 255) / 256));
+  if (t == F32) hipLaunchKernelGGL((distill_rows_of_kernel<float>), grid, dim3(256), 0, s, a, (const float*)h, (float*)out, D);
+  else hipLaunchKernelGGL((distill_rows_of_kernel<bf16>), grid, dim3(256), 0, s, a, (const bf16*)h, (bf16*)out, D);
+  return hipGetLastError();
+}
+
+}  // namespace bpt

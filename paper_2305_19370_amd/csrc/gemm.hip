@@ -62,6 +62,27 @@ BPT_DEV float xent_grad_t(const GemmArgs& a, int64_t m, int64_t n, float v) {
   return xent_grad_t_l2(a, m, v, a.rowv[n] * 1.4426950408889634f, a.tgt[n]);
 }
 
+// EPI_LIST_T: what the column (token) contributes, loaded once per column where a tile allows it
+struct ListCol {
+  float l2, g, l21, g1;          // base-2 log-sum-exps and factors
+  BPT_DEV void load(const GemmArgs& a, int64_t n) {
+    l2 = a.rowv[n] * 1.4426950408889634f;
+    g = a.rowg[n];
+    l21 = 0.0f;
+    g1 = a.rowg1[n];
+    if (a.two) l21 = a.rowv1[n] * 1.4426950408889634f;
+    else g += g1, g1 = 0.0f;
+    g *= a.gscale;
+    g1 *= a.gscale;
+  }
+  BPT_DEV float grad(const GemmArgs& a, int64_t m, float v) const {
+    if (m >= a.nvalid || (g == 0.0f && g1 == 0.0f)) return 0.0f;
+    float r = g * __builtin_amdgcn_exp2f(fmaf(v, a.alpha, -l2));
+    if (a.two) r = fmaf(g1, __builtin_amdgcn_exp2f(fmaf(v, 1.4426950408889634f, -l21)), r);
+    return r;
+  }
+};
+
 template <int EPI, typename CT, typename RT>
 BPT_DEV void epi_store(const GemmArgs& a, int64_t z, int64_t m, int64_t n, float v) {
   CT* C = (CT*)a.C + z * a.sC;
@@ -90,6 +111,10 @@ BPT_DEV void epi_store(const GemmArgs& a, int64_t z, int64_t m, int64_t n, float
     if (a.C2) c2_store(a, z * a.sC2 + m * a.ldc2 + n, gp);
   } else if constexpr (EPI == EPI_XENT_T) {
     C[idx] = from_f32<CT>(xent_grad_t(a, m, n, v));
+  } else if constexpr (EPI == EPI_LIST_T) {
+    ListCol c;
+    c.load(a, n);
+    C[idx] = from_f32<CT>(c.grad(a, m, v));
   } else if constexpr (EPI == EPI_MUL) {
     const RT* R = (const RT*)a.R + z * a.sR;
     C[idx] = from_f32<CT>(v * to_f32<RT>(R[m * a.ldr + n]));
@@ -155,6 +180,13 @@ BPT_DEV void epi_store4(const GemmArgs& a, int64_t z, int64_t m, int64_t n, int6
   } else if constexpr (EPI == EPI_XENT_T) {
 #pragma unroll
     for (int e = 0; e < 4; ++e) v[e] = xent_grad_t(a, m, n + e, v[e]);
+  } else if constexpr (EPI == EPI_LIST_T) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      ListCol c;
+      c.load(a, n + e);
+      v[e] = c.grad(a, m, v[e]);
+    }
   } else if constexpr (EPI == EPI_MUL) {
     v *= V4<RT>::ld((const RT*)a.R + z * a.sR + m * a.ldr + n);
   }
@@ -739,6 +771,48 @@ __global__ __launch_bounds__(128 * NWN * KG, 1) void gemm_bf16_kernel(GemmArgs a
       }
       continue;
     }
+    if constexpr (EPI == EPI_LIST) {
+      // as EPI_LSE, with the listed logits of a row instead of one target's
+      static_assert(Cfg::WN == 64, "summaries of 64 columns");
+      const int c0 = 4 * (lane % C4);
+      const bool all = ncol + 64 <= a.nvalid;
+#pragma unroll 4
+      for (int it = 0; it < 32 / RSTEP; ++it) {
+        const int row = lane / C4 + RSTEP * it;
+        const int64_t m = mrow + row;
+        const bool in = m < a.M && ncol < ncols;
+        int from = 0, to = 0;
+        if (in) {
+          const uint16_t* sg = a.seg + m * a.ldseg + ncol / 64;
+          from = sg[0];
+          to = sg[1];
+        }
+        const f32x4 v = *(const f32x4*)(strip + row * PITCHF + c0);
+        float mx = -__builtin_inff(), sum = 0.0f, sum1 = 0.0f;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) mx = all || ncol + c0 + e < a.nvalid ? fmaxf(mx, v[e]) : mx;
+        mx = max16(mx);
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          sum += all || ncol + c0 + e < a.nvalid ? __builtin_amdgcn_exp2f((v[e] - mx) * a.alpha) : 0.0f;
+        sum = sum16(sum);
+        if (a.two) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            sum1 += all || ncol + c0 + e < a.nvalid ? __builtin_amdgcn_exp2f((v[e] - mx) * 1.4426950408889634f) : 0.0f;
+          sum1 = sum16(sum1);
+        }
+        if (in && c0 == 0) {
+          *(u32x2*)((float*)a.C + 2 * (m * a.ldc + ncol / 64)) = u32x2{__float_as_uint(mx), __float_as_uint(sum)};
+          if (a.two) ((float*)a.C2)[m * a.ldc + ncol / 64] = sum1;
+        }
+        for (int e = from; e < to; ++e) {
+          const int64_t k = a.list[m * a.ldlist + e] - ncol - c0;
+          if (k >= 0 && k < 4) a.list_z[m * a.ldlist + e] = k == 0 ? v[0] : k == 1 ? v[1] : k == 2 ? v[2] : v[3];
+        }
+      }
+      continue;
+    }
     if (inside) {
       // rows are (lane / C4) + (64 / C4) * it; columns 4 * (lane % C4)
       const int r0 = lane / C4, c0 = 4 * (lane % C4);
@@ -768,6 +842,20 @@ __global__ __launch_bounds__(128 * NWN * KG, 1) void gemm_bf16_kernel(GemmArgs a
           f32x4 v = *(const f32x4*)(strip + row * PITCHF + c0);
 #pragma unroll
           for (int e = 0; e < 4; ++e) v[e] = xent_grad_t_l2(a, m, v[e], l2[e], y4[e]);
+          V4<CT>::st(cb + (int64_t)RSTEP * it * a.ldc, v);
+        }
+        continue;
+      }
+      if constexpr (EPI == EPI_LIST_T) {
+        ListCol col[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) col[e].load(a, ncol + c0 + e);
+#pragma unroll 4
+        for (int it = 0; it < 32 / RSTEP; ++it) {
+          const int row = r0 + RSTEP * it;
+          f32x4 v = *(const f32x4*)(strip + row * PITCHF + c0);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) v[e] = col[e].grad(a, mrow + row, v[e]);
           V4<CT>::st(cb + (int64_t)RSTEP * it * a.ldc, v);
         }
         continue;
@@ -1003,13 +1091,14 @@ static hipError_t launch_ops(const GemmArgs& a, hipStream_t s) {
   if ((TA && ((a.a_cols > 0 ? a.a_cols : a.M) % 8 || a.lda % 8)) || (TB && ((a.b_cols > 0 ? a.b_cols : a.N) % 8 || a.ldb % 8)))
     return hipErrorInvalidValue;
   // the head's products are in_order: none shares K
-  constexpr bool ordered = EPI == EPI_LSE || EPI == EPI_XENT_T || (EPI == EPI_STORE && sizeof(CT) == 2 && TA);
+  constexpr bool summary = EPI == EPI_LSE || EPI == EPI_LIST;
+  constexpr bool ordered = summary || EPI == EPI_XENT_T || EPI == EPI_LIST_T || (EPI == EPI_STORE && sizeof(CT) == 2 && TA);
   if (ordered && !a.in_order) return hipErrorInvalidValue;
   switch (pick_tile(a, EPI == EPI_RESID || EPI == EPI_MUL)) {
     case T256: return launch_bf16<256, 256, 4, 1, EPI, CT, RT, TA, TB, KF>(a, s);
     case T128: return launch_bf16<128, 128, 2, 1, EPI, CT, RT, TA, TB, KF>(a, s);
     case T64:
-      if constexpr (EPI != EPI_LSE) return launch_bf16<64, 64, 2, 1, EPI, CT, RT, TA, TB, KF>(a, s);
+      if constexpr (!summary) return launch_bf16<64, 64, 2, 1, EPI, CT, RT, TA, TB, KF>(a, s);
       else return launch_bf16<128, 128, 2, 1, EPI, CT, RT, TA, TB, KF>(a, s);   // waves of 64 columns
     case T64K4:
       if constexpr (!ordered) return launch_bf16<64, 64, 2, 4, EPI, CT, RT, TA, TB, KF>(a, s);
@@ -1077,7 +1166,7 @@ static hipError_t run_bf16(const GemmArgs& a, hipStream_t s) {
     BPT_GEMM_FORM(launch_ops, 1, 0, 0);                // its recompute
   } else if constexpr (EPI == EPI_MUL) {
     BPT_GEMM_FORM(launch_ops, 0, 0, 0);                // dZ
-  } else if constexpr (EPI == EPI_LSE) {
+  } else if constexpr (EPI == EPI_LSE || EPI == EPI_LIST) {
     BPT_GEMM_FORM(launch_ops, 0, 1, 0);                // logits' row summaries
   } else {
     BPT_GEMM_FORM(launch_ops, 1, 0, 0);                // head gradient
@@ -1127,6 +1216,8 @@ hipError_t gemm(Dt ab, Epi epi, Dt ct, Dt rt, const GemmArgs& a, hipStream_t s) 
       case EPI_RELU: return ct == F32 ? run_f32<EPI_RELU, float, float>(a, s) : hipErrorInvalidValue;
       case EPI_XENT_T: return ct == F32 ? run_f32<EPI_XENT_T, float, float>(a, s) : hipErrorInvalidValue;
       case EPI_LSE: return hipErrorInvalidValue;
+      case EPI_LIST: return hipErrorInvalidValue;
+      case EPI_LIST_T: return ct == F32 ? run_f32<EPI_LIST_T, float, float>(a, s) : hipErrorInvalidValue;
       case EPI_MUL: return ct == F32 && rt == F32 ? run_f32<EPI_MUL, float, float>(a, s) : hipErrorInvalidValue;
       case EPI_RESID:
         if (rt != F32) return hipErrorInvalidValue;
@@ -1140,6 +1231,8 @@ hipError_t gemm(Dt ab, Epi epi, Dt ct, Dt rt, const GemmArgs& a, hipStream_t s) 
     case EPI_RELU: return ct == BF16 ? run_bf16<EPI_RELU, bf16, float>(a, s) : hipErrorInvalidValue;
     case EPI_LSE: return ct == F32 ? run_bf16<EPI_LSE, float, float>(a, s) : hipErrorInvalidValue;
     case EPI_XENT_T: return ct == BF16 ? run_bf16<EPI_XENT_T, bf16, float>(a, s) : hipErrorInvalidValue;
+    case EPI_LIST: return ct == F32 ? run_bf16<EPI_LIST, float, float>(a, s) : hipErrorInvalidValue;
+    case EPI_LIST_T: return ct == BF16 ? run_bf16<EPI_LIST_T, bf16, float>(a, s) : hipErrorInvalidValue;
     case EPI_MUL: return ct == BF16 && rt == F16 ? run_bf16<EPI_MUL, bf16, f16>(a, s) : hipErrorInvalidValue;
     case EPI_RESID:
       if (ct == F32) return rt == F32 ? run_bf16<EPI_RESID, float, float>(a, s) : run_bf16<EPI_RESID, float, bf16>(a, s);

@@ -24,6 +24,12 @@ enum Epi {
   EPI_LSE = 7,     // bf16 operands; row summaries of the logits acc instead of the logits: for
                    // every 64 columns j, C[m, j] = (max, sum of exp(acc - max)) over columns
                    // below nvalid, as two floats; tlogit[m] = acc[m, tgt[m]] for 0 <= tgt[m] < nvalid
+  EPI_LIST = 8,    // bf16 operands; the same with exp2(alpha (acc - max)) and, with `two`, the sums of exp(acc - max)
+                   // in C2[m, j]; list_z[m, e] = acc[m, list[m, e]] for the entries e of row m, sorted by column: those of
+                   // 64 columns j are seg[m, j] .. seg[m, j + 1]
+  EPI_LIST_T = 9,  // gradient of transposed logits acc (rows m = vocabulary, columns n = tokens) without a list: for m < nvalid
+                   // C = gscale (rowg[n] exp2(alpha acc - rowv[n] log2e) + rowg1[n] exp(acc - rowv1[n])), or without `two`
+                   // gscale (rowg + rowg1)[n] exp2(..); C = 0 for nvalid <= m, and where rowg and rowg1 are 0
 };
 
 struct GemmArgs {
@@ -73,6 +79,14 @@ struct GemmArgs {
   int64_t kper = 0;
   const void* Bx[3] = {nullptr, nullptr, nullptr};
   void* Cx[3] = {nullptr, nullptr, nullptr};
+  // EPI_LIST, EPI_LIST_T
+  const uint16_t* seg = nullptr;
+  const int32_t* list = nullptr;
+  float* list_z = nullptr;
+  int64_t ldseg = 0, ldlist = 0;
+  const float *rowg = nullptr, *rowv1 = nullptr, *rowg1 = nullptr;
+  float gscale = 1.0f;
+  int two = 0;
 };
 
 // Whether a GEMM of M x 3 nper may be given as one with nper > 0
@@ -277,6 +291,31 @@ hipError_t xent_merge(const float* part, int64_t ng, int64_t rows, int64_t V, co
                       float* lse, float* tok, hipStream_t s);
 // out[0] = mean of x[0..n), summed in a fixed order
 hipError_t mean_of(const float* x, int64_t n, float* out, hipStream_t s);
+// ---------------------------------------------------------------- distillation from a teacher's largest logits
+constexpr int kDistillMaxK = 256;
+// Tokens t0 .. T of Tall; pointers are those of token 0, [T] or [T, K] or [T, K1], K1 = K + 1 with targets.
+struct DistillArgs {
+  const float* values = nullptr;        // the teacher's lists
+  const int32_t *index = nullptr, *targets = nullptr;
+  const float* weights = nullptr;       // or null: `weight` for each
+  int32_t* sidx = nullptr;              // lists sorted by index, with probabilities and the student's logits
+  float *sq = nullptr, *sz = nullptr;
+  int32_t *ypos = nullptr, *count = nullptr;   // the target's entry (-1: none), entries
+  float *lt = nullptr, *l1 = nullptr;   // log-sum-exp of z / tau, of z
+  float *gs = nullptr, *gh = nullptr, *w = nullptr;   // factors of p_tau - q and of p_1 - onehot; weight
+  float* tokens = nullptr;              // [2, Tall] kl, ce
+  uint16_t* seg = nullptr;              // block's rows of ldseg: entries before every 64 columns, or null
+  int64_t t0 = 0, T = 0, Tall = 0, V = 0, ng = 0, ldseg = 0;
+  int K = 0, K1 = 0, two = 0;           // two: hard targets at another temperature than 1
+  float tau = 1, scale = 1, soft = 0, hard = 0, weight = 0;   // scale: log2(e) / tau
+};
+hipError_t distill_prep(const DistillArgs& a, hipStream_t s);
+hipError_t distill_merge(const DistillArgs& a, const float* part, const float* part1, hipStream_t s);   // EPI_LIST's C, C2
+hipError_t distill_rows(const DistillArgs& a, const float* z, int64_t ld, hipStream_t s);
+hipError_t distill_loss(const DistillArgs& a, float* loss, hipStream_t s);
+hipError_t distill_listed(Dt t, const DistillArgs& a, float dloss, void* G, int64_t ld, hipStream_t s);
+hipError_t distill_rows_of(Dt t, const DistillArgs& a, const void* h, void* out, int64_t D, hipStream_t s);
+
 // ---------------------------------------------------------------- GPT step pieces
 // X[t] = Wte[tok[t]] + Wpe[t mod S] (Wpe may be null); NaN row for tok outside [0, V). D % 8 == 0.
 hipError_t embed_fwd(Dt t, const int32_t* tok, const void* Wte, const void* Wpe, void* X, int64_t rows,

@@ -1871,4 +1871,194 @@ bpt_status bpt_recur_bwd(const bpt_recur_config* cfg, const void* x, const void*
   return BPT_OK;
 }
 
+// ---------------------------------------------------------------- distillation from a teacher's largest logits
+static bpt_status distill_check(const bpt_distill_config* c) {
+  if (!c) return fail(BPT_ERR_INVALID_ARG, "config is NULL");
+  bpt_xent_config x = {c->T, c->D, c->V, c->ldw, c->block_rows, c->dtype, c->reserved};
+  bpt_status st = xent_check(&x);
+  if (st != BPT_OK) return st;
+  if (c->K < 1) return fail(BPT_ERR_INVALID_ARG, "K must be >= 1");
+  if (!(c->tau > 0.0f) || !std::isfinite(c->tau) || !std::isfinite(1.0f / c->tau)) return fail(BPT_ERR_INVALID_ARG, "tau must be > 0");
+  if (!(c->soft >= 0.0f) || !(c->hard >= 0.0f) || !std::isfinite(c->soft) || !std::isfinite(c->hard))
+    return fail(BPT_ERR_INVALID_ARG, "soft and hard must be >= 0");
+  if ((st = dtype_ok(c->grad_dtype, "grad_dtype")) != BPT_OK) return st;
+  if (c->grad_dtype == BPT_BF16 && c->dtype != BPT_BF16)
+    return fail(BPT_ERR_UNSUPPORTED, "grad_dtype BPT_BF16 needs dtype BPT_BF16");
+  if (c->K > kDistillMaxK) return fail(BPT_ERR_UNSUPPORTED, "K must be <= %d (got %lld)", kDistillMaxK, (long long)c->K);
+  if (c->V > ((int64_t)1 << 31) - 65 || c->ldw > (int64_t)1 << 31 || c->D * c->ldw > (int64_t)1 << 33)
+    return fail(BPT_ERR_UNSUPPORTED, "V or D V too large");
+  // threads of a launch over a block's lists, and over its rows of h
+  const int64_t R = std::min(c->block_rows > 0 ? c->block_rows : kDefaultXentRows, c->T);
+  if (R > (int64_t)1 << 22 || R * std::max(c->K + 1, c->D / 4) >= (int64_t)1 << 32)
+    return fail(BPT_ERR_UNSUPPORTED, "block_rows too large");
+  return BPT_OK;
+}
+
+static XentDims distill_dims(const bpt_distill_config& c) {
+  return xent_dims({c.T, c.D, c.V, c.ldw, c.block_rows, c.dtype, 0});
+}
+
+static DistillArgs distill_args(const bpt_distill_config& c, const void* saved, int64_t* total) {
+  DistillArgs a;
+  a.K = (int)c.K; a.K1 = (int)(c.K + (c.hard > 0.0f)); a.two = c.hard > 0.0f && c.tau != 1.0f;
+  a.tau = c.tau; a.scale = (float)(1.4426950408889634 / (double)c.tau); a.soft = c.soft; a.hard = c.hard;
+  a.weight = (float)(1.0 / (double)c.T);
+  a.Tall = c.T; a.V = c.V; a.ng = c.ldw / 64; a.ldseg = rup(a.ng + 1, 8);
+  Bump bp((void*)saved);
+  a.sidx = (int32_t*)bp.take(c.T * a.K1 * 4);
+  a.sq = (float*)bp.take(c.T * a.K1 * 4);
+  a.sz = (float*)bp.take(c.T * a.K1 * 4);
+  a.ypos = (int32_t*)bp.take(c.T * 4);
+  a.count = (int32_t*)bp.take(c.T * 4);
+  for (float** f : {&a.lt, &a.l1, &a.gs, &a.gh, &a.w}) *f = (float*)bp.take(c.T * 4);
+  *total = rup(bp.off, kAlign);
+  return a;
+}
+
+struct DistillWs {
+  float *logits, *part1;  // forward: fp32 logits of a block, or their summaries and the second sums
+  uint16_t* seg;          // forward, bf16
+  void *g, *hz;           // backward: the block's gradient, transposed; its rows of h
+  float *part, *dw;       // backward: slices of dh; fp32 sums of a bf16 dW over the blocks
+};
+static DistillWs distill_ws(const bpt_distill_config& c, const XentDims& d, void* base, int backward, int64_t* total) {
+  Bump bp(base);
+  DistillWs w{};
+  if (backward) {
+    w.g = bp.take(d.Rp * d.ldw * (int64_t)d.E);
+    w.hz = bp.take(d.R * d.D * (int64_t)d.E);
+    if (d.zdh > 1) w.part = (float*)bp.take(d.zdh * d.R * d.D * 4);
+    if (c.grad_dtype == BPT_BF16 && d.T > d.R) w.dw = (float*)bp.take(d.D * d.ldw * 4);
+  } else if (d.E == 4) {
+    w.logits = (float*)bp.take(d.R * d.ldw * 4);
+  } else {
+    const int64_t ng = d.ldw / 64;
+    w.logits = (float*)bp.take(d.R * ng * 8);
+    w.part1 = (float*)bp.take(d.R * ng * 4);
+    w.seg = (uint16_t*)bp.take(d.R * rup(ng + 1, 8) * 2);
+  }
+  *total = rup(bp.off, kAlign);
+  return w;
+}
+
+bpt_status bpt_distill_validate(const bpt_distill_config* cfg) { return distill_check(cfg); }
+
+size_t bpt_distill_saved_bytes(const bpt_distill_config* cfg) {
+  if (distill_check(cfg) != BPT_OK) return 0;
+  int64_t total;
+  distill_args(*cfg, nullptr, &total);
+  return (size_t)total;
+}
+
+size_t bpt_distill_workspace_bytes(const bpt_distill_config* cfg, int backward) {
+  if (distill_check(cfg) != BPT_OK) return 0;
+  int64_t total;
+  distill_ws(*cfg, distill_dims(*cfg), nullptr, backward, &total);
+  return (size_t)total;
+}
+
+bpt_status bpt_distill_fwd(const bpt_distill_config* cfg, const void* h, const void* W, const float* values, const int32_t* index,
+                           const int32_t* targets, const float* weights, float* loss, float* tokens, void* saved, void* ws,
+                           size_t ws_bytes, void* stream) {
+  bpt_status st = distill_check(cfg);
+  if (st != BPT_OK) return st;
+  if (cfg->hard > 0.0f && !targets) return fail(BPT_ERR_INVALID_ARG, "targets must not be NULL where hard > 0");
+  for (const void* q : {h, W, (const void*)values, (const void*)index, (const void*)loss, (const void*)tokens, (const void*)saved, (const void*)ws})
+    if (!q) return fail(BPT_ERR_INVALID_ARG, "h, W, values, index, loss, tokens, saved and workspace must not be NULL");
+  for (const void* q : {h, W, (const void*)values, (const void*)index, (const void*)targets, (const void*)weights, (const void*)loss,
+                        (const void*)tokens, (const void*)saved, (const void*)ws})
+    if (q && !aligned16(q)) return fail(BPT_ERR_INVALID_ARG, "pointer %p is not 16-byte aligned", q);
+  const XentDims d = distill_dims(*cfg);
+  int64_t need, stotal;
+  const DistillWs w = distill_ws(*cfg, d, ws, 0, &need);
+  if ((int64_t)ws_bytes < need)
+    return fail(BPT_ERR_WORKSPACE, "workspace %zu bytes < required %lld", ws_bytes, (long long)need);
+  DistillArgs a = distill_args(*cfg, saved, &stotal);
+  a.values = values; a.index = index; a.targets = cfg->hard > 0.0f ? targets : nullptr; a.weights = weights; a.tokens = tokens; a.seg = w.seg;
+  hipStream_t s = (hipStream_t)stream;
+  const Dt E = dt_of(cfg->dtype);
+  const int64_t E_ = (int64_t)d.E, ng = a.ng;
+  for (int64_t t0 = 0; t0 < d.T; t0 += d.R) {
+    const int64_t r = std::min(d.R, d.T - t0);
+    a.t0 = t0; a.T = t0 + r;
+    RUN("distill.prep", 0, (double)r * (20.0 * a.K1 + 2.0 * ng), distill_prep(a, s));
+    GemmArgs g;   // logits of the block: h W, W read as it is stored (B operand K-major)
+    g.A = (const char*)h + t0 * d.D * E_; g.lda = d.D;
+    g.B = W; g.ldb = d.ldw; g.trans_b = 1; g.in_order = 1;
+    g.C = w.logits; g.ldc = d.ldw; g.M = r; g.N = d.ldw; g.K = d.D;
+    if (E == BF16) {
+      g.ldc = ng; g.nvalid = d.V; g.alpha = a.scale; g.two = a.two; g.C2 = w.part1;
+      g.seg = w.seg; g.ldseg = a.ldseg; g.list = a.sidx + t0 * a.K1; g.list_z = a.sz + t0 * a.K1; g.ldlist = a.K1;
+      RUN("distill.logits", gemm_flops(g), ((double)r * d.D + (double)d.ldw * d.D) * E_ + (double)r * ng * 10,
+          gemm(E, EPI_LIST, F32, F32, g, s));
+      RUN("distill.rows", 0, (double)r * ng * 8, distill_merge(a, w.logits, w.part1, s));
+    } else {
+      RUN("distill.logits", gemm_flops(g), gemm_bytes(g, E_, 4), gemm(E, EPI_STORE, F32, F32, g, s));
+      RUN("distill.rows", 0, (double)r * d.ldw * 8, distill_rows(a, w.logits, d.ldw, s));
+    }
+  }
+  RUN("distill.loss", 0, (double)d.T * 12, distill_loss(a, loss, s));
+  return BPT_OK;
+}
+
+bpt_status bpt_distill_bwd(const bpt_distill_config* cfg, const void* h, const void* W, const void* saved, float dloss, void* dh,
+                           void* dW, void* ws, size_t ws_bytes, void* stream) {
+  bpt_status st = distill_check(cfg);
+  if (st != BPT_OK) return st;
+  for (const void* q : {h, W, saved, (const void*)dh, (const void*)ws}) {
+    if (!q) return fail(BPT_ERR_INVALID_ARG, "h, W, saved, dh and workspace must not be NULL");
+    if (!aligned16(q)) return fail(BPT_ERR_INVALID_ARG, "pointer %p is not 16-byte aligned", q);
+  }
+  if (!aligned16(dW)) return fail(BPT_ERR_INVALID_ARG, "pointer %p is not 16-byte aligned", dW);
+  if (dh == h || dh == W || dW == h || dW == W || dh == dW) return fail(BPT_ERR_INVALID_ARG, "dh and dW must not alias h, W or one another");
+  const XentDims d = distill_dims(*cfg);
+  int64_t need, stotal;
+  const DistillWs w = distill_ws(*cfg, d, ws, 1, &need);
+  if ((int64_t)ws_bytes < need)
+    return fail(BPT_ERR_WORKSPACE, "workspace %zu bytes < required %lld", ws_bytes, (long long)need);
+  DistillArgs a = distill_args(*cfg, saved, &stotal);
+  hipStream_t s = (hipStream_t)stream;
+  const Dt E = dt_of(cfg->dtype), GT = dt_of(cfg->grad_dtype);
+  const int64_t E_ = (int64_t)d.E;
+  for (int64_t t0 = 0; t0 < d.T; t0 += d.R) {
+    const int64_t r = std::min(d.R, d.T - t0), rp = rup(r, 64);
+    const char* hb = (const char*)h + t0 * d.D * E_;
+    a.t0 = t0; a.T = t0 + r;
+    {   // G^T [ldw, rp] of the block's logits, recomputed transposed as in bpt_xent_bwd, then its listed elements
+      GemmArgs g;
+      g.A = W; g.lda = d.ldw; g.trans_a = 1; g.B = hb; g.ldb = d.D;
+      g.C = w.g; g.ldc = d.Rp; g.M = d.ldw; g.N = r; g.Nstore = rp; g.K = d.D;
+      g.in_order = 1; g.alpha = a.scale; g.gscale = dloss; g.two = a.two; g.nvalid = d.V;
+      g.rowv = a.lt + t0; g.rowg = a.gs + t0; g.rowv1 = a.l1 + t0; g.rowg1 = a.gh + t0;
+      RUN("distill.grad_logits", gemm_flops(g), gemm_bytes(g, E_, E_), gemm(E, EPI_LIST_T, E, F32, g, s));
+      RUN("distill.listed", 0, (double)r * a.K1 * 16, distill_listed(E, a, dloss, w.g, d.Rp, s));
+    }
+    {   // dh = G W^T
+      GemmArgs g;
+      g.A = w.g; g.lda = d.Rp; g.trans_a = 1; g.a_cols = d.Rp; g.B = W; g.ldb = d.ldw;
+      g.C = (char*)dh + t0 * d.D * E_; g.ldc = d.D; g.M = r; g.N = d.D; g.K = d.ldw; g.in_order = 1;
+      if (d.zdh > 1) {
+        void* out = g.C;
+        g.ksplit = d.zdh; g.C = w.part; g.sC = r * d.D;
+        RUN("distill.dh", gemm_flops(g), gemm_bytes(g, E_, 4), gemm(E, EPI_STORE, F32, F32, g, s));
+        RUN("reduce.ksplit", 0, (double)r * d.D * (4 * d.zdh + E_), sum_slices_add(w.part, d.zdh, r, d.D, F32, nullptr, nullptr, E, out, s));
+      } else {
+        RUN("distill.dh", gemm_flops(g), gemm_bytes(g, E_, E_), gemm(E, EPI_STORE, E, F32, g, s));
+      }
+    }
+    if (dW) {   // dW = h^T G
+      RUN("distill.h", 0, 2.0 * r * d.D * E_, distill_rows_of(E, a, hb, w.hz, d.D, s));
+      GemmArgs g;
+      g.A = w.hz; g.lda = d.D; g.trans_a = 1; g.a_rows = r;
+      g.B = w.g; g.ldb = d.Rp;
+      g.C = w.dw ? (void*)w.dw : dW; g.ldc = d.ldw; g.M = d.D; g.N = d.ldw; g.K = rp; g.accumulate = t0 > 0;
+      g.in_order = 1;
+      const Dt CT = w.dw ? F32 : GT;
+      RUN("distill.dW", gemm_flops(g), gemm_bytes(g, E_, CT == F32 ? 4 : 2), gemm(E, EPI_STORE, CT, F32, g, s));
+    }
+  }
+  if (dW && w.dw) RUN("distill.dW_round", 0, 6.0 * d.D * d.ldw, sum_slices_add(w.dw, 1, d.D, d.ldw, F32, nullptr, nullptr, BF16, dW, s));
+  return BPT_OK;
+}
+
 }  // extern "C"

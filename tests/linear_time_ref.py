@@ -87,3 +87,73 @@ def recur(x, r, i, lam, c: float, h0=None, lens=None, dy=None, dhT=None) -> Dict
     adds = 160 + B * ((S + 127) // 128) / 16
     out["dlam"], out["dlam_err"] = ratio * w.sum((0, 1)), ratio * (ew.sum((0, 1)) + (adds + 24) * U32 * w.abs().sum((0, 1)))
     return out
+
+
+def distill(h, W, V: int, values, index, tau: float, soft: float, hard: float = 0.0, targets=None, weights=None,
+            dloss: float = 1.0, half: float = U32, half_dw: Optional[float] = None) -> Dict[str, torch.Tensor]:
+    """loss, tokens, dh and dW from the whole logits, each with its bound as "name_err". half: half a step of h's type, to which the
+    logits' gradient and dh are rounded; half_dw: that of dW's."""
+    h, W, values = (t.detach().cpu().to(F64) for t in (h, W, values))
+    index = index.detach().cpu().long()
+    T, D = h.shape
+    K = index.shape[1]
+    w = torch.full((T,), 1.0 / T, dtype=F64) if weights is None else weights.detach().cpu().to(F64)
+    y = torch.full((T,), -1) if targets is None or not hard else targets.detach().cpu().long()
+    valid = (index >= 0) & (index < V) & (values > -math.inf)
+    some, has = valid.any(dim=1), (y >= 0) & (y < V)
+    left = (w != 0) & (some | has)
+    h = torch.where(left[:, None], h, 0.0)
+    z = h @ W[:, :V]
+    # sums of D exact products
+    dz = (D + 2) * U32 * (h.abs() @ W[:, :V].abs())
+    v = torch.where(valid, values / tau, -math.inf)
+    mx = torch.where(some, v.amax(dim=1), 0.0)[:, None]
+    e = torch.exp(v - mx)
+    q = e / torch.where(some, e.sum(dim=1), 1.0)[:, None]
+    # exponents: a difference, its factor and the product (and log2 e in the factor); a sum of K, a quotient, K of the doubles
+    eq = torch.where(valid, (mx - v), 0.0).nan_to_num(posinf=0.0) * 4 * U32 + (2 * K + 8) * U32
+    Q = torch.zeros(T, V, dtype=F64).scatter_add_(1, torch.where(valid, index, 0), torch.where(valid, q, 0.0))
+    EQ = torch.zeros(T, V, dtype=F64).scatter_add_(1, torch.where(valid, index, 0), torch.where(valid, q * eq, 0.0))
+
+    def soft_of(scale):
+        s = z * scale
+        lse = torch.logsumexp(s, dim=1, keepdim=True)
+        p = torch.exp(s - lse)
+        span = s.amax(dim=1, keepdim=True) - s
+        # each weight: its logit, the exponent's roundings; a sum of at most 64 + V / 64 parts and their rescaling; the logarithm
+        e_lse = (p * (dz * scale + (5 * span + 8) * U32)).sum(dim=1, keepdim=True) + (V / 64 + 80) * U32 + 8 * U32 * lse.abs()
+        e_p = dz * scale + e_lse + (6 * (s.abs() + lse.abs()) + 8) * U32        # relative
+        return s, lse, p, e_lse, e_p
+
+    s, lt, pt, elt, ept = soft_of(1.0 / tau)
+    logq = torch.log(torch.where(Q > 0, Q, 1.0))
+    term = torch.where(Q > 0, logq - s + lt, 0.0)
+    kl = (Q * term).sum(dim=1)
+    ekl = (EQ * (term.abs() + 1) + Q * (dz / tau + elt + 8 * U32 * (logq.abs() + s.abs() + lt.abs()))).sum(dim=1) + (K + 8) * U32 * (Q * term.abs()).sum(dim=1)
+    s1, l1, p1, el1, ep1 = soft_of(1.0)
+    at = torch.where(has, y, 0)[:, None]
+    ce = torch.where(has, (l1 - z.gather(1, at))[:, 0], 0.0)
+    ece = torch.where(has, (el1 + dz.gather(1, at) + 4 * U32 * (l1.abs() + z.gather(1, at).abs()))[:, 0], 0.0)
+    kl, ekl, ce, ece = (torch.where(left, t, 0.0) for t in (kl, ekl, ce, ece))
+    out = {"tokens": torch.stack([kl, ce]), "tokens_err": torch.stack([ekl, ece])}
+    sums = torch.stack([(w * kl).sum(), (w * ce).sum()])
+    adds = (T / 1024 + 14) * U32
+    esums = torch.stack([(w.abs() * (ekl + adds * kl.abs())).sum(), (w.abs() * (ece + adds * ce.abs())).sum()])
+    total = soft * tau * tau * sums[0] + hard * sums[1]
+    out["loss"] = torch.cat([total[None], sums])
+    out["loss_err"] = torch.cat([(soft * tau * tau * (esums[0] + 5 * U32 * sums[0].abs()) + hard * (esums[1] + 3 * U32 * sums[1].abs()))[None], esums])
+    gs, gh = (dloss * w * soft * tau * some)[:, None], (dloss * w * hard * has)[:, None]
+    hot = torch.zeros(T, V, dtype=F64)
+    hot[torch.arange(T)[has], y[has]] = 1.0
+    G = gs * (pt - Q) + gh * (p1 - hot)
+    eG = gs.abs() * (pt * ept + EQ) + gh.abs() * p1 * ep1 + 8 * U32 * (gs.abs() * (pt + Q) + gh.abs() * (p1 + hot)) + half * G.abs()
+    G, eG = torch.where(left[:, None], G, 0.0), torch.where(left[:, None], eG, 0.0)
+    Wv = W[:, :V]
+    dh = G @ Wv.t()
+    out["dh"], out["dh_err"] = dh, eG @ Wv.abs().t() + (V + 2) * U32 * (G.abs() @ Wv.abs().t()) + half * dh.abs()
+    dW = torch.zeros_like(W)
+    dW[:, :V] = h.t() @ G
+    e = torch.zeros_like(W)
+    e[:, :V] = h.abs().t() @ eG + (T + 2) * U32 * (h.abs().t() @ G.abs())
+    out["dW"], out["dW_err"] = dW, e + (U32 if half_dw is None else half_dw) * dW.abs()
+    return out
