@@ -477,8 +477,8 @@ typedef struct {
 
 bpt_status bpt_recur_validate(const bpt_recur_config* cfg);
 
-/* What the forward keeps for the backward: the states before steps 128, 256, .. (fp32 [B, (S - 1) / 128, D]), 0 bytes for
- * S <= 128. And the workspace of bpt_recur_fwd (backward = 0) or bpt_recur_bwd (backward = 1). 0 for an invalid configuration.
+/* What the forward keeps for the backward: the states before steps 64, 128, .. (fp32 [B, (S - 1) / 64, D]), 0 bytes for
+ * S <= 64. And the workspace of bpt_recur_fwd (backward = 0) or bpt_recur_bwd (backward = 1). 0 for an invalid configuration.
  * Host-only. */
 size_t bpt_recur_saved_bytes(const bpt_recur_config* cfg);
 size_t bpt_recur_workspace_bytes(const bpt_recur_config* cfg, int backward);

@@ -176,7 +176,7 @@ hipError_t win_sinks(Dt t, const WinArgs& a, int slots, hipStream_t s);   // add
 
 // ---------------------------------------------------------------- gated linear recurrence
 constexpr int kRecurCh = 64;            // channels of a workgroup
-constexpr int kRecurKeep = 128;         // steps between the states that the forward keeps
+constexpr int kRecurKeep = 64;          // steps between the states that the forward keeps
 // Element (b, t, d) of a tensor is at b * sb + t * st + d; dy is laid out like y, dx, dr and di like x, r and i.
 struct RecurArgs {
   const void *x = nullptr, *r = nullptr, *i = nullptr, *dy = nullptr;
@@ -188,11 +188,19 @@ struct RecurArgs {
   float* saved = nullptr;               // [B, (S - 1) / kRecurKeep, D]: the states before steps kRecurKeep, 2 kRecurKeep .., or null
   const int32_t* lens = nullptr;        // [B] or null: all of S
   float* part = nullptr;                // backward: [B, recur_bwd_chunks(S), D] sums of w
-  int64_t S = 0, nchunks = 0;           // nchunks, nct: the launcher's
-  int B = 0, D = 0, nct = 0;
+  int64_t S = 0;
+  int B = 0, D = 0;
   float c = 0;
+  void* chain = nullptr;                // recur_chain_bytes of it
+  // the launcher's: chunks of a sequence and groups of them, runs of channels, parts of `chain`
+  int64_t nchunks = 0, ngroups = 0;
+  int nct = 0;
+  unsigned long long *runs = nullptr, *groups = nullptr;
+  float* k2 = nullptr;
+  uint32_t* counter = nullptr;
 };
 int64_t recur_bwd_chunks(int64_t S);
+int64_t recur_chain_bytes(RecurArgs p, int backward);   // of B, S, D
 hipError_t recur_fwd(Dt t, RecurArgs p, hipStream_t s);
 hipError_t recur_bwd(Dt t, RecurArgs p, hipStream_t s);
 hipError_t recur_dlam(const RecurArgs& p, float* dlam, hipStream_t s);

@@ -1768,7 +1768,7 @@ static bpt_status recur_check(const bpt_recur_config* c) {
   for (const bpt_recur_strides* t : {&c->x, &c->r, &c->i, &c->y}) {
     if (t->sb < 0 || t->st < 0) return fail(BPT_ERR_INVALID_ARG, "strides must be >= 0");
     if (t->sb % unit || t->st % unit) return fail(BPT_ERR_INVALID_ARG, "strides must be multiples of 16 bytes");
-    if (t->sb >= (int64_t)1 << 40 || t->st >= (int64_t)1 << 40) return fail(BPT_ERR_UNSUPPORTED, "a stride is too large");
+    if (t->sb >= (int64_t)1 << 40 || t->st >= (int64_t)1 << 21) return fail(BPT_ERR_UNSUPPORTED, "a stride is too large");
   }
   if (c->D % 8) return fail(BPT_ERR_UNSUPPORTED, "D must be a multiple of 8 (got %lld)", (long long)c->D);
   if (c->S > kAttnMax || c->D > (int64_t)1 << 20) return fail(BPT_ERR_UNSUPPORTED, "S must be <= 2^28 and D <= 2^20");
@@ -1783,11 +1783,15 @@ static int64_t recur_saved(const bpt_recur_config& c) { return c.B * ((c.S - 1) 
 
 struct RecurWs {
   float* part;           // backward: sums of w per chunk
+  void* chain;           // what the workgroups of a sequence tell one another (null: a workgroup takes a whole one)
 };
 static RecurWs recur_ws(const bpt_recur_config& c, void* base, int backward, int64_t* total) {
   Bump bp(base);
   RecurWs w{};
   if (backward) w.part = (float*)bp.take(c.B * recur_bwd_chunks(c.S) * c.D * 4);
+  RecurArgs a;
+  a.B = (int)c.B; a.S = c.S; a.D = (int)c.D;
+  if (const int64_t n = recur_chain_bytes(a, backward); n > 0) w.chain = bp.take(n);
   *total = rup(bp.off, kAlign);
   return w;
 }
@@ -1824,11 +1828,11 @@ bpt_status bpt_recur_fwd(const bpt_recur_config* cfg, const void* x, const void*
                         (const void*)saved, (const void*)ws})
     if (q && !aligned16(q)) return fail(BPT_ERR_INVALID_ARG, "pointer %p is not 16-byte aligned", q);
   int64_t need;
-  recur_ws(*cfg, ws, 0, &need);
+  const RecurWs w = recur_ws(*cfg, ws, 0, &need);
   if (need > 0 && (!ws || (int64_t)ws_bytes < need))
     return fail(BPT_ERR_WORKSPACE, "workspace %zu bytes < required %lld", ws ? ws_bytes : (size_t)0, (long long)need);
   RecurArgs a = recur_args(*cfg, x, r, i, lambda, lens, h0, saved);
-  a.y = y; a.hT = hT;
+  a.y = y; a.hT = hT; a.chain = w.chain;
   hipStream_t s = (hipStream_t)stream;
   const double n = (double)cfg->B * cfg->S * cfg->D;
   RUN("recur.fwd", 20.0 * n, 4.0 * n * esize(cfg->dtype), recur_fwd(dt_of(cfg->dtype), a, s));
@@ -1863,7 +1867,7 @@ bpt_status bpt_recur_bwd(const bpt_recur_config* cfg, const void* x, const void*
   const RecurWs w = recur_ws(*cfg, ws, 1, &need);
   if ((int64_t)ws_bytes < need) return fail(BPT_ERR_WORKSPACE, "workspace %zu bytes < required %lld", ws_bytes, (long long)need);
   RecurArgs a = recur_args(*cfg, x, r, i, lambda, lens, h0, saved);
-  a.dy = dy; a.dhT = dhT; a.dx = dx; a.dr = dr; a.di = di; a.dh0 = dh0; a.part = w.part;
+  a.dy = dy; a.dhT = dhT; a.dx = dx; a.dr = dr; a.di = di; a.dh0 = dh0; a.part = w.part; a.chain = w.chain;
   hipStream_t s = (hipStream_t)stream;
   const double n = (double)cfg->B * cfg->S * cfg->D;
   RUN("recur.bwd", 35.0 * n, 7.0 * n * esize(cfg->dtype), recur_bwd(dt_of(cfg->dtype), a, s));

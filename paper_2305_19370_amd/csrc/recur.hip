@@ -8,9 +8,15 @@
 //
 // A run of steps maps h to A h + B (A the product of its a); runs join as (A1, B1), (A2, B2) -> (A1 A2, A2 B1 + B2), and the
 // gradient's e does the same from the right. A thread takes M steps of four channels, the four threads of a wave that share the channels
-// and the waves of a workgroup join theirs, and a workgroup walks along the sequence, its state in registers. States every
-// 128 steps are kept for the backward, which rebuilds those between: y is not read again, and a bf16 y
-// costs the gradients nothing.
+// and the waves of a workgroup join theirs. States every 64 steps are kept for the backward, which rebuilds those between: y is
+// not read again, and a bf16 y costs the gradients nothing.
+//
+// Where sequences and channels alone fill the chip, a workgroup walks along its sequence, the state in registers. Elsewhere every chunk
+// of steps is a workgroup (CHAIN): it reads its steps, makes its (A, B) known, learns the state before it from those of
+// up to 15 chunks before it and the state before those, and goes on, so that elements are read once whatever the split. A word
+// that is made known holds its number and a mark in 64 bits, written and read at once: no fence is needed. Workgroups
+// draw their chunks from a counter, in order: whatever a workgroup waits for, a workgroup that has started before it gives without waiting
+// for later ones, so every wait ends. States join in the order of the steps, always the same.
 #include <algorithm>
 
 #include "common.h"
@@ -23,7 +29,7 @@ namespace {
 constexpr int kLanes = kRecurCh / 4;                 // threads of a wave side by side on the channels
 constexpr int kTs = 64 / kLanes;                     // and behind one another on the steps
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.69314718055994531f;
-constexpr int kMaxWaves = 8;
+constexpr int kMaxWaves = 8, kBwdWaves = 4;          // of a workgroup
 
 // four elements as they are in memory, and as numbers
 template <typename T> struct Raw4;
@@ -71,9 +77,82 @@ BPT_DEV float one_minus_a2(float a, float w) {
   return w > -0.0625f ? series : fmaf(-a, a, 1.0f);
 }
 
+// Keeps the compiler from forming values later, where they are used: it would hold what they are formed from, in more registers
+BPT_DEV void formed(float& x, float& y, float& z) { asm volatile("" : "+v"(x), "+v"(y), "+v"(z)); }
+
 // value of the thread `o` lanes before (after) this one; kept where there is none
 BPT_DEV float up(float v, int o) { return __shfl_up(v, (unsigned)o, 64); }
 BPT_DEV float down(float v, int o) { return __shfl_down(v, (unsigned)o, 64); }
+
+// A number and its mark, made known to (learned from) other workgroups
+typedef unsigned long long Word;
+BPT_DEV void tell(Word* p, float v) {
+  __hip_atomic_store(p, (Word)1 << 32 | __float_as_uint(v), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+BPT_DEV Word look(const Word* p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+BPT_DEV bool known(Word w) { return (w >> 32) != 0; }
+BPT_DEV float number(Word w) { return __uint_as_float((uint32_t)w); }
+
+// Chunk `at` of a chain (of one sequence and 64 channels), by one wave, a channel per lane: tells its (A, B) and returns the
+// state before it; start: the state before the chain. A group of kGroup chunks tells its last state too.
+constexpr int kGroup = 16;
+constexpr int kTries = 1 << 24;        // some ten seconds; a state that is not known by then becomes NaN
+BPT_DEV float chained(Word* run, Word* group, int lane, int at, int last, float A, float B, float start) {
+  const int pos = at % kGroup, g = at / kGroup;
+  run += (int64_t)at * 128 + lane;
+  if (pos + 1 < kGroup && at < last) {
+    tell(run, A);
+    tell(run + 64, B);
+  }
+  // the chunks of the group before this one, joined; four at a time, which is one access' time as long as they are known
+  float a = 1.0f, b = 0.0f, state = start;
+  for (int k0 = 0; k0 < pos; k0 += 4) {
+    Word wa[4], wb[4];
+    bool all = false;
+    for (int tries = 0; !all && tries < kTries; ++tries) {
+      all = true;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const Word* p = run - 128 * (int64_t)(pos - min(k0 + k, pos - 1));
+        wa[k] = look(p);
+        wb[k] = look(p + 64);
+      }
+#pragma unroll
+      for (int k = 0; k < 4; ++k) all = all && known(wa[k]) && known(wb[k]);
+      all = __all(all);
+      if (!all) __builtin_amdgcn_s_sleep(1);
+    }
+    if (!all) a = b = __builtin_nanf("");
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      if (k0 + k < pos) {
+        b = fmaf(number(wa[k]), b, number(wb[k]));
+        a *= number(wa[k]);
+      }
+  }
+  if (g > 0) {
+    const Word* p = group + (int64_t)(g - 1) * 64 + lane;
+    Word w = look(p);
+    for (int tries = 0; !__all(known(w)) && tries < kTries; ++tries) {
+      __builtin_amdgcn_s_sleep(1);
+      w = look(p);
+    }
+    state = known(w) ? number(w) : __builtin_nanf("");
+  }
+  state = fmaf(a, state, b);
+  if (pos + 1 == kGroup && at < last) tell(group + (int64_t)g * 64 + lane, fmaf(A, state, B));
+  return state;
+}
+
+// A tensor's rows of one chunk: a base that is the same for all threads and 32-bit offsets (strides are under 2^21 elements)
+template <typename T>
+struct Rows {
+  const char* base;
+  uint32_t st, col;                    // bytes
+  BPT_DEV Rows(const void* t, int64_t sb, int64_t stride, int b, int64_t first, int ch)
+      : base((const char*)t + (b * sb + first * stride) * (int64_t)sizeof(T)), st((uint32_t)stride * sizeof(T)), col((uint32_t)ch * sizeof(T)) {}
+  BPT_DEV T* at(int row) const { return (T*)(base + (uint32_t)(row * st + col)); }
+};
 
 BPT_DEV int64_t steps_of(const RecurArgs& p, int b) {
   return p.lens ? min(max((int64_t)p.lens[b], (int64_t)0), p.S) : p.S;
@@ -84,33 +163,45 @@ BPT_DEV int64_t steps_of(const RecurArgs& p, int b) {
 // ------------------------------------------------------------------ forward
 // Steps [chunk L, chunk L + L), L = waves * kTs * M. Steps behind a sequence's length leave the state as it is (a = 1, no
 // input), whatever their elements hold; their y is 0.
-template <typename T, int M>
-__global__ __launch_bounds__(64 * kMaxWaves) void recur_fwd_kernel(RecurArgs p) {
+template <typename T, int M, bool CHAIN>
+__global__ __launch_bounds__(64 * kMaxWaves, 4) void recur_fwd_kernel(RecurArgs p) {
   __shared__ __attribute__((aligned(16))) float sa[kMaxWaves][kRecurCh], sb[kMaxWaves][kRecurCh], sh[kMaxWaves][kRecurCh];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, nw = blockDim.x >> 6;
+  __shared__ uint32_t drawn;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), nw = blockDim.x >> 6;
   const int cl = lane % kLanes, ts = lane / kLanes;
   const int L = nw * kTs * M;
-  const int b = blockIdx.x / p.nct, ct = blockIdx.x % p.nct;
+  uint32_t bc = blockIdx.x;                            // sequence and channels
+  int64_t chunk = 0;
+  if constexpr (CHAIN) {
+    if (tid == 0) drawn = atomicAdd(p.counter, 1u);
+    __syncthreads();
+    const uint32_t chains = (uint32_t)(p.B * p.nct);
+    const uint32_t at = __builtin_amdgcn_readfirstlane(drawn);
+    bc = at % chains;
+    chunk = at / chains;
+  }
+  const int b = bc / p.nct, ct = bc % p.nct;
   const int ch = ct * kRecurCh + 4 * cl;               // this thread's channels
   const int chr = min(ch, p.D - 4);                    // those it reads: the last ones instead of none
   const int cw = ct * kRecurCh + lane, cwr = min(cw, p.D - 1);   // wave 0: a channel per lane
+  const int row0 = (wave * kTs + ts) * M;
   const int64_t n = steps_of(p, b);
-  const T *x = (const T*)p.x + b * p.x_sb + chr, *gr = (const T*)p.r + b * p.r_sb + chr, *gi = (const T*)p.i + b * p.i_sb + chr;
-  T* y = (T*)p.y + b * p.y_sb + chr;
   float k2[4];
 #pragma unroll
-  for (int e = 0; e < 4; ++e) k2[e] = decay2(p.lam[chr + e], p.c);
+  for (int e = 0; e < 4; ++e) k2[e] = CHAIN ? p.k2[chr + e] : decay2(p.lam[chr + e], p.c);
   float state = wave == 0 && p.h0 ? p.h0[(int64_t)b * p.D + cwr] : 0.0f;
 
-  for (int64_t chunk = 0; chunk < p.nchunks; ++chunk) {
-    const int64_t t0 = chunk * L + (wave * kTs + ts) * M;
+  do {
+    const int64_t first = chunk * L;
+    const Rows<T> x(p.x, p.x_sb, p.x_st, b, first, chr), gr(p.r, p.r_sb, p.r_st, b, first, chr), gi(p.i, p.i_sb, p.i_st, b, first, chr);
+    const int have = (int)min(max(n - first, (int64_t)0), (int64_t)L);   // steps of the chunk that exist
     Raw4<T> rx[M], rr[M], ri[M];
 #pragma unroll
     for (int j = 0; j < M; ++j) {
-      const int64_t t = min(t0 + j, max(n - 1, (int64_t)0));
-      rx[j].load(x + t * p.x_st);
-      rr[j].load(gr + t * p.r_st);
-      ri[j].load(gi + t * p.i_st);
+      const int t = max(min(row0 + j, have - 1), 0);
+      rx[j].load(x.at(t));
+      rr[j].load(gr.at(t));
+      ri[j].load(gi.at(t));
     }
     float a[M][4], u[M][4], A[4] = {1, 1, 1, 1}, B[4] = {0, 0, 0, 0};
 #pragma unroll
@@ -120,7 +211,7 @@ __global__ __launch_bounds__(64 * kMaxWaves) void recur_fwd_kernel(RecurArgs p) 
         const float l2 = k2[e] * sigma(rr[j][e]);
         const float al = __builtin_amdgcn_exp2f(l2);
         const float m = __builtin_amdgcn_sqrtf(one_minus_a2(al, 2.0f * kLn2 * l2));
-        const bool live = t0 + j < n;
+        const bool live = row0 + j < have;
         a[j][e] = live ? al : 1.0f;
         u[j][e] = live ? m * (sigma(ri[j][e]) * rx[j][e]) : 0.0f;
         B[e] = fmaf(a[j][e], B[e], u[j][e]);
@@ -148,6 +239,15 @@ __global__ __launch_bounds__(64 * kMaxWaves) void recur_fwd_kernel(RecurArgs p) 
     }
     __syncthreads();
     if (wave == 0) {
+      if constexpr (CHAIN) {
+        float At = 1.0f, Bt = 0.0f;
+        for (int w = 0; w < nw; ++w) {
+          Bt = fmaf(sa[w][lane], Bt, sb[w][lane]);
+          At *= sa[w][lane];
+        }
+        state = chained(p.runs + (int64_t)bc * p.nchunks * 128, p.groups + (int64_t)bc * p.ngroups * 64, lane, (int)chunk,
+                        (int)p.nchunks - 1, At, Bt, state);
+      }
       for (int w = 0; w < nw; ++w) {
         sh[w][lane] = state;
         const int64_t t = chunk * L + (int64_t)w * kTs * M;
@@ -169,56 +269,70 @@ __global__ __launch_bounds__(64 * kMaxWaves) void recur_fwd_kernel(RecurArgs p) 
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         h[e] = fmaf(a[j][e], h[e], u[j][e]);
-        out[e] = t0 + j < n ? h[e] : 0.0f;
+        out[e] = row0 + j < have ? h[e] : 0.0f;
       }
-      if (t0 + j < p.S && ch < p.D) store4(y + (t0 + j) * p.y_st, out);
+      if (first + row0 + j < p.S && ch < p.D) store4(Rows<T>(p.y, p.y_sb, p.y_st, b, first, ch).at(row0 + j), out);
     }
-  }
-  if (wave == 0 && p.hT && cw < p.D) p.hT[(int64_t)b * p.D + cw] = state;
+  } while (!CHAIN && ++chunk < p.nchunks);
+  if (wave == 0 && p.hT && cw < p.D && (!CHAIN || chunk == p.nchunks - 1)) p.hT[(int64_t)b * p.D + cw] = state;
 }
 
 // ------------------------------------------------------------------ backward
-// The chunks from the last one down, e in registers. States within a chunk of 128 steps from the one kept before it.
-template <typename T, int M>
-__global__ __launch_bounds__(64 * kMaxWaves) void recur_bwd_kernel(RecurArgs p) {
-  __shared__ __attribute__((aligned(16))) float sa[kMaxWaves][kRecurCh], sb[kMaxWaves][kRecurCh], se[kMaxWaves][kRecurCh];
-  __shared__ __attribute__((aligned(16))) float sh[kMaxWaves][kRecurCh], sd[kMaxWaves][kRecurCh], sw[kMaxWaves][kRecurCh];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, nw = blockDim.x >> 6;
+// The chunks from the last one down, e in registers. States within a chunk of 64 steps from the one kept before it.
+template <typename T, int M, bool CHAIN>
+__global__ __launch_bounds__(64 * kBwdWaves, 3) void recur_bwd_kernel(RecurArgs p) {
+  extern __shared__ __attribute__((aligned(16))) f32x4 keep[];   // per thread and step: factors of d in dx and di
+  __shared__ uint32_t drawn;
+  __shared__ __attribute__((aligned(16))) float sa[kBwdWaves][kRecurCh], sb[kBwdWaves][kRecurCh], se[kBwdWaves][kRecurCh];
+  __shared__ __attribute__((aligned(16))) float sh[kBwdWaves][kRecurCh], sd[kBwdWaves][kRecurCh], sw[kBwdWaves][kRecurCh];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), nw = blockDim.x >> 6;
   const int cl = lane % kLanes, ts = lane / kLanes;
   const int L = nw * kTs * M;                          // at most kRecurKeep
-  const int b = blockIdx.x / p.nct, ct = blockIdx.x % p.nct;
+  uint32_t bc = blockIdx.x;
+  int64_t chunk = p.nchunks - 1;
+  if constexpr (CHAIN) {
+    if (tid == 0) drawn = atomicAdd(p.counter, 1u);
+    __syncthreads();
+    const uint32_t chains = (uint32_t)(p.B * p.nct);
+    const uint32_t at = __builtin_amdgcn_readfirstlane(drawn);
+    bc = at % chains;
+    chunk -= at / chains;
+  }
+  const int b = bc / p.nct, ct = bc % p.nct;
   const int ch = ct * kRecurCh + 4 * cl, chr = min(ch, p.D - 4);
   const int cw = ct * kRecurCh + lane, cwr = min(cw, p.D - 1);
+  const int row0 = (wave * kTs + ts) * M;
   const int64_t n = steps_of(p, b), row = (int64_t)b * p.D + cwr, kept = (p.S - 1) / kRecurKeep;
-  const T *x = (const T*)p.x + b * p.x_sb + chr, *gr = (const T*)p.r + b * p.r_sb + chr, *gi = (const T*)p.i + b * p.i_sb + chr;
-  const T* dy = (const T*)p.dy + b * p.y_sb + chr;
-  T *dx = (T*)p.dx + b * p.x_sb + chr, *dr = (T*)p.dr + b * p.r_sb + chr, *di = (T*)p.di + b * p.i_sb + chr;
   float k2[4];
 #pragma unroll
-  for (int e = 0; e < 4; ++e) k2[e] = decay2(p.lam[chr + e], p.c);
+  for (int e = 0; e < 4; ++e) k2[e] = CHAIN ? p.k2[chr + e] : decay2(p.lam[chr + e], p.c);
   float back = wave == 0 && p.dhT ? p.dhT[row] : 0.0f;   // e of the step behind the chunk
 
-  for (int64_t chunk = p.nchunks - 1; chunk >= 0; --chunk) {
-    const int64_t t0 = chunk * L + (wave * kTs + ts) * M;
+  do {
+    const int64_t first = chunk * L;
+    const Rows<T> x(p.x, p.x_sb, p.x_st, b, first, chr), gr(p.r, p.r_sb, p.r_st, b, first, chr), gi(p.i, p.i_sb, p.i_st, b, first, chr),
+        dy(p.dy, p.y_sb, p.y_st, b, first, chr);
+    const int have = (int)min(max(n - first, (int64_t)0), (int64_t)L);
     Raw4<T> rx[M], rr[M], ri[M], ry[M];
 #pragma unroll
     for (int j = 0; j < M; ++j) {
-      const int64_t t = min(t0 + j, max(n - 1, (int64_t)0));
-      rr[j].load(gr + t * p.r_st);
-      ri[j].load(gi + t * p.i_st);
-      rx[j].load(x + t * p.x_st);
-      ry[j].load(dy + t * p.y_st);
+      const int t = max(min(row0 + j, have - 1), 0);
+      rr[j].load(gr.at(t));
+      ri[j].load(gi.at(t));
+      rx[j].load(x.at(t));
+      ry[j].load(dy.at(t));
     }
     float state = 0.0f;
     if (wave == 0) state = chunk > 0 ? p.saved[((int64_t)b * kept + chunk - 1) * p.D + cwr] : p.h0 ? p.h0[row] : 0.0f;
-    // per step: a, the state before it, dy, and the factors of d (and of d h) in the results
-    float a[M][4], h[M][4], d[M][4], l[M][4], q[M][4], r1[M][4], fx[M][4], fi[M][4];
+    // per step: a, the state before it, and the factors of d (and of d h) in the results
+    float a[M][4], h[M][4], l[M][4], q[M][4], r1[M][4];
     float A[4] = {1, 1, 1, 1}, B[4] = {0, 0, 0, 0}, E[4] = {0, 0, 0, 0};
 #pragma unroll
-    for (int j = 0; j < M; ++j)
+    for (int j = 0; j < M; ++j) {
+      float fx[4], fi[4];
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const bool live = t0 + j < n;
+        const bool live = row0 + j < have;
         float r, i, i1;
         sigma_both(rr[j][e], r, r1[j][e]);
         sigma_both(ri[j][e], i, i1);
@@ -227,19 +341,22 @@ __global__ __launch_bounds__(64 * kMaxWaves) void recur_bwd_kernel(RecurArgs p) 
         const float im = s >= 1.17549435e-38f ? __builtin_amdgcn_rsqf(s) : 0.0f, m = s * im, xe = rx[j][e], u = i * xe;
         l[j][e] = live ? kLn2 * l2 * al : 0.0f;                       // w = d (l a h - q)
         q[j][e] = live ? al * al * u * (kLn2 * l2 * im) : 0.0f;
-        fx[j][e] = live ? m * i : 0.0f;
-        fi[j][e] = live ? m * u * i1 : 0.0f;
+        fx[e] = m * i;
+        fi[e] = m * u * i1;
         a[j][e] = live ? al : 1.0f;
         h[j][e] = live ? m * u : 0.0f;
-        d[j][e] = live ? ry[j][e] : 0.0f;
-        if (!live) r1[j][e] = 0.0f;
         B[e] = fmaf(a[j][e], B[e], h[j][e]);
         A[e] *= a[j][e];
       }
+      store4((float*)(keep + (2 * j) * blockDim.x + tid), fx);
+      store4((float*)(keep + (2 * j + 1) * blockDim.x + tid), fi);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) formed(l[j][e], q[j][e], r1[j][e]);
+    }
 #pragma unroll
     for (int j = M - 1; j >= 0; --j)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) E[e] = a[j][e] * (d[j][e] + E[e]);
+      for (int e = 0; e < 4; ++e) E[e] = a[j][e] * ((row0 + j < have ? ry[j][e] : 0.0f) + E[e]);
     float Ax[4], Bx[4], Az[4], Ez[4];                  // the threads of the wave before this one, and behind it
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
@@ -270,6 +387,15 @@ __global__ __launch_bounds__(64 * kMaxWaves) void recur_bwd_kernel(RecurArgs p) 
     if (ts == 0) store4(&se[wave][4 * cl], E);
     __syncthreads();
     if (wave == 0) {
+      if constexpr (CHAIN) {
+        float At = 1.0f, Et = 0.0f;
+        for (int w = nw - 1; w >= 0; --w) {
+          Et = fmaf(sa[w][lane], Et, se[w][lane]);
+          At *= sa[w][lane];
+        }
+        back = chained(p.runs + (int64_t)bc * p.nchunks * 128, p.groups + (int64_t)bc * p.ngroups * 64, lane,
+                       (int)(p.nchunks - 1 - chunk), (int)p.nchunks - 1, At, Et, back);
+      }
       for (int w = 0; w < nw; ++w) {
         sh[w][lane] = state;
         state = fmaf(sa[w][lane], state, sb[w][lane]);
@@ -300,20 +426,22 @@ __global__ __launch_bounds__(64 * kMaxWaves) void recur_bwd_kernel(RecurArgs p) 
 #pragma unroll
     for (int j = M - 1; j >= 0; --j) {
       float ox[4], og[4], oi[4];
+      const f32x4 fx = keep[(2 * j) * blockDim.x + tid], fi = keep[(2 * j + 1) * blockDim.x + tid];
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const float g = d[j][e] + ee[e], w = t0 + j < n ? g * (l[j][e] * h[j][e] - q[j][e]) : 0.0f;
+        const float g = (row0 + j < have ? ry[j][e] : 0.0f) + ee[e], w = row0 + j < have ? g * (l[j][e] * h[j][e] - q[j][e]) : 0.0f;
         ws[e] += w;
-        og[e] = w * r1[j][e];
-        ox[e] = t0 + j < n ? g * fx[j][e] : 0.0f;
-        oi[e] = t0 + j < n ? g * fi[j][e] : 0.0f;
+        og[e] = row0 + j < have ? w * r1[j][e] : 0.0f;
+        ox[e] = row0 + j < have ? g * fx[e] : 0.0f;
+        oi[e] = row0 + j < have ? g * fi[e] : 0.0f;
         ee[e] = a[j][e] * g;
       }
-      if (t0 + j < p.S && ch < p.D) {
-        store4(dx + (t0 + j) * p.x_st, ox);
-        store4(dr + (t0 + j) * p.r_st, og);
-        store4(di + (t0 + j) * p.i_st, oi);
+      if (first + row0 + j < p.S && ch < p.D) {
+        store4(Rows<T>(p.dx, p.x_sb, p.x_st, b, first, ch).at(row0 + j), ox);
+        store4(Rows<T>(p.dr, p.r_sb, p.r_st, b, first, ch).at(row0 + j), og);
+        store4(Rows<T>(p.di, p.i_sb, p.i_st, b, first, ch).at(row0 + j), oi);
       }
+      __builtin_amdgcn_sched_barrier(0);
     }
     // sum of w over the chunk, in the order of the steps' threads and waves
 #pragma unroll
@@ -328,8 +456,16 @@ __global__ __launch_bounds__(64 * kMaxWaves) void recur_bwd_kernel(RecurArgs p) 
       for (int w = 0; w < nw; ++w) sum += sw[w][lane];
       p.part[((int64_t)b * p.nchunks + chunk) * p.D + cw] = sum;
     }
-  }
-  if (wave == 0 && p.dh0 && cw < p.D) p.dh0[row] = back;
+  } while (!CHAIN && --chunk >= 0);
+  if (wave == 0 && p.dh0 && cw < p.D && (!CHAIN || chunk == 0)) p.dh0[row] = back;
+}
+
+// Before the chained kernels: nothing is known yet, and log2 a of a fully open gate per channel
+__global__ __launch_bounds__(256) void recur_start_kernel(RecurArgs p, int64_t words) {
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, step = (int64_t)gridDim.x * 256;
+  if (i == 0) *p.counter = 0;
+  if (i < p.D) p.k2[i] = decay2(p.lam[i], p.c);
+  for (int64_t k = i; k < words / 2; k += step) ((u32x4*)p.runs)[k] = u32x4{0, 0, 0, 0};
 }
 
 // dlambda from the sums of w of the chunks, [rows, D], added in a fixed order: 16 runs of rows, then those
@@ -350,30 +486,83 @@ __global__ __launch_bounds__(1024) void recur_dlam_kernel(const float* part, int
 // ------------------------------------------------------------------ launchers
 namespace {
 constexpr int kFwdM = 8, kBwdM = 4;
-int waves_for(int64_t S, int per) { return (int)std::min<int64_t>(kMaxWaves, (S + per - 1) / per); }
+
+int64_t words_of(const RecurArgs& p) { return (int64_t)p.B * p.nct * (p.nchunks * 128 + p.ngroups * 64); }
+
+// chunks, their number of waves, and whether they are chained
+int plan(RecurArgs& p, bool backward) {
+  const int per = kTs * (backward ? kBwdM : kFwdM);
+  const int nw = (int)std::min<int64_t>(backward ? kBwdWaves : kMaxWaves, (p.S + per - 1) / per);
+  p.nct = (p.D + kRecurCh - 1) / kRecurCh;
+  p.nchunks = (p.S + nw * per - 1) / (nw * per);
+  p.ngroups = (p.nchunks + kGroup - 1) / kGroup;
+  return nw;
+}
+bool chains(const RecurArgs& p) { return p.nchunks > 1 && p.B * p.nct < 512; }
+
+hipError_t start(RecurArgs& p, hipStream_t s) {
+  p.runs = (unsigned long long*)p.chain;
+  p.groups = p.runs + (int64_t)p.B * p.nct * p.nchunks * 128;
+  p.k2 = (float*)(p.runs + words_of(p));
+  p.counter = (uint32_t*)(p.k2 + p.D);
+  const int64_t blocks = std::max<int64_t>((p.D + 255) / 256, std::min<int64_t>((words_of(p) + 511) / 512, 2048));
+  hipLaunchKernelGGL(recur_start_kernel, dim3((unsigned)blocks), dim3(256), 0, s, p, words_of(p));
+  return hipGetLastError();
+}
 }  // namespace
 
 int64_t recur_bwd_chunks(int64_t S) { return (S + kRecurKeep - 1) / kRecurKeep; }
 
+int64_t recur_chain_bytes(RecurArgs p, int backward) {
+  plan(p, backward);
+  return chains(p) ? words_of(p) * 8 + ((int64_t)p.D + 4) * 4 : 0;
+}
+
 hipError_t recur_fwd(Dt t, RecurArgs p, hipStream_t s) {
-  const int nw = waves_for(p.S, kTs * kFwdM);
-  p.nct = (p.D + kRecurCh - 1) / kRecurCh;
-  p.nchunks = (p.S + nw * kTs * kFwdM - 1) / (nw * kTs * kFwdM);
-  const dim3 grid((unsigned)(p.B * p.nct)), block((unsigned)(64 * nw));
-  if (t == F32) hipLaunchKernelGGL((recur_fwd_kernel<float, kFwdM>), grid, block, 0, s, p);
-  else hipLaunchKernelGGL((recur_fwd_kernel<bf16, kFwdM>), grid, block, 0, s, p);
+  const int nw = plan(p, false);
+  const bool chain = chains(p);
+  if (chain) {
+    const hipError_t e = start(p, s);
+    if (e != hipSuccess) return e;
+  }
+  const dim3 grid((unsigned)(p.B * p.nct * (chain ? p.nchunks : 1))), block((unsigned)(64 * nw));
+  if (t == F32) {
+    if (chain) hipLaunchKernelGGL((recur_fwd_kernel<float, kFwdM, true>), grid, block, 0, s, p);
+    else hipLaunchKernelGGL((recur_fwd_kernel<float, kFwdM, false>), grid, block, 0, s, p);
+  } else {
+    if (chain) hipLaunchKernelGGL((recur_fwd_kernel<bf16, kFwdM, true>), grid, block, 0, s, p);
+    else hipLaunchKernelGGL((recur_fwd_kernel<bf16, kFwdM, false>), grid, block, 0, s, p);
+  }
   return hipGetLastError();
 }
 
-hipError_t recur_bwd(Dt t, RecurArgs p, hipStream_t s) {
-  static_assert(kMaxWaves * kTs * kBwdM == kRecurKeep, "a chunk starts at a state that was kept");
-  const int nw = waves_for(p.S, kTs * kBwdM);
-  p.nct = (p.D + kRecurCh - 1) / kRecurCh;
-  p.nchunks = recur_bwd_chunks(p.S);
-  const dim3 grid((unsigned)(p.B * p.nct)), block((unsigned)(64 * nw));
-  if (t == F32) hipLaunchKernelGGL((recur_bwd_kernel<float, kBwdM>), grid, block, 0, s, p);
-  else hipLaunchKernelGGL((recur_bwd_kernel<bf16, kBwdM>), grid, block, 0, s, p);
+namespace {
+template <typename T, bool CHAIN>
+hipError_t launch_bwd(const RecurArgs& p, int nw, hipStream_t s) {
+  auto kern = recur_bwd_kernel<T, kBwdM, CHAIN>;
+  constexpr int most = 2 * kBwdM * 64 * kBwdWaves * 16;
+  static bool attr_set = false;
+  if (!attr_set) {
+    const hipError_t e = hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, most);
+    if (e != hipSuccess) return e;
+    attr_set = true;
+  }
+  hipLaunchKernelGGL(kern, dim3((unsigned)(p.B * p.nct * (CHAIN ? p.nchunks : 1))), dim3((unsigned)(64 * nw)),
+                     2 * kBwdM * 64 * nw * 16, s, p);
   return hipGetLastError();
+}
+}  // namespace
+
+hipError_t recur_bwd(Dt t, RecurArgs p, hipStream_t s) {
+  static_assert(kBwdWaves * kTs * kBwdM == kRecurKeep, "a chunk starts at a state that was kept");
+  const int nw = plan(p, true);
+  const bool chain = chains(p);
+  if (chain) {
+    const hipError_t e = start(p, s);
+    if (e != hipSuccess) return e;
+  }
+  if (t == F32) return chain ? launch_bwd<float, true>(p, nw, s) : launch_bwd<float, false>(p, nw, s);
+  return chain ? launch_bwd<bf16, true>(p, nw, s) : launch_bwd<bf16, false>(p, nw, s);
 }
 
 hipError_t recur_dlam(const RecurArgs& p, float* dlam, hipStream_t s) {
