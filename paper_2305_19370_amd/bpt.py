@@ -987,6 +987,15 @@ def recur_bwd(cfg: RecurConfig, x: torch.Tensor, r: torch.Tensor, i: torch.Tenso
                                 di.data_ptr(), dlp, dh0p, workspace.data_ptr(), _nbytes(workspace), stream))
 
 
+@functools.lru_cache(maxsize=1024)
+def _recur_plan(dtype: torch.dtype, shape: Tuple[int, ...], sx, sr, si, c: float):
+    """Configuration of a forward into a dense y, its bytes of saved and workspace, and the shape of the states."""
+    meta = lambda st: torch.empty_strided(shape, st, dtype=dtype, device="meta")  # noqa: E731
+    cfg = recur_config_of(meta(sx), meta(sr), meta(si), torch.empty(shape, dtype=dtype, device="meta"), c)
+    _check(recur_validate(cfg))
+    return cfg, recur_saved_bytes(cfg), recur_workspace_bytes(cfg, False), (cfg.B, cfg.D)
+
+
 class GatedRecurrence:
     """A gated linear recurrence through libbpt; allocates its buffers with torch. For one new token of each sequence, call
     forward with S = 1 and the states as h0."""
@@ -1002,12 +1011,23 @@ class GatedRecurrence:
                 lens: Optional[torch.Tensor] = None,
                 save: bool = False) -> Tuple[torch.Tensor, torch.Tensor, Optional[torch.Tensor]]:
         """y [B, S, D], the last states [B, D] (float32), and with `save` what backward takes."""
-        y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-        cfg = recur_config_of(x, r, i, y, self.c)
-        hT = torch.empty((cfg.B, cfg.D), dtype=torch.float32, device=x.device)
-        saved = self._bytes(recur_saved_bytes(cfg), x.device) if save else None
-        nb = recur_workspace_bytes(cfg, False)
-        recur_fwd(cfg, x, r, i, lam, y, h0, hT, saved, self._bytes(nb, x.device) if nb else None, lens)
+        if not x.dtype == r.dtype == i.dtype or not x.shape == r.shape == i.shape:
+            raise ValueError("x, r and i must share a type and a shape")
+        cfg, ns, nb, states = _recur_plan(x.dtype, x.shape, x.stride(), r.stride(), i.stride(), self.c)
+        dev = x.device
+        y, hT = torch.empty(x.shape, dtype=x.dtype, device=dev), torch.empty(states, dtype=torch.float32, device=dev)
+        saved = self._bytes(ns, dev) if save else None
+        ws = self._bytes(nb, dev) if nb else None
+        at = x.get_device()
+        same = at == r.get_device() == i.get_device() == lam.get_device()
+        hp = lp = None
+        if h0 is not None:
+            hp, same = _f32(h0, states, "h0"), same and h0.get_device() == at
+        if lens is not None:
+            lp, same = _int32(lens, cfg.B, "lens"), same and lens.get_device() == at
+        _check(load().bpt_recur_fwd(cfg, x.data_ptr(), r.data_ptr(), i.data_ptr(), _f32(lam, states[1:], "lam"), lp, hp, y.data_ptr(),
+                                    hT.data_ptr(), saved.data_ptr() if save and ns else None, ws.data_ptr() if nb else None, nb,
+                                    _stream_on(at, same)))
         return y, hT, saved
 
     def backward(self, x: torch.Tensor, r: torch.Tensor, i: torch.Tensor, lam: torch.Tensor, saved: torch.Tensor, dy: torch.Tensor,

@@ -277,6 +277,41 @@ __global__ __launch_bounds__(64 * kMaxWaves, 4) void recur_fwd_kernel(RecurArgs 
   if (wave == 0 && p.hT && cw < p.D && (!CHAIN || chunk == p.nchunks - 1)) p.hT[(int64_t)b * p.D + cw] = state;
 }
 
+// Few steps (new tokens of many sequences): a thread walks along the steps of four channels, and over a few sequences, for which
+// it forms the channels' decay once. Bound by the launch and one access there and back for a handful of
+// sequences, by the copy for many.
+template <typename T>
+__global__ __launch_bounds__(64) void recur_few_kernel(RecurArgs p, int per) {
+  const int ch = blockIdx.x * 256 + 4 * (int)threadIdx.x;
+  if (ch >= p.D) return;
+  float k2[4];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) k2[e] = decay2(p.lam[ch + e], p.c);
+  const int b0 = blockIdx.y * per, b1 = min(b0 + per, p.B);
+  for (int b = b0; b < b1; ++b) {
+    const int n = (int)steps_of(p, b);
+    f32x4 h = {0, 0, 0, 0};
+    if (p.h0) h = *(const f32x4*)(p.h0 + (int64_t)b * p.D + ch);
+    for (int t = 0; t < (int)p.S; ++t) {
+      Raw4<T> rx, rr, ri;
+      rx.load((const T*)p.x + b * p.x_sb + t * p.x_st + ch);
+      rr.load((const T*)p.r + b * p.r_sb + t * p.r_st + ch);
+      ri.load((const T*)p.i + b * p.i_sb + t * p.i_st + ch);
+      float out[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float l2 = k2[e] * sigma(rr[e]), a = __builtin_amdgcn_exp2f(l2);
+        const float m = __builtin_amdgcn_sqrtf(one_minus_a2(a, 2.0f * kLn2 * l2));
+        const float next = fmaf(a, h[e], m * (sigma(ri[e]) * rx[e]));
+        h[e] = t < n ? next : h[e];
+        out[e] = t < n ? next : 0.0f;
+      }
+      store4((T*)p.y + b * p.y_sb + t * p.y_st + ch, out);
+    }
+    if (p.hT) *(f32x4*)(p.hT + (int64_t)b * p.D + ch) = h;
+  }
+}
+
 // ------------------------------------------------------------------ backward
 // The chunks from the last one down, e in registers. States within a chunk of 64 steps from the one kept before it.
 template <typename T, int M, bool CHAIN>
@@ -486,6 +521,7 @@ __global__ __launch_bounds__(1024) void recur_dlam_kernel(const float* part, int
 // ------------------------------------------------------------------ launchers
 namespace {
 constexpr int kFwdM = 8, kBwdM = 4;
+constexpr int kFewSteps = 8;           // of the forward in which a thread walks alone
 
 int64_t words_of(const RecurArgs& p) { return (int64_t)p.B * p.nct * (p.nchunks * 128 + p.ngroups * 64); }
 
@@ -519,6 +555,13 @@ int64_t recur_chain_bytes(RecurArgs p, int backward) {
 }
 
 hipError_t recur_fwd(Dt t, RecurArgs p, hipStream_t s) {
+  if (p.S <= kFewSteps) {
+    const int gx = (p.D + 255) / 256, per = std::max((int)(((int64_t)p.B * gx + 8191) / 8192), (p.B + 65534) / 65535);
+    const dim3 grid((unsigned)gx, (unsigned)((p.B + per - 1) / per));
+    if (t == F32) hipLaunchKernelGGL((recur_few_kernel<float>), grid, dim3(64), 0, s, p, per);
+    else hipLaunchKernelGGL((recur_few_kernel<bf16>), grid, dim3(64), 0, s, p, per);
+    return hipGetLastError();
+  }
   const int nw = plan(p, false);
   const bool chain = chains(p);
   if (chain) {
