@@ -187,7 +187,7 @@ struct RecurArgs {
   float *hT = nullptr, *dh0 = nullptr;  // [B, D] or null; may be h0, dhT
   float* saved = nullptr;               // [B, (S - 1) / kRecurKeep, D]: the states before steps kRecurKeep, 2 kRecurKeep .., or null
   const int32_t* lens = nullptr;        // [B] or null: all of S
-  float* part = nullptr;                // backward: [B, recur_bwd_chunks(S), D] sums of w
+  float* part = nullptr;                // backward: [B, recur_bwd_chunks(S), D] dlambda of each chunk
   int64_t S = 0;
   int B = 0, D = 0;
   float c = 0;
@@ -196,14 +196,15 @@ struct RecurArgs {
   int64_t nchunks = 0, ngroups = 0;
   int nct = 0;
   unsigned long long *runs = nullptr, *groups = nullptr;
-  float* k2 = nullptr;
+  float *k2 = nullptr, *ratio = nullptr;
   uint32_t* counter = nullptr;
 };
 int64_t recur_bwd_chunks(int64_t S);
-int64_t recur_chain_bytes(RecurArgs p, int backward);   // of B, S, D
+int64_t recur_chain_bytes(Dt t, RecurArgs p, int backward);   // of B, S, D
 hipError_t recur_fwd(Dt t, RecurArgs p, hipStream_t s);
 hipError_t recur_bwd(Dt t, RecurArgs p, hipStream_t s);
-hipError_t recur_dlam(const RecurArgs& p, float* dlam, hipStream_t s);
+int64_t recur_dlam_floats(int64_t rows, int64_t D);   // of `partial`
+hipError_t recur_dlam(const RecurArgs& p, float* dlam, float* partial, hipStream_t s);   // adds p.part up
 
 // ---------------------------------------------------------------- rotary positions
 struct RopeArgs {

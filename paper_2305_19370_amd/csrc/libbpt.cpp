@@ -1772,9 +1772,9 @@ static bpt_status recur_check(const bpt_recur_config* c) {
   }
   if (c->D % 8) return fail(BPT_ERR_UNSUPPORTED, "D must be a multiple of 8 (got %lld)", (long long)c->D);
   if (c->S > kAttnMax || c->D > (int64_t)1 << 20) return fail(BPT_ERR_UNSUPPORTED, "S must be <= 2^28 and D <= 2^20");
-  // workgroups of a launch, 512 threads each
-  if (c->B > (int64_t)1 << 22 || c->B * ((c->D + kRecurCh - 1) / kRecurCh) > (int64_t)1 << 22)
-    return fail(BPT_ERR_UNSUPPORTED, "B * D too large");
+  // workgroups of a launch: 256 threads for 64 channels of 64 steps
+  const int64_t chunks = (c->S + kRecurKeep - 1) / kRecurKeep * ((c->D + kRecurCh - 1) / kRecurCh);
+  if (c->B > (int64_t)1 << 24 || c->B * chunks >= (int64_t)1 << 24) return fail(BPT_ERR_UNSUPPORTED, "B * S * D too large");
   if (!apart({c->y.sb, c->y.st, 0}, c->B, c->S, 1, c->D)) return fail(BPT_ERR_INVALID_ARG, "strides of y overlap");
   return BPT_OK;
 }
@@ -1782,16 +1782,20 @@ static bpt_status recur_check(const bpt_recur_config* c) {
 static int64_t recur_saved(const bpt_recur_config& c) { return c.B * ((c.S - 1) / kRecurKeep) * c.D * 4; }
 
 struct RecurWs {
-  float* part;           // backward: sums of w per chunk
-  void* chain;           // what the workgroups of a sequence tell one another (null: a workgroup takes a whole one)
+  float *part, *partial; // backward: dlambda of each chunk, and sums of those
+  void* chain;           // what the workgroups of a sequence tell one another (null: one workgroup takes it whole)
 };
 static RecurWs recur_ws(const bpt_recur_config& c, void* base, int backward, int64_t* total) {
   Bump bp(base);
   RecurWs w{};
-  if (backward) w.part = (float*)bp.take(c.B * recur_bwd_chunks(c.S) * c.D * 4);
+  if (backward) {
+    const int64_t rows = c.B * recur_bwd_chunks(c.S);
+    w.part = (float*)bp.take(rows * c.D * 4);
+    w.partial = (float*)bp.take(recur_dlam_floats(rows, c.D) * 4);
+  }
   RecurArgs a;
   a.B = (int)c.B; a.S = c.S; a.D = (int)c.D;
-  if (const int64_t n = recur_chain_bytes(a, backward); n > 0) w.chain = bp.take(n);
+  if (const int64_t n = recur_chain_bytes(dt_of(c.dtype), a, backward); n > 0) w.chain = bp.take(n);
   *total = rup(bp.off, kAlign);
   return w;
 }
@@ -1871,7 +1875,7 @@ bpt_status bpt_recur_bwd(const bpt_recur_config* cfg, const void* x, const void*
   hipStream_t s = (hipStream_t)stream;
   const double n = (double)cfg->B * cfg->S * cfg->D;
   RUN("recur.bwd", 35.0 * n, 7.0 * n * esize(cfg->dtype), recur_bwd(dt_of(cfg->dtype), a, s));
-  if (dlambda) RUN("recur.dlambda", 0, (double)cfg->B * recur_bwd_chunks(cfg->S) * cfg->D * 4, recur_dlam(a, dlambda, s));
+  if (dlambda) RUN("recur.dlambda", 0, (double)cfg->B * recur_bwd_chunks(cfg->S) * cfg->D * 4, recur_dlam(a, dlambda, w.partial, s));
   return BPT_OK;
 }
 

@@ -11,13 +11,13 @@
 // and the waves of a workgroup join theirs. States every 64 steps are kept for the backward, which rebuilds those between: y is
 // not read again, and a bf16 y costs the gradients nothing.
 //
-// Where sequences and channels alone fill the chip, a workgroup walks along its sequence, the state in registers. Elsewhere every chunk
-// of steps is a workgroup (CHAIN): it reads its steps, makes its (A, B) known, learns the state before it from those of
-// up to 15 chunks before it and the state before those, and goes on, so that elements are read once whatever the split. A word
+// Every chunk of steps is a workgroup: it reads its steps, makes its (A, B) known, learns the state before it from those of up to 15
+// chunks before it and the state before those, and goes on, so that elements are read once whatever the split. A word
 // that is made known holds its number and a mark in 64 bits, written and read at once: no fence is needed. Workgroups
 // draw their chunks from a counter, in order: whatever a workgroup waits for, a workgroup that has started before it gives without waiting
 // for later ones, so every wait ends. States join in the order of the steps, always the same.
 #include <algorithm>
+#include <type_traits>
 
 #include "common.h"
 #include "internal.h"
@@ -29,7 +29,7 @@ namespace {
 constexpr int kLanes = kRecurCh / 4;                 // threads of a wave side by side on the channels
 constexpr int kTs = 64 / kLanes;                     // and behind one another on the steps
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.69314718055994531f;
-constexpr int kMaxWaves = 8, kBwdWaves = 4;          // of a workgroup
+constexpr int kFwdWaves = 4, kBwdWaves = 4;          // of a workgroup
 
 // four elements as they are in memory, and as numbers
 template <typename T> struct Raw4;
@@ -64,17 +64,20 @@ BPT_DEV float sigma_over_softplus(float lam) {
 }
 
 BPT_DEV float sigma(float g) { return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-kLog2e * g)); }
-// sigma(g) and sigma(-g), both to a few units of their last place
+// sigma(g) and sigma(-g), both to a few units of their last place; far below 0, where e is infinite, both 0: all that the second
+// one multiplies has the first as a factor
 BPT_DEV void sigma_both(float g, float& s, float& rest) {
-  const float e = __builtin_amdgcn_exp2f(-kLog2e * fabsf(g)), q = __builtin_amdgcn_rcpf(1.0f + e), p = e * q;
-  s = g >= 0.0f ? q : p;
-  rest = g >= 0.0f ? p : q;
+  const float e = __builtin_amdgcn_exp2f(-kLog2e * g);
+  s = __builtin_amdgcn_rcpf(1.0f + e);
+  rest = s * fminf(e, 3.0e38f);                        // not 0 times infinity; a NaN stays one in s
 }
-// 1 - a^2 for a = e^l, w = 2 l <= 0: near 0 the series of -expm1, whose next term is under 2^-29 of it; a^2 carries 2^-22 of
-// 1, so the difference is good to 2^-18 where the series ends
-BPT_DEV float one_minus_a2(float a, float w) {
-  const float series = -w * fmaf(w, fmaf(w, fmaf(w, fmaf(w, 1.0f / 120.0f, 1.0f / 24.0f), 1.0f / 6.0f), 0.5f), 1.0f);
-  return w > -0.0625f ? series : fmaf(-a, a, 1.0f);
+// 1 - a^2 for a = 2^l2, l2 <= 0: where a^2 > 15/16 the series of 1 - e^w, w = 2 ln(2) l2, whose next term is under 2^-29 of it;
+// a^2 carries 2^-22 of 1, so the difference is good to 2^-18 where the series ends
+BPT_DEV float one_minus_a2(float a, float l2) {
+  constexpr float c = 2.0f * kLn2;
+  const float series = l2 * fmaf(l2, fmaf(l2, fmaf(l2, fmaf(l2, -c * c * c * c * c / 120.0f, -c * c * c * c / 24.0f), -c * c * c / 6.0f),
+                                          -c * c / 2.0f), -c);
+  return l2 > -0.0625f / c ? series : fmaf(-a, a, 1.0f);
 }
 
 // Keeps the compiler from forming values later, where they are used: it would hold what they are formed from, in more registers
@@ -164,14 +167,14 @@ BPT_DEV int64_t steps_of(const RecurArgs& p, int b) {
 // Steps [chunk L, chunk L + L), L = waves * kTs * M. Steps behind a sequence's length leave the state as it is (a = 1, no
 // input), whatever their elements hold; their y is 0.
 template <typename T, int M, bool CHAIN>
-__global__ __launch_bounds__(64 * kMaxWaves, 4) void recur_fwd_kernel(RecurArgs p) {
-  __shared__ __attribute__((aligned(16))) float sa[kMaxWaves][kRecurCh], sb[kMaxWaves][kRecurCh], sh[kMaxWaves][kRecurCh];
+__global__ __launch_bounds__(64 * kFwdWaves, CHAIN ? 3 : 2) void recur_fwd_kernel(RecurArgs p) {
+  __shared__ __attribute__((aligned(16))) float sa[kFwdWaves][kRecurCh], sb[kFwdWaves][kRecurCh], sh[kFwdWaves][kRecurCh];
   __shared__ uint32_t drawn;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), nw = blockDim.x >> 6;
   const int cl = lane % kLanes, ts = lane / kLanes;
   const int L = nw * kTs * M;
   uint32_t bc = blockIdx.x;                            // sequence and channels
-  int64_t chunk = 0;
+  int64_t chunk = 0;                                   // the only one, unless CHAIN
   if constexpr (CHAIN) {
     if (tid == 0) drawn = atomicAdd(p.counter, 1u);
     __syncthreads();
@@ -191,90 +194,99 @@ __global__ __launch_bounds__(64 * kMaxWaves, 4) void recur_fwd_kernel(RecurArgs 
   for (int e = 0; e < 4; ++e) k2[e] = CHAIN ? p.k2[chr + e] : decay2(p.lam[chr + e], p.c);
   float state = wave == 0 && p.h0 ? p.h0[(int64_t)b * p.D + cwr] : 0.0f;
 
-  do {
-    const int64_t first = chunk * L;
-    const Rows<T> x(p.x, p.x_sb, p.x_st, b, first, chr), gr(p.r, p.r_sb, p.r_st, b, first, chr), gi(p.i, p.i_sb, p.i_st, b, first, chr);
-    const int have = (int)min(max(n - first, (int64_t)0), (int64_t)L);   // steps of the chunk that exist
-    Raw4<T> rx[M], rr[M], ri[M];
+  const int64_t first = chunk * L;
+  const Rows<T> x(p.x, p.x_sb, p.x_st, b, first, chr), gr(p.r, p.r_sb, p.r_st, b, first, chr), gi(p.i, p.i_sb, p.i_st, b, first, chr);
+  const int have = (int)min(max(n - first, (int64_t)0), (int64_t)L);   // steps of the chunk that exist
+  Raw4<T> rx[M], rr[M], ri[M];
 #pragma unroll
-    for (int j = 0; j < M; ++j) {
-      const int t = max(min(row0 + j, have - 1), 0);
-      rx[j].load(x.at(t));
-      rr[j].load(gr.at(t));
-      ri[j].load(gi.at(t));
-    }
-    float a[M][4], u[M][4], A[4] = {1, 1, 1, 1}, B[4] = {0, 0, 0, 0};
+  for (int j = 0; j < M; ++j) {
+    const int t = max(min(row0 + j, have - 1), 0);
+    rx[j].load(x.at(t));
+    rr[j].load(gr.at(t));
+    ri[j].load(gi.at(t));
+  }
+  float a[M][4], u[M][4], A[4] = {1, 1, 1, 1}, B[4] = {0, 0, 0, 0};
+  auto form = [&](auto whole) {
 #pragma unroll
     for (int j = 0; j < M; ++j)
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         const float l2 = k2[e] * sigma(rr[j][e]);
-        const float al = __builtin_amdgcn_exp2f(l2);
-        const float m = __builtin_amdgcn_sqrtf(one_minus_a2(al, 2.0f * kLn2 * l2));
-        const bool live = row0 + j < have;
-        a[j][e] = live ? al : 1.0f;
-        u[j][e] = live ? m * (sigma(ri[j][e]) * rx[j][e]) : 0.0f;
-        B[e] = fmaf(a[j][e], B[e], u[j][e]);
-        A[e] *= a[j][e];
-      }
-    // the threads before this one in the wave, then the waves before this one
-    float Ax[4], Bx[4];
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-#pragma unroll
-      for (int o = kLanes; o < 64; o *= 2) {
-        const float A1 = up(A[e], o), B1 = up(B[e], o);
-        if (lane >= o) {
-          B[e] = fmaf(A[e], B1, B[e]);
-          A[e] *= A1;
+        a[j][e] = __builtin_amdgcn_exp2f(l2);
+        u[j][e] = __builtin_amdgcn_sqrtf(one_minus_a2(a[j][e], l2)) * (sigma(ri[j][e]) * rx[j][e]);
+        if constexpr (!decltype(whole)::value) {
+          const bool live = row0 + j < have;
+          a[j][e] = live ? a[j][e] : 1.0f;
+          u[j][e] = live ? u[j][e] : 0.0f;
         }
+        B[e] = j ? fmaf(a[j][e], B[e], u[j][e]) : u[j][e];
+        A[e] = j ? A[e] * a[j][e] : a[j][e];
       }
-      Ax[e] = up(A[e], kLanes);
-      Bx[e] = up(B[e], kLanes);
-      if (ts == 0) Ax[e] = 1.0f, Bx[e] = 0.0f;
-    }
-    if (ts == kTs - 1) {
-      store4(&sa[wave][4 * cl], A);
-      store4(&sb[wave][4 * cl], B);
-    }
-    __syncthreads();
-    if (wave == 0) {
-      if constexpr (CHAIN) {
-        float At = 1.0f, Bt = 0.0f;
-        for (int w = 0; w < nw; ++w) {
-          Bt = fmaf(sa[w][lane], Bt, sb[w][lane]);
-          At *= sa[w][lane];
-        }
-        state = chained(p.runs + (int64_t)bc * p.nchunks * 128, p.groups + (int64_t)bc * p.ngroups * 64, lane, (int)chunk,
-                        (int)p.nchunks - 1, At, Bt, state);
+  };
+  if (have == L) form(std::true_type{});
+  else form(std::false_type{});
+  // the threads before this one in the wave, then the waves before this one
+  float Ax[4], Bx[4];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+#pragma unroll
+    for (int o = kLanes; o < 64; o *= 2) {
+      const float A1 = up(A[e], o), B1 = up(B[e], o);
+      if (lane >= o) {
+        B[e] = fmaf(A[e], B1, B[e]);
+        A[e] *= A1;
       }
+    }
+    Ax[e] = up(A[e], kLanes);
+    Bx[e] = up(B[e], kLanes);
+    if (ts == 0) Ax[e] = 1.0f, Bx[e] = 0.0f;
+  }
+  if (ts == kTs - 1) {
+    store4(&sa[wave][4 * cl], A);
+    store4(&sb[wave][4 * cl], B);
+  }
+  __syncthreads();
+  if (wave == 0) {
+    if constexpr (CHAIN) {
+      float At = 1.0f, Bt = 0.0f;
       for (int w = 0; w < nw; ++w) {
-        sh[w][lane] = state;
-        const int64_t t = chunk * L + (int64_t)w * kTs * M;
-        if (p.saved && t % kRecurKeep == 0 && t > 0 && t < p.S && cw < p.D)
-          p.saved[((int64_t)b * ((p.S - 1) / kRecurKeep) + t / kRecurKeep - 1) * p.D + cw] = state;
-        state = fmaf(sa[w][lane], state, sb[w][lane]);
+        Bt = fmaf(sa[w][lane], Bt, sb[w][lane]);
+        At *= sa[w][lane];
       }
+      state = chained(p.runs + (int64_t)bc * p.nchunks * 128, p.groups + (int64_t)bc * p.ngroups * 64, lane, (int)chunk,
+                      (int)p.nchunks - 1, At, Bt, state);
     }
-    __syncthreads();
-    float h[4];
-    {
-      const f32x4 hw = *(const f32x4*)&sh[wave][4 * cl];
+    for (int w = 0; w < nw; ++w) {
+      sh[w][lane] = state;
+      const int64_t t = chunk * L + (int64_t)w * kTs * M;
+      if (p.saved && t % kRecurKeep == 0 && t > 0 && t < p.S && cw < p.D)
+        p.saved[((int64_t)b * ((p.S - 1) / kRecurKeep) + t / kRecurKeep - 1) * p.D + cw] = state;
+      state = fmaf(sa[w][lane], state, sb[w][lane]);
+    }
+  }
+  __syncthreads();
+  float h[4];
+  {
+    const f32x4 hw = *(const f32x4*)&sh[wave][4 * cl];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) h[e] = fmaf(Ax[e], hw[e], Bx[e]);
-    }
+    for (int e = 0; e < 4; ++e) h[e] = fmaf(Ax[e], hw[e], Bx[e]);
+  }
+  const Rows<T> y(p.y, p.y_sb, p.y_st, b, first, ch);
+  auto give = [&](auto whole) {
 #pragma unroll
     for (int j = 0; j < M; ++j) {
       float out[4];
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         h[e] = fmaf(a[j][e], h[e], u[j][e]);
-        out[e] = row0 + j < have ? h[e] : 0.0f;
+        out[e] = decltype(whole)::value || row0 + j < have ? h[e] : 0.0f;
       }
-      if (first + row0 + j < p.S && ch < p.D) store4(Rows<T>(p.y, p.y_sb, p.y_st, b, first, ch).at(row0 + j), out);
+      if ((decltype(whole)::value || first + row0 + j < p.S) && ch < p.D) store4(y.at(row0 + j), out);
     }
-  } while (!CHAIN && ++chunk < p.nchunks);
-  if (wave == 0 && p.hT && cw < p.D && (!CHAIN || chunk == p.nchunks - 1)) p.hT[(int64_t)b * p.D + cw] = state;
+  };
+  if (have == L) give(std::true_type{});
+  else give(std::false_type{});
+  if (wave == 0 && p.hT && cw < p.D && chunk == p.nchunks - 1) p.hT[(int64_t)b * p.D + cw] = state;
 }
 
 // Few steps (new tokens of many sequences): a thread walks along the steps of four channels, and over a few sequences, for which
@@ -301,7 +313,7 @@ __global__ __launch_bounds__(64) void recur_few_kernel(RecurArgs p, int per) {
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         const float l2 = k2[e] * sigma(rr[e]), a = __builtin_amdgcn_exp2f(l2);
-        const float m = __builtin_amdgcn_sqrtf(one_minus_a2(a, 2.0f * kLn2 * l2));
+        const float m = __builtin_amdgcn_sqrtf(one_minus_a2(a, l2));
         const float next = fmaf(a, h[e], m * (sigma(ri[e]) * rx[e]));
         h[e] = t < n ? next : h[e];
         out[e] = t < n ? next : 0.0f;
@@ -313,9 +325,9 @@ __global__ __launch_bounds__(64) void recur_few_kernel(RecurArgs p, int per) {
 }
 
 // ------------------------------------------------------------------ backward
-// The chunks from the last one down, e in registers. States within a chunk of 64 steps from the one kept before it.
+// The chunks from the last one down. States within a chunk of 64 steps from the one kept before it.
 template <typename T, int M, bool CHAIN>
-__global__ __launch_bounds__(64 * kBwdWaves, 3) void recur_bwd_kernel(RecurArgs p) {
+__global__ __launch_bounds__(64 * kBwdWaves, sizeof(T) == 4 ? 2 : 3) void recur_bwd_kernel(RecurArgs p) {
   extern __shared__ __attribute__((aligned(16))) f32x4 keep[];   // per thread and step: factors of d in dx and di
   __shared__ uint32_t drawn;
   __shared__ __attribute__((aligned(16))) float sa[kBwdWaves][kRecurCh], sb[kBwdWaves][kRecurCh], se[kBwdWaves][kRecurCh];
@@ -324,14 +336,14 @@ __global__ __launch_bounds__(64 * kBwdWaves, 3) void recur_bwd_kernel(RecurArgs 
   const int cl = lane % kLanes, ts = lane / kLanes;
   const int L = nw * kTs * M;                          // at most kRecurKeep
   uint32_t bc = blockIdx.x;
-  int64_t chunk = p.nchunks - 1;
+  int64_t chunk = 0;
   if constexpr (CHAIN) {
     if (tid == 0) drawn = atomicAdd(p.counter, 1u);
     __syncthreads();
     const uint32_t chains = (uint32_t)(p.B * p.nct);
     const uint32_t at = __builtin_amdgcn_readfirstlane(drawn);
     bc = at % chains;
-    chunk -= at / chains;
+    chunk = p.nchunks - 1 - at / chains;
   }
   const int b = bc / p.nct, ct = bc % p.nct;
   const int ch = ct * kRecurCh + 4 * cl, chr = min(ch, p.D - 4);
@@ -343,45 +355,49 @@ __global__ __launch_bounds__(64 * kBwdWaves, 3) void recur_bwd_kernel(RecurArgs 
   for (int e = 0; e < 4; ++e) k2[e] = CHAIN ? p.k2[chr + e] : decay2(p.lam[chr + e], p.c);
   float back = wave == 0 && p.dhT ? p.dhT[row] : 0.0f;   // e of the step behind the chunk
 
-  do {
-    const int64_t first = chunk * L;
-    const Rows<T> x(p.x, p.x_sb, p.x_st, b, first, chr), gr(p.r, p.r_sb, p.r_st, b, first, chr), gi(p.i, p.i_sb, p.i_st, b, first, chr),
-        dy(p.dy, p.y_sb, p.y_st, b, first, chr);
-    const int have = (int)min(max(n - first, (int64_t)0), (int64_t)L);
-    Raw4<T> rx[M], rr[M], ri[M], ry[M];
+  const int64_t first = chunk * L;
+  const Rows<T> x(p.x, p.x_sb, p.x_st, b, first, chr), gr(p.r, p.r_sb, p.r_st, b, first, chr), gi(p.i, p.i_sb, p.i_st, b, first, chr),
+      dy(p.dy, p.y_sb, p.y_st, b, first, chr);
+  const int have = (int)min(max(n - first, (int64_t)0), (int64_t)L);
+  Raw4<T> rx[M], rr[M], ri[M], ry[M];
 #pragma unroll
-    for (int j = 0; j < M; ++j) {
-      const int t = max(min(row0 + j, have - 1), 0);
-      rr[j].load(gr.at(t));
-      ri[j].load(gi.at(t));
-      rx[j].load(x.at(t));
-      ry[j].load(dy.at(t));
-    }
-    float state = 0.0f;
-    if (wave == 0) state = chunk > 0 ? p.saved[((int64_t)b * kept + chunk - 1) * p.D + cwr] : p.h0 ? p.h0[row] : 0.0f;
-    // per step: a, the state before it, and the factors of d (and of d h) in the results
-    float a[M][4], h[M][4], l[M][4], q[M][4], r1[M][4];
-    float A[4] = {1, 1, 1, 1}, B[4] = {0, 0, 0, 0}, E[4] = {0, 0, 0, 0};
+  for (int j = 0; j < M; ++j) {
+    const int t = max(min(row0 + j, have - 1), 0);
+    rr[j].load(gr.at(t));
+    ri[j].load(gi.at(t));
+    rx[j].load(x.at(t));
+    ry[j].load(dy.at(t));
+  }
+  float state = 0.0f;
+  if (wave == 0) state = chunk > 0 ? p.saved[((int64_t)b * kept + chunk - 1) * p.D + cwr] : p.h0 ? p.h0[row] : 0.0f;
+  // per step: a, the state before it, and the factors of d (and of d h) in the results
+  float a[M][4], h[M][4], l[M][4], q[M][4], r1[M][4];
+  float A[4], B[4], E[4];
+  auto form = [&](auto whole) {
 #pragma unroll
     for (int j = 0; j < M; ++j) {
       float fx[4], fi[4];
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const bool live = row0 + j < have;
         float r, i, i1;
         sigma_both(rr[j][e], r, r1[j][e]);
         sigma_both(ri[j][e], i, i1);
-        const float l2 = k2[e] * r, al = __builtin_amdgcn_exp2f(l2), s = one_minus_a2(al, 2.0f * kLn2 * l2);
+        const float l2 = k2[e] * r, al = __builtin_amdgcn_exp2f(l2), s = one_minus_a2(al, l2);
         // 1 / m; an s below the normal numbers counts as 0 (m < 2^-63): l / m is smaller still
-        const float im = s >= 1.17549435e-38f ? __builtin_amdgcn_rsqf(s) : 0.0f, m = s * im, xe = rx[j][e], u = i * xe;
-        l[j][e] = live ? kLn2 * l2 * al : 0.0f;                       // w = d (l a h - q)
-        q[j][e] = live ? al * al * u * (kLn2 * l2 * im) : 0.0f;
-        fx[e] = m * i;
-        fi[e] = m * u * i1;
-        a[j][e] = live ? al : 1.0f;
-        h[j][e] = live ? m * u : 0.0f;
-        B[e] = fmaf(a[j][e], B[e], h[j][e]);
-        A[e] *= a[j][e];
+        const float im = s >= 1.17549435e-38f ? __builtin_amdgcn_rsqf(s) : 0.0f, v = i * rx[j][e] * im;
+        a[j][e] = al;
+        h[j][e] = s * v;                             // m u
+        l[j][e] = kLn2 * l2 * al;                    // w = d (l a h - q)
+        q[j][e] = al * (kLn2 * l2 * al) * v;
+        fx[e] = s * im * i;
+        fi[e] = h[j][e] * i1;
+        if constexpr (!decltype(whole)::value) {
+          const bool live = row0 + j < have;
+          a[j][e] = live ? a[j][e] : 1.0f;
+          h[j][e] = live ? h[j][e] : 0.0f;
+        }
+        B[e] = j ? fmaf(a[j][e], B[e], h[j][e]) : h[j][e];
+        A[e] = j ? A[e] * a[j][e] : a[j][e];
       }
       store4((float*)(keep + (2 * j) * blockDim.x + tid), fx);
       store4((float*)(keep + (2 * j + 1) * blockDim.x + tid), fi);
@@ -391,65 +407,73 @@ __global__ __launch_bounds__(64 * kBwdWaves, 3) void recur_bwd_kernel(RecurArgs 
 #pragma unroll
     for (int j = M - 1; j >= 0; --j)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) E[e] = a[j][e] * ((row0 + j < have ? ry[j][e] : 0.0f) + E[e]);
-    float Ax[4], Bx[4], Az[4], Ez[4];                  // the threads of the wave before this one, and behind it
+      for (int e = 0; e < 4; ++e) {
+        const float d = decltype(whole)::value || row0 + j < have ? ry[j][e] : 0.0f;
+        E[e] = a[j][e] * (j < M - 1 ? d + E[e] : d);
+      }
+  };
+  if (have == L) form(std::true_type{});
+  else form(std::false_type{});
+  float Ax[4], Bx[4], Az[4], Ez[4];                  // the threads of the wave before this one, and behind it
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    float Ad = A[e];
+#pragma unroll
+    for (int o = kLanes; o < 64; o *= 2) {
+      const float A1 = up(A[e], o), B1 = up(B[e], o), A2 = down(Ad, o), E2 = down(E[e], o);
+      if (lane >= o) {
+        B[e] = fmaf(A[e], B1, B[e]);
+        A[e] *= A1;
+      }
+      if (lane < 64 - o) {
+        E[e] = fmaf(Ad, E2, E[e]);
+        Ad *= A2;
+      }
+    }
+    Ax[e] = up(A[e], kLanes);
+    Bx[e] = up(B[e], kLanes);
+    Az[e] = down(Ad, kLanes);
+    Ez[e] = down(E[e], kLanes);
+    if (ts == 0) Ax[e] = 1.0f, Bx[e] = 0.0f;
+    if (ts == kTs - 1) Az[e] = 1.0f, Ez[e] = 0.0f;
+  }
+  if (ts == kTs - 1) {
+    store4(&sa[wave][4 * cl], A);
+    store4(&sb[wave][4 * cl], B);
+  }
+  if (ts == 0) store4(&se[wave][4 * cl], E);
+  __syncthreads();
+  if (wave == 0) {
+    if constexpr (CHAIN) {
+      float At = 1.0f, Et = 0.0f;
+      for (int w = nw - 1; w >= 0; --w) {
+        Et = fmaf(sa[w][lane], Et, se[w][lane]);
+        At *= sa[w][lane];
+      }
+      back = chained(p.runs + (int64_t)bc * p.nchunks * 128, p.groups + (int64_t)bc * p.ngroups * 64, lane,
+                     (int)(p.nchunks - 1 - chunk), (int)p.nchunks - 1, At, Et, back);
+    }
+    for (int w = 0; w < nw; ++w) {
+      sh[w][lane] = state;
+      state = fmaf(sa[w][lane], state, sb[w][lane]);
+    }
+    for (int w = nw - 1; w >= 0; --w) {
+      sd[w][lane] = back;
+      back = fmaf(sa[w][lane], back, se[w][lane]);
+    }
+  }
+  __syncthreads();
+  float hh[4], ee[4], ws[4] = {0, 0, 0, 0};
+  {
+    const f32x4 hw = *(const f32x4*)&sh[wave][4 * cl], ew = *(const f32x4*)&sd[wave][4 * cl];
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      float Ad = A[e];
-#pragma unroll
-      for (int o = kLanes; o < 64; o *= 2) {
-        const float A1 = up(A[e], o), B1 = up(B[e], o), A2 = down(Ad, o), E2 = down(E[e], o);
-        if (lane >= o) {
-          B[e] = fmaf(A[e], B1, B[e]);
-          A[e] *= A1;
-        }
-        if (lane < 64 - o) {
-          E[e] = fmaf(Ad, E2, E[e]);
-          Ad *= A2;
-        }
-      }
-      Ax[e] = up(A[e], kLanes);
-      Bx[e] = up(B[e], kLanes);
-      Az[e] = down(Ad, kLanes);
-      Ez[e] = down(E[e], kLanes);
-      if (ts == 0) Ax[e] = 1.0f, Bx[e] = 0.0f;
-      if (ts == kTs - 1) Az[e] = 1.0f, Ez[e] = 0.0f;
+      hh[e] = fmaf(Ax[e], hw[e], Bx[e]);
+      ee[e] = fmaf(Az[e], ew[e], Ez[e]);
     }
-    if (ts == kTs - 1) {
-      store4(&sa[wave][4 * cl], A);
-      store4(&sb[wave][4 * cl], B);
-    }
-    if (ts == 0) store4(&se[wave][4 * cl], E);
-    __syncthreads();
-    if (wave == 0) {
-      if constexpr (CHAIN) {
-        float At = 1.0f, Et = 0.0f;
-        for (int w = nw - 1; w >= 0; --w) {
-          Et = fmaf(sa[w][lane], Et, se[w][lane]);
-          At *= sa[w][lane];
-        }
-        back = chained(p.runs + (int64_t)bc * p.nchunks * 128, p.groups + (int64_t)bc * p.ngroups * 64, lane,
-                       (int)(p.nchunks - 1 - chunk), (int)p.nchunks - 1, At, Et, back);
-      }
-      for (int w = 0; w < nw; ++w) {
-        sh[w][lane] = state;
-        state = fmaf(sa[w][lane], state, sb[w][lane]);
-      }
-      for (int w = nw - 1; w >= 0; --w) {
-        sd[w][lane] = back;
-        back = fmaf(sa[w][lane], back, se[w][lane]);
-      }
-    }
-    __syncthreads();
-    float hh[4], ee[4], ws[4] = {0, 0, 0, 0};
-    {
-      const f32x4 hw = *(const f32x4*)&sh[wave][4 * cl], ew = *(const f32x4*)&sd[wave][4 * cl];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        hh[e] = fmaf(Ax[e], hw[e], Bx[e]);
-        ee[e] = fmaf(Az[e], ew[e], Ez[e]);
-      }
-    }
+  }
+  const Rows<T> dx(p.dx, p.x_sb, p.x_st, b, first, ch), dr(p.dr, p.r_sb, p.r_st, b, first, ch), di(p.di, p.i_sb, p.i_st, b, first, ch);
+  auto give = [&](auto whole) {
 #pragma unroll
     for (int j = 0; j < M; ++j)
 #pragma unroll
@@ -462,49 +486,54 @@ __global__ __launch_bounds__(64 * kBwdWaves, 3) void recur_bwd_kernel(RecurArgs 
     for (int j = M - 1; j >= 0; --j) {
       float ox[4], og[4], oi[4];
       const f32x4 fx = keep[(2 * j) * blockDim.x + tid], fi = keep[(2 * j + 1) * blockDim.x + tid];
+      const bool live = decltype(whole)::value || row0 + j < have;
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const float g = (row0 + j < have ? ry[j][e] : 0.0f) + ee[e], w = row0 + j < have ? g * (l[j][e] * h[j][e] - q[j][e]) : 0.0f;
+        const float g = (live ? ry[j][e] : 0.0f) + ee[e], w = live ? g * fmaf(l[j][e], h[j][e], -q[j][e]) : 0.0f;
         ws[e] += w;
-        og[e] = row0 + j < have ? w * r1[j][e] : 0.0f;
-        ox[e] = row0 + j < have ? g * fx[e] : 0.0f;
-        oi[e] = row0 + j < have ? g * fi[e] : 0.0f;
+        og[e] = live ? w * r1[j][e] : 0.0f;
+        ox[e] = live ? g * fx[e] : 0.0f;
+        oi[e] = live ? g * fi[e] : 0.0f;
         ee[e] = a[j][e] * g;
       }
-      if (first + row0 + j < p.S && ch < p.D) {
-        store4(Rows<T>(p.dx, p.x_sb, p.x_st, b, first, ch).at(row0 + j), ox);
-        store4(Rows<T>(p.dr, p.r_sb, p.r_st, b, first, ch).at(row0 + j), og);
-        store4(Rows<T>(p.di, p.i_sb, p.i_st, b, first, ch).at(row0 + j), oi);
+      if ((decltype(whole)::value || first + row0 + j < p.S) && ch < p.D) {
+        store4(dx.at(row0 + j), ox);
+        store4(dr.at(row0 + j), og);
+        store4(di.at(row0 + j), oi);
       }
-      __builtin_amdgcn_sched_barrier(0);
     }
-    // sum of w over the chunk, in the order of the steps' threads and waves
+  };
+  if (have == L) give(std::true_type{});
+  else give(std::false_type{});
+  // sum of w over the chunk, in the order of the steps' threads and waves
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
+  for (int e = 0; e < 4; ++e) {
 #pragma unroll
-      for (int o = kLanes; o < 64; o *= 2) ws[e] += __shfl_xor(ws[e], o, 64);
-    }
-    if (ts == 0) store4(&sw[wave][4 * cl], ws);
-    __syncthreads();
-    if (wave == 0 && cw < p.D) {
-      float sum = 0.0f;
-      for (int w = 0; w < nw; ++w) sum += sw[w][lane];
-      p.part[((int64_t)b * p.nchunks + chunk) * p.D + cw] = sum;
-    }
-  } while (!CHAIN && --chunk >= 0);
-  if (wave == 0 && p.dh0 && cw < p.D && (!CHAIN || chunk == 0)) p.dh0[row] = back;
+    for (int o = kLanes; o < 64; o *= 2) ws[e] += __shfl_xor(ws[e], o, 64);
+  }
+  if (ts == 0) store4(&sw[wave][4 * cl], ws);
+  __syncthreads();
+  if (wave == 0 && cw < p.D) {
+    float sum = 0.0f;
+    for (int w = 0; w < nw; ++w) sum += sw[w][lane];
+    p.part[((int64_t)b * p.nchunks + chunk) * p.D + cw] = sum * (CHAIN ? p.ratio[cw] : sigma_over_softplus(p.lam[cw]));
+  }
+  if (wave == 0 && p.dh0 && cw < p.D && chunk == 0) p.dh0[row] = back;
 }
 
-// Before the chained kernels: nothing is known yet, and log2 a of a fully open gate per channel
+// Before the chained kernels: nothing is known yet; per channel log2 a of a fully open gate, and what dlambda's sum is multiplied by
 __global__ __launch_bounds__(256) void recur_start_kernel(RecurArgs p, int64_t words) {
   const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, step = (int64_t)gridDim.x * 256;
   if (i == 0) *p.counter = 0;
-  if (i < p.D) p.k2[i] = decay2(p.lam[i], p.c);
+  if (i < p.D) {
+    p.k2[i] = decay2(p.lam[i], p.c);
+    p.ratio[i] = sigma_over_softplus(p.lam[i]);
+  }
   for (int64_t k = i; k < words / 2; k += step) ((u32x4*)p.runs)[k] = u32x4{0, 0, 0, 0};
 }
 
-// dlambda from the sums of w of the chunks, [rows, D], added in a fixed order: 16 runs of rows, then those
-__global__ __launch_bounds__(1024) void recur_dlam_kernel(const float* part, int64_t rows, int D, const float* lam, float* dlam) {
+// dlambda from the chunks' sums, [rows, D], added in a fixed order: 16 runs of rows, then those
+__global__ __launch_bounds__(1024) void recur_dlam_kernel(const float* part, int64_t rows, int D, float* dlam) {
   __shared__ float s[16][64];
   const int lane = threadIdx.x & 63, g = threadIdx.x >> 6, c = blockIdx.x * 64 + lane;
   float sum = 0.0f;
@@ -514,33 +543,34 @@ __global__ __launch_bounds__(1024) void recur_dlam_kernel(const float* part, int
   __syncthreads();
   if (g == 0 && c < D) {
     for (int k = 1; k < 16; ++k) sum += s[k][lane];
-    dlam[c] = sum * sigma_over_softplus(lam[c]);
+    dlam[c] = sum;
   }
 }
 
 // ------------------------------------------------------------------ launchers
 namespace {
-constexpr int kFwdM = 8, kBwdM = 4;
+constexpr int kFwdM = 8, kBwdM = 4;                  // steps of a thread
 constexpr int kFewSteps = 8;           // of the forward in which a thread walks alone
 
 int64_t words_of(const RecurArgs& p) { return (int64_t)p.B * p.nct * (p.nchunks * 128 + p.ngroups * 64); }
 
 // chunks, their number of waves, and whether they are chained
-int plan(RecurArgs& p, bool backward) {
-  const int per = kTs * (backward ? kBwdM : kFwdM);
-  const int nw = (int)std::min<int64_t>(backward ? kBwdWaves : kMaxWaves, (p.S + per - 1) / per);
+int plan(RecurArgs& p, Dt t, bool backward) {
+  const int per = kTs * (backward ? kBwdM : t == F32 ? kFwdM / 2 : kFwdM);
+  const int nw = (int)std::min<int64_t>(backward ? kBwdWaves : kFwdWaves, (p.S + per - 1) / per);
   p.nct = (p.D + kRecurCh - 1) / kRecurCh;
   p.nchunks = (p.S + nw * per - 1) / (nw * per);
   p.ngroups = (p.nchunks + kGroup - 1) / kGroup;
   return nw;
 }
-bool chains(const RecurArgs& p) { return p.nchunks > 1 && p.B * p.nct < 512; }
+bool chains(const RecurArgs& p) { return p.nchunks > 1; }
 
 hipError_t start(RecurArgs& p, hipStream_t s) {
   p.runs = (unsigned long long*)p.chain;
   p.groups = p.runs + (int64_t)p.B * p.nct * p.nchunks * 128;
   p.k2 = (float*)(p.runs + words_of(p));
-  p.counter = (uint32_t*)(p.k2 + p.D);
+  p.ratio = p.k2 + p.D;
+  p.counter = (uint32_t*)(p.ratio + p.D);
   const int64_t blocks = std::max<int64_t>((p.D + 255) / 256, std::min<int64_t>((words_of(p) + 511) / 512, 2048));
   hipLaunchKernelGGL(recur_start_kernel, dim3((unsigned)blocks), dim3(256), 0, s, p, words_of(p));
   return hipGetLastError();
@@ -549,9 +579,9 @@ hipError_t start(RecurArgs& p, hipStream_t s) {
 
 int64_t recur_bwd_chunks(int64_t S) { return (S + kRecurKeep - 1) / kRecurKeep; }
 
-int64_t recur_chain_bytes(RecurArgs p, int backward) {
-  plan(p, backward);
-  return chains(p) ? words_of(p) * 8 + ((int64_t)p.D + 4) * 4 : 0;
+int64_t recur_chain_bytes(Dt t, RecurArgs p, int backward) {
+  plan(p, t, backward);
+  return chains(p) ? words_of(p) * 8 + (2 * (int64_t)p.D + 4) * 4 : 0;
 }
 
 hipError_t recur_fwd(Dt t, RecurArgs p, hipStream_t s) {
@@ -562,7 +592,7 @@ hipError_t recur_fwd(Dt t, RecurArgs p, hipStream_t s) {
     else hipLaunchKernelGGL((recur_few_kernel<bf16>), grid, dim3(64), 0, s, p, per);
     return hipGetLastError();
   }
-  const int nw = plan(p, false);
+  const int nw = plan(p, t, false);
   const bool chain = chains(p);
   if (chain) {
     const hipError_t e = start(p, s);
@@ -570,8 +600,8 @@ hipError_t recur_fwd(Dt t, RecurArgs p, hipStream_t s) {
   }
   const dim3 grid((unsigned)(p.B * p.nct * (chain ? p.nchunks : 1))), block((unsigned)(64 * nw));
   if (t == F32) {
-    if (chain) hipLaunchKernelGGL((recur_fwd_kernel<float, kFwdM, true>), grid, block, 0, s, p);
-    else hipLaunchKernelGGL((recur_fwd_kernel<float, kFwdM, false>), grid, block, 0, s, p);
+    if (chain) hipLaunchKernelGGL((recur_fwd_kernel<float, kFwdM / 2, true>), grid, block, 0, s, p);
+    else hipLaunchKernelGGL((recur_fwd_kernel<float, kFwdM / 2, false>), grid, block, 0, s, p);
   } else {
     if (chain) hipLaunchKernelGGL((recur_fwd_kernel<bf16, kFwdM, true>), grid, block, 0, s, p);
     else hipLaunchKernelGGL((recur_fwd_kernel<bf16, kFwdM, false>), grid, block, 0, s, p);
@@ -598,7 +628,7 @@ hipError_t launch_bwd(const RecurArgs& p, int nw, hipStream_t s) {
 
 hipError_t recur_bwd(Dt t, RecurArgs p, hipStream_t s) {
   static_assert(kBwdWaves * kTs * kBwdM == kRecurKeep, "a chunk starts at a state that was kept");
-  const int nw = plan(p, true);
+  const int nw = plan(p, t, true);
   const bool chain = chains(p);
   if (chain) {
     const hipError_t e = start(p, s);
@@ -608,9 +638,12 @@ hipError_t recur_bwd(Dt t, RecurArgs p, hipStream_t s) {
   return chain ? launch_bwd<bf16, true>(p, nw, s) : launch_bwd<bf16, false>(p, nw, s);
 }
 
-hipError_t recur_dlam(const RecurArgs& p, float* dlam, hipStream_t s) {
-  hipLaunchKernelGGL(recur_dlam_kernel, dim3((unsigned)((p.D + 63) / 64)), dim3(1024), 0, s, p.part,
-                     p.B * recur_bwd_chunks(p.S), p.D, p.lam, dlam);
+// Few rows in one launch, many by col_sum's two: 1500 rows of 1024 43 us in one
+int64_t recur_dlam_floats(int64_t rows, int64_t D) { return rows > 128 ? std::min<int64_t>(rows / 16, 512) * D : 0; }
+hipError_t recur_dlam(const RecurArgs& p, float* dlam, float* partial, hipStream_t s) {
+  const int64_t rows = p.B * recur_bwd_chunks(p.S), n = recur_dlam_floats(rows, p.D);
+  if (n > 0) return col_sum(F32, p.part, p.D, rows, p.D, dlam, partial, n, s);
+  hipLaunchKernelGGL(recur_dlam_kernel, dim3((unsigned)((p.D + 63) / 64)), dim3(1024), 0, s, p.part, rows, p.D, dlam);
   return hipGetLastError();
 }
 
