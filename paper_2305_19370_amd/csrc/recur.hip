@@ -83,10 +83,6 @@ BPT_DEV float one_minus_a2(float a, float l2) {
 // Keeps the compiler from forming values later, where they are used: it would hold what they are formed from, in more registers
 BPT_DEV void formed(float& x, float& y, float& z) { asm volatile("" : "+v"(x), "+v"(y), "+v"(z)); }
 
-// value of the thread `o` lanes before (after) this one; kept where there is none
-BPT_DEV float up(float v, int o) { return __shfl_up(v, (unsigned)o, 64); }
-BPT_DEV float down(float v, int o) { return __shfl_down(v, (unsigned)o, 64); }
-
 // A number and its mark, made known to (learned from) other workgroups
 typedef unsigned long long Word;
 BPT_DEV void tell(Word* p, float v) {
@@ -96,55 +92,52 @@ BPT_DEV Word look(const Word* p) { return __hip_atomic_load(p, __ATOMIC_RELAXED,
 BPT_DEV bool known(Word w) { return (w >> 32) != 0; }
 BPT_DEV float number(Word w) { return __uint_as_float((uint32_t)w); }
 
-// Chunk `at` of a chain (of one sequence and 64 channels), by one wave, a channel per lane: tells its (A, B) and returns the
-// state before it; start: the state before the chain. A group of kGroup chunks tells its last state too.
+// What chunk `at` of a chain (of one sequence and 64 channels) learns from those before it, a channel per lane: wave w joins chunks
+// 4 w .. 4 w + 3 of its group as far as they lie before it; wave 0 also takes the state before the group (start: before the chain).
 constexpr int kGroup = 16;
-constexpr int kTries = 1 << 24;        // some ten seconds; a state that is not known by then becomes NaN
-BPT_DEV float chained(Word* run, Word* group, int lane, int at, int last, float A, float B, float start) {
-  const int pos = at % kGroup, g = at / kGroup;
-  run += (int64_t)at * 128 + lane;
-  if (pos + 1 < kGroup && at < last) {
-    tell(run, A);
-    tell(run + 64, B);
-  }
-  // the chunks of the group before this one, joined; four at a time, which is one access' time as long as they are known
-  float a = 1.0f, b = 0.0f, state = start;
-  for (int k0 = 0; k0 < pos; k0 += 4) {
-    Word wa[4], wb[4];
-    bool all = false;
-    for (int tries = 0; !all && tries < kTries; ++tries) {
-      all = true;
+constexpr int kTries = 1 << 24;        // some ten seconds; what is not known by then becomes NaN
+BPT_DEV void learn(const Word* runs, const Word* groups, int lane, int wave, int at, float start, float& a, float& b, float& state) {
+  const int first = at - at % kGroup + 4 * wave, before = min(at - first, 4);
+  a = 1.0f;
+  b = 0.0f;
+  state = start;
+  const bool ask = wave == 0 && at >= kGroup;
+  if (before <= 0 && !ask) return;
+  const Word* g = groups + (int64_t)(at / kGroup - 1) * 64 + lane;
+  Word wa[4], wb[4], ws = (Word)1 << 32;
+  bool all = false;
+  for (int tries = 0; !all && tries < kTries; ++tries) {
+    all = true;
+    if (ask) ws = look(g);
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const Word* p = run - 128 * (int64_t)(pos - min(k0 + k, pos - 1));
+    for (int k = 0; k < 4; ++k)
+      if (k < before) {
+        const Word* p = runs + (int64_t)(first + k) * 128 + lane;
         wa[k] = look(p);
         wb[k] = look(p + 64);
       }
-#pragma unroll
-      for (int k = 0; k < 4; ++k) all = all && known(wa[k]) && known(wb[k]);
-      all = __all(all);
-      if (!all) __builtin_amdgcn_s_sleep(1);
-    }
-    if (!all) a = b = __builtin_nanf("");
+    all = known(ws);
 #pragma unroll
     for (int k = 0; k < 4; ++k)
-      if (k0 + k < pos) {
-        b = fmaf(number(wa[k]), b, number(wb[k]));
-        a *= number(wa[k]);
-      }
+      if (k < before) all = all && known(wa[k]) && known(wb[k]);
+    all = __all(all);
+    if (!all) __builtin_amdgcn_s_sleep(1);
   }
-  if (g > 0) {
-    const Word* p = group + (int64_t)(g - 1) * 64 + lane;
-    Word w = look(p);
-    for (int tries = 0; !__all(known(w)) && tries < kTries; ++tries) {
-      __builtin_amdgcn_s_sleep(1);
-      w = look(p);
+#pragma unroll
+  for (int k = 0; k < 4; ++k)
+    if (k < before) {
+      b = fmaf(number(wa[k]), b, number(wb[k]));
+      a *= number(wa[k]);
     }
-    state = known(w) ? number(w) : __builtin_nanf("");
-  }
-  state = fmaf(a, state, b);
-  if (pos + 1 == kGroup && at < last) tell(group + (int64_t)g * 64 + lane, fmaf(A, state, B));
-  return state;
+  if (ask) state = number(ws);
+  if (!all) b = __builtin_nanf("");
+}
+
+// LDS of a wave becomes readable by its other threads
+BPT_DEV void wave_sync() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
 }
 
 // A tensor's rows of one chunk: a base that is the same for all threads and 32-bit offsets (strides are under 2^21 elements)
@@ -168,7 +161,9 @@ BPT_DEV int64_t steps_of(const RecurArgs& p, int b) {
 // input), whatever their elements hold; their y is 0.
 template <typename T, int M, bool CHAIN>
 __global__ __launch_bounds__(64 * kFwdWaves, CHAIN ? 3 : 2) void recur_fwd_kernel(RecurArgs p) {
-  __shared__ __attribute__((aligned(16))) float sa[kFwdWaves][kRecurCh], sb[kFwdWaves][kRecurCh], sh[kFwdWaves][kRecurCh];
+  __shared__ __attribute__((aligned(16))) float run[kFwdWaves][2][kTs][kRecurCh];   // (A, B) of the threads' runs; the states before them
+  __shared__ float sa[kFwdWaves][kRecurCh], sb[kFwdWaves][kRecurCh];              // of the waves'
+  __shared__ float fa[kFwdWaves][kRecurCh], fb[kFwdWaves][kRecurCh], fs[kRecurCh];   // what the waves learned
   __shared__ uint32_t drawn;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), nw = blockDim.x >> 6;
   const int cl = lane % kLanes, ts = lane / kLanes;
@@ -186,13 +181,12 @@ __global__ __launch_bounds__(64 * kFwdWaves, CHAIN ? 3 : 2) void recur_fwd_kerne
   const int b = bc / p.nct, ct = bc % p.nct;
   const int ch = ct * kRecurCh + 4 * cl;               // this thread's channels
   const int chr = min(ch, p.D - 4);                    // those it reads: the last ones instead of none
-  const int cw = ct * kRecurCh + lane, cwr = min(cw, p.D - 1);   // wave 0: a channel per lane
+  const int cw = ct * kRecurCh + lane, cwr = min(cw, p.D - 1);   // where a lane is one channel
   const int row0 = (wave * kTs + ts) * M;
   const int64_t n = steps_of(p, b);
   float k2[4];
 #pragma unroll
   for (int e = 0; e < 4; ++e) k2[e] = CHAIN ? p.k2[chr + e] : decay2(p.lam[chr + e], p.c);
-  float state = wave == 0 && p.h0 ? p.h0[(int64_t)b * p.D + cwr] : 0.0f;
 
   const int64_t first = chunk * L;
   const Rows<T> x(p.x, p.x_sb, p.x_st, b, first, chr), gr(p.r, p.r_sb, p.r_st, b, first, chr), gi(p.i, p.i_sb, p.i_st, b, first, chr);
@@ -225,51 +219,60 @@ __global__ __launch_bounds__(64 * kFwdWaves, CHAIN ? 3 : 2) void recur_fwd_kerne
   };
   if (have == L) form(std::true_type{});
   else form(std::false_type{});
-  // the threads before this one in the wave, then the waves before this one
-  float Ax[4], Bx[4];
+  // From here to the states before the threads' runs, a lane is a channel. The wave's four runs of it:
+  store4(&run[wave][0][ts][4 * cl], A);
+  store4(&run[wave][1][ts][4 * cl], B);
+  wave_sync();
+  float Ax[kTs], Bx[kTs], Aw = 1.0f, Bw = 0.0f;        // what lies before a run in its wave, and the wave
 #pragma unroll
-  for (int e = 0; e < 4; ++e) {
-#pragma unroll
-    for (int o = kLanes; o < 64; o *= 2) {
-      const float A1 = up(A[e], o), B1 = up(B[e], o);
-      if (lane >= o) {
-        B[e] = fmaf(A[e], B1, B[e]);
-        A[e] *= A1;
-      }
-    }
-    Ax[e] = up(A[e], kLanes);
-    Bx[e] = up(B[e], kLanes);
-    if (ts == 0) Ax[e] = 1.0f, Bx[e] = 0.0f;
+  for (int k = 0; k < kTs; ++k) {
+    const float Ak = run[wave][0][k][lane], Bk = run[wave][1][k][lane];
+    Ax[k] = Aw;
+    Bx[k] = Bw;
+    Bw = fmaf(Ak, Bw, Bk);
+    Aw *= Ak;
   }
-  if (ts == kTs - 1) {
-    store4(&sa[wave][4 * cl], A);
-    store4(&sb[wave][4 * cl], B);
-  }
+  sa[wave][lane] = Aw;
+  sb[wave][lane] = Bw;
   __syncthreads();
-  if (wave == 0) {
-    if constexpr (CHAIN) {
-      float At = 1.0f, Bt = 0.0f;
-      for (int w = 0; w < nw; ++w) {
+  float state = p.h0 ? p.h0[(int64_t)b * p.D + cwr] : 0.0f, At = 1.0f, Bt = 0.0f;
+  if constexpr (CHAIN) {
+    Word *runs = p.runs + (int64_t)bc * p.nchunks * 128, *groups = p.groups + (int64_t)bc * p.ngroups * 64;
+    const int at = (int)chunk, last = (int)p.nchunks - 1;
+    if (wave == 0) {
+#pragma unroll
+      for (int w = 0; w < kFwdWaves; ++w) {
         Bt = fmaf(sa[w][lane], Bt, sb[w][lane]);
         At *= sa[w][lane];
       }
-      state = chained(p.runs + (int64_t)bc * p.nchunks * 128, p.groups + (int64_t)bc * p.ngroups * 64, lane, (int)chunk,
-                      (int)p.nchunks - 1, At, Bt, state);
+      if (at < last && (at + 1) % kGroup) {
+        tell(runs + (int64_t)at * 128 + lane, At);
+        tell(runs + (int64_t)at * 128 + 64 + lane, Bt);
+      }
     }
-    for (int w = 0; w < nw; ++w) {
-      sh[w][lane] = state;
-      const int64_t t = chunk * L + (int64_t)w * kTs * M;
-      if (p.saved && t % kRecurKeep == 0 && t > 0 && t < p.S && cw < p.D)
-        p.saved[((int64_t)b * ((p.S - 1) / kRecurKeep) + t / kRecurKeep - 1) * p.D + cw] = state;
-      state = fmaf(sa[w][lane], state, sb[w][lane]);
-    }
+    learn(runs, groups, lane, wave, at, state, fa[wave][lane], fb[wave][lane], state);
+    if (wave == 0) fs[lane] = state;
+    __syncthreads();
+    state = fs[lane];
+#pragma unroll
+    for (int w = 0; w < kFwdWaves; ++w) state = fmaf(fa[w][lane], state, fb[w][lane]);
+    if (wave == 0 && at < last && (at + 1) % kGroup == 0) tell(groups + (int64_t)(at / kGroup) * 64 + lane, fmaf(At, state, Bt));
   }
-  __syncthreads();
+  for (int w = 0; w < wave; ++w) state = fmaf(sa[w][lane], state, sb[w][lane]);
+  {
+    const int64_t t = first + (int64_t)wave * kTs * M;
+    if (p.saved && t % kRecurKeep == 0 && t > 0 && t < p.S && cw < p.D)
+      p.saved[((int64_t)b * ((p.S - 1) / kRecurKeep) + t / kRecurKeep - 1) * p.D + cw] = state;
+  }
+#pragma unroll
+  for (int k = 0; k < kTs; ++k) run[wave][0][k][lane] = fmaf(Ax[k], state, Bx[k]);
+  if (wave == nw - 1 && p.hT && cw < p.D && chunk == p.nchunks - 1) p.hT[(int64_t)b * p.D + cw] = fmaf(Aw, state, Bw);
+  wave_sync();
   float h[4];
   {
-    const f32x4 hw = *(const f32x4*)&sh[wave][4 * cl];
+    const f32x4 before = *(const f32x4*)&run[wave][0][ts][4 * cl];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) h[e] = fmaf(Ax[e], hw[e], Bx[e]);
+    for (int e = 0; e < 4; ++e) h[e] = before[e];
   }
   const Rows<T> y(p.y, p.y_sb, p.y_st, b, first, ch);
   auto give = [&](auto whole) {
@@ -286,7 +289,6 @@ __global__ __launch_bounds__(64 * kFwdWaves, CHAIN ? 3 : 2) void recur_fwd_kerne
   };
   if (have == L) give(std::true_type{});
   else give(std::false_type{});
-  if (wave == 0 && p.hT && cw < p.D && chunk == p.nchunks - 1) p.hT[(int64_t)b * p.D + cw] = state;
 }
 
 // Few steps (new tokens of many sequences): a thread walks along the steps of four channels, and over a few sequences, for which
@@ -330,8 +332,9 @@ template <typename T, int M, bool CHAIN>
 __global__ __launch_bounds__(64 * kBwdWaves, sizeof(T) == 4 ? 2 : 3) void recur_bwd_kernel(RecurArgs p) {
   extern __shared__ __attribute__((aligned(16))) f32x4 keep[];   // per thread and step: factors of d in dx and di
   __shared__ uint32_t drawn;
-  __shared__ __attribute__((aligned(16))) float sa[kBwdWaves][kRecurCh], sb[kBwdWaves][kRecurCh], se[kBwdWaves][kRecurCh];
-  __shared__ __attribute__((aligned(16))) float sh[kBwdWaves][kRecurCh], sd[kBwdWaves][kRecurCh], sw[kBwdWaves][kRecurCh];
+  __shared__ __attribute__((aligned(16))) float run[kBwdWaves][3][kTs][kRecurCh];   // (A, B) and E of the threads' runs; h before, e behind
+  __shared__ float sa[kBwdWaves][kRecurCh], sb[kBwdWaves][kRecurCh], se[kBwdWaves][kRecurCh];
+  __shared__ float sw[kBwdWaves][kRecurCh], fa[kBwdWaves][kRecurCh], fb[kBwdWaves][kRecurCh], fs[kRecurCh];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), nw = blockDim.x >> 6;
   const int cl = lane % kLanes, ts = lane / kLanes;
   const int L = nw * kTs * M;                          // at most kRecurKeep
@@ -353,7 +356,6 @@ __global__ __launch_bounds__(64 * kBwdWaves, sizeof(T) == 4 ? 2 : 3) void recur_
   float k2[4];
 #pragma unroll
   for (int e = 0; e < 4; ++e) k2[e] = CHAIN ? p.k2[chr + e] : decay2(p.lam[chr + e], p.c);
-  float back = wave == 0 && p.dhT ? p.dhT[row] : 0.0f;   // e of the step behind the chunk
 
   const int64_t first = chunk * L;
   const Rows<T> x(p.x, p.x_sb, p.x_st, b, first, chr), gr(p.r, p.r_sb, p.r_st, b, first, chr), gi(p.i, p.i_sb, p.i_st, b, first, chr),
@@ -368,8 +370,6 @@ __global__ __launch_bounds__(64 * kBwdWaves, sizeof(T) == 4 ? 2 : 3) void recur_
     rx[j].load(x.at(t));
     ry[j].load(dy.at(t));
   }
-  float state = 0.0f;
-  if (wave == 0) state = chunk > 0 ? p.saved[((int64_t)b * kept + chunk - 1) * p.D + cwr] : p.h0 ? p.h0[row] : 0.0f;
   // per step: a, the state before it, and the factors of d (and of d h) in the results
   float a[M][4], h[M][4], l[M][4], q[M][4], r1[M][4];
   float A[4], B[4], E[4];
@@ -414,63 +414,71 @@ __global__ __launch_bounds__(64 * kBwdWaves, sizeof(T) == 4 ? 2 : 3) void recur_
   };
   if (have == L) form(std::true_type{});
   else form(std::false_type{});
-  float Ax[4], Bx[4], Az[4], Ez[4];                  // the threads of the wave before this one, and behind it
+  // a lane is a channel, as in the forward
+  store4(&run[wave][0][ts][4 * cl], A);
+  store4(&run[wave][1][ts][4 * cl], B);
+  store4(&run[wave][2][ts][4 * cl], E);
+  wave_sync();
+  float Ax[kTs], Bx[kTs], Az[kTs], Ez[kTs], Aw = 1.0f, Bw = 0.0f, Ew = 0.0f;
 #pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    float Ad = A[e];
+  for (int k = 0; k < kTs; ++k) {
+    const float Ak = run[wave][0][k][lane];
+    Ax[k] = Aw;
+    Bx[k] = Bw;
+    Bw = fmaf(Ak, Bw, run[wave][1][k][lane]);
+    Aw *= Ak;
+  }
+  float Ab = 1.0f;
 #pragma unroll
-    for (int o = kLanes; o < 64; o *= 2) {
-      const float A1 = up(A[e], o), B1 = up(B[e], o), A2 = down(Ad, o), E2 = down(E[e], o);
-      if (lane >= o) {
-        B[e] = fmaf(A[e], B1, B[e]);
-        A[e] *= A1;
-      }
-      if (lane < 64 - o) {
-        E[e] = fmaf(Ad, E2, E[e]);
-        Ad *= A2;
-      }
-    }
-    Ax[e] = up(A[e], kLanes);
-    Bx[e] = up(B[e], kLanes);
-    Az[e] = down(Ad, kLanes);
-    Ez[e] = down(E[e], kLanes);
-    if (ts == 0) Ax[e] = 1.0f, Bx[e] = 0.0f;
-    if (ts == kTs - 1) Az[e] = 1.0f, Ez[e] = 0.0f;
+  for (int k = kTs - 1; k >= 0; --k) {
+    const float Ak = run[wave][0][k][lane];
+    Az[k] = Ab;
+    Ez[k] = Ew;
+    Ew = fmaf(Ak, Ew, run[wave][2][k][lane]);
+    Ab *= Ak;
   }
-  if (ts == kTs - 1) {
-    store4(&sa[wave][4 * cl], A);
-    store4(&sb[wave][4 * cl], B);
-  }
-  if (ts == 0) store4(&se[wave][4 * cl], E);
+  sa[wave][lane] = Aw;
+  sb[wave][lane] = Bw;
+  se[wave][lane] = Ew;
   __syncthreads();
-  if (wave == 0) {
-    if constexpr (CHAIN) {
-      float At = 1.0f, Et = 0.0f;
-      for (int w = nw - 1; w >= 0; --w) {
+  float state = chunk > 0 ? p.saved[((int64_t)b * kept + chunk - 1) * p.D + cwr] : p.h0 ? p.h0[row] : 0.0f;
+  float back = p.dhT ? p.dhT[row] : 0.0f, At = 1.0f, Et = 0.0f;   // e of the step behind the chunk
+  if constexpr (CHAIN) {
+    Word *runs = p.runs + (int64_t)bc * p.nchunks * 128, *groups = p.groups + (int64_t)bc * p.ngroups * 64;
+    const int at = (int)(p.nchunks - 1 - chunk), last = (int)p.nchunks - 1;
+    if (wave == 0) {
+#pragma unroll
+      for (int w = kBwdWaves - 1; w >= 0; --w) {
         Et = fmaf(sa[w][lane], Et, se[w][lane]);
         At *= sa[w][lane];
       }
-      back = chained(p.runs + (int64_t)bc * p.nchunks * 128, p.groups + (int64_t)bc * p.ngroups * 64, lane,
-                     (int)(p.nchunks - 1 - chunk), (int)p.nchunks - 1, At, Et, back);
+      if (at < last && (at + 1) % kGroup) {
+        tell(runs + (int64_t)at * 128 + lane, At);
+        tell(runs + (int64_t)at * 128 + 64 + lane, Et);
+      }
     }
-    for (int w = 0; w < nw; ++w) {
-      sh[w][lane] = state;
-      state = fmaf(sa[w][lane], state, sb[w][lane]);
-    }
-    for (int w = nw - 1; w >= 0; --w) {
-      sd[w][lane] = back;
-      back = fmaf(sa[w][lane], back, se[w][lane]);
-    }
+    learn(runs, groups, lane, wave, at, back, fa[wave][lane], fb[wave][lane], back);
+    if (wave == 0) fs[lane] = back;
+    __syncthreads();
+    back = fs[lane];
+#pragma unroll
+    for (int w = 0; w < kBwdWaves; ++w) back = fmaf(fa[w][lane], back, fb[w][lane]);
+    if (wave == 0 && at < last && (at + 1) % kGroup == 0) tell(groups + (int64_t)(at / kGroup) * 64 + lane, fmaf(At, back, Et));
   }
-  __syncthreads();
+  for (int w = 0; w < wave; ++w) state = fmaf(sa[w][lane], state, sb[w][lane]);
+  for (int w = nw - 1; w > wave; --w) back = fmaf(sa[w][lane], back, se[w][lane]);
+#pragma unroll
+  for (int k = 0; k < kTs; ++k) {
+    run[wave][0][k][lane] = fmaf(Ax[k], state, Bx[k]);
+    run[wave][1][k][lane] = fmaf(Az[k], back, Ez[k]);
+  }
+  if (wave == 0 && p.dh0 && cw < p.D && chunk == 0) p.dh0[row] = fmaf(Aw, back, Ew);
+  wave_sync();
   float hh[4], ee[4], ws[4] = {0, 0, 0, 0};
   {
-    const f32x4 hw = *(const f32x4*)&sh[wave][4 * cl], ew = *(const f32x4*)&sd[wave][4 * cl];
+    const f32x4 hw = *(const f32x4*)&run[wave][0][ts][4 * cl], ew = *(const f32x4*)&run[wave][1][ts][4 * cl];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      hh[e] = fmaf(Ax[e], hw[e], Bx[e]);
-      ee[e] = fmaf(Az[e], ew[e], Ez[e]);
-    }
+    for (int e = 0; e < 4; ++e) hh[e] = hw[e], ee[e] = ew[e];
   }
   const Rows<T> dx(p.dx, p.x_sb, p.x_st, b, first, ch), dr(p.dr, p.r_sb, p.r_st, b, first, ch), di(p.di, p.i_sb, p.i_st, b, first, ch);
   auto give = [&](auto whole) {
@@ -505,20 +513,19 @@ __global__ __launch_bounds__(64 * kBwdWaves, sizeof(T) == 4 ? 2 : 3) void recur_
   };
   if (have == L) give(std::true_type{});
   else give(std::false_type{});
-  // sum of w over the chunk, in the order of the steps' threads and waves
+  // sum of w over the chunk, in the order of its runs
+  store4(&run[wave][2][ts][4 * cl], ws);
+  wave_sync();
+  float part = 0.0f;
 #pragma unroll
-  for (int e = 0; e < 4; ++e) {
-#pragma unroll
-    for (int o = kLanes; o < 64; o *= 2) ws[e] += __shfl_xor(ws[e], o, 64);
-  }
-  if (ts == 0) store4(&sw[wave][4 * cl], ws);
+  for (int k = 0; k < kTs; ++k) part += run[wave][2][k][lane];
+  sw[wave][lane] = part;
   __syncthreads();
   if (wave == 0 && cw < p.D) {
     float sum = 0.0f;
     for (int w = 0; w < nw; ++w) sum += sw[w][lane];
     p.part[((int64_t)b * p.nchunks + chunk) * p.D + cw] = sum * (CHAIN ? p.ratio[cw] : sigma_over_softplus(p.lam[cw]));
   }
-  if (wave == 0 && p.dh0 && cw < p.D && chunk == 0) p.dh0[row] = back;
 }
 
 // Before the chained kernels: nothing is known yet; per channel log2 a of a fully open gate, and what dlambda's sum is multiplied by
