@@ -29,7 +29,7 @@ namespace {
 constexpr int kLanes = kRecurCh / 4;                 // threads of a wave side by side on the channels
 constexpr int kTs = 64 / kLanes;                     // and behind one another on the steps
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.69314718055994531f;
-constexpr int kFwdWaves = 4, kBwdWaves = 4;          // of a workgroup
+constexpr int kFwdWaves = 8, kBwdWaves = 4;          // of a workgroup
 
 // four elements as they are in memory, and as numbers
 template <typename T> struct Raw4;
@@ -83,6 +83,9 @@ BPT_DEV float one_minus_a2(float a, float l2) {
 // Keeps the compiler from forming values later, where they are used: it would hold what they are formed from, in more registers
 BPT_DEV void formed(float& x, float& y, float& z) { asm volatile("" : "+v"(x), "+v"(y), "+v"(z)); }
 
+// value of the thread `o` lanes before this one
+BPT_DEV float up(float v, int o) { return __shfl_up(v, (unsigned)o, 64); }
+
 // A number and its mark, made known to (learned from) other workgroups
 typedef unsigned long long Word;
 BPT_DEV void tell(Word* p, float v) {
@@ -92,25 +95,27 @@ BPT_DEV Word look(const Word* p) { return __hip_atomic_load(p, __ATOMIC_RELAXED,
 BPT_DEV bool known(Word w) { return (w >> 32) != 0; }
 BPT_DEV float number(Word w) { return __uint_as_float((uint32_t)w); }
 
-// What chunk `at` of a chain (of one sequence and 64 channels) learns from those before it, a channel per lane: wave w joins chunks
-// 4 w .. 4 w + 3 of its group as far as they lie before it; wave 0 also takes the state before the group (start: before the chain).
+// What chunk `at` of a chain (of one sequence and 64 channels) learns from those before it, a channel per lane: wave w of NW joins 16 / NW
+// chunks of its group as far as they lie before it; wave 0 also takes the state before the group (start: before the chain).
 constexpr int kGroup = 16;
 constexpr int kTries = 1 << 24;        // some ten seconds; what is not known by then becomes NaN
+template <int NW>
 BPT_DEV void learn(const Word* runs, const Word* groups, int lane, int wave, int at, float start, float& a, float& b, float& state) {
-  const int first = at - at % kGroup + 4 * wave, before = min(at - first, 4);
+  constexpr int C = kGroup / NW;                       // chunks of a wave
+  const int first = at - at % kGroup + C * wave, before = min(at - first, C);
   a = 1.0f;
   b = 0.0f;
   state = start;
   const bool ask = wave == 0 && at >= kGroup;
   if (before <= 0 && !ask) return;
   const Word* g = groups + (int64_t)(at / kGroup - 1) * 64 + lane;
-  Word wa[4], wb[4], ws = (Word)1 << 32;
+  Word wa[C], wb[C], ws = (Word)1 << 32;
   bool all = false;
   for (int tries = 0; !all && tries < kTries; ++tries) {
     all = true;
     if (ask) ws = look(g);
 #pragma unroll
-    for (int k = 0; k < 4; ++k)
+    for (int k = 0; k < C; ++k)
       if (k < before) {
         const Word* p = runs + (int64_t)(first + k) * 128 + lane;
         wa[k] = look(p);
@@ -118,13 +123,13 @@ BPT_DEV void learn(const Word* runs, const Word* groups, int lane, int wave, int
       }
     all = known(ws);
 #pragma unroll
-    for (int k = 0; k < 4; ++k)
+    for (int k = 0; k < C; ++k)
       if (k < before) all = all && known(wa[k]) && known(wb[k]);
     all = __all(all);
     if (!all) __builtin_amdgcn_s_sleep(1);
   }
 #pragma unroll
-  for (int k = 0; k < 4; ++k)
+  for (int k = 0; k < C; ++k)
     if (k < before) {
       b = fmaf(number(wa[k]), b, number(wb[k]));
       a *= number(wa[k]);
@@ -159,11 +164,16 @@ BPT_DEV int64_t steps_of(const RecurArgs& p, int b) {
 // ------------------------------------------------------------------ forward
 // Steps [chunk L, chunk L + L), L = waves * kTs * M. Steps behind a sequence's length leave the state as it is (a = 1, no
 // input), whatever their elements hold; their y is 0.
+//
+// 256 steps of 64 channels (fp32: 128), two workgroups on a CU. Bound by HBM with the vector units more than half busy (33
+// instructions and 6 of them exponentials, reciprocals or roots an element): 96000 steps of width 1024, bf16 177 us, 4.4 TB/s; fp32
+// 163840 steps 480 us, 5.6 TB/s. Chunks of 128 steps with 4 waves of 168 registers 200; a workgroup that takes chunk after
+// chunk, the next one's elements under way, 239; one state that goes from group to group of 256 chunks 205; halves of a
+// chunk's threads in loops without selects 195.
 template <typename T, int M, bool CHAIN>
-__global__ __launch_bounds__(64 * kFwdWaves, CHAIN ? 3 : 2) void recur_fwd_kernel(RecurArgs p) {
-  __shared__ __attribute__((aligned(16))) float run[kFwdWaves][2][kTs][kRecurCh];   // (A, B) of the threads' runs; the states before them
-  __shared__ float sa[kFwdWaves][kRecurCh], sb[kFwdWaves][kRecurCh];              // of the waves'
-  __shared__ float fa[kFwdWaves][kRecurCh], fb[kFwdWaves][kRecurCh], fs[kRecurCh];   // what the waves learned
+__global__ __launch_bounds__(64 * kFwdWaves, 4) void recur_fwd_kernel(RecurArgs p) {
+  __shared__ __attribute__((aligned(16))) float sa[kFwdWaves][kRecurCh], sb[kFwdWaves][kRecurCh], sh[kFwdWaves][kRecurCh];
+  __shared__ float fa[kFwdWaves][kRecurCh], fb[kFwdWaves][kRecurCh];
   __shared__ uint32_t drawn;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), nw = blockDim.x >> 6;
   const int cl = lane % kLanes, ts = lane / kLanes;
@@ -183,12 +193,12 @@ __global__ __launch_bounds__(64 * kFwdWaves, CHAIN ? 3 : 2) void recur_fwd_kerne
   const int chr = min(ch, p.D - 4);                    // those it reads: the last ones instead of none
   const int cw = ct * kRecurCh + lane, cwr = min(cw, p.D - 1);   // where a lane is one channel
   const int row0 = (wave * kTs + ts) * M;
-  const int64_t n = steps_of(p, b);
+  const int64_t n = steps_of(p, b), first = chunk * L;
   float k2[4];
 #pragma unroll
   for (int e = 0; e < 4; ++e) k2[e] = CHAIN ? p.k2[chr + e] : decay2(p.lam[chr + e], p.c);
+  float state = wave == 0 && p.h0 ? p.h0[(int64_t)b * p.D + cwr] : 0.0f;
 
-  const int64_t first = chunk * L;
   const Rows<T> x(p.x, p.x_sb, p.x_st, b, first, chr), gr(p.r, p.r_sb, p.r_st, b, first, chr), gi(p.i, p.i_sb, p.i_st, b, first, chr);
   const int have = (int)min(max(n - first, (int64_t)0), (int64_t)L);   // steps of the chunk that exist
   Raw4<T> rx[M], rr[M], ri[M];
@@ -200,47 +210,45 @@ __global__ __launch_bounds__(64 * kFwdWaves, CHAIN ? 3 : 2) void recur_fwd_kerne
     ri[j].load(gi.at(t));
   }
   float a[M][4], u[M][4], A[4] = {1, 1, 1, 1}, B[4] = {0, 0, 0, 0};
-  auto form = [&](auto whole) {
 #pragma unroll
-    for (int j = 0; j < M; ++j)
+  for (int j = 0; j < M; ++j)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const float l2 = k2[e] * sigma(rr[j][e]);
-        a[j][e] = __builtin_amdgcn_exp2f(l2);
-        u[j][e] = __builtin_amdgcn_sqrtf(one_minus_a2(a[j][e], l2)) * (sigma(ri[j][e]) * rx[j][e]);
-        if constexpr (!decltype(whole)::value) {
-          const bool live = row0 + j < have;
-          a[j][e] = live ? a[j][e] : 1.0f;
-          u[j][e] = live ? u[j][e] : 0.0f;
-        }
-        B[e] = j ? fmaf(a[j][e], B[e], u[j][e]) : u[j][e];
-        A[e] = j ? A[e] * a[j][e] : a[j][e];
+    for (int e = 0; e < 4; ++e) {
+      const float l2 = k2[e] * sigma(rr[j][e]);
+      const float al = __builtin_amdgcn_exp2f(l2);
+      const float m = __builtin_amdgcn_sqrtf(one_minus_a2(al, l2));
+      const bool live = row0 + j < have;
+      a[j][e] = live ? al : 1.0f;
+      u[j][e] = live ? m * (sigma(ri[j][e]) * rx[j][e]) : 0.0f;
+      B[e] = fmaf(a[j][e], B[e], u[j][e]);
+      A[e] *= a[j][e];
+    }
+  // the threads before this one in the wave, then the waves before this one
+  float Ax[4], Bx[4];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+#pragma unroll
+    for (int o = kLanes; o < 64; o *= 2) {
+      const float A1 = up(A[e], o), B1 = up(B[e], o);
+      if (lane >= o) {
+        B[e] = fmaf(A[e], B1, B[e]);
+        A[e] *= A1;
       }
-  };
-  if (have == L) form(std::true_type{});
-  else form(std::false_type{});
-  // From here to the states before the threads' runs, a lane is a channel. The wave's four runs of it:
-  store4(&run[wave][0][ts][4 * cl], A);
-  store4(&run[wave][1][ts][4 * cl], B);
-  wave_sync();
-  float Ax[kTs], Bx[kTs], Aw = 1.0f, Bw = 0.0f;        // what lies before a run in its wave, and the wave
-#pragma unroll
-  for (int k = 0; k < kTs; ++k) {
-    const float Ak = run[wave][0][k][lane], Bk = run[wave][1][k][lane];
-    Ax[k] = Aw;
-    Bx[k] = Bw;
-    Bw = fmaf(Ak, Bw, Bk);
-    Aw *= Ak;
+    }
+    Ax[e] = up(A[e], kLanes);
+    Bx[e] = up(B[e], kLanes);
+    if (ts == 0) Ax[e] = 1.0f, Bx[e] = 0.0f;
   }
-  sa[wave][lane] = Aw;
-  sb[wave][lane] = Bw;
+  if (ts == kTs - 1) {
+    store4(&sa[wave][4 * cl], A);
+    store4(&sb[wave][4 * cl], B);
+  }
   __syncthreads();
-  float state = p.h0 ? p.h0[(int64_t)b * p.D + cwr] : 0.0f, At = 1.0f, Bt = 0.0f;
   if constexpr (CHAIN) {
     Word *runs = p.runs + (int64_t)bc * p.nchunks * 128, *groups = p.groups + (int64_t)bc * p.ngroups * 64;
     const int at = (int)chunk, last = (int)p.nchunks - 1;
+    float At = 1.0f, Bt = 0.0f;
     if (wave == 0) {
-#pragma unroll
       for (int w = 0; w < kFwdWaves; ++w) {
         Bt = fmaf(sa[w][lane], Bt, sb[w][lane]);
         At *= sa[w][lane];
@@ -250,45 +258,41 @@ __global__ __launch_bounds__(64 * kFwdWaves, CHAIN ? 3 : 2) void recur_fwd_kerne
         tell(runs + (int64_t)at * 128 + 64 + lane, Bt);
       }
     }
-    learn(runs, groups, lane, wave, at, state, fa[wave][lane], fb[wave][lane], state);
-    if (wave == 0) fs[lane] = state;
+    learn<kFwdWaves>(runs, groups, lane, wave, at, state, fa[wave][lane], fb[wave][lane], state);
     __syncthreads();
-    state = fs[lane];
-#pragma unroll
-    for (int w = 0; w < kFwdWaves; ++w) state = fmaf(fa[w][lane], state, fb[w][lane]);
-    if (wave == 0 && at < last && (at + 1) % kGroup == 0) tell(groups + (int64_t)(at / kGroup) * 64 + lane, fmaf(At, state, Bt));
+    if (wave == 0) {
+      for (int w = 0; w < kFwdWaves; ++w) state = fmaf(fa[w][lane], state, fb[w][lane]);
+      if (at < last && (at + 1) % kGroup == 0) tell(groups + (int64_t)(at / kGroup) * 64 + lane, fmaf(At, state, Bt));
+    }
   }
-  for (int w = 0; w < wave; ++w) state = fmaf(sa[w][lane], state, sb[w][lane]);
-  {
-    const int64_t t = first + (int64_t)wave * kTs * M;
-    if (p.saved && t % kRecurKeep == 0 && t > 0 && t < p.S && cw < p.D)
-      p.saved[((int64_t)b * ((p.S - 1) / kRecurKeep) + t / kRecurKeep - 1) * p.D + cw] = state;
+  if (wave == 0) {
+    for (int w = 0; w < nw; ++w) {
+      sh[w][lane] = state;
+      const int64_t t = first + (int64_t)w * kTs * M;
+      if (p.saved && t % kRecurKeep == 0 && t > 0 && t < p.S && cw < p.D)
+        p.saved[((int64_t)b * ((p.S - 1) / kRecurKeep) + t / kRecurKeep - 1) * p.D + cw] = state;
+      state = fmaf(sa[w][lane], state, sb[w][lane]);
+    }
+    if (p.hT && cw < p.D && chunk == p.nchunks - 1) p.hT[(int64_t)b * p.D + cw] = state;
   }
-#pragma unroll
-  for (int k = 0; k < kTs; ++k) run[wave][0][k][lane] = fmaf(Ax[k], state, Bx[k]);
-  if (wave == nw - 1 && p.hT && cw < p.D && chunk == p.nchunks - 1) p.hT[(int64_t)b * p.D + cw] = fmaf(Aw, state, Bw);
-  wave_sync();
+  __syncthreads();
   float h[4];
   {
-    const f32x4 before = *(const f32x4*)&run[wave][0][ts][4 * cl];
+    const f32x4 hw = *(const f32x4*)&sh[wave][4 * cl];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) h[e] = before[e];
+    for (int e = 0; e < 4; ++e) h[e] = fmaf(Ax[e], hw[e], Bx[e]);
   }
   const Rows<T> y(p.y, p.y_sb, p.y_st, b, first, ch);
-  auto give = [&](auto whole) {
 #pragma unroll
-    for (int j = 0; j < M; ++j) {
-      float out[4];
+  for (int j = 0; j < M; ++j) {
+    float out[4];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        h[e] = fmaf(a[j][e], h[e], u[j][e]);
-        out[e] = decltype(whole)::value || row0 + j < have ? h[e] : 0.0f;
-      }
-      if ((decltype(whole)::value || first + row0 + j < p.S) && ch < p.D) store4(y.at(row0 + j), out);
+    for (int e = 0; e < 4; ++e) {
+      h[e] = fmaf(a[j][e], h[e], u[j][e]);
+      out[e] = row0 + j < have ? h[e] : 0.0f;
     }
-  };
-  if (have == L) give(std::true_type{});
-  else give(std::false_type{});
+    if (first + row0 + j < p.S && ch < p.D) store4(y.at(row0 + j), out);
+  }
 }
 
 // Few steps (new tokens of many sequences): a thread walks along the steps of four channels, and over a few sequences, for which
@@ -327,7 +331,13 @@ __global__ __launch_bounds__(64) void recur_few_kernel(RecurArgs p, int per) {
 }
 
 // ------------------------------------------------------------------ backward
-// The chunks from the last one down. States within a chunk of 64 steps from the one kept before it.
+// The chunks of 64 steps from the last one down; the states within one from the one kept before it.
+//
+// A thread's 16 elements take five registers each between the two passes over them and 8 bytes of LDS, three workgroups of four
+// waves on a CU. Bound by that: half of the time the vector units are busy (65 instructions an element), elements under way for
+// 70 % of HBM's rate. 96000 steps of width 1024, bf16 365 us, 3.8 TB/s; fp32 163840 steps 985 us, 4.8 TB/s. Runs joined by
+// lane exchanges instead of through LDS 372; 8 waves with half as many elements a thread 407; with selects for
+// steps that do not exist in whole chunks too 408.
 template <typename T, int M, bool CHAIN>
 __global__ __launch_bounds__(64 * kBwdWaves, sizeof(T) == 4 ? 2 : 3) void recur_bwd_kernel(RecurArgs p) {
   extern __shared__ __attribute__((aligned(16))) f32x4 keep[];   // per thread and step: factors of d in dx and di
@@ -337,7 +347,7 @@ __global__ __launch_bounds__(64 * kBwdWaves, sizeof(T) == 4 ? 2 : 3) void recur_
   __shared__ float sw[kBwdWaves][kRecurCh], fa[kBwdWaves][kRecurCh], fb[kBwdWaves][kRecurCh], fs[kRecurCh];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), nw = blockDim.x >> 6;
   const int cl = lane % kLanes, ts = lane / kLanes;
-  const int L = nw * kTs * M;                          // at most kRecurKeep
+  const int L = nw * kTs * M;                          // kRecurKeep, unless there is one chunk
   uint32_t bc = blockIdx.x;
   int64_t chunk = 0;
   if constexpr (CHAIN) {
@@ -419,24 +429,15 @@ __global__ __launch_bounds__(64 * kBwdWaves, sizeof(T) == 4 ? 2 : 3) void recur_
   store4(&run[wave][1][ts][4 * cl], B);
   store4(&run[wave][2][ts][4 * cl], E);
   wave_sync();
-  float Ax[kTs], Bx[kTs], Az[kTs], Ez[kTs], Aw = 1.0f, Bw = 0.0f, Ew = 0.0f;
+  float Aw = 1.0f, Bw = 0.0f, Ew = 0.0f;
 #pragma unroll
   for (int k = 0; k < kTs; ++k) {
     const float Ak = run[wave][0][k][lane];
-    Ax[k] = Aw;
-    Bx[k] = Bw;
     Bw = fmaf(Ak, Bw, run[wave][1][k][lane]);
     Aw *= Ak;
   }
-  float Ab = 1.0f;
 #pragma unroll
-  for (int k = kTs - 1; k >= 0; --k) {
-    const float Ak = run[wave][0][k][lane];
-    Az[k] = Ab;
-    Ez[k] = Ew;
-    Ew = fmaf(Ak, Ew, run[wave][2][k][lane]);
-    Ab *= Ak;
-  }
+  for (int k = kTs - 1; k >= 0; --k) Ew = fmaf(run[wave][0][k][lane], Ew, run[wave][2][k][lane]);
   sa[wave][lane] = Aw;
   sb[wave][lane] = Bw;
   se[wave][lane] = Ew;
@@ -457,7 +458,7 @@ __global__ __launch_bounds__(64 * kBwdWaves, sizeof(T) == 4 ? 2 : 3) void recur_
         tell(runs + (int64_t)at * 128 + 64 + lane, Et);
       }
     }
-    learn(runs, groups, lane, wave, at, back, fa[wave][lane], fb[wave][lane], back);
+    learn<kBwdWaves>(runs, groups, lane, wave, at, back, fa[wave][lane], fb[wave][lane], back);
     if (wave == 0) fs[lane] = back;
     __syncthreads();
     back = fs[lane];
@@ -469,14 +470,21 @@ __global__ __launch_bounds__(64 * kBwdWaves, sizeof(T) == 4 ? 2 : 3) void recur_
   for (int w = nw - 1; w > wave; --w) back = fmaf(sa[w][lane], back, se[w][lane]);
 #pragma unroll
   for (int k = 0; k < kTs; ++k) {
-    run[wave][0][k][lane] = fmaf(Ax[k], state, Bx[k]);
-    run[wave][1][k][lane] = fmaf(Az[k], back, Ez[k]);
+    const float Bk = run[wave][1][k][lane];
+    run[wave][1][k][lane] = state;
+    state = fmaf(run[wave][0][k][lane], state, Bk);
   }
-  if (wave == 0 && p.dh0 && cw < p.D && chunk == 0) p.dh0[row] = fmaf(Aw, back, Ew);
+#pragma unroll
+  for (int k = kTs - 1; k >= 0; --k) {
+    const float Ek = run[wave][2][k][lane];
+    run[wave][2][k][lane] = back;
+    back = fmaf(run[wave][0][k][lane], back, Ek);
+  }
+  if (wave == 0 && p.dh0 && cw < p.D && chunk == 0) p.dh0[row] = back;
   wave_sync();
   float hh[4], ee[4], ws[4] = {0, 0, 0, 0};
   {
-    const f32x4 hw = *(const f32x4*)&run[wave][0][ts][4 * cl], ew = *(const f32x4*)&run[wave][1][ts][4 * cl];
+    const f32x4 hw = *(const f32x4*)&run[wave][1][ts][4 * cl], ew = *(const f32x4*)&run[wave][2][ts][4 * cl];
 #pragma unroll
     for (int e = 0; e < 4; ++e) hh[e] = hw[e], ee[e] = ew[e];
   }

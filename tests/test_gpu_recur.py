@@ -51,7 +51,7 @@ CASES = [
     (1, 1, 8, False, True), (3, 1, 2048, True, True), (2, 2, 24, True, False), (1, 15, 64, False, True), (2, 33, 72, False, True),
     (1, 127, 128, True, False), (2, 128, 40, False, True), (1, 129, 64, False, True), (3, 255, 8, False, False), (1, 256, 200, True, True),
     (2, 257, 64, False, True), (1, 1000, 136, False, True), (5, 640, 16, True, False), (1, 4100, 8, False, True),
-    (1, 8200, 16, False, False), (4, 5, 520, True, True), (9001, 2, 8, False, True), (3, 8, 264, False, False), (600, 130, 8, False, True),
+    (1, 8200, 16, False, False), (1, 35000, 8, True, True), (4, 5, 520, True, True), (9001, 2, 8, False, True), (3, 8, 264, False, False), (600, 130, 8, False, True),
 ]
 
 
