@@ -512,7 +512,7 @@ bpt_status bpt_recur_bwd(const bpt_recur_config* cfg, const void* x, const void*
 typedef struct {
   int64_t T, D, V, K;    /* tokens, hidden width, vocabulary, pairs of a list (<= 256)           */
   int64_t ldw;           /* columns of W as stored, as in bpt_xent_config                       */
-  int64_t block_rows;    /* tokens whose logits are live at once; 0 = automatic (8192)          */
+  int64_t block_rows;    /* tokens whose logits are live at once; 0 = automatic (16384)         */
   float tau;             /* temperature, > 0                                                    */
   float soft, hard;      /* >= 0; hard = 0: no targets                                          */
   int32_t dtype;         /* bpt_dtype of h, W and dh                                            */

@@ -16,7 +16,6 @@ namespace bpt {
 
 namespace {
 constexpr float kLog2e = 1.4426950408889634f;
-constexpr int kPer = (kDistillMaxK + 1 + 63) / 64;   // entries of a lane
 constexpr int kNone = 0x7FFFFFFF;
 
 BPT_DEV float wave_max(float v) {
@@ -27,8 +26,9 @@ BPT_DEV float wave_max(float v) {
 }  // namespace
 
 // One wave per token: valid entries sorted by index, an index that is given twice once with the sum of its probabilities; the
-// target's place among them; the token's factors. With seg, also how many entries lie before every 64 columns.
-// The order comes from counting smaller indices: K steps over LDS, 256 entries 4 times 256.
+// target's place among them; the token's factors. With seg, also where the entries of every 64 columns are.
+// The order comes from counting smaller indices: K steps over LDS for each of a lane's entries.
+template <int kPer>                                    // entries of a lane
 __global__ __launch_bounds__(256) void distill_prep_kernel(DistillArgs a) {
   __shared__ int skey[4][64 * kPer];
   __shared__ float sq[4][64 * kPer];
@@ -130,14 +130,19 @@ __global__ __launch_bounds__(256) void distill_prep_kernel(DistillArgs a) {
     a.w[t] = w;
   }
   if (a.seg) {
-    for (int g = lane; g <= a.ng; g += 64) {
-      int lo = 0, hi = n;                              // entries below 64 g
+    auto before = [&](int column) {                    // entries below a column
+      int lo = 0, hi = n;
       while (lo < hi) {
         const int mid = (lo + hi) >> 1;
-        if (skey[wv][mid] < 64 * g) lo = mid + 1;
+        if (skey[wv][mid] < column) lo = mid + 1;
         else hi = mid;
       }
-      a.seg[(t - a.t0) * a.ldseg + g] = (uint16_t)lo;
+      return lo;
+    };
+    for (int64_t g0 = 0; g0 < a.ng; g0 += 63) {        // a lane's end is its neighbour's start
+      const int64_t g = g0 + lane;
+      const int lo = before((int)std::min<int64_t>(64 * g, kNone)), hi = __shfl_down(lo, 1, 64);
+      if (lane < 63 && g < a.ng) a.seg[(t - a.t0) * a.ldseg + g] = (uint16_t)(lo << 7 | (hi - lo));
     }
   }
 }
@@ -269,7 +274,11 @@ hipError_t distill_prep(const DistillArgs& a, hipStream_t s) {
   if (b.weights) b.weights += a.t0;
   b.sidx += a.t0 * a.K1; b.sq += a.t0 * a.K1; b.ypos += a.t0; b.count += a.t0; b.gs += a.t0; b.gh += a.t0; b.w += a.t0;
   b.T = n; b.t0 = 0;
-  hipLaunchKernelGGL(distill_prep_kernel, dim3((unsigned)((n + 3) / 4)), dim3(256), 0, s, b);
+  const dim3 grid((unsigned)((n + 3) / 4));
+  static_assert(kDistillMaxK + 1 <= 64 * 5, "entries of a lane");
+  if (a.K1 <= 64) hipLaunchKernelGGL((distill_prep_kernel<1>), grid, dim3(256), 0, s, b);
+  else if (a.K1 <= 128) hipLaunchKernelGGL((distill_prep_kernel<2>), grid, dim3(256), 0, s, b);
+  else hipLaunchKernelGGL((distill_prep_kernel<5>), grid, dim3(256), 0, s, b);
   return hipGetLastError();
 }
 hipError_t distill_merge(const DistillArgs& a, const float* part, const float* part1, hipStream_t s) {

@@ -75,8 +75,8 @@ struct ListCol {
     g *= a.gscale;
     g1 *= a.gscale;
   }
-  BPT_DEV float grad(const GemmArgs& a, int64_t m, float v) const {
-    if (m >= a.nvalid || (g == 0.0f && g1 == 0.0f)) return 0.0f;
+  BPT_DEV bool none() const { return g == 0.0f && g1 == 0.0f; }
+  BPT_DEV float grad(const GemmArgs& a, float v) const {
     float r = g * __builtin_amdgcn_exp2f(fmaf(v, a.alpha, -l2));
     if (a.two) r = fmaf(g1, __builtin_amdgcn_exp2f(fmaf(v, 1.4426950408889634f, -l21)), r);
     return r;
@@ -114,7 +114,7 @@ BPT_DEV void epi_store(const GemmArgs& a, int64_t z, int64_t m, int64_t n, float
   } else if constexpr (EPI == EPI_LIST_T) {
     ListCol c;
     c.load(a, n);
-    C[idx] = from_f32<CT>(c.grad(a, m, v));
+    C[idx] = from_f32<CT>(m >= a.nvalid || c.none() ? 0.0f : c.grad(a, v));
   } else if constexpr (EPI == EPI_MUL) {
     const RT* R = (const RT*)a.R + z * a.sR;
     C[idx] = from_f32<CT>(v * to_f32<RT>(R[m * a.ldr + n]));
@@ -185,7 +185,7 @@ BPT_DEV void epi_store4(const GemmArgs& a, int64_t z, int64_t m, int64_t n, int6
     for (int e = 0; e < 4; ++e) {
       ListCol c;
       c.load(a, n + e);
-      v[e] = c.grad(a, m, v[e]);
+      v[e] = m >= a.nvalid || c.none() ? 0.0f : c.grad(a, v[e]);
     }
   } else if constexpr (EPI == EPI_MUL) {
     v *= V4<RT>::ld((const RT*)a.R + z * a.sR + m * a.ldr + n);
@@ -728,6 +728,27 @@ __global__ __launch_bounds__(128 * NWN * KG, 1) void gemm_bf16_kernel(GemmArgs a
 #pragma unroll
     for (int i = 0; i < PD; ++i) preload(i);
   }
+  // what the list epilogues read beside the accumulators, for all strips at once: the places of the listed logits among the
+  // wave's 64 columns, and what a lane's four columns contribute (the same ones in every strip)
+  uint32_t seg[EPI == EPI_LIST ? Cfg::TM : 1][EPI == EPI_LIST ? NIT : 1];
+  ListCol col[EPI == EPI_LIST_T ? 4 : 1];
+  bool none[4] = {};
+  if constexpr (EPI == EPI_LIST) {
+    const int64_t row0 = m0 + wm * Cfg::WM + lane / C4, g = std::min((n0 + wn * Cfg::WN) / 64, (ncols - 1) / 64);
+#pragma unroll
+    for (int i = 0; i < Cfg::TM; ++i)
+#pragma unroll
+      for (int it = 0; it < NIT; ++it) seg[i][it] = a.seg[std::min(row0 + 32 * i + RSTEP * it, a.M - 1) * a.ldseg + g];
+  }
+  if constexpr (EPI == EPI_LIST_T) {
+    if (inside) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        col[e].load(a, n0 + wn * Cfg::WN + 4 * (lane % C4) + e);
+        none[e] = col[e].none();
+      }
+    }
+  }
 #pragma unroll
   for (int i = 0; i < Cfg::TM; ++i) {
 #pragma unroll
@@ -776,17 +797,11 @@ __global__ __launch_bounds__(128 * NWN * KG, 1) void gemm_bf16_kernel(GemmArgs a
       static_assert(Cfg::WN == 64, "summaries of 64 columns");
       const int c0 = 4 * (lane % C4);
       const bool all = ncol + 64 <= a.nvalid;
-#pragma unroll 4
+#pragma unroll
       for (int it = 0; it < 32 / RSTEP; ++it) {
         const int row = lane / C4 + RSTEP * it;
         const int64_t m = mrow + row;
         const bool in = m < a.M && ncol < ncols;
-        int from = 0, to = 0;
-        if (in) {
-          const uint16_t* sg = a.seg + m * a.ldseg + ncol / 64;
-          from = sg[0];
-          to = sg[1];
-        }
         const f32x4 v = *(const f32x4*)(strip + row * PITCHF + c0);
         float mx = -__builtin_inff(), sum = 0.0f, sum1 = 0.0f;
 #pragma unroll
@@ -806,6 +821,7 @@ __global__ __launch_bounds__(128 * NWN * KG, 1) void gemm_bf16_kernel(GemmArgs a
           *(u32x2*)((float*)a.C + 2 * (m * a.ldc + ncol / 64)) = u32x2{__float_as_uint(mx), __float_as_uint(sum)};
           if (a.two) ((float*)a.C2)[m * a.ldc + ncol / 64] = sum1;
         }
+        const int from = (int)(seg[i][it] >> 7), to = in ? from + (int)(seg[i][it] & 127) : from;
         for (int e = from; e < to; ++e) {
           const int64_t k = a.list[m * a.ldlist + e] - ncol - c0;
           if (k >= 0 && k < 4) a.list_z[m * a.ldlist + e] = k == 0 ? v[0] : k == 1 ? v[1] : k == 2 ? v[2] : v[3];
@@ -847,15 +863,14 @@ __global__ __launch_bounds__(128 * NWN * KG, 1) void gemm_bf16_kernel(GemmArgs a
         continue;
       }
       if constexpr (EPI == EPI_LIST_T) {
-        ListCol col[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) col[e].load(a, ncol + c0 + e);
+        const bool words = mrow + 32 <= a.nvalid;      // every row of the strip is a logit
 #pragma unroll 4
         for (int it = 0; it < 32 / RSTEP; ++it) {
           const int row = r0 + RSTEP * it;
           f32x4 v = *(const f32x4*)(strip + row * PITCHF + c0);
+          const bool word = words || mrow + row < a.nvalid;
 #pragma unroll
-          for (int e = 0; e < 4; ++e) v[e] = col[e].grad(a, mrow + row, v[e]);
+          for (int e = 0; e < 4; ++e) v[e] = none[e] || !word ? 0.0f : col[e].grad(a, v[e]);
           V4<CT>::st(cb + (int64_t)RSTEP * it * a.ldc, v);
         }
         continue;

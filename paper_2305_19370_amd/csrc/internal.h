@@ -26,7 +26,7 @@ enum Epi {
                    // below nvalid, as two floats; tlogit[m] = acc[m, tgt[m]] for 0 <= tgt[m] < nvalid
   EPI_LIST = 8,    // bf16 operands; the same with exp2(alpha (acc - max)) and, with `two`, the sums of exp(acc - max)
                    // in C2[m, j]; list_z[m, e] = acc[m, list[m, e]] for the entries e of row m, sorted by column: those of
-                   // 64 columns j are seg[m, j] .. seg[m, j + 1]
+                   // 64 columns j are (seg[m, j] & 127) from seg[m, j] >> 7 on
   EPI_LIST_T = 9,  // gradient of transposed logits acc (rows m = vocabulary, columns n = tokens) without a list: for m < nvalid
                    // C = gscale (rowg[n] exp2(alpha acc - rowv[n] log2e) + rowg1[n] exp(acc - rowv1[n])), or without `two`
                    // gscale (rowg + rowg1)[n] exp2(..); C = 0 for nvalid <= m, and where rowg and rowg1 are 0
@@ -313,7 +313,7 @@ struct DistillArgs {
   float *lt = nullptr, *l1 = nullptr;   // log-sum-exp of z / tau, of z
   float *gs = nullptr, *gh = nullptr, *w = nullptr;   // factors of p_tau - q and of p_1 - onehot; weight
   float* tokens = nullptr;              // [2, Tall] kl, ce
-  uint16_t* seg = nullptr;              // block's rows of ldseg: entries before every 64 columns, or null
+  uint16_t* seg = nullptr;              // block's rows of ldseg: per 64 columns, entries before them << 7 | in them; or null
   int64_t t0 = 0, T = 0, Tall = 0, V = 0, ng = 0, ldseg = 0;
   int K = 0, K1 = 0, two = 0;           // two: hard targets at another temperature than 1
   float tau = 1, scale = 1, soft = 0, hard = 0, weight = 0;   // scale: log2(e) / tau
