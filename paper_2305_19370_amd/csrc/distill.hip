@@ -194,21 +194,47 @@ __global__ __launch_bounds__(256) void distill_merge_kernel(DistillArgs a, const
   finish(a, t, lane, m, l, l1);
 }
 
-// fp32: from the logits [rows, ld]
+// fp32: from the logits [rows, ld], ld a multiple of 64, by one workgroup per token: maximum, then sums and the listed logits, the
+// second time from the L2. (A wave per token walked 200 steps of 14302 logits.)
 __global__ __launch_bounds__(256) void distill_rows_kernel(DistillArgs a, const float* z, int64_t ld) {
-  const int lane = threadIdx.x & 63;
-  const int64_t t = a.t0 + (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (t >= a.T) return;
+  __shared__ float part[3][4];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int64_t t = a.t0 + blockIdx.x, whole = a.V / 4 * 4;
   const float* row = z + (t - a.t0) * ld;
   float m = -__builtin_inff(), l = 0.0f, l1 = 0.0f;
-  for (int64_t j = lane; j < a.V; j += 64) m = fmaxf(m, row[j]);
-  for (int64_t j = lane; j < a.V; j += 64) {
-    l += __builtin_amdgcn_exp2f((row[j] - m) * a.scale);
-    if (a.two) l1 += __builtin_amdgcn_exp2f((row[j] - m) * kLog2e);
+#pragma unroll 4
+  for (int64_t j = 4 * tid; j < whole; j += 1024) {
+    const f32x4 v = *(const f32x4*)(row + j);
+    m = fmaxf(m, fmaxf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3])));
   }
+  for (int64_t j = whole + tid; j < a.V; j += 256) m = fmaxf(m, row[j]);
+  m = wave_max(m);
+  if (lane == 0) part[0][wave] = m;
+  __syncthreads();
+  m = fmaxf(fmaxf(part[0][0], part[0][1]), fmaxf(part[0][2], part[0][3]));
+  auto add = [&](float v) {
+    l += __builtin_amdgcn_exp2f((v - m) * a.scale);
+    if (a.two) l1 += __builtin_amdgcn_exp2f((v - m) * kLog2e);
+  };
+#pragma unroll 2
+  for (int64_t j = 4 * tid; j < whole; j += 1024) {
+    const f32x4 v = *(const f32x4*)(row + j);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) add(v[e]);
+  }
+  for (int64_t j = whole + tid; j < a.V; j += 256) add(row[j]);
+  l = warp_sum(l);
+  l1 = warp_sum(l1);
+  if (lane == 0) part[1][wave] = l, part[2][wave] = l1;
+  __syncthreads();
+  if (wave > 0) return;
   const int n = a.count[t];
   for (int j = lane; j < n; j += 64) a.sz[t * a.K1 + j] = row[a.sidx[t * a.K1 + j]];
-  finish(a, t, lane, m, l, l1);
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "workgroup");   // finish() reads them by other lanes
+  // lane 0 holds the whole, the others nothing
+  l = (part[1][0] + part[1][1]) + (part[1][2] + part[1][3]);
+  l1 = (part[2][0] + part[2][1]) + (part[2][2] + part[2][3]);
+  finish(a, t, lane, lane ? -__builtin_inff() : m, lane ? 0.0f : l, lane ? 0.0f : l1);
 }
 
 // loss = (sum w (soft tau^2 kl + hard ce), sum w kl, sum w ce), in a fixed order by one workgroup
@@ -278,6 +304,7 @@ hipError_t distill_prep(const DistillArgs& a, hipStream_t s) {
   static_assert(kDistillMaxK + 1 <= 64 * 5, "entries of a lane");
   if (a.K1 <= 64) hipLaunchKernelGGL((distill_prep_kernel<1>), grid, dim3(256), 0, s, b);
   else if (a.K1 <= 128) hipLaunchKernelGGL((distill_prep_kernel<2>), grid, dim3(256), 0, s, b);
+  else if (a.K1 <= 192) hipLaunchKernelGGL((distill_prep_kernel<3>), grid, dim3(256), 0, s, b);
   else hipLaunchKernelGGL((distill_prep_kernel<5>), grid, dim3(256), 0, s, b);
   return hipGetLastError();
 }
@@ -286,7 +313,7 @@ hipError_t distill_merge(const DistillArgs& a, const float* part, const float* p
   return hipGetLastError();
 }
 hipError_t distill_rows(const DistillArgs& a, const float* z, int64_t ld, hipStream_t s) {
-  hipLaunchKernelGGL(distill_rows_kernel, dim3((unsigned)((a.T - a.t0 + 3) / 4)), dim3(256), 0, s, a, z, ld);
+  hipLaunchKernelGGL(distill_rows_kernel, dim3((unsigned)(a.T - a.t0)), dim3(256), 0, s, a, z, ld);
   return hipGetLastError();
 }
 hipError_t distill_loss(const DistillArgs& a, float* loss, hipStream_t s) {
