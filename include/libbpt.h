@@ -498,6 +498,27 @@ bpt_status bpt_recur_bwd(const bpt_recur_config* cfg, const void* x, const void*
                          const int32_t* lens, const float* h0, const void* saved, const void* dy, const float* dhT, void* dx,
                          void* dr, void* di, float* dlambda, float* dh0, void* workspace, size_t workspace_bytes, void* stream);
 
+/* The layer with the recurrence in place of attention: x = U Wq, r = U Wk and i = U Wv of its projection are the recurrence's input and
+ * gates, its y (D wide, no heads) is the O that Wo takes. cfg->causal must be 1, cfg->H only has to be valid. Everything else is as
+ * for bpt_layer_fwd / bpt_layer_bwd but the sizes of `saved` and of the workspace: bpt_layer_recurrent_*_bytes. (bpt_bwd_qkv_grad_offset
+ * does not hold: the backward leaves dx, dr, di token-major, [T, 3D].) */
+typedef struct {
+  float c;               /* as in bpt_recur_config                                              */
+  const float* lambda;   /* [D] fp32                                                            */
+  const float* h0;       /* [B, D] fp32, states before the first token, or NULL: zeros          */
+  float* hT;             /* [B, D] fp32, gets the last states (forward), or NULL; may be h0 if no backward follows */
+} bpt_recur_mixer;
+
+bpt_status bpt_layer_recurrent_validate(const bpt_config* cfg, const bpt_recur_mixer* mixer);
+size_t bpt_layer_recurrent_saved_bytes(const bpt_config* cfg);
+size_t bpt_layer_recurrent_workspace_bytes(const bpt_config* cfg, int backward);
+bpt_status bpt_layer_fwd_recurrent(const bpt_config* cfg, const bpt_recur_mixer* mixer, const void* X, const bpt_params* params,
+                                   void* Y, void* saved, void* workspace, size_t workspace_bytes, void* stream);
+/* dhT: gradient of the last states, or NULL. dlambda [D] and dh0 [B, D] fp32, overwritten; NULL skips. dh0 may be dhT. */
+bpt_status bpt_layer_bwd_recurrent(const bpt_config* cfg, const bpt_recur_mixer* mixer, const void* X, const bpt_params* params,
+                                   const void* saved, const void* dY, const float* dhT, void* dX, const bpt_grads* grads,
+                                   float* dlambda, float* dh0, void* workspace, size_t workspace_bytes, void* stream);
+
 /* Distillation of a language-model head from a teacher's largest logits, blockwise over tokens like bpt_xent_*: the [T, V]
  * logits never exist at once. Token t has the student's logits z = h W and a list of K pairs of the teacher, values v_j
  * and vocabulary indices k_j in any order:

@@ -102,6 +102,10 @@ class RecurConfig(ctypes.Structure):
                 ("y", RecurStrides), ("c", c_f32), ("dtype", c_i32), ("reserved", c_i64)]
 
 
+class RecurMixer(ctypes.Structure):
+    _fields_ = [("c", c_f32), ("lam", c_vp), ("h0", c_vp), ("hT", c_vp)]
+
+
 class DistillConfig(ctypes.Structure):
     _fields_ = [("T", c_i64), ("D", c_i64), ("V", c_i64), ("K", c_i64), ("ldw", c_i64), ("block_rows", c_i64), ("tau", c_f32),
                 ("soft", c_f32), ("hard", c_f32), ("dtype", c_i32), ("grad_dtype", c_i32), ("reserved", c_i32)]
@@ -126,7 +130,9 @@ EXPORTS = ("bpt_validate", "bpt_group_rows", "bpt_saved_bytes", "bpt_saved_layou
            "bpt_attn_workspace_bytes", "bpt_attn_fwd", "bpt_attn_bwd", "bpt_adamw_multi", "bpt_layer_options_validate",
            "bpt_layer_fwd_options", "bpt_layer_bwd_options", "bpt_recur_validate", "bpt_recur_saved_bytes",
            "bpt_recur_workspace_bytes", "bpt_recur_fwd", "bpt_recur_bwd", "bpt_distill_validate", "bpt_distill_saved_bytes",
-           "bpt_distill_workspace_bytes", "bpt_distill_fwd", "bpt_distill_bwd")
+           "bpt_distill_workspace_bytes", "bpt_distill_fwd", "bpt_distill_bwd", "bpt_layer_recurrent_validate",
+           "bpt_layer_recurrent_saved_bytes", "bpt_layer_recurrent_workspace_bytes", "bpt_layer_fwd_recurrent",
+           "bpt_layer_bwd_recurrent")
 
 _lib = None
 
@@ -220,6 +226,17 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.bpt_recur_fwd.restype = c_i32
     lib.bpt_recur_bwd.argtypes = [P(RecurConfig)] + [c_vp] * 15 + [c_sz, c_vp]
     lib.bpt_recur_bwd.restype = c_i32
+    lib.bpt_layer_recurrent_validate.argtypes = [P(Config), P(RecurMixer)]
+    lib.bpt_layer_recurrent_validate.restype = c_i32
+    lib.bpt_layer_recurrent_saved_bytes.argtypes = [P(Config)]
+    lib.bpt_layer_recurrent_saved_bytes.restype = c_sz
+    lib.bpt_layer_recurrent_workspace_bytes.argtypes = [P(Config), c_i32]
+    lib.bpt_layer_recurrent_workspace_bytes.restype = c_sz
+    lib.bpt_layer_fwd_recurrent.argtypes = [P(Config), P(RecurMixer), c_vp, P(Params), c_vp, c_vp, c_vp, c_sz, c_vp]
+    lib.bpt_layer_fwd_recurrent.restype = c_i32
+    lib.bpt_layer_bwd_recurrent.argtypes = [P(Config), P(RecurMixer), c_vp, P(Params), c_vp, c_vp, c_vp, c_vp, P(Grads), c_vp, c_vp,
+                                            c_vp, c_sz, c_vp]
+    lib.bpt_layer_bwd_recurrent.restype = c_i32
     lib.bpt_distill_validate.argtypes = [P(DistillConfig)]
     lib.bpt_distill_validate.restype = c_i32
     lib.bpt_distill_saved_bytes.argtypes = [P(DistillConfig)]
@@ -411,6 +428,21 @@ class Layer:
     def _bytes(self, n: int) -> torch.Tensor:
         return torch.empty(max(n, 256), dtype=torch.uint8, device=self.device)
 
+    def _grads(self, params: Dict[str, Optional[torch.Tensor]], want: Optional[Tuple[str, ...]]) -> Dict[str, torch.Tensor]:
+        """Buffers of the parameter gradients: those wanted (None: all) of the parameters that are there."""
+        D, F = self.cfg.D, self.cfg.F
+        shapes = {"dln1_g": (D,), "dln1_b": (D,), "dWq": (D, D), "dWk": (D, D), "dWv": (D, D), "dWo": (D, D),
+                  "dln2_g": (D,), "dln2_b": (D,), "dW1": (D, F), "db1": (F,), "dW2": (F, D), "db2": (D,)}
+        src = {"dln1_g": "ln1_g", "dln1_b": "ln1_b", "dln2_g": "ln2_g", "dln2_b": "ln2_b", "db1": "b1", "db2": "b2"}
+        grads = {}
+        for n, shp in shapes.items():
+            if want is not None and n not in want:
+                continue
+            if n in src and params.get(src[n]) is None:
+                continue
+            grads[n] = torch.empty(shp, dtype=torch.float32, device=self.device)
+        return grads
+
     def forward(self, X: torch.Tensor, params: Dict[str, Optional[torch.Tensor]],
                 workspace: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:
         Y = torch.empty(X.shape, dtype=self.out_dtype, device=self.device)
@@ -427,17 +459,7 @@ class Layer:
         Q = U Wq, K, V (copies of what the backward leaves in its workspace, bpt_bwd_qkv_grad_offset; not with a window)."""
         if qkv_grads and self.options is not None and self.options.window:
             raise ValueError("qkv_grads is for a layer without a window")
-        D, F = self.cfg.D, self.cfg.F
-        shapes = {"dln1_g": (D,), "dln1_b": (D,), "dWq": (D, D), "dWk": (D, D), "dWv": (D, D), "dWo": (D, D),
-                  "dln2_g": (D,), "dln2_b": (D,), "dW1": (D, F), "db1": (F,), "dW2": (F, D), "db2": (D,)}
-        src = {"dln1_g": "ln1_g", "dln1_b": "ln1_b", "dln2_g": "ln2_g", "dln2_b": "ln2_b", "db1": "b1", "db2": "b2"}
-        grads = {}
-        for n, shp in shapes.items():
-            if want is not None and n not in want:
-                continue
-            if n in src and params.get(src[n]) is None:
-                continue
-            grads[n] = torch.empty(shp, dtype=torch.float32, device=self.device)
+        grads = self._grads(params, want)
         dX = torch.empty(X.shape, dtype=self.out_dtype, device=self.device)
         ws = workspace if workspace is not None else self._bytes(workspace_bytes(self.cfg, True))
         layer_bwd(self.cfg, X, params, saved, dY, dX, grads, ws, self.options)
@@ -1053,6 +1075,88 @@ class GatedRecurrence:
         dh0 = torch.empty((cfg.B, cfg.D), dtype=torch.float32, device=x.device)
         recur_bwd(cfg, x, r, i, lam, saved, dy, *grads, self._bytes(recur_workspace_bytes(cfg, True), x.device), dlam, h0, dhT, dh0, lens)
         return dict(zip(("dx", "dr", "di"), grads), dlam=dlam, dh0=dh0)
+
+
+# ---------------------------------------------------------------- the layer with a recurrence
+def recur_mixer(cfg: Config, lam: torch.Tensor, c: float = 8.0, h0: Optional[torch.Tensor] = None,
+                hT: Optional[torch.Tensor] = None) -> RecurMixer:
+    """The recurrence of a layer: lam [D], states before and after [B, D], float32 on the GPU. It holds addresses alone."""
+    tensors = [t for t in (lam, h0, hT) if t is not None]
+    _stream_on(lam.get_device(), all(t.get_device() == lam.get_device() for t in tensors))
+    return RecurMixer(c, _f32(lam, (cfg.D,), "lam"), _f32(h0, (cfg.B, cfg.D), "h0"), _f32(hT, (cfg.B, cfg.D), "hT"))
+
+
+def layer_recurrent_validate(cfg: Config, c: float = 8.0) -> int:
+    return load().bpt_layer_recurrent_validate(ctypes.byref(cfg), RecurMixer(c, None, None, None))
+
+
+def layer_recurrent_saved_bytes(cfg: Config) -> int:
+    return load().bpt_layer_recurrent_saved_bytes(ctypes.byref(cfg))
+
+
+def layer_recurrent_workspace_bytes(cfg: Config, backward: bool) -> int:
+    return load().bpt_layer_recurrent_workspace_bytes(ctypes.byref(cfg), int(backward))
+
+
+def _check_layer(cfg: Config, saved: torch.Tensor, **tensors: torch.Tensor) -> None:
+    """Raises unless X, Y, dX (and dY) hold the tokens of a configuration, contiguous, and saved a recurrent layer's bytes."""
+    for name, t in tensors.items():
+        dt = _TORCH_DT.get(cfg.dtype if name in ("X", "dY") else cfg.out_dtype)
+        if t.dtype != dt or t.numel() != cfg.B * cfg.S * cfg.D or not t.is_contiguous():
+            raise ValueError(f"{name} must be {cfg.B} x {cfg.S} x {cfg.D} contiguous {dt}, not {tuple(t.shape)} of {t.dtype}")
+    _saved_ptr(saved, layer_recurrent_saved_bytes(cfg))
+
+
+def layer_fwd_recurrent(cfg: Config, mixer: RecurMixer, X: torch.Tensor, params: Dict[str, Optional[torch.Tensor]], Y: torch.Tensor,
+                        saved: torch.Tensor, workspace: torch.Tensor) -> None:
+    _check_layer(cfg, saved, X=X, Y=Y)
+    p = params_struct(params)
+    _check(load().bpt_layer_fwd_recurrent(ctypes.byref(cfg), ctypes.byref(mixer), X.data_ptr(), ctypes.byref(p), Y.data_ptr(),
+                                          saved.data_ptr(), workspace.data_ptr(), _nbytes(workspace), _stream()))
+
+
+def layer_bwd_recurrent(cfg: Config, mixer: RecurMixer, X: torch.Tensor, params: Dict[str, Optional[torch.Tensor]], saved: torch.Tensor,
+                        dY: torch.Tensor, dX: torch.Tensor, grads: Dict[str, Optional[torch.Tensor]], workspace: torch.Tensor,
+                        dlam: Optional[torch.Tensor] = None, dhT: Optional[torch.Tensor] = None,
+                        dh0: Optional[torch.Tensor] = None) -> None:
+    _check_layer(cfg, saved, X=X, dY=dY, dX=dX)
+    p = params_struct(params)
+    g = Grads(*[_ptr(grads.get(n)) for n in GRAD_FIELDS])
+    _check(load().bpt_layer_bwd_recurrent(ctypes.byref(cfg), ctypes.byref(mixer), X.data_ptr(), ctypes.byref(p), saved.data_ptr(),
+                                          dY.data_ptr(), _f32(dhT, (cfg.B, cfg.D), "dhT"), dX.data_ptr(), ctypes.byref(g),
+                                          _f32(dlam, (cfg.D,), "dlam"), _f32(dh0, (cfg.B, cfg.D), "dh0"), workspace.data_ptr(),
+                                          _nbytes(workspace), _stream()))
+
+
+class RecurrentLayer(Layer):
+    """A layer with the recurrence in place of attention; parameters as for Layer, and "lam" [D] (float32)."""
+
+    def __init__(self, cfg: Config, device: str = "cuda", c: float = 8.0):
+        super().__init__(cfg, device)
+        _check(layer_recurrent_validate(cfg, c))
+        self.c = c
+
+    def forward(self, X: torch.Tensor, params: Dict[str, Optional[torch.Tensor]], h0: Optional[torch.Tensor] = None,
+                workspace: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor, torch.Tensor]:
+        """Y, the last states [B, D] and what backward takes."""
+        Y = torch.empty(X.shape, dtype=self.out_dtype, device=self.device)
+        hT = torch.empty((self.cfg.B, self.cfg.D), dtype=torch.float32, device=self.device)
+        saved = self._bytes(layer_recurrent_saved_bytes(self.cfg))
+        ws = workspace if workspace is not None else self._bytes(layer_recurrent_workspace_bytes(self.cfg, False))
+        layer_fwd_recurrent(self.cfg, recur_mixer(self.cfg, params["lam"], self.c, h0, hT), X, params, Y, saved, ws)
+        return Y, hT, saved
+
+    def backward(self, X: torch.Tensor, params: Dict[str, Optional[torch.Tensor]], saved: torch.Tensor, dY: torch.Tensor,
+                 h0: Optional[torch.Tensor] = None, dhT: Optional[torch.Tensor] = None, want: Optional[Tuple[str, ...]] = None,
+                 workspace: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, Dict[str, torch.Tensor]]:
+        """dX and the parameter gradients, with "dlam" and "dh0"; h0 as it was."""
+        grads = self._grads(params, want)
+        dX = torch.empty(X.shape, dtype=self.out_dtype, device=self.device)
+        ws = workspace if workspace is not None else self._bytes(layer_recurrent_workspace_bytes(self.cfg, True))
+        dlam = torch.empty(self.cfg.D, dtype=torch.float32, device=self.device)
+        dh0 = torch.empty((self.cfg.B, self.cfg.D), dtype=torch.float32, device=self.device)
+        layer_bwd_recurrent(self.cfg, recur_mixer(self.cfg, params["lam"], self.c, h0), X, params, saved, dY, dX, grads, ws, dlam, dhT, dh0)
+        return dX, dict(grads, dlam=dlam, dh0=dh0)
 
 
 # ---------------------------------------------------------------- distillation from a teacher's largest logits

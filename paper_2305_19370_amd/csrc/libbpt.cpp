@@ -642,6 +642,87 @@ WinArgs layer_win(const bpt_config& c, const bpt_layer_options& o, const Dims& d
   return a;
 }
 
+// ---------------------------------------------------------------- gated linear recurrence: checks and arguments
+bpt_status recur_check(const bpt_recur_config* c) {
+  if (!c) return fail(BPT_ERR_INVALID_ARG, "config is NULL");
+  if (c->B < 1 || c->S < 1 || c->D < 1) return fail(BPT_ERR_INVALID_ARG, "B, S, D must be >= 1");
+  if (!(c->c > 0.0f) || !std::isfinite(c->c)) return fail(BPT_ERR_INVALID_ARG, "c must be > 0");
+  if (c->reserved != 0) return fail(BPT_ERR_INVALID_ARG, "reserved must be 0");
+  bpt_status st = dtype_ok(c->dtype, "dtype");
+  if (st != BPT_OK) return st;
+  const int64_t unit = 16 / (int64_t)esize(c->dtype);
+  for (const bpt_recur_strides* t : {&c->x, &c->r, &c->i, &c->y}) {
+    if (t->sb < 0 || t->st < 0) return fail(BPT_ERR_INVALID_ARG, "strides must be >= 0");
+    if (t->sb % unit || t->st % unit) return fail(BPT_ERR_INVALID_ARG, "strides must be multiples of 16 bytes");
+    if (t->sb >= (int64_t)1 << 40 || t->st >= (int64_t)1 << 21) return fail(BPT_ERR_UNSUPPORTED, "a stride is too large");
+  }
+  if (c->D % 8) return fail(BPT_ERR_UNSUPPORTED, "D must be a multiple of 8 (got %lld)", (long long)c->D);
+  if (c->S > kAttnMax || c->D > (int64_t)1 << 20) return fail(BPT_ERR_UNSUPPORTED, "S must be <= 2^28 and D <= 2^20");
+  // workgroups of a launch: 256 threads for 64 channels of 64 steps
+  const int64_t chunks = (c->S + kRecurKeep - 1) / kRecurKeep * ((c->D + kRecurCh - 1) / kRecurCh);
+  if (c->B > (int64_t)1 << 24 || c->B * chunks >= (int64_t)1 << 24) return fail(BPT_ERR_UNSUPPORTED, "B * S * D too large");
+  if (!apart({c->y.sb, c->y.st, 0}, c->B, c->S, 1, c->D)) return fail(BPT_ERR_INVALID_ARG, "strides of y overlap");
+  return BPT_OK;
+}
+
+int64_t recur_saved(const bpt_recur_config& c) { return c.B * ((c.S - 1) / kRecurKeep) * c.D * 4; }
+
+struct RecurWs {
+  float *part, *partial; // backward: dlambda of each chunk, and sums of those
+  void* chain;           // what the workgroups of a sequence tell one another (null: one workgroup takes it whole)
+};
+RecurWs recur_ws(const bpt_recur_config& c, void* base, int backward, int64_t* total) {
+  Bump bp(base);
+  RecurWs w{};
+  if (backward) {
+    const int64_t rows = c.B * recur_bwd_chunks(c.S);
+    w.part = (float*)bp.take(rows * c.D * 4);
+    w.partial = (float*)bp.take(recur_dlam_floats(rows, c.D) * 4);
+  }
+  RecurArgs a;
+  a.B = (int)c.B; a.S = c.S; a.D = (int)c.D;
+  if (const int64_t n = recur_chain_bytes(dt_of(c.dtype), a, backward); n > 0) w.chain = bp.take(n);
+  *total = rup(bp.off, kAlign);
+  return w;
+}
+
+RecurArgs recur_args(const bpt_recur_config& c, const void* x, const void* r, const void* i, const float* lambda,
+                            const int32_t* lens, const float* h0, const void* saved) {
+  RecurArgs a;
+  a.x = x; a.r = r; a.i = i; a.lam = lambda; a.lens = lens; a.h0 = h0; a.saved = (float*)saved;
+  a.x_sb = c.x.sb; a.x_st = c.x.st; a.r_sb = c.r.sb; a.r_st = c.r.st;
+  a.i_sb = c.i.sb; a.i_st = c.i.st; a.y_sb = c.y.sb; a.y_st = c.y.st;
+  a.B = (int)c.B; a.S = c.S; a.D = (int)c.D; a.c = c.c;
+  return a;
+}
+
+// The recurrence of a layer: the projection [T, 3D] is input and gates, its result the layer's O
+struct LayerRecur {
+  const bpt_recur_mixer* m;
+  const float* dhT;
+  float *dlambda, *dh0;
+};
+bpt_recur_config layer_recur(const bpt_config& c, float decay) {
+  bpt_recur_config r = {};
+  r.B = c.B; r.S = c.S; r.D = c.D;
+  r.x = r.r = r.i = {c.S * 3 * c.D, 3 * c.D};
+  r.y = {c.S * c.D, c.D};
+  r.c = decay; r.dtype = c.dtype;
+  return r;
+}
+bpt_status layer_recur_check(const bpt_config* c, const bpt_recur_mixer* m) {
+  bpt_status st = check(c);
+  if (st != BPT_OK) return st;
+  if (!m) return fail(BPT_ERR_INVALID_ARG, "mixer is NULL");
+  if (c->causal != 1) return fail(BPT_ERR_INVALID_ARG, "a recurrence is causal: causal must be 1");
+  const bpt_recur_config r = layer_recur(*c, m->c);
+  return recur_check(&r);
+}
+RecurArgs layer_recur_args(const bpt_config& c, const Dims& d, const LayerRecur& r, const SavedPtrs& sv, void* states) {
+  const int64_t E = (int64_t)d.E;
+  return recur_args(layer_recur(c, r.m->c), sv.qkv, off(sv.qkv, d.D * E), off(sv.qkv, 2 * d.D * E), r.m->lambda, nullptr, r.m->h0, states);
+}
+
 }  // namespace
 
 // Workspace of bpt_layer_fwd_noalloc: the library's own device memory, one copy per GPU,
@@ -825,9 +906,9 @@ bpt_status bpt_layer_fwd_noalloc(const bpt_config* cfg, const void* X, const bpt
   return bpt_layer_fwd(cfg, X, p, Y, saved, ws, kScratchBytes, stream);
 }
 
-static bpt_status layer_fwd(const bpt_config* cfg, const bpt_layer_options* opt, const void* X, const bpt_params* p, void* Y,
-                            void* saved, void* ws, size_t ws_bytes, void* stream) {
-  bpt_status st = opt ? options_check(cfg, opt) : check(cfg);
+static bpt_status layer_fwd(const bpt_config* cfg, const bpt_layer_options* opt, const LayerRecur* rec, const void* X,
+                            const bpt_params* p, void* Y, void* saved, void* ws, size_t ws_bytes, void* stream) {
+  bpt_status st = opt ? options_check(cfg, opt) : rec ? layer_recur_check(cfg, rec->m) : check(cfg);
   if (st != BPT_OK) return st;
   if (!X || !p || !Y || !saved || !ws) return fail(BPT_ERR_INVALID_ARG, "NULL X, params, Y, saved or workspace");
   if (!p->Wq || !p->Wk || !p->Wv || !p->Wo || !p->W1 || !p->W2)
@@ -841,6 +922,15 @@ static bpt_status layer_fwd(const bpt_config* cfg, const bpt_layer_options* opt,
   const Epi act = cfg->activation == BPT_RELU ? EPI_RELU : EPI_GELU;   // FFN epilogue of eq. (2)
   int64_t need, stotal;
   FwdWs w = fwd_ws(d, ws, &need);
+  RecurWs rw{};
+  if (rec) {
+    if (!rec->m->lambda) return fail(BPT_ERR_INVALID_ARG, "NULL lambda");
+    for (const void* q : {(const void*)rec->m->lambda, (const void*)rec->m->h0, (const void*)rec->m->hT})
+      if (q && !aligned16(q)) return fail(BPT_ERR_INVALID_ARG, "pointer %p is not 16-byte aligned", q);
+    int64_t more;
+    rw = recur_ws(layer_recur(*cfg, rec->m->c), off(ws, need), 0, &more);
+    need += more;
+  }
   if ((int64_t)ws_bytes < need)
     return fail(BPT_ERR_WORKSPACE, "workspace %zu bytes < required %lld", ws_bytes, (long long)need);
   SavedPtrs sv = saved_layout(d, saved, &stotal);
@@ -860,7 +950,7 @@ static bpt_status layer_fwd(const bpt_config* cfg, const bpt_layer_options* opt,
     GemmArgs g;
     g.A = w.u; g.lda = D; g.B = wqkv[i]; g.ldb = D; g.trans_b = 1;
     // bf16 attention takes Q multiplied by log2(e)/sqrt(dh): scores in base-2 units
-    if (i == 0 && E == BF16) g.alpha = (float)(1.4426950408889634 / std::sqrt((double)d.dh));
+    if (i == 0 && E == BF16 && !rec) g.alpha = (float)(1.4426950408889634 / std::sqrt((double)d.dh));
     g.C = off(sv.qkv, i * D * E_); g.ldc = 3 * D; g.M = T; g.N = D; g.K = D;
     if (one) {
       g.N = 3 * D; g.nper = D;
@@ -881,6 +971,11 @@ static bpt_status layer_fwd(const bpt_config* cfg, const bpt_layer_options* opt,
     a.few = attn_few(ac);
     RUN("win.fwd", 4.0 * d.dh * attn_seen(ac), 4.0 * T * D * E_, E == BF16 ? win_fwd_bf16(a, s) : win_fwd_f32(a, s));
   }
+  if (rec) {
+    RecurArgs a = layer_recur_args(*cfg, d, *rec, sv, off(saved, stotal));
+    a.y = sv.o; a.hT = rec->m->hT; a.chain = rw.chain;
+    RUN("recur.fwd", 20.0 * T * D, 4.0 * T * D * E_, recur_fwd(E, a, s));
+  }
 
   // Outer loop over groups of query blocks: attention for the group, then the
   // output projection, LN2, FFN and both residuals for the same rows.
@@ -898,7 +993,7 @@ static bpt_status layer_fwd(const bpt_config* cfg, const bpt_layer_options* opt,
       a.S = d.S; a.Sp = d.Sp; a.B = (int)d.B; a.H = (int)d.H; a.dh = (int)d.dh; a.causal = cfg->causal;
       a.q_begin = s0; a.q_end = s0 + rs; a.b_begin = (int)b; a.nb = (int)nb;
       const double pairs = attn_pairs(s0, s0 + rs, d.S, cfg->causal) * d.H * nb;
-      if (!win) RUN("attn.fwd", 4.0 * d.dh * pairs, (3.0 * rs + 2.0 * (s0 + rs)) * nb * D * E_, attn_fwd(E, a, s));
+      if (!win && !rec) RUN("attn.fwd", 4.0 * d.dh * pairs, (3.0 * rs + 2.0 * (s0 + rs)) * nb * D * E_, attn_fwd(E, a, s));
 
       GemmArgs go;     // h = X + O Wo
       go.A = off(sv.o, t0 * D * E_); go.lda = D; go.B = p->Wo; go.ldb = D; go.trans_b = 1;
@@ -952,7 +1047,7 @@ static bpt_status layer_fwd(const bpt_config* cfg, const bpt_layer_options* opt,
 
 bpt_status bpt_layer_fwd(const bpt_config* cfg, const void* X, const bpt_params* p, void* Y, void* saved,
                          void* ws, size_t ws_bytes, void* stream) {
-  return layer_fwd(cfg, nullptr, X, p, Y, saved, ws, ws_bytes, stream);
+  return layer_fwd(cfg, nullptr, nullptr, X, p, Y, saved, ws, ws_bytes, stream);
 }
 
 bpt_status bpt_layer_options_validate(const bpt_config* cfg, const bpt_layer_options* options) {
@@ -962,7 +1057,7 @@ bpt_status bpt_layer_options_validate(const bpt_config* cfg, const bpt_layer_opt
 bpt_status bpt_layer_fwd_options(const bpt_config* cfg, const bpt_layer_options* options, const void* X, const bpt_params* p,
                                  void* Y, void* saved, void* ws, size_t ws_bytes, void* stream) {
   if (!options) return fail(BPT_ERR_INVALID_ARG, "options is NULL");
-  return layer_fwd(cfg, options, X, p, Y, saved, ws, ws_bytes, stream);
+  return layer_fwd(cfg, options, nullptr, X, p, Y, saved, ws, ws_bytes, stream);
 }
 
 // QKV projection and LN1 backward from dQ, dK, dV token-major in w.dqkvT ([T, 3D], as the window kernels leave them). dU is three
@@ -1002,10 +1097,10 @@ static bpt_status layer_bwd_proj(const bpt_config& cfg, const Dims& d, Dt E, Dt 
   return BPT_OK;
 }
 
-static bpt_status layer_bwd(const bpt_config* cfg, const bpt_layer_options* opt, const void* X, const bpt_params* p,
-                            const void* saved, const void* dY, void* dX, const bpt_grads* gr, void* ws, size_t ws_bytes,
-                            void* stream) {
-  bpt_status st = opt ? options_check(cfg, opt) : check(cfg);
+static bpt_status layer_bwd(const bpt_config* cfg, const bpt_layer_options* opt, const LayerRecur* rec, const void* X,
+                            const bpt_params* p, const void* saved, const void* dY, void* dX, const bpt_grads* gr, void* ws,
+                            size_t ws_bytes, void* stream) {
+  bpt_status st = opt ? options_check(cfg, opt) : rec ? layer_recur_check(cfg, rec->m) : check(cfg);
   if (st != BPT_OK) return st;
   if (!X || !p || !saved || !dY || !dX || !ws)
     return fail(BPT_ERR_INVALID_ARG, "NULL X, params, saved, dY, dX or workspace");
@@ -1023,6 +1118,16 @@ static bpt_status layer_bwd(const bpt_config* cfg, const bpt_layer_options* opt,
   const Epi act = cfg->activation == BPT_RELU ? EPI_RELU : EPI_GELU;   // FFN epilogue of eq. (2)
   int64_t need, stotal;
   BwdWs w = bwd_ws(d, ws, &need);
+  RecurWs rw{};
+  if (rec) {
+    if (!rec->m->lambda) return fail(BPT_ERR_INVALID_ARG, "NULL lambda");
+    for (const void* q : {(const void*)rec->m->lambda, (const void*)rec->m->h0, (const void*)rec->dhT, (const void*)rec->dlambda, (const void*)rec->dh0})
+      if (q && !aligned16(q)) return fail(BPT_ERR_INVALID_ARG, "pointer %p is not 16-byte aligned", q);
+    if (rec->dh0 && (rec->dh0 == rec->m->h0 || rec->dh0 == rec->dlambda)) return fail(BPT_ERR_INVALID_ARG, "dh0 must not alias h0 or dlambda");
+    int64_t more;
+    rw = recur_ws(layer_recur(*cfg, rec->m->c), off(ws, need), 1, &more);
+    need += more;
+  }
   if ((int64_t)ws_bytes < need)
     return fail(BPT_ERR_WORKSPACE, "workspace %zu bytes < required %lld", ws_bytes, (long long)need);
   SavedPtrs sv = saved_layout(d, (void*)saved, &stotal);
@@ -1185,6 +1290,15 @@ static bpt_status layer_bwd(const bpt_config* cfg, const bpt_layer_options* opt,
           rope(E, rope_args(rc, nullptr, w.dqkvT, 3 * D, w.dqkvT, 3 * D, -1.0f), s));
     return layer_bwd_proj(*cfg, d, E, OUT, X, p, sv, w, G, dX, ln_part, ln_part_n, s);
   }
+  if (rec) {   // gradients of input and gates token-major, as the projection is
+    RecurArgs a = layer_recur_args(*cfg, d, *rec, sv, off(saved, stotal));
+    a.dy = w.dO; a.dhT = rec->dhT; a.dh0 = rec->dh0; a.part = rw.part; a.chain = rw.chain;
+    a.dx = w.dqkvT; a.dr = off(w.dqkvT, D * E_); a.di = off(w.dqkvT, 2 * D * E_);
+    RUN("recur.bwd", 35.0 * T * D, 7.0 * T * D * E_, recur_bwd(E, a, s));
+    if (rec->dlambda)
+      RUN("recur.dlambda", 0, (double)B * recur_bwd_chunks(S) * D * 4, recur_dlam(a, rec->dlambda, rw.partial, s));
+    return layer_bwd_proj(*cfg, d, E, OUT, X, p, sv, w, G, dX, ln_part, ln_part_n, s);
+  }
   RUN("attn.delta", 0, 2.0 * T * D * E_, attn_delta(E, w.dO, sv.o, D, sv.lse, w.ndelta, w.nlse2, B, S, Sp, (int)d.H, (int)d.dh, s));
   {
     AttnArgs a;
@@ -1252,14 +1366,44 @@ static bpt_status layer_bwd(const bpt_config* cfg, const bpt_layer_options* opt,
 
 bpt_status bpt_layer_bwd(const bpt_config* cfg, const void* X, const bpt_params* p, const void* saved,
                          const void* dY, void* dX, const bpt_grads* gr, void* ws, size_t ws_bytes, void* stream) {
-  return layer_bwd(cfg, nullptr, X, p, saved, dY, dX, gr, ws, ws_bytes, stream);
+  return layer_bwd(cfg, nullptr, nullptr, X, p, saved, dY, dX, gr, ws, ws_bytes, stream);
 }
 
 bpt_status bpt_layer_bwd_options(const bpt_config* cfg, const bpt_layer_options* options, const void* X, const bpt_params* p,
                                  const void* saved, const void* dY, void* dX, const bpt_grads* gr, void* ws, size_t ws_bytes,
                                  void* stream) {
   if (!options) return fail(BPT_ERR_INVALID_ARG, "options is NULL");
-  return layer_bwd(cfg, options, X, p, saved, dY, dX, gr, ws, ws_bytes, stream);
+  return layer_bwd(cfg, options, nullptr, X, p, saved, dY, dX, gr, ws, ws_bytes, stream);
+}
+
+// ---------------------------------------------------------------- the layer with a recurrence
+bpt_status bpt_layer_recurrent_validate(const bpt_config* cfg, const bpt_recur_mixer* mixer) { return layer_recur_check(cfg, mixer); }
+
+size_t bpt_layer_recurrent_saved_bytes(const bpt_config* cfg) {
+  const bpt_recur_mixer m = {1.0f, nullptr, nullptr, nullptr};
+  if (layer_recur_check(cfg, &m) != BPT_OK) return 0;
+  return bpt_saved_bytes(cfg) + (size_t)recur_saved(layer_recur(*cfg, 1.0f));
+}
+
+size_t bpt_layer_recurrent_workspace_bytes(const bpt_config* cfg, int backward) {
+  const bpt_recur_mixer m = {1.0f, nullptr, nullptr, nullptr};
+  if (layer_recur_check(cfg, &m) != BPT_OK) return 0;
+  int64_t more;
+  recur_ws(layer_recur(*cfg, 1.0f), nullptr, backward, &more);
+  return bpt_workspace_bytes(cfg, backward) + (size_t)more;
+}
+
+bpt_status bpt_layer_fwd_recurrent(const bpt_config* cfg, const bpt_recur_mixer* mixer, const void* X, const bpt_params* p, void* Y,
+                                   void* saved, void* ws, size_t ws_bytes, void* stream) {
+  const LayerRecur r = {mixer, nullptr, nullptr, nullptr};
+  return layer_fwd(cfg, nullptr, &r, X, p, Y, saved, ws, ws_bytes, stream);
+}
+
+bpt_status bpt_layer_bwd_recurrent(const bpt_config* cfg, const bpt_recur_mixer* mixer, const void* X, const bpt_params* p,
+                                   const void* saved, const void* dY, const float* dhT, void* dX, const bpt_grads* gr, float* dlambda,
+                                   float* dh0, void* ws, size_t ws_bytes, void* stream) {
+  const LayerRecur r = {mixer, dhT, dlambda, dh0};
+  return layer_bwd(cfg, nullptr, &r, X, p, saved, dY, dX, gr, ws, ws_bytes, stream);
 }
 
 // ---------------------------------------------------------------- cross-entropy of an LM head
@@ -1757,59 +1901,6 @@ bpt_status bpt_adamw_multi(const bpt_adamw_multi_config* cfg, const bpt_adamw_te
 }
 
 // ---------------------------------------------------------------- gated linear recurrence
-static bpt_status recur_check(const bpt_recur_config* c) {
-  if (!c) return fail(BPT_ERR_INVALID_ARG, "config is NULL");
-  if (c->B < 1 || c->S < 1 || c->D < 1) return fail(BPT_ERR_INVALID_ARG, "B, S, D must be >= 1");
-  if (!(c->c > 0.0f) || !std::isfinite(c->c)) return fail(BPT_ERR_INVALID_ARG, "c must be > 0");
-  if (c->reserved != 0) return fail(BPT_ERR_INVALID_ARG, "reserved must be 0");
-  bpt_status st = dtype_ok(c->dtype, "dtype");
-  if (st != BPT_OK) return st;
-  const int64_t unit = 16 / (int64_t)esize(c->dtype);
-  for (const bpt_recur_strides* t : {&c->x, &c->r, &c->i, &c->y}) {
-    if (t->sb < 0 || t->st < 0) return fail(BPT_ERR_INVALID_ARG, "strides must be >= 0");
-    if (t->sb % unit || t->st % unit) return fail(BPT_ERR_INVALID_ARG, "strides must be multiples of 16 bytes");
-    if (t->sb >= (int64_t)1 << 40 || t->st >= (int64_t)1 << 21) return fail(BPT_ERR_UNSUPPORTED, "a stride is too large");
-  }
-  if (c->D % 8) return fail(BPT_ERR_UNSUPPORTED, "D must be a multiple of 8 (got %lld)", (long long)c->D);
-  if (c->S > kAttnMax || c->D > (int64_t)1 << 20) return fail(BPT_ERR_UNSUPPORTED, "S must be <= 2^28 and D <= 2^20");
-  // workgroups of a launch: 256 threads for 64 channels of 64 steps
-  const int64_t chunks = (c->S + kRecurKeep - 1) / kRecurKeep * ((c->D + kRecurCh - 1) / kRecurCh);
-  if (c->B > (int64_t)1 << 24 || c->B * chunks >= (int64_t)1 << 24) return fail(BPT_ERR_UNSUPPORTED, "B * S * D too large");
-  if (!apart({c->y.sb, c->y.st, 0}, c->B, c->S, 1, c->D)) return fail(BPT_ERR_INVALID_ARG, "strides of y overlap");
-  return BPT_OK;
-}
-
-static int64_t recur_saved(const bpt_recur_config& c) { return c.B * ((c.S - 1) / kRecurKeep) * c.D * 4; }
-
-struct RecurWs {
-  float *part, *partial; // backward: dlambda of each chunk, and sums of those
-  void* chain;           // what the workgroups of a sequence tell one another (null: one workgroup takes it whole)
-};
-static RecurWs recur_ws(const bpt_recur_config& c, void* base, int backward, int64_t* total) {
-  Bump bp(base);
-  RecurWs w{};
-  if (backward) {
-    const int64_t rows = c.B * recur_bwd_chunks(c.S);
-    w.part = (float*)bp.take(rows * c.D * 4);
-    w.partial = (float*)bp.take(recur_dlam_floats(rows, c.D) * 4);
-  }
-  RecurArgs a;
-  a.B = (int)c.B; a.S = c.S; a.D = (int)c.D;
-  if (const int64_t n = recur_chain_bytes(dt_of(c.dtype), a, backward); n > 0) w.chain = bp.take(n);
-  *total = rup(bp.off, kAlign);
-  return w;
-}
-
-static RecurArgs recur_args(const bpt_recur_config& c, const void* x, const void* r, const void* i, const float* lambda,
-                            const int32_t* lens, const float* h0, const void* saved) {
-  RecurArgs a;
-  a.x = x; a.r = r; a.i = i; a.lam = lambda; a.lens = lens; a.h0 = h0; a.saved = (float*)saved;
-  a.x_sb = c.x.sb; a.x_st = c.x.st; a.r_sb = c.r.sb; a.r_st = c.r.st;
-  a.i_sb = c.i.sb; a.i_st = c.i.st; a.y_sb = c.y.sb; a.y_st = c.y.st;
-  a.B = (int)c.B; a.S = c.S; a.D = (int)c.D; a.c = c.c;
-  return a;
-}
-
 bpt_status bpt_recur_validate(const bpt_recur_config* cfg) { return recur_check(cfg); }
 
 size_t bpt_recur_saved_bytes(const bpt_recur_config* cfg) { return recur_check(cfg) == BPT_OK ? (size_t)recur_saved(*cfg) : 0; }

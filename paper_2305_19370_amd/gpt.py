@@ -14,6 +14,10 @@ For long contexts the layers' Q and K may carry rotary positions (GPTShape.rope)
 table, attention may be limited to a window and sinks (window, sinks), and AdamW may hold its moments in
 8 bits (opt_bits = 8: bpt_adamw_multi, both groups in one launch).
 
+A GPT whose cost per token does not grow with the context has layers with a gated recurrence in place of attention
+(GPTShape.recurrent), and learns what a teacher answers from the teacher's largest logits (distill_step: bpt_distill_* in place
+of bpt_xent_*).
+
 Parameters live in two flat fp32 buffers (weight matrices and embeddings, which take
 weight decay; LayerNorm gains/shifts and biases, which do not), each with matching
 flat gradient and moment buffers, so one optimiser step is two launches. Entries
@@ -60,6 +64,8 @@ class GPTShape:
     rope_orig_len: int = 0
     window: int = 0                # tokens that attention sees, 0 = all
     sinks: int = 0                 # first tokens that stay visible beyond the window
+    recurrent: bool = False        # layers with a gated recurrence in place of attention
+    recur_c: float = 8.0           # its decay: a = exp(-recur_c softplus(lam) sigmoid(gate))
     opt_bits: int = 32             # AdamW moments: 32 or 8 bits
     opt_seed: int = 0              # of the 8-bit moments' rounding
 
@@ -68,7 +74,7 @@ class GPTShape:
         return (self.V + 63) // 64 * 64
 
     def n_params(self) -> int:
-        per = 4 * self.D * self.D + 2 * self.D * self.F + 4 * self.D + (self.F + self.D if self.biases else 0)
+        per = 4 * self.D * self.D + 2 * self.D * self.F + 4 * self.D + (self.F + self.D if self.biases else 0) + (self.D if self.recurrent else 0)
         return (self.L * per + self.V * self.D + (self.S * self.D if self.pos_table else 0)
                 + 2 * self.D + self.D * self.V)
 
@@ -119,6 +125,10 @@ class GPT:
                                                   scaling=s.rope_scaling if rot else "none", factor=s.rope_factor,
                                                   orig_len=s.rope_orig_len, window=s.window, sinks=s.sinks)
             bpt._check(bpt.layer_options_validate(self.cfg, self.options))
+        if s.recurrent:
+            if self.options is not None:
+                raise ValueError("a recurrent model takes no rope, window or sinks")
+            bpt._check(bpt.layer_recurrent_validate(self.cfg, s.recur_c))
         bpt._check(bpt.validate(self.cfg))
         T = s.B * s.S
         self.xcfg = bpt.make_xent_config(T, s.D, s.V, ldw=s.ldw, block_rows=s.xent_block_rows, dtype=s.dtype)
@@ -134,13 +144,14 @@ class GPT:
         for l in range(s.L):
             mats += [(f"{l}.{k}", dims[k]) for k in LAYER_MATS]
             vecs += [(f"{l}.{k}", dims[k]) for k in LAYER_VECS if s.biases or k not in ("b1", "b2")]
+            vecs += [(f"{l}.lam", (s.D,))] if s.recurrent else []
         self.decay = _Flat(mats, device, lowp, s.opt_bits)
         self.nodecay = _Flat(vecs, device, None, s.opt_bits)     # vectors are read in fp32 by the kernels
         self.step_count = 0
 
         # activations, saved state, workspace
         self.X = [torch.empty((T, s.D), dtype=self.tdt, device=device) for _ in range(s.L + 1)]
-        sb = bpt.saved_bytes(self.cfg)
+        sb = bpt.layer_recurrent_saved_bytes(self.cfg) if s.recurrent else bpt.saved_bytes(self.cfg)
         self.saved = [torch.empty(max(sb, 256), dtype=torch.uint8, device=device) for _ in range(s.L)]
         self.hf = torch.empty((T, s.D), dtype=self.tdt, device=device)
         self.mean = torch.empty(T, dtype=torch.float32, device=device)
@@ -152,6 +163,9 @@ class GPT:
         ws = max(bpt.workspace_bytes(self.cfg, False), bpt.workspace_bytes(self.cfg, True),
                  bpt.xent_workspace_bytes(self.xcfg, False), bpt.xent_workspace_bytes(self.xcfg, True),
                  bpt.ln_workspace_bytes(self.lcfg), 256)
+        if s.recurrent:
+            ws = max(ws, *(bpt.layer_recurrent_workspace_bytes(self.cfg, k) for k in (False, True)))
+        self.distill = None                          # configuration and buffers of the last distill_forward
         self.ws = torch.empty(ws, dtype=torch.uint8, device=device)
         if init:
             self.init_params(seed)
@@ -184,7 +198,8 @@ class GPT:
 
     def init_params(self, seed: int) -> None:
         """GPT-2 style initialisation: N(0, 0.02) matrices and tables, residual
-        projections (Wo, W2) scaled by 1/sqrt(2L), gains 1, shifts and biases 0."""
+        projections (Wo, W2) scaled by 1/sqrt(2L), gains 1, shifts and biases 0; decays of a recurrence between 0.9 and
+        0.999 where its gate is fully open."""
         gen = torch.Generator(device="cpu").manual_seed(seed)
         s = self.shape
         for name in self.decay.index:
@@ -195,6 +210,10 @@ class GPT:
                 w[:, s.V:] = 0.0
             m.copy_(w)
         for name in self.nodecay.index:
+            if name.endswith(".lam"):
+                sp = -torch.log(torch.rand(s.D, generator=gen) * 0.099 + 0.9) / s.recur_c
+                self.master(name).copy_(torch.log(torch.expm1(sp)))
+                continue
             self.master(name).fill_(1.0 if name.endswith("_g") else 0.0)
         self.sync_lowp()
 
@@ -220,31 +239,77 @@ class GPT:
             self.cfg.dropout_seed = (self.shape.dropout_seed + (self.step_count << 20) + l) & (2 ** 64 - 1)
         return self.cfg
 
-    def forward(self, tokens: torch.Tensor, targets: torch.Tensor, saving: bool = True) -> torch.Tensor:
-        """Loss (a one-element fp32 tensor) of tokens [B*S] int32 with targets [B*S] int32."""
+    def _mixer(self, l: int) -> bpt.RecurMixer:
+        return bpt.recur_mixer(self.cfg, self.master(f"{l}.lam"), self.shape.recur_c)
+
+    def _body_forward(self, tokens: torch.Tensor) -> None:
+        """The head's input, self.hf, from tokens [B*S] int32."""
         s = self.shape
         bpt.embed_fwd(self.ecfg, tokens, self.weight("Wte"), self.weight("Wpe") if s.pos_table else None, self.X[0])
         for l in range(s.L):
+            if s.recurrent:
+                bpt.layer_fwd_recurrent(self._layer_cfg(l), self._mixer(l), self.X[l], self.layer_params(l), self.X[l + 1],
+                                        self.saved[l], self.ws)
+                continue
             bpt.layer_fwd(self._layer_cfg(l), self.X[l], self.layer_params(l), self.X[l + 1], self.saved[l], self.ws,
                           self.options)
         bpt.ln_fwd(self.lcfg, self.X[s.L], self.master("lnf_g"), self.master("lnf_b"), self.hf, self.mean, self.rstd)
+
+    def _body_backward(self, tokens: torch.Tensor) -> None:
+        """Gradients of what leads to self.hf from that of it, self.dh."""
+        s = self.shape
+        cur, nxt = self.dX
+        bpt.ln_bwd(self.lcfg, self.X[s.L], self.master("lnf_g"), self.mean, self.rstd, self.dh, cur,
+                   self.grad("lnf_g"), self.grad("lnf_b"), self.ws)
+        for l in range(s.L - 1, -1, -1):
+            if s.recurrent:
+                bpt.layer_bwd_recurrent(self._layer_cfg(l), self._mixer(l), self.X[l], self.layer_params(l), self.saved[l], cur, nxt,
+                                        self.layer_grads(l), self.ws, dlam=self.grad(f"{l}.lam"))
+            else:
+                bpt.layer_bwd(self._layer_cfg(l), self.X[l], self.layer_params(l), self.saved[l], cur, nxt, self.layer_grads(l),
+                              self.ws, self.options)
+            cur, nxt = nxt, cur
+        bpt.embed_bwd(self.ecfg, tokens, cur, self.grad("Wte"), self.grad("Wpe") if s.pos_table else None)
+        self.dX0 = cur
+
+    def forward(self, tokens: torch.Tensor, targets: torch.Tensor, saving: bool = True) -> torch.Tensor:
+        """Loss (a one-element fp32 tensor) of tokens [B*S] int32 with targets [B*S] int32."""
+        self._body_forward(tokens)
         bpt.xent_fwd(self.xcfg, self.hf, self.weight("Wout"), targets, self.loss, self.lse, self.ws)
         return self.loss
 
     def backward(self, tokens: torch.Tensor, targets: torch.Tensor, dloss: float = 1.0) -> None:
         """Gradients of dloss * loss into the flat gradient buffers (overwritten)."""
-        s = self.shape
         bpt.xent_bwd(self.xcfg, self.hf, self.weight("Wout"), targets, self.lse, dloss, self.dh, self.grad("Wout"),
                      self.ws)
-        cur, nxt = self.dX
-        bpt.ln_bwd(self.lcfg, self.X[s.L], self.master("lnf_g"), self.mean, self.rstd, self.dh, cur,
-                   self.grad("lnf_g"), self.grad("lnf_b"), self.ws)
-        for l in range(s.L - 1, -1, -1):
-            bpt.layer_bwd(self._layer_cfg(l), self.X[l], self.layer_params(l), self.saved[l], cur, nxt, self.layer_grads(l),
-                          self.ws, self.options)
-            cur, nxt = nxt, cur
-        bpt.embed_bwd(self.ecfg, tokens, cur, self.grad("Wte"), self.grad("Wpe") if s.pos_table else None)
-        self.dX0 = cur
+        self._body_backward(tokens)
+
+    def distill_forward(self, tokens: torch.Tensor, values: torch.Tensor, index: torch.Tensor, targets: Optional[torch.Tensor] = None,
+                        weights: Optional[torch.Tensor] = None, tau: float = 1.0, soft: float = 1.0, hard: float = 0.0) -> torch.Tensor:
+        """(loss, weighted kl, weighted ce) of tokens [B*S] int32 against a teacher's largest logits: values and index [B*S, K]
+        float32 and int32 (bpt.make_distill_config has the terms)."""
+        s, T = self.shape, self.shape.B * self.shape.S
+        cfg = bpt.make_distill_config(T, s.D, s.V, values.shape[1], ldw=s.ldw, block_rows=s.xent_block_rows, tau=tau, soft=soft,
+                                      hard=hard, dtype=s.dtype)
+        if self.distill is None or bytes(self.distill[0]) != bytes(cfg):
+            bpt._check(bpt.distill_validate(cfg))
+            new = lambda *n: torch.empty(n, dtype=torch.float32, device=self.device)  # noqa: E731
+            raw = lambda n: torch.empty(max(n, 256), dtype=torch.uint8, device=self.device)  # noqa: E731
+            self.distill = None                      # the old buffers go before new ones come
+            self.distill = (cfg, new(3), new(2, T), raw(bpt.distill_saved_bytes(cfg)),
+                            raw(max(bpt.distill_workspace_bytes(cfg, k) for k in (False, True))))
+        _, loss, per_token, saved, ws = self.distill
+        self._body_forward(tokens)
+        bpt.distill_fwd(cfg, self.hf, self.weight("Wout"), values, index, loss, per_token, saved, ws, targets, weights)
+        return loss
+
+    def distill_backward(self, tokens: torch.Tensor, dloss: float = 1.0) -> None:
+        """Gradients of dloss * the loss of the last distill_forward into the flat gradient buffers (overwritten)."""
+        if self.distill is None:
+            raise ValueError("distill_backward follows distill_forward")
+        cfg, _, _, saved, ws = self.distill
+        bpt.distill_bwd(cfg, self.hf, self.weight("Wout"), saved, dloss, self.dh, self.grad("Wout"), ws)
+        self._body_backward(tokens)
 
     def optimizer_step(self, lr: float, weight_decay: float = 0.1, beta1: float = 0.9, beta2: float = 0.95,
                        eps: float = 1e-8) -> None:
@@ -260,6 +325,15 @@ class GPT:
     def train_step(self, tokens: torch.Tensor, targets: torch.Tensor, lr: float, **opt) -> torch.Tensor:
         loss = self.forward(tokens, targets)
         self.backward(tokens, targets)
+        self.optimizer_step(lr, **opt)
+        return loss
+
+    def distill_step(self, tokens: torch.Tensor, values: torch.Tensor, index: torch.Tensor, lr: float,
+                     targets: Optional[torch.Tensor] = None, weights: Optional[torch.Tensor] = None, tau: float = 1.0,
+                     soft: float = 1.0, hard: float = 0.0, **opt) -> torch.Tensor:
+        """train_step on a teacher's largest logits."""
+        loss = self.distill_forward(tokens, values, index, targets, weights, tau, soft, hard)
+        self.distill_backward(tokens)
         self.optimizer_step(lr, **opt)
         return loss
 
