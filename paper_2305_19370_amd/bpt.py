@@ -980,12 +980,12 @@ def recur_fwd(cfg: RecurConfig, x: torch.Tensor, r: torch.Tensor, i: torch.Tenso
             _check_layout(t, at, name)
     B, D = cfg.B, cfg.D
     lp, h0p, hTp = _f32(lam, (D,), "lam"), _f32(h0, (B, D), "h0"), _f32(hT, (B, D), "hT")
+    sp = None if saved is None else _saved_ptr(saved, recur_saved_bytes(cfg))
     dev, nb = x.get_device(), _nbytes(workspace)
     same = all(t is None or t.get_device() == dev for t in (r, i, lam, y, h0, hT, saved, workspace, lens))
     stream = _stream_on(dev, same)
     _check(load().bpt_recur_fwd(cfg, x.data_ptr(), r.data_ptr(), i.data_ptr(), lp, _int32(lens, B, "lens"), h0p, y.data_ptr(), hTp,
-                                None if saved is None else _saved_ptr(saved, recur_saved_bytes(cfg)),
-                                workspace.data_ptr() if nb else None, nb, stream))
+                                sp, workspace.data_ptr() if nb else None, nb, stream))
 
 
 def recur_bwd(cfg: RecurConfig, x: torch.Tensor, r: torch.Tensor, i: torch.Tensor, lam: torch.Tensor, saved: Optional[torch.Tensor],
@@ -1001,11 +1001,11 @@ def recur_bwd(cfg: RecurConfig, x: torch.Tensor, r: torch.Tensor, i: torch.Tenso
     B, D = cfg.B, cfg.D
     lp, dlp = _f32(lam, (D,), "lam"), _f32(dlam, (D,), "dlam")
     h0p, dhTp, dh0p = _f32(h0, (B, D), "h0"), _f32(dhT, (B, D), "dhT"), _f32(dh0, (B, D), "dh0")
-    dev = x.get_device()
+    sp, dev = _saved_ptr(saved, recur_saved_bytes(cfg)), x.get_device()
     same = all(t is None or t.get_device() == dev for t in (r, i, lam, saved, dy, dx, dr, di, workspace, dlam, h0, dhT, dh0, lens))
     stream = _stream_on(dev, same)
     _check(load().bpt_recur_bwd(cfg, x.data_ptr(), r.data_ptr(), i.data_ptr(), lp, _int32(lens, B, "lens"), h0p,
-                                _saved_ptr(saved, recur_saved_bytes(cfg)), dy.data_ptr(), dhTp, dx.data_ptr(), dr.data_ptr(),
+                                sp, dy.data_ptr(), dhTp, dx.data_ptr(), dr.data_ptr(),
                                 di.data_ptr(), dlp, dh0p, workspace.data_ptr(), _nbytes(workspace), stream))
 
 
@@ -1196,11 +1196,10 @@ def distill_fwd(cfg: DistillConfig, h: torch.Tensor, W: torch.Tensor, values: to
             _dense(index, torch.int32, (T, K), "index"), _dense(targets, torch.int32, (T,), "targets"),
             _dense(weights, torch.float32, (T,), "weights"), _dense(loss, torch.float32, (3,), "loss"),
             _dense(tokens, torch.float32, (2, T), "tokens"))
-    dev = h.get_device()
+    sp, dev = _saved_ptr(saved, distill_saved_bytes(cfg)), h.get_device()
     same = all(t is None or t.get_device() == dev for t in (W, values, index, targets, weights, loss, tokens, saved, workspace))
     stream = _stream_on(dev, same)
-    _check(load().bpt_distill_fwd(cfg, *ptrs, _saved_ptr(saved, distill_saved_bytes(cfg)), workspace.data_ptr(), _nbytes(workspace),
-                                  stream))
+    _check(load().bpt_distill_fwd(cfg, *ptrs, sp, workspace.data_ptr(), _nbytes(workspace), stream))
 
 
 def distill_bwd(cfg: DistillConfig, h: torch.Tensor, W: torch.Tensor, saved: torch.Tensor, dloss: float, dh: torch.Tensor,
@@ -1208,11 +1207,10 @@ def distill_bwd(cfg: DistillConfig, h: torch.Tensor, W: torch.Tensor, saved: tor
     T, D, dt = cfg.T, cfg.D, _TORCH_DT.get(cfg.dtype)
     hp, Wp = _dense(h, dt, (T, D), "h"), _dense(W, dt, (D, cfg.ldw), "W")
     dhp, dWp = _dense(dh, dt, (T, D), "dh"), _dense(dW, _TORCH_DT.get(cfg.grad_dtype), (D, cfg.ldw), "dW")
-    dev = h.get_device()
+    sp, dev = _saved_ptr(saved, distill_saved_bytes(cfg)), h.get_device()
     same = all(t is None or t.get_device() == dev for t in (W, saved, dh, dW, workspace))
     stream = _stream_on(dev, same)
-    _check(load().bpt_distill_bwd(cfg, hp, Wp, _saved_ptr(saved, distill_saved_bytes(cfg)), float(dloss), dhp, dWp,
-                                  workspace.data_ptr(), _nbytes(workspace), stream))
+    _check(load().bpt_distill_bwd(cfg, hp, Wp, sp, float(dloss), dhp, dWp, workspace.data_ptr(), _nbytes(workspace), stream))
 
 
 class DistillLoss:

@@ -654,7 +654,7 @@ bpt_status recur_check(const bpt_recur_config* c) {
   for (const bpt_recur_strides* t : {&c->x, &c->r, &c->i, &c->y}) {
     if (t->sb < 0 || t->st < 0) return fail(BPT_ERR_INVALID_ARG, "strides must be >= 0");
     if (t->sb % unit || t->st % unit) return fail(BPT_ERR_INVALID_ARG, "strides must be multiples of 16 bytes");
-    if (t->sb >= (int64_t)1 << 40 || t->st >= (int64_t)1 << 21) return fail(BPT_ERR_UNSUPPORTED, "a stride is too large");
+    if (t->sb >= (int64_t)1 << 39 || t->st >= (int64_t)1 << 21) return fail(BPT_ERR_UNSUPPORTED, "a stride is too large");
   }
   if (c->D % 8) return fail(BPT_ERR_UNSUPPORTED, "D must be a multiple of 8 (got %lld)", (long long)c->D);
   if (c->S > kAttnMax || c->D > (int64_t)1 << 20) return fail(BPT_ERR_UNSUPPORTED, "S must be <= 2^28 and D <= 2^20");
@@ -1989,7 +1989,7 @@ static bpt_status distill_check(const bpt_distill_config* c) {
   if (c->grad_dtype == BPT_BF16 && c->dtype != BPT_BF16)
     return fail(BPT_ERR_UNSUPPORTED, "grad_dtype BPT_BF16 needs dtype BPT_BF16");
   if (c->K > kDistillMaxK) return fail(BPT_ERR_UNSUPPORTED, "K must be <= %d (got %lld)", kDistillMaxK, (long long)c->K);
-  if (c->V > ((int64_t)1 << 31) - 65 || c->ldw > (int64_t)1 << 31 || c->D * c->ldw > (int64_t)1 << 33)
+  if (c->V > ((int64_t)1 << 31) - 65 || c->ldw > (int64_t)1 << 31 || c->D > (int64_t)1 << 20 || c->D * c->ldw > (int64_t)1 << 33)
     return fail(BPT_ERR_UNSUPPORTED, "V or D V too large");
   // threads of a launch over a block's lists, and over its rows of h
   const int64_t R = distill_rows_of_block(*c);
