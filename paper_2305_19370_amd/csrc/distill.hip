@@ -17,6 +17,15 @@ namespace bpt {
 namespace {
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kNone = 0x7FFFFFFF;
+typedef __attribute__((__vector_size__(4 * sizeof(int)))) int i32x4;
+constexpr int kPiece = 1024;                         // of a token's row of `seg`
+
+// LDS that a wave's threads wrote becomes readable by its others
+BPT_DEV void lds_sync() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
 
 BPT_DEV float wave_max(float v) {
 #pragma unroll
@@ -30,8 +39,9 @@ BPT_DEV float wave_max(float v) {
 // The order comes from counting smaller indices: K steps over LDS for each of a lane's entries.
 template <int kPer>                                    // entries of a lane
 __global__ __launch_bounds__(256) void distill_prep_kernel(DistillArgs a) {
-  __shared__ int skey[4][64 * kPer];
-  __shared__ float sq[4][64 * kPer];
+  __shared__ __attribute__((aligned(16))) int skey[4][64 * kPer];
+  __shared__ __attribute__((aligned(16))) float sq[4][64 * kPer];
+  __shared__ __attribute__((aligned(16))) uint16_t sseg[4][kPiece];
   const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
   const int64_t t = (int64_t)blockIdx.x * 4 + wv;      // a wave past the end works on the last token and stores nothing
   const bool real = t < a.T;
@@ -83,16 +93,19 @@ __global__ __launch_bounds__(256) void distill_prep_kernel(DistillArgs a) {
   float qs[kPer];
 #pragma unroll
   for (int e = 0; e < kPer; ++e) first[e] = key[e] != kNone, qs[e] = 0.0f;
-  for (int i = 0; i < K1; ++i) {
-    const int k = skey[wv][i];
-    const float v = sq[wv][i];
+  // four entries at a time, without branches; those behind the last one are kNone, which no entry that counts is
+#pragma unroll 2
+  for (int i = 0; i < K1; i += 4) {
+    const i32x4 k = *(const i32x4*)&skey[wv][i];
+    const f32x4 v = *(const f32x4*)&sq[wv][i];
 #pragma unroll
-    for (int e = 0; e < kPer; ++e) {
-      if (k == key[e]) {
-        qs[e] += v;
-        if (i < lane + 64 * e) first[e] = false;
+    for (int u = 0; u < 4; ++u)
+#pragma unroll
+      for (int e = 0; e < kPer; ++e) {
+        const bool same = k[u] == key[e];
+        qs[e] += same ? v[u] : 0.0f;
+        first[e] = first[e] && !(same && i + u < lane + 64 * e);
       }
-    }
   }
   __syncthreads();
 #pragma unroll
@@ -102,11 +115,15 @@ __global__ __launch_bounds__(256) void distill_prep_kernel(DistillArgs a) {
   int rank[kPer], n = 0;
 #pragma unroll
   for (int e = 0; e < kPer; ++e) rank[e] = 0;
-  for (int i = 0; i < K1; ++i) {
-    const int k = skey[wv][i];
-    n += k != kNone;
+#pragma unroll 2
+  for (int i = 0; i < K1; i += 4) {
+    const i32x4 k = *(const i32x4*)&skey[wv][i];
 #pragma unroll
-    for (int e = 0; e < kPer; ++e) rank[e] += k < key[e];
+    for (int u = 0; u < 4; ++u) {
+      n += k[u] != kNone;
+#pragma unroll
+      for (int e = 0; e < kPer; ++e) rank[e] += k[u] < key[e];
+    }
   }
   __syncthreads();
 #pragma unroll
@@ -130,19 +147,23 @@ __global__ __launch_bounds__(256) void distill_prep_kernel(DistillArgs a) {
     a.w[t] = w;
   }
   if (a.seg) {
-    auto before = [&](int column) {                    // entries below a column
-      int lo = 0, hi = n;
-      while (lo < hi) {
-        const int mid = (lo + hi) >> 1;
-        if (skey[wv][mid] < column) lo = mid + 1;
-        else hi = mid;
+    // pieces of the row in LDS: zeros, then from the first entry of every 64 columns that have any
+    uint16_t* piece = sseg[wv];
+    for (int64_t g0 = 0; g0 < a.ng; g0 += kPiece) {
+      const int len = (int)std::min<int64_t>(a.ldseg - g0, kPiece);   // a multiple of 8
+      for (int c = 8 * lane; c < len; c += 512) *(u32x4*)(piece + c) = u32x4{0, 0, 0, 0};
+      lds_sync();
+      for (int e = lane; e < n; e += 64) {
+        const int g = skey[wv][e] >> 6;
+        if (g < g0 || g >= g0 + len || (e > 0 && skey[wv][e - 1] >> 6 == g)) continue;
+        int many = 1;
+        while (e + many < n && skey[wv][e + many] >> 6 == g) ++many;
+        piece[g - g0] = (uint16_t)(e << 7 | many);
       }
-      return lo;
-    };
-    for (int64_t g0 = 0; g0 < a.ng; g0 += 63) {        // a lane's end is its neighbour's start
-      const int64_t g = g0 + lane;
-      const int lo = before((int)std::min<int64_t>(64 * g, kNone)), hi = __shfl_down(lo, 1, 64);
-      if (lane < 63 && g < a.ng) a.seg[(t - a.t0) * a.ldseg + g] = (uint16_t)(lo << 7 | (hi - lo));
+      lds_sync();
+      u32x4* out = (u32x4*)(a.seg + (t - a.t0) * a.ldseg + g0);
+      for (int c = lane; c < len / 8; c += 64) out[c] = ((const u32x4*)piece)[c];
+      lds_sync();
     }
   }
 }
@@ -186,10 +207,17 @@ __global__ __launch_bounds__(256) void distill_merge_kernel(DistillArgs a, const
   const int64_t t = a.t0 + (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
   if (t >= a.T) return;
   float m = -__builtin_inff(), l = 0.0f, l1 = 0.0f;
-  for (int64_t j = lane; j < a.ng; j += 64) {
-    const int64_t at = (t - a.t0) * a.ng + j;
-    const u32x2 v = *(const u32x2*)(part + 2 * at);
-    join(m, l, l1, __uint_as_float(v[0]), __uint_as_float(v[1]), a.two ? part1[at] : 0.0f, a.scale);
+  for (int64_t j0 = lane; j0 < a.ng; j0 += 512) {      // eight in flight
+    u32x2 v[8];
+    float v1[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const int64_t j = j0 + 64 * k, at = (t - a.t0) * a.ng + j;
+      v[k] = j < a.ng ? *(const u32x2*)(part + 2 * at) : u32x2{0xFF800000u, 0u};   // -inf, 0
+      v1[k] = a.two && j < a.ng ? part1[at] : 0.0f;
+    }
+#pragma unroll
+    for (int k = 0; k < 8; ++k) join(m, l, l1, __uint_as_float(v[k][0]), __uint_as_float(v[k][1]), v1[k], a.scale);
   }
   finish(a, t, lane, m, l, l1);
 }
@@ -266,28 +294,28 @@ __global__ __launch_bounds__(1024) void distill_loss_kernel(DistillArgs a, float
   }
 }
 
-// The listed elements of the logits' gradient, transposed [V, ld] with the block's tokens as columns
+// Workgroups from `first` on: the listed elements of the logits' gradient, transposed [V, ld] with the block's tokens as columns. Those
+// before it: h of the tokens that have a gradient, zeros for the others, so that what those hold does not reach dW.
 template <typename T>
-__global__ __launch_bounds__(256) void distill_listed_kernel(DistillArgs a, float dloss, T* G, int64_t ld) {
-  const int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x, rows = a.T - a.t0;
+__global__ __launch_bounds__(256) void distill_listed_kernel(DistillArgs a, float dloss, T* G, int64_t ld, const T* h, T* out, int64_t D,
+                                                             uint32_t first) {
+  const int64_t rows = a.T - a.t0;
+  if (blockIdx.x < first) {
+    constexpr int N = 16 / sizeof(T);
+    const int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x, t = e / (D / N);
+    if (t >= rows) return;
+    const bool in = a.gs[a.t0 + t] != 0.0f || a.gh[a.t0 + t] != 0.0f;
+    ((u32x4*)out)[e] = in ? ((const u32x4*)h)[e] : u32x4{0, 0, 0, 0};
+    return;
+  }
   // neighbouring threads take neighbouring tokens: their lists' columns of G are neighbours
-  const int64_t j = e / rows, t = a.t0 + e % rows;
+  const int64_t e = (int64_t)(blockIdx.x - first) * 256 + threadIdx.x, j = e / rows, t = a.t0 + e % rows;
   if (j >= a.K1 || j >= a.count[t]) return;
   const float gs = a.gs[t], gh = a.gh[t], z = a.sz[t * a.K1 + j];
   if (gs == 0.0f && gh == 0.0f) return;
   const float p = __builtin_amdgcn_exp2f(z * a.scale - a.lt[t] * kLog2e), p1 = a.two ? __builtin_amdgcn_exp2f((z - a.l1[t]) * kLog2e) : p;
   const float g = gs * (p - a.sq[t * a.K1 + j]) + gh * (a.ypos[t] == j ? p1 - 1.0f : p1);
   G[(int64_t)a.sidx[t * a.K1 + j] * ld + (t - a.t0)] = from_f32<T>(dloss * g);
-}
-
-// h of the tokens that have a gradient, zeros for the others, so that what those hold does not reach dW
-template <typename T>
-__global__ __launch_bounds__(256) void distill_rows_of_kernel(DistillArgs a, const T* h, T* out, int64_t D) {
-  constexpr int N = 16 / sizeof(T);
-  const int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x, per = D / N, t = e / per;
-  if (t >= a.T - a.t0) return;
-  const bool in = a.gs[a.t0 + t] != 0.0f || a.gh[a.t0 + t] != 0.0f;
-  ((u32x4*)out)[e] = in ? ((const u32x4*)h)[e] : u32x4{0, 0, 0, 0};
 }
 
 // ------------------------------------------------------------------ launchers
@@ -320,17 +348,14 @@ hipError_t distill_loss(const DistillArgs& a, float* loss, hipStream_t s) {
   hipLaunchKernelGGL(distill_loss_kernel, dim3(1), dim3(1024), 0, s, a, loss);
   return hipGetLastError();
 }
-hipError_t distill_listed(Dt t, const DistillArgs& a, float dloss, void* G, int64_t ld, hipStream_t s) {
-  const dim3 grid((unsigned)(((a.T - a.t0) * a.K1 + 255) / 256));
-  if (t == F32) hipLaunchKernelGGL((distill_listed_kernel<float>), grid, dim3(256), 0, s, a, dloss, (float*)G, ld);
-  else hipLaunchKernelGGL((distill_listed_kernel<bf16>), grid, dim3(256), 0, s, a, dloss, (bf16*)G, ld);
-  return hipGetLastError();
-}
-hipError_t distill_rows_of(Dt t, const DistillArgs& a, const void* h, void* out, int64_t D, hipStream_t s) {
-  const int64_t n = (a.T - a.t0) * D / (t == F32 ? 4 : 8);
-  const dim3 grid((unsigned)((n + 255) / 256));
-  if (t == F32) hipLaunchKernelGGL((distill_rows_of_kernel<float>), grid, dim3(256), 0, s, a, (const float*)h, (float*)out, D);
-  else hipLaunchKernelGGL((distill_rows_of_kernel<bf16>), grid, dim3(256), 0, s, a, (const bf16*)h, (bf16*)out, D);
+hipError_t distill_listed(Dt t, const DistillArgs& a, float dloss, void* G, int64_t ld, const void* h, void* out, int64_t D,
+                          hipStream_t s) {
+  const int64_t rows = a.T - a.t0, n = out ? (rows * D / (t == F32 ? 4 : 8) + 255) / 256 : 0;
+  const dim3 grid((unsigned)(n + (rows * a.K1 + 255) / 256));
+  if (t == F32)
+    hipLaunchKernelGGL((distill_listed_kernel<float>), grid, dim3(256), 0, s, a, dloss, (float*)G, ld, (const float*)h, (float*)out, D, (uint32_t)n);
+  else
+    hipLaunchKernelGGL((distill_listed_kernel<bf16>), grid, dim3(256), 0, s, a, dloss, (bf16*)G, ld, (const bf16*)h, (bf16*)out, D, (uint32_t)n);
   return hipGetLastError();
 }
 

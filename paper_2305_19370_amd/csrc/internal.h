@@ -322,8 +322,8 @@ hipError_t distill_prep(const DistillArgs& a, hipStream_t s);
 hipError_t distill_merge(const DistillArgs& a, const float* part, const float* part1, hipStream_t s);   // EPI_LIST's C, C2
 hipError_t distill_rows(const DistillArgs& a, const float* z, int64_t ld, hipStream_t s);
 hipError_t distill_loss(const DistillArgs& a, float* loss, hipStream_t s);
-hipError_t distill_listed(Dt t, const DistillArgs& a, float dloss, void* G, int64_t ld, hipStream_t s);
-hipError_t distill_rows_of(Dt t, const DistillArgs& a, const void* h, void* out, int64_t D, hipStream_t s);
+// the listed elements of G, and unless out is null the block's rows of h there, zeros for those without a gradient
+hipError_t distill_listed(Dt t, const DistillArgs& a, float dloss, void* G, int64_t ld, const void* h, void* out, int64_t D, hipStream_t s);
 
 // ---------------------------------------------------------------- GPT step pieces
 // X[t] = Wte[tok[t]] + Wpe[t mod S] (Wpe may be null); NaN row for tok outside [0, V). D % 8 == 0.

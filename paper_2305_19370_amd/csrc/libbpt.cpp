@@ -1991,15 +1991,18 @@ static bpt_status distill_check(const bpt_distill_config* c) {
   if (c->K > kDistillMaxK) return fail(BPT_ERR_UNSUPPORTED, "K must be <= %d (got %lld)", kDistillMaxK, (long long)c->K);
   if (c->V > ((int64_t)1 << 31) - 65 || c->ldw > (int64_t)1 << 31 || c->D > (int64_t)1 << 20 || c->D * c->ldw > (int64_t)1 << 33)
     return fail(BPT_ERR_UNSUPPORTED, "V or D V too large");
-  // threads of a launch over a block's lists, and over its rows of h
+  // threads of a launch over a block's lists and its rows of h
   const int64_t R = distill_rows_of_block(*c);
-  if (R > (int64_t)1 << 22 || R * std::max(c->K + 1, c->D / 4) >= (int64_t)1 << 32)
+  if (R > (int64_t)1 << 22 || R * (c->K + 1 + c->D / 4) >= (int64_t)1 << 32)
     return fail(BPT_ERR_UNSUPPORTED, "block_rows too large");
   return BPT_OK;
 }
 
 static XentDims distill_dims(const bpt_distill_config& c) {
-  return xent_dims({c.T, c.D, c.V, c.ldw, distill_rows_of_block(c), c.dtype, 0});
+  XentDims d = xent_dims({c.T, c.D, c.V, c.ldw, distill_rows_of_block(c), c.dtype, 0});
+  // fp32 too: 38 tokens, D = 2496, V = 14302 the backward takes 188 us, with dh in one slice 248
+  if (d.E == 4) d.zdh = gemm_ksplit(F32, std::min(d.T, kDefaultXentRows), d.D, d.ldw, kMaxKSplit);
+  return d;
 }
 
 static DistillArgs distill_args(const bpt_distill_config& c, const void* saved, int64_t* total) {
@@ -2088,7 +2091,7 @@ bpt_status bpt_distill_fwd(const bpt_distill_config* cfg, const void* h, const v
     RUN("distill.prep", 0, (double)r * (20.0 * a.K1 + 2.0 * ng), distill_prep(a, s));
     GemmArgs g;   // logits of the block: h W, W read as it is stored (B operand K-major)
     g.A = (const char*)h + t0 * d.D * E_; g.lda = d.D;
-    g.B = W; g.ldb = d.ldw; g.trans_b = 1; g.in_order = 1;
+    g.B = W; g.ldb = d.ldw; g.trans_b = 1; g.in_order = E == BF16;
     g.C = w.logits; g.ldc = d.ldw; g.M = r; g.N = d.ldw; g.K = d.D;
     if (E == BF16) {
       g.ldc = ng; g.nvalid = d.V; g.alpha = a.scale; g.two = a.two; g.C2 = w.part1;
@@ -2132,15 +2135,16 @@ bpt_status bpt_distill_bwd(const bpt_distill_config* cfg, const void* h, const v
       GemmArgs g;
       g.A = W; g.lda = d.ldw; g.trans_a = 1; g.B = hb; g.ldb = d.D;
       g.C = w.g; g.ldc = d.Rp; g.M = d.ldw; g.N = r; g.Nstore = rp; g.K = d.D;
-      g.in_order = 1; g.alpha = a.scale; g.gscale = dloss; g.two = a.two; g.nvalid = d.V;
+      g.in_order = E == BF16; g.alpha = a.scale; g.gscale = dloss; g.two = a.two; g.nvalid = d.V;
       g.rowv = a.lt + t0; g.rowg = a.gs + t0; g.rowv1 = a.l1 + t0; g.rowg1 = a.gh + t0;
       RUN("distill.grad_logits", gemm_flops(g), gemm_bytes(g, E_, E_), gemm(E, EPI_LIST_T, E, F32, g, s));
-      RUN("distill.listed", 0, (double)r * a.K1 * 16, distill_listed(E, a, dloss, w.g, d.Rp, s));
+      RUN("distill.listed", 0, (double)r * a.K1 * 16 + (dW ? 2.0 * r * d.D * E_ : 0.0),
+          distill_listed(E, a, dloss, w.g, d.Rp, hb, dW ? w.hz : nullptr, d.D, s));
     }
     {   // dh = G W^T
       GemmArgs g;
       g.A = w.g; g.lda = d.Rp; g.trans_a = 1; g.a_cols = d.Rp; g.B = W; g.ldb = d.ldw;
-      g.C = (char*)dh + t0 * d.D * E_; g.ldc = d.D; g.M = r; g.N = d.D; g.K = d.ldw; g.in_order = 1;
+      g.C = (char*)dh + t0 * d.D * E_; g.ldc = d.D; g.M = r; g.N = d.D; g.K = d.ldw; g.in_order = E == BF16;
       if (d.zdh > 1) {
         void* out = g.C;
         g.ksplit = d.zdh; g.C = w.part; g.sC = r * d.D;
@@ -2151,12 +2155,11 @@ bpt_status bpt_distill_bwd(const bpt_distill_config* cfg, const void* h, const v
       }
     }
     if (dW) {   // dW = h^T G
-      RUN("distill.h", 0, 2.0 * r * d.D * E_, distill_rows_of(E, a, hb, w.hz, d.D, s));
       GemmArgs g;
       g.A = w.hz; g.lda = d.D; g.trans_a = 1; g.a_rows = r;
       g.B = w.g; g.ldb = d.Rp;
       g.C = w.dw ? (void*)w.dw : dW; g.ldc = d.ldw; g.M = d.D; g.N = d.ldw; g.K = rp; g.accumulate = t0 > 0;
-      g.in_order = 1;
+      g.in_order = E == BF16;
       const Dt CT = w.dw ? F32 : GT;
       RUN("distill.dW", gemm_flops(g), gemm_bytes(g, E_, CT == F32 ? 4 : 2), gemm(E, EPI_STORE, CT, F32, g, s));
     }
