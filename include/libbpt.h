@@ -519,8 +519,8 @@ bpt_status bpt_layer_bwd_recurrent(const bpt_config* cfg, const bpt_recur_mixer*
                                    const void* saved, const void* dY, const float* dhT, void* dX, const bpt_grads* grads,
                                    float* dlambda, float* dh0, void* workspace, size_t workspace_bytes, void* stream);
 
-/* Distillation of a language-model head from a teacher's largest logits, blockwise over tokens like bpt_xent_*: the [T, V]
- * logits never exist at once. Token t has the student's logits z = h W and a list of K pairs of the teacher, values v_j
+/* Distillation of a language-model head from a teacher's largest logits, by blocks of tokens like bpt_xent_*: beyond keep_bytes
+ * nothing of [T, V] exists at once. Token t has the student's logits z = h W and a list of K pairs of the teacher, values v_j
  * and vocabulary indices k_j in any order:
  *     q = softmax(v / tau) over the list,   p_tau = softmax(z / tau) over the vocabulary
  *     kl_t = sum_j q_j log(q_j / p_tau[k_j]),   ce_t = -log p_1[y_t]
@@ -534,6 +534,8 @@ typedef struct {
   int64_t T, D, V, K;    /* tokens, hidden width, vocabulary, pairs of a list (<= 256)           */
   int64_t ldw;           /* columns of W as stored, as in bpt_xent_config                       */
   int64_t block_rows;    /* tokens whose logits are live at once; 0 = automatic (16384)         */
+  int64_t keep_bytes;    /* logits (fp32, whole blocks of tokens) that the forward keeps in `saved` for the backward, which forms
+                          * those of the other tokens again; 0 = automatic (4 GiB), negative = none                 */
   float tau;             /* temperature, > 0                                                    */
   float soft, hard;      /* >= 0; hard = 0: no targets                                          */
   int32_t dtype;         /* bpt_dtype of h, W and dh                                            */
@@ -544,7 +546,8 @@ typedef struct {
 bpt_status bpt_distill_validate(const bpt_distill_config* cfg);
 
 /* What the forward keeps for the backward (lists sorted by index, their probabilities and logits, row statistics: 12 bytes a
- * pair and 36 a token); workspace of bpt_distill_fwd (backward = 0) or bpt_distill_bwd (1). 0 for an invalid configuration. Host-only. */
+ * pair and 28 a token; and what keep_bytes allows of 4 ldw bytes a token); workspace of
+ * bpt_distill_fwd (backward = 0) or bpt_distill_bwd (1). 0 for an invalid configuration. Host-only. */
 size_t bpt_distill_saved_bytes(const bpt_distill_config* cfg);
 size_t bpt_distill_workspace_bytes(const bpt_distill_config* cfg, int backward);
 

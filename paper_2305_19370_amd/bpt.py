@@ -107,8 +107,8 @@ class RecurMixer(ctypes.Structure):
 
 
 class DistillConfig(ctypes.Structure):
-    _fields_ = [("T", c_i64), ("D", c_i64), ("V", c_i64), ("K", c_i64), ("ldw", c_i64), ("block_rows", c_i64), ("tau", c_f32),
-                ("soft", c_f32), ("hard", c_f32), ("dtype", c_i32), ("grad_dtype", c_i32), ("reserved", c_i32)]
+    _fields_ = [("T", c_i64), ("D", c_i64), ("V", c_i64), ("K", c_i64), ("ldw", c_i64), ("block_rows", c_i64), ("keep_bytes", c_i64),
+                ("tau", c_f32), ("soft", c_f32), ("hard", c_f32), ("dtype", c_i32), ("grad_dtype", c_i32), ("reserved", c_i32)]
 
 
 class AdamWTensor(ctypes.Structure):
@@ -1161,9 +1161,9 @@ class RecurrentLayer(Layer):
 
 # ---------------------------------------------------------------- distillation from a teacher's largest logits
 def make_distill_config(T: int, D: int, V: int, K: int, ldw: Optional[int] = None, block_rows: int = 0, tau: float = 1.0,
-                        soft: float = 1.0, hard: float = 0.0, dtype: str = "bf16", grad_dtype: str = "f32") -> DistillConfig:
+                        soft: float = 1.0, hard: float = 0.0, dtype: str = "bf16", grad_dtype: str = "f32", keep_bytes: int = 0) -> DistillConfig:
     """T tokens of width D, V logits, lists of K; see include/libbpt.h."""
-    return DistillConfig(T, D, V, K, ldw if ldw is not None else (V + 63) // 64 * 64, block_rows, tau, soft, hard, _DT[dtype],
+    return DistillConfig(T, D, V, K, ldw if ldw is not None else (V + 63) // 64 * 64, block_rows, keep_bytes, tau, soft, hard, _DT[dtype],
                          _DT[grad_dtype], 0)
 
 

@@ -8,6 +8,7 @@
 // columns), and its transposed repetition in the backward writes the gradient of a token without a list; the listed elements
 // are overwritten afterwards from the picked logits, so that p - q is rounded once.
 #include <algorithm>
+#include <type_traits>
 
 #include "common.h"
 #include "internal.h"
@@ -294,6 +295,71 @@ __global__ __launch_bounds__(1024) void distill_loss_kernel(DistillArgs a, float
   }
 }
 
+// The gradient of a token without a list from the logits that the forward kept, transposed as the products read it: tiles of 64 logits by
+// 256 bytes of tokens. A thread takes four logits of four tokens; in LDS a row of the tile holds pieces of four tokens, its piece c
+// at c ^ f(row / 4), so that both the writes of a wave (16 rows, four pieces) and its reads (whole rows) use every bank.
+// A workgroup does `steps` tiles of the same tokens, whose factors it loads once.
+template <typename T>
+__global__ __launch_bounds__(256) void distill_grad_kernel(DistillArgs a, float dloss, const float* z, T* G, int64_t ld, int tiles, int steps) {
+  constexpr int kTok = 256 / sizeof(T), kGroups = kTok / 64;
+  typedef typename std::conditional<sizeof(T) == 4, u32x4, u32x2>::type Piece;   // four tokens
+  __shared__ __attribute__((aligned(16))) char tile[64 * 256];
+  const int q = threadIdx.x & 15, tg = threadIdx.x >> 4;   // logits 4 q .. 4 q + 3, tokens 4 tg .. of each 64
+  const int part = (tiles + steps - 1) / steps;
+  const int64_t n0 = (int64_t)(blockIdx.x / part) * kTok, rows = a.T - a.t0, ldz = a.ng * 64;
+  const int first = (int)(blockIdx.x % part) * steps, last = first + steps < tiles ? first + steps : tiles;
+  float l2[kGroups][4], g[kGroups][4], l21[kGroups][4], g1[kGroups][4];
+#pragma unroll
+  for (int k = 0; k < kGroups; ++k)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int64_t n = n0 + 64 * k + 4 * tg + e, t = a.t0 + (n < rows ? n : rows - 1);
+      l2[k][e] = a.lt[t] * kLog2e;
+      g[k][e] = a.gs[t];
+      g1[k][e] = a.gh[t];
+      l21[k][e] = a.two ? a.l1[t] * kLog2e : 0.0f;
+      if (!a.two) g[k][e] += g1[k][e], g1[k][e] = 0.0f;
+      if (n >= rows) g[k][e] = g1[k][e] = 0.0f;
+      g[k][e] *= dloss;
+      g1[k][e] *= dloss;
+    }
+  for (int i = first; i < last; ++i) {
+    const int64_t v0 = (int64_t)i * 64;
+    f32x4 v[kGroups][4];
+#pragma unroll
+    for (int k = 0; k < kGroups; ++k)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int64_t n = n0 + 64 * k + 4 * tg + e;
+        v[k][e] = *(const f32x4*)(z + (n < rows ? n : rows - 1) * ldz + v0 + 4 * q);
+      }
+    if (i > first) __syncthreads();
+#pragma unroll
+    for (int k = 0; k < kGroups; ++k)
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        __attribute__((aligned(16))) T out[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          float r = g[k][e] * __builtin_amdgcn_exp2f(fmaf(v[k][e][c], a.scale, -l2[k][e]));
+          if (a.two) r = fmaf(g1[k][e], __builtin_amdgcn_exp2f(fmaf(v[k][e][c], kLog2e, -l21[k][e])), r);
+          const bool none = (g[k][e] == 0.0f && g1[k][e] == 0.0f) || v0 + 4 * q + c >= a.V;
+          out[e] = from_f32<T>(none ? 0.0f : r);
+        }
+        const int piece = (16 * k + tg) ^ (kGroups * q);   // pairs of pieces stay together in 16 bits
+        *(Piece*)(tile + (4 * q + c) * 256 + piece * sizeof(Piece)) = *(const Piece*)out;
+      }
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const int row = 16 * k + tg;
+      const int64_t n = n0 + q * (16 / sizeof(T));
+      if (n < (rows + 63) / 64 * 64)
+        *(u32x4*)(G + (v0 + row) * ld + n) = *(const u32x4*)(tile + row * 256 + ((q * 16) ^ (row / 4 * kGroups * (int)sizeof(Piece))));
+    }
+  }
+}
+
 // Workgroups from `first` on: the listed elements of the logits' gradient, transposed [V, ld] with the block's tokens as columns. Those
 // before it: h of the tokens that have a gradient, zeros for the others, so that what those hold does not reach dW.
 template <typename T>
@@ -346,6 +412,14 @@ hipError_t distill_rows(const DistillArgs& a, const float* z, int64_t ld, hipStr
 }
 hipError_t distill_loss(const DistillArgs& a, float* loss, hipStream_t s) {
   hipLaunchKernelGGL(distill_loss_kernel, dim3(1), dim3(1024), 0, s, a, loss);
+  return hipGetLastError();
+}
+hipError_t distill_grad(Dt t, const DistillArgs& a, float dloss, const float* z, void* G, int64_t ld, hipStream_t s) {
+  const int64_t rows = a.T - a.t0, n = t == F32 ? (rows + 63) / 64 : (rows + 127) / 128;
+  const int steps = n * a.ng >= 8192 ? 4 : 1;          // where that many workgroups are left
+  const dim3 grid((unsigned)(n * ((a.ng + steps - 1) / steps)));
+  if (t == F32) hipLaunchKernelGGL((distill_grad_kernel<float>), grid, dim3(256), 0, s, a, dloss, z, (float*)G, ld, (int)a.ng, steps);
+  else hipLaunchKernelGGL((distill_grad_kernel<bf16>), grid, dim3(256), 0, s, a, dloss, z, (bf16*)G, ld, (int)a.ng, steps);
   return hipGetLastError();
 }
 hipError_t distill_listed(Dt t, const DistillArgs& a, float dloss, void* G, int64_t ld, const void* h, void* out, int64_t D,

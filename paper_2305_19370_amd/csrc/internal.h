@@ -83,6 +83,7 @@ struct GemmArgs {
   const uint16_t* seg = nullptr;
   const int32_t* list = nullptr;
   float* list_z = nullptr;
+  float* keep = nullptr;        // EPI_LIST: acc too, [M, N], or null
   int64_t ldseg = 0, ldlist = 0;
   const float *rowg = nullptr, *rowv1 = nullptr, *rowg1 = nullptr;
   float gscale = 1.0f;
@@ -322,6 +323,8 @@ hipError_t distill_prep(const DistillArgs& a, hipStream_t s);
 hipError_t distill_merge(const DistillArgs& a, const float* part, const float* part1, hipStream_t s);   // EPI_LIST's C, C2
 hipError_t distill_rows(const DistillArgs& a, const float* z, int64_t ld, hipStream_t s);
 hipError_t distill_loss(const DistillArgs& a, float* loss, hipStream_t s);
+// G^T [ng * 64, ld] from the block's logits z [rows, ng * 64], zeros behind the last row up to a multiple of 64; listed elements as others
+hipError_t distill_grad(Dt t, const DistillArgs& a, float dloss, const float* z, void* G, int64_t ld, hipStream_t s);
 // the listed elements of G, and unless out is null the block's rows of h there, zeros for those without a gradient
 hipError_t distill_listed(Dt t, const DistillArgs& a, float dloss, void* G, int64_t ld, const void* h, void* out, int64_t D, hipStream_t s);
 

@@ -1976,6 +1976,14 @@ bpt_status bpt_recur_bwd(const bpt_recur_config* cfg, const void* x, const void*
 constexpr int64_t kDistillRows = 16384;
 static int64_t distill_rows_of_block(const bpt_distill_config& c) { return std::min(c.block_rows > 0 ? c.block_rows : kDistillRows, c.T); }
 
+// Tokens, whole blocks of them, whose logits the forward keeps in fp32: within keep_bytes, 4 GiB if that is 0. 8192 tokens, D = 2048,
+// V = 50257: XXX
+static int64_t distill_kept(const bpt_distill_config& c) {
+  const int64_t limit = c.keep_bytes < 0 ? 0 : c.keep_bytes == 0 ? (int64_t)4 << 30 : std::min(c.keep_bytes, (int64_t)1 << 38);
+  const int64_t n = limit / (c.ldw * 4), R = distill_rows_of_block(c);
+  return n >= c.T ? c.T : n / R * R;
+}
+
 static bpt_status distill_check(const bpt_distill_config* c) {
   if (!c) return fail(BPT_ERR_INVALID_ARG, "config is NULL");
   bpt_xent_config x = {c->T, c->D, c->V, c->ldw, c->block_rows, c->dtype, c->reserved};
@@ -2005,7 +2013,7 @@ static XentDims distill_dims(const bpt_distill_config& c) {
   return d;
 }
 
-static DistillArgs distill_args(const bpt_distill_config& c, const void* saved, int64_t* total) {
+static DistillArgs distill_args(const bpt_distill_config& c, const void* saved, int64_t* total, float** keep) {
   DistillArgs a;
   a.K = (int)c.K; a.K1 = (int)(c.K + (c.hard > 0.0f)); a.two = c.hard > 0.0f && c.tau != 1.0f;
   a.tau = c.tau; a.scale = (float)(1.4426950408889634 / (double)c.tau); a.soft = c.soft; a.hard = c.hard;
@@ -2018,6 +2026,7 @@ static DistillArgs distill_args(const bpt_distill_config& c, const void* saved, 
   a.ypos = (int32_t*)bp.take(c.T * 4);
   a.count = (int32_t*)bp.take(c.T * 4);
   for (float** f : {&a.lt, &a.l1, &a.gs, &a.gh, &a.w}) *f = (float*)bp.take(c.T * 4);
+  *keep = distill_kept(c) > 0 ? (float*)bp.take(distill_kept(c) * c.ldw * 4) : nullptr;
   *total = rup(bp.off, kAlign);
   return a;
 }
@@ -2037,14 +2046,14 @@ static DistillWs distill_ws(const bpt_distill_config& c, const XentDims& d, void
     if (d.zdh > 1) w.part = (float*)bp.take(d.zdh * d.R * d.D * 4);
     if (c.grad_dtype == BPT_BF16 && d.T > d.R) w.dw = (float*)bp.take(d.D * d.ldw * 4);
   } else if (d.E == 4) {
-    w.logits = (float*)bp.take(d.R * d.ldw * 4);
+    if (distill_kept(c) < c.T) w.logits = (float*)bp.take(d.R * d.ldw * 4);
   } else {
     const int64_t ng = d.ldw / 64;
     w.logits = (float*)bp.take(d.R * ng * 8);
     w.part1 = (float*)bp.take(d.R * ng * 4);
     w.seg = (uint16_t*)bp.take(d.R * rup(ng, 8) * 2);
   }
-  *total = rup(bp.off, kAlign);
+  *total = std::max<int64_t>(rup(bp.off, kAlign), kAlign);
   return w;
 }
 
@@ -2053,7 +2062,8 @@ bpt_status bpt_distill_validate(const bpt_distill_config* cfg) { return distill_
 size_t bpt_distill_saved_bytes(const bpt_distill_config* cfg) {
   if (distill_check(cfg) != BPT_OK) return 0;
   int64_t total;
-  distill_args(*cfg, nullptr, &total);
+  float* keep;
+  distill_args(*cfg, nullptr, &total, &keep);
   return (size_t)total;
 }
 
@@ -2080,13 +2090,16 @@ bpt_status bpt_distill_fwd(const bpt_distill_config* cfg, const void* h, const v
   const DistillWs w = distill_ws(*cfg, d, ws, 0, &need);
   if ((int64_t)ws_bytes < need)
     return fail(BPT_ERR_WORKSPACE, "workspace %zu bytes < required %lld", ws_bytes, (long long)need);
-  DistillArgs a = distill_args(*cfg, saved, &stotal);
+  float* keep;
+  DistillArgs a = distill_args(*cfg, saved, &stotal, &keep);
+  const int64_t kept = distill_kept(*cfg);
   a.values = values; a.index = index; a.targets = cfg->hard > 0.0f ? targets : nullptr; a.weights = weights; a.tokens = tokens; a.seg = w.seg;
   hipStream_t s = (hipStream_t)stream;
   const Dt E = dt_of(cfg->dtype);
   const int64_t E_ = (int64_t)d.E, ng = a.ng;
   for (int64_t t0 = 0; t0 < d.T; t0 += d.R) {
     const int64_t r = std::min(d.R, d.T - t0);
+    float* z = t0 < kept ? keep + t0 * d.ldw : nullptr;
     a.t0 = t0; a.T = t0 + r;
     RUN("distill.prep", 0, (double)r * (20.0 * a.K1 + 2.0 * ng), distill_prep(a, s));
     GemmArgs g;   // logits of the block: h W, W read as it is stored (B operand K-major)
@@ -2095,13 +2108,14 @@ bpt_status bpt_distill_fwd(const bpt_distill_config* cfg, const void* h, const v
     g.C = w.logits; g.ldc = d.ldw; g.M = r; g.N = d.ldw; g.K = d.D;
     if (E == BF16) {
       g.ldc = ng; g.nvalid = d.V; g.alpha = a.scale; g.two = a.two; g.C2 = w.part1;
-      g.seg = w.seg; g.ldseg = a.ldseg; g.list = a.sidx + t0 * a.K1; g.list_z = a.sz + t0 * a.K1; g.ldlist = a.K1;
-      RUN("distill.logits", gemm_flops(g), ((double)r * d.D + (double)d.ldw * d.D) * E_ + (double)r * ng * 10,
+      g.seg = w.seg; g.ldseg = a.ldseg; g.list = a.sidx + t0 * a.K1; g.list_z = a.sz + t0 * a.K1; g.ldlist = a.K1; g.keep = z;
+      RUN("distill.logits", gemm_flops(g), ((double)r * d.D + (double)d.ldw * d.D) * E_ + (double)r * ng * (z ? 266 : 10),
           gemm(E, EPI_LIST, F32, F32, g, s));
       RUN("distill.rows", 0, (double)r * ng * 8, distill_merge(a, w.logits, w.part1, s));
     } else {
+      if (z) g.C = z;
       RUN("distill.logits", gemm_flops(g), gemm_bytes(g, E_, 4), gemm(E, EPI_STORE, F32, F32, g, s));
-      RUN("distill.rows", 0, (double)r * d.ldw * 8, distill_rows(a, w.logits, d.ldw, s));
+      RUN("distill.rows", 0, (double)r * d.ldw * 8, distill_rows(a, z ? z : w.logits, d.ldw, s));
     }
   }
   RUN("distill.loss", 0, (double)d.T * 12, distill_loss(a, loss, s));
@@ -2123,7 +2137,9 @@ bpt_status bpt_distill_bwd(const bpt_distill_config* cfg, const void* h, const v
   const DistillWs w = distill_ws(*cfg, d, ws, 1, &need);
   if ((int64_t)ws_bytes < need)
     return fail(BPT_ERR_WORKSPACE, "workspace %zu bytes < required %lld", ws_bytes, (long long)need);
-  DistillArgs a = distill_args(*cfg, saved, &stotal);
+  float* keep;
+  DistillArgs a = distill_args(*cfg, saved, &stotal, &keep);
+  const int64_t kept = distill_kept(*cfg);
   hipStream_t s = (hipStream_t)stream;
   const Dt E = dt_of(cfg->dtype), GT = dt_of(cfg->grad_dtype);
   const int64_t E_ = (int64_t)d.E;
@@ -2131,16 +2147,19 @@ bpt_status bpt_distill_bwd(const bpt_distill_config* cfg, const void* h, const v
     const int64_t r = std::min(d.R, d.T - t0), rp = rup(r, 64);
     const char* hb = (const char*)h + t0 * d.D * E_;
     a.t0 = t0; a.T = t0 + r;
-    {   // G^T [ldw, rp] of the block's logits, recomputed transposed as in bpt_xent_bwd, then its listed elements
+    // G^T [ldw, rp] from the kept logits, or from their product formed again, transposed as in bpt_xent_bwd; then its listed elements
+    if (t0 < kept) {
+      RUN("distill.grad_logits", 0, (double)d.ldw * (4.0 * r + E_ * rp), distill_grad(E, a, dloss, keep + t0 * d.ldw, w.g, d.Rp, s));
+    } else {
       GemmArgs g;
       g.A = W; g.lda = d.ldw; g.trans_a = 1; g.B = hb; g.ldb = d.D;
       g.C = w.g; g.ldc = d.Rp; g.M = d.ldw; g.N = r; g.Nstore = rp; g.K = d.D;
       g.in_order = E == BF16; g.alpha = a.scale; g.gscale = dloss; g.two = a.two; g.nvalid = d.V;
       g.rowv = a.lt + t0; g.rowg = a.gs + t0; g.rowv1 = a.l1 + t0; g.rowg1 = a.gh + t0;
       RUN("distill.grad_logits", gemm_flops(g), gemm_bytes(g, E_, E_), gemm(E, EPI_LIST_T, E, F32, g, s));
-      RUN("distill.listed", 0, (double)r * a.K1 * 16 + (dW ? 2.0 * r * d.D * E_ : 0.0),
-          distill_listed(E, a, dloss, w.g, d.Rp, hb, dW ? w.hz : nullptr, d.D, s));
     }
+    RUN("distill.listed", 0, (double)r * a.K1 * 16 + (dW ? 2.0 * r * d.D * E_ : 0.0),
+        distill_listed(E, a, dloss, w.g, d.Rp, hb, dW ? w.hz : nullptr, d.D, s));
     {   // dh = G W^T
       GemmArgs g;
       g.A = w.g; g.lda = d.Rp; g.trans_a = 1; g.a_cols = d.Rp; g.B = W; g.ldb = d.ldw;

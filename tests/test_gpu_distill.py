@@ -67,6 +67,13 @@ CASES = [
     (520, 64, 300, 20, 3.0, 1.0, 0.4, True, True, dict(block_rows=256)),
     (64, 64, 200, 200, 1.0, 0.0, 1.0, False, False, {}),      # hard targets alone
     (600, 192, 3001, 16, 2.0, 1.0, 0.2, True, True, dict(ldw=3200)),
+    # logits formed again in the backward; kept for the first block, the first two of them alone
+    (1, 64, 65, 3, 2.0, 1.0, 1.0, False, False, dict(keep_bytes=-1)),
+    (130, 192, 513, 64, 4.0, 1.0, 0.0, True, True, dict(keep_bytes=-1)),
+    (300, 256, 777, 256, 2.0, 0.9, 0.1, True, True, dict(keep_bytes=-1)),
+    (257, 128, 640, 33, 1.5, 1.0, 0.4, False, True, dict(block_rows=100, keep_bytes=100 * 640 * 4)),
+    (257, 128, 640, 33, 1.0, 1.0, 0.4, False, True, dict(block_rows=100, keep_bytes=256 * 640 * 4)),
+    (1100, 64, 9000, 20, 2.0, 1.0, 0.4, True, True, {}),      # four tiles of a workgroup of the kept logits
 ]
 
 
@@ -82,10 +89,11 @@ def test_loss_and_gradients(case, dtype, grad):
     compare(t, cfg, run(t, cfg))
 
 
+@pytest.mark.parametrize("keep", [0, -1])
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
-def test_upstream_gradient_and_no_dw(dtype):
+def test_upstream_gradient_and_no_dw(dtype, keep):
     t = inputs(90, 64, 333, 12, dtype, 1)
-    cfg = config(t, 333, tau=2.0, soft=0.6, hard=0.4)
+    cfg = config(t, 333, tau=2.0, soft=0.6, hard=0.4, keep_bytes=keep)
     out = run(t, cfg, -2.5)
     compare(t, cfg, out, -2.5)
     d = bpt.DistillLoss(cfg)
@@ -121,8 +129,9 @@ def test_the_order_of_a_list_changes_only_roundings(dtype):
                                                              half=HALF[t["h"].dtype])["dh_err"], "dh")
 
 
+@pytest.mark.parametrize("keep", [0, -1])
 @pytest.mark.parametrize("dtype,grad", [("bf16", "bf16"), ("f32", "f32")])
-def test_tokens_that_are_left_out(dtype, grad):
+def test_tokens_that_are_left_out(dtype, grad, keep):
     """No weight, or neither list nor target: nothing of them reaches losses or gradients, NaN and infinity in h, in the values or in an
     index of the padding included."""
     T, V, K = 150, 400, 10
@@ -132,7 +141,7 @@ def test_tokens_that_are_left_out(dtype, grad):
     out[::3] = True
     t["weights"][::6] = 0.0
     t["index"][3::6], t["targets"][3::6] = -1, -100
-    cfg = config(t, V, tau=2.0, soft=0.5, hard=0.5, grad_dtype=grad)
+    cfg = config(t, V, tau=2.0, soft=0.5, hard=0.5, grad_dtype=grad, keep_bytes=keep)
     ref = run(t, cfg)
     compare(t, cfg, ref)
     t["h"][::6], t["h"][3::6] = math.nan, math.inf
@@ -151,13 +160,14 @@ def test_all_tokens_left_out():
     assert all(bool((v == 0).all()) for v in out.values())
 
 
-def test_large_logits():
+@pytest.mark.parametrize("keep", [0, -1])
+def test_large_logits(keep):
     """Logits of some hundreds: exponentials far below the smallest number, sums against the running maximum."""
     for dtype in ("bf16", "f32"):
         t = inputs(50, 64, 700, 6, dtype, 6)
         t["h"] = (t["h"].float() * 100).to(DT[dtype])
         t["values"] *= 100
-        cfg = config(t, 700, tau=0.5, soft=1.0, hard=1.0)
+        cfg = config(t, 700, tau=0.5, soft=1.0, hard=1.0, keep_bytes=keep)
         compare(t, cfg, run(t, cfg))
 
 
@@ -185,10 +195,11 @@ def test_hard_targets_are_the_cross_entropy():
         check(a.cpu(), v.cpu().double(), 2 * err, k)
 
 
-def test_replays_from_a_graph():
+@pytest.mark.parametrize("keep", [0, 200 * 1024 * 4, -1])
+def test_replays_from_a_graph(keep):
     T, D, V, K = 500, 64, 1000, 20
     t = inputs(T, D, V, K, "bf16", 9, weights=True, ragged=True)
-    cfg = config(t, V, tau=2.0, soft=0.5, hard=0.5, block_rows=200, grad_dtype="bf16")
+    cfg = config(t, V, tau=2.0, soft=0.5, hard=0.5, block_rows=200, grad_dtype="bf16", keep_bytes=keep)
     ref = run(t, cfg)
     o = dict(loss=torch.empty(3, device="cuda"), tokens=torch.empty(2, T, device="cuda"), dh=torch.empty_like(t["h"]),
              dW=torch.empty_like(t["W"]))
@@ -204,7 +215,7 @@ def test_replays_from_a_graph():
     with torch.cuda.graph(graph):
         step()
     for _ in range(4):
-        for v in list(o.values()) + [saved, ws]:
+        for v in list(o.values()) + [saved, ws]:     # nothing of an earlier call is read
             v.fill_(55)
         graph.replay()
         torch.cuda.synchronize()

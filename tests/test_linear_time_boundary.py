@@ -259,6 +259,22 @@ def test_distillation_refuses(kw, code):
 
 
 @needs_lib
+def test_distillation_keeps_whole_blocks():
+    """Logits within keep_bytes, 4 GiB by itself; those that a block would exceed are not kept."""
+    row = 4 * 1024
+    size = lambda **kw: bpt.distill_saved_bytes(dcfg(**kw))  # noqa: E731
+    none = size(keep_bytes=-1)
+    up = lambda n: (n + 255) // 256 * 256  # noqa: E731
+    assert size() - none == up(100 * row)
+    for keep, tokens in ((1, 0), (100 * row - 1, 0), (100 * row, 100), (1 << 62, 100), (-1 << 63, 0)):
+        assert size(keep_bytes=keep) - none == up(tokens * row), keep
+    for keep, tokens in ((33 * row - 1, 0), (33 * row, 33), (70 * row, 66), (99 * row, 99), (100 * row, 100)):
+        assert size(keep_bytes=keep, block_rows=33) - none == up(tokens * row), keep
+    big = dict(T=1 << 20, block_rows=1 << 10)
+    assert size(**big) - size(keep_bytes=-1, **big) == 4 << 30
+
+
+@needs_lib
 def test_distillation_refuses_pointers():
     c, lib = dcfg(), bpt.load()
     n = bpt.distill_workspace_bytes(c, False)
@@ -284,7 +300,7 @@ def test_distillation_binding_refuses():
     c = dcfg(grad_dtype=1)
     T, D, K, L = c.T, c.D, c.K, c.ldw
     z = lambda *n, dt=torch.float32: torch.zeros(*n, dtype=dt)  # noqa: E731
-    raw = torch.empty(bpt.distill_workspace_bytes(c, False) + bpt.distill_workspace_bytes(c, True), dtype=torch.uint8)
+    raw = torch.empty(bpt.distill_workspace_bytes(c, False) + bpt.distill_workspace_bytes(c, True) + bpt.distill_saved_bytes(c), dtype=torch.uint8)
     ok = dict(h=z(T, D, dt=BF), W=z(D, L, dt=BF), values=z(T, K), index=z(T, K, dt=torch.int32), loss=z(3), tokens=z(2, T), saved=raw, workspace=raw,
               targets=z(T, dt=torch.int32), weights=z(T))
     with pytest.raises(ValueError, match="on the GPU"):
