@@ -5,8 +5,9 @@
 //   d loss / d z = w (soft tau (p_tau - q) + hard (p_1 - onehot(y)))
 // The list (and the target, an entry of q = 0) is sorted by index first. The product that forms the logits then reduces them to
 // maximum and sums of 64 columns in its epilogue and picks the listed ones out (a table says which entries fall into which 64
-// columns), and its transposed repetition in the backward writes the gradient of a token without a list; the listed elements
-// are overwritten afterwards from the picked logits, so that p - q is rounded once.
+// columns). The backward writes the gradient of a token without a list from the logits that the forward kept, or else in the epilogue
+// of their product formed again, transposed; the listed elements are overwritten afterwards from the picked logits, so that p - q is
+// rounded once.
 #include <algorithm>
 #include <type_traits>
 
@@ -299,6 +300,7 @@ __global__ __launch_bounds__(1024) void distill_loss_kernel(DistillArgs a, float
 // 256 bytes of tokens. A thread takes four logits of four tokens; in LDS a row of the tile holds pieces of four tokens, its piece c
 // at c ^ f(row / 4), so that both the writes of a wave (16 rows, four pieces) and its reads (whole rows) use every bank.
 // A workgroup does `steps` tiles of the same tokens, whose factors it loads once.
+// Bound by memory: 8192 tokens, 50304 columns 531 us, 4.65 TB/s (the product formed again 1540).
 template <typename T>
 __global__ __launch_bounds__(256) void distill_grad_kernel(DistillArgs a, float dloss, const float* z, T* G, int64_t ld, int tiles, int steps) {
   constexpr int kTok = 256 / sizeof(T), kGroups = kTok / 64;

