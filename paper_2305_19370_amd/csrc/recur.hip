@@ -82,6 +82,8 @@ BPT_DEV float one_minus_a2(float a, float l2) {
 
 // Keeps the compiler from forming values later, where they are used: it would hold what they are formed from, in more registers
 BPT_DEV void formed(float& x, float& y, float& z) { asm volatile("" : "+v"(x), "+v"(y), "+v"(z)); }
+// A load is over: what it read may be overwritten (hT may be h0, dh0 may be dhT)
+BPT_DEV void loaded(float& x) { asm volatile("" : "+v"(x) : : "memory"); }
 
 // value of the thread `o` lanes before this one
 BPT_DEV float up(float v, int o) { return __shfl_up(v, (unsigned)o, 64); }
@@ -243,6 +245,7 @@ __global__ __launch_bounds__(64 * kFwdWaves, 4) void recur_fwd_kernel(RecurArgs 
     store4(&sa[wave][4 * cl], A);
     store4(&sb[wave][4 * cl], B);
   }
+  loaded(state);
   __syncthreads();
   if constexpr (CHAIN) {
     Word *runs = p.runs + (int64_t)bc * p.nchunks * 128, *groups = p.groups + (int64_t)bc * p.ngroups * 64;
@@ -367,6 +370,8 @@ __global__ __launch_bounds__(64 * kBwdWaves, sizeof(T) == 4 ? 2 : 3) void recur_
 #pragma unroll
   for (int e = 0; e < 4; ++e) k2[e] = CHAIN ? p.k2[chr + e] : decay2(p.lam[chr + e], p.c);
 
+  float back = p.dhT ? p.dhT[row] : 0.0f;              // e of the step behind the chunk
+
   const int64_t first = chunk * L;
   const Rows<T> x(p.x, p.x_sb, p.x_st, b, first, chr), gr(p.r, p.r_sb, p.r_st, b, first, chr), gi(p.i, p.i_sb, p.i_st, b, first, chr),
       dy(p.dy, p.y_sb, p.y_st, b, first, chr);
@@ -441,9 +446,10 @@ __global__ __launch_bounds__(64 * kBwdWaves, sizeof(T) == 4 ? 2 : 3) void recur_
   sa[wave][lane] = Aw;
   sb[wave][lane] = Bw;
   se[wave][lane] = Ew;
+  loaded(back);
   __syncthreads();
   float state = chunk > 0 ? p.saved[((int64_t)b * kept + chunk - 1) * p.D + cwr] : p.h0 ? p.h0[row] : 0.0f;
-  float back = p.dhT ? p.dhT[row] : 0.0f, At = 1.0f, Et = 0.0f;   // e of the step behind the chunk
+  float At = 1.0f, Et = 0.0f;
   if constexpr (CHAIN) {
     Word *runs = p.runs + (int64_t)bc * p.nchunks * 128, *groups = p.groups + (int64_t)bc * p.ngroups * 64;
     const int at = (int)(p.nchunks - 1 - chunk), last = (int)p.nchunks - 1;

@@ -135,8 +135,10 @@ def test_state_in_place():
     check(h.cpu(), ref["hT"], ref["hT_err"] * 1.01, "hT")
 
 
-def test_gradient_of_the_state_in_place():
-    t = inputs(2, 150, 64, "f32", 4)
+@pytest.mark.parametrize("S", [1, 20, 50, 64, 150, 3000])
+def test_gradient_of_the_state_in_place(S):
+    """dh0 is dhT: every wave and every chunk has read it before the first chunk's result is written."""
+    t = inputs(2, S, 64, "f32", 4)
     rec = bpt.GatedRecurrence()
     _, _, saved = rec.forward(t["x"], t["r"], t["i"], t["lam"], t["h0"], save=True)
     ref = rec.backward(t["x"], t["r"], t["i"], t["lam"], saved, t["dy"], t["dhT"], t["h0"])
