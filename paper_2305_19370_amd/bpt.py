@@ -1098,34 +1098,37 @@ def layer_recurrent_workspace_bytes(cfg: Config, backward: bool) -> int:
     return load().bpt_layer_recurrent_workspace_bytes(ctypes.byref(cfg), int(backward))
 
 
-def _check_layer(cfg: Config, saved: torch.Tensor, **tensors: torch.Tensor) -> None:
-    """Raises unless X, Y, dX (and dY) hold the tokens of a configuration, contiguous, and saved a recurrent layer's bytes."""
+def _check_layer(cfg: Config, saved: torch.Tensor, others, **tensors: torch.Tensor) -> int:
+    """Raises unless X, Y, dX (and dY) hold the tokens of a configuration, contiguous, and saved a recurrent layer's bytes. Their
+    stream: others are on their device too."""
     for name, t in tensors.items():
         dt = _TORCH_DT.get(cfg.dtype if name in ("X", "dY") else cfg.out_dtype)
         if t.dtype != dt or t.numel() != cfg.B * cfg.S * cfg.D or not t.is_contiguous():
             raise ValueError(f"{name} must be {cfg.B} x {cfg.S} x {cfg.D} contiguous {dt}, not {tuple(t.shape)} of {t.dtype}")
     _saved_ptr(saved, layer_recurrent_saved_bytes(cfg))
+    dev = tensors["X"].get_device()
+    return _stream_on(dev, all(t is None or t.get_device() == dev for t in (saved, *others, *tensors.values())))
 
 
 def layer_fwd_recurrent(cfg: Config, mixer: RecurMixer, X: torch.Tensor, params: Dict[str, Optional[torch.Tensor]], Y: torch.Tensor,
                         saved: torch.Tensor, workspace: torch.Tensor) -> None:
-    _check_layer(cfg, saved, X=X, Y=Y)
+    stream = _check_layer(cfg, saved, (workspace, *params.values()), X=X, Y=Y)
     p = params_struct(params)
     _check(load().bpt_layer_fwd_recurrent(ctypes.byref(cfg), ctypes.byref(mixer), X.data_ptr(), ctypes.byref(p), Y.data_ptr(),
-                                          saved.data_ptr(), workspace.data_ptr(), _nbytes(workspace), _stream()))
+                                          saved.data_ptr(), workspace.data_ptr(), _nbytes(workspace), stream))
 
 
 def layer_bwd_recurrent(cfg: Config, mixer: RecurMixer, X: torch.Tensor, params: Dict[str, Optional[torch.Tensor]], saved: torch.Tensor,
                         dY: torch.Tensor, dX: torch.Tensor, grads: Dict[str, Optional[torch.Tensor]], workspace: torch.Tensor,
                         dlam: Optional[torch.Tensor] = None, dhT: Optional[torch.Tensor] = None,
                         dh0: Optional[torch.Tensor] = None) -> None:
-    _check_layer(cfg, saved, X=X, dY=dY, dX=dX)
+    stream = _check_layer(cfg, saved, (workspace, dlam, dhT, dh0, *params.values(), *grads.values()), X=X, dY=dY, dX=dX)
     p = params_struct(params)
     g = Grads(*[_ptr(grads.get(n)) for n in GRAD_FIELDS])
     _check(load().bpt_layer_bwd_recurrent(ctypes.byref(cfg), ctypes.byref(mixer), X.data_ptr(), ctypes.byref(p), saved.data_ptr(),
                                           dY.data_ptr(), _f32(dhT, (cfg.B, cfg.D), "dhT"), dX.data_ptr(), ctypes.byref(g),
                                           _f32(dlam, (cfg.D,), "dlam"), _f32(dh0, (cfg.B, cfg.D), "dh0"), workspace.data_ptr(),
-                                          _nbytes(workspace), _stream()))
+                                          _nbytes(workspace), stream))
 
 
 class RecurrentLayer(Layer):

@@ -1918,7 +1918,11 @@ bpt_status bpt_recur_fwd(const bpt_recur_config* cfg, const void* x, const void*
   bpt_status st = recur_check(cfg);
   if (st != BPT_OK) return st;
   if (!x || !r || !i || !lambda || !y) return fail(BPT_ERR_INVALID_ARG, "NULL x, r, i, lambda or y");
-  if (y == x || y == r || y == i) return fail(BPT_ERR_INVALID_ARG, "y must not alias x, r or i");
+  for (const void* q : {x, r, i, (const void*)lambda, (const void*)lens}) {
+    if (y == q) return fail(BPT_ERR_INVALID_ARG, "y must not alias an input");
+    if (hT && hT == q) return fail(BPT_ERR_INVALID_ARG, "hT must not alias an input but h0");
+  }
+  if (y == h0 || y == hT || (saved && (saved == y || saved == hT))) return fail(BPT_ERR_INVALID_ARG, "y, the states and saved must not alias one another");
   for (const void* q : {x, r, i, (const void*)lambda, (const void*)lens, (const void*)h0, (const void*)y, (const void*)hT,
                         (const void*)saved, (const void*)ws})
     if (q && !aligned16(q)) return fail(BPT_ERR_INVALID_ARG, "pointer %p is not 16-byte aligned", q);
@@ -1991,7 +1995,9 @@ static bpt_status distill_check(const bpt_distill_config* c) {
   bpt_status st = xent_check(&x);
   if (st != BPT_OK) return st;
   if (c->K < 1) return fail(BPT_ERR_INVALID_ARG, "K must be >= 1");
-  if (!(c->tau > 0.0f) || !std::isfinite(c->tau) || !std::isfinite(1.0f / c->tau)) return fail(BPT_ERR_INVALID_ARG, "tau must be > 0");
+  if (!(c->tau > 0.0f) || !std::isfinite(c->tau)) return fail(BPT_ERR_INVALID_ARG, "tau must be > 0");
+  // tau^2 and log2(e) / tau are formed in fp32
+  if (c->tau < 1e-18f || c->tau > 1e18f) return fail(BPT_ERR_INVALID_ARG, "tau must be between 1e-18 and 1e18");
   if (!(c->soft >= 0.0f) || !(c->hard >= 0.0f) || !std::isfinite(c->soft) || !std::isfinite(c->hard))
     return fail(BPT_ERR_INVALID_ARG, "soft and hard must be >= 0");
   if ((st = dtype_ok(c->grad_dtype, "grad_dtype")) != BPT_OK) return st;

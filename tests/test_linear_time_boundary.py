@@ -108,8 +108,11 @@ def test_recurrence_refuses_pointers():
         assert call(**{k: None}) == 1, k
     for k in ("x", "r", "i", "lam", "lens", "h0", "y", "hT", "saved", "ws"):
         assert call(**{k: good[k] + 8}) == 1, k
-    for k in ("x", "r", "i"):
+    for k in ("x", "r", "i", "lam", "lens", "h0"):
         assert call(y=good[k]) == 1, k
+    for k in ("x", "r", "i", "lam", "lens", "y"):
+        assert call(hT=good[k]) == 1, k
+    assert call(saved=good["y"]) == 1 and call(saved=good["hT"]) == 1
     assert call(n=n - 1) == 3 and call(ws=None) == 3
     n = bpt.recur_workspace_bytes(c, True)
     good = dict(x=A, r=2 * A, i=3 * A, lam=4 * A, lens=5 * A, h0=6 * A, saved=9 * A, dy=7 * A, dhT=8 * A, dx=11 * A, dr=12 * A, di=13 * A,
@@ -221,6 +224,16 @@ def test_recurrent_gpt_refuses():
     assert m.shape.n_params() == sum(m.master(n).numel() for n in m.names()) - 64 * (m.shape.ldw - 10)
 
 
+@needs_lib
+def test_recurrent_layer_binding_refuses_the_place():
+    cfg = bpt.make_config(1, 64, 64, 1, 64, 64, 64, True, "bf16")
+    X, raw, p = torch.zeros(1, 64, 64, dtype=BF), torch.zeros(1 << 21, dtype=torch.uint8), dict.fromkeys(bpt.PARAM_FIELDS)
+    with pytest.raises(ValueError, match="on the GPU"):
+        bpt.layer_fwd_recurrent(cfg, bpt.RecurMixer(8.0, A, None, None), X, p, X.clone(), raw, raw)
+    with pytest.raises(ValueError, match="on the GPU"):
+        bpt.layer_bwd_recurrent(cfg, bpt.RecurMixer(8.0, A, None, None), X, p, raw, X, X.clone(), {}, raw)
+
+
 # ---------------------------------------------------------------- the distillation loss
 def dcfg(**kw):
     c = bpt.make_distill_config(100, 64, 1000, 20, tau=2.0, soft=0.5, hard=0.5)
@@ -239,7 +252,7 @@ def test_distillation_accepts():
 
 
 DBAD = [(dict(T=0), 1), (dict(D=0), 1), (dict(V=0), 1), (dict(K=0), 1), (dict(K=-1), 1), (dict(ldw=960), 1), (dict(block_rows=-1), 1),
-        (dict(tau=0.0), 1), (dict(tau=-1.0), 1), (dict(tau=math.nan), 1), (dict(tau=math.inf), 1), (dict(tau=1e-40), 1), (dict(soft=-0.1), 1),
+        (dict(tau=0.0), 1), (dict(tau=-1.0), 1), (dict(tau=math.nan), 1), (dict(tau=math.inf), 1), (dict(tau=1e-40), 1), (dict(tau=3e-39), 1), (dict(tau=1e19), 1), (dict(soft=-0.1), 1),
         (dict(hard=-0.1), 1), (dict(soft=math.nan), 1), (dict(hard=math.inf), 1), (dict(dtype=3), 1), (dict(grad_dtype=2), 1), (dict(reserved=1), 1),
         (dict(K=257), 2), (dict(D=65), 2), (dict(ldw=1001), 2), (dict(dtype=0, grad_dtype=1), 2), (dict(T=1 << 31), 2),
         (dict(D=1 << 40), 2), (dict(D=1 << 20, ldw=1 << 20), 2), (dict(V=(1 << 31) - 64, ldw=1 << 31), 2),
