@@ -180,6 +180,35 @@ def test_blocks_give_the_same_losses():
         assert torch.equal(a[k], b[k]), k
 
 
+def test_a_large_vocabulary():
+    """Pieces of a token's table, 1024 groups of 64 logits each."""
+    for dtype in ("bf16", "f32"):
+        t = inputs(5, 64, 140001, 40, dtype, 10, ragged=True)
+        t["index"][:, 1], t["index"][:, 2], t["index"][:, 3] = 65535, 65536, 131072
+        cfg = config(t, 140001, tau=2.0, soft=1.0, hard=0.5)
+        compare(t, cfg, run(t, cfg))
+
+
+@pytest.mark.parametrize("keep", [1 << 34, -1])
+def test_offsets_past_32_bits(keep):
+    """A block of more than 2^31 logits. Some tokens count, those behind that limit among them: what they give hangs on no other."""
+    T, D, V, K = 45056, 64, 50257, 8
+    g = torch.Generator(device="cuda").manual_seed(11)
+    t = dict(h=torch.randn(T, D, generator=g, device="cuda").bfloat16(),
+             W=(torch.randn(D, 50304, generator=g, device="cuda") / 4).bfloat16(), values=torch.randn(T, K, generator=g, device="cuda") * 3,
+             index=torch.randint(0, V, (T, K), generator=g, device="cuda", dtype=torch.int32),
+             targets=torch.randint(0, V, (T,), generator=g, device="cuda", dtype=torch.int32), weights=torch.zeros(T, device="cuda"))
+    some = torch.cat([torch.arange(0, T, 4501), torch.arange(T - 12, T)]).cuda()
+    t["weights"][some] = 1.0 / len(some)
+    cfg = config(t, V, tau=1.5, soft=1.0, hard=0.5, block_rows=T, keep_bytes=keep)
+    out = run(t, cfg)
+    left = torch.ones(T, dtype=torch.bool, device="cuda")
+    left[some] = False
+    assert bool((out["dh"][left] == 0).all()) and bool((out["tokens"][:, left] == 0).all())
+    few = {k: v if k == "W" else v[some].contiguous() for k, v in t.items()}
+    compare(few, cfg, dict(out, dh=out["dh"][some], tokens=out["tokens"][:, some]))
+
+
 def test_hard_targets_are_the_cross_entropy():
     """soft = 0: bpt_xent's loss and gradients."""
     T, D, V = 260, 128, 900

@@ -178,6 +178,31 @@ def test_strides_and_what_lies_beside():
         assert bool((w[:, :, :8] == fill).all()) and bool((w[:, :, 8 + D:] == fill).all())
 
 
+def test_offsets_past_32_bits():
+    """Sequences more than 2^31 elements apart: what dense tensors give."""
+    B, S, D = 2, 300, 72
+    t = inputs(B, S, D, "bf16", 7)
+    ref = run(t)
+    gap = (1 << 31) + 64                             # between the starts of two sequences of one projection
+
+    def far(*values):
+        flat = torch.empty(gap + S * 3 * D, dtype=torch.bfloat16, device="cuda")
+        views = [flat.as_strided((B, S, D), (gap, 3 * D, 1), k * D) for k in range(3)]
+        for view, v in zip(views, values):
+            view.copy_(v)
+        return views
+
+    (x, r, i), (y, dy, _), (dx, dr, di) = far(t["x"], t["r"], t["i"]), far(t["dy"], t["dy"]), far()
+    cfg = bpt.recur_config_of(x, r, i, y)
+    ws = torch.empty(max(bpt.recur_workspace_bytes(cfg, k) for k in (False, True)), dtype=torch.uint8, device="cuda")
+    saved, hT = torch.empty(bpt.recur_saved_bytes(cfg), dtype=torch.uint8, device="cuda"), torch.empty(B, D, device="cuda")
+    bpt.recur_fwd(cfg, x, r, i, t["lam"], y, t["h0"], hT, saved, ws)
+    dlam, dh0 = torch.empty(D, device="cuda"), torch.empty(B, D, device="cuda")
+    bpt.recur_bwd(cfg, x, r, i, t["lam"], saved, dy, dx, dr, di, ws, dlam, t["h0"], t["dhT"], dh0)
+    for k, v in dict(y=y, hT=hT, dx=dx, dr=dr, di=di, dlam=dlam, dh0=dh0).items():
+        assert torch.equal(v, ref[k]), k
+
+
 def test_a_nan_stays_in_its_channel_and_after_its_step():
     t = inputs(2, 300, 64, "f32", 6)
     ref = run(t)
