@@ -731,14 +731,26 @@ __global__ __launch_bounds__(128 * NWN * KG, 1) void gemm_bf16_kernel(GemmArgs a
   // what the list epilogues read beside the accumulators, for all strips at once: the places of the listed logits among the
   // wave's 64 columns, and what a lane's four columns contribute (the same ones in every strip)
   uint32_t seg[EPI == EPI_LIST ? Cfg::TM : 1][EPI == EPI_LIST ? NIT : 1];
+  int32_t ent[EPI == EPI_LIST ? 2 : 1][EPI == EPI_LIST ? NIT : 1];   // a lane's entry of its row, a strip ahead; some column without one
   ListCol col[EPI == EPI_LIST_T ? 4 : 1];
   bool none[4] = {};
+  auto entries = [&](int i) {
+    if constexpr (EPI == EPI_LIST) {
+      const int64_t row0 = m0 + wm * Cfg::WM + lane / C4 + 32 * i;
+#pragma unroll
+      for (int it = 0; it < NIT; ++it) {
+        const int e = std::min((int)(seg[i][it] >> 7) + lane % C4, (int)a.ldlist - 1);
+        ent[i % 2][it] = a.list[std::min(row0 + RSTEP * it, a.M - 1) * a.ldlist + e];
+      }
+    }
+  };
   if constexpr (EPI == EPI_LIST) {
     const int64_t row0 = m0 + wm * Cfg::WM + lane / C4, g = std::min((n0 + wn * Cfg::WN) / 64, (ncols - 1) / 64);
 #pragma unroll
     for (int i = 0; i < Cfg::TM; ++i)
 #pragma unroll
       for (int it = 0; it < NIT; ++it) seg[i][it] = a.seg[std::min(row0 + 32 * i + RSTEP * it, a.M - 1) * a.ldseg + g];
+    entries(0);
   }
   if constexpr (EPI == EPI_LIST_T) {
     if (inside) {
@@ -793,40 +805,78 @@ __global__ __launch_bounds__(128 * NWN * KG, 1) void gemm_bf16_kernel(GemmArgs a
       continue;
     }
     if constexpr (EPI == EPI_LIST) {
-      // as EPI_LSE, with the listed logits of a row instead of one target's
+      // As EPI_LSE, with the listed logits of a row instead of one target's. Four rows of a lane at a time and no branch
+      // between them, so that their exchanges and exponentials overlap.
       static_assert(Cfg::WN == 64, "summaries of 64 columns");
-      const int c0 = 4 * (lane % C4);
-      const bool all = ncol + 64 <= a.nvalid;
+      if (i + 1 < Cfg::TM) entries(i + 1);
+      const int c16 = lane % C4, c0 = 4 * c16;
+      const bool all = ncol + 64 <= a.nvalid, whole = mrow + 32 <= a.M && ncol < ncols;
+      float mx[NIT], sum[NIT], sum1[NIT];
 #pragma unroll
-      for (int it = 0; it < 32 / RSTEP; ++it) {
-        const int row = lane / C4 + RSTEP * it;
-        const int64_t m = mrow + row;
-        const bool in = m < a.M && ncol < ncols;
-        const f32x4 v = *(const f32x4*)(strip + row * PITCHF + c0);
-        // read once, by a later kernel: past the caches, where they would take the operands' place (1003 tokens, D 2048: 293 us, else 317)
-        if (in && a.keep) __builtin_nontemporal_store(v, (f32x4*)(a.keep + m * a.N + ncol + c0));
-        float mx = -__builtin_inff(), sum = 0.0f, sum1 = 0.0f;
+      for (int h = 0; h < NIT; h += 4) {
+        f32x4 v[4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) mx = all || ncol + c0 + e < a.nvalid ? fmaxf(mx, v[e]) : mx;
-        mx = max16(mx);
+        for (int k = 0; k < 4; ++k) v[k] = *(const f32x4*)(strip + (lane / C4 + RSTEP * (h + k)) * PITCHF + c0);
+        if (a.keep) {
+          // read once, by a later kernel: past the caches, where they would take the operands' place (1003 tokens, D 2048: 293 us, else 317)
+          float* to = a.keep + (mrow + lane / C4 + RSTEP * h) * a.N + ncol + c0;
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-          sum += all || ncol + c0 + e < a.nvalid ? __builtin_amdgcn_exp2f((v[e] - mx) * a.alpha) : 0.0f;
-        sum = sum16(sum);
+          for (int k = 0; k < 4; ++k)
+            if (whole || (mrow + lane / C4 + RSTEP * (h + k) < a.M && ncol < ncols)) __builtin_nontemporal_store(v[k], (f32x4*)(to + RSTEP * k * a.N));
+        }
+        if (!all) {
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[k][e] = ncol + c0 + e < a.nvalid ? v[k][e] : -__builtin_inff();
+        }
+        float at[4];                                   // what exponents count from; 0 where no column is valid
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          mx[h + k] = max16(fmaxf(fmaxf(v[k][0], v[k][1]), fmaxf(v[k][2], v[k][3])));
+          at[k] = mx[h + k] == -__builtin_inff() ? 0.0f : mx[h + k];
+        }
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          float t = 0.0f;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) t += __builtin_amdgcn_exp2f((v[k][e] - at[k]) * a.alpha);
+          sum[h + k] = sum16(t);
+        }
         if (a.two) {
 #pragma unroll
-          for (int e = 0; e < 4; ++e)
-            sum1 += all || ncol + c0 + e < a.nvalid ? __builtin_amdgcn_exp2f((v[e] - mx) * 1.4426950408889634f) : 0.0f;
-          sum1 = sum16(sum1);
+          for (int k = 0; k < 4; ++k) {
+            float t = 0.0f;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) t += __builtin_amdgcn_exp2f((v[k][e] - at[k]) * 1.4426950408889634f);
+            sum1[h + k] = sum16(t);
+          }
         }
-        if (in && c0 == 0) {
-          *(u32x2*)((float*)a.C + 2 * (m * a.ldc + ncol / 64)) = u32x2{__float_as_uint(mx), __float_as_uint(sum)};
-          if (a.two) ((float*)a.C2)[m * a.ldc + ncol / 64] = sum1;
-        }
-        const int from = (int)(seg[i][it] >> 7), to = in ? from + (int)(seg[i][it] & 127) : from;
-        for (int e = from; e < to; ++e) {
-          const int64_t k = a.list[m * a.ldlist + e] - ncol - c0;
-          if (k >= 0 && k < 4) a.list_z[m * a.ldlist + e] = k == 0 ? v[0] : k == 1 ? v[1] : k == 2 ? v[2] : v[3];
+      }
+      // lane `it` of the 16 of a row stores it: one store for the strip
+      float om = 0.0f, os = 0.0f, os1 = 0.0f;
+#pragma unroll
+      for (int it = 0; it < NIT; ++it) {
+        om = c16 == it ? mx[it] : om;
+        os = c16 == it ? sum[it] : os;
+        if (a.two) os1 = c16 == it ? sum1[it] : os1;
+      }
+      const int64_t mine = mrow + lane / C4 + RSTEP * c16;
+      if (c16 < NIT && mine < a.M && ncol < ncols) {
+        *(u32x2*)((float*)a.C + 2 * (mine * a.ldc + ncol / 64)) = u32x2{__float_as_uint(om), __float_as_uint(os)};
+        if (a.two) ((float*)a.C2)[mine * a.ldc + ncol / 64] = os1;
+      }
+      // an entry per lane; more than 16 of a row in 64 columns are rare
+#pragma unroll
+      for (int it = 0; it < NIT; ++it) {
+        const int row = lane / C4 + RSTEP * it;
+        const int64_t m = mrow + row;
+        const int from = (int)(seg[i][it] >> 7), many = m < a.M && ncol < ncols ? (int)(seg[i][it] & 127) : 0;
+        if (c16 < many) {
+          float* out = a.list_z + m * a.ldlist + from;
+          const float* z = strip + row * PITCHF - ncol;
+          out[c16] = z[ent[i % 2][it]];
+          for (int e = c16 + 16; e < many; e += 16) out[e] = z[a.list[m * a.ldlist + from + e]];
         }
       }
       continue;
