@@ -819,10 +819,10 @@ __global__ __launch_bounds__(128 * NWN * KG, 1) void gemm_bf16_kernel(GemmArgs a
         for (int k = 0; k < 4; ++k) v[k] = *(const f32x4*)(strip + (lane / C4 + RSTEP * (h + k)) * PITCHF + c0);
         if (a.keep) {
           // read once, by a later kernel: past the caches, where they would take the operands' place (1003 tokens, D 2048: 293 us, else 317)
-          float* to = a.keep + (mrow + lane / C4 + RSTEP * h) * a.N + ncol + c0;
+          float* to = a.keep + (mrow + lane / C4 + RSTEP * h) * a.ldkeep + ncol + c0;
 #pragma unroll
           for (int k = 0; k < 4; ++k)
-            if (whole || (mrow + lane / C4 + RSTEP * (h + k) < a.M && ncol < ncols)) __builtin_nontemporal_store(v[k], (f32x4*)(to + RSTEP * k * a.N));
+            if (whole || (mrow + lane / C4 + RSTEP * (h + k) < a.M && ncol < ncols)) __builtin_nontemporal_store(v[k], (f32x4*)(to + RSTEP * k * a.ldkeep));
         }
         if (!all) {
 #pragma unroll
@@ -874,7 +874,7 @@ __global__ __launch_bounds__(128 * NWN * KG, 1) void gemm_bf16_kernel(GemmArgs a
         const int from = (int)(seg[i][it] >> 7), many = m < a.M && ncol < ncols ? (int)(seg[i][it] & 127) : 0;
         if (c16 < many) {
           float* out = a.list_z + m * a.ldlist + from;
-          const float* z = strip + row * PITCHF - ncol;
+          const float* z = strip + row * PITCHF - (a.col0 + ncol);
           out[c16] = z[ent[i % 2][it]];
           for (int e = c16 + 16; e < many; e += 16) out[e] = z[a.list[m * a.ldlist + from + e]];
         }

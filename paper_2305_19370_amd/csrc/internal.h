@@ -83,7 +83,8 @@ struct GemmArgs {
   const uint16_t* seg = nullptr;
   const int32_t* list = nullptr;
   float* list_z = nullptr;
-  float* keep = nullptr;        // EPI_LIST: acc too, [M, N], or null
+  float* keep = nullptr;        // EPI_LIST: acc too, rows of ldkeep, or null
+  int64_t ldkeep = 0, col0 = 0; // col0: of the whole product, this one's first column
   int64_t ldseg = 0, ldlist = 0;
   const float *rowg = nullptr, *rowv1 = nullptr, *rowg1 = nullptr;
   float gscale = 1.0f;

@@ -74,6 +74,9 @@ CASES = [
     (257, 128, 640, 33, 1.5, 1.0, 0.4, False, True, dict(block_rows=100, keep_bytes=100 * 640 * 4)),
     (257, 128, 640, 33, 1.0, 1.0, 0.4, False, True, dict(block_rows=100, keep_bytes=256 * 640 * 4)),
     (1100, 64, 9000, 20, 2.0, 1.0, 0.4, True, True, {}),      # four tiles of a workgroup of the kept logits
+    # columns of a last round of tiles in a product of their own
+    (300, 64, 33000, 40, 2.0, 1.0, 0.3, True, True, {}),
+    (257, 128, 32900, 9, 1.0, 1.0, 0.0, False, True, dict(keep_bytes=-1)),
 ]
 
 
