@@ -300,7 +300,7 @@ __global__ __launch_bounds__(1024) void distill_loss_kernel(DistillArgs a, float
 // 256 bytes of tokens. A thread takes four logits of four tokens; in LDS a row of the tile holds pieces of four tokens, its piece c
 // at c ^ f(row / 4), so that both the writes of a wave (16 rows, four pieces) and its reads (whole rows) use every bank.
 // A workgroup does `steps` tiles of the same tokens, whose factors it loads once.
-// Bound by memory: 8192 tokens, 50304 columns 531 us, 4.65 TB/s (the product formed again 1540).
+// Bound by memory: 8192 tokens, 50304 columns 503 us, 4.9 TB/s (the product formed again 1540).
 template <typename T>
 __global__ __launch_bounds__(256) void distill_grad_kernel(DistillArgs a, float dloss, const float* z, T* G, int64_t ld, int tiles, int steps) {
   constexpr int kTok = 256 / sizeof(T), kGroups = kTok / 64;

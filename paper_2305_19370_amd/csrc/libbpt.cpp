@@ -1981,8 +1981,8 @@ constexpr int64_t kDistillRows = 16384;
 static int64_t distill_rows_of_block(const bpt_distill_config& c) { return std::min(c.block_rows > 0 ? c.block_rows : kDistillRows, c.T); }
 
 // Tokens, whole blocks of them, whose logits the forward keeps in fp32: within keep_bytes, 4 GiB if that is 0 (1.4 % of the memory).
-// 8192 tokens, D = 2048, V = 50257 (1.5 GiB): forward and backward 1.83 + 3.27 ms, without 1.74 + 4.31; D = 768, 4000 tokens 0.65 +
-// 0.91, without 0.58 + 1.17.
+// 8192 tokens, D = 2048, V = 50257 (1.5 GiB): forward and backward 1.70 + 3.12 ms, without 1.58 + 4.13; D = 768, 4000 tokens 0.47 +
+// 0.90, without 0.43 + 1.14.
 static int64_t distill_kept(const bpt_distill_config& c) {
   const int64_t limit = c.keep_bytes < 0 ? 0 : c.keep_bytes == 0 ? (int64_t)4 << 30 : std::min(c.keep_bytes, (int64_t)1 << 38);
   const int64_t n = limit / (c.ldw * 4), R = distill_rows_of_block(c);
@@ -2015,15 +2015,15 @@ static bpt_status distill_check(const bpt_distill_config* c) {
 
 static XentDims distill_dims(const bpt_distill_config& c) {
   XentDims d = xent_dims({c.T, c.D, c.V, c.ldw, distill_rows_of_block(c), c.dtype, 0});
-  // fp32 too: 38 tokens, D = 2496, V = 14302 the backward takes 188 us, with dh in one slice 248
+  // fp32 too: 38 tokens, D = 2496, V = 14302 the backward takes 60 us less than with dh in one slice (127 us)
   if (d.E == 4) d.zdh = gemm_ksplit(F32, std::min(d.T, kDefaultXentRows), d.D, d.ldw, kMaxKSplit);
   return d;
 }
 
 // A product of bf16 [M, K] by [K, N] (N K-major) in tiles of 256 x 256, of which a CU takes one at a time: where a last round
 // would have few of them (at most 64, which are 256 tiles of 128 x 128), its columns are a product of their own, which takes smaller
-// tiles: 1003 tokens, D = 2048, V = 50257 the forward 245 us, in one product (3.08 rounds) 270; dW of 8192 tokens (6.16) 1.28 ms,
-// 1.37. With 81 tiles left (dW, D = 768: 2.31 rounds) 331, in one 313. The first product's columns.
+// tiles: 1003 tokens, D = 2048, V = 50257 the forward 233 us, in one product (3.08 rounds) 255; the backward of 8192 tokens (dW
+// 6.16 rounds) 3.12 ms, 3.20. With 81 tiles left (dW, D = 768: 2.31 rounds) 331, in one 313. The first product's columns.
 static int64_t whole_rounds(int64_t M, int64_t N) {
   const int64_t tm = (M + 255) / 256, tiles = tm * ((N + 255) / 256), full = tiles / 256 * 256 / tm;
   const int64_t rest = tiles - tm * full;
