@@ -1036,20 +1036,21 @@ class GatedRecurrence:
         if not x.dtype == r.dtype == i.dtype or not x.shape == r.shape == i.shape:
             raise ValueError("x, r and i must share a type and a shape")
         cfg, ns, nb, states = _recur_plan(x.dtype, x.shape, x.stride(), r.stride(), i.stride(), self.c)
-        dev = x.device
-        y, hT = torch.empty(x.shape, dtype=x.dtype, device=dev), torch.empty(states, dtype=torch.float32, device=dev)
-        saved = self._bytes(ns, dev) if save else None
-        ws = self._bytes(nb, dev) if nb else None
         at = x.get_device()
         same = at == r.get_device() == i.get_device() == lam.get_device()
-        hp = lp = None
+        ap, hp, lp = _f32(lam, states[1:], "lam"), None, None
         if h0 is not None:
             hp, same = _f32(h0, states, "h0"), same and h0.get_device() == at
         if lens is not None:
             lp, same = _int32(lens, cfg.B, "lens"), same and lens.get_device() == at
-        _check(load().bpt_recur_fwd(cfg, x.data_ptr(), r.data_ptr(), i.data_ptr(), _f32(lam, states[1:], "lam"), lp, hp, y.data_ptr(),
-                                    hT.data_ptr(), saved.data_ptr() if save and ns else None, ws.data_ptr() if nb else None, nb,
-                                    _stream_on(at, same)))
+        stream = _stream_on(at, same)
+        # a new token is a call of some 8 us: tensors like others are made in half the time
+        y = torch.empty_like(x, memory_format=torch.contiguous_format)
+        hT = lam.new_empty(states) if h0 is None else torch.empty_like(h0)
+        saved = self._bytes(ns, x.device) if save else None
+        ws = self._bytes(nb, x.device) if nb else None
+        _check(load().bpt_recur_fwd(cfg, x.data_ptr(), r.data_ptr(), i.data_ptr(), ap, lp, hp, y.data_ptr(),
+                                    hT.data_ptr(), saved.data_ptr() if save and ns else None, ws.data_ptr() if nb else None, nb, stream))
         return y, hT, saved
 
     def backward(self, x: torch.Tensor, r: torch.Tensor, i: torch.Tensor, lam: torch.Tensor, saved: torch.Tensor, dy: torch.Tensor,
