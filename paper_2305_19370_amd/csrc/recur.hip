@@ -553,19 +553,27 @@ __global__ __launch_bounds__(256) void recur_start_kernel(RecurArgs p, int64_t w
   for (int64_t k = i; k < words / 2; k += step) ((u32x4*)p.runs)[k] = u32x4{0, 0, 0, 0};
 }
 
-// dlambda from the chunks' sums, [rows, D], added in a fixed order: 16 runs of rows, then those
+// dlambda from the chunks' sums, [rows, D], added in a fixed order: a workgroup's 256 runs of rows of 16 channels, 16 of them, then
+// those by exchanges
 __global__ __launch_bounds__(1024) void recur_dlam_kernel(const float* part, int64_t rows, int D, float* dlam) {
-  __shared__ float s[16][64];
-  const int lane = threadIdx.x & 63, g = threadIdx.x >> 6, c = blockIdx.x * 64 + lane;
-  float sum = 0.0f;
-  if (c < D)
-    for (int64_t i = g; i < rows; i += 16) sum += part[i * D + c];
-  s[g][lane] = sum;
-  __syncthreads();
-  if (g == 0 && c < D) {
-    for (int k = 1; k < 16; ++k) sum += s[k][lane];
-    dlam[c] = sum;
+  __shared__ f32x4 s[256][4];
+  const int q = threadIdx.x & 3, g = threadIdx.x >> 2, c = blockIdx.x * 16 + 4 * q;
+  f32x4 sum = {0, 0, 0, 0};
+  if (c < D) {
+#pragma unroll 4
+    for (int64_t i = g; i < rows; i += 256) sum += *(const f32x4*)(part + i * D + c);
   }
+  s[g][q] = sum;
+  __syncthreads();
+  if (threadIdx.x >= 64) return;
+  sum = s[16 * g][q];
+#pragma unroll
+  for (int k = 1; k < 16; ++k) sum += s[16 * g + k][q];
+#pragma unroll
+  for (int o = 4; o < 64; o *= 2)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) sum[e] += __shfl_xor(sum[e], o, 64);
+  if (g == 0 && c < D) *(f32x4*)(dlam + c) = sum;
 }
 
 // ------------------------------------------------------------------ launchers
@@ -659,12 +667,12 @@ hipError_t recur_bwd(Dt t, RecurArgs p, hipStream_t s) {
   return chain ? launch_bwd<bf16, true>(p, nw, s) : launch_bwd<bf16, false>(p, nw, s);
 }
 
-// Few rows in one launch, many by col_sum's two: 1500 rows of 1024 43 us in one
-int64_t recur_dlam_floats(int64_t rows, int64_t D) { return rows > 128 ? std::min<int64_t>(rows / 16, 512) * D : 0; }
+// Up to 2048 rows in one launch, more by col_sum's two: 256 rows of 2048 4.7 us (two launches 9.5 and a gap), 1500 of 1024 7.6 (9.6)
+int64_t recur_dlam_floats(int64_t rows, int64_t D) { return rows > 2048 ? std::min<int64_t>(rows / 16, 512) * D : 0; }
 hipError_t recur_dlam(const RecurArgs& p, float* dlam, float* partial, hipStream_t s) {
   const int64_t rows = p.B * recur_bwd_chunks(p.S), n = recur_dlam_floats(rows, p.D);
   if (n > 0) return col_sum(F32, p.part, p.D, rows, p.D, dlam, partial, n, s);
-  hipLaunchKernelGGL(recur_dlam_kernel, dim3((unsigned)((p.D + 63) / 64)), dim3(1024), 0, s, p.part, rows, p.D, dlam);
+  hipLaunchKernelGGL(recur_dlam_kernel, dim3((unsigned)((p.D + 15) / 16)), dim3(1024), 0, s, p.part, rows, p.D, dlam);
   return hipGetLastError();
 }
 
