@@ -1018,6 +1018,27 @@ def _recur_plan(dtype: torch.dtype, shape: Tuple[int, ...], sx, sr, si, c: float
     return cfg, recur_saved_bytes(cfg), recur_workspace_bytes(cfg, False), (cfg.B, cfg.D)
 
 
+@functools.lru_cache(maxsize=1024)
+def _recur_back_plan(dtype: torch.dtype, shape: Tuple[int, ...], strides, sdy, offsets: Optional[Tuple[int, ...]], c: float):
+    """For x, r and i of these strides (offsets: of parts of one tensor from the first of them, or None) at whole 16 bytes: the configuration of
+    a backward, its bytes of saved and workspace, the shape of the states; elements of the tensor whose parts the gradients
+    are (0: each its own) with their strides and offsets, and which of x, r and i are copied. Formed once: 25 us of a call."""
+    size = max(1 + sum((n - 1) * st for n, st in zip(shape, sts)) for sts in strides) + (max(offsets) if offsets else 0)
+    base = torch.empty(size, dtype=dtype, device="meta")
+    views = [base.as_strided(shape, st, offsets[k] if offsets else 0) for k, st in enumerate(strides)]
+    four = tuple(t.unsqueeze(2) for t in views)
+    parts = _side_by_side(four) if offsets else None
+    if parts is not None:
+        n, copied = parts[0].untyped_storage().nbytes() // parts[0].element_size(), (False,) * 3
+        at = tuple((t.stride(), g.storage_offset()) for t, g in zip(views, parts))
+    else:
+        n, copied = 0, tuple(not (_apart(f) and _span(t) == t.numel()) for t, f in zip(views, four))
+        views, at = [torch.empty(shape, dtype=dtype, device="meta") if no else t for t, no in zip(views, copied)], ()
+    cfg = recur_config_of(*views, torch.empty_strided(shape, sdy, dtype=dtype, device="meta"), c)
+    _check(recur_validate(cfg))
+    return cfg, recur_saved_bytes(cfg), recur_workspace_bytes(cfg, True), (cfg.B, cfg.D), n, at, copied
+
+
 class GatedRecurrence:
     """A gated linear recurrence through libbpt; allocates its buffers with torch. For one new token of each sequence, call
     forward with S = 1 and the states as h0."""
@@ -1061,20 +1082,33 @@ class GatedRecurrence:
         their input is copied)."""
         if dy.dim() != 3 or dy.shape != x.shape or dy.dtype != x.dtype:
             raise ValueError(f"dy must be {tuple(x.shape)} of {x.dtype}, not {tuple(dy.shape)} of {dy.dtype}")
-        unit = 16 // dy.element_size()
-        if dy.stride(2) != 1 or any(n > 1 and st % unit for n, st in zip(dy.shape[:2], dy.stride())) or dy.data_ptr() % 16:
-            dy = dy.contiguous()
-        four = tuple(t.unsqueeze(2) for t in (x, r, i))
-        grads = _side_by_side(four)
-        if grads is None:
-            x, r, i = (t if _apart(f) and _span(t) == t.numel() else t.contiguous() for t, f in zip((x, r, i), four))
-            grads = [torch.empty_strided(t.shape, t.stride(), dtype=t.dtype, device=t.device) for t in (x, r, i)]
+        if not x.dtype == r.dtype == i.dtype or not x.shape == r.shape == i.shape:
+            raise ValueError("x, r and i must share a type and a shape")
+        if not dy.is_contiguous() or dy.data_ptr() % 16:
+            unit = 16 // dy.element_size()
+            if dy.stride(2) != 1 or any(n > 1 and st % unit for n, st in zip(dy.shape[:2], dy.stride())) or dy.data_ptr() % 16:
+                dy = dy.clone(memory_format=torch.contiguous_format)
+        x, r, i = (t.clone(memory_format=torch.contiguous_format) if t.data_ptr() % 16 else t for t in (x, r, i))
+        offsets = None
+        if not (x.is_contiguous() and r.is_contiguous() and i.is_contiguous()) or x.shape[0] * x.shape[1] == 1:
+            where = x.untyped_storage().data_ptr()
+            if where == r.untyped_storage().data_ptr() == i.untyped_storage().data_ptr():
+                low = min(x.storage_offset(), r.storage_offset(), i.storage_offset())
+                offsets = (x.storage_offset() - low, r.storage_offset() - low, i.storage_offset() - low)
+        cfg, ns, nb, states, n, at, copied = _recur_back_plan(x.dtype, x.shape, (x.stride(), r.stride(), i.stride()), dy.stride(), offsets, self.c)
+        x, r, i = (t.contiguous() if no else t for t, no in zip((x, r, i), copied)) if any(copied) else (x, r, i)
+        sp, lp = _saved_ptr(saved, ns), _f32(lam, states[1:], "lam")
+        h0p, dhTp, dev = _f32(h0, states, "h0"), _f32(dhT, states, "dhT"), x.get_device()
+        same = all(t is None or t.get_device() == dev for t in (r, i, lam, saved, dy, dhT, h0, lens))
+        np, stream = _int32(lens, cfg.B, "lens"), _stream_on(dev, same)
+        if n:
+            buf = x.new_empty(n)
+            grads = [buf.as_strided(x.shape, st, first) for st, first in at]
         else:
-            grads = [g.squeeze(2) for g in grads]
-        cfg = recur_config_of(x, r, i, dy, self.c)
-        dlam = torch.empty(cfg.D, dtype=torch.float32, device=x.device)
-        dh0 = torch.empty((cfg.B, cfg.D), dtype=torch.float32, device=x.device)
-        recur_bwd(cfg, x, r, i, lam, saved, dy, *grads, self._bytes(recur_workspace_bytes(cfg, True), x.device), dlam, h0, dhT, dh0, lens)
+            grads = [torch.empty_like(t) for t in (x, r, i)]      # without gaps: their strides too
+        dlam, dh0, ws = torch.empty_like(lam), lam.new_empty(states), self._bytes(nb, x.device)
+        _check(load().bpt_recur_bwd(cfg, x.data_ptr(), r.data_ptr(), i.data_ptr(), lp, np, h0p, sp, dy.data_ptr(), dhTp, grads[0].data_ptr(),
+                                    grads[1].data_ptr(), grads[2].data_ptr(), dlam.data_ptr(), dh0.data_ptr(), ws.data_ptr(), nb, stream))
         return dict(zip(("dx", "dr", "di"), grads), dlam=dlam, dh0=dh0)
 
 

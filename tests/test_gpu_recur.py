@@ -178,6 +178,38 @@ def test_strides_and_what_lies_beside():
         assert bool((w[:, :, :8] == fill).all()) and bool((w[:, :, 8 + D:] == fill).all())
 
 
+@pytest.mark.parametrize("S", [1, 3, 140])
+def test_layouts_of_a_backward(S):
+    """Inputs that lie otherwise than dense ones: the same gradients, laid out like them where that leaves no gaps."""
+    B, D = 3, 72
+    t = inputs(B, S, D, "bf16", 8)
+    ref = run(t)
+    full = lambda *n: torch.full(n, 3.0, dtype=torch.bfloat16, device="cuda")  # noqa: E731
+    turned = full(S, B, D).transpose(0, 1)
+    wide = full(B, S, 2 * D)[..., 8:8 + D]
+    odd = full(B * S * D + 1)[1:].view(B, S, D)      # off the 16 bytes
+    for name, view in (("x", turned), ("r", wide), ("i", odd), ("dy", odd), ("dy", wide), ("dy", turned)):
+        view.copy_(t[name])
+        got = run({**t, name: view}) if name != "i" else None
+        if got is None:                              # the forward takes no such pointer; the backward copies
+            rec = bpt.GatedRecurrence()
+            _, _, saved = rec.forward(t["x"], t["r"], t["i"], t["lam"], t["h0"], save=True)
+            got = rec.backward(t["x"], t["r"], view, t["lam"], saved, t["dy"], t["dhT"], t["h0"])
+        for k, v in got.items():
+            assert torch.equal(v, ref[k]), (name, k)
+        if name == "x":
+            assert got["dx"].stride() == turned.stride()
+    p = full(B, S, 3 * D)
+    for order in ("xri", "irx"):
+        v = {k: p[..., n * D:(n + 1) * D] for n, k in enumerate(order)}
+        for k in order:
+            v[k].copy_(t[k])
+        got = run({**t, **v})
+        for k, g in got.items():
+            assert torch.equal(g, ref[k]), (order, k)
+        assert all(got["d" + k].data_ptr() == got["d" + order[0]].data_ptr() + 2 * n * D for n, k in enumerate(order))
+
+
 def test_offsets_past_32_bits():
     """Sequences more than 2^31 elements apart: what dense tensors give."""
     B, S, D = 2, 300, 72
