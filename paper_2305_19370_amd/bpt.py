@@ -956,7 +956,7 @@ def _f32(t: Optional[torch.Tensor], shape: Tuple[int, ...], name: str) -> Option
     """The address of contiguous float32 of a shape, or None."""
     if t is None:
         return None
-    if t.dtype != torch.float32 or tuple(t.shape) != shape or not t.is_contiguous():
+    if t.dtype != torch.float32 or t.shape != shape or not t.is_contiguous():
         raise ValueError(f"{name} must be {list(shape)} contiguous float32, not {list(t.shape)} of {t.dtype}")
     return t.data_ptr()
 
@@ -1217,11 +1217,18 @@ def distill_workspace_bytes(cfg: DistillConfig, backward: bool) -> int:
     return load().bpt_distill_workspace_bytes(ctypes.byref(cfg), int(backward))
 
 
+@functools.lru_cache(maxsize=256)
+def _distill_sizes(cfg: bytes) -> Tuple[int, int, int]:
+    """Bytes of saved and of a forward's and a backward's workspace."""
+    c = DistillConfig.from_buffer_copy(cfg)
+    return distill_saved_bytes(c), distill_workspace_bytes(c, False), distill_workspace_bytes(c, True)
+
+
 def _dense(t: Optional[torch.Tensor], dtype: torch.dtype, shape: Tuple[int, ...], name: str) -> Optional[int]:
     """The address of a contiguous tensor of a type and shape, or None."""
     if t is None:
         return None
-    if t.dtype != dtype or tuple(t.shape) != shape or not t.is_contiguous():
+    if t.dtype != dtype or t.shape != shape or not t.is_contiguous():
         raise ValueError(f"{name} must be {list(shape)} contiguous {dtype}, not {list(t.shape)} of {t.dtype}")
     return t.data_ptr()
 
@@ -1234,7 +1241,7 @@ def distill_fwd(cfg: DistillConfig, h: torch.Tensor, W: torch.Tensor, values: to
             _dense(index, torch.int32, (T, K), "index"), _dense(targets, torch.int32, (T,), "targets"),
             _dense(weights, torch.float32, (T,), "weights"), _dense(loss, torch.float32, (3,), "loss"),
             _dense(tokens, torch.float32, (2, T), "tokens"))
-    sp, dev = _saved_ptr(saved, distill_saved_bytes(cfg)), h.get_device()
+    sp, dev = _saved_ptr(saved, _distill_sizes(bytes(cfg))[0]), h.get_device()
     same = all(t is None or t.get_device() == dev for t in (W, values, index, targets, weights, loss, tokens, saved, workspace))
     stream = _stream_on(dev, same)
     _check(load().bpt_distill_fwd(cfg, *ptrs, sp, workspace.data_ptr(), _nbytes(workspace), stream))
@@ -1245,7 +1252,7 @@ def distill_bwd(cfg: DistillConfig, h: torch.Tensor, W: torch.Tensor, saved: tor
     T, D, dt = cfg.T, cfg.D, _TORCH_DT.get(cfg.dtype)
     hp, Wp = _dense(h, dt, (T, D), "h"), _dense(W, dt, (D, cfg.ldw), "W")
     dhp, dWp = _dense(dh, dt, (T, D), "dh"), _dense(dW, _TORCH_DT.get(cfg.grad_dtype), (D, cfg.ldw), "dW")
-    sp, dev = _saved_ptr(saved, distill_saved_bytes(cfg)), h.get_device()
+    sp, dev = _saved_ptr(saved, _distill_sizes(bytes(cfg))[0]), h.get_device()
     same = all(t is None or t.get_device() == dev for t in (W, saved, dh, dW, workspace))
     stream = _stream_on(dev, same)
     _check(load().bpt_distill_bwd(cfg, hp, Wp, sp, float(dloss), dhp, dWp, workspace.data_ptr(), _nbytes(workspace), stream))
@@ -1268,14 +1275,15 @@ class DistillLoss:
         c, dev = self.cfg, h.device
         loss = torch.empty(3, dtype=torch.float32, device=dev)
         tokens = torch.empty((2, c.T), dtype=torch.float32, device=dev)
-        saved = self._bytes(distill_saved_bytes(c), dev)
-        distill_fwd(c, h, W, values, index, loss, tokens, saved, self._bytes(distill_workspace_bytes(c, False), dev), targets, weights)
+        ns, nb, _ = _distill_sizes(bytes(c))
+        saved = self._bytes(ns, dev)
+        distill_fwd(c, h, W, values, index, loss, tokens, saved, self._bytes(nb, dev), targets, weights)
         return loss, tokens, saved
 
     def backward(self, h: torch.Tensor, W: torch.Tensor, saved: torch.Tensor, dloss: float = 1.0,
                  want_dW: bool = True) -> Tuple[torch.Tensor, Optional[torch.Tensor]]:
         c = self.cfg
-        dh = torch.empty(h.shape, dtype=h.dtype, device=h.device)
-        dW = torch.empty((c.D, c.ldw), dtype=_TORCH_DT[c.grad_dtype], device=h.device) if want_dW else None
-        distill_bwd(c, h, W, saved, dloss, dh, dW, self._bytes(distill_workspace_bytes(c, True), h.device))
+        dh = torch.empty_like(h)
+        dW = torch.empty_like(W, dtype=_TORCH_DT[c.grad_dtype]) if want_dW else None
+        distill_bwd(c, h, W, saved, dloss, dh, dW, self._bytes(_distill_sizes(bytes(c))[2], h.device))
         return dh, dW
