@@ -38,7 +38,7 @@ BPT_DEV float wave_max(float v) {
 
 // One wave per token: valid entries sorted by index, an index that is given twice once with the sum of its probabilities; the
 // target's place among them; the token's factors. With seg, also where the entries of every 64 columns are.
-// The order comes from counting smaller indices: K steps over LDS for each of a lane's entries.
+// The order comes from counting smaller indices: K steps over LDS for each of a lane's entries, a comparison and an addition each.
 template <int kPer>                                    // entries of a lane
 __global__ __launch_bounds__(256) void distill_prep_kernel(DistillArgs a) {
   __shared__ __attribute__((aligned(16))) int skey[4][64 * kPer];
@@ -90,55 +90,64 @@ __global__ __launch_bounds__(256) void distill_prep_kernel(DistillArgs a) {
     skey[wv][lane + 64 * e] = key[e];
     sq[wv][lane + 64 * e] = q[e];
   }
-  __syncthreads();
-  bool first[kPer];
-  float qs[kPer];
-#pragma unroll
-  for (int e = 0; e < kPer; ++e) first[e] = key[e] != kNone, qs[e] = 0.0f;
-  // four entries at a time, without branches; those behind the last one are kNone, which no entry that counts is
-#pragma unroll 2
-  for (int i = 0; i < K1; i += 4) {
-    const i32x4 k = *(const i32x4*)&skey[wv][i];
-    const f32x4 v = *(const f32x4*)&sq[wv][i];
-#pragma unroll
-    for (int u = 0; u < 4; ++u)
-#pragma unroll
-      for (int e = 0; e < kPer; ++e) {
-        const bool same = k[u] == key[e];
-        qs[e] += same ? v[u] : 0.0f;
-        first[e] = first[e] && !(same && i + u < lane + 64 * e);
-      }
-  }
-  __syncthreads();
-#pragma unroll
-  for (int e = 0; e < kPer; ++e)
-    if (!first[e]) skey[wv][lane + 64 * e] = kNone;
-  __syncthreads();
-  int rank[kPer], n = 0;
+  lds_sync();
+  // places in the sorted list: smaller indices, and equal ones that come before
+  int rank[kPer], valid = 0, n = 0;
 #pragma unroll
   for (int e = 0; e < kPer; ++e) rank[e] = 0;
+#pragma unroll
+  for (int b = 0; b < kPer; ++b) {
+    const int end = K1 < 64 * b + 64 ? K1 : 64 * b + 64;   // kNone behind the last entry: smaller than nothing
 #pragma unroll 2
-  for (int i = 0; i < K1; i += 4) {
-    const i32x4 k = *(const i32x4*)&skey[wv][i];
+    for (int i = 64 * b; i < end; i += 4) {
+      const i32x4 k = *(const i32x4*)&skey[wv][i];
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      n += k[u] != kNone;
+      for (int u = 0; u < 4; ++u)
 #pragma unroll
-      for (int e = 0; e < kPer; ++e) rank[e] += k[u] < key[e];
+        for (int e = 0; e < kPer; ++e) {
+          if (b == e) rank[e] += k[u] - (i + u - 64 * b < lane) < key[e];
+          else rank[e] += b < e ? k[u] <= key[e] : k[u] < key[e];
+        }
     }
   }
-  __syncthreads();
+  lds_sync();
 #pragma unroll
   for (int e = 0; e < kPer; ++e) {
-    if (!first[e]) continue;
-    skey[wv][rank[e]] = key[e];
-    if (real) {
-      a.sidx[t * K1 + rank[e]] = key[e];
-      a.sq[t * K1 + rank[e]] = qs[e];
-      if (a.targets && key[e] == y) a.ypos[t] = rank[e];
+    const bool counts = key[e] != kNone;
+    if (counts) {
+      skey[wv][rank[e]] = key[e];
+      sq[wv][rank[e]] = q[e];
+    }
+    valid += __popcll(__ballot(counts));
+  }
+  lds_sync();
+  // the first of equal ones takes the sum of their probabilities
+  bool first[kPer];
+#pragma unroll
+  for (int e = 0; e < kPer; ++e) {
+    const int at = lane + 64 * e;
+    first[e] = at < valid && (at == 0 || skey[wv][at - 1] != skey[wv][at]);
+    if (first[e]) {
+      key[e] = skey[wv][at];
+      q[e] = sq[wv][at];
+      for (int j = at + 1; j < valid && skey[wv][j] == key[e]; ++j) q[e] += sq[wv][j];
     }
   }
-  __syncthreads();
+  lds_sync();
+#pragma unroll
+  for (int e = 0; e < kPer; ++e) {
+    const unsigned long long mask = __ballot(first[e]);
+    const int at = n + __popcll(mask & ((1ull << lane) - 1));
+    n += __popcll(mask);
+    if (!first[e]) continue;
+    skey[wv][at] = key[e];
+    if (real) {
+      a.sidx[t * K1 + at] = key[e];
+      a.sq[t * K1 + at] = q[e];
+      if (a.targets && key[e] == y) a.ypos[t] = at;
+    }
+  }
+  lds_sync();
   if (!real) return;
   if (lane == 0) {
     const float w = a.weights ? a.weights[t] : a.weight;
