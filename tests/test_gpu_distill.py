@@ -118,6 +118,20 @@ def test_an_index_given_twice(dtype):
     compare(t, cfg, run(t, cfg))
 
 
+@pytest.mark.parametrize("K", [63, 64, 128, 190, 256])
+def test_lists_longer_than_the_vocabulary(K):
+    """Ten logits: most indices of a list are given many times, in one row all of them the same; the target is one more entry."""
+    T, V = 21, 10
+    t = inputs(T, 64, 300, K, "f32", 12)
+    t["W"][:, V:] = 0.0
+    g = torch.Generator(device="cuda").manual_seed(13)
+    t["index"] = torch.randint(-1, V + 1, (T, K), generator=g, device="cuda", dtype=torch.int32)
+    t["index"][4] = 3
+    t["targets"] = torch.randint(0, V, (T,), generator=g, device="cuda", dtype=torch.int32)
+    cfg = config(t, V, tau=1.5, soft=1.0, hard=0.5, ldw=t["W"].shape[1])
+    compare(t, cfg, run(t, cfg))
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_the_order_of_a_list_changes_only_roundings(dtype):
     T, V, K = 33, 500, 70
