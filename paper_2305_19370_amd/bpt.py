@@ -1198,6 +1198,9 @@ class RecurrentLayer(Layer):
 
 
 # ---------------------------------------------------------------- distillation from a teacher's largest logits
+DISTILL_MAX_K = 256                                  # pairs of a list
+
+
 def make_distill_config(T: int, D: int, V: int, K: int, ldw: Optional[int] = None, block_rows: int = 0, tau: float = 1.0,
                         soft: float = 1.0, hard: float = 0.0, dtype: str = "bf16", grad_dtype: str = "f32", keep_bytes: int = 0) -> DistillConfig:
     """T tokens of width D, V logits, lists of K; see include/libbpt.h."""

@@ -55,6 +55,7 @@ class GPTShape:
     causal: bool = True
     ln_eps: float = 1e-5
     xent_block_rows: int = 0       # 0 = the library's default
+    distill_keep_bytes: int = 0    # logits that distill_forward keeps for its backward: 0 = the library's default, negative = none
     dropout: float = 0.0           # residual-branch dropout rate of every layer
     dropout_seed: int = 0          # base of the per-layer, per-step mask keys
     rope: str = "none"             # rotary positions of every layer: "half" or "interleaved" pairs
@@ -165,7 +166,8 @@ class GPT:
                  bpt.ln_workspace_bytes(self.lcfg), 256)
         if s.recurrent:
             ws = max(ws, *(bpt.layer_recurrent_workspace_bytes(self.cfg, k) for k in (False, True)))
-        self.distill = None                          # configuration and buffers of the last distill_forward
+        self.distill = None                          # configuration of the last distill_forward
+        self.distill_bufs = None                     # its buffers, from the first one on
         self.ws = torch.empty(ws, dtype=torch.uint8, device=device)
         if init:
             self.init_params(seed)
@@ -287,28 +289,39 @@ class GPT:
     def distill_forward(self, tokens: torch.Tensor, values: torch.Tensor, index: torch.Tensor, targets: Optional[torch.Tensor] = None,
                         weights: Optional[torch.Tensor] = None, tau: float = 1.0, soft: float = 1.0, hard: float = 0.0) -> torch.Tensor:
         """(loss, weighted kl, weighted ce) of tokens [B*S] int32 against a teacher's largest logits: values and index [B*S, K]
-        float32 and int32 (bpt.make_distill_config has the terms)."""
-        s, T = self.shape, self.shape.B * self.shape.S
-        cfg = bpt.make_distill_config(T, s.D, s.V, values.shape[1], ldw=s.ldw, block_rows=s.xent_block_rows, tau=tau, soft=soft,
-                                      hard=hard, dtype=s.dtype)
-        if self.distill is None or bytes(self.distill[0]) != bytes(cfg):
-            bpt._check(bpt.distill_validate(cfg))
-            new = lambda *n: torch.empty(n, dtype=torch.float32, device=self.device)  # noqa: E731
-            raw = lambda n: torch.empty(max(n, 256), dtype=torch.uint8, device=self.device)  # noqa: E731
-            self.distill = None                      # the old buffers go before new ones come
-            self.distill = (cfg, new(3), new(2, T), raw(bpt.distill_saved_bytes(cfg)),
-                            raw(max(bpt.distill_workspace_bytes(cfg, k) for k in (False, True))))
-        _, loss, per_token, saved, ws = self.distill
+        float32 and int32 (bpt.make_distill_config has the terms). The result is a buffer that the next call overwrites."""
+        cfg = self._distill_config(values.shape[1], tau, soft, hard)
+        bpt._check(bpt.distill_validate(cfg))
+        if self.distill_bufs is None:
+            self.distill_bufs = self._distill_buffers(values.shape[1])
+        loss, per_token, saved, ws = self.distill_bufs
+        self.distill = None                          # until the call has been made
         self._body_forward(tokens)
         bpt.distill_fwd(cfg, self.hf, self.weight("Wout"), values, index, loss, per_token, saved, ws, targets, weights)
+        self.distill = cfg
         return loss
+
+    def _distill_config(self, K: int, tau: float = 1.0, soft: float = 1.0, hard: float = 1.0) -> bpt.DistillConfig:
+        s = self.shape
+        return bpt.make_distill_config(s.B * s.S, s.D, s.V, K, ldw=s.ldw, block_rows=s.xent_block_rows, tau=tau, soft=soft, hard=hard,
+                                       dtype=s.dtype, keep_bytes=s.distill_keep_bytes)
+
+    def _distill_buffers(self, K: int) -> Tuple[torch.Tensor, ...]:
+        """Losses, what the forward keeps and the workspace: made once and never replaced, since a captured graph may hold their addresses, so
+        for the longest lists that this head takes (at least K), with targets."""
+        cfg = next((c for c in map(self._distill_config, range(bpt.DISTILL_MAX_K, K, -1)) if bpt.distill_validate(c) == 0),
+                   self._distill_config(K))
+        f32 = lambda *n: torch.empty(n, dtype=torch.float32, device=self.device)  # noqa: E731
+        raw = lambda n: torch.empty(max(n, 256), dtype=torch.uint8, device=self.device)  # noqa: E731
+        return (f32(3), f32(2, cfg.T), raw(bpt.distill_saved_bytes(cfg)),
+                raw(max(bpt.distill_workspace_bytes(cfg, back) for back in (False, True))))
 
     def distill_backward(self, tokens: torch.Tensor, dloss: float = 1.0) -> None:
         """Gradients of dloss * the loss of the last distill_forward into the flat gradient buffers (overwritten)."""
         if self.distill is None:
             raise ValueError("distill_backward follows distill_forward")
-        cfg, _, _, saved, ws = self.distill
-        bpt.distill_bwd(cfg, self.hf, self.weight("Wout"), saved, dloss, self.dh, self.grad("Wout"), ws)
+        _, _, saved, ws = self.distill_bufs
+        bpt.distill_bwd(self.distill, self.hf, self.weight("Wout"), saved, dloss, self.dh, self.grad("Wout"), ws)
         self._body_backward(tokens)
 
     def optimizer_step(self, lr: float, weight_decay: float = 0.1, beta1: float = 0.9, beta2: float = 0.95,

@@ -1,0 +1,48 @@
+"""Calls that the recurrence, the layer with it and the distillation loss take or refuse on the host: buffers that stay where a captured
+graph has them, gradients that lie otherwise than dense ones, arguments that must not share memory."""
+import os
+
+import pytest
+import torch
+
+from paper_2305_19370_amd import bpt
+
+needs_lib = pytest.mark.skipif(not os.path.exists(bpt.LIB_PATH), reason="libbpt.so not built")
+
+
+# ---------------------------------------------------------------- a GPT's buffers for the distillation loss
+@needs_lib
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_distillation_buffers_of_a_gpt_stay(monkeypatch, dtype):
+    """A graph may hold their addresses: they are made once, large enough for every list, with and without targets."""
+    from paper_2305_19370_amd.gpt import GPT, GPTShape
+    m = GPT(GPTShape(L=1, B=3, S=50, D=64, H=1, F=64, V=300, Bq=50, Bkv=50, dtype=dtype, xent_block_rows=64), device="cpu", init=False)
+    calls = []
+
+    def fwd(cfg, h, W, values, index, loss, tokens, saved, ws, targets, weights):
+        calls.append((cfg, loss, tokens, saved, ws))
+
+    monkeypatch.setattr(m, "_body_forward", lambda tokens: None)
+    monkeypatch.setattr(bpt, "distill_fwd", fwd)
+    tok = torch.zeros(150, dtype=torch.int32)
+    for K, tau, hard in ((8, 2.0, 0.0), (8, 2.0, 0.2), (256, 1.0, 0.5), (1, 1.5, 0.0), (64, 1.0, 0.0), (8, 2.0, 0.0)):
+        values, index = torch.zeros(150, K), torch.zeros(150, K, dtype=torch.int32)
+        m.distill_forward(tok, values, index, tok if hard else None, tau=tau, hard=hard)
+        cfg, *bufs = calls[-1]
+        assert (cfg.K, cfg.tau, cfg.hard) == (K, tau, pytest.approx(hard))
+        assert all(a is b for a, b in zip(bufs, calls[0][1:])), (K, tau, hard)
+        assert bufs[2].numel() >= bpt.distill_saved_bytes(cfg)
+        assert bufs[3].numel() >= max(bpt.distill_workspace_bytes(cfg, back) for back in (False, True))
+
+
+@needs_lib
+def test_distillation_of_a_gpt_keeps_what_its_shape_says(monkeypatch):
+    from paper_2305_19370_amd.gpt import GPT, GPTShape
+    sizes = []
+    for keep in (0, -1, 64 * 320 * 4):
+        m = GPT(GPTShape(L=1, B=3, S=50, D=64, H=1, F=64, V=300, Bq=50, Bkv=50, xent_block_rows=64, distill_keep_bytes=keep), device="cpu", init=False)
+        monkeypatch.setattr(m, "_body_forward", lambda tokens: None)
+        monkeypatch.setattr(bpt, "distill_fwd", lambda cfg, h, W, values, index, loss, tokens, saved, *rest: sizes.append((cfg.keep_bytes, saved.numel())))
+        m.distill_forward(torch.zeros(150, dtype=torch.int32), torch.zeros(150, 4), torch.zeros(150, 4, dtype=torch.int32))
+    assert [k for k, _ in sizes] == [0, -1, 64 * 320 * 4]
+    assert sizes[0][1] - sizes[1][1] == 150 * 320 * 4 and sizes[2][1] - sizes[1][1] == 64 * 320 * 4
