@@ -514,7 +514,8 @@ size_t bpt_layer_recurrent_saved_bytes(const bpt_config* cfg);
 size_t bpt_layer_recurrent_workspace_bytes(const bpt_config* cfg, int backward);
 bpt_status bpt_layer_fwd_recurrent(const bpt_config* cfg, const bpt_recur_mixer* mixer, const void* X, const bpt_params* params,
                                    void* Y, void* saved, void* workspace, size_t workspace_bytes, void* stream);
-/* dhT: gradient of the last states, or NULL. dlambda [D] and dh0 [B, D] fp32, overwritten; NULL skips. dh0 may be dhT. */
+/* dhT: gradient of the last states, or NULL. dlambda [D] and dh0 [B, D] fp32, overwritten; NULL skips. dh0 may be dhT. Neither
+ * dlambda, dh0 nor the forward's hT may be any other argument, and no other output lambda, h0 or dhT. */
 bpt_status bpt_layer_bwd_recurrent(const bpt_config* cfg, const bpt_recur_mixer* mixer, const void* X, const bpt_params* params,
                                    const void* saved, const void* dY, const float* dhT, void* dX, const bpt_grads* grads,
                                    float* dlambda, float* dh0, void* workspace, size_t workspace_bytes, void* stream);

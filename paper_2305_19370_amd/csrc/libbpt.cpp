@@ -282,6 +282,16 @@ DropArgs drop_args(const bpt_config& c, uint32_t site, int64_t row0) {
 
 bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
 
+// Whether an output is one of some other pointers (NULL is none)
+template <typename Outs, typename Others>
+bool any_alias(const Outs& outs, const Others& others) {
+  for (const void* o : outs)
+    for (const void* q : others)
+      if (o && o == q) return true;
+  return false;
+}
+typedef std::initializer_list<const void*> Ptrs;
+
 #define HIPCHK(expr)                                                                   \
   do {                                                                                 \
     hipError_t _e = (expr);                                                            \
@@ -927,6 +937,10 @@ static bpt_status layer_fwd(const bpt_config* cfg, const bpt_layer_options* opt,
     if (!rec->m->lambda) return fail(BPT_ERR_INVALID_ARG, "NULL lambda");
     for (const void* q : {(const void*)rec->m->lambda, (const void*)rec->m->h0, (const void*)rec->m->hT})
       if (q && !aligned16(q)) return fail(BPT_ERR_INVALID_ARG, "pointer %p is not 16-byte aligned", q);
+    const Ptrs hT = {rec->m->hT}, own = {rec->m->lambda, rec->m->h0};
+    if (any_alias(hT, ptrs) || any_alias(hT, Ptrs{rec->m->lambda}))
+      return fail(BPT_ERR_INVALID_ARG, "hT must not alias Y, saved, the workspace or an input but h0");
+    if (any_alias(Ptrs{Y, saved, ws}, own)) return fail(BPT_ERR_INVALID_ARG, "Y, saved and the workspace must not alias lambda or h0");
     int64_t more;
     rw = recur_ws(layer_recur(*cfg, rec->m->c), off(ws, need), 0, &more);
     need += more;
@@ -1123,7 +1137,11 @@ static bpt_status layer_bwd(const bpt_config* cfg, const bpt_layer_options* opt,
     if (!rec->m->lambda) return fail(BPT_ERR_INVALID_ARG, "NULL lambda");
     for (const void* q : {(const void*)rec->m->lambda, (const void*)rec->m->h0, (const void*)rec->dhT, (const void*)rec->dlambda, (const void*)rec->dh0})
       if (q && !aligned16(q)) return fail(BPT_ERR_INVALID_ARG, "pointer %p is not 16-byte aligned", q);
-    if (rec->dh0 && (rec->dh0 == rec->m->h0 || rec->dh0 == rec->dlambda)) return fail(BPT_ERR_INVALID_ARG, "dh0 must not alias h0 or dlambda");
+    const Ptrs outs = {rec->dlambda, rec->dh0}, own = {rec->m->lambda, rec->m->h0, rec->dhT};
+    if (any_alias(outs, ptrs) || any_alias(outs, Ptrs{rec->m->lambda, rec->m->h0}) || any_alias(Ptrs{rec->dlambda}, Ptrs{rec->dhT, rec->dh0}))
+      return fail(BPT_ERR_INVALID_ARG, "dlambda and dh0 must not alias an input, an output or the workspace (dh0 may be dhT)");
+    if (any_alias(Ptrs{dX, ws, G.dln1_g, G.dln1_b, G.dWq, G.dWk, G.dWv, G.dWo, G.dln2_g, G.dln2_b, G.dW1, G.db1, G.dW2, G.db2}, own))
+      return fail(BPT_ERR_INVALID_ARG, "gradients and the workspace must not alias lambda, h0 or dhT");
     int64_t more;
     rw = recur_ws(layer_recur(*cfg, rec->m->c), off(ws, need), 1, &more);
     need += more;

@@ -46,3 +46,46 @@ def test_distillation_of_a_gpt_keeps_what_its_shape_says(monkeypatch):
         m.distill_forward(torch.zeros(150, dtype=torch.int32), torch.zeros(150, 4), torch.zeros(150, 4, dtype=torch.int32))
     assert [k for k, _ in sizes] == [0, -1, 64 * 320 * 4]
     assert sizes[0][1] - sizes[1][1] == 150 * 320 * 4 and sizes[2][1] - sizes[1][1] == 64 * 320 * 4
+
+
+# ---------------------------------------------------------------- arguments that must not share memory
+A = 1 << 20                                          # an aligned address that nothing may touch
+
+
+@needs_lib
+def test_recurrent_layer_refuses_shared_memory():
+    lib, cfg = bpt.load(), bpt.make_config(2, 300, 256, 4, 512, 64, 64, True, "bf16")
+    names = ("lam", "h0", "hT", "X", "Y", "saved", "ws") + bpt.PARAM_FIELDS
+    good = {k: (n + 1) * A for n, k in enumerate(names)}
+
+    def fwd(n=0, **kw):                              # n = 0: without a workspace, the last check before anything runs
+        a = {**good, **kw}
+        return lib.bpt_layer_fwd_recurrent(cfg, bpt.RecurMixer(8.0, a["lam"], a["h0"], a["hT"]), a["X"], bpt.Params(*[a[k] for k in bpt.PARAM_FIELDS]),
+                                           a["Y"], a["saved"], a["ws"], n, None)
+
+    assert fwd() == 3 and fwd(hT=good["h0"]) == 3 and fwd(hT=None) == 3 and fwd(h0=None) == 3
+    for k in names:
+        if k not in ("h0", "hT"):
+            assert fwd(hT=good[k]) == 1, k
+    for k in ("Y", "saved", "ws"):
+        for q in ("lam", "h0", "hT"):
+            assert fwd(**{k: good[q]}) == 1, (k, q)
+
+    names = ("lam", "h0", "dhT", "X", "saved", "dY", "dX", "dlam", "dh0", "ws") + bpt.PARAM_FIELDS + bpt.GRAD_FIELDS
+    good = {k: (n + 1) * A for n, k in enumerate(names)}
+
+    def bwd(n=0, **kw):
+        a = {**good, **kw}
+        return lib.bpt_layer_bwd_recurrent(cfg, bpt.RecurMixer(8.0, a["lam"], a["h0"], None), a["X"], bpt.Params(*[a[k] for k in bpt.PARAM_FIELDS]),
+                                           a["saved"], a["dY"], a["dhT"], a["dX"], bpt.Grads(*[a[k] for k in bpt.GRAD_FIELDS]), a["dlam"], a["dh0"],
+                                           a["ws"], n, None)
+
+    assert bwd() == 3 and bwd(dh0=good["dhT"]) == 3 and bwd(dlam=None, dh0=None, dhT=None, h0=None) == 3
+    for k in names:
+        if k != "dlam":
+            assert bwd(dlam=good[k]) == 1, k
+        if k not in ("dh0", "dhT"):
+            assert bwd(dh0=good[k]) == 1, k
+    for k in ("dX", "ws") + bpt.GRAD_FIELDS:
+        for q in ("lam", "h0", "dhT"):
+            assert bwd(**{k: good[q]}) == 1, (k, q)
