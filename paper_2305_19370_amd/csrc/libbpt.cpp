@@ -1936,11 +1936,10 @@ bpt_status bpt_recur_fwd(const bpt_recur_config* cfg, const void* x, const void*
   bpt_status st = recur_check(cfg);
   if (st != BPT_OK) return st;
   if (!x || !r || !i || !lambda || !y) return fail(BPT_ERR_INVALID_ARG, "NULL x, r, i, lambda or y");
-  for (const void* q : {x, r, i, (const void*)lambda, (const void*)lens}) {
-    if (y == q) return fail(BPT_ERR_INVALID_ARG, "y must not alias an input");
-    if (hT && hT == q) return fail(BPT_ERR_INVALID_ARG, "hT must not alias an input but h0");
-  }
-  if (y == h0 || y == hT || (saved && (saved == y || saved == hT))) return fail(BPT_ERR_INVALID_ARG, "y, the states and saved must not alias one another");
+  const Ptrs in = {x, r, i, lambda, lens};
+  if (any_alias(Ptrs{y, saved, ws}, in) || any_alias(Ptrs{y, saved, ws}, Ptrs{h0, hT}) || any_alias(Ptrs{hT}, in))
+    return fail(BPT_ERR_INVALID_ARG, "y, hT, saved and the workspace must not alias an input (hT may be h0)");
+  if (any_alias(Ptrs{y, ws}, Ptrs{saved}) || y == ws) return fail(BPT_ERR_INVALID_ARG, "y, saved and the workspace must not alias one another");
   for (const void* q : {x, r, i, (const void*)lambda, (const void*)lens, (const void*)h0, (const void*)y, (const void*)hT,
                         (const void*)saved, (const void*)ws})
     if (q && !aligned16(q)) return fail(BPT_ERR_INVALID_ARG, "pointer %p is not 16-byte aligned", q);
@@ -1966,6 +1965,8 @@ bpt_status bpt_recur_bwd(const bpt_recur_config* cfg, const void* x, const void*
   if (!saved && recur_saved(*cfg) > 0) return fail(BPT_ERR_INVALID_ARG, "NULL saved");
   const void* in[] = {x, r, i, lambda, lens, h0, saved, dy, ws};
   void* out[] = {dx, dr, di, dlambda, dh0};
+  if (any_alias(Ptrs{ws}, Ptrs{x, r, i, lambda, lens, h0, saved, dy, dhT}))
+    return fail(BPT_ERR_INVALID_ARG, "the workspace must not alias an input");
   for (const void* q : in)
     if (q && !aligned16(q)) return fail(BPT_ERR_INVALID_ARG, "pointer %p is not 16-byte aligned", q);
   if (!aligned16(dhT)) return fail(BPT_ERR_INVALID_ARG, "pointer %p is not 16-byte aligned", (const void*)dhT);
@@ -2120,6 +2121,9 @@ bpt_status bpt_distill_fwd(const bpt_distill_config* cfg, const void* h, const v
   for (const void* q : {h, W, (const void*)values, (const void*)index, (const void*)targets, (const void*)weights, (const void*)loss,
                         (const void*)tokens, (const void*)saved, (const void*)ws})
     if (q && !aligned16(q)) return fail(BPT_ERR_INVALID_ARG, "pointer %p is not 16-byte aligned", q);
+  if (any_alias(Ptrs{loss, tokens, saved, ws}, Ptrs{h, W, values, index, targets, weights}) || any_alias(Ptrs{loss}, Ptrs{tokens, saved, ws}) ||
+      any_alias(Ptrs{tokens}, Ptrs{saved, ws}) || saved == ws)
+    return fail(BPT_ERR_INVALID_ARG, "loss, tokens, saved and the workspace must not alias an input or one another");
   const XentDims d = distill_dims(*cfg);
   int64_t need, stotal;
   const DistillWs w = distill_ws(*cfg, d, ws, 0, &need);
@@ -2171,7 +2175,8 @@ bpt_status bpt_distill_bwd(const bpt_distill_config* cfg, const void* h, const v
     if (!aligned16(q)) return fail(BPT_ERR_INVALID_ARG, "pointer %p is not 16-byte aligned", q);
   }
   if (!aligned16(dW)) return fail(BPT_ERR_INVALID_ARG, "pointer %p is not 16-byte aligned", dW);
-  if (dh == h || dh == W || dW == h || dW == W || dh == dW) return fail(BPT_ERR_INVALID_ARG, "dh and dW must not alias h, W or one another");
+  if (any_alias(Ptrs{dh, dW, ws}, Ptrs{h, W, saved}) || any_alias(Ptrs{dh}, Ptrs{dW, ws}) || any_alias(Ptrs{dW}, Ptrs{ws}))
+    return fail(BPT_ERR_INVALID_ARG, "dh, dW and the workspace must not alias h, W, saved or one another");
   const XentDims d = distill_dims(*cfg);
   int64_t need, stotal;
   const DistillWs w = distill_ws(*cfg, d, ws, 1, &need);

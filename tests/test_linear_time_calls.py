@@ -89,3 +89,23 @@ def test_recurrent_layer_refuses_shared_memory():
     for k in ("dX", "ws") + bpt.GRAD_FIELDS:
         for q in ("lam", "h0", "dhT"):
             assert bwd(**{k: good[q]}) == 1, (k, q)
+
+
+@needs_lib
+def test_operators_refuse_shared_memory():
+    """Every pair of arguments of which one is written, but hT = h0 and dh0 = dhT."""
+    lib, x = bpt.load(), torch.empty(2, 300, 72, dtype=torch.bfloat16)
+    rec, dis = bpt.recur_config_of(x, x, x, x), bpt.make_distill_config(100, 64, 1000, 20, tau=2.0, soft=0.5, hard=0.5)
+    for f, names, written, may in (
+            (lambda *a: lib.bpt_recur_fwd(rec, *a, 1, None), "x r i lam lens h0 y hT saved ws", "y hT saved ws", ("h0", "hT")),
+            (lambda *a: lib.bpt_recur_bwd(rec, *a, 1, None), "x r i lam lens h0 saved dy dhT dx dr di dlam dh0 ws", "dx dr di dlam dh0 ws", ("dhT", "dh0")),
+            (lambda *a: lib.bpt_distill_fwd(dis, *a, 1, None), "h W values index targets weights loss tokens saved ws", "loss tokens saved ws", None),
+            (lambda h, W, saved, *a: lib.bpt_distill_bwd(dis, h, W, saved, 1.0, *a, 1, None), "h W saved dh dW ws", "dh dW ws", None)):
+        names = names.split()
+        good = {k: (n + 1) * A for n, k in enumerate(names)}
+        assert f(*good.values()) == 3, names         # the workspace of one byte, the last check
+        for k in written.split():
+            for q in names:
+                if q != k:
+                    want = 3 if may and {k, q} == set(may) else 1
+                    assert f(*{**good, k: good[q]}.values()) == want, (names, k, q)
