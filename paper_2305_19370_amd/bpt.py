@@ -1084,10 +1084,9 @@ class GatedRecurrence:
             raise ValueError(f"dy must be {tuple(x.shape)} of {x.dtype}, not {tuple(dy.shape)} of {dy.dtype}")
         if not x.dtype == r.dtype == i.dtype or not x.shape == r.shape == i.shape:
             raise ValueError("x, r and i must share a type and a shape")
-        if not dy.is_contiguous() or dy.data_ptr() % 16:
-            unit = 16 // dy.element_size()
-            if dy.stride(2) != 1 or any(n > 1 and st % unit for n, st in zip(dy.shape[:2], dy.stride())) or dy.data_ptr() % 16:
-                dy = dy.clone(memory_format=torch.contiguous_format)
+        # a broadcast one too: its rows share memory, as those of the y that it is laid out like may not
+        if (not dy.is_contiguous() or dy.data_ptr() % 16) and not _apart(dy):
+            dy = dy.clone(memory_format=torch.contiguous_format)
         x, r, i = (t.clone(memory_format=torch.contiguous_format) if t.data_ptr() % 16 else t for t in (x, r, i))
         offsets = None
         if not (x.is_contiguous() and r.is_contiguous() and i.is_contiguous()) or x.shape[0] * x.shape[1] == 1:

@@ -3,7 +3,9 @@ import pytest
 import torch
 
 from gpu_util import say
+from paper_2305_19370_amd import bpt
 from paper_2305_19370_amd.gpt import GPT, GPTShape
+from test_linear_time_calls import BROADCAST
 
 pytestmark = pytest.mark.gpu
 KW = dict(L=2, B=2, S=150, D=256, H=4, F=512, V=500, Bq=64, Bkv=64)
@@ -45,3 +47,20 @@ def test_other_lists_between_the_replays_of_a_graph():
         graph.replay()
         assert all(torch.equal(a, b) for a, b in zip(result(loss), refs[0])), k
         assert all(bool((t == 7).all()) for t in others), k
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("name", BROADCAST)
+def test_a_broadcast_gradient(name, dtype):
+    """The gradient of a mean or a sum, expanded over steps or sequences: what its dense copy gives."""
+    for B, S in ((3, 140), (2, 1), (1, 70)):
+        say(f"case broadcast dy {name} {B} {S}")
+        g = torch.Generator(device="cuda").manual_seed(S)
+        rn = lambda *n: torch.randn(*n, generator=g, device="cuda")  # noqa: E731
+        x, r, i = (rn(B, S, 72).to(dtype) for _ in range(3))
+        lam, rec, part = rn(72), bpt.GatedRecurrence(), BROADCAST[name](B, S, 72, dtype)
+        dy = torch.randn(part.untyped_storage().nbytes() // part.element_size(), generator=g, device="cuda").to(dtype).as_strided(part.shape, part.stride())
+        _, _, saved = rec.forward(x, r, i, lam, save=True)
+        got, ref = (rec.backward(x, r, i, lam, saved, d) for d in (dy, dy.contiguous().clone()))
+        for k in ref:
+            assert torch.equal(got[k], ref[k]), k

@@ -109,3 +109,21 @@ def test_operators_refuse_shared_memory():
                 if q != k:
                     want = 3 if may and {k, q} == set(may) else 1
                     assert f(*{**good, k: good[q]}.values()) == want, (names, k, q)
+
+
+# ---------------------------------------------------------------- layouts that the class takes, on the CPU: the last refusal is that of the place
+BROADCAST = {"mean over tokens": lambda B, S, D, dt: torch.ones(B, 1, D, dtype=dt).expand(B, S, D),
+             "one gradient of all sequences": lambda B, S, D, dt: torch.ones(1, S, D, dtype=dt).expand(B, S, D),
+             "one row": lambda B, S, D, dt: torch.ones(D, dtype=dt).expand(B, S, D),
+             "one number": lambda B, S, D, dt: torch.ones((), dtype=dt).expand(B, S, D),
+             "windows of one sequence": lambda B, S, D, dt: torch.ones(B + S, D, dtype=dt).as_strided((B, S, D), (D, D, 1))}
+
+
+@needs_lib
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("name", BROADCAST)
+def test_a_broadcast_gradient_is_taken(name, dtype):
+    for B, S in ((2, 30), (2, 1), (1, 30), (1, 1)):
+        x, lam = torch.zeros(B, S, 72, dtype=dtype), torch.zeros(72)
+        with pytest.raises(ValueError, match="on the GPU"):
+            bpt.GatedRecurrence().backward(x, x, x, lam, torch.empty(1 << 16, dtype=torch.uint8), BROADCAST[name](B, S, 72, dtype))
