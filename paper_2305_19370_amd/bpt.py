@@ -1053,9 +1053,13 @@ class GatedRecurrence:
     def forward(self, x: torch.Tensor, r: torch.Tensor, i: torch.Tensor, lam: torch.Tensor, h0: Optional[torch.Tensor] = None,
                 lens: Optional[torch.Tensor] = None,
                 save: bool = False) -> Tuple[torch.Tensor, torch.Tensor, Optional[torch.Tensor]]:
-        """y [B, S, D], the last states [B, D] (float32), and with `save` what backward takes."""
+        """y [B, S, D], the last states [B, D] (float32), and with `save` what backward takes. Inputs off 16 bytes are copied."""
         if not x.dtype == r.dtype == i.dtype or not x.shape == r.shape == i.shape:
             raise ValueError("x, r and i must share a type and a shape")
+        xp, rp, ip = x.data_ptr(), r.data_ptr(), i.data_ptr()
+        if (xp | rp | ip) & 15:
+            x, r, i = (t.clone(memory_format=torch.contiguous_format) if t.data_ptr() % 16 else t for t in (x, r, i))
+            xp, rp, ip = x.data_ptr(), r.data_ptr(), i.data_ptr()
         cfg, ns, nb, states = _recur_plan(x.dtype, x.shape, x.stride(), r.stride(), i.stride(), self.c)
         at = x.get_device()
         same = at == r.get_device() == i.get_device() == lam.get_device()
@@ -1070,7 +1074,7 @@ class GatedRecurrence:
         hT = lam.new_empty(states) if h0 is None else torch.empty_like(h0)
         saved = self._bytes(ns, x.device) if save else None
         ws = self._bytes(nb, x.device) if nb else None
-        _check(load().bpt_recur_fwd(cfg, x.data_ptr(), r.data_ptr(), i.data_ptr(), ap, lp, hp, y.data_ptr(),
+        _check(load().bpt_recur_fwd(cfg, xp, rp, ip, ap, lp, hp, y.data_ptr(),
                                     hT.data_ptr(), saved.data_ptr() if save and ns else None, ws.data_ptr() if nb else None, nb, stream))
         return y, hT, saved
 

@@ -64,3 +64,24 @@ def test_a_broadcast_gradient(name, dtype):
         got, ref = (rec.backward(x, r, i, lam, saved, d) for d in (dy, dy.contiguous().clone()))
         for k in ref:
             assert torch.equal(got[k], ref[k]), k
+
+
+@pytest.mark.parametrize("S", [1, 140])
+def test_inputs_off_16_bytes(S):
+    """Views that start anywhere: what aligned copies give, forward and backward."""
+    B, D = 3, 72
+    g = torch.Generator(device="cuda").manual_seed(S)
+    v = [torch.randn(B, S, D, generator=g, device="cuda").bfloat16() for _ in range(4)]
+    lam, rec = torch.randn(D, generator=g, device="cuda"), bpt.GatedRecurrence()
+
+    def run(x, r, i, dy):
+        y, hT, saved = rec.forward(x, r, i, lam, save=True)
+        return dict(rec.backward(x, r, i, lam, saved, dy), y=y, hT=hT)
+
+    ref = run(*v)
+    for k in range(4):
+        for first in (1, 4):
+            say(f"case input {k} off by {first} elements")
+            odd = torch.empty(B * S * D + first, dtype=torch.bfloat16, device="cuda")[first:].view(B, S, D)
+            got = run(*(odd.copy_(t) if n == k else t for n, t in enumerate(v)))
+            assert all(torch.equal(got[n], ref[n]) for n in ref)

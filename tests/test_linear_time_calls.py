@@ -127,3 +127,17 @@ def test_a_broadcast_gradient_is_taken(name, dtype):
         x, lam = torch.zeros(B, S, 72, dtype=dtype), torch.zeros(72)
         with pytest.raises(ValueError, match="on the GPU"):
             bpt.GatedRecurrence().backward(x, x, x, lam, torch.empty(1 << 16, dtype=torch.uint8), BROADCAST[name](B, S, 72, dtype))
+
+
+@needs_lib
+@pytest.mark.parametrize("S", [1, 30])
+def test_a_forward_takes_inputs_off_16_bytes(monkeypatch, S):
+    """As the backward does: they are copied, and what the library gets is aligned. (Here it stands in for the library.)"""
+    got = []
+    monkeypatch.setattr(bpt, "_stream_on", lambda dev, same: 0)
+    monkeypatch.setattr(bpt.load(), "bpt_recur_fwd", lambda cfg, *a: got.append(a) or 0)
+    x, odd = torch.ones(2, S, 72), torch.ones(2 * S * 72 + 1)[1:].view(2, S, 72)
+    for t in ((odd, x, x), (x, odd, x), (x, x, odd), (x, x, x)):
+        y, _, _ = bpt.GatedRecurrence().forward(*t, torch.zeros(72))
+        assert all(p % 16 == 0 for p in got[-1][:3]) and y.shape == x.shape
+        assert [p == a.data_ptr() for p, a in zip(got[-1], t)] == [a is x for a in t]      # aligned ones are not copied
