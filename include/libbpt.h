@@ -529,7 +529,8 @@ bpt_status bpt_layer_bwd_recurrent(const bpt_config* cfg, const bpt_recur_mixer*
  * An entry whose index lies outside [0, V) or whose value is -inf is left out (a list may be shorter than K); an index that is
  * given twice counts with the sum of its probabilities; a token without entries has kl_t = 0, one whose target lies outside
  * [0, V) ce_t = 0. A token of weight 0, or that has neither, is left out of losses and gradients whatever its row of h holds
- * (its own row of dh is 0). Logits, sums and losses are fp32; the gradient of the logits is rounded to cfg->dtype as the operand of
+ * (its own row of dh is 0). Logits, sums and losses are fp32, weights are formed from differences to the row's maximum: what a small tau
+ * magnifies is the logits' own rounding, as z / tau asks for, and no other. The gradient of the logits is rounded to cfg->dtype as the operand of
  * dh = G W^T and dW = h^T G. */
 typedef struct {
   int64_t T, D, V, K;    /* tokens, hidden width, vocabulary, pairs of a list (<= 256)           */
@@ -546,8 +547,8 @@ typedef struct {
 
 bpt_status bpt_distill_validate(const bpt_distill_config* cfg);
 
-/* What the forward keeps for the backward (lists sorted by index, their probabilities and logits, row statistics: 12 bytes a
- * pair and 28 a token; and what keep_bytes allows of 4 ldw bytes a token); workspace of
+/* What the forward keeps for the backward (lists sorted by index, their probabilities and logits: 12 bytes a pair and, if hard > 0,
+ * 12 a target; row statistics: 32 a token; and what keep_bytes allows of 4 ldw bytes a token); workspace of
  * bpt_distill_fwd (backward = 0) or bpt_distill_bwd (1). 0 for an invalid configuration. Host-only. */
 size_t bpt_distill_saved_bytes(const bpt_distill_config* cfg);
 size_t bpt_distill_workspace_bytes(const bpt_distill_config* cfg, int backward);

@@ -195,20 +195,22 @@ BPT_DEV void join(float& m, float& l, float& l1, float m2, float l2, float l12, 
 BPT_DEV void finish(const DistillArgs& a, int64_t t, int lane, float m, float l, float l1) {
 #pragma unroll
   for (int o = 32; o >= 1; o >>= 1) join(m, l, l1, __shfl_xor(m, o, 64), __shfl_xor(l, o, 64), __shfl_xor(l1, o, 64), a.scale);
-  const float lt = m / a.tau + logf(l), lo = a.two ? m + logf(l1) : lt;
+  // maximum and logarithms apart: with a small tau z / tau is large, and one number would hold of ll what is left behind z / tau
+  const float ll = logf(l), lo = a.two ? logf(l1) : ll;
   float kl = 0.0f;
   for (int j = lane; j < a.count[t]; j += 64) {
     const float q = a.sq[t * a.K1 + j];
-    if (q != 0.0f) kl += q * (logf(q) - a.sz[t * a.K1 + j] / a.tau + lt);
+    if (q != 0.0f) kl += q * (logf(q) + (m - a.sz[t * a.K1 + j]) / a.tau + ll);
   }
   kl = warp_sum(kl);
   if (lane) return;
   const int y = a.ypos[t];
   const bool in = a.w[t] != 0.0f;                      // a token of no weight is left out, whatever it holds
-  a.lt[t] = lt;
+  a.mx[t] = m;
+  a.lt[t] = ll;
   a.l1[t] = lo;
   a.tokens[t] = in ? kl : 0.0f;
-  a.tokens[a.Tall + t] = in && y >= 0 ? lo - a.sz[t * a.K1 + y] : 0.0f;
+  a.tokens[a.Tall + t] = in && y >= 0 ? (m - a.sz[t * a.K1 + y]) + lo : 0.0f;
 }
 }  // namespace
 
@@ -319,12 +321,13 @@ __global__ __launch_bounds__(256) void distill_grad_kernel(DistillArgs a, float 
   const int part = (tiles + steps - 1) / steps;
   const int64_t n0 = (int64_t)(blockIdx.x / part) * kTok, rows = a.T - a.t0, ldz = a.ng * 64;
   const int first = (int)(blockIdx.x % part) * steps, last = first + steps < tiles ? first + steps : tiles;
-  float l2[kGroups][4], g[kGroups][4], l21[kGroups][4], g1[kGroups][4];
+  float mx[kGroups][4], l2[kGroups][4], g[kGroups][4], l21[kGroups][4], g1[kGroups][4];
 #pragma unroll
   for (int k = 0; k < kGroups; ++k)
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       const int64_t n = n0 + 64 * k + 4 * tg + e, t = a.t0 + (n < rows ? n : rows - 1);
+      mx[k][e] = a.mx[t];
       l2[k][e] = a.lt[t] * kLog2e;
       g[k][e] = a.gs[t];
       g1[k][e] = a.gh[t];
@@ -352,8 +355,9 @@ __global__ __launch_bounds__(256) void distill_grad_kernel(DistillArgs a, float 
         __attribute__((aligned(16))) T out[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          float r = g[k][e] * __builtin_amdgcn_exp2f(fmaf(v[k][e][c], a.scale, -l2[k][e]));
-          if (a.two) r = fmaf(g1[k][e], __builtin_amdgcn_exp2f(fmaf(v[k][e][c], kLog2e, -l21[k][e])), r);
+          const float d = v[k][e][c] - mx[k][e];
+          float r = g[k][e] * __builtin_amdgcn_exp2f(fmaf(d, a.scale, -l2[k][e]));
+          if (a.two) r = fmaf(g1[k][e], __builtin_amdgcn_exp2f(fmaf(d, kLog2e, -l21[k][e])), r);
           const bool none = (g[k][e] == 0.0f && g1[k][e] == 0.0f) || v0 + 4 * q + c >= a.V;
           out[e] = from_f32<T>(none ? 0.0f : r);
         }
@@ -388,9 +392,9 @@ __global__ __launch_bounds__(256) void distill_listed_kernel(DistillArgs a, floa
   // neighbouring threads take neighbouring tokens: their lists' columns of G are neighbours
   const int64_t e = (int64_t)(blockIdx.x - first) * 256 + threadIdx.x, j = e / rows, t = a.t0 + e % rows;
   if (j >= a.K1 || j >= a.count[t]) return;
-  const float gs = a.gs[t], gh = a.gh[t], z = a.sz[t * a.K1 + j];
+  const float gs = a.gs[t], gh = a.gh[t], d = a.sz[t * a.K1 + j] - a.mx[t];
   if (gs == 0.0f && gh == 0.0f) return;
-  const float p = __builtin_amdgcn_exp2f(z * a.scale - a.lt[t] * kLog2e), p1 = a.two ? __builtin_amdgcn_exp2f((z - a.l1[t]) * kLog2e) : p;
+  const float p = __builtin_amdgcn_exp2f(fmaf(d, a.scale, -a.lt[t] * kLog2e)), p1 = a.two ? __builtin_amdgcn_exp2f(fmaf(d, kLog2e, -a.l1[t] * kLog2e)) : p;
   const float g = gs * (p - a.sq[t * a.K1 + j]) + gh * (a.ypos[t] == j ? p1 - 1.0f : p1);
   G[(int64_t)a.sidx[t * a.K1 + j] * ld + (t - a.t0)] = from_f32<T>(dloss * g);
 }

@@ -64,8 +64,9 @@ BPT_DEV float xent_grad_t(const GemmArgs& a, int64_t m, int64_t n, float v) {
 
 // EPI_LIST_T: what the column (token) contributes, loaded once per column where a tile allows it
 struct ListCol {
-  float l2, g, l21, g1;          // base-2 log-sum-exps and factors
+  float mx, l2, g, l21, g1;      // maximum, base-2 logarithms of the sums and factors
   BPT_DEV void load(const GemmArgs& a, int64_t n) {
+    mx = a.rowm[n];
     l2 = a.rowv[n] * 1.4426950408889634f;
     g = a.rowg[n];
     l21 = 0.0f;
@@ -77,8 +78,9 @@ struct ListCol {
   }
   BPT_DEV bool none() const { return g == 0.0f && g1 == 0.0f; }
   BPT_DEV float grad(const GemmArgs& a, float v) const {
-    float r = g * __builtin_amdgcn_exp2f(fmaf(v, a.alpha, -l2));
-    if (a.two) r = fmaf(g1, __builtin_amdgcn_exp2f(fmaf(v, 1.4426950408889634f, -l21)), r);
+    const float d = v - mx;
+    float r = g * __builtin_amdgcn_exp2f(fmaf(d, a.alpha, -l2));
+    if (a.two) r = fmaf(g1, __builtin_amdgcn_exp2f(fmaf(d, 1.4426950408889634f, -l21)), r);
     return r;
   }
 };

@@ -28,7 +28,7 @@ enum Epi {
                    // in C2[m, j]; list_z[m, e] = acc[m, list[m, e]] for the entries e of row m, sorted by column: those of
                    // 64 columns j are (seg[m, j] & 127) from seg[m, j] >> 7 on
   EPI_LIST_T = 9,  // gradient of transposed logits acc (rows m = vocabulary, columns n = tokens) without a list: for m < nvalid
-                   // C = gscale (rowg[n] exp2(alpha acc - rowv[n] log2e) + rowg1[n] exp(acc - rowv1[n])), or without `two`
+                   // C = gscale (rowg[n] exp2(alpha d - rowv[n] log2e) + rowg1[n] exp(d - rowv1[n])), d = acc - rowm[n], or without `two`
                    // gscale (rowg + rowg1)[n] exp2(..); C = 0 for nvalid <= m, and where rowg and rowg1 are 0
 };
 
@@ -86,7 +86,7 @@ struct GemmArgs {
   float* keep = nullptr;        // EPI_LIST: acc too, rows of ldkeep, or null
   int64_t ldkeep = 0, col0 = 0; // col0: of the whole product, this one's first column
   int64_t ldseg = 0, ldlist = 0;
-  const float *rowg = nullptr, *rowv1 = nullptr, *rowg1 = nullptr;
+  const float *rowm = nullptr, *rowg = nullptr, *rowv1 = nullptr, *rowg1 = nullptr;
   float gscale = 1.0f;
   int two = 0;
 };
@@ -312,7 +312,7 @@ struct DistillArgs {
   int32_t* sidx = nullptr;              // lists sorted by index, with probabilities and the student's logits
   float *sq = nullptr, *sz = nullptr;
   int32_t *ypos = nullptr, *count = nullptr;   // the target's entry (-1: none), entries
-  float *lt = nullptr, *l1 = nullptr;   // log-sum-exp of z / tau, of z
+  float *mx = nullptr, *lt = nullptr, *l1 = nullptr;   // max z; logarithms of the sums of exp((z - mx) / tau), of exp(z - mx)
   float *gs = nullptr, *gh = nullptr, *w = nullptr;   // factors of p_tau - q and of p_1 - onehot; weight
   float* tokens = nullptr;              // [2, Tall] kl, ce
   uint16_t* seg = nullptr;              // block's rows of ldseg: per 64 columns, entries before them << 7 | in them; or null

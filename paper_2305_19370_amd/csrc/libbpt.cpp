@@ -2061,7 +2061,7 @@ static DistillArgs distill_args(const bpt_distill_config& c, const void* saved, 
   a.sz = (float*)bp.take(c.T * a.K1 * 4);
   a.ypos = (int32_t*)bp.take(c.T * 4);
   a.count = (int32_t*)bp.take(c.T * 4);
-  for (float** f : {&a.lt, &a.l1, &a.gs, &a.gh, &a.w}) *f = (float*)bp.take(c.T * 4);
+  for (float** f : {&a.mx, &a.lt, &a.l1, &a.gs, &a.gh, &a.w}) *f = (float*)bp.take(c.T * 4);
   *keep = distill_kept(c) > 0 ? (float*)bp.take(distill_kept(c) * c.ldw * 4) : nullptr;
   *total = rup(bp.off, kAlign);
   return a;
@@ -2143,7 +2143,8 @@ bpt_status bpt_distill_fwd(const bpt_distill_config* cfg, const void* h, const v
     RUN("distill.prep", 0, (double)r * (20.0 * a.K1 + 2.0 * ng), distill_prep(a, s));
     GemmArgs g;   // logits of the block: h W, W read as it is stored (B operand K-major)
     g.A = (const char*)h + t0 * d.D * E_; g.lda = d.D;
-    g.B = W; g.ldb = d.ldw; g.trans_b = 1; g.in_order = E == BF16;
+    // logits that are formed again have to be the same: the temperature magnifies what they differ by
+    g.B = W; g.ldb = d.ldw; g.trans_b = 1; g.in_order = E == BF16 || kept < d.T;
     g.C = w.logits; g.ldc = d.ldw; g.M = r; g.N = d.ldw; g.K = d.D;
     if (E == BF16) {
       g.ldc = ng; g.nvalid = d.V; g.alpha = a.scale; g.two = a.two; g.C2 = w.part1;
@@ -2199,8 +2200,8 @@ bpt_status bpt_distill_bwd(const bpt_distill_config* cfg, const void* h, const v
       GemmArgs g;
       g.A = W; g.lda = d.ldw; g.trans_a = 1; g.B = hb; g.ldb = d.D;
       g.C = w.g; g.ldc = d.Rp; g.M = d.ldw; g.N = r; g.Nstore = rp; g.K = d.D;
-      g.in_order = E == BF16; g.alpha = a.scale; g.gscale = dloss; g.two = a.two; g.nvalid = d.V;
-      g.rowv = a.lt + t0; g.rowg = a.gs + t0; g.rowv1 = a.l1 + t0; g.rowg1 = a.gh + t0;
+      g.in_order = 1; g.alpha = a.scale; g.gscale = dloss; g.two = a.two; g.nvalid = d.V;
+      g.rowm = a.mx + t0; g.rowv = a.lt + t0; g.rowg = a.gs + t0; g.rowv1 = a.l1 + t0; g.rowg1 = a.gh + t0;
       RUN("distill.grad_logits", gemm_flops(g), gemm_bytes(g, E_, E_), gemm(E, EPI_LIST_T, E, F32, g, s));
     }
     RUN("distill.listed", 0, (double)r * a.K1 * 16 + (dW ? 2.0 * r * d.D * E_ : 0.0),
