@@ -183,7 +183,11 @@ namespace {
 // (m, l) of two sets: l = sum of 2^((z - m) s)
 BPT_DEV void join(float& m, float& l, float& l1, float m2, float l2, float l12, float s) {
   const float M = fmaxf(m, m2);
-  if (M == -__builtin_inff()) return;
+  if (M == -__builtin_inff()) {                        // sums of nothing, 0, or of NaN, which a maximum does not show
+    l += l2;
+    l1 += l12;
+    return;
+  }
   const float f = __builtin_amdgcn_exp2f((m - M) * s), f2 = __builtin_amdgcn_exp2f((m2 - M) * s);
   const float g = __builtin_amdgcn_exp2f((m - M) * kLog2e), g2 = __builtin_amdgcn_exp2f((m2 - M) * kLog2e);
   l = l * f + l2 * f2;

@@ -130,3 +130,64 @@ def test_logits_formed_again_are_those_that_were_summed(dtype):
             for o in out[1:]:
                 assert all(bool(torch.isfinite(a).all()) for a in o)
                 assert all(torch.equal(a, b) for a, b in zip(o, out[0])), tau
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("V,first,last", [(65, 64, 65), (200, 64, 128), (200, 0, 64), (5000, 4480, 4544), (300, 130, 131), (64, 0, 64)])
+def test_a_nan_among_the_logits_reaches_losses_and_gradients(V, first, last, dtype):
+    """Whole groups of 64 columns of NaN, a last group of one column, one column: in no list and no target, but in every sum."""
+    say(f"case NaN in columns {first}..{last} of {V} {dtype}")
+    T, K = 40, 5
+    t = inputs(T, V, K, 1.0, torch.float32 if dtype == "f32" else torch.bfloat16, 1)
+    t["W"][:, first:last] = math.nan
+    t["index"].clamp_(max=V - 1)
+    keep = [v for v in range(V) if not first <= v < last] or [0]
+    t["index"][:], t["targets"][:] = keep[0], keep[-1]
+    weights = torch.ones(T, device="cuda")
+    weights[::3] = 0.0
+    for hard, tau in ((0.0, 1.0), (0.5, 2.0)):
+        d = bpt.DistillLoss(bpt.make_distill_config(T, 64, V, K, tau=tau, hard=hard, dtype=dtype))
+        loss, tokens, saved = d.forward(t["h"], t["W"], t["values"], t["index"], t["targets"] if hard else None, weights)
+        dh, _ = d.backward(t["h"], t["W"], saved)
+        on = weights != 0
+        assert bool(loss[:2].isnan().all()) and bool(tokens[0, on].isnan().all()) and bool(dh[on].isnan().all())
+        assert bool((tokens[:, ~on] == 0).all())
+        if hard:
+            assert bool(loss[2].isnan()) and bool(tokens[1, on].isnan().all())
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_infinite_values_and_logits(dtype):
+    """A value of +inf has no probability in a softmax: its token's kl and gradient are NaN, those of other tokens as without it. A logit of
+    -inf has probability 0: a gradient of 0 where no list asks for it, an infinite kl where one does."""
+    T, V, K = 12, 200, 5
+    t = inputs(T, V, K, 1.0, torch.float32 if dtype == "f32" else torch.bfloat16, 2)
+    t["index"][:] = torch.arange(10, 10 + K, device="cuda", dtype=torch.int32)
+    d = bpt.DistillLoss(bpt.make_distill_config(T, 64, V, K, tau=1.5, dtype=dtype))
+
+    def run(**kw):
+        a = {**t, **kw}
+        loss, tokens, saved = d.forward(a["h"], a["W"], a["values"], a["index"])
+        return (tokens[0].clone(), *d.backward(a["h"], a["W"], saved))
+
+    ref = run()
+    values = t["values"].clone()
+    values[3, 2] = math.inf
+    kl, dh, _ = run(values=values)
+    rest = torch.arange(T, device="cuda") != 3
+    assert bool(kl[3].isnan()) and bool(dh[3].isnan().all()) and torch.equal(kl[rest], ref[0][rest]) and torch.equal(dh[rest], ref[1][rest])
+    h, W = t["h"].clone(), t["W"].clone()
+    h[:], h[:, 2] = 0.0, 1.0                         # the logits are row 2 of W
+    W[2] = 0.5
+    W[2, 100] = -math.inf
+    loss, tokens, saved = d.forward(h, W, t["values"], t["index"])
+    want = math.log(V - 1)                           # the others have 1 / (V - 1) each
+    q = torch.softmax(t["values"].double().cpu() / 1.5, dim=1)
+    kl = (q * torch.log(q)).sum(dim=1) + want
+    # K terms of some units, a sum of V / 64 + 80 parts, its logarithm
+    check(tokens[0].cpu(), kl, (V / 64 + 120) * U32 * (1 + want) + 20 * K * U32 * (1 + kl.abs()), "kl")
+    _, dW = d.backward(h, W, saved)
+    assert bool((dW[:, 100] == 0).all()) and bool(torch.isfinite(dW).all())
+    t["index"][5, 1] = 100
+    _, tokens, _ = d.forward(h, W, t["values"], t["index"])
+    assert float(tokens[0, 5]) == math.inf and bool(torch.isfinite(tokens[0, :5]).all())
