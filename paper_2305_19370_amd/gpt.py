@@ -214,7 +214,7 @@ class GPT:
         for name in self.nodecay.index:
             if name.endswith(".lam"):
                 sp = -torch.log(torch.rand(s.D, generator=gen) * 0.099 + 0.9) / s.recur_c
-                self.master(name).copy_(torch.log(torch.expm1(sp)))
+                self.master(name).copy_(torch.where(sp > 20.0, sp, torch.log(torch.expm1(sp))))    # softplus(lam) = sp; expm1 ends at 88
                 continue
             self.master(name).fill_(1.0 if name.endswith("_g") else 0.0)
         self.sync_lowp()

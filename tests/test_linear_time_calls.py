@@ -141,3 +141,14 @@ def test_a_forward_takes_inputs_off_16_bytes(monkeypatch, S):
         y, _, _ = bpt.GatedRecurrence().forward(*t, torch.zeros(72))
         assert all(p % 16 == 0 for p in got[-1][:3]) and y.shape == x.shape
         assert [p == a.data_ptr() for p, a in zip(got[-1], t)] == [a is x for a in t]      # aligned ones are not copied
+
+
+# ---------------------------------------------------------------- decays at the start
+@needs_lib
+@pytest.mark.parametrize("c", [1e-4, 1e-3, 0.01, 1.0, 8.0, 1e3])
+def test_decays_of_a_new_gpt(c):
+    """Between 0.9 and 0.999 where the gate is open, whatever their scale is."""
+    from paper_2305_19370_amd.gpt import GPT, GPTShape
+    m = GPT(GPTShape(L=1, B=1, S=8, D=256, H=4, F=64, V=10, Bq=8, Bkv=8, recurrent=True, recur_c=c), device="cpu")
+    a = torch.exp(-c * torch.nn.functional.softplus(m.master("0.lam").double()))
+    assert float(a.min()) >= 0.8999 and float(a.max()) <= 0.99901
