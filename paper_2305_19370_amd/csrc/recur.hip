@@ -641,15 +641,9 @@ hipError_t recur_fwd(Dt t, RecurArgs p, hipStream_t s) {
 namespace {
 template <typename T, bool CHAIN>
 hipError_t launch_bwd(const RecurArgs& p, int nw, hipStream_t s) {
-  auto kern = recur_bwd_kernel<T, kBwdM, CHAIN>;
-  constexpr int most = 2 * kBwdM * 64 * kBwdWaves * 16;
-  static bool attr_set = false;
-  if (!attr_set) {
-    const hipError_t e = hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, most);
-    if (e != hipSuccess) return e;
-    attr_set = true;
-  }
-  hipLaunchKernelGGL(kern, dim3((unsigned)(p.B * p.nct * (CHAIN ? p.nchunks : 1))), dim3((unsigned)(64 * nw)),
+  // with what the kernel declares under 64 KiB of LDS, which a launch may have as it is
+  static_assert(2 * kBwdM * 64 * kBwdWaves * 16 <= 32768, "keep, beside 19 KiB");
+  hipLaunchKernelGGL((recur_bwd_kernel<T, kBwdM, CHAIN>), dim3((unsigned)(p.B * p.nct * (CHAIN ? p.nchunks : 1))), dim3((unsigned)(64 * nw)),
                      2 * kBwdM * 64 * nw * 16, s, p);
   return hipGetLastError();
 }
