@@ -22,13 +22,6 @@ constexpr int kNone = 0x7FFFFFFF;
 typedef __attribute__((__vector_size__(4 * sizeof(int)))) int i32x4;
 constexpr int kPiece = 1024;                         // of a token's row of `seg`
 
-// LDS that a wave's threads wrote becomes readable by its others
-BPT_DEV void lds_sync() {
-  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-  __builtin_amdgcn_wave_barrier();
-  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-}
-
 BPT_DEV float wave_max(float v) {
 #pragma unroll
   for (int o = 32; o >= 1; o >>= 1) v = fmaxf(v, __shfl_xor(v, o, 64));
@@ -90,7 +83,7 @@ __global__ __launch_bounds__(256) void distill_prep_kernel(DistillArgs a) {
     skey[wv][lane + 64 * e] = key[e];
     sq[wv][lane + 64 * e] = q[e];
   }
-  lds_sync();
+  wave_sync();
   // places in the sorted list: smaller indices, and equal ones that come before
   int rank[kPer], valid = 0, n = 0;
 #pragma unroll
@@ -110,7 +103,7 @@ __global__ __launch_bounds__(256) void distill_prep_kernel(DistillArgs a) {
         }
     }
   }
-  lds_sync();
+  wave_sync();
 #pragma unroll
   for (int e = 0; e < kPer; ++e) {
     const bool counts = key[e] != kNone;
@@ -120,7 +113,7 @@ __global__ __launch_bounds__(256) void distill_prep_kernel(DistillArgs a) {
     }
     valid += __popcll(__ballot(counts));
   }
-  lds_sync();
+  wave_sync();
   // the first of equal ones takes the sum of their probabilities
   bool first[kPer];
 #pragma unroll
@@ -133,7 +126,7 @@ __global__ __launch_bounds__(256) void distill_prep_kernel(DistillArgs a) {
       for (int j = at + 1; j < valid && skey[wv][j] == key[e]; ++j) q[e] += sq[wv][j];
     }
   }
-  lds_sync();
+  wave_sync();
 #pragma unroll
   for (int e = 0; e < kPer; ++e) {
     const unsigned long long mask = __ballot(first[e]);
@@ -147,7 +140,7 @@ __global__ __launch_bounds__(256) void distill_prep_kernel(DistillArgs a) {
       if (a.targets && key[e] == y) a.ypos[t] = at;
     }
   }
-  lds_sync();
+  wave_sync();
   if (!real) return;
   if (lane == 0) {
     const float w = a.weights ? a.weights[t] : a.weight;
@@ -163,7 +156,7 @@ __global__ __launch_bounds__(256) void distill_prep_kernel(DistillArgs a) {
     for (int64_t g0 = 0; g0 < a.ng; g0 += kPiece) {
       const int len = (int)std::min<int64_t>(a.ldseg - g0, kPiece);   // a multiple of 8
       for (int c = 8 * lane; c < len; c += 512) *(u32x4*)(piece + c) = u32x4{0, 0, 0, 0};
-      lds_sync();
+      wave_sync();
       for (int e = lane; e < n; e += 64) {
         const int g = skey[wv][e] >> 6;
         if (g < g0 || g >= g0 + len || (e > 0 && skey[wv][e - 1] >> 6 == g)) continue;
@@ -171,10 +164,10 @@ __global__ __launch_bounds__(256) void distill_prep_kernel(DistillArgs a) {
         while (e + many < n && skey[wv][e + many] >> 6 == g) ++many;
         piece[g - g0] = (uint16_t)(e << 7 | many);
       }
-      lds_sync();
+      wave_sync();
       u32x4* out = (u32x4*)(a.seg + (t - a.t0) * a.ldseg + g0);
       for (int c = lane; c < len / 8; c += 64) out[c] = ((const u32x4*)piece)[c];
-      lds_sync();
+      wave_sync();
     }
   }
 }

@@ -140,13 +140,6 @@ BPT_DEV void learn(const Word* runs, const Word* groups, int lane, int wave, int
   if (!all) b = __builtin_nanf("");
 }
 
-// LDS of a wave becomes readable by its other threads
-BPT_DEV void wave_sync() {
-  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-  __builtin_amdgcn_wave_barrier();
-  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-}
-
 // A tensor's rows of one chunk: a base that is the same for all threads and 32-bit offsets (strides are under 2^21 elements)
 template <typename T>
 struct Rows {

@@ -317,7 +317,8 @@ class GPT:
                 raw(max(bpt.distill_workspace_bytes(cfg, back) for back in (False, True))))
 
     def distill_backward(self, tokens: torch.Tensor, dloss: float = 1.0) -> None:
-        """Gradients of dloss * the loss of the last distill_forward into the flat gradient buffers (overwritten)."""
+        """Gradients of dloss * the loss of the last distill_forward into the flat gradient buffers (overwritten). No other pass may
+        come between: each overwrites the activations."""
         if self.distill is None:
             raise ValueError("distill_backward follows distill_forward")
         _, _, saved, ws = self.distill_bufs
