@@ -1277,7 +1277,8 @@ class DistillLoss:
 
     def forward(self, h: torch.Tensor, W: torch.Tensor, values: torch.Tensor, index: torch.Tensor, targets: Optional[torch.Tensor] = None,
                 weights: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor, torch.Tensor]:
-        """(loss, sum w kl, sum w ce) as three floats, kl and ce of each token [2, T], and what backward takes."""
+        """(loss, sum w kl, sum w ce) as three floats, kl and ce of each token [2, T], and what backward takes. For a loss without a
+        backward, a configuration with keep_bytes = -1 stores no logits."""
         c, dev = self.cfg, h.device
         loss = torch.empty(3, dtype=torch.float32, device=dev)
         tokens = torch.empty((2, c.T), dtype=torch.float32, device=dev)
